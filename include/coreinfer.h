@@ -378,6 +378,142 @@ coreinfer_status coreinfer_prefill_activations(const void* x, int32_t T, coreinf
                                                void* workspace, size_t workspace_bytes,
                                                void* cuda_stream);
 
+/* ------------------------------------------------------------------ (7) --
+ * Four-bit storage of weights and of the key/value cache: what a decode step streams beside the
+ * core-sparse FFN (the projections around attention, and attention itself).  The paper decodes
+ * through models whose attention is left as it is; these calls have no counterpart in it.
+ *
+ * Format.  A group of `group` (32, 64 or 128) consecutive values x of a row is held as codes
+ * c in 0..15 and one fp16 pair (s, o):   x^ = s * c + o   with
+ *   o = fp16(min x),  s = fp16((max x - min x) / 15),  c = clamp(round((x - o) / s), 0, 15)
+ * (fp32 arithmetic, ties to even; c = 0 where s is 0; o and s are clamped to the finite fp16
+ * range; a group that holds a NaN is stored as NaN).  A row piece of 32 H values takes 16 H bytes
+ * in units of two bytes: unit i * H + h (i = 0..7, h = 0..H-1) holds values 32 h + 4 i .. + 3,
+ * the first in the lowest four bits.
+ *   Weights [N, K]: padded to 16 rows and 128 columns (zeros), codes [N/16][K/128][16][64 bytes]
+ *   (row pieces of 128 values, H = 4), pairs [N/16][K/group][16][2] fp16 (s, o).  The last group of a
+ *   row ends at K: its pair is that of the values it has.
+ *   Cache: see (8), H = head_dim / 32. */
+typedef enum { COREINFER_ACT_NONE = 0, COREINFER_ACT_RELU = 1, COREINFER_ACT_SILU = 2 } coreinfer_act;
+
+typedef struct {
+    const void* codes;      /* device, coreinfer_w4_codes_bytes(N, K) */
+    const void* pairs;      /* device, coreinfer_w4_pairs_bytes(N, K, group) */
+    int32_t N;              /* output rows */
+    int32_t K;              /* input columns */
+    int32_t group;
+    int32_t reserved;
+} coreinfer_w4_matrix;
+
+/* Bytes of the two buffers of a weight matrix; 0 for sizes out of range. */
+size_t coreinfer_w4_codes_bytes(int32_t N, int32_t K);
+size_t coreinfer_w4_pairs_bytes(int32_t N, int32_t K, int32_t group);
+
+/* Quantises and lays out a weight matrix once (at load time).
+ *   w       device, element (n, k) at n * stride_n + k * stride_k in `dtype` (element aligned): with
+ *           strides (1, d_model) the transposed compacted down projection [K, d_model] serves
+ *           as the matrix [d_model, K].
+ *   codes, pairs  device out, 16-byte aligned, sizes as above; every byte is written.
+ * Errors: INVALID_ARG, UNSUPPORTED (dtype, group), CUDA. */
+coreinfer_status coreinfer_w4_quantize(const void* w, coreinfer_dtype dtype, int32_t N, int32_t K,
+                                       int64_t stride_n, int64_t stride_k, int32_t group,
+                                       void* codes, void* pairs, void* cuda_stream);
+
+/* Matrix-vector products with a 4-bit weight matrix:
+ *   y[b, n] = act( sum_k x[b, k] * w^[n, k] + bias[n] ) * mul[b, n]
+ * for 1 <= batch <= COREINFER_MAX_BATCH rows of x; every weight byte is read once for all rows.
+ * Sums are fp32 in an order that does not change from run to run; y is rounded once.
+ *   x      device [batch, K] in `dtype` with row stride ld_x (element aligned)
+ *   bias   device [N] in `dtype` or NULL;   mul  device [batch, N] in y_dtype with row stride ld_mul, or NULL
+ *   y      device out [batch, N] in y_dtype (fp32 or `dtype`) with row stride ld_y; may be `mul`, not x
+ * A gated FFN is two calls: g = act(W_gate x), then h = (W_up x) * g with mul = g.
+ * An infinity or NaN in a row of x makes that row of y NaN or infinite as the formula says for at
+ * least the outputs it reaches; other rows are not touched by it.
+ * Errors: INVALID_ARG, UNSUPPORTED (dtype, group, batch), CUDA. */
+coreinfer_status coreinfer_w4_matvec(const coreinfer_w4_matrix* w, const void* x, int32_t batch, int64_t ld_x,
+                                     coreinfer_dtype dtype, coreinfer_act act,
+                                     const void* bias, const void* mul, int64_t ld_mul,
+                                     void* y, coreinfer_dtype y_dtype, int64_t ld_y, void* cuda_stream);
+
+/* ------------------------------------------------------------------ (8) --
+ * A key/value cache held in four bits, attention over it, and eviction from it.
+ *
+ * Buffers (device, the caller's, codes and pairs 16-byte aligned), in slots of one token and head:
+ *   k_codes, v_codes  [batch][kv_heads][capacity][head_dim / 2] bytes
+ *   k_pairs, v_pairs  [batch][kv_heads][capacity][head_dim / group][2] fp16
+ *   weight            [batch][kv_heads][capacity] fp32: attention weight accumulated per slot
+ *   position          [batch][kv_heads][capacity] int32: which token of the sequence a slot holds
+ *                     (weight and position both NULL for a cache that is never evicted from)
+ *   state             [batch][4] int32: slots in use, tokens ever appended, tokens refused because
+ *                     they did not fit, scratch.  All zero = empty; zero it to start new sequences.
+ * head_dim is 64, 128 or 256, group 32, 64 or 128 and at most head_dim, capacity a multiple of 16,
+ * batch at most COREINFER_KV4_MAX_BATCH.  Slots beyond the first `state[b][0]` may hold anything. */
+#define COREINFER_KV4_MAX_BATCH 1024
+#define COREINFER_KV4_MAX_QUERIES 16
+
+typedef struct {
+    void* k_codes;
+    void* k_pairs;
+    void* v_codes;
+    void* v_pairs;
+    int32_t* state;
+    float* weight;
+    int32_t* position;
+    int32_t batch;
+    int32_t kv_heads;
+    int32_t capacity;
+    int32_t head_dim;
+    int32_t group;
+    int32_t reserved;
+} coreinfer_kv4_cache;
+
+/* Appends T tokens to every sequence: quantises their keys and values into the next T slots, sets
+ * those slots' weight to 0 and their position to the running token number, and advances the state.
+ * A sequence whose free slots do not hold all T is left as it is and counts T refused tokens.
+ *   k, v     device, token t of sequence b at (b * T + t) * ld_token, its heads [kv_heads][head_dim]
+ *            contiguous; 16-byte aligned, ld_token * element size a multiple of 16
+ *   k_stored, v_stored  device out [batch][T][kv_heads][head_dim] in `dtype` (16-byte aligned), the values
+ *            as the cache now holds them (x^ rounded to dtype), or both NULL.  Written for refused
+ *            tokens too.
+ * Errors: INVALID_ARG, UNSUPPORTED (head_dim, group, dtype, batch), CUDA. */
+coreinfer_status coreinfer_kv4_append(const coreinfer_kv4_cache* cache, const void* k, const void* v,
+                                      coreinfer_dtype dtype, int32_t T, int64_t ld_token,
+                                      void* k_stored, void* v_stored, void* cuda_stream);
+
+/* Attention of the T newest tokens of every sequence (1 <= T <= COREINFER_KV4_MAX_QUERIES; append
+ * first) over the cache:
+ *   p[t, head, n] = softmax over n of  scale * q[t, head] . k^[n]      out[t, head] = sum_n p v^[n]
+ * where token t sees the slots n < state[b][0] - (T - 1 - t) and `q_heads / kv_heads` consecutive query heads
+ * share a key head.  A token that sees no slot (an empty sequence) gets zeros.  With `accumulate`,
+ * weight[b, kv head, n] += sum of p over the tokens and heads that read the slot.
+ * Sums, maxima and accumulated weights are fp32 in a fixed order (the same call gives the same bits).
+ *   q        device, token t of sequence b at (b * T + t) * ld_q, [q_heads][head_dim] contiguous, in
+ *            `dtype`; 16-byte aligned, ld_q * element size a multiple of 16.  out likewise with ld_out.
+ *   workspace  device, 16-byte aligned, at least coreinfer_kv4_attention_workspace_bytes() (0 on bad sizes)
+ * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, CUDA. */
+size_t coreinfer_kv4_attention_workspace_bytes(const coreinfer_kv4_cache* cache, int32_t q_heads, int32_t T);
+
+coreinfer_status coreinfer_kv4_attention(const coreinfer_kv4_cache* cache, const void* q, coreinfer_dtype dtype,
+                                         int32_t q_heads, int32_t T, int64_t ld_q, float scale,
+                                         void* out, int64_t ld_out, int32_t accumulate,
+                                         void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Evicts from every sequence and head down to min(state[b][0], budget) slots.  Kept are the tokens with
+ * position >= state[b][1] - recent, those with position < first, and of the others the ones with the
+ * largest weight (equal weights: the lower slot; a NaN weight goes first).  recent + first <= budget.
+ *   dst == src (the same buffers): in place.  Kept slots below the new length stay where they are; the
+ *     kept ones above it move, in ascending order, into the free ones below it.
+ *   dst another cache of the same batch, kv_heads, head_dim and group, with capacity >= min(budget,
+ *     src capacity): the kept slots are copied in ascending slot order; src is not changed; slots of
+ *     dst beyond the new length are not written.
+ *   state[b][0] of dst becomes the new length, state[b][1] is taken over.
+ * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, CUDA. */
+size_t coreinfer_kv4_evict_workspace_bytes(const coreinfer_kv4_cache* src);
+
+coreinfer_status coreinfer_kv4_evict(const coreinfer_kv4_cache* src, const coreinfer_kv4_cache* dst,
+                                     int32_t budget, int32_t recent, int32_t first,
+                                     void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

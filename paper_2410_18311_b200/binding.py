@@ -16,7 +16,9 @@ from . import _build
 
 F32, BF16, F16 = 0, 1, 2
 FFN_RELU, FFN_RELU_GATED, FFN_SILU_GATED = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
 MAX_BATCH, MAX_LAYERS = 8, 128
+KV4_MAX_BATCH, KV4_MAX_QUERIES = 1024, 16
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT = range(6)
 
 # every symbol include/coreinfer.h declares
@@ -34,6 +36,9 @@ SYMBOLS = (
     "coreinfer_counts_add", "coreinfer_counts_add_set", "coreinfer_top_by_count", "coreinfer_core_similarity",
     "coreinfer_nearest_centroid_workspace_bytes", "coreinfer_nearest_centroid",
     "coreinfer_update_core_set_workspace_bytes", "coreinfer_update_core_set",
+    "coreinfer_w4_codes_bytes", "coreinfer_w4_pairs_bytes", "coreinfer_w4_quantize", "coreinfer_w4_matvec",
+    "coreinfer_kv4_append", "coreinfer_kv4_attention_workspace_bytes", "coreinfer_kv4_attention",
+    "coreinfer_kv4_evict_workspace_bytes", "coreinfer_kv4_evict",
 )
 STAMP_SLOTS = 16
 
@@ -49,6 +54,21 @@ class Layer(ctypes.Structure):
     _fields_ = [("w_up_c", ctypes.c_void_p), ("w_gate_c", ctypes.c_void_p),
                 ("w_downT_c", ctypes.c_void_p), ("b_up_c", ctypes.c_void_p),
                 ("b_down", ctypes.c_void_p), ("K", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class W4Matrix(ctypes.Structure):
+    """coreinfer_w4_matrix"""
+    _fields_ = [("codes", ctypes.c_void_p), ("pairs", ctypes.c_void_p), ("N", ctypes.c_int32), ("K", ctypes.c_int32),
+                ("group", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class KV4Cache(ctypes.Structure):
+    """coreinfer_kv4_cache"""
+    _fields_ = [("k_codes", ctypes.c_void_p), ("k_pairs", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+                ("v_pairs", ctypes.c_void_p), ("state", ctypes.c_void_p), ("weight", ctypes.c_void_p),
+                ("position", ctypes.c_void_p), ("batch", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("capacity", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("group", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
 
 
 _lib = None
@@ -130,6 +150,25 @@ def load() -> ctypes.CDLL:
     lib.coreinfer_update_core_set.restype = ctypes.c_int
     lib.coreinfer_update_core_set.argtypes = [vp, vp, vp, vp, ctypes.c_int, i32, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp,
                                               sz, vp]
+    pw, pc, f32 = ctypes.POINTER(W4Matrix), ctypes.POINTER(KV4Cache), ctypes.c_float
+    lib.coreinfer_w4_codes_bytes.restype = sz
+    lib.coreinfer_w4_codes_bytes.argtypes = [i32, i32]
+    lib.coreinfer_w4_pairs_bytes.restype = sz
+    lib.coreinfer_w4_pairs_bytes.argtypes = [i32, i32, i32]
+    lib.coreinfer_w4_quantize.restype = ctypes.c_int
+    lib.coreinfer_w4_quantize.argtypes = [vp, ctypes.c_int, i32, i32, i64, i64, i32, vp, vp, vp]
+    lib.coreinfer_w4_matvec.restype = ctypes.c_int
+    lib.coreinfer_w4_matvec.argtypes = [pw, vp, i32, i64, ctypes.c_int, ctypes.c_int, vp, vp, i64, vp, ctypes.c_int, i64, vp]
+    lib.coreinfer_kv4_append.restype = ctypes.c_int
+    lib.coreinfer_kv4_append.argtypes = [pc, vp, vp, ctypes.c_int, i32, i64, vp, vp, vp]
+    lib.coreinfer_kv4_attention_workspace_bytes.restype = sz
+    lib.coreinfer_kv4_attention_workspace_bytes.argtypes = [pc, i32, i32]
+    lib.coreinfer_kv4_attention.restype = ctypes.c_int
+    lib.coreinfer_kv4_attention.argtypes = [pc, vp, ctypes.c_int, i32, i32, i64, f32, vp, i64, i32, vp, sz, vp]
+    lib.coreinfer_kv4_evict_workspace_bytes.restype = sz
+    lib.coreinfer_kv4_evict_workspace_bytes.argtypes = [pc]
+    lib.coreinfer_kv4_evict.restype = ctypes.c_int
+    lib.coreinfer_kv4_evict.argtypes = [pc, pc, i32, i32, i32, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -321,3 +360,114 @@ def coreinfer_update_core_set(w_up, w_gate, w_down, b_up, slot_neuron, core_idx_
                                             _p(slot_neuron), _p(core_idx_new), slot_neuron.numel(), _p(w_up_c),
                                             _p(w_gate_c), _p(w_downT_c), _p(b_up_c), _p(n_changed_out), _p(workspace),
                                             workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def coreinfer_w4_codes_bytes(N: int, K: int) -> int:
+    return int(load().coreinfer_w4_codes_bytes(N, K))
+
+
+def coreinfer_w4_pairs_bytes(N: int, K: int, group: int) -> int:
+    return int(load().coreinfer_w4_pairs_bytes(N, K, group))
+
+
+def make_w4_matrix(codes, pairs, N: int, K: int, group: int) -> W4Matrix:
+    """coreinfer_w4_matrix over the caller's two CUDA buffers (which must outlive it)."""
+    if (codes.numel() * codes.element_size() < coreinfer_w4_codes_bytes(N, K)
+            or pairs.numel() * pairs.element_size() < coreinfer_w4_pairs_bytes(N, K, group)):
+        raise CoreInferError(ERR_INVALID_ARG, "codes or pairs smaller than a %d x %d matrix takes" % (N, K))
+    if not (codes.is_contiguous() and pairs.is_contiguous()):
+        raise CoreInferError(ERR_INVALID_ARG, "codes and pairs must be contiguous")
+    return W4Matrix(codes.data_ptr(), pairs.data_ptr(), N, K, group, 0)
+
+
+def coreinfer_w4_quantize(w, group, codes, pairs, stream=None):
+    """w [N, K] fp32, bf16 or fp16 with any strides (a transposed view is fine) -> codes, pairs."""
+    N, K = w.shape
+    _check(load().coreinfer_w4_quantize(_p(w), dtype_code(w), N, K, w.stride(0), w.stride(1), int(group), _p(codes), _p(pairs),
+                                        _stream(stream)))
+
+
+def _row_stride(t):
+    """Elements between the rows of a [rows, n] tensor whose rows are contiguous."""
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise CoreInferError(ERR_INVALID_ARG, "rows must be contiguous (strides %s)" % (tuple(t.stride()),))
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def coreinfer_w4_matvec(w4, x, act, bias, mul, y, stream=None):
+    """y [batch, N] = act(x [batch, K] W^T + bias) * mul, batch 1..8; w4 from make_w4_matrix()."""
+    if tuple(y.shape) != (x.shape[0], w4.N) or x.shape[1] != w4.K or (mul is not None and (mul.shape != y.shape or mul.dtype != y.dtype)) \
+            or (bias is not None and (bias.shape != (w4.N,) or bias.dtype != x.dtype or not bias.is_contiguous())):
+        raise CoreInferError(ERR_INVALID_ARG, "x %s, y %s, bias or mul do not fit the %d x %d matrix"
+                             % (tuple(x.shape), tuple(y.shape), w4.N, w4.K))
+    _check(load().coreinfer_w4_matvec(w4, x.data_ptr(), x.shape[0], _row_stride(x), dtype_code(x), act,
+                                      None if bias is None else bias.data_ptr(), None if mul is None else mul.data_ptr(),
+                                      0 if mul is None else _row_stride(mul), y.data_ptr(), dtype_code(y), _row_stride(y),
+                                      _stream(stream)))
+
+
+def make_kv4_cache(k_codes, k_pairs, v_codes, v_pairs, state, weight=None, position=None) -> KV4Cache:
+    """coreinfer_kv4_cache over the caller's CUDA buffers (which must outlive it): codes
+    [batch, kv_heads, capacity, head_dim / 2] uint8, pairs [.., head_dim / group, 2] fp16, state [batch, 4]
+    int32, weight fp32 and position int32 [batch, kv_heads, capacity] (both or neither)."""
+    B, H, n, half = k_codes.shape
+    groups = k_pairs.shape[3]
+    want = ((k_codes, torch.uint8, (B, H, n, half)), (v_codes, torch.uint8, (B, H, n, half)),
+            (k_pairs, torch.float16, (B, H, n, groups, 2)), (v_pairs, torch.float16, (B, H, n, groups, 2)),
+            (state, torch.int32, (B, 4)), (weight, torch.float32, (B, H, n)), (position, torch.int32, (B, H, n)))
+    for t, dtype, shape in want:
+        if t is not None and (t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous()):
+            raise CoreInferError(ERR_INVALID_ARG, "a cache buffer of %s %s was expected contiguous as %s %s"
+                                 % (t.dtype, tuple(t.shape), dtype, shape))
+    return KV4Cache(k_codes.data_ptr(), k_pairs.data_ptr(), v_codes.data_ptr(), v_pairs.data_ptr(), state.data_ptr(),
+                    None if weight is None else weight.data_ptr(), None if position is None else position.data_ptr(),
+                    B, H, n, 2 * half, 2 * half // groups, 0)
+
+
+def _token_stride(t, heads, head_dim):
+    """Elements between the tokens of a [batch, T, heads, head_dim] tensor (a slice of a wider projection is fine)."""
+    B, T, h, d = t.shape
+    ld = t.stride(1) if T > 1 else (t.stride(0) if B > 1 else h * d)
+    if (h, d) != (heads, head_dim) or t.stride(3) != 1 or (h > 1 and t.stride(2) != d) or (B > 1 and t.stride(0) != T * ld):
+        raise CoreInferError(ERR_INVALID_ARG, "a [batch, T, %d, %d] tensor with evenly spaced tokens was expected: shape %s, "
+                             "strides %s" % (heads, head_dim, tuple(t.shape), tuple(t.stride())))
+    return ld
+
+
+def coreinfer_kv4_append(cache, k, v, k_stored=None, v_stored=None, stream=None):
+    """k, v [batch, T, kv_heads, head_dim] into the cache; k_stored / v_stored: the values as stored, or None."""
+    ld = _token_stride(k, cache.kv_heads, cache.head_dim)
+    if v.shape != k.shape or v.dtype != k.dtype or _token_stride(v, cache.kv_heads, cache.head_dim) != ld or k.shape[0] != cache.batch:
+        raise CoreInferError(ERR_INVALID_ARG, "k %s and v %s do not match each other or the cache" % (tuple(k.shape), tuple(v.shape)))
+    for t in (k_stored, v_stored):
+        if t is not None and (t.shape != k.shape or t.dtype != k.dtype or not t.is_contiguous()):
+            raise CoreInferError(ERR_INVALID_ARG, "k_stored and v_stored must be contiguous and shaped as k")
+    _check(load().coreinfer_kv4_append(cache, k.data_ptr(), v.data_ptr(), dtype_code(k), k.shape[1], ld,
+                                       None if k_stored is None else k_stored.data_ptr(),
+                                       None if v_stored is None else v_stored.data_ptr(), _stream(stream)))
+
+
+def coreinfer_kv4_attention_workspace_bytes(cache, q_heads: int, T: int) -> int:
+    return int(load().coreinfer_kv4_attention_workspace_bytes(cache, q_heads, T))
+
+
+def coreinfer_kv4_attention(cache, q, scale, out, accumulate, workspace, stream=None):
+    """q [batch, T, q_heads, head_dim] -> out of the same shape and type; accumulate: add every slot's
+    attention weight to the cache's weights."""
+    heads = q.shape[2]
+    if out.shape != q.shape or out.dtype != q.dtype or q.shape[0] != cache.batch:
+        raise CoreInferError(ERR_INVALID_ARG, "q %s and out %s do not match each other or the cache" % (tuple(q.shape), tuple(out.shape)))
+    _check(load().coreinfer_kv4_attention(cache, q.data_ptr(), dtype_code(q), heads, q.shape[1],
+                                          _token_stride(q, heads, cache.head_dim), scale, out.data_ptr(),
+                                          _token_stride(out, heads, cache.head_dim), 1 if accumulate else 0, workspace.data_ptr(),
+                                          workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def coreinfer_kv4_evict_workspace_bytes(cache) -> int:
+    return int(load().coreinfer_kv4_evict_workspace_bytes(cache))
+
+
+def coreinfer_kv4_evict(src, dst, budget, recent, first, workspace, stream=None):
+    """Keep `budget` slots per head (the first and recent tokens, then the heaviest); dst is src for in place."""
+    _check(load().coreinfer_kv4_evict(src, dst, budget, recent, first, workspace.data_ptr(),
+                                      workspace.numel() * workspace.element_size(), _stream(stream)))

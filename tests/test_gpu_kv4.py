@@ -1,0 +1,308 @@
+"""The 4-bit key/value cache: append and eviction bit-exact against plain loops, attention against the
+same sums in 64 bits within bounds that follow from the arithmetic."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2410_18311_b200 as ci
+from helpers import require_gpu
+from quant4_ref import EPS16, EPS32, OUT_EPS, CacheRef, values_np
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def handle(d):
+    return ci.make_kv4_cache(d["k_codes"], d["k_pairs"], d["v_codes"], d["v_pairs"], d["state"], d["weight"], d["position"])
+
+
+def scratch(n, fill=0xFF):
+    return torch.full((n,), fill, dtype=torch.uint8, device="cuda")
+
+
+# -------------------------------------------------------------------------------- append --
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("D,group", [(64, 32), (64, 64), (128, 32), (128, 64), (128, 128), (256, 32), (256, 128)])
+def test_append(D, group, dtype):
+    """Ragged sequences, several calls, one sequence that has no room left; k and v slices of one projection."""
+    require_gpu()
+    B, H, cap = 3, 2, 48
+    rng = np.random.default_rng(D + group)
+    ref = CacheRef(B, H, cap, D, group, rng)
+    ref.set_lengths([0, 17, 40])
+    ref.seen = [0, 30, 40]
+    d = ref.to_cuda()
+    h = handle(d)
+    for T in (1, 7, 2):
+        fused = torch.from_numpy(rng.standard_normal((B, T, 3 * H * D)).astype(np.float32)).cuda().to(DT[dtype])
+        k, v = fused[..., H * D:2 * H * D].unflatten(-1, (H, D)), fused[..., 2 * H * D:].unflatten(-1, (H, D))
+        ks, vs = torch.full((B, T, H, D), float("nan"), dtype=DT[dtype], device="cuda"), torch.zeros(B, T, H, D, dtype=DT[dtype], device="cuda")
+        ci.coreinfer_kv4_append(h, k, v, ks, vs)
+        stored = ref.append(values_np(k), values_np(v))
+        for got, want in zip((ks, vs), stored):
+            want = torch.from_numpy(want.astype(np.float32)).to(DT[dtype])       # s c is exact in fp32, one rounding each
+            assert torch.equal(got.cpu(), want)
+    assert ref.refused == [0, 0, 2]
+    ref.assert_equal(d)
+
+
+def test_append_unusual_values_and_without_weights():
+    require_gpu()
+    B, H, cap, D, group, T = 1, 1, 16, 64, 32, 5
+    ref = CacheRef(B, H, cap, D, group, np.random.default_rng(0))
+    d = ref.to_cuda()
+    bare = ci.make_kv4_cache(d["k_codes"], d["k_pairs"], d["v_codes"], d["v_pairs"], d["state"])
+    k = np.random.default_rng(1).standard_normal((B, T, H, D)).astype(np.float32)
+    v = k.copy()
+    k[0, 0, 0, :32], k[0, 1, 0, 3], k[0, 2, 0, 40], k[0, 3, 0, 0] = 0.5, np.inf, -np.inf, 1e30
+    weight, position = ref.weight.copy(), ref.position.copy()
+    ci.coreinfer_kv4_append(bare, torch.from_numpy(k).cuda(), torch.from_numpy(v).cuda())
+    ref.append(k, v)
+    ref.weight, ref.position = weight, position                    # a cache without them: nothing is written there
+    ref.assert_equal(d)
+    k[0, 4, 0, 9] = np.nan
+    ks, vs = torch.empty(B, T, H, D, device="cuda"), torch.empty(B, T, H, D, device="cuda")
+    ci.coreinfer_kv4_append(bare, torch.from_numpy(k).cuda(), torch.from_numpy(v).cuda(), ks, vs)
+    bad = np.isnan(ks.cpu().numpy())
+    assert bad[0, 4, 0, :32].all() and bad.sum() == 32 and not torch.isnan(vs).any()
+
+
+def test_append_full_prompt():
+    """A prompt that fills the cache exactly, many thread blocks per sequence."""
+    require_gpu()
+    B, H, cap, D, group = 2, 8, 304, 128, 64
+    rng = np.random.default_rng(2)
+    ref = CacheRef(B, H, cap, D, group, rng)
+    d = ref.to_cuda()
+    k, v = (rng.standard_normal((B, cap, H, D)).astype(np.float32) for _ in "kv")
+    ci.coreinfer_kv4_append(handle(d), torch.from_numpy(k).cuda(), torch.from_numpy(v).cuda())
+    ref.append(k, v)
+    ref.assert_equal(d)
+    assert ref.length == [cap, cap]
+
+
+# ----------------------------------------------------------------------------- attention --
+
+def attend(ref, d, q, accumulate=True, scale=None, out=None, stream=None):
+    h = handle(d)
+    out = torch.full(q.shape, float("nan"), dtype=q.dtype, device="cuda") if out is None else out
+    ws = scratch(ci.coreinfer_kv4_attention_workspace_bytes(h, q.shape[2], q.shape[1]))
+    ci.coreinfer_kv4_attention(h, q, ref.D ** -0.5 if scale is None else scale, out, accumulate, ws, stream=stream)
+    return out
+
+
+def check_attention(ref, d, q, out, scale, before):
+    """Bounds.  A logit is a sum of D products and their groups in fp32: it is off by at most (D / 8 + 32) spacings of
+    its absolute terms (fp32 q enters with 22 bits: 4 spacings more), and by 2^-20 in its exponential.  An error e of a
+    logit moves its p and the sum by factors e^(+-e) each.  The weights p s enter the second product with at least
+    11 bits for bf16 and 22 for the others; its sums over n slots add n / 8 + 32 spacings at most; then one rounding."""
+    o, add, mass, logit_mass = ref.attention(values_np(q).astype(np.float64), scale)
+    n = max(ref.length)
+    e = 2 * ((ref.D / 8 + 36) * EPS32 * logit_mass + 2.0 ** -20)[..., None]
+    rel = e + (EPS16 if q.dtype == torch.bfloat16 else 2.0 ** -21) + (n / 8 + 32) * EPS32
+    tol = rel * mass + (OUT_EPS[q.dtype] * np.abs(o)) + 1e-30
+    err = np.abs(values_np(out) - o)
+    assert (err <= tol).all(), "outputs: worst %.3g of the bound" % (err / tol).max()
+    if before is not None:
+        got = values_np(d["weight"]).astype(np.float64)
+        worst = float(e.max()) + (q.shape[1] * q.shape[2] + 4) * EPS32
+        tol = worst * add + 2.0 ** -23 * np.abs(before) + 2.0 ** -126
+        err = np.abs(got - (before + add))
+        live = np.arange(ref.cap) < np.array(ref.length)[:, None, None]
+        assert (err <= tol)[np.broadcast_to(live, err.shape)].all(), "weights: worst %.3g of the bound" % (err / tol).max()
+        np.testing.assert_array_equal(got[~np.broadcast_to(live, got.shape)], before[~np.broadcast_to(live, before.shape)])
+
+
+ATTN = [
+    # B, H, share, T, D, group, lengths, dtype
+    (1, 1, 1, 1, 64, 32, [1], "f32"), (1, 2, 1, 1, 64, 64, [16], "bf16"), (2, 12, 1, 1, 64, 32, [77, 3], "f32"),
+    (3, 2, 4, 1, 128, 64, [0, 200, 129], "bf16"), (2, 2, 8, 1, 128, 128, [1000, 17], "f16"), (1, 1, 8, 1, 128, 32, [640], "f32"),
+    (2, 3, 5, 3, 128, 32, [300, 2], "bf16"), (2, 1, 12, 2, 64, 64, [65, 128], "f16"), (1, 2, 7, 7, 128, 64, [513], "bf16"),
+    (1, 1, 40, 16, 64, 32, [90], "f32"), (2, 2, 1, 16, 128, 128, [15, 100], "f16"), (1, 1, 71, 1, 64, 64, [257], "bf16"),
+    (2, 2, 4, 1, 256, 32, [150, 31], "bf16"), (1, 2, 2, 3, 256, 128, [400], "f32"), (1, 1, 16, 5, 256, 64, [97], "f16"),
+    (1, 4, 2, 1, 128, 64, [3000], "bf16"), (40, 2, 1, 1, 64, 32, [5 * i for i in range(40)], "bf16"),
+    (2, 32, 1, 1, 128, 64, [1100, 700], "bf16"),
+]
+
+
+@pytest.mark.parametrize("B,H,share,T,D,group,lengths,dtype", ATTN)
+def test_attention(B, H, share, T, D, group, lengths, dtype):
+    require_gpu()
+    rng = np.random.default_rng(sum(lengths) + share)
+    cap = max(16, -(-max(lengths) // 16) * 16 + 16 * (share % 2))
+    ref = CacheRef(B, H, cap, D, group, rng)
+    ref.set_lengths(lengths)
+    d = ref.to_cuda()
+    # what lies beyond the slots in use must not be looked at: all of it NaN
+    for b, n in enumerate(lengths):
+        d["k_pairs"][b, :, n:] = float("nan")
+        d["v_pairs"][b, :, n:] = float("nan")
+    before = ref.weight.copy()
+    q = torch.from_numpy(rng.standard_normal((B, T, H * share, D)).astype(np.float32)).cuda().to(DT[dtype])
+    out = attend(ref, d, q)
+    check_attention(ref, d, q, out, D ** -0.5, before)
+    # without accumulation: the same outputs, the weights stay
+    w = d["weight"].clone()
+    again = attend(ref, d, q, accumulate=False)
+    assert torch.equal(out, again) and torch.equal(d["weight"], w)
+
+
+def test_attention_strides_stream_and_bits():
+    """q a slice of a fused projection, out a slice of a wider tensor, a side stream; the same call gives the same bits."""
+    require_gpu()
+    B, H, share, T, D = 2, 4, 2, 2, 128
+    rng = np.random.default_rng(4)
+    ref = CacheRef(B, H, 256, D, 64, rng)
+    ref.set_lengths([200, 91])
+    fused = torch.from_numpy(rng.standard_normal((B, T, (share + 2) * H * D)).astype(np.float32)).cuda().bfloat16()
+    q = fused[..., : share * H * D].unflatten(-1, (share * H, D))
+    wide = torch.zeros(B, T, 3 * share * H * D, dtype=torch.bfloat16, device="cuda")
+    out = wide[..., share * H * D:2 * share * H * D].unflatten(-1, (share * H, D))
+    runs = []
+    for k in range(2):
+        d = ref.to_cuda()
+        torch.cuda.synchronize()
+        s = torch.cuda.Stream()
+        attend(ref, d, q, out=out, stream=s)
+        s.synchronize()
+        check_attention(ref, d, q, out, D ** -0.5, ref.weight)
+        assert not wide[..., : share * H * D].any() and not wide[..., 2 * share * H * D:].any()
+        runs.append((out.clone(), d["weight"].clone()))
+    assert torch.equal(runs[0][0], runs[1][0]) and torch.equal(runs[0][1], runs[1][1])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_attention_sharp_and_scaled(dtype):
+    """Logits in the hundreds (one slot takes all, its place differs per head), values from 1e-4 to 1e4 in one cache,
+    queries far from 1: nothing overflows on the way."""
+    require_gpu()
+    B, H, share, T, D, group = 2, 2, 2, 1, 128, 64
+    rng = np.random.default_rng(6)
+    ref = CacheRef(B, H, 512, D, group, rng)
+    ref.set_lengths([500, 333])
+    scales = 10.0 ** rng.uniform(-4, 4, size=(B, H, 512, 1))
+    ref.s[1], ref.o[1] = (ref.s[1] * scales).astype(np.float16), (ref.o[1] * scales).astype(np.float16)
+    for factor in (40.0, 1e-4, 1e4 if dtype == "f16" else 1e8):
+        q = torch.from_numpy((factor * rng.standard_normal((B, T, H * share, D))).astype(np.float32)).cuda().to(DT[dtype])
+        scale = D ** -0.5 * (1.0 if factor < 1e3 else 100.0 / factor)
+        d = ref.to_cuda()
+        out = attend(ref, d, q, scale=scale)
+        check_attention(ref, d, q, out, scale, ref.weight)
+
+
+def test_attention_nan_in_a_value_reaches_its_heads_only():
+    require_gpu()
+    ref = CacheRef(2, 2, 64, 64, 32, np.random.default_rng(9))
+    ref.set_lengths([50, 50])
+    d = ref.to_cuda()
+    d["v_pairs"][0, 1, 10, 0] = float("nan")
+    q = torch.randn(2, 1, 4, 64, device="cuda", dtype=torch.bfloat16)
+    out = attend(ref, d, q).float().cpu()
+    assert torch.isnan(out[0, 0, 2:, :32]).all()
+    assert torch.isfinite(out[0, 0, :2]).all() and torch.isfinite(out[0, 0, 2:, 32:]).all() and torch.isfinite(out[1]).all()
+
+
+def test_attention_equal_keys_give_the_mean():
+    """All keys alike: every p is 1 / n, so the weights are equal and out is the mean of the values."""
+    require_gpu()
+    ref = CacheRef(1, 1, 112, 64, 64, np.random.default_rng(11))
+    ref.set_lengths([100])
+    ref.codes[0][:], ref.s[0][:], ref.o[0][:] = 7, 0.5, -2.0
+    ref.weight[:] = 0
+    d = ref.to_cuda()
+    q = torch.ones(1, 1, 1, 64, device="cuda")
+    out = attend(ref, d, q)
+    np.testing.assert_allclose(out.cpu().numpy()[0, 0, 0], ref.values(1)[0, 0, :100].mean(0), atol=2e-6)
+    np.testing.assert_allclose(d["weight"].cpu().numpy()[0, 0, :100], 0.01, rtol=1e-6)
+
+
+# ------------------------------------------------------------------------------- evict --
+
+def evict(src, dst, budget, recent, first):
+    ws = scratch(ci.coreinfer_kv4_evict_workspace_bytes(src), 0xA5)
+    ci.coreinfer_kv4_evict(src, dst, budget, recent, first, ws)
+
+
+EVICT = [
+    # B, H, lengths, budget, recent, first, D, group, ties
+    (1, 1, [1], 1, 0, 0, 64, 32, False), (2, 2, [40, 10], 20, 4, 2, 64, 64, False), (3, 3, [0, 100, 33], 32, 32, 0, 128, 128, False),
+    (2, 4, [300, 257], 256, 10, 4, 128, 64, True), (1, 2, [1500], 100, 0, 0, 256, 32, True), (2, 2, [64, 64], 64, 0, 0, 64, 32, False),
+    (1, 3, [2000], 1999, 5, 5, 64, 32, False), (4, 1, [5000, 4096, 1, 1025], 1024, 256, 4, 64, 64, True),
+]
+
+
+@pytest.mark.parametrize("B,H,lengths,budget,recent,first,D,group,ties", EVICT)
+@pytest.mark.parametrize("in_place", [True, False])
+def test_evict(B, H, lengths, budget, recent, first, D, group, ties, in_place):
+    require_gpu()
+    rng = np.random.default_rng(budget + len(lengths))
+    cap = -(-max(lengths) // 16) * 16
+    ref = CacheRef(B, H, cap, D, group, rng)
+    if ties:
+        ref.weight = np.floor(ref.weight * 3) / 4                  # few distinct values, many zeros
+        ref.weight[0, 0, ::11] *= -0.0
+    ref.set_lengths(lengths)
+    for b in range(B):
+        for h in range(H):
+            ref.position[b, h, : lengths[b]] = rng.permutation(lengths[b])
+    d = ref.to_cuda()
+    src = handle(d)
+    if in_place:
+        evict(src, src, budget, recent, first)
+        ref.evict_here(budget, recent, first)
+        ref.assert_equal(d)
+        evict(src, src, budget, recent, first)                     # nothing is over the budget: nothing changes
+        ref.assert_equal(d)
+    else:
+        small = CacheRef(B, H, max(16, -(-budget // 16) * 16), D, group, rng)
+        z = small.to_cuda()
+        evict(src, handle(z), budget, recent, first)
+        ref.evict_to(small, budget, recent, first)
+        small.assert_equal(z)
+        ref.assert_equal(d)
+
+
+def test_evict_odd_weights():
+    """NaN weights go first, infinities stay, negative numbers order as numbers."""
+    require_gpu()
+    ref = CacheRef(1, 1, 64, 64, 32, np.random.default_rng(3))
+    ref.set_lengths([60])
+    ref.weight[0, 0, 5:25] = np.nan
+    ref.weight[0, 0, 40:44] = np.inf
+    ref.weight[0, 0, 44:50] = -np.arange(1.0, 7.0)
+    for budget in (50, 40, 36, 3):
+        d = ref.to_cuda()
+        other = CacheRef(1, 1, 64, 64, 32, np.random.default_rng(4))
+        z = other.to_cuda()
+        evict(handle(d), handle(z), budget, 0, 0)
+        ref.evict_to(other, budget, 0, 0)
+        other.assert_equal(z)
+
+
+def test_append_attend_evict_loop():
+    """A decode loop at a full budget: 40 steps of append, attention with accumulation, and eviction in place.  Positions
+    stay distinct, the recent tokens stay, and the attention over what is left matches the plain one."""
+    require_gpu()
+    B, H, share, D, group, budget, recent, first = 2, 2, 2, 64, 32, 48, 8, 2
+    rng = np.random.default_rng(12)
+    ref = CacheRef(B, H, 64, D, group, rng)
+    d = ref.to_cuda()
+    h = handle(d)
+    for step in range(40):
+        T = 1 + step % 3
+        k, v = (torch.from_numpy(rng.standard_normal((B, T, H, D)).astype(np.float32)).cuda() for _ in "kv")
+        ci.coreinfer_kv4_append(h, k, v)
+        ref.append(values_np(k), values_np(v))
+        q = torch.from_numpy(rng.standard_normal((B, T, H * share, D)).astype(np.float32)).cuda()
+        out = attend(ref, d, q)
+        check_attention(ref, d, q, out, D ** -0.5, ref.weight)
+        ref.weight = values_np(d["weight"]).astype(np.float64)     # eviction decides by the weights as accumulated
+        evict(h, h, budget, recent, first)
+        ref.evict_here(budget, recent, first)
+        ref.assert_equal(d)
+    pos = d["position"].cpu().numpy()[:, :, :budget]
+    seen = ref.seen[0]
+    for b in range(B):
+        for g in range(H):
+            assert len(set(pos[b, g])) == budget and set(range(seen - recent, seen)) <= set(pos[b, g]) and {0, 1} <= set(pos[b, g])
