@@ -1,82 +1,767 @@
-// Attention of a few new tokens over the 4-bit key/value cache.
+// Attention of a few new tokens per sequence over the 4-bit key/value cache.
+//
+// Mathematics.  With x^ = s c + o per group, a logit is  sum_g [ s_g sum_{d in g} q_d c_d + o_g sum_{d in g} q_d ]
+// and an output  sum_n (p_n s_n) c_nd + sum_n p_n o_n : both products run over the codes themselves, scales enter
+// as factors of fp32 sums (keys) or of the fp32 weights p (values).  One pass over the cache with a running
+// maximum per query row; rows = new tokens x query heads that share a key head.
+//
+// What bounds it: the bytes of the cache (codes and pairs of keys and values, each read once).  The work per
+// byte is what has to be kept small, so the codes go to mma.sync.m16n8k16 as fp16 subnormals (quant4.cuh: one AND
+// per two codes), 16 slots on the M side and 8 query rows on the N side: S^T = K Q^T, then O^T = V^T P^T with
+// P^T made from the accumulators of S^T by movmatrix.  tcgen05 would leave most of its 128 rows empty, and its
+// operands would have to be widened in shared memory first.
+//
+// kv4_attention_kernel: persistent CTAs of 8 warps over a ring of stages (128 slots of one sequence and head: four
+// bulk copies, all contiguous).  The warps take turns at refilling the stage of the tile before: a ninth warp for
+// the copies would cut the registers of a thread from 128 to 96 at two CTAs per SM.  The tiles of all (sequence, head)
+// units form one list, cut into equal pieces, one per CTA, whatever the lengths are; a unit that is cut leaves
+// partial results (maximum, sum, output) in the workspace.  kv4_finish_kernel joins those, and turns the
+// logits into weights that it adds to the cache's where that is asked for.
+// fp32 and fp16 calls carry query rows and p s as two fp16 parts in neighbouring columns (22 bits; four rows per
+// tile instead of eight): with one part the rounding of p s (2^-12, times the ratio of s c to the centred
+// value, about 3) would exceed fp16's own rounding.
 #include "kv4.cuh"
 
+#include <type_traits>
+
 namespace coreinfer {
+
+constexpr int kAttnTile = 128;              // slots per stage
+constexpr int kAttnWarps = 8;
+constexpr int kAttnThreads = 32 * kAttnWarps;
+constexpr int kAttnMaxStages = 8;
+constexpr int kAttnMaxCtas = 320;
+constexpr float kNoLogit = -1e30f;
 
 struct AttnArgs {
     Kv4 c;
     const void* q;
     void* out;
     long long ld_q, ld_out;
-    int Hq, T;
+    int Hq, T, share;
+    int R;                  // query rows per key head: T * share, row r = t * share + head
+    int RT;                 // row tiles (of 8 or 4 rows) per CTA, dividing the warps
+    int RU;                 // rows per unit: RT * 8 or RT * 4
+    int RB;                 // units per (sequence, key head)
+    int n_ctas;             // CTAs of the main kernel
+    int stages;
     float scale;
-    float* logits;          // [B][T][Hq][cap]
+    int accumulate;
+    unsigned* status;
+    float2* part_ml;        // [n_ctas][2][RU]: reference exponent and sum of a cut unit's piece
+    float* part_o;          // [n_ctas][2][RU][D]
+    float2* stats;          // [B][H][RB][RU]: the same of whole units, for the weights
+    float* logits;          // [B][H][R][cap], base-2 logits; only with accumulate
 };
 
-__device__ __forceinline__ float kv4_value(const Kv4& c, int which, size_t slot, int d)
+__device__ __forceinline__ int attn_tiles(int len) { return (len + kAttnTile - 1) / kAttnTile; }
+// CTA i of n takes the tiles from attn_start(i) to attn_start(i + 1), n at most the number of tiles, so that each
+// CTA has one at least; attn_owner is the CTA of tile t.
+__device__ __forceinline__ int attn_ctas(int n_ctas, int total) { return total < n_ctas ? total : n_ctas; }
+__device__ __forceinline__ int attn_start(int i, int total, int n) { return (int)((long long)i * total / n); }
+__device__ __forceinline__ int attn_owner(int t, int total, int n) { return (int)((((long long)t + 1) * n - 1) / total); }
+
+__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t a)
 {
-    const unsigned unit = *reinterpret_cast<const uint16_t*>(c.codes[which] + slot * (c.D / 2) + unit_offset(d & ~3, c.D / 32));
-    const __half2 p = c.pairs[which][slot * (c.D / c.G) + d / c.G];
-    return fmaf(__low2float(p), (float)((unit >> (4 * (d & 3))) & 15u), __high2float(p));
+    uint32_t d;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+    return d;
 }
 
-// One CTA per token and query head.
+// N consecutive 32-bit words of shared memory.
+template <int N>
+__device__ __forceinline__ void ld_words(uint32_t (&w)[N], const uint8_t* p)
+{
+    if constexpr (N == 1) w[0] = *reinterpret_cast<const uint32_t*>(p);
+    else if constexpr (N == 2) {
+        const uint2 v = *reinterpret_cast<const uint2*>(p);
+        w[0] = v.x; w[1] = v.y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            const uint4 v = *reinterpret_cast<const uint4*>(p + 4 * i);
+            w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
+        }
+    }
+}
+__device__ __forceinline__ float2 pair_f32(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+
+// Position in the list of tiles.
+struct Cursor {
+    int b, hr, tile, nt;
+};
+
+template <typename T, int D, int G, bool SPLIT>
+__global__ void __launch_bounds__(kAttnThreads, D <= 128 ? 2 : 1)
+kv4_attention_kernel(const __grid_constant__ AttnArgs a)
+{
+    constexpr int H32 = D / 32, NG = D / G, RPT = SPLIT ? 4 : 8, NV = SPLIT ? 1 : 2;
+    constexpr uint32_t CODE_ROW = D / 2, PAIR_ROW = NG * 4;
+    constexpr uint32_t CODE_TILE = kAttnTile * CODE_ROW, PAIR_TILE = kAttnTile * PAIR_ROW;
+    constexpr uint32_t STAGE = 2 * (CODE_TILE + PAIR_TILE);
+    const Kv4& c = a.c;
+
+    extern __shared__ __align__(128) uint8_t smem[];
+    float* obuf = reinterpret_cast<float*>(smem + (size_t)a.stages * STAGE);                // [8 warps][RPT][D]
+    float2* mlbuf = reinterpret_cast<float2*>(obuf + kAttnWarps * RPT * D);                  // [8 warps][RPT]
+    int* pre = reinterpret_cast<int*>(mlbuf + kAttnWarps * RPT);                             // [B + 1] tiles of a head before sequence b
+    int* lens = pre + c.B + 1;                                                               // [B]
+    __shared__ uint64_t full_bar[kAttnMaxStages], empty_bar[kAttnMaxStages];
+    __shared__ int abort_s;
+    volatile int* abort_flag = &abort_s;
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid == 0) {
+        for (int s = 0; s < a.stages; ++s) {
+            mbar_init(smem_u32(&full_bar[s]), 1);
+            mbar_init(smem_u32(&empty_bar[s]), kAttnWarps);
+        }
+        abort_s = 0;
+        mbar_fence_init();
+        if (blockIdx.x == 0) *a.status = kStatusOk;          // a wait gives up seconds later at the earliest
+    }
+    if (warp == 0) {
+        int run = 0;
+        for (int b0 = 0; b0 < c.B; b0 += 32) {
+            const int b = b0 + lane;
+            const int len = b < c.B ? kv4_length(c, b) : 0;
+            const int v = attn_tiles(len);
+            int incl = v;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int u = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += u;
+            }
+            if (b < c.B) {
+                lens[b] = len;
+                pre[b] = run + incl - v;
+            }
+            run += __shfl_sync(0xffffffffu, incl, 31);
+        }
+        if (lane == 0) pre[c.B] = run;
+    }
+    __syncthreads();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+    const int HR = c.H * a.RB;
+    const int total = pre[c.B] * HR;
+    const int n_ctas = attn_ctas(a.n_ctas, total), me = blockIdx.x;
+    const int begin = me < n_ctas ? attn_start(me, total, n_ctas) : 0, end = me < n_ctas ? attn_start(me + 1, total, n_ctas) : 0;
+    auto seek = [&](int t) {
+        Cursor k;
+        int lo = 0, hi = c.B - 1;                           // last b with pre[b] * HR <= t: it has tiles
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (pre[mid] * HR <= t) lo = mid; else hi = mid - 1;
+        }
+        k.b = lo;
+        k.nt = attn_tiles(lens[lo]);
+        const unsigned rem = (unsigned)(t - pre[lo] * HR);
+        k.hr = (int)(rem / (unsigned)k.nt);
+        k.tile = (int)(rem % (unsigned)k.nt);
+        return k;
+    };
+    // One thread: the copies of a tile into stage s.
+    auto fetch = [&](int b, int hr, int tile, int s) {
+        const int t0 = tile * kAttnTile;
+        // whole 16-slot pieces: the capacity is a multiple of 16, so they lie within the buffers
+        const int left = (lens[b] - t0 + 15) & ~15;
+        const uint32_t rows = left < kAttnTile ? left : kAttnTile;
+        const size_t slot = ((size_t)b * c.H + hr / a.RB) * c.cap + t0;
+        const uint32_t bar = smem_u32(&full_bar[s]), dst = smem_u32(smem + (size_t)s * STAGE);
+        mbar_arrive_expect_tx(bar, 2 * rows * (CODE_ROW + PAIR_ROW));
+        bulk_g2s(dst, c.codes[0] + slot * CODE_ROW, rows * CODE_ROW, bar);
+        bulk_g2s(dst + CODE_TILE, reinterpret_cast<const uint8_t*>(c.pairs[0]) + slot * PAIR_ROW, rows * PAIR_ROW, bar);
+        bulk_g2s(dst + CODE_TILE + PAIR_TILE, c.codes[1] + slot * CODE_ROW, rows * CODE_ROW, bar);
+        bulk_g2s(dst + 2 * CODE_TILE + PAIR_TILE, reinterpret_cast<const uint8_t*>(c.pairs[1]) + slot * PAIR_ROW, rows * PAIR_ROW, bar);
+    };
+
+    if (begin < end) {
+        if (tid == 0)
+            for (int s = 0; s < a.stages && begin + s < end; ++s) {
+                const Cursor p = seek(begin + s);
+                fetch(p.b, p.hr, p.tile, s);
+            }
+        const int rt = warp % a.RT, sg = warp / a.RT, nsg = kAttnWarps / a.RT;
+        const int gid = lane >> 2, tig = lane & 3;
+        const int tok0 = (gid >> 1) + (gid & 1) * 4;         // slot of accumulator row gid within 8; row gid + 8: tok0 + 8
+        Cursor k = seek(begin);
+        int s = 0;
+        uint32_t ph = 0;
+        int t = begin, prev = a.stages - 1;                  // prev: the stage of the tile before
+        uint32_t prev_ph = 0;
+        while (t < end) {
+            const int first_tile = k.tile, b = k.b, len = lens[b], h = k.hr / a.RB, rb = k.hr % a.RB;
+            const int n_tiles = end - t < k.nt - first_tile ? end - t : k.nt - first_tile;
+            const int row0 = rb * a.RU + rt * RPT;           // first query row of this warp's tile
+
+            // query rows as the B operand: column gid = row gid (or part gid & 1 of row gid >> 1), 8 values per 32
+            uint32_t qf[H32][4];
+            float qsum[NG][NV], f[NV];
+            int lim[NV];                                     // slots this lane's columns see
+            {
+                const int r = row0 + (SPLIT ? gid >> 1 : gid);
+                const bool valid = r < a.R;
+                const T* src = (const T*)a.q + ((long long)b * a.T + (valid ? r / a.share : 0)) * a.ld_q +
+                               (long long)(h * a.share + (valid ? r % a.share : 0)) * D + 8 * tig;
+                float v[H32][8], m = 0.f;
+#pragma unroll
+                for (int j = 0; j < H32; ++j) {
+                    T in[8];
+                    const uint4* p = reinterpret_cast<const uint4*>(src + j * 32);
+                    *reinterpret_cast<uint4*>(in) = p[0];
+                    if (sizeof(T) == 4) reinterpret_cast<uint4*>(in)[1] = p[1];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        v[j][e] = valid ? to_f32<T>(in[e]) : 0.f;
+                        m = fmaxf(m, fabsf(v[j][e]));
+                    }
+                }
+                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
+                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
+                const int x = range_exponent(m);             // the largest value goes to [2^13, 2^14)
+                const float up = ldexpf(1.f, 14 - x);
+                float gs[NG];
+#pragma unroll
+                for (int g = 0; g < NG; ++g) gs[g] = 0.f;
+#pragma unroll
+                for (int j = 0; j < H32; ++j) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        v[j][e] *= up;
+                        gs[j * 32 / G] += v[j][e];
+                    }
+                    const int low = SPLIT ? gid & 1 : 0;
+                    const float lo16 = 1.f / 16.f;           // odd codes stand 16 times higher
+                    qf[j][0] = pack_half2(half_part(v[j][0], low), half_part(v[j][4], low));
+                    qf[j][1] = pack_half2(half_part(v[j][2], low), half_part(v[j][6], low));
+                    qf[j][2] = pack_half2(half_part(v[j][1] * lo16, low), half_part(v[j][5] * lo16, low));
+                    qf[j][3] = pack_half2(half_part(v[j][3] * lo16, low), half_part(v[j][7] * lo16, low));
+                }
+                // sums of c q carry 2^-24, so the sums of q do too; f undoes both scalings
+                const float ff = ldexpf(a.scale * 1.44269504088896341f, x - 14 + 24);
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                    gs[g] += __shfl_xor_sync(0xffffffffu, gs[g], 1);
+                    gs[g] += __shfl_xor_sync(0xffffffffu, gs[g], 2);
+                    gs[g] *= 1.f / kCodeScaleLow;
+                }
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    const int from = (2 * tig + i) * 4;      // a lane of column 2 tig + i
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) qsum[g][i] = __shfl_sync(0xffffffffu, gs[g], from);
+                    f[i] = __shfl_sync(0xffffffffu, ff, from);
+                    const int rr = row0 + (SPLIT ? tig : 2 * tig + i);
+                    lim[i] = rr < a.R ? len - (a.T - 1 - rr / a.share) : 0;
+                }
+            }
+            float* lg[NV];
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int rr = row0 + (SPLIT ? tig : 2 * tig + i);
+                lg[i] = a.accumulate && rr < a.R ? a.logits + (((size_t)b * c.H + h) * a.R + rr) * c.cap : nullptr;
+            }
+            const int all_see = len - (a.T - 1);             // slots below this are seen by every row
+
+            float o[H32][2][4], om[NG][NV], l[NV], mx[NV];
+            // The weights enter the second product as p s 2^E in fp16: E keeps the largest s near 2^9, so
+            // that p s neither overflows nor loses bits to fp16's bottom for p down to about 2^-20.
+            float E = 0.f, s_most = -1.f;
+#pragma unroll
+            for (int j = 0; j < H32; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[j][0][e] = o[j][1][e] = 0.f;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                l[i] = 0.f;
+                mx[i] = kNoLogit;
+#pragma unroll
+                for (int g = 0; g < NG; ++g) om[g][i] = 0.f;
+            }
+
+            for (int it = 0; it < n_tiles; ++it) {
+                const int t0 = (first_tile + it) * kAttnTile;
+                const int refill = t + it - 1 + a.stages;    // goes where tile t + it - 1 was
+                if (warp == ((t + it) & (kAttnWarps - 1)) && lane == 0 && t + it > begin && refill < end) {
+                    bounded_wait(smem_u32(&empty_bar[prev]), prev_ph, abort_flag, a.status);
+                    if (!*abort_flag) {
+                        if (first_tile + it - 1 + a.stages < k.nt) {
+                            fetch(b, k.hr, first_tile + it - 1 + a.stages, prev);
+                        } else {
+                            const Cursor p = seek(refill);
+                            fetch(p.b, p.hr, p.tile, prev);
+                        }
+                    }
+                }
+                __syncwarp();
+                bounded_wait(smem_u32(&full_bar[s]), ph, abort_flag, a.status);
+                const uint8_t* st = smem + (size_t)s * STAGE;
+                for (int sub = sg; sub < kAttnTile / 16; sub += nsg) {
+                    const int n0 = t0 + sub * 16;
+                    if (n0 >= len) break;
+                    // ---- logits: S^T [16 slots][8 columns] ----
+                    const uint8_t* krow = st + (sub * 16 + tok0) * CODE_ROW + tig * (D / 8);
+                    uint32_t w0[D / 32], w1[D / 32], kp0[NG], kp1[NG];
+                    ld_words<D / 32>(w0, krow);
+                    ld_words<D / 32>(w1, krow + 8 * CODE_ROW);
+                    const uint8_t* kpr = st + CODE_TILE + (sub * 16 + tok0) * PAIR_ROW;
+                    ld_words<NG>(kp0, kpr);
+                    ld_words<NG>(kp1, kpr + 8 * PAIR_ROW);
+                    float lo0[NV], lo1[NV];                  // slots tok0 and tok0 + 8
+#pragma unroll
+                    for (int i = 0; i < NV; ++i) lo0[i] = lo1[i] = 0.f;
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) {
+                        float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int j = g * G / 32; j < (g + 1) * G / 32; ++j) {
+                            const uint32_t x0 = __byte_perm(w0[j / 2], w0[H32 / 2 + j / 2], j & 1 ? 0x7632 : 0x5410);
+                            const uint32_t x1 = __byte_perm(w1[j / 2], w1[H32 / 2 + j / 2], j & 1 ? 0x7632 : 0x5410);
+                            const uint32_t y0 = x0 >> 8, y1 = x1 >> 8;
+                            mma_16816(acc, x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, qf[j][0], qf[j][1]);
+                            mma_16816(acc, x0 & 0x00f000f0u, x1 & 0x00f000f0u, y0 & 0x00f000f0u, y1 & 0x00f000f0u, qf[j][2], qf[j][3]);
+                        }
+                        const float2 p0 = pair_f32(kp0[g]), p1 = pair_f32(kp1[g]);
+                        if (SPLIT) {
+                            lo0[0] = fmaf(p0.x, acc[0] + acc[1], fmaf(p0.y, qsum[g][0], lo0[0]));
+                            lo1[0] = fmaf(p1.x, acc[2] + acc[3], fmaf(p1.y, qsum[g][0], lo1[0]));
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < NV; ++i) {
+                                lo0[i] = fmaf(p0.x, acc[i], fmaf(p0.y, qsum[g][i], lo0[i]));
+                                lo1[i] = fmaf(p1.x, acc[2 + i], fmaf(p1.y, qsum[g][i], lo1[i]));
+                            }
+                        }
+                    }
+                    const int na = n0 + tok0, nb = na + 8;
+                    const bool edge = n0 + 16 > all_see;     // some row does not see some slot
+#pragma unroll
+                    for (int i = 0; i < NV; ++i) {
+                        lo0[i] *= f[i];
+                        lo1[i] *= f[i];
+                        if (edge) {
+                            if (na >= lim[i]) lo0[i] = -__int_as_float(0x7f800000);
+                            if (nb >= lim[i]) lo1[i] = -__int_as_float(0x7f800000);
+                        }
+                        if (lg[i]) {
+                            if (na < lim[i]) lg[i][na] = lo0[i];
+                            if (nb < lim[i]) lg[i][nb] = lo1[i];
+                        }
+                    }
+                    // ---- value pairs, running maximum ----
+                    const uint8_t* vpr = st + 2 * CODE_TILE + PAIR_TILE + (sub * 16 + tok0) * PAIR_ROW;
+                    uint32_t vp0[NG], vp1[NG];
+                    ld_words<NG>(vp0, vpr);
+                    ld_words<NG>(vp1, vpr + 8 * PAIR_ROW);
+                    if (edge) {                              // what lies beyond the sequence is never used
+#pragma unroll
+                        for (int g = 0; g < NG; ++g) {
+                            if (na >= len) vp0[g] = 0u;
+                            if (nb >= len) vp1[g] = 0u;
+                        }
+                    }
+                    float smax = 0.f;
+                    float2 v0[NG], v1[NG];
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) {
+                        v0[g] = pair_f32(vp0[g]);
+                        v1[g] = pair_f32(vp1[g]);
+                        smax = fmaxf(smax, fmaxf(v0[g].x, v1[g].x));
+                    }
+                    bool change = smax > s_most;
+#pragma unroll
+                    for (int i = 0; i < NV; ++i) change |= fmaxf(lo0[i], lo1[i]) > mx[i];
+                    if (__any_sync(0xffffffffu, change)) {
+                        float e_new = E;
+                        if (__any_sync(0xffffffffu, smax > s_most)) {
+#pragma unroll
+                            for (int d = 1; d < 32; d <<= 1) smax = fmaxf(smax, __shfl_xor_sync(0xffffffffu, smax, d));
+                            int x;
+                            frexpf(smax, &x);
+                            x = smax > 0.f ? (x < -15 ? -15 : x) : -15;
+                            e_new = (float)(9 - x);
+                            s_most = ldexpf(1.f, x + 5);     // room for scales up to 32 times larger before E moves
+                        }
+#pragma unroll
+                        for (int i = 0; i < NV; ++i) {
+                            float m = fmaxf(lo0[i], lo1[i]);
+                            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+                            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+                            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+                            m = fmaxf(m, mx[i]);
+                            const float corr = exp2_fast((mx[i] - E) - (m - e_new));
+                            mx[i] = m;
+                            l[i] *= corr;
+#pragma unroll
+                            for (int g = 0; g < NG; ++g) om[g][i] *= corr;
+#pragma unroll
+                            for (int j = 0; j < H32; ++j)
+#pragma unroll
+                                for (int e = 0; e < 2; ++e) {
+                                    o[j][e][i] *= corr;
+                                    o[j][e][2 + i] *= corr;
+                                    if (SPLIT) {
+                                        o[j][e][1] *= corr;
+                                        o[j][e][3] *= corr;
+                                    }
+                                }
+                        }
+                        E = e_new;
+                    }
+                    float p0[NV], p1[NV];
+#pragma unroll
+                    for (int i = 0; i < NV; ++i) {
+                        const float ref = mx[i] - E;
+                        p0[i] = exp2_fast(lo0[i] - ref);
+                        p1[i] = exp2_fast(lo1[i] - ref);
+                        l[i] += p0[i] + p1[i];
+                    }
+                    // ---- O^T += V^T P^T, per group of scales ----
+                    const uint8_t* vrow = st + CODE_TILE + PAIR_TILE + (sub * 16 + tig) * CODE_ROW + gid * (D / 16);
+                    uint32_t va[H32 / 2], vb[H32 / 2], vc[H32 / 2], vd[H32 / 2];
+                    ld_words<H32 / 2>(va, vrow);
+                    ld_words<H32 / 2>(vb, vrow + 4 * CODE_ROW);
+                    ld_words<H32 / 2>(vc, vrow + 8 * CODE_ROW);
+                    ld_words<H32 / 2>(vd, vrow + 12 * CODE_ROW);
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) {
+                        uint32_t b0, b1;
+                        float ps0[NV], ps1[NV];
+#pragma unroll
+                        for (int i = 0; i < NV; ++i) {
+                            ps0[i] = p0[i] * v0[g].x;
+                            ps1[i] = p1[i] * v1[g].x;
+                            float po0 = p0[i] * v0[g].y, po1 = p1[i] * v1[g].y;
+                            if (edge) {                      // a slot a row does not see adds nothing, whatever it holds
+                                if (na >= lim[i]) ps0[i] = po0 = 0.f;
+                                if (nb >= lim[i]) ps1[i] = po1 = 0.f;
+                            }
+                            om[g][i] += po0 + po1;
+                        }
+                        if (SPLIT) {
+                            const float h0 = __half2float(__float2half_rn(ps0[0])), h1 = __half2float(__float2half_rn(ps1[0]));
+                            b0 = movmatrix_trans(pack_half2(h0, ps0[0] - h0));
+                            b1 = movmatrix_trans(pack_half2(h1, ps1[0] - h1));
+                        } else {
+                            b0 = movmatrix_trans(pack_half2(ps0[0], ps0[NV - 1]));
+                            b1 = movmatrix_trans(pack_half2(ps1[0], ps1[NV - 1]));
+                        }
+#pragma unroll
+                        for (int j = g * G / 32; j < (g + 1) * G / 32; ++j) {
+                            const uint32_t x = __byte_perm(va[j / 2], vb[j / 2], j & 1 ? 0x7632 : 0x5410);
+                            const uint32_t y = __byte_perm(vc[j / 2], vd[j / 2], j & 1 ? 0x7632 : 0x5410);
+                            const uint32_t x8 = x >> 8, y8 = y >> 8;
+                            mma_16816(o[j][0], x & 0x000f000fu, x8 & 0x000f000fu, y & 0x000f000fu, y8 & 0x000f000fu, b0, b1);
+                            mma_16816(o[j][1], x & 0x00f000f0u, x8 & 0x00f000f0u, y & 0x00f000f0u, y8 & 0x00f000f0u, b0, b1);
+                        }
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&empty_bar[s]));
+                prev = s;
+                prev_ph = ph;
+                if (++s == a.stages) { s = 0; ph ^= 1u; }
+            }
+
+            // ---- join the warps of a row tile ----
+            __syncthreads();                                 // the buffer's last use is over
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) {
+                    l[i] += __shfl_xor_sync(0xffffffffu, l[i], d);
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) om[g][i] += __shfl_xor_sync(0xffffffffu, om[g][i], d);
+                }
+                const int r = SPLIT ? tig : 2 * tig + i;
+                if (gid == 0) mlbuf[warp * RPT + r] = make_float2(mx[i] - E, l[i]);
+#pragma unroll
+                for (int j = 0; j < H32; ++j) {
+                    const float add = om[j * 32 / G][i];
+                    float4 v;
+                    if (SPLIT) {
+                        v.x = o[j][0][0] + o[j][0][1];
+                        v.y = o[j][1][0] + o[j][1][1];
+                        v.z = o[j][0][2] + o[j][0][3];
+                        v.w = o[j][1][2] + o[j][1][3];
+                    } else {
+                        v.x = o[j][0][i];
+                        v.y = o[j][1][i];
+                        v.z = o[j][0][2 + i];
+                        v.w = o[j][1][2 + i];
+                    }
+                    v.x = fmaf(v.x, kCodeScaleLow, add);
+                    v.y = fmaf(v.y, kCodeScaleHigh, add);
+                    v.z = fmaf(v.z, kCodeScaleLow, add);
+                    v.w = fmaf(v.w, kCodeScaleHigh, add);
+                    *reinterpret_cast<float4*>(obuf + ((size_t)warp * RPT + r) * D + j * 32 + gid * 4) = v;
+                }
+            }
+            __syncthreads();
+            const bool whole = n_tiles == k.nt;
+            const int piece = blockIdx.x * 2 + (first_tile == 0 ? 1 : 0);
+            for (int i = tid; i < a.RU * (D / 4); i += 32 * kAttnWarps) {
+                const int ru = i / (D / 4), d4 = i % (D / 4);
+                const int r = rb * a.RU + ru;
+                if (r >= a.R) break;
+                const int wrt = ru / RPT, slot = ru % RPT;
+                float top = kNoLogit * 2.f;
+                for (int w = wrt; w < kAttnWarps; w += a.RT) top = fmaxf(top, mlbuf[w * RPT + slot].x);
+                float sum = 0.f;
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int w = wrt; w < kAttnWarps; w += a.RT) {
+                    const float2 ml = mlbuf[w * RPT + slot];
+                    const float e = exp2_fast(ml.x - top);
+                    const float4 x = *reinterpret_cast<const float4*>(obuf + ((size_t)w * RPT + slot) * D + d4 * 4);
+                    sum = fmaf(ml.y, e, sum);
+                    v.x = fmaf(x.x, e, v.x);
+                    v.y = fmaf(x.y, e, v.y);
+                    v.z = fmaf(x.z, e, v.z);
+                    v.w = fmaf(x.w, e, v.w);
+                }
+                if (whole) {
+                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                    T* dst = (T*)a.out + ((long long)b * a.T + r / a.share) * a.ld_out + (long long)(h * a.share + r % a.share) * D + d4 * 4;
+                    dst[0] = from_f32<T>(v.x * inv);
+                    dst[1] = from_f32<T>(v.y * inv);
+                    dst[2] = from_f32<T>(v.z * inv);
+                    dst[3] = from_f32<T>(v.w * inv);
+                    if (d4 == 0 && a.accumulate) a.stats[(((size_t)b * c.H + h) * a.RB + rb) * a.RU + ru] = make_float2(top, sum);
+                } else {
+                    *reinterpret_cast<float4*>(a.part_o + ((size_t)piece * a.RU + ru) * D + d4 * 4) = v;
+                    if (d4 == 0) a.part_ml[(size_t)piece * a.RU + ru] = make_float2(top, sum);
+                }
+            }
+            t += n_tiles;
+            if (t < end) k = seek(t);
+        }
+    }
+    __syncthreads();
+    if (tid == 0 && *abort_flag) {
+        // after a wait that gave up copies may be in flight: give them a bounded time to land
+        const long long t0 = clock64();
+        while (clock64() - t0 < 20000000LL) __nanosleep(1000);
+    }
+    __syncthreads();
+}
+
+// ------------------------------------------------------------------------------ finish --
+// Blocks x < R of a (sequence, head): query row x, joined from the pieces of its unit where that was cut
+// (zeros where the sequence is empty).  Blocks beyond: 1024 slots each, whose weights get the
+// sum over rows of 2^(logit - maximum) / sum.
+constexpr int kFinishThreads = 256;
+constexpr int kFinishSlots = 1024;
+
+template <typename V, typename Op>
+__device__ __forceinline__ V finish_reduce(V v, V* buf, Op op)
+{
+#pragma unroll
+    for (int d = 16; d; d >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, d));
+    if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = buf[0];
+#pragma unroll
+    for (int i = 1; i < kFinishThreads / 32; ++i) v = op(v, buf[i]);
+    __syncthreads();
+    return v;
+}
+
 template <typename T>
-__global__ void __launch_bounds__(256) kv4_attention_kernel(AttnArgs a)
+__global__ void __launch_bounds__(kFinishThreads) kv4_finish_kernel(const __grid_constant__ AttnArgs a)
 {
-    __shared__ float q[256], red[8];
-    const int qh = blockIdx.x, t = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ int redi[8];
+    __shared__ float redf[8];
     const Kv4& c = a.c;
-    const int h = qh / (a.Hq / c.H);
-    const int n = kv4_length(c, b) - (a.T - 1 - t);
-    const size_t base = ((size_t)b * c.H + h) * c.cap;
-    float* lg = a.logits + (((size_t)b * a.T + t) * a.Hq + qh) * c.cap;
-    if (tid < c.D) q[tid] = to_f32<T>(((const T*)a.q)[((long long)b * a.T + t) * a.ld_q + (long long)qh * c.D + tid]) * a.scale;
-    __syncthreads();
-    float top = -__int_as_float(0x7f800000);
-    for (int i = warp; i < n; i += 8) {
-        float s = 0.f;
-        for (int d = lane; d < c.D; d += 32) s = fmaf(q[d], kv4_value(c, 0, base + i, d), s);
-#pragma unroll
-        for (int e = 16; e; e >>= 1) s += __shfl_xor_sync(0xffffffffu, s, e);
-        if (lane == 0) lg[i] = s;
-        top = fmaxf(top, s);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int b = blockIdx.y / c.H, h = blockIdx.y % c.H, D = c.D;
+    const int len = kv4_length(c, b);
+    if ((int)blockIdx.x >= a.R && ((int)blockIdx.x - a.R) * kFinishSlots >= len) return;
+    int before = 0, all = 0;
+    for (int i = tid; i < c.B; i += kFinishThreads) {
+        const int n = attn_tiles(kv4_length(c, i));
+        all += n;
+        if (i < b) before += n;
     }
-    if (lane == 0) red[warp] = top;
-    __syncthreads();
-    for (int i = 0; i < 8; ++i) top = fmaxf(top, red[i]);
-    __syncthreads();
-    float sum = 0.f;
-    for (int i = tid; i < n; i += 256) {
-        const float p = expf(lg[i] - top);
-        lg[i] = p;
-        sum += p;
+    auto add = [](int x, int y) { return x + y; };
+    before = finish_reduce(before, redi, add);
+    all = finish_reduce(all, redi, add);
+    const int HR = c.H * a.RB, nt = attn_tiles(len), total = all * HR, n_ctas = attn_ctas(a.n_ctas, total);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+
+    if ((int)blockIdx.x < a.R) {
+        const int r = blockIdx.x, rb = r / a.RU, ru = r % a.RU;
+        T* dst = (T*)a.out + ((long long)b * a.T + r / a.share) * a.ld_out + (long long)(h * a.share + r % a.share) * D;
+        if (nt == 0) {
+            for (int d = tid; d < D; d += kFinishThreads) dst[d] = from_f32<T>(0.f);
+            return;
+        }
+        const int u0 = before * HR + (h * a.RB + rb) * nt;
+        const int i0 = attn_owner(u0, total, n_ctas), i1 = attn_owner(u0 + nt - 1, total, n_ctas);
+        if (i0 == i1) return;
+        float* wgt = reinterpret_cast<float*>(smem);                     // [pieces]
+        const int n = i1 - i0 + 1;
+        auto piece = [&](int i) { return (size_t)(i0 + i) * 2 + (i == 0 ? 1 : 0); };
+        float top = kNoLogit * 2.f;
+        for (int i = tid; i < n; i += kFinishThreads) top = fmaxf(top, a.part_ml[piece(i) * a.RU + ru].x);
+        top = finish_reduce(top, redf, [](float x, float y) { return fmaxf(x, y); });
+        float sum = 0.f;
+        for (int i = tid; i < n; i += kFinishThreads) {
+            const float2 ml = a.part_ml[piece(i) * a.RU + ru];
+            const float e = exp2_fast(ml.x - top);
+            wgt[i] = e;
+            sum = fmaf(ml.y, e, sum);
+        }
+        sum = finish_reduce(sum, redf, [](float x, float y) { return x + y; });
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        // D / 4 threads cover the row, 256 / (D / 4) of such groups take the pieces in turn
+        const int quads = D / 4, groups = kFinishThreads / quads, d4 = tid % quads, g = tid / quads;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int i = g; i < n; i += groups) {
+            const float4 x = *reinterpret_cast<const float4*>(a.part_o + (piece(i) * a.RU + ru) * D + d4 * 4);
+            const float e = wgt[i];
+            v.x = fmaf(x.x, e, v.x);
+            v.y = fmaf(x.y, e, v.y);
+            v.z = fmaf(x.z, e, v.z);
+            v.w = fmaf(x.w, e, v.w);
+        }
+        float4* buf = reinterpret_cast<float4*>(smem + kAttnMaxCtas * sizeof(float));
+        buf[tid] = v;
+        __syncthreads();
+        if (g == 0) {
+            for (int j = 1; j < groups; ++j) {
+                const float4 x = buf[j * quads + d4];
+                v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+            }
+            dst[d4 * 4] = from_f32<T>(v.x * inv);
+            dst[d4 * 4 + 1] = from_f32<T>(v.y * inv);
+            dst[d4 * 4 + 2] = from_f32<T>(v.z * inv);
+            dst[d4 * 4 + 3] = from_f32<T>(v.w * inv);
+        }
+        return;
     }
+
+    // weights: maximum and 1 / sum of every row, one warp per row
+    float2* rows = reinterpret_cast<float2*>(smem);                      // [R]
+    for (int r = warp; r < a.R; r += kFinishThreads / 32) {
+        const int rb = r / a.RU, ru = r % a.RU;
+        const int u0 = before * HR + (h * a.RB + rb) * nt;
+        const int i0 = attn_owner(u0, total, n_ctas), i1 = attn_owner(u0 + nt - 1, total, n_ctas);
+        float top, sum;
+        if (i0 == i1) {
+            const float2 ml = a.stats[(((size_t)b * c.H + h) * a.RB + rb) * a.RU + ru];
+            top = ml.x;
+            sum = ml.y;
+        } else {
+            top = kNoLogit * 2.f;
+            for (int i = i0 + lane; i <= i1; i += 32) top = fmaxf(top, a.part_ml[((size_t)i * 2 + (i == i0)) * a.RU + ru].x);
 #pragma unroll
-    for (int e = 16; e; e >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, e);
-    if (lane == 0) red[warp] = sum;
+            for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            sum = 0.f;
+            for (int i = i0 + lane; i <= i1; i += 32) {
+                const float2 ml = a.part_ml[((size_t)i * 2 + (i == i0)) * a.RU + ru];
+                sum = fmaf(ml.y, exp2_fast(ml.x - top), sum);
+            }
+#pragma unroll
+            for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        }
+        if (lane == 0) rows[r] = make_float2(top, sum == 0.f ? 0.f : 1.f / sum);
+    }
     __syncthreads();
-    sum = 0.f;
-    for (int i = 0; i < 8; ++i) sum += red[i];
-    for (int i = tid; i < c.cap; i += 256) lg[i] = i < n ? lg[i] / sum : 0.f;
-    __syncthreads();
-    if (tid < c.D) {
-        float o = 0.f;
-        for (int i = 0; i < n; ++i) o = fmaf(lg[i], kv4_value(c, 1, base + i, tid), o);
-        ((T*)a.out)[((long long)b * a.T + t) * a.ld_out + (long long)qh * c.D + tid] = from_f32<T>(o);
+    const int n0 = ((int)blockIdx.x - a.R) * kFinishSlots;
+    const float* lg = a.logits + ((size_t)b * c.H + h) * a.R * c.cap;
+    float* weight = c.weight + ((size_t)b * c.H + h) * c.cap;
+    for (int n = n0 + tid; n < n0 + kFinishSlots && n < len; n += kFinishThreads) {
+        float w = 0.f;
+        for (int r = 0; r < a.R; ++r)
+            if (n < len - (a.T - 1 - r / a.share)) w = fmaf(exp2_fast(lg[(size_t)r * c.cap + n] - rows[r].x), rows[r].y, w);
+        weight[n] += w;
     }
 }
 
-__global__ void kv4_accumulate_kernel(AttnArgs a)
+// -------------------------------------------------------------------------------- host --
+static inline size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// Rows per unit and units per key head for R query rows.
+static void attn_rows(int R, bool split, int* RT, int* RU, int* RB)
 {
-    const Kv4& c = a.c;
-    const int i = blockIdx.x * blockDim.x + threadIdx.x, h = blockIdx.y, b = blockIdx.z, share = a.Hq / c.H;
-    if (i >= kv4_length(c, b)) return;
-    float w = 0.f;
-    for (int t = 0; t < a.T; ++t)
-        for (int g = 0; g < share; ++g) w += a.logits[(((size_t)b * a.T + t) * a.Hq + h * share + g) * c.cap + i];
-    c.weight[((size_t)b * c.H + h) * c.cap + i] += w;
+    const int rpt = split ? 4 : 8, tiles = (R + rpt - 1) / rpt;
+    *RT = tiles > 4 ? 8 : (tiles > 2 ? 4 : tiles);
+    *RU = *RT * rpt;
+    *RB = (R + *RU - 1) / *RU;
 }
+
+struct AttnLayout {
+    size_t ml, o, stats, logits, total;
+};
+static AttnLayout attn_layout(const Kv4& c, int R, bool split)
+{
+    int RT, RU, RB;
+    attn_rows(R, split, &RT, &RU, &RB);
+    AttnLayout w;
+    w.ml = 256;
+    w.o = w.ml + up256((size_t)kAttnMaxCtas * 2 * RU * sizeof(float2));
+    w.stats = w.o + up256((size_t)kAttnMaxCtas * 2 * RU * c.D * sizeof(float));
+    w.logits = w.stats + up256((size_t)c.B * c.H * RB * RU * sizeof(float2));
+    w.total = w.logits + (c.weight ? up256((size_t)c.B * c.H * R * c.cap * sizeof(float)) : 0);
+    return w;
+}
+
+template <typename T, int D, int G>
+static coreinfer_status launch_attention(AttnArgs& a, const DeviceInfo& di, cudaStream_t st)
+{
+    constexpr bool SPLIT = sizeof(T) == 4 || std::is_same<T, __half>::value;
+    constexpr int RPT = SPLIT ? 4 : 8, NG = D / G;
+    constexpr size_t STAGE = (size_t)2 * kAttnTile * (D / 2 + NG * 4);
+    auto kernel = kv4_attention_kernel<T, D, G, SPLIT>;
+    const int per_sm = D <= 128 ? 2 : 1;
+    const size_t fixed = (size_t)kAttnWarps * RPT * (D * sizeof(float) + sizeof(float2)) + (2 * a.c.B + 1) * sizeof(int);
+    const size_t room = (size_t)di.smem_optin / per_sm - 2048;
+    int stages = (int)((room - fixed) / STAGE);
+    if (stages > kAttnMaxStages) stages = kAttnMaxStages;
+    if (room < fixed || stages < 2) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "not enough shared memory for two pipeline stages");
+    a.stages = stages;
+    const size_t smem = fixed + stages * STAGE;
+    const long long tiles = (long long)a.c.B * a.c.H * a.RB * ((a.c.cap + kAttnTile - 1) / kAttnTile);
+    if (tiles > (1LL << 30)) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "the cache has %lld tiles of %d slots: too many for one call", tiles, kAttnTile);
+    long long ctas = (long long)di.sm_count * per_sm;
+    if (ctas > kAttnMaxCtas) ctas = kAttnMaxCtas;
+    if (ctas > tiles) ctas = tiles;
+    a.n_ctas = (int)ctas;
+    CI_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    kernel<<<a.n_ctas, kAttnThreads, smem, st>>>(a);
+    CI_CUDA(cudaGetLastError());
+
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(a.R + (a.accumulate ? (a.c.cap + kFinishSlots - 1) / kFinishSlots : 0), a.c.B * a.c.H);
+    cfg.blockDim = dim3(kFinishThreads);
+    const size_t join = kAttnMaxCtas * sizeof(float) + kFinishThreads * sizeof(float4), rows = (size_t)a.R * sizeof(float2);
+    cfg.dynamicSmemBytes = join > rows ? join : rows;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    CI_CUDA(cudaLaunchKernelEx(&cfg, kv4_finish_kernel<T>, a));
+    return COREINFER_OK;
+}
+
+template <typename T>
+static coreinfer_status pick_attention(AttnArgs& a, const DeviceInfo& di, cudaStream_t st)
+{
+    const int D = a.c.D, G = a.c.G;
+    if (D == 64) return G == 32 ? launch_attention<T, 64, 32>(a, di, st) : launch_attention<T, 64, 64>(a, di, st);
+    if (D == 128)
+        return G == 32 ? launch_attention<T, 128, 32>(a, di, st)
+                       : (G == 64 ? launch_attention<T, 128, 64>(a, di, st) : launch_attention<T, 128, 128>(a, di, st));
+    return G == 32 ? launch_attention<T, 256, 32>(a, di, st)
+                   : (G == 64 ? launch_attention<T, 256, 64>(a, di, st) : launch_attention<T, 256, 128>(a, di, st));
+}
+
+constexpr int kAttnMaxRows = 4096;          // query rows per key head (they sit in shared memory of the finishing kernel)
 
 }  // namespace coreinfer
 
@@ -89,7 +774,10 @@ size_t coreinfer_kv4_attention_workspace_bytes(const coreinfer_kv4_cache* cache,
     Kv4 c;
     if (kv4_take(cache, "the", &c) != COREINFER_OK) return 0;
     if (q_heads < 1 || T < 1 || q_heads % c.H != 0 || T > COREINFER_KV4_MAX_QUERIES) return 0;
-    return (size_t)c.B * T * q_heads * c.cap * sizeof(float);
+    const long long R = (long long)(q_heads / c.H) * T;
+    if (R > kAttnMaxRows) return 0;
+    const size_t x = attn_layout(c, (int)R, false).total, y = attn_layout(c, (int)R, true).total;
+    return x > y ? x : y;
 }
 
 coreinfer_status coreinfer_kv4_attention(const coreinfer_kv4_cache* cache, const void* q, coreinfer_dtype dtype,
@@ -105,7 +793,9 @@ coreinfer_status coreinfer_kv4_attention(const coreinfer_kv4_cache* cache, const
         CI_FAIL(COREINFER_ERR_UNSUPPORTED, "T %d: 1..%d tokens a sequence", T, COREINFER_KV4_MAX_QUERIES);
     if (q_heads < 1 || q_heads % a.c.H != 0)
         CI_FAIL(COREINFER_ERR_INVALID_ARG, "q_heads %d is not a multiple of kv_heads %d", q_heads, a.c.H);
-    if (q_heads > 65535) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "q_heads %d: at most 65535", q_heads);
+    const long long R = (long long)(q_heads / a.c.H) * T;
+    if (R > kAttnMaxRows) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "%lld query rows per key head: at most %d", R, kAttnMaxRows);
+    if ((long long)a.c.B * a.c.H > 65535) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "batch * kv_heads: at most 65535");
     if (!q || !out || !aligned16(q) || !aligned16(out)) CI_FAIL(COREINFER_ERR_INVALID_ARG, "q / out NULL or not 16-byte aligned");
     const int64_t row = (int64_t)q_heads * a.c.D, e = (int64_t)dtype_size(dtype);
     if (ld_q < row || ld_out < row || (ld_q * e) % 16 != 0 || (ld_out * e) % 16 != 0)
@@ -117,25 +807,29 @@ coreinfer_status coreinfer_kv4_attention(const coreinfer_kv4_cache* cache, const
     if (workspace_bytes < need) CI_FAIL(COREINFER_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
     DeviceInfo di;
     if ((s = device_info(&di)) != COREINFER_OK) return s;
-    cudaStream_t st = (cudaStream_t)cuda_stream;
+    const bool split = dtype != COREINFER_BF16;
+    const AttnLayout w = attn_layout(a.c, (int)R, split);
+    uint8_t* ws = (uint8_t*)workspace;
     a.q = q;
     a.out = out;
     a.ld_q = ld_q;
     a.ld_out = ld_out;
     a.Hq = q_heads;
     a.T = T;
+    a.share = q_heads / a.c.H;
+    a.R = (int)R;
+    attn_rows(a.R, split, &a.RT, &a.RU, &a.RB);
     a.scale = scale;
-    a.logits = (float*)workspace;
-    const dim3 grid(q_heads, T, a.c.B);
-    if (dtype == COREINFER_F32) kv4_attention_kernel<float><<<grid, 256, 0, st>>>(a);
-    else if (dtype == COREINFER_BF16) kv4_attention_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>(a);
-    else kv4_attention_kernel<__half><<<grid, 256, 0, st>>>(a);
-    CI_CUDA(cudaGetLastError());
-    if (accumulate) {
-        kv4_accumulate_kernel<<<dim3((a.c.cap + 255) / 256, a.c.H, a.c.B), 256, 0, st>>>(a);
-        CI_CUDA(cudaGetLastError());
-    }
-    return COREINFER_OK;
+    a.accumulate = accumulate ? 1 : 0;
+    a.status = (unsigned*)ws;
+    a.part_ml = (float2*)(ws + w.ml);
+    a.part_o = (float*)(ws + w.o);
+    a.stats = (float2*)(ws + w.stats);
+    a.logits = (float*)(ws + w.logits);
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (dtype == COREINFER_F32) return pick_attention<float>(a, di, st);
+    if (dtype == COREINFER_BF16) return pick_attention<__nv_bfloat16>(a, di, st);
+    return pick_attention<__half>(a, di, st);
 }
 
 }  // extern "C"

@@ -58,6 +58,65 @@ __device__ __forceinline__ unsigned quant_code(float x, float s, float o)
     return (unsigned)fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(x, o), s)), 0.f), 15.f);
 }
 
+// ---- codes as matrix operands ----
+// Four bits masked into the low end of a 16-bit lane ARE an fp16 number: the subnormal c * 2^-24 (bits 0-3)
+// or c * 2^-20 (bits 4-7), exact, and mma takes fp16 subnormals at their value.  One AND therefore turns
+// two codes into a pair of operands; the factor 2^24 (2^20) is applied to the fp32 sums.
+constexpr float kCodeScaleLow = 16777216.f;     // 2^24
+constexpr float kCodeScaleHigh = 1048576.f;     // 2^20
+
+__device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi)
+{
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+// v rounded to fp16, or what that rounding left over: together 22 bits of v.
+__device__ __forceinline__ float half_part(float v, int low)
+{
+    const float h = __half2float(__float2half_rn(v));
+    return low ? v - h : v;
+}
+// Exponent x with m = max |v| in [2^(x-1), 2^x); 0 where no scaling can help (m = 0, infinite or NaN).
+__device__ __forceinline__ int range_exponent(float m)
+{
+    if (!(m > 0.f) || m > 3.4028235e38f) return 14;
+    int x;
+    frexpf(m, &x);
+    return x < -100 ? -100 : x;
+}
+__device__ __forceinline__ float exp2_fast(float v)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+// ---- bounded wait on a copy barrier ----
+// Once a wait has given up, `abort_flag` (shared memory of the CTA) is up and every later wait returns at
+// once: all warps run to their end without waiting, so none is left behind at a barrier.
+constexpr long long kQuantWaitCycles = 3000000000LL;
+__device__ __forceinline__ void bounded_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, unsigned* status)
+{
+    if (mbar_try_wait(bar, parity)) return;
+    const long long t0 = clock64();
+    for (;;) {
+        if (mbar_try_wait_parked(bar, parity, 2000u)) return;
+        if (*abort_flag) return;
+        if (clock64() - t0 > kQuantWaitCycles) {
+            *abort_flag = 1;
+            if (status) atomicMax(status, (unsigned)kStatusTimeout);
+            return;
+        }
+    }
+}
+
 #endif  // __CUDACC__
 
 }  // namespace coreinfer
