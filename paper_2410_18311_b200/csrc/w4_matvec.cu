@@ -63,10 +63,32 @@ w4_quantize_kernel(const T* __restrict__ w, int N, int K, long long sn, long lon
 }
 
 // -------------------------------------------------------------------------------- matvec --
+// y[b, n] = sum over groups g of  s[n, g] sum_k x c + o[n, g] sum_k x : the inner sums run over the codes themselves on
+// mma.sync.m16n8k16 (16 output rows on the M side, up to 8 rows of x on the N side, codes as fp16
+// subnormals: quant4.cuh), the scales are factors of fp32 sums.  Bound by the bytes of the weights,
+// read once.  x enters as fp16 after a power-of-two scaling per row and group that puts the group's largest
+// entry into [2^13, 2^14) - exact for bf16 and fp16 x, two parts of 22 bits for fp32 - so that no value of x
+// is out of fp16's range.
+// One persistent CTA per SM: a producer warp streams its row tiles (16 rows, contiguous in memory) through a ring of
+// stages of 16 column blocks; 16 consumer warps take a block of 128 columns of each stage, and their
+// sums meet in shared memory at the end of a row tile.  x is laid out once per CTA as MMA fragments
+// in shared memory; where it does not fit, the columns go in chunks (x laid out again per chunk and 32 row
+// tiles).
+constexpr int kW4Warps = 16;                // consumer warps = column blocks per stage
+constexpr int kW4Threads = 32 * (kW4Warps + 1);
+constexpr int kW4MaxStages = 8;
+constexpr int kW4TileGroup = 32;            // row tiles whose sums are kept over the chunks
+constexpr size_t kW4MaxX = 150 * 1024;      // bytes of x fragments and group factors
+
 struct W4Args {
     const uint8_t* codes;
-    const __half2* pairs;
-    int N, K, group, batch, act;
+    const uint8_t* pairs;
+    int N, K, batch, act;
+    int KB;                 // column blocks of 128
+    int chunk;              // column blocks per chunk of x
+    int tiles;              // row tiles
+    int stages;
+    int vec;                // rows of x are 16-byte aligned
     const void* x;
     const void* bias;
     const void* mul;
@@ -81,42 +103,278 @@ __device__ __forceinline__ float w4_act(float v, int act)
     return v;
 }
 
-// One warp per output and row of x.
-template <typename T, typename Y>
-__global__ void __launch_bounds__(256) w4_matvec_kernel(W4Args a)
+// Eight entries of a row of x from column k on, zeros beyond K.
+template <typename T>
+__device__ __forceinline__ void load_x8(const T* row, int k, int K, int vec, float (&v)[8])
 {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int n = blockIdx.x * 8 + warp, b = blockIdx.y;
-    if (n >= a.N) return;
-    const int KB = (a.K + 127) / 128, per = 128 / a.group;
-    const T* x = (const T*)a.x + (long long)b * a.ld_x;
-    float acc = 0.f;
-    for (int kb = 0; kb < KB; ++kb) {
-        const size_t tile = (size_t)(n >> 4) * KB + kb;
-        const uint8_t* row = a.codes + (tile * 16 + (n & 15)) * 64;
-        const unsigned unit = *reinterpret_cast<const uint16_t*>(row + unit_offset(lane * 4, 4));
-        const __half2 p = a.pairs[(tile * per + lane * 4 / a.group) * 16 + (n & 15)];
-        const float s = __low2float(p), o = __high2float(p);
+    if (vec && k + 8 <= K) {
+        T in[8];
+        *reinterpret_cast<uint4*>(in) = *reinterpret_cast<const uint4*>(row + k);
+        if (sizeof(T) == 4) reinterpret_cast<uint4*>(in)[1] = *reinterpret_cast<const uint4*>(row + k + 4);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int k = kb * 128 + lane * 4 + e;
-            if (k < a.K) acc = fmaf(to_f32<T>(x[k]), fmaf(s, (float)((unit >> (4 * e)) & 15u), o), acc);
-        }
-    }
+        for (int e = 0; e < 8; ++e) v[e] = to_f32<T>(in[e]);
+    } else {
 #pragma unroll
-    for (int d = 16; d; d >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, d);
-    if (lane == 0) {
-        if (a.bias) acc += to_f32<T>(((const T*)a.bias)[n]);
-        acc = w4_act(acc, a.act);
-        if (a.mul) acc *= to_f32<Y>(((const Y*)a.mul)[(long long)b * a.ld_mul + n]);
-        ((Y*)a.y)[(long long)b * a.ld_y + n] = from_f32<Y>(acc);
+        for (int e = 0; e < 8; ++e) v[e] = k + e < K ? to_f32<T>(row[k + e]) : 0.f;
     }
 }
 
-template <typename T, typename Y>
-static void launch_matvec(const W4Args& a, cudaStream_t st)
+// Lays columns [kb0, kb0 + nkb) of x out as B fragments: xs[block][32-value piece][column of the MMA][4 lanes] of 16 bytes,
+// and xg[group][row] = (2^(x - 14), sum of the group's entries).  A half-warp per block and row of x.
+template <typename T, int G>
+__device__ __forceinline__ void stage_x(const W4Args& a, int kb0, int nkb, uint4* xs, float2* xg, int tid)
 {
-    w4_matvec_kernel<T, Y><<<dim3((a.N + 7) / 8, a.batch), 256, 0, st>>>(a);
+    constexpr bool SPLIT = sizeof(T) == 4;
+    constexpr int PER = 128 / G, UNROLL = 2;
+    const int l16 = tid & 15, h = l16 >> 2, tig = l16 & 3, hw = tid >> 4;
+    const int slots = a.batch * (SPLIT ? 2 : 1), tasks = nkb * a.batch;
+    for (int base = hw & ~1; base < tasks; base += 2 * kW4Warps * UNROLL) {         // the same count for both halves of a warp
+        const int t0 = base | (hw & 1);
+        float v[UNROLL][8];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const int t = t0 + u * 2 * kW4Warps;
+            const int b = t / nkb, kb = t % nkb;
+            if (t < tasks) load_x8<T>((const T*)a.x + (long long)b * a.ld_x, (kb0 + kb) * 128 + h * 32 + tig * 8, a.K, a.vec, v[u]);
+            else
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[u][e] = 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const int t = t0 + u * 2 * kW4Warps;
+            const int b = t / nkb, kb = t % nkb;
+            float m = 0.f, sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                m = fmaxf(m, fabsf(v[u][e]));
+                sum += v[u][e];
+            }
+#pragma unroll
+            for (int d = 1; d < G / 8; d <<= 1) {            // within the half-warp: both halves take part
+                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+                sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            }
+            if (t >= tasks) continue;
+            const int x = range_exponent(m);
+            const float up = ldexpf(1.f, 14 - x), up16 = up * (1.f / 16.f);   // odd codes stand 16 times higher
+#pragma unroll
+            for (int part = 0; part < (SPLIT ? 2 : 1); ++part) {
+                uint4 f;
+                f.x = pack_half2(half_part(v[u][0] * up, part), half_part(v[u][4] * up, part));
+                f.y = pack_half2(half_part(v[u][2] * up, part), half_part(v[u][6] * up, part));
+                f.z = pack_half2(half_part(v[u][1] * up16, part), half_part(v[u][5] * up16, part));
+                f.w = pack_half2(half_part(v[u][3] * up16, part), half_part(v[u][7] * up16, part));
+                xs[((kb * 4 + h) * slots + (SPLIT ? 2 * b + part : b)) * 4 + tig] = f;
+            }
+            if ((l16 & (G / 8 - 1)) == 0) xg[(kb * PER + l16 / (G / 8)) * a.batch + b] = make_float2(ldexpf(1.f, x - 14), sum);
+        }
+    }
+}
+
+template <typename T, typename Y, int G>
+__global__ void __launch_bounds__(kW4Threads, 1) w4_matvec_kernel(const __grid_constant__ W4Args a)
+{
+    constexpr bool SPLIT = sizeof(T) == 4;
+    constexpr int PER = 128 / G;
+    constexpr uint32_t CODES = kW4Warps * 1024, STAGE = CODES + kW4Warps * PER * 64;
+    const int slots = a.batch * (SPLIT ? 2 : 1);
+    const int halves = SPLIT ? (a.batch + 3) / 4 : 1;        // MMAs of 8 columns: fp32 x of more than 4 rows takes two
+
+    extern __shared__ __align__(128) uint8_t smem[];
+    uint4* xs = reinterpret_cast<uint4*>(smem + (size_t)a.stages * STAGE);
+    float2* xg = reinterpret_cast<float2*>(xs + (size_t)a.chunk * 16 * slots);
+    float* red = reinterpret_cast<float*>(xg + (size_t)a.chunk * PER * a.batch);            // [2][16 warps][8][16]
+    float* ysum = red + 2 * kW4Warps * 128;                                                  // [tile group][8][16], with chunks
+    __shared__ uint64_t full_bar[kW4MaxStages], empty_bar[kW4MaxStages];
+    __shared__ int abort_s;
+    volatile int* abort_flag = &abort_s;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid == 0) {
+        for (int s = 0; s < a.stages; ++s) {
+            mbar_init(smem_u32(&full_bar[s]), 1);
+            mbar_init(smem_u32(&empty_bar[s]), kW4Warps);
+        }
+        abort_s = 0;
+        mbar_fence_init();
+    }
+    __syncthreads();
+    const int first = (int)((long long)blockIdx.x * a.tiles / gridDim.x), last = (int)((long long)(blockIdx.x + 1) * a.tiles / gridDim.x);
+    int s = 0;
+    uint32_t ph = 0;
+
+    if (warp == kW4Warps) {
+        // ---------------------------------------------------------------- producer --
+        if (lane == 0) {
+            for (int g0 = first; g0 < last && !*abort_flag; g0 += kW4TileGroup) {
+                const int g1 = g0 + kW4TileGroup < last ? g0 + kW4TileGroup : last;
+                for (int c0 = 0; c0 < a.KB && !*abort_flag; c0 += a.chunk) {
+                    const int c1 = c0 + a.chunk < a.KB ? c0 + a.chunk : a.KB;
+                    for (int tile = g0; tile < g1 && !*abort_flag; ++tile)
+                        for (int kb = c0; kb < c1; kb += kW4Warps) {
+                            bounded_wait(smem_u32(&empty_bar[s]), ph ^ 1u, abort_flag, nullptr);
+                            if (*abort_flag) break;
+                            const uint32_t n = c1 - kb < kW4Warps ? c1 - kb : kW4Warps;
+                            const size_t at = (size_t)tile * a.KB + kb;
+                            const uint32_t bar = smem_u32(&full_bar[s]), dst = smem_u32(smem + (size_t)s * STAGE);
+                            mbar_arrive_expect_tx(bar, n * (1024 + PER * 64));
+                            bulk_g2s(dst, a.codes + at * 1024, n * 1024, bar);
+                            bulk_g2s(dst + CODES, a.pairs + at * (PER * 64), n * PER * 64, bar);
+                            if (++s == a.stages) { s = 0; ph ^= 1u; }
+                        }
+                }
+            }
+        }
+    } else {
+        // --------------------------------------------------------------- consumers --
+        const int gid = lane >> 2, tig = lane & 3;
+        int par = 0;
+        for (int g0 = first; g0 < last; g0 += kW4TileGroup) {
+            const int g1 = g0 + kW4TileGroup < last ? g0 + kW4TileGroup : last;
+            for (int c0 = 0; c0 < a.KB; c0 += a.chunk) {
+                const int c1 = c0 + a.chunk < a.KB ? c0 + a.chunk : a.KB;
+                if (g0 == first || a.chunk < a.KB) {
+                    if (c0 > 0 || g0 > first) named_bar_sync(1, 32 * kW4Warps);      // the last chunk's use is over
+                    stage_x<T, G>(a, c0, c1 - c0, xs, xg, tid);
+                    named_bar_sync(1, 32 * kW4Warps);
+                }
+                for (int tile = g0; tile < g1; ++tile) {
+                    float y[2][4];                           // [MMA of 8 columns][rows gid, gid + 8 x two columns]
+#pragma unroll
+                    for (int m = 0; m < 2; ++m)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) y[m][e] = 0.f;
+                    for (int kb0 = c0; kb0 < c1; kb0 += kW4Warps) {
+                        bounded_wait(smem_u32(&full_bar[s]), ph, abort_flag, nullptr);
+                        const int kb = kb0 + warp - c0;      // within the chunk
+                        if (kb < c1 - c0) {
+                            const uint8_t* st = smem + (size_t)s * STAGE;
+                            const uint4 r0 = *reinterpret_cast<const uint4*>(st + warp * 1024 + gid * 64 + tig * 16);
+                            const uint4 r1 = *reinterpret_cast<const uint4*>(st + warp * 1024 + 512 + gid * 64 + tig * 16);
+                            const uint32_t w0[4] = {r0.x, r0.y, r0.z, r0.w}, w1[4] = {r1.x, r1.y, r1.z, r1.w};
+                            const __half2* pr = reinterpret_cast<const __half2*>(st + CODES + warp * (PER * 64));
+#pragma unroll
+                            for (int g = 0; g < PER; ++g) {
+                                float acc[2][4];
+#pragma unroll
+                                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) acc[m][e] = 0.f;
+#pragma unroll
+                                for (int j = g * G / 32; j < (g + 1) * G / 32; ++j) {
+                                    const uint32_t x0 = __byte_perm(w0[j / 2], w0[2 + j / 2], j & 1 ? 0x7632 : 0x5410);
+                                    const uint32_t x1 = __byte_perm(w1[j / 2], w1[2 + j / 2], j & 1 ? 0x7632 : 0x5410);
+                                    const uint32_t y0 = x0 >> 8, y1 = x1 >> 8;
+                                    const uint4* xf = xs + (size_t)(kb * 4 + j) * slots * 4;
+#pragma unroll
+                                    for (int m = 0; m < (SPLIT ? 2 : 1); ++m) {
+                                        if (m == 1 && halves == 1) break;
+                                        uint4 f = make_uint4(0u, 0u, 0u, 0u);
+                                        if (m * 8 + gid < slots) f = xf[(m * 8 + gid) * 4 + tig];
+                                        mma_16816(acc[m], x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, f.x, f.y);
+                                        mma_16816(acc[m], x0 & 0x00f000f0u, x1 & 0x00f000f0u, y0 & 0x00f000f0u, y1 & 0x00f000f0u, f.z, f.w);
+                                    }
+                                }
+                                const float2 p0 = __half22float2(pr[g * 16 + gid]), p1 = __half22float2(pr[g * 16 + gid + 8]);
+                                const float s0 = p0.x * kCodeScaleLow, s1 = p1.x * kCodeScaleLow;
+                                const float2* gx = xg + (size_t)(kb * PER + g) * a.batch;
+#pragma unroll
+                                for (int m = 0; m < (SPLIT ? 2 : 1); ++m) {
+                                    if (m == 1 && halves == 1) break;
+                                    if (SPLIT) {             // the two parts of a row of x stand in neighbouring columns
+                                        const int b = m * 4 + tig;
+                                        const float2 e = gx[b < a.batch ? b : 0];
+                                        y[m][0] = fmaf(s0 * (acc[m][0] + acc[m][1]), e.x, fmaf(p0.y, e.y, y[m][0]));
+                                        y[m][2] = fmaf(s1 * (acc[m][2] + acc[m][3]), e.x, fmaf(p1.y, e.y, y[m][2]));
+                                    } else {
+#pragma unroll
+                                        for (int i = 0; i < 2; ++i) {
+                                            const int b = 2 * tig + i;
+                                            const float2 e = gx[b < a.batch ? b : 0];
+                                            y[m][i] = fmaf(s0 * acc[m][i], e.x, fmaf(p0.y, e.y, y[m][i]));
+                                            y[m][2 + i] = fmaf(s1 * acc[m][2 + i], e.x, fmaf(p1.y, e.y, y[m][2 + i]));
+                                        }
+                                    }
+                                }
+                            }
+                        }
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(&empty_bar[s]));
+                        if (++s == a.stages) { s = 0; ph ^= 1u; }
+                    }
+                    // the warps' sums, [row of x][output row]; the other buffer may still be read for the tile before
+                    float* buf = red + (size_t)par * kW4Warps * 128;
+                    par ^= 1;
+#pragma unroll
+                    for (int m = 0; m < (SPLIT ? 2 : 1); ++m)
+#pragma unroll
+                        for (int i = 0; i < (SPLIT ? 1 : 2); ++i) {
+                            const int b = SPLIT ? m * 4 + tig : 2 * tig + i;
+                            buf[warp * 128 + b * 16 + gid] = y[m][i];
+                            buf[warp * 128 + b * 16 + gid + 8] = y[m][2 + i];
+                        }
+                    named_bar_sync(1, 32 * kW4Warps);
+                    if (tid < a.batch * 16) {
+                        float v = 0.f;
+#pragma unroll
+                        for (int w = 0; w < kW4Warps; ++w) v += buf[w * 128 + tid];
+                        const int b = tid >> 4, n = tile * 16 + (tid & 15);
+                        if (a.chunk < a.KB) {
+                            float* keep = ysum + (tile - g0) * 128 + tid;
+                            if (c0 > 0) v += *keep;
+                            *keep = v;
+                        }
+                        if (c1 == a.KB && n < a.N) {
+                            if (a.bias) v += to_f32<T>(((const T*)a.bias)[n]);
+                            v = w4_act(v, a.act);
+                            if (a.mul) v *= to_f32<Y>(((const Y*)a.mul)[(long long)b * a.ld_mul + n]);
+                            if (*abort_flag) v = __int_as_float(0x7fffffff);         // no sum of what did not arrive
+                            ((Y*)a.y)[(long long)b * a.ld_y + n] = from_f32<Y>(v);
+                        }
+                    }
+                }
+            }
+        }
+    }
+    __syncthreads();
+    if (tid == 0 && *abort_flag) {
+        // after a wait that gave up copies may be in flight: give them a bounded time to land
+        const long long t0 = clock64();
+        while (clock64() - t0 < 20000000LL) __nanosleep(1000);
+    }
+    __syncthreads();
+}
+
+template <typename T, typename Y, int G>
+static coreinfer_status launch_group(W4Args& a, const DeviceInfo& di, cudaStream_t st)
+{
+    constexpr int PER = 128 / G;
+    constexpr size_t STAGE = (size_t)kW4Warps * (1024 + PER * 64);
+    const int slots = a.batch * (sizeof(T) == 4 ? 2 : 1);
+    const size_t per_block = (size_t)slots * 256 + (size_t)PER * a.batch * sizeof(float2);
+    a.chunk = a.KB;
+    if (a.chunk * per_block > kW4MaxX) a.chunk = (int)(kW4MaxX / per_block) / kW4Warps * kW4Warps;
+    const size_t fixed = a.chunk * per_block + 2 * kW4Warps * 128 * sizeof(float) +
+                         (a.chunk < a.KB ? (size_t)kW4TileGroup * 128 * sizeof(float) : 0);
+    const size_t room = (size_t)di.smem_optin - 1024;
+    int stages = (int)((room - fixed) / STAGE);
+    if (stages > kW4MaxStages) stages = kW4MaxStages;
+    if (room < fixed || stages < 2) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "not enough shared memory for two pipeline stages");
+    a.stages = stages;
+    const size_t smem = fixed + stages * STAGE;
+    auto kernel = w4_matvec_kernel<T, Y, G>;
+    CI_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    kernel<<<a.tiles < di.sm_count ? a.tiles : di.sm_count, kW4Threads, smem, st>>>(a);
+    CI_CUDA(cudaGetLastError());
+    return COREINFER_OK;
+}
+
+template <typename T, typename Y>
+static coreinfer_status launch_matvec(W4Args& a, int group, const DeviceInfo& di, cudaStream_t st)
+{
+    if (group == 32) return launch_group<T, Y, 32>(a, di, st);
+    if (group == 64) return launch_group<T, Y, 64>(a, di, st);
+    return launch_group<T, Y, 128>(a, di, st);
 }
 
 }  // namespace coreinfer
@@ -190,12 +448,14 @@ coreinfer_status coreinfer_w4_matvec(const coreinfer_w4_matrix* w, const void* x
     cudaStream_t st = (cudaStream_t)cuda_stream;
     W4Args a;
     a.codes = (const uint8_t*)w->codes;
-    a.pairs = (const __half2*)w->pairs;
+    a.pairs = (const uint8_t*)w->pairs;
     a.N = w->N;
     a.K = w->K;
-    a.group = w->group;
+    a.KB = (int)w4_blocks128(w->K);
+    a.tiles = (int)w4_rows16(w->N);
     a.batch = batch;
     a.act = (int)act;
+    a.vec = aligned16(x) && (ld_x * (int64_t)xe) % 16 == 0;
     a.x = x;
     a.bias = bias;
     a.mul = mul;
@@ -203,16 +463,12 @@ coreinfer_status coreinfer_w4_matvec(const coreinfer_w4_matrix* w, const void* x
     a.ld_x = ld_x;
     a.ld_mul = ld_mul;
     a.ld_y = ld_y;
-    if (dtype == COREINFER_F32) launch_matvec<float, float>(a, st);
-    else if (dtype == COREINFER_BF16) {
-        if (y_dtype == COREINFER_F32) launch_matvec<__nv_bfloat16, float>(a, st);
-        else launch_matvec<__nv_bfloat16, __nv_bfloat16>(a, st);
-    } else {
-        if (y_dtype == COREINFER_F32) launch_matvec<__half, float>(a, st);
-        else launch_matvec<__half, __half>(a, st);
-    }
-    CI_CUDA(cudaGetLastError());
-    return COREINFER_OK;
+    if (dtype == COREINFER_F32) return launch_matvec<float, float>(a, w->group, di, st);
+    if (dtype == COREINFER_BF16)
+        return y_dtype == COREINFER_F32 ? launch_matvec<__nv_bfloat16, float>(a, w->group, di, st)
+                                        : launch_matvec<__nv_bfloat16, __nv_bfloat16>(a, w->group, di, st);
+    return y_dtype == COREINFER_F32 ? launch_matvec<__half, float>(a, w->group, di, st)
+                                    : launch_matvec<__half, __half>(a, w->group, di, st);
 }
 
 }  // extern "C"
