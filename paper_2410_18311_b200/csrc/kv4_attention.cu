@@ -26,7 +26,9 @@
 
 namespace coreinfer {
 
-constexpr int kAttnTile = 128;              // slots per stage
+// Slots per stage: two pieces of 16 per warp, so that waits, votes and addresses are paid once per 32 slots; one piece
+// where two stages of that size do not fit beside the join buffer (head_dim 256, and 128 in groups of 32).
+template <int D, int G> constexpr int kAttnTile = D == 256 || (D == 128 && G == 32) ? 128 : 256;
 constexpr int kAttnWarps = 8;
 constexpr int kAttnThreads = 32 * kAttnWarps;
 constexpr int kAttnMaxStages = 8;
@@ -45,6 +47,7 @@ struct AttnArgs {
     int RB;                 // units per (sequence, key head)
     int n_ctas;             // CTAs of the main kernel
     int stages;
+    int tile;               // slots per stage
     float scale;
     int accumulate;
     unsigned* status;
@@ -54,7 +57,7 @@ struct AttnArgs {
     float* logits;          // [B][H][R][cap], base-2 logits; only with accumulate
 };
 
-__device__ __forceinline__ int attn_tiles(int len) { return (len + kAttnTile - 1) / kAttnTile; }
+__device__ __forceinline__ int attn_tiles(int len, int tile) { return (len + tile - 1) / tile; }
 // CTA i of n takes the tiles from attn_start(i) to attn_start(i + 1), n at most the number of tiles, so that each
 // CTA has one at least; attn_owner is the CTA of tile t.
 __device__ __forceinline__ int attn_ctas(int n_ctas, int total) { return total < n_ctas ? total : n_ctas; }
@@ -91,13 +94,19 @@ struct Cursor {
     int b, hr, tile, nt;
 };
 
-template <typename T, int D, int G, bool SPLIT>
+// How query rows sit in the 8 columns of an MMA: a row per column; a row per two columns with the second empty
+// (up to 4 rows: half the softmax work per lane); a row per two columns, the second for the low part.
+enum { kRows8 = 0, kRows4 = 1, kRows4Parts = 2 };
+
+template <typename T, int D, int G, int MODE>
 __global__ void __launch_bounds__(kAttnThreads, D <= 128 ? 2 : 1)
 kv4_attention_kernel(const __grid_constant__ AttnArgs a)
 {
-    constexpr int H32 = D / 32, NG = D / G, RPT = SPLIT ? 4 : 8, NV = SPLIT ? 1 : 2;
+    constexpr bool PARTS = MODE == kRows4Parts, WIDE = MODE != kRows8;
+    constexpr int H32 = D / 32, NG = D / G, RPT = WIDE ? 4 : 8, NV = WIDE ? 1 : 2, TILE = kAttnTile<D, G>;
+    constexpr int UN = TILE / (16 * kAttnWarps);             // pieces of 16 slots per step of a warp
     constexpr uint32_t CODE_ROW = D / 2, PAIR_ROW = NG * 4;
-    constexpr uint32_t CODE_TILE = kAttnTile * CODE_ROW, PAIR_TILE = kAttnTile * PAIR_ROW;
+    constexpr uint32_t CODE_TILE = TILE * CODE_ROW, PAIR_TILE = TILE * PAIR_ROW;
     constexpr uint32_t STAGE = 2 * (CODE_TILE + PAIR_TILE);
     const Kv4& c = a.c;
 
@@ -125,7 +134,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
         for (int b0 = 0; b0 < c.B; b0 += 32) {
             const int b = b0 + lane;
             const int len = b < c.B ? kv4_length(c, b) : 0;
-            const int v = attn_tiles(len);
+            const int v = attn_tiles(len, TILE);
             int incl = v;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -155,7 +164,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
             if (pre[mid] * HR <= t) lo = mid; else hi = mid - 1;
         }
         k.b = lo;
-        k.nt = attn_tiles(lens[lo]);
+        k.nt = attn_tiles(lens[lo], TILE);
         const unsigned rem = (unsigned)(t - pre[lo] * HR);
         k.hr = (int)(rem / (unsigned)k.nt);
         k.tile = (int)(rem % (unsigned)k.nt);
@@ -163,10 +172,10 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
     };
     // One thread: the copies of a tile into stage s.
     auto fetch = [&](int b, int hr, int tile, int s) {
-        const int t0 = tile * kAttnTile;
+        const int t0 = tile * TILE;
         // whole 16-slot pieces: the capacity is a multiple of 16, so they lie within the buffers
         const int left = (lens[b] - t0 + 15) & ~15;
-        const uint32_t rows = left < kAttnTile ? left : kAttnTile;
+        const uint32_t rows = left < TILE ? left : TILE;
         const size_t slot = ((size_t)b * c.H + hr / a.RB) * c.cap + t0;
         const uint32_t bar = smem_u32(&full_bar[s]), dst = smem_u32(smem + (size_t)s * STAGE);
         mbar_arrive_expect_tx(bar, 2 * rows * (CODE_ROW + PAIR_ROW));
@@ -200,8 +209,8 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
             float qsum[NG][NV], f[NV];
             int lim[NV];                                     // slots this lane's columns see
             {
-                const int r = row0 + (SPLIT ? gid >> 1 : gid);
-                const bool valid = r < a.R;
+                const int r = row0 + (WIDE ? gid >> 1 : gid);
+                const bool valid = r < a.R && (MODE != kRows4 || (gid & 1) == 0);
                 const T* src = (const T*)a.q + ((long long)b * a.T + (valid ? r / a.share : 0)) * a.ld_q +
                                (long long)(h * a.share + (valid ? r % a.share : 0)) * D + 8 * tig;
                 float v[H32][8], m = 0.f;
@@ -231,7 +240,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                         v[j][e] *= up;
                         gs[j * 32 / G] += v[j][e];
                     }
-                    const int low = SPLIT ? gid & 1 : 0;
+                    const int low = PARTS ? gid & 1 : 0;
                     const float lo16 = 1.f / 16.f;           // odd codes stand 16 times higher
                     qf[j][0] = pack_half2(half_part(v[j][0], low), half_part(v[j][4], low));
                     qf[j][1] = pack_half2(half_part(v[j][2], low), half_part(v[j][6], low));
@@ -252,15 +261,15 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
 #pragma unroll
                     for (int g = 0; g < NG; ++g) qsum[g][i] = __shfl_sync(0xffffffffu, gs[g], from);
                     f[i] = __shfl_sync(0xffffffffu, ff, from);
-                    const int rr = row0 + (SPLIT ? tig : 2 * tig + i);
+                    const int rr = row0 + (WIDE ? tig : 2 * tig + i);
                     lim[i] = rr < a.R ? len - (a.T - 1 - rr / a.share) : 0;
                 }
             }
-            float* lg[NV];
+            float* lg[NV];                                   // this lane's logits, NULL where none are kept
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int rr = row0 + (SPLIT ? tig : 2 * tig + i);
-                lg[i] = a.accumulate && rr < a.R ? a.logits + (((size_t)b * c.H + h) * a.R + rr) * c.cap : nullptr;
+                const int rr = row0 + (WIDE ? tig : 2 * tig + i);
+                lg[i] = a.accumulate && rr < a.R ? a.logits + (((size_t)b * c.H + h) * a.R + rr) * c.cap + tok0 : nullptr;
             }
             const int all_see = len - (a.T - 1);             // slots below this are seen by every row
 
@@ -281,7 +290,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
             }
 
             for (int it = 0; it < n_tiles; ++it) {
-                const int t0 = (first_tile + it) * kAttnTile;
+                const int t0 = (first_tile + it) * TILE;
                 const int refill = t + it - 1 + a.stages;    // goes where tile t + it - 1 was
                 if (warp == ((t + it) & (kAttnWarps - 1)) && lane == 0 && t + it > begin && refill < end) {
                     bounded_wait(smem_u32(&empty_bar[prev]), prev_ph, abort_flag, a.status);
@@ -297,95 +306,100 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                 __syncwarp();
                 bounded_wait(smem_u32(&full_bar[s]), ph, abort_flag, a.status);
                 const uint8_t* st = smem + (size_t)s * STAGE;
-                for (int sub = sg; sub < kAttnTile / 16; sub += nsg) {
+                for (int sub = UN * sg; sub < TILE / 16; sub += UN * nsg) {
                     const int n0 = t0 + sub * 16;
                     if (n0 >= len) break;
-                    // ---- logits: S^T [16 slots][8 columns] ----
-                    const uint8_t* krow = st + (sub * 16 + tok0) * CODE_ROW + tig * (D / 8);
-                    uint32_t w0[D / 32], w1[D / 32], kp0[NG], kp1[NG];
-                    ld_words<D / 32>(w0, krow);
-                    ld_words<D / 32>(w1, krow + 8 * CODE_ROW);
-                    const uint8_t* kpr = st + CODE_TILE + (sub * 16 + tok0) * PAIR_ROW;
-                    ld_words<NG>(kp0, kpr);
-                    ld_words<NG>(kp1, kpr + 8 * PAIR_ROW);
-                    float lo0[NV], lo1[NV];                  // slots tok0 and tok0 + 8
+                    // ---- logits: S^T [UN][16 slots][8 columns]; lo[u][v]: slot n0 + 16 u + 8 v + tok0 ----
+                    float lo[UN][2][NV];
 #pragma unroll
-                    for (int i = 0; i < NV; ++i) lo0[i] = lo1[i] = 0.f;
+                    for (int u = 0; u < UN; ++u) {
+                        const uint8_t* krow = st + (sub * 16 + u * 16 + tok0) * CODE_ROW + tig * (D / 8);
+                        uint32_t w0[D / 32], w1[D / 32], kp0[NG], kp1[NG];
+                        ld_words<D / 32>(w0, krow);
+                        ld_words<D / 32>(w1, krow + 8 * CODE_ROW);
+                        const uint8_t* kpr = st + CODE_TILE + (sub * 16 + u * 16 + tok0) * PAIR_ROW;
+                        ld_words<NG>(kp0, kpr);
+                        ld_words<NG>(kp1, kpr + 8 * PAIR_ROW);
 #pragma unroll
-                    for (int g = 0; g < NG; ++g) {
-                        float acc[4] = {0.f, 0.f, 0.f, 0.f};
+                        for (int g = 0; g < NG; ++g) {
+                            float acc[4];
 #pragma unroll
-                        for (int j = g * G / 32; j < (g + 1) * G / 32; ++j) {
-                            const uint32_t x0 = __byte_perm(w0[j / 2], w0[H32 / 2 + j / 2], j & 1 ? 0x7632 : 0x5410);
-                            const uint32_t x1 = __byte_perm(w1[j / 2], w1[H32 / 2 + j / 2], j & 1 ? 0x7632 : 0x5410);
-                            const uint32_t y0 = x0 >> 8, y1 = x1 >> 8;
-                            mma_16816(acc, x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, qf[j][0], qf[j][1]);
-                            mma_16816(acc, x0 & 0x00f000f0u, x1 & 0x00f000f0u, y0 & 0x00f000f0u, y1 & 0x00f000f0u, qf[j][2], qf[j][3]);
-                        }
-                        const float2 p0 = pair_f32(kp0[g]), p1 = pair_f32(kp1[g]);
-                        if (SPLIT) {
-                            lo0[0] = fmaf(p0.x, acc[0] + acc[1], fmaf(p0.y, qsum[g][0], lo0[0]));
-                            lo1[0] = fmaf(p1.x, acc[2] + acc[3], fmaf(p1.y, qsum[g][0], lo1[0]));
-                        } else {
+                            for (int j = g * G / 32; j < (g + 1) * G / 32; ++j) {
+                                const uint32_t x0 = __byte_perm(w0[j / 2], w0[H32 / 2 + j / 2], j & 1 ? 0x7632 : 0x5410);
+                                const uint32_t x1 = __byte_perm(w1[j / 2], w1[H32 / 2 + j / 2], j & 1 ? 0x7632 : 0x5410);
+                                const uint32_t y0 = x0 >> 8, y1 = x1 >> 8;
+                                if (j == g * G / 32)
+                                    mma_16816_zero(acc, x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, qf[j][0], qf[j][1]);
+                                else
+                                    mma_16816(acc, x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, qf[j][0], qf[j][1]);
+                                mma_16816(acc, x0 & 0x00f000f0u, x1 & 0x00f000f0u, y0 & 0x00f000f0u, y1 & 0x00f000f0u, qf[j][2], qf[j][3]);
+                            }
+                            const float2 p0 = pair_f32(kp0[g]), p1 = pair_f32(kp1[g]);
 #pragma unroll
                             for (int i = 0; i < NV; ++i) {
-                                lo0[i] = fmaf(p0.x, acc[i], fmaf(p0.y, qsum[g][i], lo0[i]));
-                                lo1[i] = fmaf(p1.x, acc[2 + i], fmaf(p1.y, qsum[g][i], lo1[i]));
+                                const float a0 = PARTS ? acc[0] + acc[1] : acc[i], a1 = PARTS ? acc[2] + acc[3] : acc[2 + i];
+                                const float o0 = p0.y * qsum[g][i], o1 = p1.y * qsum[g][i];
+                                lo[u][0][i] = fmaf(p0.x, a0, g ? lo[u][0][i] + o0 : o0);
+                                lo[u][1][i] = fmaf(p1.x, a1, g ? lo[u][1][i] + o1 : o1);
                             }
                         }
                     }
-                    const int na = n0 + tok0, nb = na + 8;
-                    const bool edge = n0 + 16 > all_see;     // some row does not see some slot
+                    const int na = n0 + tok0;
+                    const bool edge = n0 + 16 * UN > all_see;     // some row does not see some slot
+                    float most[NV];
 #pragma unroll
                     for (int i = 0; i < NV; ++i) {
-                        lo0[i] *= f[i];
-                        lo1[i] *= f[i];
-                        if (edge) {
-                            if (na >= lim[i]) lo0[i] = -__int_as_float(0x7f800000);
-                            if (nb >= lim[i]) lo1[i] = -__int_as_float(0x7f800000);
-                        }
+#pragma unroll
+                        for (int u = 0; u < UN; ++u)
+#pragma unroll
+                            for (int v = 0; v < 2; ++v) {
+                                lo[u][v][i] *= f[i];
+                                if (edge && na + 16 * u + 8 * v >= lim[i]) lo[u][v][i] = -__int_as_float(0x7f800000);
+                            }
+                        most[i] = fmaxf(lo[0][0][i], lo[0][1][i]);
+#pragma unroll
+                        for (int u = 1; u < UN; ++u) most[i] = fmaxf(most[i], fmaxf(lo[u][0][i], lo[u][1][i]));
                         if (lg[i]) {
-                            if (na < lim[i]) lg[i][na] = lo0[i];
-                            if (nb < lim[i]) lg[i][nb] = lo1[i];
+                            float* to = lg[i] + n0;
+#pragma unroll
+                            for (int u = 0; u < UN; ++u)
+#pragma unroll
+                                for (int v = 0; v < 2; ++v)
+                                    if (!edge || na + 16 * u + 8 * v < lim[i]) to[16 * u + 8 * v] = lo[u][v][i];
                         }
                     }
                     // ---- value pairs, running maximum ----
-                    const uint8_t* vpr = st + 2 * CODE_TILE + PAIR_TILE + (sub * 16 + tok0) * PAIR_ROW;
-                    uint32_t vp0[NG], vp1[NG];
-                    ld_words<NG>(vp0, vpr);
-                    ld_words<NG>(vp1, vpr + 8 * PAIR_ROW);
-                    if (edge) {                              // what lies beyond the sequence is never used
+                    uint32_t vp[UN][2][NG];
+                    __half2 smax = __float2half2_rn(0.f);
 #pragma unroll
-                        for (int g = 0; g < NG; ++g) {
-                            if (na >= len) vp0[g] = 0u;
-                            if (nb >= len) vp1[g] = 0u;
+                    for (int u = 0; u < UN; ++u)
+#pragma unroll
+                        for (int v = 0; v < 2; ++v) {
+                            ld_words<NG>(vp[u][v], st + 2 * CODE_TILE + PAIR_TILE + (sub * 16 + 16 * u + 8 * v + tok0) * PAIR_ROW);
+#pragma unroll
+                            for (int g = 0; g < NG; ++g) {
+                                if (edge && na + 16 * u + 8 * v >= len) vp[u][v][g] = 0u;     // never used
+                                smax = __hmax2(smax, *reinterpret_cast<const __half2*>(&vp[u][v][g]));
+                            }
                         }
-                    }
-                    float smax = 0.f;
-                    float2 v0[NG], v1[NG];
+                    float s_here = __low2float(smax);
+                    bool change = s_here > s_most;
 #pragma unroll
-                    for (int g = 0; g < NG; ++g) {
-                        v0[g] = pair_f32(vp0[g]);
-                        v1[g] = pair_f32(vp1[g]);
-                        smax = fmaxf(smax, fmaxf(v0[g].x, v1[g].x));
-                    }
-                    bool change = smax > s_most;
-#pragma unroll
-                    for (int i = 0; i < NV; ++i) change |= fmaxf(lo0[i], lo1[i]) > mx[i];
+                    for (int i = 0; i < NV; ++i) change |= most[i] > mx[i];
                     if (__any_sync(0xffffffffu, change)) {
                         float e_new = E;
-                        if (__any_sync(0xffffffffu, smax > s_most)) {
+                        if (__any_sync(0xffffffffu, s_here > s_most)) {
 #pragma unroll
-                            for (int d = 1; d < 32; d <<= 1) smax = fmaxf(smax, __shfl_xor_sync(0xffffffffu, smax, d));
+                            for (int d = 1; d < 32; d <<= 1) s_here = fmaxf(s_here, __shfl_xor_sync(0xffffffffu, s_here, d));
                             int x;
-                            frexpf(smax, &x);
-                            x = smax > 0.f ? (x < -15 ? -15 : x) : -15;
+                            frexpf(s_here, &x);
+                            x = s_here > 0.f ? (x < -15 ? -15 : x) : -15;
                             e_new = (float)(9 - x);
                             s_most = ldexpf(1.f, x + 5);     // room for scales up to 32 times larger before E moves
                         }
 #pragma unroll
                         for (int i = 0; i < NV; ++i) {
-                            float m = fmaxf(lo0[i], lo1[i]);
+                            float m = most[i];
                             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
                             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
                             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
@@ -401,7 +415,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                                 for (int e = 0; e < 2; ++e) {
                                     o[j][e][i] *= corr;
                                     o[j][e][2 + i] *= corr;
-                                    if (SPLIT) {
+                                    if (PARTS) {
                                         o[j][e][1] *= corr;
                                         o[j][e][3] *= corr;
                                     }
@@ -409,51 +423,57 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                         }
                         E = e_new;
                     }
-                    float p0[NV], p1[NV];
 #pragma unroll
                     for (int i = 0; i < NV; ++i) {
                         const float ref = mx[i] - E;
-                        p0[i] = exp2_fast(lo0[i] - ref);
-                        p1[i] = exp2_fast(lo1[i] - ref);
-                        l[i] += p0[i] + p1[i];
+#pragma unroll
+                        for (int u = 0; u < UN; ++u)
+#pragma unroll
+                            for (int v = 0; v < 2; ++v) {
+                                lo[u][v][i] = exp2_fast(lo[u][v][i] - ref);          // p from here on
+                                l[i] += lo[u][v][i];
+                            }
                     }
                     // ---- O^T += V^T P^T, per group of scales ----
-                    const uint8_t* vrow = st + CODE_TILE + PAIR_TILE + (sub * 16 + tig) * CODE_ROW + gid * (D / 16);
-                    uint32_t va[H32 / 2], vb[H32 / 2], vc[H32 / 2], vd[H32 / 2];
-                    ld_words<H32 / 2>(va, vrow);
-                    ld_words<H32 / 2>(vb, vrow + 4 * CODE_ROW);
-                    ld_words<H32 / 2>(vc, vrow + 8 * CODE_ROW);
-                    ld_words<H32 / 2>(vd, vrow + 12 * CODE_ROW);
 #pragma unroll
-                    for (int g = 0; g < NG; ++g) {
-                        uint32_t b0, b1;
-                        float ps0[NV], ps1[NV];
+                    for (int u = 0; u < UN; ++u) {
+                        const uint8_t* vrow = st + CODE_TILE + PAIR_TILE + (sub * 16 + u * 16 + tig) * CODE_ROW + gid * (D / 16);
+                        uint32_t va[H32 / 2], vb[H32 / 2], vc[H32 / 2], vd[H32 / 2];
+                        ld_words<H32 / 2>(va, vrow);
+                        ld_words<H32 / 2>(vb, vrow + 4 * CODE_ROW);
+                        ld_words<H32 / 2>(vc, vrow + 8 * CODE_ROW);
+                        ld_words<H32 / 2>(vd, vrow + 12 * CODE_ROW);
 #pragma unroll
-                        for (int i = 0; i < NV; ++i) {
-                            ps0[i] = p0[i] * v0[g].x;
-                            ps1[i] = p1[i] * v1[g].x;
-                            float po0 = p0[i] * v0[g].y, po1 = p1[i] * v1[g].y;
-                            if (edge) {                      // a slot a row does not see adds nothing, whatever it holds
-                                if (na >= lim[i]) ps0[i] = po0 = 0.f;
-                                if (nb >= lim[i]) ps1[i] = po1 = 0.f;
+                        for (int g = 0; g < NG; ++g) {
+                            uint32_t bf[2];
+#pragma unroll
+                            for (int v = 0; v < 2; ++v) {
+                                const float2 so = pair_f32(vp[u][v][g]);
+                                float ps[NV];
+#pragma unroll
+                                for (int i = 0; i < NV; ++i) {
+                                    ps[i] = lo[u][v][i] * so.x;
+                                    if (edge && na + 16 * u + 8 * v >= lim[i]) {     // adds nothing, whatever the slot holds
+                                        ps[i] = 0.f;
+                                    } else {
+                                        om[g][i] = fmaf(lo[u][v][i], so.y, om[g][i]);
+                                    }
+                                }
+                                if (PARTS) {
+                                    const float high = __half2float(__float2half_rn(ps[0]));
+                                    bf[v] = movmatrix_trans(pack_half2(high, ps[0] - high));
+                                } else {
+                                    bf[v] = movmatrix_trans(pack_half2(ps[0], WIDE ? 0.f : ps[NV - 1]));
+                                }
                             }
-                            om[g][i] += po0 + po1;
-                        }
-                        if (SPLIT) {
-                            const float h0 = __half2float(__float2half_rn(ps0[0])), h1 = __half2float(__float2half_rn(ps1[0]));
-                            b0 = movmatrix_trans(pack_half2(h0, ps0[0] - h0));
-                            b1 = movmatrix_trans(pack_half2(h1, ps1[0] - h1));
-                        } else {
-                            b0 = movmatrix_trans(pack_half2(ps0[0], ps0[NV - 1]));
-                            b1 = movmatrix_trans(pack_half2(ps1[0], ps1[NV - 1]));
-                        }
 #pragma unroll
-                        for (int j = g * G / 32; j < (g + 1) * G / 32; ++j) {
-                            const uint32_t x = __byte_perm(va[j / 2], vb[j / 2], j & 1 ? 0x7632 : 0x5410);
-                            const uint32_t y = __byte_perm(vc[j / 2], vd[j / 2], j & 1 ? 0x7632 : 0x5410);
-                            const uint32_t x8 = x >> 8, y8 = y >> 8;
-                            mma_16816(o[j][0], x & 0x000f000fu, x8 & 0x000f000fu, y & 0x000f000fu, y8 & 0x000f000fu, b0, b1);
-                            mma_16816(o[j][1], x & 0x00f000f0u, x8 & 0x00f000f0u, y & 0x00f000f0u, y8 & 0x00f000f0u, b0, b1);
+                            for (int j = g * G / 32; j < (g + 1) * G / 32; ++j) {
+                                const uint32_t x = __byte_perm(va[j / 2], vb[j / 2], j & 1 ? 0x7632 : 0x5410);
+                                const uint32_t y = __byte_perm(vc[j / 2], vd[j / 2], j & 1 ? 0x7632 : 0x5410);
+                                const uint32_t x8 = x >> 8, y8 = y >> 8;
+                                mma_16816(o[j][0], x & 0x000f000fu, x8 & 0x000f000fu, y & 0x000f000fu, y8 & 0x000f000fu, bf[0], bf[1]);
+                                mma_16816(o[j][1], x & 0x00f000f0u, x8 & 0x00f000f0u, y & 0x00f000f0u, y8 & 0x00f000f0u, bf[0], bf[1]);
+                            }
                         }
                     }
                 }
@@ -474,13 +494,13 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
 #pragma unroll
                     for (int g = 0; g < NG; ++g) om[g][i] += __shfl_xor_sync(0xffffffffu, om[g][i], d);
                 }
-                const int r = SPLIT ? tig : 2 * tig + i;
+                const int r = WIDE ? tig : 2 * tig + i;
                 if (gid == 0) mlbuf[warp * RPT + r] = make_float2(mx[i] - E, l[i]);
 #pragma unroll
                 for (int j = 0; j < H32; ++j) {
                     const float add = om[j * 32 / G][i];
                     float4 v;
-                    if (SPLIT) {
+                    if (PARTS) {
                         v.x = o[j][0][0] + o[j][0][1];
                         v.y = o[j][1][0] + o[j][1][1];
                         v.z = o[j][0][2] + o[j][0][3];
@@ -580,14 +600,14 @@ __global__ void __launch_bounds__(kFinishThreads) kv4_finish_kernel(const __grid
     if ((int)blockIdx.x >= a.R && ((int)blockIdx.x - a.R) * kFinishSlots >= len) return;
     int before = 0, all = 0;
     for (int i = tid; i < c.B; i += kFinishThreads) {
-        const int n = attn_tiles(kv4_length(c, i));
+        const int n = attn_tiles(kv4_length(c, i), a.tile);
         all += n;
         if (i < b) before += n;
     }
     auto add = [](int x, int y) { return x + y; };
     before = finish_reduce(before, redi, add);
     all = finish_reduce(all, redi, add);
-    const int HR = c.H * a.RB, nt = attn_tiles(len), total = all * HR, n_ctas = attn_ctas(a.n_ctas, total);
+    const int HR = c.H * a.RB, nt = attn_tiles(len, a.tile), total = all * HR, n_ctas = attn_ctas(a.n_ctas, total);
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
     if ((int)blockIdx.x < a.R) {
@@ -670,24 +690,32 @@ __global__ void __launch_bounds__(kFinishThreads) kv4_finish_kernel(const __grid
         if (lane == 0) rows[r] = make_float2(top, sum == 0.f ? 0.f : 1.f / sum);
     }
     __syncthreads();
-    const int n0 = ((int)blockIdx.x - a.R) * kFinishSlots;
-    const float* lg = a.logits + ((size_t)b * c.H + h) * a.R * c.cap;
-    float* weight = c.weight + ((size_t)b * c.H + h) * c.cap;
-    for (int n = n0 + tid; n < n0 + kFinishSlots && n < len; n += kFinishThreads) {
-        float w = 0.f;
-        for (int r = 0; r < a.R; ++r)
-            if (n < len - (a.T - 1 - r / a.share)) w = fmaf(exp2_fast(lg[(size_t)r * c.cap + n] - rows[r].x), rows[r].y, w);
-        weight[n] += w;
+    // four slots a thread: the capacity is a multiple of 16, so they lie within a row of logits
+    const int n = ((int)blockIdx.x - a.R) * kFinishSlots + tid * 4;
+    if (n >= len) return;
+    const float* lg = a.logits + ((size_t)b * c.H + h) * a.R * c.cap + n;
+    float4* weight = reinterpret_cast<float4*>(c.weight + ((size_t)b * c.H + h) * c.cap + n);
+    float4 w = *weight;
+#pragma unroll 8
+    for (int r = 0; r < a.R; ++r) {
+        const float4 x = *reinterpret_cast<const float4*>(lg + (size_t)r * c.cap);
+        const float2 ml = rows[r];
+        const int see = len - (a.T - 1 - r / a.share) - n;  // slots of the four that the row sees
+        if (see > 0) w.x = fmaf(exp2_fast(x.x - ml.x), ml.y, w.x);
+        if (see > 1) w.y = fmaf(exp2_fast(x.y - ml.x), ml.y, w.y);
+        if (see > 2) w.z = fmaf(exp2_fast(x.z - ml.x), ml.y, w.z);
+        if (see > 3) w.w = fmaf(exp2_fast(x.w - ml.x), ml.y, w.w);
     }
+    *weight = w;
 }
 
 // -------------------------------------------------------------------------------- host --
 static inline size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Rows per unit and units per key head for R query rows.
-static void attn_rows(int R, bool split, int* RT, int* RU, int* RB)
+static void attn_rows(int R, int rpt, int* RT, int* RU, int* RB)
 {
-    const int rpt = split ? 4 : 8, tiles = (R + rpt - 1) / rpt;
+    const int tiles = (R + rpt - 1) / rpt;
     *RT = tiles > 4 ? 8 : (tiles > 2 ? 4 : tiles);
     *RU = *RT * rpt;
     *RB = (R + *RU - 1) / *RU;
@@ -696,10 +724,10 @@ static void attn_rows(int R, bool split, int* RT, int* RU, int* RB)
 struct AttnLayout {
     size_t ml, o, stats, logits, total;
 };
-static AttnLayout attn_layout(const Kv4& c, int R, bool split)
+static AttnLayout attn_layout(const Kv4& c, int R, int rpt)
 {
     int RT, RU, RB;
-    attn_rows(R, split, &RT, &RU, &RB);
+    attn_rows(R, rpt, &RT, &RU, &RB);
     AttnLayout w;
     w.ml = 256;
     w.o = w.ml + up256((size_t)kAttnMaxCtas * 2 * RU * sizeof(float2));
@@ -709,29 +737,33 @@ static AttnLayout attn_layout(const Kv4& c, int R, bool split)
     return w;
 }
 
-template <typename T, int D, int G>
-static coreinfer_status launch_attention(AttnArgs& a, const DeviceInfo& di, cudaStream_t st)
+template <typename T, int D, int G, int MODE>
+static coreinfer_status launch_mode(AttnArgs& a, const DeviceInfo& di, cudaStream_t st)
 {
-    constexpr bool SPLIT = sizeof(T) == 4 || std::is_same<T, __half>::value;
-    constexpr int RPT = SPLIT ? 4 : 8, NG = D / G;
-    constexpr size_t STAGE = (size_t)2 * kAttnTile * (D / 2 + NG * 4);
-    auto kernel = kv4_attention_kernel<T, D, G, SPLIT>;
-    const int per_sm = D <= 128 ? 2 : 1;
+    constexpr int RPT = MODE == kRows8 ? 8 : 4, NG = D / G, TILE = kAttnTile<D, G>;
+    constexpr size_t STAGE = (size_t)2 * TILE * (D / 2 + NG * 4);
     const size_t fixed = (size_t)kAttnWarps * RPT * (D * sizeof(float) + sizeof(float2)) + (2 * a.c.B + 1) * sizeof(int);
-    const size_t room = (size_t)di.smem_optin / per_sm - 2048;
-    int stages = (int)((room - fixed) / STAGE);
+    // two CTAs per SM where registers (head_dim up to 128) and two stages each allow it
+    int per_sm = D <= 128 ? 2 : 1, stages = 0;
+    for (; per_sm >= 1 && stages < 2; --per_sm) {
+        const size_t room = (smem_room(di) - (per_sm - 1) * 1024) / per_sm;
+        stages = room > fixed ? (int)((room - fixed) / STAGE) : 0;
+        if (stages >= 2) break;
+    }
+    if (stages < 2) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "not enough shared memory for two pipeline stages");
     if (stages > kAttnMaxStages) stages = kAttnMaxStages;
-    if (room < fixed || stages < 2) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "not enough shared memory for two pipeline stages");
     a.stages = stages;
+    a.tile = TILE;
     const size_t smem = fixed + stages * STAGE;
-    const long long tiles = (long long)a.c.B * a.c.H * a.RB * ((a.c.cap + kAttnTile - 1) / kAttnTile);
-    if (tiles > (1LL << 30)) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "the cache has %lld tiles of %d slots: too many for one call", tiles, kAttnTile);
+    const long long tiles = (long long)a.c.B * a.c.H * a.RB * ((a.c.cap + TILE - 1) / TILE);
+    if (tiles > (1LL << 30)) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "the cache has %lld tiles of %d slots: too many for one call", tiles, TILE);
     long long ctas = (long long)di.sm_count * per_sm;
     if (ctas > kAttnMaxCtas) ctas = kAttnMaxCtas;
     if (ctas > tiles) ctas = tiles;
     a.n_ctas = (int)ctas;
-    CI_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    kernel<<<a.n_ctas, kAttnThreads, smem, st>>>(a);
+    const coreinfer_status s = allow_smem<kv4_attention_kernel<T, D, G, MODE>>(di);
+    if (s != COREINFER_OK) return s;
+    kv4_attention_kernel<T, D, G, MODE><<<a.n_ctas, kAttnThreads, smem, st>>>(a);
     CI_CUDA(cudaGetLastError());
 
     cudaLaunchConfig_t cfg = {};
@@ -747,6 +779,19 @@ static coreinfer_status launch_attention(AttnArgs& a, const DeviceInfo& di, cuda
     cfg.numAttrs = 1;
     CI_CUDA(cudaLaunchKernelEx(&cfg, kv4_finish_kernel<T>, a));
     return COREINFER_OK;
+}
+
+// Rows per MMA tile for R query rows: fp32 and fp16 always carry two parts; bf16 takes the form with four rows where that
+// is enough.
+static inline int attn_rpt(coreinfer_dtype dtype, long long R) { return dtype != COREINFER_BF16 || R <= 4 ? 4 : 8; }
+
+template <typename T, int D, int G>
+static coreinfer_status launch_attention(AttnArgs& a, const DeviceInfo& di, cudaStream_t st)
+{
+    if constexpr (std::is_same<T, __nv_bfloat16>::value)
+        return a.R <= 4 ? launch_mode<T, D, G, kRows4>(a, di, st) : launch_mode<T, D, G, kRows8>(a, di, st);
+    else
+        return launch_mode<T, D, G, kRows4Parts>(a, di, st);
 }
 
 template <typename T>
@@ -776,7 +821,7 @@ size_t coreinfer_kv4_attention_workspace_bytes(const coreinfer_kv4_cache* cache,
     if (q_heads < 1 || T < 1 || q_heads % c.H != 0 || T > COREINFER_KV4_MAX_QUERIES) return 0;
     const long long R = (long long)(q_heads / c.H) * T;
     if (R > kAttnMaxRows) return 0;
-    const size_t x = attn_layout(c, (int)R, false).total, y = attn_layout(c, (int)R, true).total;
+    const size_t x = attn_layout(c, (int)R, 8).total, y = attn_layout(c, (int)R, 4).total;
     return x > y ? x : y;
 }
 
@@ -807,8 +852,8 @@ coreinfer_status coreinfer_kv4_attention(const coreinfer_kv4_cache* cache, const
     if (workspace_bytes < need) CI_FAIL(COREINFER_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
     DeviceInfo di;
     if ((s = device_info(&di)) != COREINFER_OK) return s;
-    const bool split = dtype != COREINFER_BF16;
-    const AttnLayout w = attn_layout(a.c, (int)R, split);
+    const int rpt = attn_rpt(dtype, R);
+    const AttnLayout w = attn_layout(a.c, (int)R, rpt);
     uint8_t* ws = (uint8_t*)workspace;
     a.q = q;
     a.out = out;
@@ -818,7 +863,7 @@ coreinfer_status coreinfer_kv4_attention(const coreinfer_kv4_cache* cache, const
     a.T = T;
     a.share = q_heads / a.c.H;
     a.R = (int)R;
-    attn_rows(a.R, split, &a.RT, &a.RU, &a.RB);
+    attn_rows(a.R, rpt, &a.RT, &a.RU, &a.RB);
     a.scale = scale;
     a.accumulate = accumulate ? 1 : 0;
     a.status = (unsigned*)ws;

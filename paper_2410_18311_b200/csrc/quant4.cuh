@@ -4,6 +4,8 @@
 
 #include "common.cuh"
 
+#include <atomic>
+
 namespace coreinfer {
 
 constexpr float kHalfMax = 65504.f;
@@ -12,6 +14,20 @@ static inline bool group_known(int g) { return g == 32 || g == 64 || g == 128; }
 static inline bool aligned_to(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
 #ifdef __CUDACC__
+
+// Dynamic shared memory that a kernel of this file's users may ask for: all but 1 KB for its static part.
+static inline size_t smem_room(const DeviceInfo& di) { return (size_t)di.smem_optin - 1024; }
+// Lets a kernel use that much; once per kernel and device, since the call costs about a microsecond of host time.
+template <auto Kernel>
+static coreinfer_status allow_smem(const DeviceInfo& di)
+{
+    static std::atomic<unsigned long long> done{0};
+    const unsigned long long bit = di.device >= 0 && di.device < 64 ? 1ull << di.device : 0ull;
+    if (done.load(std::memory_order_relaxed) & bit) return COREINFER_OK;
+    CI_CUDA(cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_room(di)));
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return COREINFER_OK;
+}
 
 // Typed views of the three storage types.
 template <typename T> __device__ __forceinline__ float to_f32(T v);
@@ -70,6 +86,14 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// The same with C = 0.
+__device__ __forceinline__ void mma_16816_zero(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 
 __device__ __forceinline__ uint32_t pack_half2(float lo, float hi)

@@ -356,15 +356,15 @@ static coreinfer_status launch_group(W4Args& a, const DeviceInfo& di, cudaStream
     if (a.chunk * per_block > kW4MaxX) a.chunk = (int)(kW4MaxX / per_block) / kW4Warps * kW4Warps;
     const size_t fixed = a.chunk * per_block + 2 * kW4Warps * 128 * sizeof(float) +
                          (a.chunk < a.KB ? (size_t)kW4TileGroup * 128 * sizeof(float) : 0);
-    const size_t room = (size_t)di.smem_optin - 1024;
+    const size_t room = smem_room(di);
     int stages = (int)((room - fixed) / STAGE);
     if (stages > kW4MaxStages) stages = kW4MaxStages;
     if (room < fixed || stages < 2) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "not enough shared memory for two pipeline stages");
     a.stages = stages;
     const size_t smem = fixed + stages * STAGE;
-    auto kernel = w4_matvec_kernel<T, Y, G>;
-    CI_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    kernel<<<a.tiles < di.sm_count ? a.tiles : di.sm_count, kW4Threads, smem, st>>>(a);
+    const coreinfer_status s = allow_smem<w4_matvec_kernel<T, Y, G>>(di);
+    if (s != COREINFER_OK) return s;
+    w4_matvec_kernel<T, Y, G><<<a.tiles < di.sm_count ? a.tiles : di.sm_count, kW4Threads, smem, st>>>(a);
     CI_CUDA(cudaGetLastError());
     return COREINFER_OK;
 }
