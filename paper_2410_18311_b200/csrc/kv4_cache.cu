@@ -4,212 +4,368 @@
 namespace coreinfer {
 
 // -------------------------------------------------------------------------------- append --
-// One thread per four values of a head (one unit of codes); the lanes of a group agree on its range
-// by shuffles.
-template <typename T, int GROUP>
-__global__ void __launch_bounds__(256)
-kv4_append_kernel(Kv4 c, const T* __restrict__ k, const T* __restrict__ v, int tokens, long long ld,
-                  T* __restrict__ k_stored, T* __restrict__ v_stored)
+// A row is one token's keys or values of one head.  A lane holds eight consecutive values of a row (D / 8 lanes
+// per row); the lanes of a group agree on its range by shuffles; neighbouring blocks of 32 values
+// exchange a unit so that codes are stored in words.  Bound by the bytes read and written; a CTA walks
+// rows of one sequence so that the sequence's state is read, and its ticket taken, a few hundred times at most.
+constexpr int kAppendThreads = 256;
+
+struct AppendArgs {
+    Kv4 c;
+    const void* src[2];
+    void* stored[2];
+    int tokens;
+    int rows;               // tokens * H * 2
+    long long ld;
+};
+
+template <typename T, int D, int G>
+__global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(const __grid_constant__ AppendArgs a)
 {
+    constexpr int LANES = D / 8, ROWS = kAppendThreads / LANES, H32 = D / 32, GL = G / 8;
+    const Kv4& c = a.c;
     const int b = blockIdx.y;
-    const int n0 = kv4_length(c, b), seen = c.state[b * 4 + kStateSeen];
-    const bool fits = tokens <= c.cap - n0;
-    const int quads = c.D / 4;
-    const long long per = (long long)tokens * c.H * quads;          // units of keys; as many of values follow
-    const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
-    if (i < 2 * per) {                                              // whole warps: 2 * H * D / 4 is a multiple of 32
-        const int which = i >= per;
-        const long long u = which ? i - per : i;
-        const int quad = (int)(u % quads);
-        const int h = (int)((u / quads) % c.H);
-        const int t = (int)(u / quads / c.H);
-        const T* src = (which ? v : k) + ((long long)b * tokens + t) * ld + (long long)h * c.D + quad * 4;
-        T in[4];
-        if (sizeof(T) == 4) *reinterpret_cast<uint4*>(in) = *reinterpret_cast<const uint4*>(src);
-        else *reinterpret_cast<uint2*>(in) = *reinterpret_cast<const uint2*>(src);
-        float x[4], lo = __int_as_float(0x7f800000), hi = -__int_as_float(0x7f800000);
-        bool nan = false;
+    const int l = threadIdx.x % LANES;
+    const int4 state = *reinterpret_cast<const int4*>(c.state + b * 4);
+    const int n0 = state.x < 0 ? 0 : (state.x > c.cap ? c.cap : state.x), seen = state.y;
+    const bool fits = a.tokens <= c.cap - n0;
+    for (int base = blockIdx.x * ROWS; base < a.rows; base += gridDim.x * ROWS) {           // the same count for a whole CTA
+        const int row = base + threadIdx.x / LANES;
+        const bool in = row < a.rows;
+        const int which = row & 1, th = in ? row >> 1 : 0;
+        const int t = th / c.H, h = th - t * c.H;
+        const T* src = (const T*)a.src[which] + ((long long)b * a.tokens + t) * a.ld + (long long)h * D + l * 8;
+        T v[8];
+        *reinterpret_cast<uint4*>(v) = *reinterpret_cast<const uint4*>(src);
+        if (sizeof(T) == 4) reinterpret_cast<uint4*>(v)[1] = reinterpret_cast<const uint4*>(src)[1];
+        float x[8], lo, hi;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            x[e] = to_f32<T>(in[e]);
-            lo = fminf(lo, x[e]);
-            hi = fmaxf(hi, x[e]);
-            nan |= x[e] != x[e];
+        for (int e = 0; e < 8; ++e) {
+            x[e] = to_f32<T>(v[e]);
+            lo = e ? min_nan(lo, x[e]) : x[e];
+            hi = e ? max_nan(hi, x[e]) : x[e];
         }
-        group_range<GROUP / 4>(lo, hi, nan);
-        const QuantPair p = quant_pair(lo, hi, nan);
-        const float s = __half2float(p.s), o = __half2float(p.o);
-        unsigned unit = 0;
-        T back[4];
+        group_range(lo, hi, GL);
+        const QuantPair p = quant_pair(lo, hi);
+        const float s = __half2float(p.s), o = __half2float(p.o), rs = quant_reciprocal(s);
+        unsigned unit[2] = {0u, 0u};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const unsigned q = quant_code(x[e], s, o);
-            unit |= q << (4 * e);
-            back[e] = from_f32<T>(fmaf(s, (float)q, o));
+        for (int e = 0; e < 8; ++e) {
+            const unsigned q = quant_code(x[e], s, o, rs);
+            unit[e / 4] |= q << (4 * (e & 3));
+            v[e] = from_f32<T>(fmaf(s, (float)q, o));
         }
-        if (fits) {
+        // this lane holds units i = 2 (l % 4), i + 1 of block h32 = l / 4; the lane of block h32 ^ 1 has its neighbours
+        const int h32 = l >> 2, odd = h32 & 1;
+        const unsigned got = __shfl_xor_sync(0xffffffffu, odd ? unit[0] : unit[1], 4);
+        const unsigned word = odd ? got | unit[1] << 16 : unit[0] | got << 16;
+        if (in && fits) {
             const size_t slot = ((size_t)b * c.H + h) * c.cap + n0 + t;
-            *reinterpret_cast<uint16_t*>(c.codes[which] + slot * (c.D / 2) + unit_offset(quad * 4, c.D / 32)) = (uint16_t)unit;
-            if (quad % (GROUP / 4) == 0) c.pairs[which][slot * (c.D / GROUP) + quad / (GROUP / 4)] = __halves2half2(p.s, p.o);
-            if (!which && quad == 0 && c.weight) {
+            uint8_t* codes = c.codes[which] + slot * (D / 2);
+            *reinterpret_cast<unsigned*>(codes + 2 * ((2 * (l & 3) + odd) * H32 + (h32 & ~1))) = word;
+            if (l % GL == 0) c.pairs[which][slot * (D / G) + l / GL] = __halves2half2(p.s, p.o);
+            if (!which && l == 0 && c.weight) {
                 c.weight[slot] = 0.f;
                 c.position[slot] = seen + t;
             }
         }
-        T* out = which ? v_stored : k_stored;
-        if (out) {
-            out += (((long long)b * tokens + t) * c.H + h) * c.D + quad * 4;
-            if (sizeof(T) == 4) *reinterpret_cast<uint4*>(out) = *reinterpret_cast<uint4*>(back);
-            else *reinterpret_cast<uint2*>(out) = *reinterpret_cast<uint2*>(back);
+        if (in && a.stored[which]) {
+            T* out = (T*)a.stored[which] + (((long long)b * a.tokens + t) * c.H + h) * D + l * 8;
+            *reinterpret_cast<uint4*>(out) = *reinterpret_cast<uint4*>(v);
+            if (sizeof(T) == 4) reinterpret_cast<uint4*>(out)[1] = reinterpret_cast<uint4*>(v)[1];
         }
     }
     if (kv4_last_of_sequence(c, b, gridDim.x)) {
         if (fits) {
-            c.state[b * 4 + kStateLength] = n0 + tokens;
-            c.state[b * 4 + kStateSeen] = seen + tokens;
+            c.state[b * 4 + kStateLength] = n0 + a.tokens;
+            c.state[b * 4 + kStateSeen] = seen + a.tokens;
         } else {
-            c.state[b * 4 + kStateRefused] += tokens;
+            c.state[b * 4 + kStateRefused] = state.z + a.tokens;
         }
     }
 }
 
-template <typename T>
-static coreinfer_status launch_append(const Kv4& c, const void* k, const void* v, int tokens, long long ld, void* ks, void* vs, cudaStream_t st)
+template <typename T, int D, int G>
+static void launch_append(const AppendArgs& a, const DeviceInfo& di, cudaStream_t st)
 {
-    const long long units = 2LL * tokens * c.H * (c.D / 4);
-    const dim3 grid((unsigned)((units + 255) / 256), (unsigned)c.B);
-    auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(c, (const T*)k, (const T*)v, tokens, ld, (T*)ks, (T*)vs); };
-    if (c.G == 32) go(kv4_append_kernel<T, 32>);
-    else if (c.G == 64) go(kv4_append_kernel<T, 64>);
-    else go(kv4_append_kernel<T, 128>);
+    constexpr int ROWS = kAppendThreads / (D / 8);
+    const int want = (a.rows + ROWS - 1) / ROWS, most = (di.sm_count * 8 + a.c.B - 1) / a.c.B;
+    kv4_append_kernel<T, D, G><<<dim3(want < most ? want : most, a.c.B), kAppendThreads, 0, st>>>(a);
+}
+
+template <typename T>
+static coreinfer_status pick_append(const AppendArgs& a, const DeviceInfo& di, cudaStream_t st)
+{
+    const int D = a.c.D, G = a.c.G;
+    if (D == 64) G == 32 ? launch_append<T, 64, 32>(a, di, st) : launch_append<T, 64, 64>(a, di, st);
+    else if (D == 128)
+        G == 32 ? launch_append<T, 128, 32>(a, di, st) : (G == 64 ? launch_append<T, 128, 64>(a, di, st) : launch_append<T, 128, 128>(a, di, st));
+    else
+        G == 32 ? launch_append<T, 256, 32>(a, di, st) : (G == 64 ? launch_append<T, 256, 64>(a, di, st) : launch_append<T, 256, 128>(a, di, st));
     CI_CUDA(cudaGetLastError());
     return COREINFER_OK;
 }
 
 // --------------------------------------------------------------------------------- evict --
-constexpr int kEvictThreads = 1024;
+// kv4_select_kernel, one CTA per sequence and head: keys (the order of eviction as unsigned numbers) into shared memory,
+// the key of the last slot that stays by radix selection (11 + 11 + 10 bits, most significant first,
+// stopping as soon as a whole bin stays), then the lists of slots that move by ballots and one scan
+// over the warps.  A warp owns a contiguous range of slots, so that list order is slot order.
+// kv4_move_kernel copies the listed slots, many CTAs per head; where few can move (in place with little room
+// above the budget) the first kernel does it itself.  Both are bound by latency at the sizes of a decode
+// step, the moves by bytes after a prompt.
+constexpr int kEvictBins = 2048;
+constexpr int kEvictFewMoves = 64;          // moves that the selecting CTA makes itself
+constexpr int kEvictKeysMost = 48 * 1024;   // keys held in shared memory; more slots are read again for each pass
+constexpr int kMoveSlots = 64;              // slots per CTA of the moving kernel
+constexpr int kMoveThreads = 256;
 
-// Order of eviction as an unsigned number: kept for certain > larger weight > smaller weight > NaN.
 __device__ __forceinline__ unsigned evict_key(float w, int pos, int seen, int recent, int first)
 {
-    if (pos >= seen - recent || pos < first) return 0xffffffffu;
-    if (w != w) return 0u;
+    if (pos >= seen - recent || pos < first) return 0xffffffffu;    // stays for certain: above every number
+    if (w != w) return 0u;                                          // NaN: below every number
     const unsigned u = __float_as_uint(w + 0.f);                    // -0 counts as 0
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-__device__ __forceinline__ int block_scan_excl(int v, int* warp_tot, int* total)
+// Copies `count` listed slots; a thread takes one piece of a slot at a time: 16 bytes of codes, or one
+// pair, or the weight, or the position.  Sources and destinations do not overlap, so four pieces are read before
+// the first is written.
+__device__ __forceinline__ void move_slots(const Kv4& a, size_t abase, const Kv4& z, size_t zbase, const int32_t* from, const int32_t* to,
+                                           int count, int tid, int threads)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int incl = v;
+    constexpr int U = 4;
+    const int chunks = a.D / 32, groups = a.D / a.G, items = 2 * chunks + 2 * groups + 2, all = count * items;
+    for (int i0 = tid; i0 < all; i0 += U * threads) {
+        uint4 v[U];
+        void* dst[U];
+        bool wide[U];
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int t = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += t;
-    }
-    if (lane == 31) warp_tot[warp] = incl;
-    __syncthreads();
-    if (warp == 0) {
-        int w = warp_tot[lane];
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int t = __shfl_up_sync(0xffffffffu, w, o);
-            if (lane >= o) w += t;
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u * threads;
+            dst[u] = nullptr;
+            if (i >= all) continue;
+            const int m = i / items;
+            int k = i - m * items;
+            const size_t s = abase + from[m], d = zbase + to[m];
+            const void* src;
+            wide[u] = k < 2 * chunks;
+            if (wide[u]) {
+                const int w = k >= chunks;
+                k -= w * chunks;
+                src = reinterpret_cast<const uint4*>(a.codes[w] + s * (a.D / 2)) + k;
+                dst[u] = reinterpret_cast<uint4*>(z.codes[w] + d * (a.D / 2)) + k;
+                v[u] = *reinterpret_cast<const uint4*>(src);
+                continue;
+            }
+            k -= 2 * chunks;
+            if (k < 2 * groups) {
+                const int w = k >= groups;
+                k -= w * groups;
+                src = a.pairs[w] + s * groups + k;
+                dst[u] = z.pairs[w] + d * groups + k;
+            } else if (k == 2 * groups) {
+                src = a.weight + s;
+                dst[u] = z.weight + d;
+            } else {
+                src = a.position + s;
+                dst[u] = z.position + d;
+            }
+            v[u].x = *reinterpret_cast<const unsigned*>(src);
         }
-        warp_tot[lane] = w;
-    }
-    __syncthreads();
-    const int base = warp > 0 ? warp_tot[warp - 1] : 0;
-    *total = warp_tot[31];
-    __syncthreads();
-    return base + incl - v;
-}
-
-// Copies one slot, `lane` of 32.
-__device__ __forceinline__ void move_slot(const Kv4& a, size_t from, const Kv4& z, size_t to, int lane)
-{
-    const int words = a.D / 8, groups = a.D / a.G;                  // of codes per row
-    for (int w = 0; w < 2; ++w) {
-        const unsigned* s = reinterpret_cast<const unsigned*>(a.codes[w] + from * (a.D / 2));
-        unsigned* d = reinterpret_cast<unsigned*>(z.codes[w] + to * (a.D / 2));
-        for (int i = lane; i < words; i += 32) d[i] = s[i];
-        for (int i = lane; i < groups; i += 32) z.pairs[w][to * groups + i] = a.pairs[w][from * groups + i];
-    }
-    if (lane == 0) {
-        z.weight[to] = a.weight[from];
-        z.position[to] = a.position[from];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (!dst[u]) continue;
+            if (wide[u]) *reinterpret_cast<uint4*>(dst[u]) = v[u];
+            else *reinterpret_cast<unsigned*>(dst[u]) = v[u].x;
+        }
     }
 }
 
-// One CTA per sequence and head: the key of the last slot that stays by four 8-bit digits, then the lists
-// of slots that move, then the moves.
-__global__ void __launch_bounds__(kEvictThreads)
-kv4_evict_kernel(Kv4 a, Kv4 z, int in_place, int budget, int recent, int first, int32_t* lists)
+struct EvictArgs {
+    Kv4 a, z;
+    int in_place, budget, recent, first;
+    int keys;               // capacity of the key buffer
+    int move_here;          // the selecting CTA moves (in place only)
+    int32_t* counts;        // [B * H] slots to move
+    int32_t* lists;         // [B * H][cap]: sources; in place destinations [0, cap / 2), sources from cap / 2 on
+};
+
+// Sum over the block's warps before this one, and over all of them.
+__device__ __forceinline__ int warps_before(int v, int* buf, int warp, int warps, int* total)
 {
-    __shared__ unsigned hist[256];
-    __shared__ int warp_tot[32];
-    __shared__ unsigned prefix_s;
-    __shared__ int left_s;
-    const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+    if ((threadIdx.x & 31) == 0) buf[warp] = v;
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int w = 0; w < warps; ++w) {
+        const int x = buf[w];
+        before += w < warp ? x : 0;
+        all += x;
+    }
+    __syncthreads();
+    *total = all;
+    return before;
+}
+
+__global__ void __launch_bounds__(1024) kv4_select_kernel(const __grid_constant__ EvictArgs e)
+{
+    extern __shared__ __align__(16) unsigned keys[];
+    __shared__ unsigned hist[kEvictBins];
+    __shared__ int buf[32];
+    __shared__ int bin_s, left_s, count_s;
+    const Kv4& a = e.a;
+    const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
     const int n = kv4_length(a, b), seen = a.state[b * 4 + kStateSeen];
-    const int keep = n < budget ? n : budget;
-    const size_t base = ((size_t)b * a.H + h) * a.cap, zbase = ((size_t)b * a.H + h) * z.cap;
-    int32_t* list = lists + base;
-    auto key = [&](int i) { return evict_key(a.weight[base + i], a.position[base + i], seen, recent, first); };
+    const int keep = n < e.budget ? n : e.budget;
+    const size_t base = ((size_t)b * a.H + h) * a.cap;
+    const float* weight = a.weight + base;
+    const int32_t* position = a.position + base;
+    int32_t* list = e.lists + base;
+    const bool held = n <= e.keys;
+    auto key = [&](int i) { return held ? keys[i] : evict_key(weight[i], position[i], seen, e.recent, e.first); };
+    // a warp's slots: [from, to)
+    const int per = ((n + warps - 1) / warps + 31) & ~31;
+    const int from = warp * per < n ? warp * per : n, to = from + per < n ? from + per : n;
 
-    unsigned prefix = 0;
-    int left = keep;                                                // slots still to be taken among those that match the prefix
-    if (keep > 0 && keep < n) {
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            if (tid < 256) hist[tid] = 0;
-            __syncthreads();
-            const unsigned mask = shift == 24 ? 0u : 0xffffffffu << (shift + 8);
-            for (int i = tid; i < n; i += blockDim.x) {
-                const unsigned u = key(i);
-                if ((u & mask) == prefix) atomicAdd(&hist[(u >> shift) & 255u], 1u);
+    // the slots with (key >> shift) > prefix stay, and the first `left` of those with equality
+    unsigned prefix = 0u;
+    int shift = 0, left = 0;
+    const bool all = keep == n;
+    if (!all && keep > 0) {
+        int certain = 0;
+        for (int i = tid; i < kEvictBins; i += blockDim.x) hist[i] = 0u;
+        __syncthreads();
+#pragma unroll 4
+        for (int i = from + lane; i < to; i += 32) {
+            const unsigned u = evict_key(weight[i], position[i], seen, e.recent, e.first);
+            if (held) keys[i] = u;
+            if (u == 0xffffffffu) ++certain;
+            else atomicAdd(&hist[u >> 21], 1u);
+        }
+        certain = __reduce_add_sync(0xffffffffu, certain);
+        int sure;
+        warps_before(certain, buf, warp, warps, &sure);
+        left = keep - sure;
+        if (left <= 0) {
+            // only slots that stay for certain do (more of them than the budget where positions are not what append
+            // wrote: the first ones)
+            prefix = 0xffffffffu;
+            left = keep;
+        } else {
+            for (int pass = 0; pass < 3; ++pass) {
+                shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0);
+                if (pass > 0) {
+                    for (int i = tid; i < kEvictBins; i += blockDim.x) hist[i] = 0u;
+                    __syncthreads();
+                    const int bits = pass == 1 ? 11 : 10;
+#pragma unroll 4
+                    for (int i = from + lane; i < to; i += 32) {
+                        const unsigned u = key(i);
+                        if (u != 0xffffffffu && u >> (shift + bits) == prefix) atomicAdd(&hist[(u >> shift) & ((1u << bits) - 1u)], 1u);
+                    }
+                    __syncthreads();
+                }
+                // from the top bin down: the bin in which the count reaches `left`
+                const int mine = kEvictBins / blockDim.x;            // bins per thread
+                const int top = kEvictBins - 1 - tid * mine;
+                int sum = 0;
+                for (int k = 0; k < mine; ++k) sum += hist[top - k];
+                int incl = sum;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int v = __shfl_up_sync(0xffffffffu, incl, d);
+                    if (lane >= d) incl += v;
+                }
+                int total;
+                const int before = warps_before(__shfl_sync(0xffffffffu, incl, 31), buf, warp, warps, &total) + incl - sum;
+                if (before < left && left <= before + sum) {
+                    int k = 0, acc = before;
+                    while (acc + (int)hist[top - k] < left) acc += hist[top - k++];
+                    bin_s = top - k;
+                    left_s = left - acc;
+                    count_s = hist[top - k];
+                }
+                __syncthreads();
+                prefix = pass == 0 ? (unsigned)bin_s : (prefix << (pass == 1 ? 11 : 10)) | (unsigned)bin_s;
+                left = left_s;
+                const bool whole = count_s == left;
+                __syncthreads();
+                if (whole) break;
             }
-            __syncthreads();
-            if (tid == 0) {
-                int d = 255, acc = 0;
-                while (d > 0 && acc + (int)hist[d] < left) acc += hist[d--];
-                prefix_s = prefix | ((unsigned)d << shift);
-                left_s = left - acc;
-            }
-            __syncthreads();
-            prefix = prefix_s;
-            left = left_s;
         }
     }
-    // the slots with a larger key stay, and the first `left` of those with this key
-    int ties = 0, movers = 0, holes = 0;
-    for (int i0 = 0; i0 < n; i0 += blockDim.x) {
-        const int i = i0 + tid;
-        const unsigned u = i < n ? key(i) : 0u;
-        const bool all = keep == n;
-        const int tie = i < n && !all && u == prefix;
-        int tot;
-        const int rank = ties + block_scan_excl(tie, warp_tot, &tot);
-        ties += tot;
-        const bool stays = i < n && keep > 0 && (all || u > prefix || (tie && rank < left));
-        const int mover = in_place ? stays && i >= keep : stays;
-        const int m = movers + block_scan_excl(mover, warp_tot, &tot);
-        movers += tot;
-        const int hole = in_place && i < keep && !stays;
-        const int e = holes + block_scan_excl(hole, warp_tot, &tot);
-        holes += tot;
-        if (mover) list[in_place ? a.cap / 2 + m : m] = i;
-        if (hole) list[e] = i;
+
+    auto tie = [&](unsigned u) { return (u >> shift) == prefix && (u != 0xffffffffu || prefix == 0xffffffffu); };
+    auto over = [&](unsigned u) { return (u >> shift) > prefix || (u == 0xffffffffu && prefix != 0xffffffffu); };
+    int movers = 0, total = 0;
+    if (keep > 0 && !(all && e.in_place)) {
+        int ties = 0;
+        if (!all) {
+            int c = 0;
+            for (int i = from + lane; i < to; i += 32) c += tie(key(i));
+            c = __reduce_add_sync(0xffffffffu, c);
+            int t;
+            ties = warps_before(c, buf, warp, warps, &t);
+        }
+        // the lists, in two rounds over the warp's slots: count, then write
+        int at[2] = {0, 0};
+        for (int round = 0; round < 2; ++round) {
+            int rank = ties, m = at[0], o = at[1];
+            for (int i0 = from; i0 < to; i0 += 32) {
+                const int i = i0 + lane;
+                bool stays = i < to;
+                if (!all) {
+                    const unsigned u = i < to ? key(i) : 0u;
+                    const bool eq = i < to && tie(u);
+                    const unsigned eqs = __ballot_sync(0xffffffffu, eq);
+                    stays = i < to && (over(u) || (eq && rank + __popc(eqs & ((1u << lane) - 1u)) < left));
+                    rank += __popc(eqs);
+                }
+                const bool mover = stays && (!e.in_place || i >= keep), hole = e.in_place && i < to && i < keep && !stays;
+                const unsigned ms = __ballot_sync(0xffffffffu, mover), os = __ballot_sync(0xffffffffu, hole);
+                if (round) {
+                    if (mover) list[(e.in_place ? a.cap / 2 : 0) + m + __popc(ms & ((1u << lane) - 1u))] = i;
+                    if (hole) list[o + __popc(os & ((1u << lane) - 1u))] = i;
+                }
+                m += __popc(ms);
+                o += __popc(os);
+            }
+            if (!round) {
+                at[0] = warps_before(m, buf, warp, warps, &movers);
+                at[1] = warps_before(o, buf, warp, warps, &total);
+            }
+        }
     }
-    __syncthreads();
-    for (int m = tid >> 5; m < movers; m += blockDim.x >> 5) {
-        const int from = list[in_place ? a.cap / 2 + m : m], to = in_place ? list[m] : m;
-        move_slot(a, base + from, z, zbase + to, tid & 31);
+    if (tid == 0) e.counts[b * a.H + h] = movers;
+    if (e.move_here) {
+        __syncthreads();
+        move_slots(a, base, e.z, ((size_t)b * a.H + h) * e.z.cap, list + a.cap / 2, list, movers, tid, blockDim.x);
     }
     if (kv4_last_of_sequence(a, b, gridDim.x)) {
-        z.state[b * 4 + kStateLength] = keep;
-        z.state[b * 4 + kStateSeen] = seen;
+        e.z.state[b * 4 + kStateLength] = keep;
+        e.z.state[b * 4 + kStateSeen] = seen;
     }
 }
+
+__global__ void __launch_bounds__(kMoveThreads) kv4_move_kernel(const __grid_constant__ EvictArgs e)
+{
+    __shared__ int32_t from_s[kMoveSlots], to_s[kMoveSlots];
+    const int bh = blockIdx.y, first = blockIdx.x * kMoveSlots, tid = threadIdx.x;
+    const size_t base = (size_t)bh * e.a.cap;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    int count = e.counts[bh] - first;
+    if (count <= 0) return;
+    if (count > kMoveSlots) count = kMoveSlots;
+    const int32_t* list = e.lists + base;
+    if (tid < count) {
+        from_s[tid] = list[(e.in_place ? e.a.cap / 2 : 0) + first + tid];
+        to_s[tid] = e.in_place ? list[first + tid] : first + tid;
+    }
+    __syncthreads();
+    move_slots(e.a, base, e.z, (size_t)bh * e.z.cap, from_s, to_s, count, tid, kMoveThreads);
+}
+
+static inline size_t evict_lists_at(const Kv4& c) { return ((size_t)c.B * c.H * sizeof(int32_t) + 15) & ~(size_t)15; }
 
 }  // namespace coreinfer
 
@@ -231,20 +387,29 @@ coreinfer_status coreinfer_kv4_append(const coreinfer_kv4_cache* cache, const vo
         CI_FAIL(COREINFER_ERR_INVALID_ARG, "ld_token must cover kv_heads * head_dim elements and be a multiple of 16 bytes");
     if ((k_stored == nullptr) != (v_stored == nullptr) || !aligned16(k_stored) || !aligned16(v_stored))
         CI_FAIL(COREINFER_ERR_INVALID_ARG, "k_stored and v_stored come both (16-byte aligned) or neither");
-    if ((long long)T * c.H > (1LL << 30)) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "T %d: too many tokens for one call", T);
+    if ((long long)T * c.H > (1LL << 29)) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "T %d: too many tokens for one call", T);
     DeviceInfo di;
     if ((s = device_info(&di)) != COREINFER_OK) return s;
+    AppendArgs a;
+    a.c = c;
+    a.src[0] = k;
+    a.src[1] = v;
+    a.stored[0] = k_stored;
+    a.stored[1] = v_stored;
+    a.tokens = T;
+    a.rows = T * c.H * 2;
+    a.ld = ld_token;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (dtype == COREINFER_F32) return launch_append<float>(c, k, v, T, ld_token, k_stored, v_stored, st);
-    if (dtype == COREINFER_BF16) return launch_append<__nv_bfloat16>(c, k, v, T, ld_token, k_stored, v_stored, st);
-    return launch_append<__half>(c, k, v, T, ld_token, k_stored, v_stored, st);
+    if (dtype == COREINFER_F32) return pick_append<float>(a, di, st);
+    if (dtype == COREINFER_BF16) return pick_append<__nv_bfloat16>(a, di, st);
+    return pick_append<__half>(a, di, st);
 }
 
 size_t coreinfer_kv4_evict_workspace_bytes(const coreinfer_kv4_cache* src)
 {
     Kv4 c;
     if (kv4_take(src, "the source", &c) != COREINFER_OK) return 0;
-    return (size_t)c.B * c.H * c.cap * sizeof(int32_t);
+    return evict_lists_at(c) + (size_t)c.B * c.H * c.cap * sizeof(int32_t);
 }
 
 coreinfer_status coreinfer_kv4_evict(const coreinfer_kv4_cache* src, const coreinfer_kv4_cache* dst,
@@ -257,6 +422,7 @@ coreinfer_status coreinfer_kv4_evict(const coreinfer_kv4_cache* src, const corei
     if (!a.weight || !z.weight) CI_FAIL(COREINFER_ERR_INVALID_ARG, "eviction needs caches with weight and position");
     if (budget < 1 || recent < 0 || first < 0 || (long long)recent + first > budget)
         CI_FAIL(COREINFER_ERR_INVALID_ARG, "budget %d must be >= 1 and hold recent %d + first %d", budget, recent, first);
+    if ((long long)a.B * a.H > 65535) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "batch * kv_heads: at most 65535");
     if (a.B != z.B || a.H != z.H || a.D != z.D || a.G != z.G)
         CI_FAIL(COREINFER_ERR_INVALID_ARG, "the two caches differ in batch, kv_heads, head_dim or group");
     int same = 0;
@@ -271,9 +437,35 @@ coreinfer_status coreinfer_kv4_evict(const coreinfer_kv4_cache* src, const corei
     if (workspace_bytes < need) CI_FAIL(COREINFER_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
     DeviceInfo di;
     if ((s = device_info(&di)) != COREINFER_OK) return s;
-    kv4_evict_kernel<<<dim3(a.H, a.B), kEvictThreads, 0, (cudaStream_t)cuda_stream>>>(a, z, same == 7, budget, recent, first,
-                                                                                      (int32_t*)workspace);
+    EvictArgs e;
+    e.a = a;
+    e.z = z;
+    e.in_place = same == 7;
+    e.budget = budget;
+    e.recent = recent;
+    e.first = first;
+    e.keys = a.cap < kEvictKeysMost ? a.cap : kEvictKeysMost;
+    // in place no more slots move than there are above the budget
+    e.move_here = e.in_place && a.cap - budget <= kEvictFewMoves;
+    e.counts = (int32_t*)workspace;
+    e.lists = (int32_t*)((uint8_t*)workspace + evict_lists_at(a));
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    if ((s = allow_smem<kv4_select_kernel>(di, 16384)) != COREINFER_OK) return s;
+    kv4_select_kernel<<<dim3(a.H, a.B), a.cap <= 4096 ? 512 : 1024, (size_t)e.keys * sizeof(unsigned), st>>>(e);
     CI_CUDA(cudaGetLastError());
+    if (e.move_here) return COREINFER_OK;
+    const int most = e.in_place ? (a.cap - budget < a.cap / 2 ? a.cap - budget : a.cap / 2) : (budget < a.cap ? budget : a.cap);
+    if (most <= 0) return COREINFER_OK;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((most + kMoveSlots - 1) / kMoveSlots, a.B * a.H);
+    cfg.blockDim = dim3(kMoveThreads);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    CI_CUDA(cudaLaunchKernelEx(&cfg, kv4_move_kernel, e));
     return COREINFER_OK;
 }
 

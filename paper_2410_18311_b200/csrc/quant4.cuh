@@ -15,16 +15,16 @@ static inline bool aligned_to(const void* p, size_t n) { return (reinterpret_cas
 
 #ifdef __CUDACC__
 
-// Dynamic shared memory that a kernel of this file's users may ask for: all but 1 KB for its static part.
-static inline size_t smem_room(const DeviceInfo& di) { return (size_t)di.smem_optin - 1024; }
+// Dynamic shared memory that a kernel may ask for beside `fixed` bytes (1 KB unless said) for its static part.
+static inline size_t smem_room(const DeviceInfo& di, int fixed = 1024) { return (size_t)di.smem_optin - fixed; }
 // Lets a kernel use that much; once per kernel and device, since the call costs about a microsecond of host time.
 template <auto Kernel>
-static coreinfer_status allow_smem(const DeviceInfo& di)
+static coreinfer_status allow_smem(const DeviceInfo& di, int fixed = 1024)
 {
     static std::atomic<unsigned long long> done{0};
     const unsigned long long bit = di.device >= 0 && di.device < 64 ? 1ull << di.device : 0ull;
     if (done.load(std::memory_order_relaxed) & bit) return COREINFER_OK;
-    CI_CUDA(cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_room(di)));
+    CI_CUDA(cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_room(di, fixed)));
     done.fetch_or(bit, std::memory_order_relaxed);
     return COREINFER_OK;
 }
@@ -42,37 +42,53 @@ template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return
 // Byte of the unit that holds values v .. v + 3 (v a multiple of 4) of a row piece of 32 H values.
 __device__ __forceinline__ int unit_offset(int v, int H) { return 2 * (((v & 31) >> 2) * H + (v >> 5)); }
 
-// Minimum, maximum and "holds a NaN" over the LANES consecutive lanes (a power of two) of a group.
-template <int LANES>
-__device__ __forceinline__ void group_range(float& lo, float& hi, bool& nan)
+// Minimum and maximum that hand a NaN on.
+__device__ __forceinline__ float min_nan(float a, float b)
 {
-#pragma unroll
-    for (int d = 1; d < LANES; d <<= 1) {
-        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
-        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, d));
-        nan |= __shfl_xor_sync(0xffffffffu, (int)nan, d) != 0;
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+// Over the `lanes` consecutive lanes (a power of two) of a group.
+__device__ __forceinline__ void group_range(float& lo, float& hi, int lanes)
+{
+    for (int d = 1; d < lanes; d <<= 1) {
+        lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, d));
+        hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, d));
     }
 }
 
-// The pair of a group from its range.  Every step is one correctly rounded operation, so the format
-// is a function of the values alone, whoever computes it.
+// The pair of a group from its range (NaN both where the group holds one).  Every step is one correctly
+// rounded operation, so the format is a function of the values alone, whoever computes it.
 struct QuantPair {
     __half s, o;
 };
-__device__ __forceinline__ QuantPair quant_pair(float lo, float hi, bool nan)
+__device__ __forceinline__ QuantPair quant_pair(float lo, float hi)
 {
     QuantPair p;
     p.o = __float2half_rn(fminf(fmaxf(lo, -kHalfMax), kHalfMax));
-    p.s = __float2half_rn(fminf(__fdiv_rn(__fsub_rn(hi, lo), 15.f), kHalfMax));
-    if (nan) p.s = p.o = __ushort_as_half((unsigned short)0x7fff);
+    p.s = __float2half_rn(min_nan(__fdiv_rn(__fsub_rn(hi, lo), 15.f), kHalfMax));
+    if (lo != lo) p.s = p.o = __ushort_as_half((unsigned short)0x7fff);
     return p;
 }
-// (x - o) / s with s <= 0 or NaN: code 0.
-__device__ __forceinline__ unsigned quant_code(float x, float s, float o)
+// clamp(round((x - o) / s), 0, 15), 0 where s is 0 or NaN.  `r` is a reciprocal of s good to a few units in the
+// last place: only a quotient that close to a tie between two codes takes the division.
+__device__ __forceinline__ unsigned quant_code(float x, float s, float o, float r)
 {
     if (!(s > 0.f)) return 0u;
-    return (unsigned)fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(x, o), s)), 0.f), 15.f);
+    const float d = __fsub_rn(x, o);
+    float q = d * r;
+    const float n = rintf(q);
+    if (fabsf(fabsf(q - n) - 0.5f) < 1e-4f) q = __fdiv_rn(d, s);
+    return (unsigned)fminf(fmaxf(rintf(q), 0.f), 15.f);
 }
+__device__ __forceinline__ float quant_reciprocal(float s) { return __fdiv_rn(1.f, s); }
 
 // ---- codes as matrix operands ----
 // Four bits masked into the low end of a 16-bit lane ARE an fp16 number: the subnormal c * 2^-24 (bits 0-3)

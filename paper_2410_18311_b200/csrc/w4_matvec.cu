@@ -28,31 +28,23 @@ w4_quantize_kernel(const T* __restrict__ w, int N, int K, long long sn, long lon
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     for (int r = warp; r < 16; r += 8) {
         float x[4], lo = __int_as_float(0x7f800000), hi = -__int_as_float(0x7f800000);
-        bool nan = false, any = false;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             x[e] = tile[r][lane * 4 + e];
             if (n0 + r < N && k0 + lane * 4 + e < K) {
-                lo = fminf(lo, x[e]);
-                hi = fmaxf(hi, x[e]);
-                nan |= x[e] != x[e];
-                any = true;
+                lo = min_nan(lo, x[e]);
+                hi = max_nan(hi, x[e]);
             }
         }
         const int lanes = group / 4;
-        for (int d = 1; d < lanes; d <<= 1) {
-            lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
-            hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, d));
-            nan |= __shfl_xor_sync(0xffffffffu, (int)nan, d) != 0;
-            any |= __shfl_xor_sync(0xffffffffu, (int)any, d) != 0;
-        }
-        QuantPair p = quant_pair(lo, hi, nan);
-        if (!any) p.s = p.o = __ushort_as_half((unsigned short)0);      // wholly beyond the matrix
-        const float s = __half2float(p.s), o = __half2float(p.o);
+        group_range(lo, hi, lanes);
+        QuantPair p = quant_pair(lo, hi);
+        if (n0 + r >= N || k0 + (lane & ~(lanes - 1)) * 4 >= K) p.s = p.o = __ushort_as_half((unsigned short)0);   // wholly beyond the matrix
+        const float s = __half2float(p.s), o = __half2float(p.o), rs = quant_reciprocal(s);
         unsigned unit = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (k0 + lane * 4 + e < K && n0 + r < N) unit |= quant_code(x[e], s, o) << (4 * e);
+            if (k0 + lane * 4 + e < K && n0 + r < N) unit |= quant_code(x[e], s, o, rs) << (4 * e);
         uint8_t* row = codes + (((size_t)rt * KB + kb) * 16 + r) * 64;
         *reinterpret_cast<uint16_t*>(row + unit_offset(lane * 4, 4)) = (uint16_t)unit;
         if ((lane & (lanes - 1)) == 0) {

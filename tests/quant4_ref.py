@@ -142,7 +142,8 @@ class CacheRef:
             keep = min(self.length[b], budget)
             for h in range(self.H):
                 stay = self.kept(b, h, budget, recent, first)
-                holes = [i for i in range(keep) if i not in set(stay)]
+                inside = set(stay)
+                holes = [i for i in range(keep) if i not in inside]
                 movers = [i for i in stay if i >= keep]
                 for a in self._rows():
                     a[b, h, holes] = a[b, h, movers].copy()

@@ -228,7 +228,8 @@ EVICT = [
     # B, H, lengths, budget, recent, first, D, group, ties
     (1, 1, [1], 1, 0, 0, 64, 32, False), (2, 2, [40, 10], 20, 4, 2, 64, 64, False), (3, 3, [0, 100, 33], 32, 32, 0, 128, 128, False),
     (2, 4, [300, 257], 256, 10, 4, 128, 64, True), (1, 2, [1500], 100, 0, 0, 256, 32, True), (2, 2, [64, 64], 64, 0, 0, 64, 32, False),
-    (1, 3, [2000], 1999, 5, 5, 64, 32, False), (4, 1, [5000, 4096, 1, 1025], 1024, 256, 4, 64, 64, True),
+    (1, 3, [2000], 1999, 5, 5, 64, 32, False), (1, 1, [60000], 45000, 1000, 4, 64, 64, True), (2, 1, [33000, 20], 700, 64, 4, 128, 32, False),
+    (4, 1, [5000, 4096, 1, 1025], 1024, 256, 4, 64, 64, True),
 ]
 
 
