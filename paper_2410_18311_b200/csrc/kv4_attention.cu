@@ -58,11 +58,22 @@ struct AttnArgs {
 };
 
 __device__ __forceinline__ int attn_tiles(int len, int tile) { return (len + tile - 1) / tile; }
-// CTA i of n takes the tiles from attn_start(i) to attn_start(i + 1), n at most the number of tiles, so that each
-// CTA has one at least; attn_owner is the CTA of tile t.
-__device__ __forceinline__ int attn_ctas(int n_ctas, int total) { return total < n_ctas ? total : n_ctas; }
-__device__ __forceinline__ int attn_start(int i, int total, int n) { return (int)((long long)i * total / n); }
-__device__ __forceinline__ int attn_owner(int t, int total, int n) { return (int)((((long long)t + 1) * n - 1) / total); }
+// The list of tiles in n equal pieces, the first `more` of them one longer; every CTA that works has one tile at least.
+struct AttnCut {
+    int n, each, more;
+    __device__ __forceinline__ AttnCut(int n_ctas, int total)
+    {
+        n = total < n_ctas ? total : n_ctas;
+        each = n ? total / n : 0;
+        more = total - each * n;
+    }
+    __device__ __forceinline__ int start(int i) const { return i * each + (i < more ? i : more); }
+    __device__ __forceinline__ int owner(int t) const
+    {
+        const int head = more * (each + 1);
+        return t < head ? t / (each + 1) : more + (t - head) / each;
+    }
+};
 
 __device__ __forceinline__ uint32_t movmatrix_trans(uint32_t a)
 {
@@ -154,8 +165,9 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
 
     const int HR = c.H * a.RB;
     const int total = pre[c.B] * HR;
-    const int n_ctas = attn_ctas(a.n_ctas, total), me = blockIdx.x;
-    const int begin = me < n_ctas ? attn_start(me, total, n_ctas) : 0, end = me < n_ctas ? attn_start(me + 1, total, n_ctas) : 0;
+    const AttnCut cut(a.n_ctas, total);
+    const int me = blockIdx.x;
+    const int begin = me < cut.n ? cut.start(me) : 0, end = me < cut.n ? cut.start(me + 1) : 0;
     auto seek = [&](int t) {
         Cursor k;
         int lo = 0, hi = c.B - 1;                           // last b with pre[b] * HR <= t: it has tiles
@@ -229,7 +241,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                 m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
                 m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
                 const int x = range_exponent(m);             // the largest value goes to [2^13, 2^14)
-                const float up = ldexpf(1.f, 14 - x);
+                const float up = pow2(14 - x);
                 float gs[NG];
 #pragma unroll
                 for (int g = 0; g < NG; ++g) gs[g] = 0.f;
@@ -240,12 +252,17 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                         v[j][e] *= up;
                         gs[j * 32 / G] += v[j][e];
                     }
-                    const int low = PARTS ? gid & 1 : 0;
-                    const float lo16 = 1.f / 16.f;           // odd codes stand 16 times higher
-                    qf[j][0] = pack_half2(half_part(v[j][0], low), half_part(v[j][4], low));
-                    qf[j][1] = pack_half2(half_part(v[j][2], low), half_part(v[j][6], low));
-                    qf[j][2] = pack_half2(half_part(v[j][1] * lo16, low), half_part(v[j][5] * lo16, low));
-                    qf[j][3] = pack_half2(half_part(v[j][3] * lo16, low), half_part(v[j][7] * lo16, low));
+                }
+                const int low = PARTS ? gid & 1 : 0;
+                const float lo16 = 1.f / 16.f;               // odd codes stand 16 times higher
+#pragma unroll
+                for (int j = 0; j < H32; ++j) {
+                    // the two entries beside each other in step j (code_word)
+                    const float *p = G == 32 ? &v[j][0] : &v[j & ~1][(j & 1) * 4], *q = G == 32 ? &v[j][4] : &v[j | 1][(j & 1) * 4];
+                    qf[j][0] = pack_half2(half_part(p[0], low), half_part(q[0], low));
+                    qf[j][1] = pack_half2(half_part(p[2], low), half_part(q[2], low));
+                    qf[j][2] = pack_half2(half_part(p[1] * lo16, low), half_part(q[1] * lo16, low));
+                    qf[j][3] = pack_half2(half_part(p[3] * lo16, low), half_part(q[3] * lo16, low));
                 }
                 // sums of c q carry 2^-24, so the sums of q do too; f undoes both scalings
                 const float ff = ldexpf(a.scale * 1.44269504088896341f, x - 14 + 24);
@@ -325,8 +342,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                             float acc[4];
 #pragma unroll
                             for (int j = g * G / 32; j < (g + 1) * G / 32; ++j) {
-                                const uint32_t x0 = __byte_perm(w0[j / 2], w0[H32 / 2 + j / 2], j & 1 ? 0x7632 : 0x5410);
-                                const uint32_t x1 = __byte_perm(w1[j / 2], w1[H32 / 2 + j / 2], j & 1 ? 0x7632 : 0x5410);
+                                const uint32_t x0 = code_word<G, H32>(w0, j), x1 = code_word<G, H32>(w1, j);
                                 const uint32_t y0 = x0 >> 8, y1 = x1 >> 8;
                                 if (j == g * G / 32)
                                     mma_16816_zero(acc, x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, qf[j][0], qf[j][1]);
@@ -607,7 +623,8 @@ __global__ void __launch_bounds__(kFinishThreads) kv4_finish_kernel(const __grid
     auto add = [](int x, int y) { return x + y; };
     before = finish_reduce(before, redi, add);
     all = finish_reduce(all, redi, add);
-    const int HR = c.H * a.RB, nt = attn_tiles(len, a.tile), total = all * HR, n_ctas = attn_ctas(a.n_ctas, total);
+    const int HR = c.H * a.RB, nt = attn_tiles(len, a.tile), total = all * HR;
+    const AttnCut cut(a.n_ctas, total);
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
     if ((int)blockIdx.x < a.R) {
@@ -618,7 +635,7 @@ __global__ void __launch_bounds__(kFinishThreads) kv4_finish_kernel(const __grid
             return;
         }
         const int u0 = before * HR + (h * a.RB + rb) * nt;
-        const int i0 = attn_owner(u0, total, n_ctas), i1 = attn_owner(u0 + nt - 1, total, n_ctas);
+        const int i0 = cut.owner(u0), i1 = cut.owner(u0 + nt - 1);
         if (i0 == i1) return;
         float* wgt = reinterpret_cast<float*>(smem);                     // [pieces]
         const int n = i1 - i0 + 1;
@@ -665,10 +682,11 @@ __global__ void __launch_bounds__(kFinishThreads) kv4_finish_kernel(const __grid
 
     // weights: maximum and 1 / sum of every row, one warp per row
     float2* rows = reinterpret_cast<float2*>(smem);                      // [R]
+    int* sees = reinterpret_cast<int*>(rows + a.R);                      // [R] slots that the row sees
     for (int r = warp; r < a.R; r += kFinishThreads / 32) {
         const int rb = r / a.RU, ru = r % a.RU;
         const int u0 = before * HR + (h * a.RB + rb) * nt;
-        const int i0 = attn_owner(u0, total, n_ctas), i1 = attn_owner(u0 + nt - 1, total, n_ctas);
+        const int i0 = cut.owner(u0), i1 = cut.owner(u0 + nt - 1);
         float top, sum;
         if (i0 == i1) {
             const float2 ml = a.stats[(((size_t)b * c.H + h) * a.RB + rb) * a.RU + ru];
@@ -687,7 +705,10 @@ __global__ void __launch_bounds__(kFinishThreads) kv4_finish_kernel(const __grid
 #pragma unroll
             for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
         }
-        if (lane == 0) rows[r] = make_float2(top, sum == 0.f ? 0.f : 1.f / sum);
+        if (lane == 0) {
+            rows[r] = make_float2(top, sum == 0.f ? 0.f : 1.f / sum);
+            sees[r] = len - (a.T - 1 - r / a.share);
+        }
     }
     __syncthreads();
     // four slots a thread: the capacity is a multiple of 16, so they lie within a row of logits
@@ -700,7 +721,7 @@ __global__ void __launch_bounds__(kFinishThreads) kv4_finish_kernel(const __grid
     for (int r = 0; r < a.R; ++r) {
         const float4 x = *reinterpret_cast<const float4*>(lg + (size_t)r * c.cap);
         const float2 ml = rows[r];
-        const int see = len - (a.T - 1 - r / a.share) - n;  // slots of the four that the row sees
+        const int see = sees[r] - n;                        // slots of the four that the row sees
         if (see > 0) w.x = fmaf(exp2_fast(x.x - ml.x), ml.y, w.x);
         if (see > 1) w.y = fmaf(exp2_fast(x.y - ml.x), ml.y, w.y);
         if (see > 2) w.z = fmaf(exp2_fast(x.z - ml.x), ml.y, w.z);
@@ -769,7 +790,7 @@ static coreinfer_status launch_mode(AttnArgs& a, const DeviceInfo& di, cudaStrea
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(a.R + (a.accumulate ? (a.c.cap + kFinishSlots - 1) / kFinishSlots : 0), a.c.B * a.c.H);
     cfg.blockDim = dim3(kFinishThreads);
-    const size_t join = kAttnMaxCtas * sizeof(float) + kFinishThreads * sizeof(float4), rows = (size_t)a.R * sizeof(float2);
+    const size_t join = kAttnMaxCtas * sizeof(float) + kFinishThreads * sizeof(float4), rows = (size_t)a.R * (sizeof(float2) + sizeof(int));
     cfg.dynamicSmemBytes = join > rows ? join : rows;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
@@ -806,7 +827,7 @@ static coreinfer_status pick_attention(AttnArgs& a, const DeviceInfo& di, cudaSt
                    : (G == 64 ? launch_attention<T, 256, 64>(a, di, st) : launch_attention<T, 256, 128>(a, di, st));
 }
 
-constexpr int kAttnMaxRows = 4096;          // query rows per key head (they sit in shared memory of the finishing kernel)
+constexpr int kAttnMaxRows = 2048;          // query rows per key head (they sit in shared memory of the finishing kernel)
 
 }  // namespace coreinfer
 

@@ -29,15 +29,23 @@ __global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(const __grid
     const int4 state = *reinterpret_cast<const int4*>(c.state + b * 4);
     const int n0 = state.x < 0 ? 0 : (state.x > c.cap ? c.cap : state.x), seen = state.y;
     const bool fits = a.tokens <= c.cap - n0;
-    for (int base = blockIdx.x * ROWS; base < a.rows; base += gridDim.x * ROWS) {           // the same count for a whole CTA
-        const int row = base + threadIdx.x / LANES;
-        const bool in = row < a.rows;
-        const int which = row & 1, th = in ? row >> 1 : 0;
-        const int t = th / c.H, h = th - t * c.H;
-        const T* src = (const T*)a.src[which] + ((long long)b * a.tokens + t) * a.ld + (long long)h * D + l * 8;
-        T v[8];
-        *reinterpret_cast<uint4*>(v) = *reinterpret_cast<const uint4*>(src);
-        if (sizeof(T) == 4) reinterpret_cast<uint4*>(v)[1] = reinterpret_cast<const uint4*>(src)[1];
+    // row r holds keys (even r) or values (odd) of head (r / 2) % H of token r / 2 / H; stepping by an even number of rows
+    // keeps `which`, and moves token and head by a fixed amount with a carry
+    const int row0 = blockIdx.x * ROWS + threadIdx.x / LANES, step = gridDim.x * ROWS;
+    const int which = row0 & 1;
+    int t = (row0 >> 1) / c.H, h = (row0 >> 1) - t * c.H;
+    const int dt = (step >> 1) / c.H, dh = (step >> 1) - dt * c.H;
+    const T* src = (const T*)a.src[which] + l * 8;
+    T* stored = (T*)a.stored[which];
+    auto load = [&](int token, int head, T (&v)[8]) {
+        const T* p = src + ((long long)b * a.tokens + token) * a.ld + (long long)head * D;
+        *reinterpret_cast<uint4*>(v) = *reinterpret_cast<const uint4*>(p);
+        if (sizeof(T) == 4) reinterpret_cast<uint4*>(v)[1] = reinterpret_cast<const uint4*>(p)[1];
+    };
+    T v[8];
+    load(t < a.tokens ? t : 0, t < a.tokens ? h : 0, v);
+    for (int base = blockIdx.x * ROWS; base < a.rows; base += step) {            // the same count for a whole CTA
+        const bool in = t < a.tokens;
         float x[8], lo, hi;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -45,16 +53,21 @@ __global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(const __grid
             lo = e ? min_nan(lo, x[e]) : x[e];
             hi = e ? max_nan(hi, x[e]) : x[e];
         }
+        int t1 = t + dt, h1 = h + dh;
+        if (h1 >= c.H) {
+            h1 -= c.H;
+            ++t1;
+        }
+        T next[8];
+        load(t1 < a.tokens ? t1 : 0, t1 < a.tokens ? h1 : 0, next);               // on its way while this row is worked on
         group_range(lo, hi, GL);
         const QuantPair p = quant_pair(lo, hi);
-        const float s = __half2float(p.s), o = __half2float(p.o), rs = quant_reciprocal(s);
-        unsigned unit[2] = {0u, 0u};
+        const float s = __half2float(p.s), o = __half2float(p.o);
+        unsigned unit[2];
+        float q[8];
+        quant_codes<8>(x, s, o, unit, q);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const unsigned q = quant_code(x[e], s, o, rs);
-            unit[e / 4] |= q << (4 * (e & 3));
-            v[e] = from_f32<T>(fmaf(s, (float)q, o));
-        }
+        for (int e = 0; e < 8; ++e) v[e] = from_f32<T>(fmaf(s, q[e], o));
         // this lane holds units i = 2 (l % 4), i + 1 of block h32 = l / 4; the lane of block h32 ^ 1 has its neighbours
         const int h32 = l >> 2, odd = h32 & 1;
         const unsigned got = __shfl_xor_sync(0xffffffffu, odd ? unit[0] : unit[1], 4);
@@ -69,11 +82,15 @@ __global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(const __grid
                 c.position[slot] = seen + t;
             }
         }
-        if (in && a.stored[which]) {
-            T* out = (T*)a.stored[which] + (((long long)b * a.tokens + t) * c.H + h) * D + l * 8;
+        if (in && stored) {
+            T* out = stored + (((long long)b * a.tokens + t) * c.H + h) * D + l * 8;
             *reinterpret_cast<uint4*>(out) = *reinterpret_cast<uint4*>(v);
             if (sizeof(T) == 4) reinterpret_cast<uint4*>(out)[1] = reinterpret_cast<uint4*>(v)[1];
         }
+        t = t1;
+        h = h1;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = next[e];
     }
     if (kv4_last_of_sequence(c, b, gridDim.x)) {
         if (fits) {
@@ -194,17 +211,13 @@ struct EvictArgs {
 // Sum over the block's warps before this one, and over all of them.
 __device__ __forceinline__ int warps_before(int v, int* buf, int warp, int warps, int* total)
 {
-    if ((threadIdx.x & 31) == 0) buf[warp] = v;
+    const int lane = threadIdx.x & 31;
+    if (lane == 0) buf[warp] = v;
     __syncthreads();
-    int before = 0, all = 0;
-    for (int w = 0; w < warps; ++w) {
-        const int x = buf[w];
-        before += w < warp ? x : 0;
-        all += x;
-    }
+    const int x = lane < warps ? buf[lane] : 0;
     __syncthreads();
-    *total = all;
-    return before;
+    *total = __reduce_add_sync(0xffffffffu, x);
+    return __reduce_add_sync(0xffffffffu, lane < warp ? x : 0);
 }
 
 __global__ void __launch_bounds__(1024) kv4_select_kernel(const __grid_constant__ EvictArgs e)
@@ -451,7 +464,7 @@ coreinfer_status coreinfer_kv4_evict(const coreinfer_kv4_cache* src, const corei
     e.lists = (int32_t*)((uint8_t*)workspace + evict_lists_at(a));
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if ((s = allow_smem<kv4_select_kernel>(di, 16384)) != COREINFER_OK) return s;
-    kv4_select_kernel<<<dim3(a.H, a.B), a.cap <= 4096 ? 512 : 1024, (size_t)e.keys * sizeof(unsigned), st>>>(e);
+    kv4_select_kernel<<<dim3(a.H, a.B), a.cap <= 4096 ? 256 : (a.cap <= 16384 ? 512 : 1024), (size_t)e.keys * sizeof(unsigned), st>>>(e);
     CI_CUDA(cudaGetLastError());
     if (e.move_here) return COREINFER_OK;
     const int most = e.in_place ? (a.cap - budget < a.cap / 2 ? a.cap - budget : a.cap / 2) : (budget < a.cap ? budget : a.cap);

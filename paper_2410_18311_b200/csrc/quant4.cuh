@@ -77,18 +77,42 @@ __device__ __forceinline__ QuantPair quant_pair(float lo, float hi)
     if (lo != lo) p.s = p.o = __ushort_as_half((unsigned short)0x7fff);
     return p;
 }
-// clamp(round((x - o) / s), 0, 15), 0 where s is 0 or NaN.  `r` is a reciprocal of s good to a few units in the
-// last place: only a quotient that close to a tie between two codes takes the division.
-__device__ __forceinline__ unsigned quant_code(float x, float s, float o, float r)
+// Codes of N values in one unit or several: clamp(round((x - o) / s), 0, 15), 0 where s is 0 or NaN.  The quotients
+// come from a reciprocal good to a few units in the last place; adding 3 * 2^22 rounds them, ties to even, and leaves
+// the code in the low bits.  A quotient within 1e-4 of a tie between two codes could round to the other one, so the
+// values then go through the division.  units[i] gets four codes; c the codes as numbers.
+constexpr float kRoundMagic = 12582912.f;
+__device__ __forceinline__ float clamp15(float q) { return fminf(fmaxf(q, 0.f), 15.f); }
+template <int N>
+__device__ __forceinline__ void quant_codes(const float (&x)[N], float s, float o, unsigned (&units)[N / 4], float (&c)[N])
 {
-    if (!(s > 0.f)) return 0u;
-    const float d = __fsub_rn(x, o);
-    float q = d * r;
-    const float n = rintf(q);
-    if (fabsf(fabsf(q - n) - 0.5f) < 1e-4f) q = __fdiv_rn(d, s);
-    return (unsigned)fminf(fmaxf(rintf(q), 0.f), 15.f);
+    float r = 0.f;
+    if (s > 0.f) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+    unsigned bits[N];
+    bool close = false;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        const float q = clamp15(__fsub_rn(x[e], o) * r), t = q + kRoundMagic;
+        bits[e] = __float_as_uint(t);
+        c[e] = t - kRoundMagic;
+        close |= fabsf(q - c[e]) > 0.4999f;
+    }
+    if (close) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float t = clamp15(__fdiv_rn(__fsub_rn(x[e], o), s)) + kRoundMagic;
+            bits[e] = __float_as_uint(t);
+            c[e] = t - kRoundMagic;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+        unsigned u = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) u |= (bits[4 * i + e] & 15u) << (4 * e);
+        units[i] = u;
+    }
 }
-__device__ __forceinline__ float quant_reciprocal(float s) { return __fdiv_rn(1.f, s); }
 
 // ---- codes as matrix operands ----
 // Four bits masked into the low end of a 16-bit lane ARE an fp16 number: the subnormal c * 2^-24 (bits 0-3)
@@ -123,19 +147,31 @@ __device__ __forceinline__ float half_part(float v, int low)
     const float h = __half2float(__float2half_rn(v));
     return low ? v - h : v;
 }
-// Exponent x with m = max |v| in [2^(x-1), 2^x); 0 where no scaling can help (m = 0, infinite or NaN).
+// Exponent x with m = max |v| in [2^(x-1), 2^x), at least -100; 14 where no scaling can help (m = 0, infinite or NaN).
 __device__ __forceinline__ int range_exponent(float m)
 {
-    if (!(m > 0.f) || m > 3.4028235e38f) return 14;
-    int x;
-    frexpf(m, &x);
-    return x < -100 ? -100 : x;
+    const int e = (int)(__float_as_uint(m) >> 23) - 126;
+    return m == 0.f || e > 128 ? 14 : (e < -100 ? -100 : e);
 }
+// 2^e for -126 <= e <= 127.
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }
 __device__ __forceinline__ float exp2_fast(float v)
 {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
+}
+
+// The word of the j-th step over a row piece of 32 H values, from the words a lane loads (units 2 tig and 2 tig + 1: H / 2
+// words each).  Steps 2 p and 2 p + 1 cover blocks 2 p and 2 p + 1 of 32 values.  In groups of 64 or 128 the words serve as
+// they are, a word's two halves being the two blocks: step 2 p takes unit 2 tig, step 2 p + 1 unit 2 tig + 1, and code e of a
+// half-word stands for value 8 tig + e (4 more in the second step).  In groups of 32 the two blocks have to stay
+// apart: step j takes block j of both units, and code e stands for values 8 tig + e and 8 tig + 4 + e.
+template <int G, int H>
+__device__ __forceinline__ uint32_t code_word(const uint32_t (&w)[H], int j)
+{
+    if (G == 32) return __byte_perm(w[j / 2], w[H / 2 + j / 2], j & 1 ? 0x7632 : 0x5410);
+    return w[(j & 1) * (H / 2) + j / 2];
 }
 
 // ---- bounded wait on a copy barrier ----

@@ -40,13 +40,15 @@ w4_quantize_kernel(const T* __restrict__ w, int N, int K, long long sn, long lon
         group_range(lo, hi, lanes);
         QuantPair p = quant_pair(lo, hi);
         if (n0 + r >= N || k0 + (lane & ~(lanes - 1)) * 4 >= K) p.s = p.o = __ushort_as_half((unsigned short)0);   // wholly beyond the matrix
-        const float s = __half2float(p.s), o = __half2float(p.o), rs = quant_reciprocal(s);
-        unsigned unit = 0;
+        unsigned unit[1];
+        float c[4];
+        quant_codes<4>(x, __half2float(p.s), __half2float(p.o), unit, c);
+        if (n0 + r >= N) unit[0] = 0u;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (k0 + lane * 4 + e < K && n0 + r < N) unit |= quant_code(x[e], s, o, rs) << (4 * e);
+            if (k0 + lane * 4 + e >= K) unit[0] &= ~(15u << (4 * e));
         uint8_t* row = codes + (((size_t)rt * KB + kb) * 16 + r) * 64;
-        *reinterpret_cast<uint16_t*>(row + unit_offset(lane * 4, 4)) = (uint16_t)unit;
+        *reinterpret_cast<uint16_t*>(row + unit_offset(lane * 4, 4)) = (uint16_t)unit[0];
         if ((lane & (lanes - 1)) == 0) {
             const size_t per = 128 / group;
             pairs[(((size_t)rt * KB + kb) * per + lane / lanes) * 16 + r] = __halves2half2(p.s, p.o);
@@ -147,19 +149,35 @@ __device__ __forceinline__ void stage_x(const W4Args& a, int kb0, int nkb, uint4
                 m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
                 sum += __shfl_xor_sync(0xffffffffu, sum, d);
             }
+            // p[e], q[e]: the two entries that code e of a lane's word stands beside (see the note on words below)
+            float p[4], q[4];
+            if (G == 32) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    p[e] = v[u][e];
+                    q[e] = v[u][4 + e];
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float other = __shfl_xor_sync(0xffffffffu, h & 1 ? v[u][e] : v[u][4 + e], 4);
+                    p[e] = h & 1 ? other : v[u][e];
+                    q[e] = h & 1 ? v[u][4 + e] : other;
+                }
+            }
             if (t >= tasks) continue;
             const int x = range_exponent(m);
-            const float up = ldexpf(1.f, 14 - x), up16 = up * (1.f / 16.f);   // odd codes stand 16 times higher
+            const float up = pow2(14 - x), up16 = up * (1.f / 16.f);          // odd codes stand 16 times higher
 #pragma unroll
             for (int part = 0; part < (SPLIT ? 2 : 1); ++part) {
                 uint4 f;
-                f.x = pack_half2(half_part(v[u][0] * up, part), half_part(v[u][4] * up, part));
-                f.y = pack_half2(half_part(v[u][2] * up, part), half_part(v[u][6] * up, part));
-                f.z = pack_half2(half_part(v[u][1] * up16, part), half_part(v[u][5] * up16, part));
-                f.w = pack_half2(half_part(v[u][3] * up16, part), half_part(v[u][7] * up16, part));
+                f.x = pack_half2(half_part(p[0] * up, part), half_part(q[0] * up, part));
+                f.y = pack_half2(half_part(p[2] * up, part), half_part(q[2] * up, part));
+                f.z = pack_half2(half_part(p[1] * up16, part), half_part(q[1] * up16, part));
+                f.w = pack_half2(half_part(p[3] * up16, part), half_part(q[3] * up16, part));
                 xs[((kb * 4 + h) * slots + (SPLIT ? 2 * b + part : b)) * 4 + tig] = f;
             }
-            if ((l16 & (G / 8 - 1)) == 0) xg[(kb * PER + l16 / (G / 8)) * a.batch + b] = make_float2(ldexpf(1.f, x - 14), sum);
+            if ((l16 & (G / 8 - 1)) == 0) xg[(kb * PER + l16 / (G / 8)) * a.batch + b] = make_float2(pow2(x - 14), sum);
         }
     }
 }
@@ -220,6 +238,8 @@ __global__ void __launch_bounds__(kW4Threads, 1) w4_matvec_kernel(const __grid_c
     } else {
         // --------------------------------------------------------------- consumers --
         const int gid = lane >> 2, tig = lane & 3;
+        // columns beyond the rows of x repeat the first one; nobody reads their sums
+        const int xcol0 = (gid < slots ? gid : 0) * 4 + tig, xcol1 = (8 + gid < slots ? 8 + gid : 0) * 4 + tig;
         int par = 0;
         for (int g0 = first; g0 < last; g0 += kW4TileGroup) {
             const int g1 = g0 + kW4TileGroup < last ? g0 + kW4TileGroup : last;
@@ -254,15 +274,13 @@ __global__ void __launch_bounds__(kW4Threads, 1) w4_matvec_kernel(const __grid_c
                                     for (int e = 0; e < 4; ++e) acc[m][e] = 0.f;
 #pragma unroll
                                 for (int j = g * G / 32; j < (g + 1) * G / 32; ++j) {
-                                    const uint32_t x0 = __byte_perm(w0[j / 2], w0[2 + j / 2], j & 1 ? 0x7632 : 0x5410);
-                                    const uint32_t x1 = __byte_perm(w1[j / 2], w1[2 + j / 2], j & 1 ? 0x7632 : 0x5410);
+                                    const uint32_t x0 = code_word<G, 4>(w0, j), x1 = code_word<G, 4>(w1, j);
                                     const uint32_t y0 = x0 >> 8, y1 = x1 >> 8;
                                     const uint4* xf = xs + (size_t)(kb * 4 + j) * slots * 4;
 #pragma unroll
                                     for (int m = 0; m < (SPLIT ? 2 : 1); ++m) {
                                         if (m == 1 && halves == 1) break;
-                                        uint4 f = make_uint4(0u, 0u, 0u, 0u);
-                                        if (m * 8 + gid < slots) f = xf[(m * 8 + gid) * 4 + tig];
+                                        const uint4 f = xf[m == 0 ? xcol0 : xcol1];
                                         mma_16816(acc[m], x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, f.x, f.y);
                                         mma_16816(acc[m], x0 & 0x00f000f0u, x1 & 0x00f000f0u, y0 & 0x00f000f0u, y1 & 0x00f000f0u, f.z, f.w);
                                     }
