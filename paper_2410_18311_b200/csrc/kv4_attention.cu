@@ -11,8 +11,10 @@
 // P^T made from the accumulators of S^T by movmatrix.  tcgen05 would leave most of its 128 rows empty, and its
 // operands would have to be widened in shared memory first.
 //
-// kv4_attention_kernel: persistent CTAs of 8 warps over a ring of stages (128 slots of one sequence and head: four
-// bulk copies, all contiguous).  The warps take turns at refilling the stage of the tile before: a ninth warp for
+// kv4_attention_kernel: persistent CTAs of 8 warps over a ring of stages, each the keys or the values of a tile of up to
+// 256 slots of one sequence and head (two bulk copies, contiguous).  Keys and values are stages of their own so
+// that the keys' buffer is on its way again while the values are worked on.  The warps take turns at
+// refilling the stage used two steps before: a ninth warp for
 // the copies would cut the registers of a thread from 128 to 96 at two CTAs per SM.  The tiles of all (sequence, head)
 // units form one list, cut into equal pieces, one per CTA, whatever the lengths are; a unit that is cut leaves
 // partial results (maximum, sum, output) in the workspace.  kv4_finish_kernel joins those, and turns the
@@ -26,12 +28,12 @@
 
 namespace coreinfer {
 
-// Slots per stage: two pieces of 16 per warp, so that waits, votes and addresses are paid once per 32 slots; one piece
-// where two stages of that size do not fit beside the join buffer (head_dim 256, and 128 in groups of 32).
+// Slots per tile: two pieces of 16 per warp, so that waits, votes and addresses are paid once per 32 slots; one piece
+// where registers (head_dim 128 in groups of 32) or shared memory (256) do not carry two.
 template <int D, int G> constexpr int kAttnTile = D == 256 || (D == 128 && G == 32) ? 128 : 256;
 constexpr int kAttnWarps = 8;
 constexpr int kAttnThreads = 32 * kAttnWarps;
-constexpr int kAttnMaxStages = 8;
+constexpr int kAttnMaxStages = 10;
 constexpr int kAttnMaxCtas = 320;
 constexpr float kNoLogit = -1e30f;
 
@@ -47,7 +49,7 @@ struct AttnArgs {
     int RB;                 // units per (sequence, key head)
     int n_ctas;             // CTAs of the main kernel
     int stages;
-    int tile;               // slots per stage
+    int tile;               // slots per tile
     float scale;
     int accumulate;
     unsigned* status;
@@ -100,6 +102,15 @@ __device__ __forceinline__ void ld_words(uint32_t (&w)[N], const uint8_t* p)
 }
 __device__ __forceinline__ float2 pair_f32(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
 
+// Four neighbouring outputs; the address is a multiple of four elements.
+template <typename T>
+__device__ __forceinline__ void store4(T* dst, float x, float y, float z, float w)
+{
+    T v[4] = {from_f32<T>(x), from_f32<T>(y), from_f32<T>(z), from_f32<T>(w)};
+    if (sizeof(T) == 4) *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<uint4*>(v);
+    else *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<uint2*>(v);
+}
+
 // Position in the list of tiles.
 struct Cursor {
     int b, hr, tile, nt;
@@ -118,7 +129,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
     constexpr int UN = TILE / (16 * kAttnWarps);             // pieces of 16 slots per step of a warp
     constexpr uint32_t CODE_ROW = D / 2, PAIR_ROW = NG * 4;
     constexpr uint32_t CODE_TILE = TILE * CODE_ROW, PAIR_TILE = TILE * PAIR_ROW;
-    constexpr uint32_t STAGE = 2 * (CODE_TILE + PAIR_TILE);
+    constexpr uint32_t STAGE = CODE_TILE + PAIR_TILE;
     const Kv4& c = a.c;
 
     extern __shared__ __align__(128) uint8_t smem[];
@@ -168,6 +179,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
     const AttnCut cut(a.n_ctas, total);
     const int me = blockIdx.x;
     const int begin = me < cut.n ? cut.start(me) : 0, end = me < cut.n ? cut.start(me + 1) : 0;
+    auto token_of = [&](int r) { return a.T == 1 ? 0 : r / a.share; };       // of a query row
     auto seek = [&](int t) {
         Cursor k;
         int lo = 0, hi = c.B - 1;                           // last b with pre[b] * HR <= t: it has tiles
@@ -182,37 +194,35 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
         k.tile = (int)(rem % (unsigned)k.nt);
         return k;
     };
-    // One thread: the copies of a tile into stage s.
-    auto fetch = [&](int b, int hr, int tile, int s) {
+    // One thread: the copies of a tile's keys (which = 0) or values into stage s.
+    auto fetch = [&](int b, int hr, int tile, int which, int s) {
         const int t0 = tile * TILE;
         // whole 16-slot pieces: the capacity is a multiple of 16, so they lie within the buffers
         const int left = (lens[b] - t0 + 15) & ~15;
         const uint32_t rows = left < TILE ? left : TILE;
         const size_t slot = ((size_t)b * c.H + hr / a.RB) * c.cap + t0;
         const uint32_t bar = smem_u32(&full_bar[s]), dst = smem_u32(smem + (size_t)s * STAGE);
-        mbar_arrive_expect_tx(bar, 2 * rows * (CODE_ROW + PAIR_ROW));
-        bulk_g2s(dst, c.codes[0] + slot * CODE_ROW, rows * CODE_ROW, bar);
-        bulk_g2s(dst + CODE_TILE, reinterpret_cast<const uint8_t*>(c.pairs[0]) + slot * PAIR_ROW, rows * PAIR_ROW, bar);
-        bulk_g2s(dst + CODE_TILE + PAIR_TILE, c.codes[1] + slot * CODE_ROW, rows * CODE_ROW, bar);
-        bulk_g2s(dst + 2 * CODE_TILE + PAIR_TILE, reinterpret_cast<const uint8_t*>(c.pairs[1]) + slot * PAIR_ROW, rows * PAIR_ROW, bar);
+        mbar_arrive_expect_tx(bar, rows * (CODE_ROW + PAIR_ROW));
+        bulk_g2s(dst, c.codes[which] + slot * CODE_ROW, rows * CODE_ROW, bar);
+        bulk_g2s(dst + CODE_TILE, reinterpret_cast<const uint8_t*>(c.pairs[which]) + slot * PAIR_ROW, rows * PAIR_ROW, bar);
     };
 
     if (begin < end) {
-        if (tid == 0)
-            for (int s = 0; s < a.stages && begin + s < end; ++s) {
-                const Cursor p = seek(begin + s);
-                fetch(p.b, p.hr, p.tile, s);
+        for (int s = warp; s < a.stages && s < 2 * (end - begin); s += kAttnWarps)       // the first stages, one warp each
+            if (lane == 0) {
+                const Cursor p = seek(begin + s / 2);
+                fetch(p.b, p.hr, p.tile, s & 1, s);
             }
+        __syncwarp();
         const int rt = warp % a.RT, sg = warp / a.RT, nsg = kAttnWarps / a.RT;
         const int gid = lane >> 2, tig = lane & 3;
         const int tok0 = (gid >> 1) + (gid & 1) * 4;         // slot of accumulator row gid within 8; row gid + 8: tok0 + 8
         Cursor k = seek(begin);
         int s = 0;
         uint32_t ph = 0;
-        int t = begin, prev = a.stages - 1;                  // prev: the stage of the tile before
-        uint32_t prev_ph = 0;
+        int t = begin, step = 0;                             // step 2 i: keys of the CTA's tile i, 2 i + 1: its values
         while (t < end) {
-            const int first_tile = k.tile, b = k.b, len = lens[b], h = k.hr / a.RB, rb = k.hr % a.RB;
+            const int first_tile = k.tile, b = k.b, len = lens[b], h = a.RB == 1 ? k.hr : k.hr / a.RB, rb = k.hr - h * a.RB;
             const int n_tiles = end - t < k.nt - first_tile ? end - t : k.nt - first_tile;
             const int row0 = rb * a.RU + rt * RPT;           // first query row of this warp's tile
 
@@ -223,8 +233,8 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
             {
                 const int r = row0 + (WIDE ? gid >> 1 : gid);
                 const bool valid = r < a.R && (MODE != kRows4 || (gid & 1) == 0);
-                const T* src = (const T*)a.q + ((long long)b * a.T + (valid ? r / a.share : 0)) * a.ld_q +
-                               (long long)(h * a.share + (valid ? r % a.share : 0)) * D + 8 * tig;
+                const int rt_ = valid ? token_of(r) : 0, rh = valid ? r - rt_ * a.share : 0;
+                const T* src = (const T*)a.q + ((long long)b * a.T + rt_) * a.ld_q + (long long)(h * a.share + rh) * D + 8 * tig;
                 float v[H32][8], m = 0.f;
 #pragma unroll
                 for (int j = 0; j < H32; ++j) {
@@ -279,7 +289,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                     for (int g = 0; g < NG; ++g) qsum[g][i] = __shfl_sync(0xffffffffu, gs[g], from);
                     f[i] = __shfl_sync(0xffffffffu, ff, from);
                     const int rr = row0 + (WIDE ? tig : 2 * tig + i);
-                    lim[i] = rr < a.R ? len - (a.T - 1 - rr / a.share) : 0;
+                    lim[i] = rr < a.R ? len - (a.T - 1 - token_of(rr)) : 0;
                 }
             }
             float* lg[NV];                                   // this lane's logits, NULL where none are kept
@@ -306,23 +316,42 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                 for (int g = 0; g < NG; ++g) om[g][i] = 0.f;
             }
 
-            for (int it = 0; it < n_tiles; ++it) {
-                const int t0 = (first_tile + it) * TILE;
-                const int refill = t + it - 1 + a.stages;    // goes where tile t + it - 1 was
-                if (warp == ((t + it) & (kAttnWarps - 1)) && lane == 0 && t + it > begin && refill < end) {
-                    bounded_wait(smem_u32(&empty_bar[prev]), prev_ph, abort_flag, a.status);
+            // Into a step: refill the stage of two steps before (every warp has left it, or will without this one), then
+            // wait for this step's stage.
+            auto enter = [&]() {
+                const int refill = step - 2 + a.stages;
+                if (warp == (step & (kAttnWarps - 1)) && lane == 0 && step >= 2 && refill < 2 * (end - begin)) {
+                    const int was = s >= 2 ? s - 2 : s - 2 + a.stages;
+                    bounded_wait(smem_u32(&empty_bar[was]), s >= 2 ? ph : ph ^ 1u, abort_flag, a.status);
                     if (!*abort_flag) {
-                        if (first_tile + it - 1 + a.stages < k.nt) {
-                            fetch(b, k.hr, first_tile + it - 1 + a.stages, prev);
+                        const int tile = begin + (refill >> 1) - t + first_tile;
+                        if (tile < k.nt) {
+                            fetch(b, k.hr, tile, refill & 1, was);
                         } else {
-                            const Cursor p = seek(refill);
-                            fetch(p.b, p.hr, p.tile, prev);
+                            const Cursor p = seek(begin + (refill >> 1));
+                            fetch(p.b, p.hr, p.tile, refill & 1, was);
                         }
                     }
                 }
                 __syncwarp();
                 bounded_wait(smem_u32(&full_bar[s]), ph, abort_flag, a.status);
-                const uint8_t* st = smem + (size_t)s * STAGE;
+                const int here = s;
+                ++step;
+                if (++s == a.stages) { s = 0; ph ^= 1u; }
+                return here;
+            };
+            auto leave = [&](int stage) {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&empty_bar[stage]));
+            };
+
+            for (int it = 0; it < n_tiles; ++it) {
+                const int t0 = (first_tile + it) * TILE;
+                const int ks = enter();
+                int vs = -1;
+                bool keys_left = false;
+                const uint8_t* kst = smem + (size_t)ks * STAGE;
+                const uint8_t* vst = nullptr;
                 for (int sub = UN * sg; sub < TILE / 16; sub += UN * nsg) {
                     const int n0 = t0 + sub * 16;
                     if (n0 >= len) break;
@@ -330,11 +359,11 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                     float lo[UN][2][NV];
 #pragma unroll
                     for (int u = 0; u < UN; ++u) {
-                        const uint8_t* krow = st + (sub * 16 + u * 16 + tok0) * CODE_ROW + tig * (D / 8);
+                        const uint8_t* krow = kst + (sub * 16 + u * 16 + tok0) * CODE_ROW + tig * (D / 8);
                         uint32_t w0[D / 32], w1[D / 32], kp0[NG], kp1[NG];
                         ld_words<D / 32>(w0, krow);
                         ld_words<D / 32>(w1, krow + 8 * CODE_ROW);
-                        const uint8_t* kpr = st + CODE_TILE + (sub * 16 + u * 16 + tok0) * PAIR_ROW;
+                        const uint8_t* kpr = kst + CODE_TILE + (sub * 16 + u * 16 + tok0) * PAIR_ROW;
                         ld_words<NG>(kp0, kpr);
                         ld_words<NG>(kp1, kpr + 8 * PAIR_ROW);
 #pragma unroll
@@ -368,21 +397,35 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
 #pragma unroll
                         for (int u = 0; u < UN; ++u)
 #pragma unroll
-                            for (int v = 0; v < 2; ++v) {
-                                lo[u][v][i] *= f[i];
-                                if (edge && na + 16 * u + 8 * v >= lim[i]) lo[u][v][i] = -__int_as_float(0x7f800000);
-                            }
-                        most[i] = fmaxf(lo[0][0][i], lo[0][1][i]);
-#pragma unroll
-                        for (int u = 1; u < UN; ++u) most[i] = fmaxf(most[i], fmaxf(lo[u][0][i], lo[u][1][i]));
-                        if (lg[i]) {
-                            float* to = lg[i] + n0;
+                            for (int v = 0; v < 2; ++v) lo[u][v][i] *= f[i];
+                        if (edge) [[unlikely]] {
 #pragma unroll
                             for (int u = 0; u < UN; ++u)
 #pragma unroll
                                 for (int v = 0; v < 2; ++v)
-                                    if (!edge || na + 16 * u + 8 * v < lim[i]) to[16 * u + 8 * v] = lo[u][v][i];
+                                    if (na + 16 * u + 8 * v >= lim[i]) lo[u][v][i] = -__int_as_float(0x7f800000);
                         }
+                        most[i] = fmaxf(lo[0][0][i], lo[0][1][i]);
+#pragma unroll
+                        for (int u = 1; u < UN; ++u) most[i] = fmaxf(most[i], fmaxf(lo[u][0][i], lo[u][1][i]));
+                        if (lg[i]) {
+                            // what a row does not see may be written too: it lies within the capacity and is never read
+                            float* to = lg[i] + n0;
+#pragma unroll
+                            for (int u = 0; u < UN; ++u)
+                                if (UN == 1 || u == 0 || n0 + 16 < len) {
+                                    to[16 * u] = lo[u][0][i];
+                                    to[16 * u + 8] = lo[u][1][i];
+                                }
+                        }
+                    }
+                    if (n0 + 16 * UN * nsg >= len || sub + UN * nsg >= TILE / 16) {      // this warp's last step of the tile
+                        leave(ks);
+                        keys_left = true;
+                    }
+                    if (!vst) {
+                        vs = enter();
+                        vst = smem + (size_t)vs * STAGE;
                     }
                     // ---- value pairs, running maximum ----
                     uint32_t vp[UN][2][NG];
@@ -391,10 +434,13 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                     for (int u = 0; u < UN; ++u)
 #pragma unroll
                         for (int v = 0; v < 2; ++v) {
-                            ld_words<NG>(vp[u][v], st + 2 * CODE_TILE + PAIR_TILE + (sub * 16 + 16 * u + 8 * v + tok0) * PAIR_ROW);
+                            ld_words<NG>(vp[u][v], vst + CODE_TILE + (sub * 16 + 16 * u + 8 * v + tok0) * PAIR_ROW);
+                            if (edge && na + 16 * u + 8 * v >= len) [[unlikely]] {                        // never used
+#pragma unroll
+                                for (int g = 0; g < NG; ++g) vp[u][v][g] = 0u;
+                            }
 #pragma unroll
                             for (int g = 0; g < NG; ++g) {
-                                if (edge && na + 16 * u + 8 * v >= len) vp[u][v][g] = 0u;     // never used
                                 smax = __hmax2(smax, *reinterpret_cast<const __half2*>(&vp[u][v][g]));
                             }
                         }
@@ -453,7 +499,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                     // ---- O^T += V^T P^T, per group of scales ----
 #pragma unroll
                     for (int u = 0; u < UN; ++u) {
-                        const uint8_t* vrow = st + CODE_TILE + PAIR_TILE + (sub * 16 + u * 16 + tig) * CODE_ROW + gid * (D / 16);
+                        const uint8_t* vrow = vst + (sub * 16 + u * 16 + tig) * CODE_ROW + gid * (D / 16);
                         uint32_t va[H32 / 2], vb[H32 / 2], vc[H32 / 2], vd[H32 / 2];
                         ld_words<H32 / 2>(va, vrow);
                         ld_words<H32 / 2>(vb, vrow + 4 * CODE_ROW);
@@ -466,14 +512,20 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                             for (int v = 0; v < 2; ++v) {
                                 const float2 so = pair_f32(vp[u][v][g]);
                                 float ps[NV];
+                                float om_was[NV];
 #pragma unroll
                                 for (int i = 0; i < NV; ++i) {
+                                    om_was[i] = om[g][i];
                                     ps[i] = lo[u][v][i] * so.x;
-                                    if (edge && na + 16 * u + 8 * v >= lim[i]) {     // adds nothing, whatever the slot holds
-                                        ps[i] = 0.f;
-                                    } else {
-                                        om[g][i] = fmaf(lo[u][v][i], so.y, om[g][i]);
-                                    }
+                                    om[g][i] = fmaf(lo[u][v][i], so.y, om[g][i]);
+                                }
+                                if (edge) [[unlikely]] {     // a slot that a row does not see adds nothing, whatever it holds
+#pragma unroll
+                                    for (int i = 0; i < NV; ++i)
+                                        if (na + 16 * u + 8 * v >= lim[i]) {
+                                            ps[i] = 0.f;
+                                            om[g][i] = om_was[i];
+                                        }
                                 }
                                 if (PARTS) {
                                     const float high = __half2float(__float2half_rn(ps[0]));
@@ -493,11 +545,9 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                         }
                     }
                 }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&empty_bar[s]));
-                prev = s;
-                prev_ph = ph;
-                if (++s == a.stages) { s = 0; ph ^= 1u; }
+                if (!keys_left) leave(ks);                   // the tile ends before this warp's slots
+                if (!vst) vs = enter();
+                leave(vs);
             }
 
             // ---- join the warps of a row tile ----
@@ -537,32 +587,32 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
             __syncthreads();
             const bool whole = n_tiles == k.nt;
             const int piece = blockIdx.x * 2 + (first_tile == 0 ? 1 : 0);
-            for (int i = tid; i < a.RU * (D / 4); i += 32 * kAttnWarps) {
-                const int ru = i / (D / 4), d4 = i % (D / 4);
-                const int r = rb * a.RU + ru;
-                if (r >= a.R) break;
-                const int wrt = ru / RPT, slot = ru % RPT;
-                float top = kNoLogit * 2.f;
-                for (int w = wrt; w < kAttnWarps; w += a.RT) top = fmaxf(top, mlbuf[w * RPT + slot].x);
-                float sum = 0.f;
-                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-                for (int w = wrt; w < kAttnWarps; w += a.RT) {
-                    const float2 ml = mlbuf[w * RPT + slot];
-                    const float e = exp2_fast(ml.x - top);
-                    const float4 x = *reinterpret_cast<const float4*>(obuf + ((size_t)w * RPT + slot) * D + d4 * 4);
-                    sum = fmaf(ml.y, e, sum);
-                    v.x = fmaf(x.x, e, v.x);
-                    v.y = fmaf(x.y, e, v.y);
-                    v.z = fmaf(x.z, e, v.z);
-                    v.w = fmaf(x.w, e, v.w);
+            // nsg neighbouring lanes take the parts of one quad of outputs and add them up by shuffles
+            const int rows_here = a.R - rb * a.RU < a.RU ? a.R - rb * a.RU : a.RU, items = rows_here * (D / 4);
+            const int part = tid % nsg, per_round = 32 * kAttnWarps / nsg;
+            for (int i0 = 0; i0 < items; i0 += per_round) {
+                const int item = i0 + tid / nsg, ru = item < items ? item / (D / 4) : 0, d4 = item % (D / 4);
+                const int from = (part * a.RT + ru / RPT) * RPT + ru % RPT;      // row of the part's warp
+                const float2 ml = mlbuf[from];
+                const float4 x = *reinterpret_cast<const float4*>(obuf + (size_t)from * D + d4 * 4);
+                float top = ml.x;
+                for (int d = 1; d < nsg; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                const float e = exp2_fast(ml.x - top);
+                float sum = ml.y * e;
+                float4 v = make_float4(x.x * e, x.y * e, x.z * e, x.w * e);
+                for (int d = 1; d < nsg; d <<= 1) {
+                    sum += __shfl_xor_sync(0xffffffffu, sum, d);
+                    v.x += __shfl_xor_sync(0xffffffffu, v.x, d);
+                    v.y += __shfl_xor_sync(0xffffffffu, v.y, d);
+                    v.z += __shfl_xor_sync(0xffffffffu, v.z, d);
+                    v.w += __shfl_xor_sync(0xffffffffu, v.w, d);
                 }
+                if (part != 0 || item >= items) continue;
                 if (whole) {
                     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-                    T* dst = (T*)a.out + ((long long)b * a.T + r / a.share) * a.ld_out + (long long)(h * a.share + r % a.share) * D + d4 * 4;
-                    dst[0] = from_f32<T>(v.x * inv);
-                    dst[1] = from_f32<T>(v.y * inv);
-                    dst[2] = from_f32<T>(v.z * inv);
-                    dst[3] = from_f32<T>(v.w * inv);
+                    const int r = rb * a.RU + ru, rt_ = token_of(r);
+                    T* dst = (T*)a.out + ((long long)b * a.T + rt_) * a.ld_out + (long long)(h * a.share + r - rt_ * a.share) * D + d4 * 4;
+                    store4(dst, v.x * inv, v.y * inv, v.z * inv, v.w * inv);
                     if (d4 == 0 && a.accumulate) a.stats[(((size_t)b * c.H + h) * a.RB + rb) * a.RU + ru] = make_float2(top, sum);
                 } else {
                     *reinterpret_cast<float4*>(a.part_o + ((size_t)piece * a.RU + ru) * D + d4 * 4) = v;
@@ -607,29 +657,28 @@ template <typename T>
 __global__ void __launch_bounds__(kFinishThreads) kv4_finish_kernel(const __grid_constant__ AttnArgs a)
 {
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ int redi[8];
     __shared__ float redf[8];
     const Kv4& c = a.c;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int b = blockIdx.y / c.H, h = blockIdx.y % c.H, D = c.D;
     const int len = kv4_length(c, b);
     if ((int)blockIdx.x >= a.R && ((int)blockIdx.x - a.R) * kFinishSlots >= len) return;
-    int before = 0, all = 0;
-    for (int i = tid; i < c.B; i += kFinishThreads) {
+    int before = 0, all = 0;                                 // tiles of a head, before this sequence and in all; every warp for itself
+    for (int i = lane; i < c.B; i += 32) {
         const int n = attn_tiles(kv4_length(c, i), a.tile);
         all += n;
         if (i < b) before += n;
     }
-    auto add = [](int x, int y) { return x + y; };
-    before = finish_reduce(before, redi, add);
-    all = finish_reduce(all, redi, add);
+    before = __reduce_add_sync(0xffffffffu, before);
+    all = __reduce_add_sync(0xffffffffu, all);
     const int HR = c.H * a.RB, nt = attn_tiles(len, a.tile), total = all * HR;
     const AttnCut cut(a.n_ctas, total);
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
     if ((int)blockIdx.x < a.R) {
         const int r = blockIdx.x, rb = r / a.RU, ru = r % a.RU;
-        T* dst = (T*)a.out + ((long long)b * a.T + r / a.share) * a.ld_out + (long long)(h * a.share + r % a.share) * D;
+        const int rt_ = a.T == 1 ? 0 : r / a.share;
+        T* dst = (T*)a.out + ((long long)b * a.T + rt_) * a.ld_out + (long long)(h * a.share + r - rt_ * a.share) * D;
         if (nt == 0) {
             for (int d = tid; d < D; d += kFinishThreads) dst[d] = from_f32<T>(0.f);
             return;
@@ -672,10 +721,7 @@ __global__ void __launch_bounds__(kFinishThreads) kv4_finish_kernel(const __grid
                 const float4 x = buf[j * quads + d4];
                 v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
             }
-            dst[d4 * 4] = from_f32<T>(v.x * inv);
-            dst[d4 * 4 + 1] = from_f32<T>(v.y * inv);
-            dst[d4 * 4 + 2] = from_f32<T>(v.z * inv);
-            dst[d4 * 4 + 3] = from_f32<T>(v.w * inv);
+            store4(dst + d4 * 4, v.x * inv, v.y * inv, v.z * inv, v.w * inv);
         }
         return;
     }
@@ -762,16 +808,16 @@ template <typename T, int D, int G, int MODE>
 static coreinfer_status launch_mode(AttnArgs& a, const DeviceInfo& di, cudaStream_t st)
 {
     constexpr int RPT = MODE == kRows8 ? 8 : 4, NG = D / G, TILE = kAttnTile<D, G>;
-    constexpr size_t STAGE = (size_t)2 * TILE * (D / 2 + NG * 4);
+    constexpr size_t STAGE = (size_t)TILE * (D / 2 + NG * 4);
     const size_t fixed = (size_t)kAttnWarps * RPT * (D * sizeof(float) + sizeof(float2)) + (2 * a.c.B + 1) * sizeof(int);
-    // two CTAs per SM where registers (head_dim up to 128) and two stages each allow it
+    // two CTAs per SM where registers (head_dim up to 128) and four stages each allow it
     int per_sm = D <= 128 ? 2 : 1, stages = 0;
-    for (; per_sm >= 1 && stages < 2; --per_sm) {
+    for (;; --per_sm) {
         const size_t room = (smem_room(di) - (per_sm - 1) * 1024) / per_sm;
         stages = room > fixed ? (int)((room - fixed) / STAGE) : 0;
-        if (stages >= 2) break;
+        if (stages >= 4 || per_sm == 1) break;
     }
-    if (stages < 2) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "not enough shared memory for two pipeline stages");
+    if (stages < 4) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "not enough shared memory for four pipeline stages");
     if (stages > kAttnMaxStages) stages = kAttnMaxStages;
     a.stages = stages;
     a.tile = TILE;
