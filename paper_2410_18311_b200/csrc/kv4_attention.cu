@@ -11,11 +11,12 @@
 // P^T made from the accumulators of S^T by movmatrix.  tcgen05 would leave most of its 128 rows empty, and its
 // operands would have to be widened in shared memory first.
 //
-// kv4_attention_kernel: persistent CTAs of 8 warps over a ring of stages, each the keys or the values of a tile of up to
-// 256 slots of one sequence and head (two bulk copies, contiguous).  Keys and values are stages of their own so
-// that the keys' buffer is on its way again while the values are worked on.  The warps take turns at
-// refilling the stage used two steps before: a ninth warp for
-// the copies would cut the registers of a thread from 128 to 96 at two CTAs per SM.  The tiles of all (sequence, head)
+// kv4_attention_kernel: persistent CTAs of 8 warps.  Each warp walks its own slots, 32 at a time, through a ring of
+// stages of its own, each the keys or the values of those slots (cp.async, 16 bytes a lane), and refills a stage as
+// soon as it has read it: no warp waits for another before the end of a unit, and a refill costs a dozen
+// instructions.  (Bulk copies with barriers cost about 70 per 32 slots: the kernel is bound by instruction issue and
+// the ALU pipe before it is bound by memory.)  Warps that hold other rows of the same slots copy for themselves, from L2.
+// The tiles of all (sequence, head)
 // units form one list, cut into equal pieces, one per CTA, whatever the lengths are; a unit that is cut leaves
 // partial results (maximum, sum, output) in the workspace.  kv4_finish_kernel joins those, and turns the
 // logits into weights that it adds to the cache's where that is asked for.
@@ -28,14 +29,17 @@
 
 namespace coreinfer {
 
-// Slots per tile: two pieces of 16 per warp, so that waits, votes and addresses are paid once per 32 slots; one piece
+// Slots per tile (a piece per warp): pieces of 32, so that waits, votes and addresses are paid once per 32 slots; of 16
 // where registers (head_dim 128 in groups of 32) or shared memory (256) do not carry two.
 template <int D, int G> constexpr int kAttnTile = D == 256 || (D == 128 && G == 32) ? 128 : 256;
 constexpr int kAttnWarps = 8;
 constexpr int kAttnThreads = 32 * kAttnWarps;
-constexpr int kAttnMaxStages = 10;
 constexpr int kAttnMaxCtas = 320;
 constexpr float kNoLogit = -1e30f;
+// A unit counts this many tiles more than it has when the list is cut: about what starting it costs a CTA (its query
+// rows, the join of its warps).  Measured at 8 sequences x 32 heads x 4096 slots: CTAs with two units ended 3 to 6 us
+// after those with one when this was 0.
+constexpr int kAttnUnitCost = 2;
 
 struct AttnArgs {
     Kv4 c;
@@ -48,11 +52,9 @@ struct AttnArgs {
     int RU;                 // rows per unit: RT * 8 or RT * 4
     int RB;                 // units per (sequence, key head)
     int n_ctas;             // CTAs of the main kernel
-    int stages;
     int tile;               // slots per tile
     float scale;
     int accumulate;
-    unsigned* status;
     float2* part_ml;        // [n_ctas][2][RU]: reference exponent and sum of a cut unit's piece
     float* part_o;          // [n_ctas][2][RU][D]
     float2* stats;          // [B][H][RB][RU]: the same of whole units, for the weights
@@ -60,7 +62,9 @@ struct AttnArgs {
 };
 
 __device__ __forceinline__ int attn_tiles(int len, int tile) { return (len + tile - 1) / tile; }
-// The list of tiles in n equal pieces, the first `more` of them one longer; every CTA that works has one tile at least.
+// Entries of a unit in the list that is cut: kAttnUnitCost without work, then its tiles.
+__device__ __forceinline__ int attn_entries(int tiles) { return tiles ? tiles + kAttnUnitCost : 0; }
+// The list in n equal pieces, the first `more` of them one longer; every piece has one entry at least.
 struct AttnCut {
     int n, each, more;
     __device__ __forceinline__ AttnCut(int n_ctas, int total)
@@ -111,6 +115,45 @@ __device__ __forceinline__ void store4(T* dst, float x, float y, float z, float 
     else *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<uint2*>(v);
 }
 
+// The eight values of one (16-bit types) or two 16-byte words.
+template <typename T>
+__device__ __forceinline__ void unpack8(const uint4* raw, float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+        const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (sizeof(T) == 4) v[4 * i + e] = __uint_as_float(w[e]);
+            else {
+                v[2 * e] = to_f32<T>(*reinterpret_cast<const T*>(&w[e]));
+                const uint32_t high = w[e] >> 16;
+                v[2 * e + 1] = to_f32<T>(*reinterpret_cast<const T*>(&high));
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// A condition that is rarely true and the same for the warp: used as the bound of a loop of at most one round, so that
+// the compiler branches around the body instead of executing it under a predicate.
+__device__ __forceinline__ int opaque_zero()
+{
+    int z;
+    asm volatile("mov.u32 %0, 0;" : "=r"(z));
+    return z;
+}
+
+// Stages of a warp's ring: as many as two CTAs per SM (head_dim 256: one) leave room for.
+template <int D, int G, int MODE> constexpr int kAttnStages =
+    D == 64 ? 9 : (D == 256 ? (G == 32 ? 6 : 8) : (G == 32 ? (MODE == 0 ? 7 : 9) : (MODE == 0 ? 4 : 5)));
+
 // Position in the list of tiles.
 struct Cursor {
     int b, hr, tile, nt;
@@ -128,51 +171,45 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
     constexpr int H32 = D / 32, NG = D / G, RPT = WIDE ? 4 : 8, NV = WIDE ? 1 : 2, TILE = kAttnTile<D, G>;
     constexpr int UN = TILE / (16 * kAttnWarps);             // pieces of 16 slots per step of a warp
     constexpr uint32_t CODE_ROW = D / 2, PAIR_ROW = NG * 4;
-    constexpr uint32_t CODE_TILE = TILE * CODE_ROW, PAIR_TILE = TILE * PAIR_ROW;
-    constexpr uint32_t STAGE = CODE_TILE + PAIR_TILE;
+    constexpr int CH = 16 * UN;                              // slots of a piece
+    constexpr int STAGES = kAttnStages<D, G, MODE>;
+    constexpr uint32_t CODES = CH * CODE_ROW, PAIRS = CH * PAIR_ROW, STAGE = CODES + PAIRS;
+    static_assert(CODES % 512 == 0 && PAIRS % 16 == 0 && PAIRS <= 512, "copies of 16 bytes a lane");
     const Kv4& c = a.c;
 
     extern __shared__ __align__(128) uint8_t smem[];
-    float* obuf = reinterpret_cast<float*>(smem + (size_t)a.stages * STAGE);                // [8 warps][RPT][D]
+    float* obuf = reinterpret_cast<float*>(smem + (size_t)kAttnWarps * STAGES * STAGE);                // [8 warps][RPT][D]
     float2* mlbuf = reinterpret_cast<float2*>(obuf + kAttnWarps * RPT * D);                  // [8 warps][RPT]
-    int* pre = reinterpret_cast<int*>(mlbuf + kAttnWarps * RPT);                             // [B + 1] tiles of a head before sequence b
-    int* lens = pre + c.B + 1;                                                               // [B]
-    __shared__ uint64_t full_bar[kAttnMaxStages], empty_bar[kAttnMaxStages];
-    __shared__ int abort_s;
-    volatile int* abort_flag = &abort_s;
-
+    int* pre = reinterpret_cast<int*>(mlbuf + kAttnWarps * RPT);                             // [B + 1] entries of a head before sequence b
+    int* tiles_before = pre + c.B + 1;                                                       // [B] tiles of a head before sequence b
+    int* lens = tiles_before + c.B;                                                          // [B]
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    if (tid == 0) {
-        for (int s = 0; s < a.stages; ++s) {
-            mbar_init(smem_u32(&full_bar[s]), 1);
-            mbar_init(smem_u32(&empty_bar[s]), kAttnWarps);
-        }
-        abort_s = 0;
-        mbar_fence_init();
-        if (blockIdx.x == 0) *a.status = kStatusOk;          // a wait gives up seconds later at the earliest
-    }
+    wait_for_stream();       // nothing of an earlier kernel is read or overwritten above
     if (warp == 0) {
-        int run = 0;
+        int run = 0, idle = 0;                               // entries, and those without work, so far
         for (int b0 = 0; b0 < c.B; b0 += 32) {
             const int b = b0 + lane;
             const int len = b < c.B ? kv4_length(c, b) : 0;
-            const int v = attn_tiles(len, TILE);
+            const int tiles = attn_tiles(len, TILE), v = attn_entries(tiles);
             int incl = v;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const int u = __shfl_up_sync(0xffffffffu, incl, o);
                 if (lane >= o) incl += u;
             }
+            const unsigned used = __ballot_sync(0xffffffffu, tiles > 0);
             if (b < c.B) {
                 lens[b] = len;
                 pre[b] = run + incl - v;
+                tiles_before[b] = pre[b] - idle - __popc(used & ((1u << lane) - 1u)) * kAttnUnitCost;
             }
+            idle += __popc(used) * kAttnUnitCost;
             run += __shfl_sync(0xffffffffu, incl, 31);
         }
         if (lane == 0) pre[c.B] = run;
     }
     __syncthreads();
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    let_next_start();
 
     const int HR = c.H * a.RB;
     const int total = pre[c.B] * HR;
@@ -180,50 +217,130 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
     const int me = blockIdx.x;
     const int begin = me < cut.n ? cut.start(me) : 0, end = me < cut.n ? cut.start(me + 1) : 0;
     auto token_of = [&](int r) { return a.T == 1 ? 0 : r / a.share; };       // of a query row
+    // The unit and tile of entry t of the list; tile < 0: an entry without work before the unit's first tile.
     auto seek = [&](int t) {
         Cursor k;
-        int lo = 0, hi = c.B - 1;                           // last b with pre[b] * HR <= t: it has tiles
+        int lo = 0, hi = c.B - 1;                            // last b with pre[b] * HR <= t: it has entries
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
             if (pre[mid] * HR <= t) lo = mid; else hi = mid - 1;
         }
         k.b = lo;
         k.nt = attn_tiles(lens[lo], TILE);
-        const unsigned rem = (unsigned)(t - pre[lo] * HR);
-        k.hr = (int)(rem / (unsigned)k.nt);
-        k.tile = (int)(rem % (unsigned)k.nt);
+        const unsigned rem = (unsigned)(t - pre[lo] * HR), per = (unsigned)(k.nt + kAttnUnitCost);
+        k.hr = (int)(rem / per);
+        k.tile = (int)(rem - k.hr * per) - kAttnUnitCost;
         return k;
     };
-    // One thread: the copies of a tile's keys (which = 0) or values into stage s.
-    auto fetch = [&](int b, int hr, int tile, int which, int s) {
-        const int t0 = tile * TILE;
-        // whole 16-slot pieces: the capacity is a multiple of 16, so they lie within the buffers
-        const int left = (lens[b] - t0 + 15) & ~15;
-        const uint32_t rows = left < TILE ? left : TILE;
-        const size_t slot = ((size_t)b * c.H + hr / a.RB) * c.cap + t0;
-        const uint32_t bar = smem_u32(&full_bar[s]), dst = smem_u32(smem + (size_t)s * STAGE);
-        mbar_arrive_expect_tx(bar, rows * (CODE_ROW + PAIR_ROW));
-        bulk_g2s(dst, c.codes[which] + slot * CODE_ROW, rows * CODE_ROW, bar);
-        bulk_g2s(dst + CODE_TILE, reinterpret_cast<const uint8_t*>(c.pairs[which]) + slot * PAIR_ROW, rows * PAIR_ROW, bar);
+    // This CTA's tiles from a cursor on: a tile, then the next one of the unit or the first of the next unit.
+    auto advance = [&](Cursor k, int tiles) {
+        while (tiles > 0) {
+            if (k.tile + tiles < k.nt) {
+                k.tile += tiles;
+                break;
+            }
+            tiles -= k.nt - k.tile;
+            k.tile = 0;
+            if (++k.hr == HR) {
+                k.hr = 0;
+                do { ++k.b; } while (k.b < c.B && lens[k.b] == 0);
+                k.nt = k.b < c.B ? attn_tiles(lens[k.b], TILE) : 0x40000000;
+            }
+        }
+        return k;
     };
 
     if (begin < end) {
-        for (int s = warp; s < a.stages && s < 2 * (end - begin); s += kAttnWarps)       // the first stages, one warp each
-            if (lane == 0) {
-                const Cursor p = seek(begin + s / 2);
-                fetch(p.b, p.hr, p.tile, s & 1, s);
-            }
-        __syncwarp();
-        const int rt = warp % a.RT, sg = warp / a.RT, nsg = kAttnWarps / a.RT;
         const int gid = lane >> 2, tig = lane & 3;
+        const int rt = warp % a.RT, sg = warp / a.RT, nsg = kAttnWarps / a.RT;
         const int tok0 = (gid >> 1) + (gid & 1) * 4;         // slot of accumulator row gid within 8; row gid + 8: tok0 + 8
         Cursor k = seek(begin);
-        int s = 0;
-        uint32_t ph = 0;
-        int t = begin, step = 0;                             // step 2 i: keys of the CTA's tile i, 2 i + 1: its values
-        while (t < end) {
+        // tiles of this CTA: from the first at or after entry `begin` to the last before entry `end`
+        auto tile_number = [&](const Cursor& k) { return tiles_before[k.b] * HR + k.hr * k.nt + (k.tile < 0 ? 0 : k.tile); };
+        const Cursor z = seek(end - 1);
+        const int n_total = tile_number(z) + (z.tile >= 0) - tile_number(k);
+        if (k.tile < 0) k.tile = 0;
+        uint4 raw[H32][sizeof(T) / 2];                       // query rows of the unit at hand as they are in memory
+        auto load_q = [&](const Cursor& k) {
+            const int h = a.RB == 1 ? k.hr : k.hr / a.RB, rb = k.hr - h * a.RB;
+            const int r = rb * a.RU + rt * RPT + (WIDE ? gid >> 1 : gid);
+            const int rr = r < a.R && (MODE != kRows4 || (gid & 1) == 0) ? r : 0, rt_ = token_of(rr);
+            const T* src = (const T*)a.q + ((long long)k.b * a.T + rt_) * a.ld_q + (long long)(h * a.share + rr - rt_ * a.share) * D + 8 * tig;
+#pragma unroll
+            for (int j = 0; j < H32; ++j)
+#pragma unroll
+                for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[j][i] = reinterpret_cast<const uint4*>(src + j * 32)[i];
+        };
+        if (n_total > 0) load_q(k);
+        // ---- this warp's ring ----
+        const int stride = nsg * CH;
+        const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * STAGES) * STAGE;
+        // Where the copies stand: the segment (the CTA's tiles of one unit) and the warp's next piece in it.
+        int f_b = k.b, f_hr = k.hr, f_t = 0, f_n0 = 0, f_end = 0;            // f_t: tiles before the segment's end
+        uint32_t f_slot = 0;                                 // 2^32 slots would be more than the GPU holds
+        auto feed_open = [&](int tile, int t) {
+            for (;;) {
+                const int len = lens[f_b], nt = attn_tiles(len, TILE), n = n_total - t < nt - tile ? n_total - t : nt - tile;
+                f_t = t + n;
+                f_n0 = tile * TILE + sg * CH;
+                f_end = (tile + n) * TILE < len ? (tile + n) * TILE : len;
+                f_slot = (uint32_t)(f_b * c.H + (a.RB == 1 ? f_hr : f_hr / a.RB)) * (uint32_t)c.cap + (uint32_t)f_n0;
+                if (f_n0 < f_end || f_t >= n_total) break;
+                tile = 0;
+                t = f_t;
+                if (++f_hr == HR) {
+                    f_hr = 0;
+                    do { ++f_b; } while (lens[f_b] == 0);    // there are tiles left, so there is such a sequence
+                }
+            }
+        };
+        // Copies the next piece's keys (which = 0) or values to shared address `at`; after the values on to the next piece.
+        auto feed = [&](uint32_t at, int which) {
+            if (f_n0 < f_end) {
+                // whole 16-slot rows: the capacity is a multiple of 16, so they lie within the buffers
+                const uint32_t rows = f_end - f_n0 > CH - 16 ? CH : 16;
+                const uint8_t* codes = c.codes[which] + (size_t)f_slot * CODE_ROW + lane * 16;
+                const uint8_t* pairs = reinterpret_cast<const uint8_t*>(c.pairs[which]) + (size_t)f_slot * PAIR_ROW + lane * 16;
+#pragma unroll
+                for (uint32_t i = 0; i < CODES; i += 512)
+                    if (i < 16 * CODE_ROW || rows == CH) copy16(at + lane * 16 + i, codes + i);
+                if (lane * 16 < rows * PAIR_ROW) copy16(at + CODES + lane * 16, pairs);
+                if (which) {
+                    f_n0 += stride;
+                    f_slot += stride;
+                    if (f_n0 >= f_end && f_t < n_total) {
+                        if (++f_hr == HR) {
+                            f_hr = 0;
+                            do { ++f_b; } while (lens[f_b] == 0);
+                        }
+                        feed_open(0, f_t);
+                    }
+                }
+            }
+            copy_commit();                                   // one group per stage, empty ones too
+        };
+        if (n_total > 0) {                                   // after the query rows, which would wait behind these copies
+            feed_open(k.tile, 0);
+#pragma unroll 1
+            for (int s = 0; s < STAGES; ++s) feed(ring + s * STAGE, s & 1);
+        }
+        uint32_t stage = 0;                                  // offset of the stage at hand in the ring
+        int t = 0;                                           // tiles done
+        // Into a step: its stage has arrived, for every lane.  Out of it: all lanes have read it; it takes the piece STAGES
+        // steps on.
+        auto enter = [&]() {
+            copy_wait<STAGES - 1>();
+            __syncwarp();
+            return smem + (size_t)(warp * STAGES) * STAGE + stage;
+        };
+        auto leave = [&](int which) {
+            __syncwarp();
+            feed(ring + stage, STAGES & 1 ? which ^ 1 : which);
+            stage = stage + STAGE == STAGES * STAGE ? 0 : stage + STAGE;
+        };
+        while (t < n_total) {
             const int first_tile = k.tile, b = k.b, len = lens[b], h = a.RB == 1 ? k.hr : k.hr / a.RB, rb = k.hr - h * a.RB;
-            const int n_tiles = end - t < k.nt - first_tile ? end - t : k.nt - first_tile;
+            const int n_tiles = n_total - t < k.nt - first_tile ? n_total - t : k.nt - first_tile;
             const int row0 = rb * a.RU + rt * RPT;           // first query row of this warp's tile
 
             // query rows as the B operand: column gid = row gid (or part gid & 1 of row gid >> 1), 8 values per 32
@@ -231,20 +348,14 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
             float qsum[NG][NV], f[NV];
             int lim[NV];                                     // slots this lane's columns see
             {
-                const int r = row0 + (WIDE ? gid >> 1 : gid);
-                const bool valid = r < a.R && (MODE != kRows4 || (gid & 1) == 0);
-                const int rt_ = valid ? token_of(r) : 0, rh = valid ? r - rt_ * a.share : 0;
-                const T* src = (const T*)a.q + ((long long)b * a.T + rt_) * a.ld_q + (long long)(h * a.share + rh) * D + 8 * tig;
+                const bool valid = row0 + (WIDE ? gid >> 1 : gid) < a.R && (MODE != kRows4 || (gid & 1) == 0);
                 float v[H32][8], m = 0.f;
 #pragma unroll
                 for (int j = 0; j < H32; ++j) {
-                    T in[8];
-                    const uint4* p = reinterpret_cast<const uint4*>(src + j * 32);
-                    *reinterpret_cast<uint4*>(in) = p[0];
-                    if (sizeof(T) == 4) reinterpret_cast<uint4*>(in)[1] = p[1];
+                    unpack8<T>(raw[j], v[j]);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        v[j][e] = valid ? to_f32<T>(in[e]) : 0.f;
+                        if (!valid) v[j][e] = 0.f;
                         m = fmaxf(m, fabsf(v[j][e]));
                     }
                 }
@@ -316,54 +427,27 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                 for (int g = 0; g < NG; ++g) om[g][i] = 0.f;
             }
 
-            // Into a step: refill the stage of two steps before (every warp has left it, or will without this one), then
-            // wait for this step's stage.
-            auto enter = [&]() {
-                const int refill = step - 2 + a.stages;
-                if (warp == (step & (kAttnWarps - 1)) && lane == 0 && step >= 2 && refill < 2 * (end - begin)) {
-                    const int was = s >= 2 ? s - 2 : s - 2 + a.stages;
-                    bounded_wait(smem_u32(&empty_bar[was]), s >= 2 ? ph : ph ^ 1u, abort_flag, a.status);
-                    if (!*abort_flag) {
-                        const int tile = begin + (refill >> 1) - t + first_tile;
-                        if (tile < k.nt) {
-                            fetch(b, k.hr, tile, refill & 1, was);
-                        } else {
-                            const Cursor p = seek(begin + (refill >> 1));
-                            fetch(p.b, p.hr, p.tile, refill & 1, was);
-                        }
-                    }
-                }
-                __syncwarp();
-                bounded_wait(smem_u32(&full_bar[s]), ph, abort_flag, a.status);
-                const int here = s;
-                ++step;
-                if (++s == a.stages) { s = 0; ph ^= 1u; }
-                return here;
-            };
-            auto leave = [&](int stage) {
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&empty_bar[stage]));
-            };
-
-            for (int it = 0; it < n_tiles; ++it) {
-                const int t0 = (first_tile + it) * TILE;
-                const int ks = enter();
-                int vs = -1;
-                bool keys_left = false;
-                const uint8_t* kst = smem + (size_t)ks * STAGE;
-                const uint8_t* vst = nullptr;
-                for (int sub = UN * sg; sub < TILE / 16; sub += UN * nsg) {
-                    const int n0 = t0 + sub * 16;
-                    if (n0 >= len) break;
+            const int seg_end = (first_tile + n_tiles) * TILE < len ? (first_tile + n_tiles) * TILE : len;
+            for (int n0 = first_tile * TILE + sg * CH; n0 < seg_end; n0 += stride) {
+                {
+                    uint8_t* kst = enter();
                     // ---- logits: S^T [UN][16 slots][8 columns]; lo[u][v]: slot n0 + 16 u + 8 v + tok0 ----
+                    const int na = n0 + tok0;
+                    const bool edge = n0 + CH > all_see;     // some row does not see some slot
+#pragma unroll 1
+                    for (int e = edge; e; e = opaque_zero()) {               // pairs beyond the sequence may be anything: zero them
+                        for (int i = lane; i < CH * NG; i += 32)
+                            if (n0 + i / NG >= len) reinterpret_cast<uint32_t*>(kst + CODES)[i] = 0u;
+                        __syncwarp();
+                    }
                     float lo[UN][2][NV];
 #pragma unroll
                     for (int u = 0; u < UN; ++u) {
-                        const uint8_t* krow = kst + (sub * 16 + u * 16 + tok0) * CODE_ROW + tig * (D / 8);
+                        const uint8_t* krow = kst + (u * 16 + tok0) * CODE_ROW + tig * (D / 8);
                         uint32_t w0[D / 32], w1[D / 32], kp0[NG], kp1[NG];
                         ld_words<D / 32>(w0, krow);
                         ld_words<D / 32>(w1, krow + 8 * CODE_ROW);
-                        const uint8_t* kpr = kst + CODE_TILE + (sub * 16 + u * 16 + tok0) * PAIR_ROW;
+                        const uint8_t* kpr = kst + CODES + (u * 16 + tok0) * PAIR_ROW;
                         ld_words<NG>(kp0, kpr);
                         ld_words<NG>(kp1, kpr + 8 * PAIR_ROW);
 #pragma unroll
@@ -389,8 +473,6 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                             }
                         }
                     }
-                    const int na = n0 + tok0;
-                    const bool edge = n0 + 16 * UN > all_see;     // some row does not see some slot
                     float most[NV];
 #pragma unroll
                     for (int i = 0; i < NV; ++i) {
@@ -398,7 +480,8 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                         for (int u = 0; u < UN; ++u)
 #pragma unroll
                             for (int v = 0; v < 2; ++v) lo[u][v][i] *= f[i];
-                        if (edge) [[unlikely]] {
+#pragma unroll 1
+                        for (int e = edge; e; e = opaque_zero()) {
 #pragma unroll
                             for (int u = 0; u < UN; ++u)
 #pragma unroll
@@ -419,14 +502,8 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                                 }
                         }
                     }
-                    if (n0 + 16 * UN * nsg >= len || sub + UN * nsg >= TILE / 16) {      // this warp's last step of the tile
-                        leave(ks);
-                        keys_left = true;
-                    }
-                    if (!vst) {
-                        vs = enter();
-                        vst = smem + (size_t)vs * STAGE;
-                    }
+                    leave(0);
+                    uint8_t* vst = enter();
                     // ---- value pairs, running maximum ----
                     uint32_t vp[UN][2][NG];
                     __half2 smax = __float2half2_rn(0.f);
@@ -434,16 +511,27 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                     for (int u = 0; u < UN; ++u)
 #pragma unroll
                         for (int v = 0; v < 2; ++v) {
-                            ld_words<NG>(vp[u][v], vst + CODE_TILE + (sub * 16 + 16 * u + 8 * v + tok0) * PAIR_ROW);
-                            if (edge && na + 16 * u + 8 * v >= len) [[unlikely]] {                        // never used
-#pragma unroll
-                                for (int g = 0; g < NG; ++g) vp[u][v][g] = 0u;
-                            }
+                            ld_words<NG>(vp[u][v], vst + CODES + (16 * u + 8 * v + tok0) * PAIR_ROW);
 #pragma unroll
                             for (int g = 0; g < NG; ++g) {
                                 smax = __hmax2(smax, *reinterpret_cast<const __half2*>(&vp[u][v][g]));
                             }
                         }
+#pragma unroll 1
+                    for (int e = edge; e; e = opaque_zero()) {
+                        // A slot beyond the sequence counts for nothing, whatever it holds; nor does one that a lane's one
+                        // column does not see (of two columns, one may: they are told apart below).
+                        smax = __float2half2_rn(0.f);
+#pragma unroll
+                        for (int u = 0; u < UN; ++u)
+#pragma unroll
+                            for (int v = 0; v < 2; ++v)
+#pragma unroll
+                                for (int g = 0; g < NG; ++g) {
+                                    if (na + 16 * u + 8 * v >= (WIDE ? lim[0] : len)) vp[u][v][g] = 0u;
+                                    smax = __hmax2(smax, *reinterpret_cast<const __half2*>(&vp[u][v][g]));
+                                }
+                    }
                     float s_here = __low2float(smax);
                     bool change = s_here > s_most;
 #pragma unroll
@@ -499,7 +587,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                     // ---- O^T += V^T P^T, per group of scales ----
 #pragma unroll
                     for (int u = 0; u < UN; ++u) {
-                        const uint8_t* vrow = vst + (sub * 16 + u * 16 + tig) * CODE_ROW + gid * (D / 16);
+                        const uint8_t* vrow = vst + (u * 16 + tig) * CODE_ROW + gid * (D / 16);
                         uint32_t va[H32 / 2], vb[H32 / 2], vc[H32 / 2], vd[H32 / 2];
                         ld_words<H32 / 2>(va, vrow);
                         ld_words<H32 / 2>(vb, vrow + 4 * CODE_ROW);
@@ -519,7 +607,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                                     ps[i] = lo[u][v][i] * so.x;
                                     om[g][i] = fmaf(lo[u][v][i], so.y, om[g][i]);
                                 }
-                                if (edge) [[unlikely]] {     // a slot that a row does not see adds nothing, whatever it holds
+                                if (!WIDE && edge) {         // a slot that a row does not see adds nothing, whatever it holds
 #pragma unroll
                                     for (int i = 0; i < NV; ++i)
                                         if (na + 16 * u + 8 * v >= lim[i]) {
@@ -545,9 +633,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                         }
                     }
                 }
-                if (!keys_left) leave(ks);                   // the tile ends before this warp's slots
-                if (!vst) vs = enter();
-                leave(vs);
+                leave(1);
             }
 
             // ---- join the warps of a row tile ----
@@ -585,7 +671,12 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                 }
             }
             __syncthreads();
-            const bool whole = n_tiles == k.nt;
+            const Cursor was = k;
+            if (t + n_tiles < n_total) {                     // the next unit's query rows are on their way during the join
+                k = advance(k, n_tiles);
+                load_q(k);
+            }
+            const bool whole = n_tiles == was.nt;
             const int piece = blockIdx.x * 2 + (first_tile == 0 ? 1 : 0);
             // nsg neighbouring lanes take the parts of one quad of outputs and add them up by shuffles
             const int rows_here = a.R - rb * a.RU < a.RU ? a.R - rb * a.RU : a.RU, items = rows_here * (D / 4);
@@ -620,16 +711,8 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                 }
             }
             t += n_tiles;
-            if (t < end) k = seek(t);
         }
     }
-    __syncthreads();
-    if (tid == 0 && *abort_flag) {
-        // after a wait that gave up copies may be in flight: give them a bounded time to land
-        const long long t0 = clock64();
-        while (clock64() - t0 < 20000000LL) __nanosleep(1000);
-    }
-    __syncthreads();
 }
 
 // ------------------------------------------------------------------------------ finish --
@@ -639,41 +722,27 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
 constexpr int kFinishThreads = 256;
 constexpr int kFinishSlots = 1024;
 
-template <typename V, typename Op>
-__device__ __forceinline__ V finish_reduce(V v, V* buf, Op op)
-{
-#pragma unroll
-    for (int d = 16; d; d >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, d));
-    if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = buf[0];
-#pragma unroll
-    for (int i = 1; i < kFinishThreads / 32; ++i) v = op(v, buf[i]);
-    __syncthreads();
-    return v;
-}
-
 template <typename T>
 __global__ void __launch_bounds__(kFinishThreads) kv4_finish_kernel(const __grid_constant__ AttnArgs a)
 {
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ float redf[8];
     const Kv4& c = a.c;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int b = blockIdx.y / c.H, h = blockIdx.y % c.H, D = c.D;
+    // the state was complete before the main kernel started, whose end is awaited below
     const int len = kv4_length(c, b);
     if ((int)blockIdx.x >= a.R && ((int)blockIdx.x - a.R) * kFinishSlots >= len) return;
     int before = 0, all = 0;                                 // tiles of a head, before this sequence and in all; every warp for itself
     for (int i = lane; i < c.B; i += 32) {
         const int n = attn_tiles(kv4_length(c, i), a.tile);
-        all += n;
-        if (i < b) before += n;
+        all += attn_entries(n);
+        if (i < b) before += attn_entries(n);
     }
     before = __reduce_add_sync(0xffffffffu, before);
     all = __reduce_add_sync(0xffffffffu, all);
     const int HR = c.H * a.RB, nt = attn_tiles(len, a.tile), total = all * HR;
     const AttnCut cut(a.n_ctas, total);
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    wait_for_stream();
 
     if ((int)blockIdx.x < a.R) {
         const int r = blockIdx.x, rb = r / a.RU, ru = r % a.RU;
@@ -683,41 +752,39 @@ __global__ void __launch_bounds__(kFinishThreads) kv4_finish_kernel(const __grid
             for (int d = tid; d < D; d += kFinishThreads) dst[d] = from_f32<T>(0.f);
             return;
         }
-        const int u0 = before * HR + (h * a.RB + rb) * nt;
+        const int u0 = before * HR + (h * a.RB + rb) * attn_entries(nt) + kAttnUnitCost;
         const int i0 = cut.owner(u0), i1 = cut.owner(u0 + nt - 1);
         if (i0 == i1) return;
-        float* wgt = reinterpret_cast<float*>(smem);                     // [pieces]
         const int n = i1 - i0 + 1;
-        auto piece = [&](int i) { return (size_t)(i0 + i) * 2 + (i == 0 ? 1 : 0); };
-        float top = kNoLogit * 2.f;
-        for (int i = tid; i < n; i += kFinishThreads) top = fmaxf(top, a.part_ml[piece(i) * a.RU + ru].x);
-        top = finish_reduce(top, redf, [](float x, float y) { return fmaxf(x, y); });
-        float sum = 0.f;
-        for (int i = tid; i < n; i += kFinishThreads) {
-            const float2 ml = a.part_ml[piece(i) * a.RU + ru];
-            const float e = exp2_fast(ml.x - top);
-            wgt[i] = e;
-            sum = fmaf(ml.y, e, sum);
+        auto piece = [&](int i) { return ((size_t)(i0 + i) * 2 + (i == 0 ? 1 : 0)) * a.RU + ru; };
+        float top = kNoLogit * 2.f, sum = 0.f;               // every warp for itself
+        for (int i = lane; i < n; i += 32) top = fmaxf(top, a.part_ml[piece(i)].x);
+#pragma unroll
+        for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        for (int i = lane; i < n; i += 32) {
+            const float2 ml = a.part_ml[piece(i)];
+            sum = fmaf(ml.y, exp2_fast(ml.x - top), sum);
         }
-        sum = finish_reduce(sum, redf, [](float x, float y) { return x + y; });
+#pragma unroll
+        for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         // D / 4 threads cover the row, 256 / (D / 4) of such groups take the pieces in turn
         const int quads = D / 4, groups = kFinishThreads / quads, d4 = tid % quads, g = tid / quads;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
         for (int i = g; i < n; i += groups) {
-            const float4 x = *reinterpret_cast<const float4*>(a.part_o + (piece(i) * a.RU + ru) * D + d4 * 4);
-            const float e = wgt[i];
+            const float4 x = *reinterpret_cast<const float4*>(a.part_o + piece(i) * D + d4 * 4);
+            const float e = exp2_fast(a.part_ml[piece(i)].x - top);
             v.x = fmaf(x.x, e, v.x);
             v.y = fmaf(x.y, e, v.y);
             v.z = fmaf(x.z, e, v.z);
             v.w = fmaf(x.w, e, v.w);
         }
-        float4* buf = reinterpret_cast<float4*>(smem + kAttnMaxCtas * sizeof(float));
+        float4* buf = reinterpret_cast<float4*>(smem);
         buf[tid] = v;
         __syncthreads();
         if (g == 0) {
-            for (int j = 1; j < groups; ++j) {
+            for (int j = 1; j < groups && j < n; ++j) {
                 const float4 x = buf[j * quads + d4];
                 v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
             }
@@ -731,7 +798,7 @@ __global__ void __launch_bounds__(kFinishThreads) kv4_finish_kernel(const __grid
     int* sees = reinterpret_cast<int*>(rows + a.R);                      // [R] slots that the row sees
     for (int r = warp; r < a.R; r += kFinishThreads / 32) {
         const int rb = r / a.RU, ru = r % a.RU;
-        const int u0 = before * HR + (h * a.RB + rb) * nt;
+        const int u0 = before * HR + (h * a.RB + rb) * attn_entries(nt) + kAttnUnitCost;
         const int i0 = cut.owner(u0), i1 = cut.owner(u0 + nt - 1);
         float top, sum;
         if (i0 == i1) {
@@ -808,21 +875,15 @@ template <typename T, int D, int G, int MODE>
 static coreinfer_status launch_mode(AttnArgs& a, const DeviceInfo& di, cudaStream_t st)
 {
     constexpr int RPT = MODE == kRows8 ? 8 : 4, NG = D / G, TILE = kAttnTile<D, G>;
-    constexpr size_t STAGE = (size_t)TILE * (D / 2 + NG * 4);
-    const size_t fixed = (size_t)kAttnWarps * RPT * (D * sizeof(float) + sizeof(float2)) + (2 * a.c.B + 1) * sizeof(int);
-    // two CTAs per SM where registers (head_dim up to 128) and four stages each allow it
-    int per_sm = D <= 128 ? 2 : 1, stages = 0;
-    for (;; --per_sm) {
-        const size_t room = (smem_room(di) - (per_sm - 1) * 1024) / per_sm;
-        stages = room > fixed ? (int)((room - fixed) / STAGE) : 0;
-        if (stages >= 4 || per_sm == 1) break;
-    }
-    if (stages < 4) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "not enough shared memory for four pipeline stages");
-    if (stages > kAttnMaxStages) stages = kAttnMaxStages;
-    a.stages = stages;
+    const size_t ring = (size_t)kAttnStages<D, G, MODE> * (TILE / kAttnWarps) * (D / 2 + NG * 4);
+    const size_t smem = kAttnWarps * (ring + RPT * (D * sizeof(float) + sizeof(float2))) + (3 * a.c.B + 1) * sizeof(int);
+    // two CTAs per SM where registers (head_dim up to 128) and shared memory (batch up to some hundreds) allow it
+    const int per_sm = D <= 128 && 2 * (smem + 1024 + 64) <= (size_t)di.smem_optin + 1024 ? 2 : 1;
+    if (smem > smem_room(di)) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "not enough shared memory");
     a.tile = TILE;
-    const size_t smem = fixed + stages * STAGE;
-    const long long tiles = (long long)a.c.B * a.c.H * a.RB * ((a.c.cap + TILE - 1) / TILE);
+    const long long tiles = (long long)a.c.B * a.c.H * a.RB * ((a.c.cap + TILE - 1) / TILE + kAttnUnitCost);
+    if ((unsigned long long)a.c.B * a.c.H * a.c.cap > 0xffffffffull)
+        CI_FAIL(COREINFER_ERR_UNSUPPORTED, "the cache has more than 2^32 slots");
     if (tiles > (1LL << 30)) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "the cache has %lld tiles of %d slots: too many for one call", tiles, TILE);
     long long ctas = (long long)di.sm_count * per_sm;
     if (ctas > kAttnMaxCtas) ctas = kAttnMaxCtas;
@@ -830,21 +891,10 @@ static coreinfer_status launch_mode(AttnArgs& a, const DeviceInfo& di, cudaStrea
     a.n_ctas = (int)ctas;
     const coreinfer_status s = allow_smem<kv4_attention_kernel<T, D, G, MODE>>(di);
     if (s != COREINFER_OK) return s;
-    kv4_attention_kernel<T, D, G, MODE><<<a.n_ctas, kAttnThreads, smem, st>>>(a);
-    CI_CUDA(cudaGetLastError());
-
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(a.R + (a.accumulate ? (a.c.cap + kFinishSlots - 1) / kFinishSlots : 0), a.c.B * a.c.H);
-    cfg.blockDim = dim3(kFinishThreads);
-    const size_t join = kAttnMaxCtas * sizeof(float) + kFinishThreads * sizeof(float4), rows = (size_t)a.R * (sizeof(float2) + sizeof(int));
-    cfg.dynamicSmemBytes = join > rows ? join : rows;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    CI_CUDA(cudaLaunchKernelEx(&cfg, kv4_finish_kernel<T>, a));
+    CI_CUDA(launch_overlapped(kv4_attention_kernel<T, D, G, MODE>, dim3(a.n_ctas), dim3(kAttnThreads), smem, st, a));
+    const size_t join = kFinishThreads * sizeof(float4), rows = (size_t)a.R * (sizeof(float2) + sizeof(int));
+    const dim3 grid(a.R + (a.accumulate ? (a.c.cap + kFinishSlots - 1) / kFinishSlots : 0), a.c.B * a.c.H);
+    CI_CUDA(launch_overlapped(kv4_finish_kernel<T>, grid, dim3(kFinishThreads), join > rows ? join : rows, st, a));
     return COREINFER_OK;
 }
 
@@ -933,7 +983,6 @@ coreinfer_status coreinfer_kv4_attention(const coreinfer_kv4_cache* cache, const
     attn_rows(a.R, rpt, &a.RT, &a.RU, &a.RB);
     a.scale = scale;
     a.accumulate = accumulate ? 1 : 0;
-    a.status = (unsigned*)ws;
     a.part_ml = (float2*)(ws + w.ml);
     a.part_o = (float*)(ws + w.o);
     a.stats = (float2*)(ws + w.stats);

@@ -29,6 +29,27 @@ static coreinfer_status allow_smem(const DeviceInfo& di, int fixed = 1024)
     return COREINFER_OK;
 }
 
+// A launch that may begin while the kernel before it on the stream still runs: its blocks get ready and wait
+// (griddepcontrol.wait) before they touch global memory, so the order of results is that of the stream.
+template <typename Args>
+static cudaError_t launch_overlapped(void (*kernel)(const Args), dim3 grid, dim3 block, size_t smem, cudaStream_t st, const Args& args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args);
+}
+__device__ __forceinline__ void wait_for_stream() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// The next kernel of the stream may get its blocks ready.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // Typed views of the three storage types.
 template <typename T> __device__ __forceinline__ float to_f32(T v);
 template <> __device__ __forceinline__ float to_f32<float>(float v) { return v; }
