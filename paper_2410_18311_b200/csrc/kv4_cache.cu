@@ -26,6 +26,8 @@ __global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(const __grid
     const Kv4& c = a.c;
     const int b = blockIdx.y;
     const int l = threadIdx.x % LANES;
+    wait_for_stream();
+    let_next_start();
     const int4 state = *reinterpret_cast<const int4*>(c.state + b * 4);
     const int n0 = state.x < 0 ? 0 : (state.x > c.cap ? c.cap : state.x), seen = state.y;
     const bool fits = a.tokens <= c.cap - n0;
@@ -103,37 +105,41 @@ __global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(const __grid
 }
 
 template <typename T, int D, int G>
-static void launch_append(const AppendArgs& a, const DeviceInfo& di, cudaStream_t st)
+static cudaError_t launch_append(const AppendArgs& a, const DeviceInfo& di, cudaStream_t st)
 {
     constexpr int ROWS = kAppendThreads / (D / 8);
     const int want = (a.rows + ROWS - 1) / ROWS, most = (di.sm_count * 8 + a.c.B - 1) / a.c.B;
-    kv4_append_kernel<T, D, G><<<dim3(want < most ? want : most, a.c.B), kAppendThreads, 0, st>>>(a);
+    return launch_overlapped(kv4_append_kernel<T, D, G>, dim3(want < most ? want : most, a.c.B), dim3(kAppendThreads), 0, st, a);
 }
 
 template <typename T>
 static coreinfer_status pick_append(const AppendArgs& a, const DeviceInfo& di, cudaStream_t st)
 {
     const int D = a.c.D, G = a.c.G;
-    if (D == 64) G == 32 ? launch_append<T, 64, 32>(a, di, st) : launch_append<T, 64, 64>(a, di, st);
+    cudaError_t r;
+    if (D == 64) r = G == 32 ? launch_append<T, 64, 32>(a, di, st) : launch_append<T, 64, 64>(a, di, st);
     else if (D == 128)
-        G == 32 ? launch_append<T, 128, 32>(a, di, st) : (G == 64 ? launch_append<T, 128, 64>(a, di, st) : launch_append<T, 128, 128>(a, di, st));
+        r = G == 32 ? launch_append<T, 128, 32>(a, di, st) : (G == 64 ? launch_append<T, 128, 64>(a, di, st) : launch_append<T, 128, 128>(a, di, st));
     else
-        G == 32 ? launch_append<T, 256, 32>(a, di, st) : (G == 64 ? launch_append<T, 256, 64>(a, di, st) : launch_append<T, 256, 128>(a, di, st));
-    CI_CUDA(cudaGetLastError());
+        r = G == 32 ? launch_append<T, 256, 32>(a, di, st) : (G == 64 ? launch_append<T, 256, 64>(a, di, st) : launch_append<T, 256, 128>(a, di, st));
+    CI_CUDA(r);
     return COREINFER_OK;
 }
 
 // --------------------------------------------------------------------------------- evict --
-// kv4_select_kernel, one CTA per sequence and head: keys (the order of eviction as unsigned numbers) into shared memory,
-// the key of the last slot that stays by radix selection (11 + 11 + 10 bits, most significant first,
-// stopping as soon as a whole bin stays), then the lists of slots that move by ballots and one scan
-// over the warps.  A warp owns a contiguous range of slots, so that list order is slot order.
-// kv4_move_kernel copies the listed slots, many CTAs per head; where few can move (in place with little room
-// above the budget) the first kernel does it itself.  Both are bound by latency at the sizes of a decode
-// step, the moves by bytes after a prompt.
+// kv4_evict_few_kernel, in place with at most 8 slots above the budget (the step of a decode loop at a full budget): one
+// CTA per sequence and head takes the smallest key out, once per slot that leaves, and moves what has to move.
+// kv4_select_kernel, otherwise: one CTA, or a cluster of up to 8 where heads are few and long, per sequence and head.  Keys
+// (the order of eviction as unsigned numbers) into shared memory, the key of the last slot that stays by
+// radix selection (11 + 11 + 10 bits, most significant first, stopping as soon as a whole bin stays; the CTAs of a cluster
+// add their histograms up in the first one's shared memory), then the lists of slots that move, by ballots and scans
+// over warps and CTAs.  A warp owns a contiguous range of slots, so that list order is slot order.
+// kv4_move_kernel copies the listed slots, many CTAs per head.
+// All are bound by latency (memory, barriers) at the sizes of a decode step, the moves by bytes after a prompt.
 constexpr int kEvictBins = 2048;
-constexpr int kEvictFewMoves = 64;          // moves that the selecting CTA makes itself
-constexpr int kEvictKeysMost = 48 * 1024;   // keys held in shared memory; more slots are read again for each pass
+constexpr int kEvictFew = 8;
+constexpr int kEvictKeysMost = 48 * 1024;   // keys a CTA holds in shared memory; more slots are read again for each pass
+constexpr int kEvictMaxCluster = 8;
 constexpr int kMoveSlots = 64;              // slots per CTA of the moving kernel
 constexpr int kMoveThreads = 256;
 
@@ -202,11 +208,75 @@ __device__ __forceinline__ void move_slots(const Kv4& a, size_t abase, const Kv4
 struct EvictArgs {
     Kv4 a, z;
     int in_place, budget, recent, first;
-    int keys;               // capacity of the key buffer
-    int move_here;          // the selecting CTA moves (in place only)
+    int keys;               // capacity of a CTA's key buffer
     int32_t* counts;        // [B * H] slots to move
     int32_t* lists;         // [B * H][cap]: sources; in place destinations [0, cap / 2), sources from cap / 2 on
 };
+
+__device__ __forceinline__ unsigned long long shfl_min(unsigned long long v)
+{
+#pragma unroll
+    for (int d = 16; d; d >>= 1) {
+        const unsigned long long o = __shfl_xor_sync(0xffffffffu, v, d);
+        if (o < v) v = o;
+    }
+    return v;
+}
+
+__global__ void __launch_bounds__(1024) kv4_evict_few_kernel(const __grid_constant__ EvictArgs e)
+{
+    __shared__ unsigned long long buf[32];
+    __shared__ int32_t out_s[kEvictFew], from_s[kEvictFew], to_s[kEvictFew];
+    __shared__ int moves_s;
+    const Kv4& a = e.a;
+    const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    wait_for_stream();
+    let_next_start();
+    const int n = kv4_length(a, b), seen = a.state[b * 4 + kStateSeen];
+    const int keep = n < e.budget ? n : e.budget, leave = n - keep;
+    const size_t base = ((size_t)b * a.H + h) * a.cap;
+    // The next to leave: the smallest key, of equal ones the highest slot; those that have left are skipped.
+    int moves = 0;
+    for (int r = 0; r < leave; ++r) {
+        unsigned long long least = ~0ull;
+#pragma unroll 8
+        for (int i = tid; i < n; i += blockDim.x) {
+            const unsigned u = evict_key(a.weight[base + i], a.position[base + i], seen, e.recent, e.first);
+            const unsigned long long v = (unsigned long long)u << 32 | (unsigned)(0x7fffffff - i);
+            bool gone = false;
+            for (int k = 0; k < r; ++k) gone |= out_s[k] == i;
+            if (!gone && v < least) least = v;
+        }
+        least = shfl_min(least);
+        if (lane == 0) buf[warp] = least;
+        __syncthreads();
+        least = shfl_min(lane < (int)blockDim.x / 32 ? buf[lane] : ~0ull);
+        if (tid == 0) out_s[r] = 0x7fffffff - (int)(least & 0xffffffffu);
+        __syncthreads();
+    }
+    if (tid == 0) {
+        // free slots below the new length and kept ones above it, both in ascending order
+        int hole = -1, at = keep;
+        for (;; ++moves) {
+            int next = n;
+            for (int k = 0; k < leave; ++k)
+                if (out_s[k] > hole && out_s[k] < next) next = out_s[k];
+            if (next >= keep) break;
+            hole = next;
+            for (;; ++at) {
+                bool left = false;
+                for (int k = 0; k < leave; ++k) left |= out_s[k] == at;
+                if (!left) break;
+            }
+            to_s[moves] = hole;
+            from_s[moves] = at++;
+        }
+        moves_s = moves;
+    }
+    __syncthreads();
+    move_slots(a, base, a, base, from_s, to_s, moves_s, tid, blockDim.x);
+    if (kv4_last_of_sequence(a, b, gridDim.x)) a.state[b * 4 + kStateLength] = keep;
+}
 
 // Sum over the block's warps before this one, and over all of them.
 __device__ __forceinline__ int warps_before(int v, int* buf, int warp, int warps, int* total)
@@ -220,119 +290,192 @@ __device__ __forceinline__ int warps_before(int v, int* buf, int warp, int warps
     return __reduce_add_sync(0xffffffffu, lane < warp ? x : 0);
 }
 
+// ---- the CTAs of a cluster; with one CTA all of this is the block's own ----
+__device__ __forceinline__ unsigned cluster_size()
+{
+    unsigned v;
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(v));
+    return v;
+}
+__device__ __forceinline__ unsigned cluster_rank()
+{
+    unsigned v;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(v));
+    return v;
+}
+__device__ __forceinline__ void cluster_sync(unsigned size)
+{
+    if (size == 1) {
+        __syncthreads();
+        return;
+    }
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_address(const void* p, unsigned rank)
+{
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void cluster_store(uint32_t at, int v) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
+__device__ __forceinline__ void cluster_add(uint32_t at, unsigned v) { asm volatile("red.shared::cluster.add.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
+
+// Sum of v (the same in all threads of a CTA) over the CTAs before this one, and over all; slots is [kEvictMaxCluster].
+__device__ __forceinline__ int ctas_before(int v, int* slots, unsigned rank, unsigned size, int* total)
+{
+    *total = v;
+    if (size == 1) return 0;
+    if (threadIdx.x < size) cluster_store(cluster_address(&slots[rank], threadIdx.x), v);
+    cluster_sync(size);
+    int before = 0, all = 0;
+    for (unsigned r = 0; r < size; ++r) {
+        all += slots[r];
+        before += r < rank ? slots[r] : 0;
+    }
+    *total = all;
+    return before;
+}
+
 __global__ void __launch_bounds__(1024) kv4_select_kernel(const __grid_constant__ EvictArgs e)
 {
     extern __shared__ __align__(16) unsigned keys[];
-    __shared__ unsigned hist[kEvictBins];
-    __shared__ int buf[32];
-    __shared__ int bin_s, left_s, count_s;
+    __shared__ unsigned hist[kEvictBins + 1];               // the last: slots that stay for certain
+    __shared__ int buf[32], found[4], ties_s[kEvictMaxCluster], movers_s[kEvictMaxCluster], holes_s[kEvictMaxCluster];
     const Kv4& a = e.a;
-    const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+    const unsigned size = cluster_size(), rank = cluster_rank();
+    const int h = blockIdx.x / size, b = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+    wait_for_stream();
     const int n = kv4_length(a, b), seen = a.state[b * 4 + kStateSeen];
     const int keep = n < e.budget ? n : e.budget;
     const size_t base = ((size_t)b * a.H + h) * a.cap;
     const float* weight = a.weight + base;
     const int32_t* position = a.position + base;
     int32_t* list = e.lists + base;
-    const bool held = n <= e.keys;
-    auto key = [&](int i) { return held ? keys[i] : evict_key(weight[i], position[i], seen, e.recent, e.first); };
-    // a warp's slots: [from, to)
-    const int per = ((n + warps - 1) / warps + 31) & ~31;
-    const int from = warp * per < n ? warp * per : n, to = from + per < n ? from + per : n;
+    // this CTA's slots [lo, hi), and of them this warp's [from, to)
+    const int share = ((n + (int)size - 1) / (int)size + 31) & ~31;
+    const int lo = (int)rank * share < n ? (int)rank * share : n, hi = lo + share < n ? lo + share : n;
+    const int per = ((hi - lo + warps - 1) / warps + 31) & ~31;
+    const int from = lo + warp * per < hi ? lo + warp * per : hi, to = from + per < hi ? from + per : hi;
+    const bool held = hi - lo <= e.keys;
+    auto key = [&](int i) { return held ? keys[i - lo] : evict_key(weight[i], position[i], seen, e.recent, e.first); };
 
     // the slots with (key >> shift) > prefix stay, and the first `left` of those with equality
     unsigned prefix = 0u;
     int shift = 0, left = 0;
     const bool all = keep == n;
+    bool whole = false;                                     // all of those with equality stay
     if (!all && keep > 0) {
-        int certain = 0;
-        for (int i = tid; i < kEvictBins; i += blockDim.x) hist[i] = 0u;
-        __syncthreads();
+        for (int pass = 0; pass < 3 && !whole; ++pass) {
+            shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0);
+            const int bits = pass == 2 ? 10 : 11;
+            for (int i = tid; i <= kEvictBins; i += blockDim.x) hist[i] = 0u;
+            cluster_sync(size);                             // nobody adds to a histogram that is still being cleared
+            if (pass == 0) {
+                int certain = 0;
 #pragma unroll 4
-        for (int i = from + lane; i < to; i += 32) {
-            const unsigned u = evict_key(weight[i], position[i], seen, e.recent, e.first);
-            if (held) keys[i] = u;
-            if (u == 0xffffffffu) ++certain;
-            else atomicAdd(&hist[u >> 21], 1u);
-        }
-        certain = __reduce_add_sync(0xffffffffu, certain);
-        int sure;
-        warps_before(certain, buf, warp, warps, &sure);
-        left = keep - sure;
-        if (left <= 0) {
-            // only slots that stay for certain do (more of them than the budget where positions are not what append
-            // wrote: the first ones)
-            prefix = 0xffffffffu;
-            left = keep;
-        } else {
-            for (int pass = 0; pass < 3; ++pass) {
-                shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0);
-                if (pass > 0) {
-                    for (int i = tid; i < kEvictBins; i += blockDim.x) hist[i] = 0u;
-                    __syncthreads();
-                    const int bits = pass == 1 ? 11 : 10;
+                for (int i = from + lane; i < to; i += 32) {
+                    const unsigned u = evict_key(weight[i], position[i], seen, e.recent, e.first);
+                    if (held) keys[i - lo] = u;
+                    if (u == 0xffffffffu) ++certain;
+                    else atomicAdd(&hist[u >> 21], 1u);
+                }
+                certain = __reduce_add_sync(0xffffffffu, certain);
+                if (lane == 0 && certain) atomicAdd(&hist[kEvictBins], (unsigned)certain);
+            } else {
 #pragma unroll 4
-                    for (int i = from + lane; i < to; i += 32) {
-                        const unsigned u = key(i);
-                        if (u != 0xffffffffu && u >> (shift + bits) == prefix) atomicAdd(&hist[(u >> shift) & ((1u << bits) - 1u)], 1u);
-                    }
-                    __syncthreads();
+                for (int i = from + lane; i < to; i += 32) {
+                    const unsigned u = key(i);
+                    if (u != 0xffffffffu && u >> (shift + bits) == prefix) atomicAdd(&hist[(u >> shift) & ((1u << bits) - 1u)], 1u);
                 }
-                // from the top bin down: the bin in which the count reaches `left`
-                const int mine = kEvictBins / blockDim.x;            // bins per thread
-                const int top = kEvictBins - 1 - tid * mine;
-                int sum = 0;
-                for (int k = 0; k < mine; ++k) sum += hist[top - k];
-                int incl = sum;
-#pragma unroll
-                for (int d = 1; d < 32; d <<= 1) {
-                    const int v = __shfl_up_sync(0xffffffffu, incl, d);
-                    if (lane >= d) incl += v;
-                }
-                int total;
-                const int before = warps_before(__shfl_sync(0xffffffffu, incl, 31), buf, warp, warps, &total) + incl - sum;
-                if (before < left && left <= before + sum) {
-                    int k = 0, acc = before;
-                    while (acc + (int)hist[top - k] < left) acc += hist[top - k++];
-                    bin_s = top - k;
-                    left_s = left - acc;
-                    count_s = hist[top - k];
-                }
-                __syncthreads();
-                prefix = pass == 0 ? (unsigned)bin_s : (prefix << (pass == 1 ? 11 : 10)) | (unsigned)bin_s;
-                left = left_s;
-                const bool whole = count_s == left;
-                __syncthreads();
-                if (whole) break;
             }
+            __syncthreads();
+            if (size > 1) {
+                if (rank != 0)
+                    for (int i = tid; i <= kEvictBins; i += blockDim.x)
+                        if (hist[i]) cluster_add(cluster_address(&hist[i], 0), hist[i]);
+                cluster_sync(size);
+            }
+            if (rank == 0) {
+                // From the top bin down: the bin in which the count reaches `left`.  A warp takes a run of bins, row by row of 32.
+                const int want = pass == 0 ? keep - (int)hist[kEvictBins] : left;
+                const int run = kEvictBins / warps, first = kEvictBins - (warp + 1) * run;
+                int sum = 0;
+                for (int k = lane; k < run; k += 32) sum += hist[first + k];
+                sum = __reduce_add_sync(0xffffffffu, sum);
+                int total;
+                int acc = warps_before(sum, buf, warp, warps, &total);
+                if (acc < want && want <= acc + sum) {
+                    for (int k = run - 32;; k -= 32) {
+                        const int v = hist[first + k + 31 - lane];          // lane 0 has the row's top bin
+                        int incl = v;
+#pragma unroll
+                        for (int d = 1; d < 32; d <<= 1) {
+                            const int u = __shfl_up_sync(0xffffffffu, incl, d);
+                            if (lane >= d) incl += u;
+                        }
+                        const unsigned hit = __ballot_sync(0xffffffffu, acc + incl >= want);
+                        if (hit) {
+                            if (lane == __ffs(hit) - 1) {
+                                found[0] = first + k + 31 - lane;
+                                found[1] = want - (acc + incl - v);
+                                found[2] = v;
+                            }
+                            break;
+                        }
+                        acc += __shfl_sync(0xffffffffu, incl, 31);
+                    }
+                }
+                if (tid == 0 && want <= 0) found[1] = 0;     // only slots that stay for certain do
+                __syncthreads();
+                if (size > 1 && tid < size && tid > 0)
+                    for (int k = 0; k < 3; ++k) cluster_store(cluster_address(&found[k], tid), found[k]);
+            }
+            cluster_sync(size);
+            const int bin = found[0], reached = found[1], count = found[2];
+            if (pass == 0 && reached == 0) {
+                // of more slots that stay for certain than the budget (positions that append did not write): the first ones
+                prefix = 0xffffffffu;
+                shift = 0;
+                left = keep;
+                break;
+            }
+            prefix = pass == 0 ? (unsigned)bin : (prefix << bits) | (unsigned)bin;
+            left = reached;
+            whole = count == left;
         }
     }
 
     auto tie = [&](unsigned u) { return (u >> shift) == prefix && (u != 0xffffffffu || prefix == 0xffffffffu); };
     auto over = [&](unsigned u) { return (u >> shift) > prefix || (u == 0xffffffffu && prefix != 0xffffffffu); };
-    int movers = 0, total = 0;
+    int movers = 0;
     if (keep > 0 && !(all && e.in_place)) {
-        int ties = 0;
-        if (!all) {
+        int ties = 0, ignored;
+        if (!all && !whole) {
             int c = 0;
             for (int i = from + lane; i < to; i += 32) c += tie(key(i));
             c = __reduce_add_sync(0xffffffffu, c);
-            int t;
-            ties = warps_before(c, buf, warp, warps, &t);
+            int here;
+            ties = warps_before(c, buf, warp, warps, &here);
+            ties += ctas_before(here, ties_s, rank, size, &ignored);
         }
         // the lists, in two rounds over the warp's slots: count, then write
         int at[2] = {0, 0};
         for (int round = 0; round < 2; ++round) {
-            int rank = ties, m = at[0], o = at[1];
+            int seen_ties = ties, m = at[0], o = at[1];
             for (int i0 = from; i0 < to; i0 += 32) {
                 const int i = i0 + lane;
                 bool stays = i < to;
                 if (!all) {
                     const unsigned u = i < to ? key(i) : 0u;
                     const bool eq = i < to && tie(u);
-                    const unsigned eqs = __ballot_sync(0xffffffffu, eq);
-                    stays = i < to && (over(u) || (eq && rank + __popc(eqs & ((1u << lane) - 1u)) < left));
-                    rank += __popc(eqs);
+                    bool in = eq;
+                    if (!whole) {
+                        const unsigned eqs = __ballot_sync(0xffffffffu, eq);
+                        in = eq && seen_ties + __popc(eqs & ((1u << lane) - 1u)) < left;
+                        seen_ties += __popc(eqs);
+                    }
+                    stays = i < to && (over(u) || in);
                 }
                 const bool mover = stays && (!e.in_place || i >= keep), hole = e.in_place && i < to && i < keep && !stays;
                 const unsigned ms = __ballot_sync(0xffffffffu, mover), os = __ballot_sync(0xffffffffu, hole);
@@ -344,16 +487,17 @@ __global__ void __launch_bounds__(1024) kv4_select_kernel(const __grid_constant_
                 o += __popc(os);
             }
             if (!round) {
-                at[0] = warps_before(m, buf, warp, warps, &movers);
-                at[1] = warps_before(o, buf, warp, warps, &total);
+                int here;
+                at[0] = warps_before(m, buf, warp, warps, &here);
+                at[0] += ctas_before(here, movers_s, rank, size, &movers);
+                at[1] = warps_before(o, buf, warp, warps, &here);
+                at[1] += ctas_before(here, holes_s, rank, size, &ignored);
             }
         }
     }
-    if (tid == 0) e.counts[b * a.H + h] = movers;
-    if (e.move_here) {
-        __syncthreads();
-        move_slots(a, base, e.z, ((size_t)b * a.H + h) * e.z.cap, list + a.cap / 2, list, movers, tid, blockDim.x);
-    }
+    if (tid == 0 && rank == 0) e.counts[b * a.H + h] = movers;
+    cluster_sync(size);                                     // no CTA ends while another may still write to its shared memory
+    let_next_start();
     if (kv4_last_of_sequence(a, b, gridDim.x)) {
         e.z.state[b * 4 + kStateLength] = keep;
         e.z.state[b * 4 + kStateSeen] = seen;
@@ -365,7 +509,8 @@ __global__ void __launch_bounds__(kMoveThreads) kv4_move_kernel(const __grid_con
     __shared__ int32_t from_s[kMoveSlots], to_s[kMoveSlots];
     const int bh = blockIdx.y, first = blockIdx.x * kMoveSlots, tid = threadIdx.x;
     const size_t base = (size_t)bh * e.a.cap;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    wait_for_stream();
+    let_next_start();
     int count = e.counts[bh] - first;
     if (count <= 0) return;
     if (count > kMoveSlots) count = kMoveSlots;
@@ -457,28 +602,25 @@ coreinfer_status coreinfer_kv4_evict(const coreinfer_kv4_cache* src, const corei
     e.budget = budget;
     e.recent = recent;
     e.first = first;
-    e.keys = a.cap < kEvictKeysMost ? a.cap : kEvictKeysMost;
-    // in place no more slots move than there are above the budget
-    e.move_here = e.in_place && a.cap - budget <= kEvictFewMoves;
     e.counts = (int32_t*)workspace;
     e.lists = (int32_t*)((uint8_t*)workspace + evict_lists_at(a));
     cudaStream_t st = (cudaStream_t)cuda_stream;
+    // in place no more slots move than there are above the budget
+    if (e.in_place && a.cap <= budget) return COREINFER_OK;
+    if (e.in_place && a.cap - budget <= kEvictFew) {
+        CI_CUDA(launch_overlapped(kv4_evict_few_kernel, dim3(a.H, a.B), dim3(a.cap <= 4096 ? 256 : 1024), 0, st, e));
+        return COREINFER_OK;
+    }
+    // Up to 8 CTAs per head while that leaves each 4096 slots at least and all of them fit on the GPU at once.
+    int cluster = 1;
+    while (cluster < kEvictMaxCluster && a.cap / (2 * cluster) >= 4096 && (long long)a.B * a.H * 2 * cluster <= di.sm_count) cluster *= 2;
+    const int slots = (a.cap + cluster - 1) / cluster + 32;
+    e.keys = slots < kEvictKeysMost ? slots : kEvictKeysMost;
     if ((s = allow_smem<kv4_select_kernel>(di, 16384)) != COREINFER_OK) return s;
-    kv4_select_kernel<<<dim3(a.H, a.B), a.cap <= 4096 ? 256 : (a.cap <= 16384 ? 512 : 1024), (size_t)e.keys * sizeof(unsigned), st>>>(e);
-    CI_CUDA(cudaGetLastError());
-    if (e.move_here) return COREINFER_OK;
+    const dim3 grid(a.H * cluster, a.B), block(slots <= 4096 + 32 ? 512 : 1024);
+    CI_CUDA(launch_overlapped(kv4_select_kernel, grid, block, (size_t)e.keys * sizeof(unsigned), st, e, cluster));
     const int most = e.in_place ? (a.cap - budget < a.cap / 2 ? a.cap - budget : a.cap / 2) : (budget < a.cap ? budget : a.cap);
-    if (most <= 0) return COREINFER_OK;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((most + kMoveSlots - 1) / kMoveSlots, a.B * a.H);
-    cfg.blockDim = dim3(kMoveThreads);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    CI_CUDA(cudaLaunchKernelEx(&cfg, kv4_move_kernel, e));
+    CI_CUDA(launch_overlapped(kv4_move_kernel, dim3((most + kMoveSlots - 1) / kMoveSlots, a.B * a.H), dim3(kMoveThreads), 0, st, e));
     return COREINFER_OK;
 }
 

@@ -30,20 +30,24 @@ static coreinfer_status allow_smem(const DeviceInfo& di, int fixed = 1024)
 }
 
 // A launch that may begin while the kernel before it on the stream still runs: its blocks get ready and wait
-// (griddepcontrol.wait) before they touch global memory, so the order of results is that of the stream.
+// (griddepcontrol.wait) before they touch global memory, so the order of results is that of the stream.  `cluster`: CTAs
+// per cluster along x.
 template <typename Args>
-static cudaError_t launch_overlapped(void (*kernel)(const Args), dim3 grid, dim3 block, size_t smem, cudaStream_t st, const Args& args)
+static cudaError_t launch_overlapped(void (*kernel)(const Args), dim3 grid, dim3 block, size_t smem, cudaStream_t st, const Args& args, int cluster = 1)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = block;
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, args);
 }
 __device__ __forceinline__ void wait_for_stream() { asm volatile("griddepcontrol.wait;" ::: "memory"); }

@@ -209,6 +209,8 @@ __global__ void __launch_bounds__(kW4Threads, 1) w4_matvec_kernel(const __grid_c
         mbar_fence_init();
     }
     __syncthreads();
+    wait_for_stream();                                       // nothing of an earlier kernel is read or overwritten above
+    let_next_start();
     const int first = (int)((long long)blockIdx.x * a.tiles / gridDim.x), last = (int)((long long)(blockIdx.x + 1) * a.tiles / gridDim.x);
     int s = 0;
     uint32_t ph = 0;
@@ -374,8 +376,7 @@ static coreinfer_status launch_group(W4Args& a, const DeviceInfo& di, cudaStream
     const size_t smem = fixed + stages * STAGE;
     const coreinfer_status s = allow_smem<w4_matvec_kernel<T, Y, G>>(di);
     if (s != COREINFER_OK) return s;
-    w4_matvec_kernel<T, Y, G><<<a.tiles < di.sm_count ? a.tiles : di.sm_count, kW4Threads, smem, st>>>(a);
-    CI_CUDA(cudaGetLastError());
+    CI_CUDA(launch_overlapped(w4_matvec_kernel<T, Y, G>, dim3(a.tiles < di.sm_count ? a.tiles : di.sm_count), dim3(kW4Threads), smem, st, a));
     return COREINFER_OK;
 }
 

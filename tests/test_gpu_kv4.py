@@ -229,7 +229,8 @@ EVICT = [
     (1, 1, [1], 1, 0, 0, 64, 32, False), (2, 2, [40, 10], 20, 4, 2, 64, 64, False), (3, 3, [0, 100, 33], 32, 32, 0, 128, 128, False),
     (2, 4, [300, 257], 256, 10, 4, 128, 64, True), (1, 2, [1500], 100, 0, 0, 256, 32, True), (2, 2, [64, 64], 64, 0, 0, 64, 32, False),
     (1, 3, [2000], 1999, 5, 5, 64, 32, False), (1, 1, [60000], 45000, 1000, 4, 64, 64, True), (2, 1, [33000, 20], 700, 64, 4, 128, 32, False),
-    (4, 1, [5000, 4096, 1, 1025], 1024, 256, 4, 64, 64, True),
+    (4, 1, [5000, 4096, 1, 1025], 1024, 256, 4, 64, 64, True), (2, 3, [129, 136], 128, 0, 1, 64, 32, True), (3, 1, [6000, 5996, 5999], 5995, 9, 0, 128, 64, True),
+    (1, 2, [140000], 30000, 500, 4, 64, 64, True), (5, 2, [9000, 16000, 0, 8191, 16], 4000, 100, 10, 64, 32, False),
 ]
 
 
@@ -279,6 +280,20 @@ def test_evict_odd_weights():
         evict(handle(d), handle(z), budget, 0, 0)
         ref.evict_to(other, budget, 0, 0)
         other.assert_equal(z)
+
+
+@pytest.mark.parametrize("budget", [3, 12])
+def test_evict_more_certain_slots_than_the_budget(budget):
+    """Positions that append did not write: every slot counts as recent; the first ones stay."""
+    require_gpu()
+    for cap, n in ((16, 15), (48, 40)):
+        ref = CacheRef(1, 2, cap, 64, 32, np.random.default_rng(5))
+        ref.set_lengths([n])
+        ref.position[:] = 10 ** 6
+        d = ref.to_cuda()
+        evict(handle(d), handle(d), budget, 1, 0)
+        ref.evict_here(budget, 1, 0)
+        ref.assert_equal(d)
 
 
 def test_append_attend_evict_loop():
