@@ -134,13 +134,6 @@ __device__ __forceinline__ void unpack8(const uint4* raw, float (&v)[8])
     }
 }
 
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 // A condition that is rarely true and the same for the warp: used as the bound of a loop of at most one round, so that
 // the compiler branches around the body instead of executing it under a predicate.
 __device__ __forceinline__ int opaque_zero()

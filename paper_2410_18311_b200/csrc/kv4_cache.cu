@@ -290,37 +290,6 @@ __device__ __forceinline__ int warps_before(int v, int* buf, int warp, int warps
     return __reduce_add_sync(0xffffffffu, lane < warp ? x : 0);
 }
 
-// ---- the CTAs of a cluster; with one CTA all of this is the block's own ----
-__device__ __forceinline__ unsigned cluster_size()
-{
-    unsigned v;
-    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(v));
-    return v;
-}
-__device__ __forceinline__ unsigned cluster_rank()
-{
-    unsigned v;
-    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(v));
-    return v;
-}
-__device__ __forceinline__ void cluster_sync(unsigned size)
-{
-    if (size == 1) {
-        __syncthreads();
-        return;
-    }
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t cluster_address(const void* p, unsigned rank)
-{
-    uint32_t r;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
-    return r;
-}
-__device__ __forceinline__ void cluster_store(uint32_t at, int v) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
-__device__ __forceinline__ void cluster_add(uint32_t at, unsigned v) { asm volatile("red.shared::cluster.add.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
-
 // Sum of v (the same in all threads of a CTA) over the CTAs before this one, and over all; slots is [kEvictMaxCluster].
 __device__ __forceinline__ int ctas_before(int v, int* slots, unsigned rank, unsigned size, int* total)
 {

@@ -199,23 +199,49 @@ __device__ __forceinline__ uint32_t code_word(const uint32_t (&w)[H], int j)
     return w[(j & 1) * (H / 2) + j / 2];
 }
 
-// ---- bounded wait on a copy barrier ----
-// Once a wait has given up, `abort_flag` (shared memory of the CTA) is up and every later wait returns at
-// once: all warps run to their end without waiting, so none is left behind at a barrier.
-constexpr long long kQuantWaitCycles = 3000000000LL;
-__device__ __forceinline__ void bounded_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, unsigned* status)
+// ---- copies into shared memory, 16 bytes a thread, complete in groups ----
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src)
 {
-    if (mbar_try_wait(bar, parity)) return;
-    const long long t0 = clock64();
-    for (;;) {
-        if (mbar_try_wait_parked(bar, parity, 2000u)) return;
-        if (*abort_flag) return;
-        if (clock64() - t0 > kQuantWaitCycles) {
-            *abort_flag = 1;
-            if (status) atomicMax(status, (unsigned)kStatusTimeout);
-            return;
-        }
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// ---- the CTAs of a cluster; with one CTA all of this is the block's own ----
+__device__ __forceinline__ unsigned cluster_size()
+{
+    unsigned v;
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(v));
+    return v;
+}
+__device__ __forceinline__ unsigned cluster_rank()
+{
+    unsigned v;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(v));
+    return v;
+}
+__device__ __forceinline__ void cluster_sync(unsigned size)
+{
+    if (size == 1) {
+        __syncthreads();
+        return;
     }
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_address(const void* p, unsigned rank)
+{
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void cluster_store(uint32_t at, int v) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
+__device__ __forceinline__ void cluster_add(uint32_t at, unsigned v) { asm volatile("red.shared::cluster.add.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory"); }
+__device__ __forceinline__ float cluster_load(uint32_t at)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    return v;
 }
 
 #endif  // __CUDACC__

@@ -63,25 +63,26 @@ w4_quantize_kernel(const T* __restrict__ w, int N, int K, long long sn, long lon
 // read once.  x enters as fp16 after a power-of-two scaling per row and group that puts the group's largest
 // entry into [2^13, 2^14) - exact for bf16 and fp16 x, two parts of 22 bits for fp32 - so that no value of x
 // is out of fp16's range.
-// One persistent CTA per SM: a producer warp streams its row tiles (16 rows, contiguous in memory) through a ring of
-// stages of 16 column blocks; 16 consumer warps take a block of 128 columns of each stage, and their
-// sums meet in shared memory at the end of a row tile.  x is laid out once per CTA as MMA fragments
-// in shared memory; where it does not fit, the columns go in chunks (x laid out again per chunk and 32 row
-// tiles).
-constexpr int kW4Warps = 16;                // consumer warps = column blocks per stage
-constexpr int kW4Threads = 32 * (kW4Warps + 1);
-constexpr int kW4MaxStages = 8;
-constexpr int kW4TileGroup = 32;            // row tiles whose sums are kept over the chunks
-constexpr size_t kW4MaxX = 150 * 1024;      // bytes of x fragments and group factors
+// Each of a CTA's 16 warps streams its own blocks of 16 rows x 128 columns through a ring of its own (cp.async, 16 bytes
+// a lane; refilled as soon as it is read), so no warp waits for another inside a row tile.  A row tile's
+// columns are split over `split` warps where row tiles are few, and over the CTAs of a cluster where the fragments
+// of x, which are laid out once per CTA in shared memory, would not fit one; the partial sums meet in shared memory,
+// in a fixed order, every kW4Round row tiles.
+constexpr int kW4Warps = 16;
+constexpr int kW4Threads = 32 * kW4Warps;
+constexpr int kW4Round = 2;                 // row tiles of a warp between two joins
+constexpr int kW4MaxCluster = 8;
+constexpr size_t kW4MaxX = 100 * 1024;      // bytes of x fragments and group factors in a CTA
+template <int G> constexpr int kW4Stages = G == 32 ? 5 : 6;
 
 struct W4Args {
     const uint8_t* codes;
     const uint8_t* pairs;
     int N, K, batch, act;
     int KB;                 // column blocks of 128
-    int chunk;              // column blocks per chunk of x
+    int share;              // column blocks per CTA of a cluster
     int tiles;              // row tiles
-    int stages;
+    int split;              // warps that share a row tile
     int vec;                // rows of x are 16-byte aligned
     const void* x;
     const void* bias;
@@ -186,197 +187,210 @@ template <typename T, typename Y, int G>
 __global__ void __launch_bounds__(kW4Threads, 1) w4_matvec_kernel(const __grid_constant__ W4Args a)
 {
     constexpr bool SPLIT = sizeof(T) == 4;
-    constexpr int PER = 128 / G;
-    constexpr uint32_t CODES = kW4Warps * 1024, STAGE = CODES + kW4Warps * PER * 64;
+    constexpr int PER = 128 / G, STAGES = kW4Stages<G>, MM = SPLIT ? 2 : 1;          // MMAs of 8 columns: two for fp32 x of over 4 rows
+    constexpr uint32_t STAGE = 1024 + PER * 64;
     const int slots = a.batch * (SPLIT ? 2 : 1);
-    const int halves = SPLIT ? (a.batch + 3) / 4 : 1;        // MMAs of 8 columns: fp32 x of more than 4 rows takes two
+    const bool both = SPLIT && a.batch > 4;
 
     extern __shared__ __align__(128) uint8_t smem[];
-    uint4* xs = reinterpret_cast<uint4*>(smem + (size_t)a.stages * STAGE);
-    float2* xg = reinterpret_cast<float2*>(xs + (size_t)a.chunk * 16 * slots);
-    float* red = reinterpret_cast<float*>(xg + (size_t)a.chunk * PER * a.batch);            // [2][16 warps][8][16]
-    float* ysum = red + 2 * kW4Warps * 128;                                                  // [tile group][8][16], with chunks
-    __shared__ uint64_t full_bar[kW4MaxStages], empty_bar[kW4MaxStages];
-    __shared__ int abort_s;
-    volatile int* abort_flag = &abort_s;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    if (tid == 0) {
-        for (int s = 0; s < a.stages; ++s) {
-            mbar_init(smem_u32(&full_bar[s]), 1);
-            mbar_init(smem_u32(&empty_bar[s]), kW4Warps);
-        }
-        abort_s = 0;
-        mbar_fence_init();
-    }
-    __syncthreads();
-    wait_for_stream();                                       // nothing of an earlier kernel is read or overwritten above
-    let_next_start();
-    const int first = (int)((long long)blockIdx.x * a.tiles / gridDim.x), last = (int)((long long)(blockIdx.x + 1) * a.tiles / gridDim.x);
-    int s = 0;
-    uint32_t ph = 0;
+    uint4* xs = reinterpret_cast<uint4*>(smem + (size_t)kW4Warps * STAGES * STAGE);
+    float2* xg = reinterpret_cast<float2*>(xs + (size_t)a.share * 16 * slots);
+    float* part = reinterpret_cast<float*>(xg + (size_t)a.share * PER * a.batch);           // [16 warps][kW4Round][8][16]
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
+    const unsigned size = cluster_size(), rank = cluster_rank();
 
-    if (warp == kW4Warps) {
-        // ---------------------------------------------------------------- producer --
-        if (lane == 0) {
-            for (int g0 = first; g0 < last && !*abort_flag; g0 += kW4TileGroup) {
-                const int g1 = g0 + kW4TileGroup < last ? g0 + kW4TileGroup : last;
-                for (int c0 = 0; c0 < a.KB && !*abort_flag; c0 += a.chunk) {
-                    const int c1 = c0 + a.chunk < a.KB ? c0 + a.chunk : a.KB;
-                    for (int tile = g0; tile < g1 && !*abort_flag; ++tile)
-                        for (int kb = c0; kb < c1; kb += kW4Warps) {
-                            bounded_wait(smem_u32(&empty_bar[s]), ph ^ 1u, abort_flag, nullptr);
-                            if (*abort_flag) break;
-                            const uint32_t n = c1 - kb < kW4Warps ? c1 - kb : kW4Warps;
-                            const size_t at = (size_t)tile * a.KB + kb;
-                            const uint32_t bar = smem_u32(&full_bar[s]), dst = smem_u32(smem + (size_t)s * STAGE);
-                            mbar_arrive_expect_tx(bar, n * (1024 + PER * 64));
-                            bulk_g2s(dst, a.codes + at * 1024, n * 1024, bar);
-                            bulk_g2s(dst + CODES, a.pairs + at * (PER * 64), n * PER * 64, bar);
-                            if (++s == a.stages) { s = 0; ph ^= 1u; }
-                        }
-                }
+    // this warp's column blocks [k0, k1), counted within the CTA's share [c0, c1) of them, and its row tiles
+    const int c0 = (int)rank * a.share < a.KB ? (int)rank * a.share : a.KB, c1 = c0 + a.share < a.KB ? c0 + a.share : a.KB;
+    const int part_of = warp % a.split, group = warp / a.split, groups = kW4Warps / a.split;
+    const int clusters = gridDim.x / size, cluster = blockIdx.x / size;
+    const int each = (c1 - c0 + a.split - 1) / a.split;
+    const int k0 = part_of * each < c1 - c0 ? part_of * each : c1 - c0, k1 = k0 + each < c1 - c0 ? k0 + each : c1 - c0;
+    // a group's i-th row tile: consecutive tiles go to different clusters
+    auto tile_of = [&](int i) { return (i * groups + group) * clusters + cluster; };
+
+    wait_for_stream();
+    let_next_start();
+    const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * STAGES) * STAGE;
+    int f_i = 0, f_k = k0;                                   // the block that is copied next
+    auto feed = [&](uint32_t at) {
+        const int tile = tile_of(f_i);
+        if (tile < a.tiles && k0 < k1) {
+            const size_t block = (size_t)tile * a.KB + c0 + f_k;
+            const uint8_t* codes = a.codes + block * 1024 + lane * 16;
+            copy16(at + lane * 16, codes);
+            copy16(at + lane * 16 + 512, codes + 512);
+            if (lane < PER * 4) copy16(at + 1024 + lane * 16, a.pairs + block * (PER * 64) + lane * 16);
+            if (++f_k == k1) {
+                f_k = k0;
+                ++f_i;
             }
         }
-    } else {
-        // --------------------------------------------------------------- consumers --
-        const int gid = lane >> 2, tig = lane & 3;
-        // columns beyond the rows of x repeat the first one; nobody reads their sums
-        const int xcol0 = (gid < slots ? gid : 0) * 4 + tig, xcol1 = (8 + gid < slots ? 8 + gid : 0) * 4 + tig;
-        int par = 0;
-        for (int g0 = first; g0 < last; g0 += kW4TileGroup) {
-            const int g1 = g0 + kW4TileGroup < last ? g0 + kW4TileGroup : last;
-            for (int c0 = 0; c0 < a.KB; c0 += a.chunk) {
-                const int c1 = c0 + a.chunk < a.KB ? c0 + a.chunk : a.KB;
-                if (g0 == first || a.chunk < a.KB) {
-                    if (c0 > 0 || g0 > first) named_bar_sync(1, 32 * kW4Warps);      // the last chunk's use is over
-                    stage_x<T, G>(a, c0, c1 - c0, xs, xg, tid);
-                    named_bar_sync(1, 32 * kW4Warps);
-                }
-                for (int tile = g0; tile < g1; ++tile) {
-                    float y[2][4];                           // [MMA of 8 columns][rows gid, gid + 8 x two columns]
+        copy_commit();                                       // one group per stage, empty ones too
+    };
+#pragma unroll 1
+    for (int s = 0; s < STAGES; ++s) feed(ring + s * STAGE);
+    stage_x<T, G>(a, c0, c1 - c0, xs, xg, tid);
+    __syncthreads();
+
+    uint32_t stage = 0;
+    // columns beyond the rows of x repeat the first one; nobody reads their sums
+    const int xcol0 = (gid < slots ? gid : 0) * 4 + tig, xcol1 = (8 + gid < slots ? 8 + gid : 0) * 4 + tig;
+    int gx[MM][SPLIT ? 1 : 2];                               // rows of x of this lane's columns
 #pragma unroll
-                    for (int m = 0; m < 2; ++m)
+    for (int m = 0; m < MM; ++m)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) y[m][e] = 0.f;
-                    for (int kb0 = c0; kb0 < c1; kb0 += kW4Warps) {
-                        bounded_wait(smem_u32(&full_bar[s]), ph, abort_flag, nullptr);
-                        const int kb = kb0 + warp - c0;      // within the chunk
-                        if (kb < c1 - c0) {
-                            const uint8_t* st = smem + (size_t)s * STAGE;
-                            const uint4 r0 = *reinterpret_cast<const uint4*>(st + warp * 1024 + gid * 64 + tig * 16);
-                            const uint4 r1 = *reinterpret_cast<const uint4*>(st + warp * 1024 + 512 + gid * 64 + tig * 16);
-                            const uint32_t w0[4] = {r0.x, r0.y, r0.z, r0.w}, w1[4] = {r1.x, r1.y, r1.z, r1.w};
-                            const __half2* pr = reinterpret_cast<const __half2*>(st + CODES + warp * (PER * 64));
+        for (int i = 0; i < (SPLIT ? 1 : 2); ++i) {
+            const int b = SPLIT ? m * 4 + tig : 2 * tig + i;
+            gx[m][i] = b < a.batch ? b : 0;
+        }
+    for (int i0 = 0; i0 * groups * clusters + cluster < a.tiles; i0 += kW4Round) {           // the same rounds for a whole cluster
+        for (int j = 0; j < kW4Round; ++j) {
+            const int tile = tile_of(i0 + j);
+            if (tile >= a.tiles) break;
+            float y[MM][4];                                  // rows gid, gid + 8 x two columns
 #pragma unroll
-                            for (int g = 0; g < PER; ++g) {
-                                float acc[2][4];
+            for (int m = 0; m < MM; ++m)
 #pragma unroll
-                                for (int m = 0; m < 2; ++m)
+                for (int e = 0; e < 4; ++e) y[m][e] = 0.f;
+#pragma unroll 1
+            for (int kb = k0; kb < k1; ++kb) {
+                copy_wait<STAGES - 1>();
+                __syncwarp();
+                const uint8_t* st = smem + (size_t)(warp * STAGES) * STAGE + stage;
+                const uint4 r0 = *reinterpret_cast<const uint4*>(st + gid * 64 + tig * 16);
+                const uint4 r1 = *reinterpret_cast<const uint4*>(st + 512 + gid * 64 + tig * 16);
+                const uint32_t w0[4] = {r0.x, r0.y, r0.z, r0.w}, w1[4] = {r1.x, r1.y, r1.z, r1.w};
+                const __half2* pr = reinterpret_cast<const __half2*>(st + 1024);
+                const uint4* xf = xs + (size_t)kb * slots * 16;
+                const float2* gk = xg + (size_t)kb * PER * a.batch;
 #pragma unroll
-                                    for (int e = 0; e < 4; ++e) acc[m][e] = 0.f;
+                for (int g = 0; g < PER; ++g) {
+                    float acc[MM][4];
 #pragma unroll
-                                for (int j = g * G / 32; j < (g + 1) * G / 32; ++j) {
-                                    const uint32_t x0 = code_word<G, 4>(w0, j), x1 = code_word<G, 4>(w1, j);
-                                    const uint32_t y0 = x0 >> 8, y1 = x1 >> 8;
-                                    const uint4* xf = xs + (size_t)(kb * 4 + j) * slots * 4;
+                    for (int q = g * G / 32; q < (g + 1) * G / 32; ++q) {
+                        const uint32_t x0 = code_word<G, 4>(w0, q), x1 = code_word<G, 4>(w1, q);
+                        const uint32_t y0 = x0 >> 8, y1 = x1 >> 8;
+                        const uint32_t a0 = x0 & 0x000f000fu, a1 = x1 & 0x000f000fu, a2 = y0 & 0x000f000fu, a3 = y1 & 0x000f000fu;
+                        const uint32_t b0 = x0 & 0x00f000f0u, b1 = x1 & 0x00f000f0u, b2 = y0 & 0x00f000f0u, b3 = y1 & 0x00f000f0u;
 #pragma unroll
-                                    for (int m = 0; m < (SPLIT ? 2 : 1); ++m) {
-                                        if (m == 1 && halves == 1) break;
-                                        const uint4 f = xf[m == 0 ? xcol0 : xcol1];
-                                        mma_16816(acc[m], x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, f.x, f.y);
-                                        mma_16816(acc[m], x0 & 0x00f000f0u, x1 & 0x00f000f0u, y0 & 0x00f000f0u, y1 & 0x00f000f0u, f.z, f.w);
-                                    }
-                                }
-                                const float2 p0 = __half22float2(pr[g * 16 + gid]), p1 = __half22float2(pr[g * 16 + gid + 8]);
-                                const float s0 = p0.x * kCodeScaleLow, s1 = p1.x * kCodeScaleLow;
-                                const float2* gx = xg + (size_t)(kb * PER + g) * a.batch;
+                        for (int m = 0; m < MM; ++m) {
+                            if (m == 1 && !both) break;
+                            const uint4 f = xf[q * slots * 4 + (m == 0 ? xcol0 : xcol1)];
+                            if (q == g * G / 32) mma_16816_zero(acc[m], a0, a1, a2, a3, f.x, f.y);
+                            else mma_16816(acc[m], a0, a1, a2, a3, f.x, f.y);
+                            mma_16816(acc[m], b0, b1, b2, b3, f.z, f.w);
+                        }
+                    }
+                    const float2 p0 = __half22float2(pr[g * 16 + gid]), p1 = __half22float2(pr[g * 16 + gid + 8]);
+                    const float s0 = p0.x * kCodeScaleLow, s1 = p1.x * kCodeScaleLow;
 #pragma unroll
-                                for (int m = 0; m < (SPLIT ? 2 : 1); ++m) {
-                                    if (m == 1 && halves == 1) break;
-                                    if (SPLIT) {             // the two parts of a row of x stand in neighbouring columns
-                                        const int b = m * 4 + tig;
-                                        const float2 e = gx[b < a.batch ? b : 0];
-                                        y[m][0] = fmaf(s0 * (acc[m][0] + acc[m][1]), e.x, fmaf(p0.y, e.y, y[m][0]));
-                                        y[m][2] = fmaf(s1 * (acc[m][2] + acc[m][3]), e.x, fmaf(p1.y, e.y, y[m][2]));
-                                    } else {
+                    for (int m = 0; m < MM; ++m) {
+                        if (m == 1 && !both) break;
+                        if (SPLIT) {                         // the two parts of a row of x stand in neighbouring columns
+                            const float2 e = gk[g * a.batch + gx[m][0]];
+                            y[m][0] = fmaf(s0 * (acc[m][0] + acc[m][1]), e.x, fmaf(p0.y, e.y, y[m][0]));
+                            y[m][2] = fmaf(s1 * (acc[m][2] + acc[m][3]), e.x, fmaf(p1.y, e.y, y[m][2]));
+                        } else {
 #pragma unroll
-                                        for (int i = 0; i < 2; ++i) {
-                                            const int b = 2 * tig + i;
-                                            const float2 e = gx[b < a.batch ? b : 0];
-                                            y[m][i] = fmaf(s0 * acc[m][i], e.x, fmaf(p0.y, e.y, y[m][i]));
-                                            y[m][2 + i] = fmaf(s1 * acc[m][2 + i], e.x, fmaf(p1.y, e.y, y[m][2 + i]));
-                                        }
-                                    }
-                                }
+                            for (int i = 0; i < 2; ++i) {
+                                const float2 e = gk[g * a.batch + gx[m][SPLIT ? 0 : i]];
+                                y[m][i] = fmaf(s0 * acc[m][i], e.x, fmaf(p0.y, e.y, y[m][i]));
+                                y[m][2 + i] = fmaf(s1 * acc[m][2 + i], e.x, fmaf(p1.y, e.y, y[m][2 + i]));
                             }
                         }
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(smem_u32(&empty_bar[s]));
-                        if (++s == a.stages) { s = 0; ph ^= 1u; }
-                    }
-                    // the warps' sums, [row of x][output row]; the other buffer may still be read for the tile before
-                    float* buf = red + (size_t)par * kW4Warps * 128;
-                    par ^= 1;
-#pragma unroll
-                    for (int m = 0; m < (SPLIT ? 2 : 1); ++m)
-#pragma unroll
-                        for (int i = 0; i < (SPLIT ? 1 : 2); ++i) {
-                            const int b = SPLIT ? m * 4 + tig : 2 * tig + i;
-                            buf[warp * 128 + b * 16 + gid] = y[m][i];
-                            buf[warp * 128 + b * 16 + gid + 8] = y[m][2 + i];
-                        }
-                    named_bar_sync(1, 32 * kW4Warps);
-                    if (tid < a.batch * 16) {
-                        float v = 0.f;
-#pragma unroll
-                        for (int w = 0; w < kW4Warps; ++w) v += buf[w * 128 + tid];
-                        const int b = tid >> 4, n = tile * 16 + (tid & 15);
-                        if (a.chunk < a.KB) {
-                            float* keep = ysum + (tile - g0) * 128 + tid;
-                            if (c0 > 0) v += *keep;
-                            *keep = v;
-                        }
-                        if (c1 == a.KB && n < a.N) {
-                            if (a.bias) v += to_f32<T>(((const T*)a.bias)[n]);
-                            v = w4_act(v, a.act);
-                            if (a.mul) v *= to_f32<Y>(((const Y*)a.mul)[(long long)b * a.ld_mul + n]);
-                            if (*abort_flag) v = __int_as_float(0x7fffffff);         // no sum of what did not arrive
-                            ((Y*)a.y)[(long long)b * a.ld_y + n] = from_f32<Y>(v);
-                        }
                     }
                 }
+                __syncwarp();                                // all lanes have read the stage
+                feed(ring + stage);
+                stage = stage + STAGE == STAGES * STAGE ? 0 : stage + STAGE;
             }
+            float* buf = part + (warp * kW4Round + j) * 128;                                 // [row of x][output row]
+#pragma unroll
+            for (int m = 0; m < MM; ++m)
+#pragma unroll
+                for (int i = 0; i < (SPLIT ? 1 : 2); ++i) {
+                    const int b = SPLIT ? m * 4 + tig : 2 * tig + i;
+                    buf[b * 16 + gid] = y[m][i];
+                    buf[b * 16 + gid + 8] = y[m][2 + i];
+                }
         }
+        cluster_sync(size);
+        // the outputs of the round: the row tiles go round the cluster's CTAs
+        const int per_tile = a.batch * 16;
+        for (int o = tid; o < groups * kW4Round * per_tile; o += kW4Threads) {
+            const int at = o / per_tile, r = o - at * per_tile, g = at / kW4Round, j = at % kW4Round;
+            if (at % (int)size != (int)rank) continue;
+            const int n = ((((i0 + j) * groups + g) * clusters + cluster) << 4) + (r & 15), b = r >> 4;
+            if (n >= a.N) continue;
+            float v = 0.f;
+            for (unsigned c = 0; c < size; ++c)
+                for (int q = 0; q < a.split; ++q) {
+                    const float* from = part + ((g * a.split + q) * kW4Round + j) * 128 + r;
+                    v += size == 1 ? *from : cluster_load(cluster_address(from, c));
+                }
+            if (a.bias) v += to_f32<T>(((const T*)a.bias)[n]);
+            v = w4_act(v, a.act);
+            if (a.mul) v *= to_f32<Y>(((const Y*)a.mul)[(long long)b * a.ld_mul + n]);
+            ((Y*)a.y)[(long long)b * a.ld_y + n] = from_f32<Y>(v);
+        }
+        cluster_sync(size);                                  // the sums may be overwritten; in the end, no CTA leaves while another reads its
     }
-    __syncthreads();
-    if (tid == 0 && *abort_flag) {
-        // after a wait that gave up copies may be in flight: give them a bounded time to land
-        const long long t0 = clock64();
-        while (clock64() - t0 < 20000000LL) __nanosleep(1000);
-    }
-    __syncthreads();
+}
+
+// Clusters of `cluster` CTAs of a kernel that the GPU holds at once, asked once per kernel, device and size.
+template <auto Kernel>
+static int clusters_at_once(const DeviceInfo& di, int cluster, size_t smem)
+{
+    if (cluster == 1) return di.sm_count;
+    static std::atomic<int> known[64][4];
+    const int log = cluster == 2 ? 1 : (cluster == 4 ? 2 : 3);
+    std::atomic<int>& slot = known[di.device & 63][log];
+    int n = slot.load(std::memory_order_relaxed);
+    if (n > 0) return n;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(cluster * di.sm_count);
+    cfg.blockDim = dim3(kW4Threads);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = cluster;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, Kernel, &cfg) != cudaSuccess || n < 1) n = di.sm_count / (2 * cluster);
+    slot.store(n, std::memory_order_relaxed);
+    return n;
 }
 
 template <typename T, typename Y, int G>
 static coreinfer_status launch_group(W4Args& a, const DeviceInfo& di, cudaStream_t st)
 {
     constexpr int PER = 128 / G;
-    constexpr size_t STAGE = (size_t)kW4Warps * (1024 + PER * 64);
+    constexpr size_t RING = (size_t)kW4Warps * kW4Stages<G> * (1024 + PER * 64), PART = (size_t)kW4Warps * kW4Round * 128 * sizeof(float);
     const int slots = a.batch * (sizeof(T) == 4 ? 2 : 1);
     const size_t per_block = (size_t)slots * 256 + (size_t)PER * a.batch * sizeof(float2);
-    a.chunk = a.KB;
-    if (a.chunk * per_block > kW4MaxX) a.chunk = (int)(kW4MaxX / per_block) / kW4Warps * kW4Warps;
-    const size_t fixed = a.chunk * per_block + 2 * kW4Warps * 128 * sizeof(float) +
-                         (a.chunk < a.KB ? (size_t)kW4TileGroup * 128 * sizeof(float) : 0);
-    const size_t room = smem_room(di);
-    int stages = (int)((room - fixed) / STAGE);
-    if (stages > kW4MaxStages) stages = kW4MaxStages;
-    if (room < fixed || stages < 2) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "not enough shared memory for two pipeline stages");
-    a.stages = stages;
-    const size_t smem = fixed + stages * STAGE;
+    int cluster = 1;
+    while (cluster < kW4MaxCluster && (size_t)((a.KB + cluster - 1) / cluster) * per_block > kW4MaxX) cluster *= 2;
+    a.share = (a.KB + cluster - 1) / cluster;
+    if (a.share * per_block > kW4MaxX)
+        CI_FAIL(COREINFER_ERR_UNSUPPORTED, "K %d: with %d rows of x at most %d columns", a.K, a.batch,
+                (int)(kW4MaxX / per_block) * kW4MaxCluster * 128);
+    const size_t smem = RING + PART + a.share * per_block;
     const coreinfer_status s = allow_smem<w4_matvec_kernel<T, Y, G>>(di);
     if (s != COREINFER_OK) return s;
-    CI_CUDA(launch_overlapped(w4_matvec_kernel<T, Y, G>, dim3(a.tiles < di.sm_count ? a.tiles : di.sm_count), dim3(kW4Threads), smem, st, a));
+    int clusters = clusters_at_once<w4_matvec_kernel<T, Y, G>>(di, cluster, smem);
+    if (clusters > a.tiles) clusters = a.tiles;
+    // Warps per row tile: as many as make the longest warp's list of blocks shortest.
+    long long best = 0;
+    for (int split = 1; split <= kW4Warps; split *= 2) {
+        const long long groups = (long long)clusters * (kW4Warps / split);
+        const long long cost = ((a.tiles + groups - 1) / groups) * ((a.share + split - 1) / split);
+        if (split == 1 || cost < best) {
+            best = cost;
+            a.split = split;
+        }
+    }
+    CI_CUDA(launch_overlapped(w4_matvec_kernel<T, Y, G>, dim3(clusters * cluster), dim3(kW4Threads), smem, st, a, cluster));
     return COREINFER_OK;
 }
 
