@@ -122,23 +122,34 @@ __device__ __forceinline__ void stage_x(const W4Args& a, int kb0, int nkb, uint4
     constexpr bool SPLIT = sizeof(T) == 4;
     constexpr int PER = 128 / G, UNROLL = 2;
     const int l16 = tid & 15, h = l16 >> 2, tig = l16 & 3, hw = tid >> 4;
-    const int slots = a.batch * (SPLIT ? 2 : 1), tasks = nkb * a.batch;
-    for (int base = hw & ~1; base < tasks; base += 2 * kW4Warps * UNROLL) {         // the same count for both halves of a warp
-        const int t0 = base | (hw & 1);
+    const int slots = a.batch * (SPLIT ? 2 : 1);
+    // task t: block t % nkb of row t / nkb; a half-warp's next task is 32 further on
+    int b0 = 0, kb0_ = hw;
+    auto settle = [&](int& b, int& kb) {
+        while (kb >= nkb) {
+            kb -= nkb;
+            ++b;
+        }
+    };
+    if (nkb == 0) return;
+    settle(b0, kb0_);
+    for (int base = hw & ~1; base < nkb * a.batch; base += 2 * kW4Warps * UNROLL) {          // the same count for both halves of a warp
         float v[UNROLL][8];
+        int bs[UNROLL], ks[UNROLL];
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
-            const int t = t0 + u * 2 * kW4Warps;
-            const int b = t / nkb, kb = t % nkb;
-            if (t < tasks) load_x8<T>((const T*)a.x + (long long)b * a.ld_x, (kb0 + kb) * 128 + h * 32 + tig * 8, a.K, a.vec, v[u]);
+            bs[u] = b0;
+            ks[u] = kb0_;
+            if (b0 < a.batch) load_x8<T>((const T*)a.x + (long long)b0 * a.ld_x, (kb0 + kb0_) * 128 + h * 32 + tig * 8, a.K, a.vec, v[u]);
             else
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[u][e] = 0.f;
+            kb0_ += 2 * kW4Warps;
+            settle(b0, kb0_);
         }
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
-            const int t = t0 + u * 2 * kW4Warps;
-            const int b = t / nkb, kb = t % nkb;
+            const int b = bs[u], kb = ks[u];
             float m = 0.f, sum = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -166,7 +177,7 @@ __device__ __forceinline__ void stage_x(const W4Args& a, int kb0, int nkb, uint4
                     q[e] = h & 1 ? v[u][4 + e] : other;
                 }
             }
-            if (t >= tasks) continue;
+            if (b >= a.batch) continue;
             const int x = range_exponent(m);
             const float up = pow2(14 - x), up16 = up * (1.f / 16.f);          // odd codes stand 16 times higher
 #pragma unroll
@@ -211,42 +222,52 @@ __global__ void __launch_bounds__(kW4Threads, 1) w4_matvec_kernel(const __grid_c
     wait_for_stream();
     let_next_start();
     const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * STAGES) * STAGE;
-    int f_i = 0, f_k = k0;                                   // the block that is copied next
-    auto feed = [&](uint32_t at) {
+    int f_i = 0, f_left = 0;                                 // the row tile that is copied, its blocks still to copy
+    const uint8_t *f_codes = nullptr, *f_pairs = nullptr;    // this lane's part of the next block
+    auto feed_open = [&]() {
         const int tile = tile_of(f_i);
-        if (tile < a.tiles && k0 < k1) {
-            const size_t block = (size_t)tile * a.KB + c0 + f_k;
-            const uint8_t* codes = a.codes + block * 1024 + lane * 16;
-            copy16(at + lane * 16, codes);
-            copy16(at + lane * 16 + 512, codes + 512);
-            if (lane < PER * 4) copy16(at + 1024 + lane * 16, a.pairs + block * (PER * 64) + lane * 16);
-            if (++f_k == k1) {
-                f_k = k0;
+        f_left = tile < a.tiles ? k1 - k0 : 0;
+        const size_t block = (size_t)tile * a.KB + c0 + k0;
+        f_codes = a.codes + block * 1024 + lane * 16;
+        f_pairs = a.pairs + block * (PER * 64) + lane * 16;
+    };
+    feed_open();
+    auto feed = [&](uint32_t at) {
+        if (f_left > 0) {
+            copy16(at, f_codes);
+            copy16(at + 512, f_codes + 512);
+            if (lane < PER * 4) copy16(at + 1024, f_pairs);
+            f_codes += 1024;
+            f_pairs += PER * 64;
+            if (--f_left == 0) {
                 ++f_i;
+                feed_open();
             }
         }
         copy_commit();                                       // one group per stage, empty ones too
     };
 #pragma unroll 1
-    for (int s = 0; s < STAGES; ++s) feed(ring + s * STAGE);
+    for (int s = 0; s < STAGES; ++s) feed(ring + lane * 16 + s * STAGE);
     stage_x<T, G>(a, c0, c1 - c0, xs, xg, tid);
     __syncthreads();
 
     uint32_t stage = 0;
     // columns beyond the rows of x repeat the first one; nobody reads their sums
-    const int xcol0 = (gid < slots ? gid : 0) * 4 + tig, xcol1 = (8 + gid < slots ? 8 + gid : 0) * 4 + tig;
-    int gx[MM][SPLIT ? 1 : 2];                               // rows of x of this lane's columns
+    const uint32_t xcol0 = ((gid < slots ? gid : 0) * 4 + tig) * 16, xcol1 = ((8 + gid < slots ? 8 + gid : 0) * 4 + tig) * 16 - xcol0;
+    const uint32_t xstep = slots * 64, gstep = a.batch * sizeof(float2);      // bytes between pieces of 32 columns, between groups
+    uint32_t gx[MM][SPLIT ? 1 : 2];                               // rows of x of this lane's columns
 #pragma unroll
     for (int m = 0; m < MM; ++m)
 #pragma unroll
         for (int i = 0; i < (SPLIT ? 1 : 2); ++i) {
             const int b = SPLIT ? m * 4 + tig : 2 * tig + i;
-            gx[m][i] = b < a.batch ? b : 0;
+            gx[m][i] = (b < a.batch ? b : 0) * sizeof(float2);
         }
     for (int i0 = 0; i0 * groups * clusters + cluster < a.tiles; i0 += kW4Round) {           // the same rounds for a whole cluster
         for (int j = 0; j < kW4Round; ++j) {
             const int tile = tile_of(i0 + j);
             if (tile >= a.tiles) break;
+            uint32_t xa = smem_u32(xs) + k0 * 4 * xstep + xcol0, ga = smem_u32(xg) + k0 * PER * gstep;
             float y[MM][4];                                  // rows gid, gid + 8 x two columns
 #pragma unroll
             for (int m = 0; m < MM; ++m)
@@ -256,13 +277,9 @@ __global__ void __launch_bounds__(kW4Threads, 1) w4_matvec_kernel(const __grid_c
             for (int kb = k0; kb < k1; ++kb) {
                 copy_wait<STAGES - 1>();
                 __syncwarp();
-                const uint8_t* st = smem + (size_t)(warp * STAGES) * STAGE + stage;
-                const uint4 r0 = *reinterpret_cast<const uint4*>(st + gid * 64 + tig * 16);
-                const uint4 r1 = *reinterpret_cast<const uint4*>(st + 512 + gid * 64 + tig * 16);
+                const uint32_t st = ring + stage;            // a lane's 16 bytes of the codes of rows gid and gid + 8 stand at lane * 16
+                const uint4 r0 = lds128(st + lane * 16), r1 = lds128(st + lane * 16 + 512);
                 const uint32_t w0[4] = {r0.x, r0.y, r0.z, r0.w}, w1[4] = {r1.x, r1.y, r1.z, r1.w};
-                const __half2* pr = reinterpret_cast<const __half2*>(st + 1024);
-                const uint4* xf = xs + (size_t)kb * slots * 16;
-                const float2* gk = xg + (size_t)kb * PER * a.batch;
 #pragma unroll
                 for (int g = 0; g < PER; ++g) {
                     float acc[MM][4];
@@ -275,25 +292,25 @@ __global__ void __launch_bounds__(kW4Threads, 1) w4_matvec_kernel(const __grid_c
 #pragma unroll
                         for (int m = 0; m < MM; ++m) {
                             if (m == 1 && !both) break;
-                            const uint4 f = xf[q * slots * 4 + (m == 0 ? xcol0 : xcol1)];
+                            const uint4 f = lds128((m == 0 ? xa : xa + xcol1) + q * xstep);
                             if (q == g * G / 32) mma_16816_zero(acc[m], a0, a1, a2, a3, f.x, f.y);
                             else mma_16816(acc[m], a0, a1, a2, a3, f.x, f.y);
                             mma_16816(acc[m], b0, b1, b2, b3, f.z, f.w);
                         }
                     }
-                    const float2 p0 = __half22float2(pr[g * 16 + gid]), p1 = __half22float2(pr[g * 16 + gid + 8]);
+                    const float2 p0 = lds_half2(st + 1024 + g * 64 + gid * 4), p1 = lds_half2(st + 1024 + g * 64 + gid * 4 + 32);
                     const float s0 = p0.x * kCodeScaleLow, s1 = p1.x * kCodeScaleLow;
 #pragma unroll
                     for (int m = 0; m < MM; ++m) {
                         if (m == 1 && !both) break;
                         if (SPLIT) {                         // the two parts of a row of x stand in neighbouring columns
-                            const float2 e = gk[g * a.batch + gx[m][0]];
+                            const float2 e = lds_f32x2(ga + g * gstep + gx[m][0]);
                             y[m][0] = fmaf(s0 * (acc[m][0] + acc[m][1]), e.x, fmaf(p0.y, e.y, y[m][0]));
                             y[m][2] = fmaf(s1 * (acc[m][2] + acc[m][3]), e.x, fmaf(p1.y, e.y, y[m][2]));
                         } else {
 #pragma unroll
                             for (int i = 0; i < 2; ++i) {
-                                const float2 e = gk[g * a.batch + gx[m][SPLIT ? 0 : i]];
+                                const float2 e = lds_f32x2(ga + g * gstep + gx[m][SPLIT ? 0 : i]);
                                 y[m][i] = fmaf(s0 * acc[m][i], e.x, fmaf(p0.y, e.y, y[m][i]));
                                 y[m][2 + i] = fmaf(s1 * acc[m][2 + i], e.x, fmaf(p1.y, e.y, y[m][2 + i]));
                             }
@@ -301,7 +318,9 @@ __global__ void __launch_bounds__(kW4Threads, 1) w4_matvec_kernel(const __grid_c
                     }
                 }
                 __syncwarp();                                // all lanes have read the stage
-                feed(ring + stage);
+                feed(ring + lane * 16 + stage);
+                xa += 4 * xstep;
+                ga += PER * gstep;
                 stage = stage + STAGE == STAGES * STAGE ? 0 : stage + STAGE;
             }
             float* buf = part + (warp * kW4Round + j) * 128;                                 // [row of x][output row]
