@@ -115,25 +115,6 @@ __device__ __forceinline__ void store4(T* dst, float x, float y, float z, float 
     else *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<uint2*>(v);
 }
 
-// The eight values of one (16-bit types) or two 16-byte words.
-template <typename T>
-__device__ __forceinline__ void unpack8(const uint4* raw, float (&v)[8])
-{
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-        const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if constexpr (sizeof(T) == 4) v[4 * i + e] = __uint_as_float(w[e]);
-            else {
-                v[2 * e] = to_f32<T>(*reinterpret_cast<const T*>(&w[e]));
-                const uint32_t high = w[e] >> 16;
-                v[2 * e + 1] = to_f32<T>(*reinterpret_cast<const T*>(&high));
-            }
-        }
-    }
-}
-
 // A condition that is rarely true and the same for the warp: used as the bound of a loop of at most one round, so that
 // the compiler branches around the body instead of executing it under a predicate.
 __device__ __forceinline__ int opaque_zero()

@@ -63,17 +63,15 @@ w4_quantize_kernel(const T* __restrict__ w, int N, int K, long long sn, long lon
 // read once.  x enters as fp16 after a power-of-two scaling per row and group that puts the group's largest
 // entry into [2^13, 2^14) - exact for bf16 and fp16 x, two parts of 22 bits for fp32 - so that no value of x
 // is out of fp16's range.
-// Each of a CTA's 16 warps streams its own blocks of 16 rows x 128 columns through a ring of its own (cp.async, 16 bytes
-// a lane; refilled as soon as it is read), so no warp waits for another inside a row tile.  A row tile's
-// columns are split over `split` warps where row tiles are few, and over the CTAs of a cluster where the fragments
-// of x, which are laid out once per CTA in shared memory, would not fit one; the partial sums meet in shared memory,
-// in a fixed order, every kW4Round row tiles.
+// Each of a CTA's 16 warps streams its own blocks of 32 rows (two row tiles: the fragments of x are read once for both) x
+// 128 columns through a ring of its own (cp.async, 16 bytes a lane; refilled as soon as it is read), so no warp waits for
+// another inside a pair of row tiles.  A pair's columns are split over `split` warps where pairs are few, and over
+// the CTAs of a cluster where the fragments of x, which are laid out once per CTA in shared memory, would not fit
+// one; the partial sums meet in shared memory, in a fixed order, after every pair.
 constexpr int kW4Warps = 16;
 constexpr int kW4Threads = 32 * kW4Warps;
-constexpr int kW4Round = 2;                 // row tiles of a warp between two joins
 constexpr int kW4MaxCluster = 8;
-constexpr size_t kW4MaxX = 100 * 1024;      // bytes of x fragments and group factors in a CTA
-template <int G> constexpr int kW4Stages = G == 32 ? 5 : 6;
+constexpr int kW4Stages = 3;                // of two column blocks
 
 struct W4Args {
     const uint8_t* codes;
@@ -82,7 +80,7 @@ struct W4Args {
     int KB;                 // column blocks of 128
     int share;              // column blocks per CTA of a cluster
     int tiles;              // row tiles
-    int split;              // warps that share a row tile
+    int split;              // warps that share a pair of row tiles
     int vec;                // rows of x are 16-byte aligned
     const void* x;
     const void* bias;
@@ -98,86 +96,106 @@ __device__ __forceinline__ float w4_act(float v, int act)
     return v;
 }
 
-// Eight entries of a row of x from column k on, zeros beyond K.
+// Eight entries of a row of x from column k on as they are in memory, zeros beyond K.
 template <typename T>
-__device__ __forceinline__ void load_x8(const T* row, int k, int K, int vec, float (&v)[8])
+__device__ __forceinline__ void load_x8(const T* row, int k, int K, int vec, uint4 (&raw)[sizeof(T) / 2])
 {
     if (vec && k + 8 <= K) {
-        T in[8];
-        *reinterpret_cast<uint4*>(in) = *reinterpret_cast<const uint4*>(row + k);
-        if (sizeof(T) == 4) reinterpret_cast<uint4*>(in)[1] = *reinterpret_cast<const uint4*>(row + k + 4);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = to_f32<T>(in[e]);
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[i] = reinterpret_cast<const uint4*>(row + k)[i];
     } else {
+        T v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = k + e < K ? to_f32<T>(row[k + e]) : 0.f;
+        for (int e = 0; e < 8; ++e) v[e] = k + e < K ? row[k + e] : from_f32<T>(0.f);
+        uint32_t w[2 * sizeof(T)];
+#pragma unroll
+        for (int i = 0; i < (int)(2 * sizeof(T)); ++i) {
+            if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(to_f32<T>(v[i]));
+            else w[i] = *reinterpret_cast<uint16_t*>(&v[2 * i]) | (uint32_t)*reinterpret_cast<uint16_t*>(&v[2 * i + 1]) << 16;
+        }
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
     }
 }
 
-// Lays columns [kb0, kb0 + nkb) of x out as B fragments: xs[block][32-value piece][column of the MMA][4 lanes] of 16 bytes,
-// and xg[group][row] = (2^(x - 14), sum of the group's entries).  A half-warp per block and row of x.
+// Lays columns [kb0, kb0 + nkb) x 128 of x out as B fragments: xs[block][step (code_word)][column of the MMA][4 lanes] of
+// 16 bytes, and xg[group][row] = (2^(x - 14), sum of the group's entries).  A half-warp per block and row of x; a round
+// of kXLoads tasks is loaded at once, and the first round before the caller fills the memory system with weights.
+constexpr int kXLoads = 5;
 template <typename T, int G>
-__device__ __forceinline__ void stage_x(const W4Args& a, int kb0, int nkb, uint4* xs, float2* xg, int tid)
-{
-    constexpr bool SPLIT = sizeof(T) == 4;
-    constexpr int PER = 128 / G, UNROLL = 2;
-    const int l16 = tid & 15, h = l16 >> 2, tig = l16 & 3, hw = tid >> 4;
-    const int slots = a.batch * (SPLIT ? 2 : 1);
-    // task t: block t % nkb of row t / nkb; a half-warp's next task is 32 further on
-    int b0 = 0, kb0_ = hw;
-    auto settle = [&](int& b, int& kb) {
-        while (kb >= nkb) {
+struct XStage {
+    static constexpr bool SPLIT = sizeof(T) == 4;
+    static constexpr int PER = 128 / G;
+    const W4Args& a;
+    const int kb0, nkb, l16, h, tig;
+    int b, kb, base;                                        // the next task: block kb of row b; a half-warp's next is 32 further on
+    uint4 raw[kXLoads][sizeof(T) / 2];
+    int bs[kXLoads], ks[kXLoads];
+
+    __device__ __forceinline__ XStage(const W4Args& args, int first, int count, int tid)
+        : a(args), kb0(first), nkb(count), l16(tid & 15), h((tid & 15) >> 2), tig(tid & 3), b(0), kb(tid >> 4), base((tid >> 4) & ~1)
+    {
+        settle();
+    }
+    __device__ __forceinline__ void settle()
+    {
+        if (nkb == 0) b = a.batch;
+        while (b < a.batch && kb >= nkb) {
             kb -= nkb;
             ++b;
         }
-    };
-    if (nkb == 0) return;
-    settle(b0, kb0_);
-    for (int base = hw & ~1; base < nkb * a.batch; base += 2 * kW4Warps * UNROLL) {          // the same count for both halves of a warp
-        float v[UNROLL][8];
-        int bs[UNROLL], ks[UNROLL];
+    }
+    // Whether there is a round left; the same for both halves of a warp.
+    __device__ __forceinline__ bool more() const { return base < nkb * a.batch; }
+    __device__ __forceinline__ void load()
+    {
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            bs[u] = b0;
-            ks[u] = kb0_;
-            if (b0 < a.batch) load_x8<T>((const T*)a.x + (long long)b0 * a.ld_x, (kb0 + kb0_) * 128 + h * 32 + tig * 8, a.K, a.vec, v[u]);
-            else
+        for (int u = 0; u < kXLoads; ++u) {
+            bs[u] = b;
+            ks[u] = kb;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[u][e] = 0.f;
-            kb0_ += 2 * kW4Warps;
-            settle(b0, kb0_);
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[u][i] = make_uint4(0u, 0u, 0u, 0u);
+            if (b < a.batch) load_x8<T>((const T*)a.x + (long long)b * a.ld_x, (kb0 + kb) * 128 + h * 32 + tig * 8, a.K, a.vec, raw[u]);
+            kb += 2 * kW4Warps;
+            settle();
         }
+        base += 2 * kW4Warps * kXLoads;
+    }
+    __device__ __forceinline__ void store(uint4* xs, float2* xg)
+    {
+        const int slots = a.batch * (SPLIT ? 2 : 1);
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            const int b = bs[u], kb = ks[u];
-            float m = 0.f, sum = 0.f;
+        for (int u = 0; u < kXLoads; ++u) {
+            if (__all_sync(0xffffffffu, bs[u] >= a.batch)) break;
+            float v[8], m = 0.f, sum = 0.f;
+            unpack8<T>(raw[u], v);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                m = fmaxf(m, fabsf(v[u][e]));
-                sum += v[u][e];
+                m = fmaxf(m, fabsf(v[e]));
+                sum += v[e];
             }
 #pragma unroll
             for (int d = 1; d < G / 8; d <<= 1) {            // within the half-warp: both halves take part
                 m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
                 sum += __shfl_xor_sync(0xffffffffu, sum, d);
             }
-            // p[e], q[e]: the two entries that code e of a lane's word stands beside (see the note on words below)
+            // p[e], q[e]: the two entries that code e of a lane's word stands beside (code_word)
             float p[4], q[4];
             if (G == 32) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    p[e] = v[u][e];
-                    q[e] = v[u][4 + e];
+                    p[e] = v[e];
+                    q[e] = v[4 + e];
                 }
             } else {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float other = __shfl_xor_sync(0xffffffffu, h & 1 ? v[u][e] : v[u][4 + e], 4);
-                    p[e] = h & 1 ? other : v[u][e];
-                    q[e] = h & 1 ? v[u][4 + e] : other;
+                    const float other = __shfl_xor_sync(0xffffffffu, h & 1 ? v[e] : v[4 + e], 4);
+                    p[e] = h & 1 ? other : v[e];
+                    q[e] = h & 1 ? v[4 + e] : other;
                 }
             }
-            if (b >= a.batch) continue;
+            if (bs[u] >= a.batch) continue;
             const int x = range_exponent(m);
             const float up = pow2(14 - x), up16 = up * (1.f / 16.f);          // odd codes stand 16 times higher
 #pragma unroll
@@ -187,47 +205,53 @@ __device__ __forceinline__ void stage_x(const W4Args& a, int kb0, int nkb, uint4
                 f.y = pack_half2(half_part(p[2] * up, part), half_part(q[2] * up, part));
                 f.z = pack_half2(half_part(p[1] * up16, part), half_part(q[1] * up16, part));
                 f.w = pack_half2(half_part(p[3] * up16, part), half_part(q[3] * up16, part));
-                xs[((kb * 4 + h) * slots + (SPLIT ? 2 * b + part : b)) * 4 + tig] = f;
+                xs[((ks[u] * 4 + h) * slots + (SPLIT ? 2 * bs[u] + part : bs[u])) * 4 + tig] = f;
             }
-            if ((l16 & (G / 8 - 1)) == 0) xg[(kb * PER + l16 / (G / 8)) * a.batch + b] = make_float2(pow2(x - 14), sum);
+            if ((l16 & (G / 8 - 1)) == 0) xg[(ks[u] * PER + l16 / (G / 8)) * a.batch + bs[u]] = make_float2(pow2(x - 14), sum);
         }
     }
-}
+};
 
 template <typename T, typename Y, int G>
 __global__ void __launch_bounds__(kW4Threads, 1) w4_matvec_kernel(const __grid_constant__ W4Args a)
 {
     constexpr bool SPLIT = sizeof(T) == 4;
-    constexpr int PER = 128 / G, STAGES = kW4Stages<G>, MM = SPLIT ? 2 : 1;          // MMAs of 8 columns: two for fp32 x of over 4 rows
-    constexpr uint32_t STAGE = 1024 + PER * 64;
+    constexpr int PER = 128 / G, STAGES = kW4Stages, MM = SPLIT ? 2 : 1;          // MMAs of 8 columns: two for fp32 x of over 4 rows
+    constexpr uint32_t BLOCK = 1024 + PER * 64, STAGE = 2 * BLOCK;           // a column block of two row tiles
     const int slots = a.batch * (SPLIT ? 2 : 1);
     const bool both = SPLIT && a.batch > 4;
 
     extern __shared__ __align__(128) uint8_t smem[];
     uint4* xs = reinterpret_cast<uint4*>(smem + (size_t)kW4Warps * STAGES * STAGE);
     float2* xg = reinterpret_cast<float2*>(xs + (size_t)a.share * 16 * slots);
-    float* part = reinterpret_cast<float*>(xg + (size_t)a.share * PER * a.batch);           // [16 warps][kW4Round][8][16]
+    float* part = reinterpret_cast<float*>(xg + (size_t)a.share * PER * a.batch);           // [16 warps][2][8][16]
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
     const unsigned size = cluster_size(), rank = cluster_rank();
 
-    // this warp's column blocks [k0, k1), counted within the CTA's share [c0, c1) of them, and its row tiles
+    // this warp's column blocks [k0, k1), counted within the CTA's share [c0, c1) of them, and its pairs of row tiles
     const int c0 = (int)rank * a.share < a.KB ? (int)rank * a.share : a.KB, c1 = c0 + a.share < a.KB ? c0 + a.share : a.KB;
     const int part_of = warp % a.split, group = warp / a.split, groups = kW4Warps / a.split;
     const int clusters = gridDim.x / size, cluster = blockIdx.x / size;
     const int each = (c1 - c0 + a.split - 1) / a.split;
     const int k0 = part_of * each < c1 - c0 ? part_of * each : c1 - c0, k1 = k0 + each < c1 - c0 ? k0 + each : c1 - c0;
-    // a group's i-th row tile: consecutive tiles go to different clusters
-    auto tile_of = [&](int i) { return (i * groups + group) * clusters + cluster; };
+    // a group's i-th pair: consecutive pairs go to different clusters
+    const int pairs = (a.tiles + 1) / 2;
+    auto pair_of = [&](int i) { return (i * groups + group) * clusters + cluster; };
 
     wait_for_stream();
     let_next_start();
+    XStage<T, G> stage_x(a, c0, c1 - c0, tid);
+    stage_x.load();
     const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * STAGES) * STAGE;
-    int f_i = 0, f_left = 0;                                 // the row tile that is copied, its blocks still to copy
-    const uint8_t *f_codes = nullptr, *f_pairs = nullptr;    // this lane's part of the next block
+    int f_i = 0, f_left = 0;                                 // the pair that is copied, its blocks still to copy
+    const uint8_t *f_codes = nullptr, *f_pairs = nullptr;    // this lane's part of the next block of its first row tile
+    bool f_two = false;                                      // it has a second one
+    const size_t codes_row = (size_t)a.KB * 1024, pairs_row = (size_t)a.KB * (PER * 64);
     auto feed_open = [&]() {
-        const int tile = tile_of(f_i);
-        f_left = tile < a.tiles ? k1 - k0 : 0;
-        const size_t block = (size_t)tile * a.KB + c0 + k0;
+        const int pair = pair_of(f_i);
+        f_left = pair < pairs ? k1 - k0 : 0;
+        f_two = 2 * pair + 1 < a.tiles;
+        const size_t block = (size_t)(2 * pair) * a.KB + c0 + k0;
         f_codes = a.codes + block * 1024 + lane * 16;
         f_pairs = a.pairs + block * (PER * 64) + lane * 16;
     };
@@ -237,6 +261,11 @@ __global__ void __launch_bounds__(kW4Threads, 1) w4_matvec_kernel(const __grid_c
             copy16(at, f_codes);
             copy16(at + 512, f_codes + 512);
             if (lane < PER * 4) copy16(at + 1024, f_pairs);
+            if (f_two) {
+                copy16(at + BLOCK, f_codes + codes_row);
+                copy16(at + BLOCK + 512, f_codes + codes_row + 512);
+                if (lane < PER * 4) copy16(at + BLOCK + 1024, f_pairs + pairs_row);
+            }
             f_codes += 1024;
             f_pairs += PER * 64;
             if (--f_left == 0) {
@@ -248,7 +277,11 @@ __global__ void __launch_bounds__(kW4Threads, 1) w4_matvec_kernel(const __grid_c
     };
 #pragma unroll 1
     for (int s = 0; s < STAGES; ++s) feed(ring + lane * 16 + s * STAGE);
-    stage_x<T, G>(a, c0, c1 - c0, xs, xg, tid);
+    stage_x.store(xs, xg);
+    while (stage_x.more()) {
+        stage_x.load();
+        stage_x.store(xs, xg);
+    }
     __syncthreads();
 
     uint32_t stage = 0;
@@ -263,56 +296,77 @@ __global__ void __launch_bounds__(kW4Threads, 1) w4_matvec_kernel(const __grid_c
             const int b = SPLIT ? m * 4 + tig : 2 * tig + i;
             gx[m][i] = (b < a.batch ? b : 0) * sizeof(float2);
         }
-    for (int i0 = 0; i0 * groups * clusters + cluster < a.tiles; i0 += kW4Round) {           // the same rounds for a whole cluster
-        for (int j = 0; j < kW4Round; ++j) {
-            const int tile = tile_of(i0 + j);
-            if (tile >= a.tiles) break;
+    for (int round = 0; round * groups * clusters + cluster < pairs; ++round) {              // the same rounds for a whole cluster
+        if (pair_of(round) < pairs) {
             uint32_t xa = smem_u32(xs) + k0 * 4 * xstep + xcol0, ga = smem_u32(xg) + k0 * PER * gstep;
-            float y[MM][4];                                  // rows gid, gid + 8 x two columns
+            float y[2][MM][4];                               // [row tile][MMA][rows gid, gid + 8 x two columns]
 #pragma unroll
-            for (int m = 0; m < MM; ++m)
+            for (int r = 0; r < 2; ++r)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) y[m][e] = 0.f;
+                for (int m = 0; m < MM; ++m)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[r][m][e] = 0.f;
 #pragma unroll 1
             for (int kb = k0; kb < k1; ++kb) {
                 copy_wait<STAGES - 1>();
                 __syncwarp();
                 const uint32_t st = ring + stage;            // a lane's 16 bytes of the codes of rows gid and gid + 8 stand at lane * 16
-                const uint4 r0 = lds128(st + lane * 16), r1 = lds128(st + lane * 16 + 512);
-                const uint32_t w0[4] = {r0.x, r0.y, r0.z, r0.w}, w1[4] = {r1.x, r1.y, r1.z, r1.w};
+                uint32_t w[2][2][4];
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint4 v = lds128(st + r * BLOCK + i * 512 + lane * 16);
+                        w[r][i][0] = v.x; w[r][i][1] = v.y; w[r][i][2] = v.z; w[r][i][3] = v.w;
+                    }
 #pragma unroll
                 for (int g = 0; g < PER; ++g) {
-                    float acc[MM][4];
+                    float acc[2][MM][4];
 #pragma unroll
                     for (int q = g * G / 32; q < (g + 1) * G / 32; ++q) {
-                        const uint32_t x0 = code_word<G, 4>(w0, q), x1 = code_word<G, 4>(w1, q);
-                        const uint32_t y0 = x0 >> 8, y1 = x1 >> 8;
-                        const uint32_t a0 = x0 & 0x000f000fu, a1 = x1 & 0x000f000fu, a2 = y0 & 0x000f000fu, a3 = y1 & 0x000f000fu;
-                        const uint32_t b0 = x0 & 0x00f000f0u, b1 = x1 & 0x00f000f0u, b2 = y0 & 0x00f000f0u, b3 = y1 & 0x00f000f0u;
+                        uint4 f[MM];
+                        f[0] = lds128(xa + q * xstep);
+                        if (SPLIT && both) f[MM - 1] = lds128(xa + xcol1 + q * xstep);
 #pragma unroll
-                        for (int m = 0; m < MM; ++m) {
-                            if (m == 1 && !both) break;
-                            const uint4 f = lds128((m == 0 ? xa : xa + xcol1) + q * xstep);
-                            if (q == g * G / 32) mma_16816_zero(acc[m], a0, a1, a2, a3, f.x, f.y);
-                            else mma_16816(acc[m], a0, a1, a2, a3, f.x, f.y);
-                            mma_16816(acc[m], b0, b1, b2, b3, f.z, f.w);
+                        for (int r = 0; r < 2; ++r) {
+                            const uint32_t x0 = code_word<G, 4>(w[r][0], q), x1 = code_word<G, 4>(w[r][1], q);
+                            const uint32_t y0 = x0 >> 8, y1 = x1 >> 8;
+                            const uint32_t a0 = x0 & 0x000f000fu, a1 = x1 & 0x000f000fu, a2 = y0 & 0x000f000fu, a3 = y1 & 0x000f000fu;
+                            const uint32_t b0 = x0 & 0x00f000f0u, b1 = x1 & 0x00f000f0u, b2 = y0 & 0x00f000f0u, b3 = y1 & 0x00f000f0u;
+#pragma unroll
+                            for (int m = 0; m < MM; ++m) {
+                                if (m == 1 && !both) break;
+                                if (q == g * G / 32) mma_16816_zero(acc[r][m], a0, a1, a2, a3, f[m].x, f[m].y);
+                                else mma_16816(acc[r][m], a0, a1, a2, a3, f[m].x, f[m].y);
+                                mma_16816(acc[r][m], b0, b1, b2, b3, f[m].z, f[m].w);
+                            }
                         }
                     }
-                    const float2 p0 = lds_half2(st + 1024 + g * 64 + gid * 4), p1 = lds_half2(st + 1024 + g * 64 + gid * 4 + 32);
-                    const float s0 = p0.x * kCodeScaleLow, s1 = p1.x * kCodeScaleLow;
+                    float2 e[MM][SPLIT ? 1 : 2];             // (scale, sum) of the group of this lane's rows of x
 #pragma unroll
                     for (int m = 0; m < MM; ++m) {
                         if (m == 1 && !both) break;
-                        if (SPLIT) {                         // the two parts of a row of x stand in neighbouring columns
-                            const float2 e = lds_f32x2(ga + g * gstep + gx[m][0]);
-                            y[m][0] = fmaf(s0 * (acc[m][0] + acc[m][1]), e.x, fmaf(p0.y, e.y, y[m][0]));
-                            y[m][2] = fmaf(s1 * (acc[m][2] + acc[m][3]), e.x, fmaf(p1.y, e.y, y[m][2]));
-                        } else {
 #pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                const float2 e = lds_f32x2(ga + g * gstep + gx[m][SPLIT ? 0 : i]);
-                                y[m][i] = fmaf(s0 * acc[m][i], e.x, fmaf(p0.y, e.y, y[m][i]));
-                                y[m][2 + i] = fmaf(s1 * acc[m][2 + i], e.x, fmaf(p1.y, e.y, y[m][2 + i]));
+                        for (int i = 0; i < (SPLIT ? 1 : 2); ++i) e[m][i] = lds_f32x2(ga + g * gstep + gx[m][i]);
+                    }
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        const uint32_t pr = st + r * BLOCK + 1024 + g * 64 + gid * 4;
+                        const float2 p0 = lds_half2(pr), p1 = lds_half2(pr + 32);
+                        const float s0 = p0.x * kCodeScaleLow, s1 = p1.x * kCodeScaleLow;
+#pragma unroll
+                        for (int m = 0; m < MM; ++m) {
+                            if (m == 1 && !both) break;
+                            if (SPLIT) {                     // the two parts of a row of x stand in neighbouring columns
+                                y[r][m][0] = fmaf(s0 * (acc[r][m][0] + acc[r][m][1]), e[m][0].x, fmaf(p0.y, e[m][0].y, y[r][m][0]));
+                                y[r][m][2] = fmaf(s1 * (acc[r][m][2] + acc[r][m][3]), e[m][0].x, fmaf(p1.y, e[m][0].y, y[r][m][2]));
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 2; ++i) {
+                                    const float2 x = e[m][SPLIT ? 0 : i];
+                                    y[r][m][i] = fmaf(s0 * acc[r][m][i], x.x, fmaf(p0.y, x.y, y[r][m][i]));
+                                    y[r][m][2 + i] = fmaf(s1 * acc[r][m][2 + i], x.x, fmaf(p1.y, x.y, y[r][m][2 + i]));
+                                }
                             }
                         }
                     }
@@ -323,28 +377,31 @@ __global__ void __launch_bounds__(kW4Threads, 1) w4_matvec_kernel(const __grid_c
                 ga += PER * gstep;
                 stage = stage + STAGE == STAGES * STAGE ? 0 : stage + STAGE;
             }
-            float* buf = part + (warp * kW4Round + j) * 128;                                 // [row of x][output row]
 #pragma unroll
-            for (int m = 0; m < MM; ++m)
+            for (int r = 0; r < 2; ++r) {
+                float* buf = part + (warp * 2 + r) * 128;    // [row of x][output row]
 #pragma unroll
-                for (int i = 0; i < (SPLIT ? 1 : 2); ++i) {
-                    const int b = SPLIT ? m * 4 + tig : 2 * tig + i;
-                    buf[b * 16 + gid] = y[m][i];
-                    buf[b * 16 + gid + 8] = y[m][2 + i];
-                }
+                for (int m = 0; m < MM; ++m)
+#pragma unroll
+                    for (int i = 0; i < (SPLIT ? 1 : 2); ++i) {
+                        const int b = SPLIT ? m * 4 + tig : 2 * tig + i;
+                        buf[b * 16 + gid] = y[r][m][i];
+                        buf[b * 16 + gid + 8] = y[r][m][2 + i];
+                    }
+            }
         }
         cluster_sync(size);
         // the outputs of the round: the row tiles go round the cluster's CTAs
         const int per_tile = a.batch * 16;
-        for (int o = tid; o < groups * kW4Round * per_tile; o += kW4Threads) {
-            const int at = o / per_tile, r = o - at * per_tile, g = at / kW4Round, j = at % kW4Round;
+        for (int o = tid; o < groups * 2 * per_tile; o += kW4Threads) {
+            const int at = o / per_tile, i = o - at * per_tile, g = at >> 1, r = at & 1;
             if (at % (int)size != (int)rank) continue;
-            const int n = ((((i0 + j) * groups + g) * clusters + cluster) << 4) + (r & 15), b = r >> 4;
+            const int n = ((((round * groups + g) * clusters + cluster) * 2 + r) << 4) + (i & 15), b = i >> 4;
             if (n >= a.N) continue;
             float v = 0.f;
             for (unsigned c = 0; c < size; ++c)
                 for (int q = 0; q < a.split; ++q) {
-                    const float* from = part + ((g * a.split + q) * kW4Round + j) * 128 + r;
+                    const float* from = part + ((g * a.split + q) * 2 + r) * 128 + i;
                     v += size == 1 ? *from : cluster_load(cluster_address(from, c));
                 }
             if (a.bias) v += to_f32<T>(((const T*)a.bias)[n]);
@@ -385,25 +442,27 @@ template <typename T, typename Y, int G>
 static coreinfer_status launch_group(W4Args& a, const DeviceInfo& di, cudaStream_t st)
 {
     constexpr int PER = 128 / G;
-    constexpr size_t RING = (size_t)kW4Warps * kW4Stages<G> * (1024 + PER * 64), PART = (size_t)kW4Warps * kW4Round * 128 * sizeof(float);
+    constexpr size_t RING = (size_t)kW4Warps * kW4Stages * 2 * (1024 + PER * 64), PART = (size_t)kW4Warps * 2 * 128 * sizeof(float);
     const int slots = a.batch * (sizeof(T) == 4 ? 2 : 1);
     const size_t per_block = (size_t)slots * 256 + (size_t)PER * a.batch * sizeof(float2);
+    const size_t most = smem_room(di) - RING - PART;         // bytes of x fragments and group factors in a CTA
     int cluster = 1;
-    while (cluster < kW4MaxCluster && (size_t)((a.KB + cluster - 1) / cluster) * per_block > kW4MaxX) cluster *= 2;
+    while (cluster < kW4MaxCluster && (size_t)((a.KB + cluster - 1) / cluster) * per_block > most) cluster *= 2;
     a.share = (a.KB + cluster - 1) / cluster;
-    if (a.share * per_block > kW4MaxX)
+    if (a.share * per_block > most)
         CI_FAIL(COREINFER_ERR_UNSUPPORTED, "K %d: with %d rows of x at most %d columns", a.K, a.batch,
-                (int)(kW4MaxX / per_block) * kW4MaxCluster * 128);
+                (int)(most / per_block) * kW4MaxCluster * 128);
     const size_t smem = RING + PART + a.share * per_block;
     const coreinfer_status s = allow_smem<w4_matvec_kernel<T, Y, G>>(di);
     if (s != COREINFER_OK) return s;
     int clusters = clusters_at_once<w4_matvec_kernel<T, Y, G>>(di, cluster, smem);
-    if (clusters > a.tiles) clusters = a.tiles;
-    // Warps per row tile: as many as make the longest warp's list of blocks shortest.
+    const int pairs = (a.tiles + 1) / 2;
+    if (clusters > pairs) clusters = pairs;
+    // Warps per pair: as many as make the longest warp's list of blocks shortest.
     long long best = 0;
     for (int split = 1; split <= kW4Warps; split *= 2) {
         const long long groups = (long long)clusters * (kW4Warps / split);
-        const long long cost = ((a.tiles + groups - 1) / groups) * ((a.share + split - 1) / split);
+        const long long cost = ((pairs + groups - 1) / groups) * ((a.share + split - 1) / split);
         if (split == 1 || cost < best) {
             best = cost;
             a.split = split;
