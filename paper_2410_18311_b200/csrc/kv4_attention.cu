@@ -157,7 +157,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
     int* pre = reinterpret_cast<int*>(mlbuf + kAttnWarps * RPT);                             // [B + 1] entries of a head before sequence b
     int* tiles_before = pre + c.B + 1;                                                       // [B] tiles of a head before sequence b
     int* lens = tiles_before + c.B;                                                          // [B]
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = warp_number(), lane = tid & 31;
     wait_for_stream();       // nothing of an earlier kernel is read or overwritten above
     if (warp == 0) {
         int run = 0, idle = 0;                               // entries, and those without work, so far
@@ -277,8 +277,9 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                 const uint8_t* pairs = reinterpret_cast<const uint8_t*>(c.pairs[which]) + (size_t)f_slot * PAIR_ROW + lane * 16;
 #pragma unroll
                 for (uint32_t i = 0; i < CODES; i += 512)
-                    if (i < 16 * CODE_ROW || rows == CH) copy16(at + lane * 16 + i, codes + i);
-                if (lane * 16 < rows * PAIR_ROW) copy16(at + CODES + lane * 16, pairs);
+                    if (i < 16 * CODE_ROW) copy16(at + lane * 16 + i, codes + i);
+                    else copy16_if(at + lane * 16 + i, codes + i, rows == CH);
+                copy16_if(at + CODES + lane * 16, pairs, lane * 16 < rows * PAIR_ROW);
                 if (which) {
                     f_n0 += stride;
                     f_slot += stride;

@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(kW4Threads, 1) w4_matvec_kernel(const __grid_c
     uint4* xs = reinterpret_cast<uint4*>(smem + (size_t)kW4Warps * STAGES * STAGE);
     float2* xg = reinterpret_cast<float2*>(xs + (size_t)a.share * 16 * slots);
     float* part = reinterpret_cast<float*>(xg + (size_t)a.share * PER * a.batch);           // [16 warps][2][8][16]
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tig = lane & 3;
+    const int tid = threadIdx.x, warp = warp_number(), lane = tid & 31, gid = lane >> 2, tig = lane & 3;
     const unsigned size = cluster_size(), rank = cluster_rank();
 
     // this warp's column blocks [k0, k1), counted within the CTA's share [c0, c1) of them, and its pairs of row tiles
@@ -260,12 +260,10 @@ __global__ void __launch_bounds__(kW4Threads, 1) w4_matvec_kernel(const __grid_c
         if (f_left > 0) {
             copy16(at, f_codes);
             copy16(at + 512, f_codes + 512);
-            if (lane < PER * 4) copy16(at + 1024, f_pairs);
-            if (f_two) {
-                copy16(at + BLOCK, f_codes + codes_row);
-                copy16(at + BLOCK + 512, f_codes + codes_row + 512);
-                if (lane < PER * 4) copy16(at + BLOCK + 1024, f_pairs + pairs_row);
-            }
+            copy16_if(at + 1024, f_pairs, lane < PER * 4);
+            copy16_if(at + BLOCK, f_codes + codes_row, f_two);
+            copy16_if(at + BLOCK + 512, f_codes + codes_row + 512, f_two);
+            copy16_if(at + BLOCK + 1024, f_pairs + pairs_row, f_two && lane < PER * 4);
             f_codes += 1024;
             f_pairs += PER * 64;
             if (--f_left == 0) {
@@ -392,12 +390,10 @@ __global__ void __launch_bounds__(kW4Threads, 1) w4_matvec_kernel(const __grid_c
         }
         cluster_sync(size);
         // the outputs of the round: the row tiles go round the cluster's CTAs
-        const int per_tile = a.batch * 16;
-        for (int o = tid; o < groups * 2 * per_tile; o += kW4Threads) {
-            const int at = o / per_tile, i = o - at * per_tile, g = at >> 1, r = at & 1;
-            if (at % (int)size != (int)rank) continue;
-            const int n = ((((round * groups + g) * clusters + cluster) * 2 + r) << 4) + (i & 15), b = i >> 4;
-            if (n >= a.N) continue;
+        const int i = tid & 127, b = i >> 4;                 // row of x and output row
+        for (int at = tid >> 7; at < groups * 2; at += kW4Threads >> 7) {
+            const int g = at >> 1, r = at & 1, n = ((((round * groups + g) * clusters + cluster) * 2 + r) << 4) + (i & 15);
+            if ((at & (size - 1)) != rank || b >= a.batch || n >= a.N) continue;
             float v = 0.f;
             for (unsigned c = 0; c < size; ++c)
                 for (int q = 0; q < a.split; ++q) {
