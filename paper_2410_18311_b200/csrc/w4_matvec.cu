@@ -1,6 +1,8 @@
 // Matrix-vector products with 4-bit weights and group scales, and the one-time layout of such weights.
 #include "quant4.cuh"
 
+#include <type_traits>
+
 namespace coreinfer {
 
 static inline long long w4_rows16(int N) { return ((long long)N + 15) / 16; }
@@ -66,11 +68,13 @@ w4_quantize_kernel(const T* __restrict__ w, int N, int K, long long sn, long lon
 // Each of a CTA's 16 warps streams its own blocks of 32 rows (two row tiles: the fragments of x are read once for both) x
 // 128 columns through a ring of its own (cp.async, 16 bytes a lane; refilled as soon as it is read), so no warp waits for
 // another inside a pair of row tiles.  A pair's columns are split over `split` warps where pairs are few, and over
-// the CTAs of a cluster where the fragments of x, which are laid out once per CTA in shared memory, would not fit
-// one; the partial sums meet in shared memory, in a fixed order, after every pair.
+// the two or four CTAs of a cluster where the fragments of x, laid out in shared memory, would not fit one (4 only then:
+// such clusters leave SMs empty, 57.6 against 36.7 us at 36864 x 9216 and 8 rows).  What does not fit four goes over
+// two in chunks of columns, laid out again for every pair.  The partial sums meet in shared memory, in a fixed
+// order, after every pair.
 constexpr int kW4Warps = 16;
 constexpr int kW4Threads = 32 * kW4Warps;
-constexpr int kW4MaxCluster = 8;
+constexpr int kW4Join = 3;                  // what the join of a pair costs, in column blocks (16384 x 4096 over clusters of two: 28.7 us without it)
 constexpr int kW4Stages = 3;                // of two column blocks
 
 struct W4Args {
@@ -79,6 +83,7 @@ struct W4Args {
     int N, K, batch, act;
     int KB;                 // column blocks of 128
     int share;              // column blocks per CTA of a cluster
+    int chunk;              // column blocks whose x is in shared memory at once
     int tiles;              // row tiles
     int split;              // warps that share a pair of row tiles
     int vec;                // rows of x are 16-byte aligned
@@ -161,6 +166,13 @@ struct XStage {
         }
         base += 2 * kW4Warps * kXLoads;
     }
+    __device__ __forceinline__ void rest(uint4* xs, float2* xg)
+    {
+        while (more()) {
+            load();
+            store(xs, xg);
+        }
+    }
     __device__ __forceinline__ void store(uint4* xs, float2* xg)
     {
         const int slots = a.batch * (SPLIT ? 2 : 1);
@@ -212,7 +224,8 @@ struct XStage {
     }
 };
 
-template <typename T, typename Y, int G>
+// CHUNKED: x does not fit the shared memory of its CTAs (a kernel of its own: the code for it costs the others 0.5 us).
+template <typename T, typename Y, int G, bool CHUNKED>
 __global__ void __launch_bounds__(kW4Threads, 1) w4_matvec_kernel(const __grid_constant__ W4Args a)
 {
     constexpr bool SPLIT = sizeof(T) == 4;
@@ -223,37 +236,54 @@ __global__ void __launch_bounds__(kW4Threads, 1) w4_matvec_kernel(const __grid_c
 
     extern __shared__ __align__(128) uint8_t smem[];
     uint4* xs = reinterpret_cast<uint4*>(smem + (size_t)kW4Warps * STAGES * STAGE);
-    float2* xg = reinterpret_cast<float2*>(xs + (size_t)a.share * 16 * slots);
-    float* part = reinterpret_cast<float*>(xg + (size_t)a.share * PER * a.batch);           // [16 warps][2][8][16]
+    float2* xg = reinterpret_cast<float2*>(xs + (size_t)a.chunk * 16 * slots);
+    float* part = reinterpret_cast<float*>(xg + (size_t)a.chunk * PER * a.batch);           // [16 warps][2][8][16]
     const int tid = threadIdx.x, warp = warp_number(), lane = tid & 31, gid = lane >> 2, tig = lane & 3;
     const unsigned size = cluster_size(), rank = cluster_rank();
 
-    // this warp's column blocks [k0, k1), counted within the CTA's share [c0, c1) of them, and its pairs of row tiles
+    // this CTA's column blocks [c0, c1) in chunks, and this warp's share of a chunk, counted from the chunk's start
     const int c0 = (int)rank * a.share < a.KB ? (int)rank * a.share : a.KB, c1 = c0 + a.share < a.KB ? c0 + a.share : a.KB;
     const int part_of = warp % a.split, group = warp / a.split, groups = kW4Warps / a.split;
     const int clusters = gridDim.x / size, cluster = blockIdx.x / size;
-    const int each = (c1 - c0 + a.split - 1) / a.split;
-    const int k0 = part_of * each < c1 - c0 ? part_of * each : c1 - c0, k1 = k0 + each < c1 - c0 ? k0 + each : c1 - c0;
+    const int chunks = CHUNKED ? (c1 - c0 + a.chunk - 1) / a.chunk : 1;
+    auto chunk_len = [&](int ch) { return !CHUNKED ? c1 - c0 : c1 - c0 - ch * a.chunk < a.chunk ? c1 - c0 - ch * a.chunk : a.chunk; };
+    auto first_of = [&](int ch) { return part_of * ((chunk_len(ch) + a.split - 1) / a.split); };
+    auto count_of = [&](int ch) {
+        const int len = chunk_len(ch), each = (len + a.split - 1) / a.split, left = len - part_of * each;
+        return left < each ? (left < 0 ? 0 : left) : each;
+    };
     // a group's i-th pair: consecutive pairs go to different clusters
     const int pairs = (a.tiles + 1) / 2;
     auto pair_of = [&](int i) { return (i * groups + group) * clusters + cluster; };
 
     wait_for_stream();
     let_next_start();
-    XStage<T, G> stage_x(a, c0, c1 - c0, tid);
+    XStage<T, G> stage_x(a, c0, c1 > c0 ? chunk_len(0) : 0, tid);
     stage_x.load();
     const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * STAGES) * STAGE;
-    int f_i = 0, f_left = 0;                                 // the pair that is copied, its blocks still to copy
+    int f_i = 0, f_ch = -1, f_left = 0;                      // the pair and chunk that are copied, the blocks still to copy
     const uint8_t *f_codes = nullptr, *f_pairs = nullptr;    // this lane's part of the next block of its first row tile
     bool f_two = false;                                      // it has a second one
     const size_t codes_row = (size_t)a.KB * 1024, pairs_row = (size_t)a.KB * (PER * 64);
-    auto feed_open = [&]() {
-        const int pair = pair_of(f_i);
-        f_left = pair < pairs ? k1 - k0 : 0;
-        f_two = 2 * pair + 1 < a.tiles;
-        const size_t block = (size_t)(2 * pair) * a.KB + c0 + k0;
-        f_codes = a.codes + block * 1024 + lane * 16;
-        f_pairs = a.pairs + block * (PER * 64) + lane * 16;
+    auto feed_open = [&]() {                                 // the next chunk, or the first of the next pair, with blocks of this warp
+        while (pair_of(f_i) < pairs) {
+            if (CHUNKED ? ++f_ch >= chunks : ++f_ch > 0) {
+                f_ch = -1;
+                ++f_i;
+                continue;
+            }
+            f_left = count_of(f_ch);
+            if (f_left == 0) {
+                if (!CHUNKED) break;
+                continue;
+            }
+            const int pair = pair_of(f_i);
+            f_two = 2 * pair + 1 < a.tiles;
+            const size_t block = (size_t)(2 * pair) * a.KB + c0 + f_ch * a.chunk + first_of(f_ch);
+            f_codes = a.codes + block * 1024 + lane * 16;
+            f_pairs = a.pairs + block * (PER * 64) + lane * 16;
+            break;
+        }
     };
     feed_open();
     auto feed = [&](uint32_t at) {
@@ -266,20 +296,14 @@ __global__ void __launch_bounds__(kW4Threads, 1) w4_matvec_kernel(const __grid_c
             copy16_if(at + BLOCK + 1024, f_pairs + pairs_row, f_two && lane < PER * 4);
             f_codes += 1024;
             f_pairs += PER * 64;
-            if (--f_left == 0) {
-                ++f_i;
-                feed_open();
-            }
+            if (--f_left == 0) feed_open();
         }
         copy_commit();                                       // one group per stage, empty ones too
     };
 #pragma unroll 1
     for (int s = 0; s < STAGES; ++s) feed(ring + lane * 16 + s * STAGE);
     stage_x.store(xs, xg);
-    while (stage_x.more()) {
-        stage_x.load();
-        stage_x.store(xs, xg);
-    }
+    stage_x.rest(xs, xg);
     __syncthreads();
 
     uint32_t stage = 0;
@@ -295,17 +319,27 @@ __global__ void __launch_bounds__(kW4Threads, 1) w4_matvec_kernel(const __grid_c
             gx[m][i] = (b < a.batch ? b : 0) * sizeof(float2);
         }
     for (int round = 0; round * groups * clusters + cluster < pairs; ++round) {              // the same rounds for a whole cluster
-        if (pair_of(round) < pairs) {
-            uint32_t xa = smem_u32(xs) + k0 * 4 * xstep + xcol0, ga = smem_u32(xg) + k0 * PER * gstep;
-            float y[2][MM][4];                               // [row tile][MMA][rows gid, gid + 8 x two columns]
+        const bool mine = pair_of(round) < pairs;
+        float y[2][MM][4];                                   // [row tile][MMA][rows gid, gid + 8 x two columns]
 #pragma unroll
-            for (int r = 0; r < 2; ++r)
+        for (int r = 0; r < 2; ++r)
 #pragma unroll
-                for (int m = 0; m < MM; ++m)
+            for (int m = 0; m < MM; ++m)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) y[r][m][e] = 0.f;
+                for (int e = 0; e < 4; ++e) y[r][m][e] = 0.f;
 #pragma unroll 1
-            for (int kb = k0; kb < k1; ++kb) {
+        for (int ch = 0; ch < (CHUNKED ? chunks : 1); ++ch) {
+            if (CHUNKED && (round > 0 || ch > 0)) {       // the chunk before is no longer read
+                __syncthreads();
+                XStage<T, G> next(a, c0 + ch * a.chunk, chunk_len(ch), tid);
+                next.rest(xs, xg);
+                __syncthreads();
+            }
+            if (!mine) continue;
+            const int k0 = first_of(ch), n = count_of(ch);
+            uint32_t xa = smem_u32(xs) + k0 * 4 * xstep + xcol0, ga = smem_u32(xg) + k0 * PER * gstep;
+#pragma unroll 1
+            for (int k = 0; k < n; ++k) {
                 copy_wait<STAGES - 1>();
                 __syncwarp();
                 const uint32_t st = ring + stage;            // a lane's 16 bytes of the codes of rows gid and gid + 8 stand at lane * 16
@@ -375,18 +409,18 @@ __global__ void __launch_bounds__(kW4Threads, 1) w4_matvec_kernel(const __grid_c
                 ga += PER * gstep;
                 stage = stage + STAGE == STAGES * STAGE ? 0 : stage + STAGE;
             }
+        }
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                float* buf = part + (warp * 2 + r) * 128;    // [row of x][output row]
+        for (int r = 0; r < 2; ++r) {
+            float* buf = part + (warp * 2 + r) * 128;        // [row of x][output row]
 #pragma unroll
-                for (int m = 0; m < MM; ++m)
+            for (int m = 0; m < MM; ++m)
 #pragma unroll
-                    for (int i = 0; i < (SPLIT ? 1 : 2); ++i) {
-                        const int b = SPLIT ? m * 4 + tig : 2 * tig + i;
-                        buf[b * 16 + gid] = y[r][m][i];
-                        buf[b * 16 + gid + 8] = y[r][m][2 + i];
-                    }
-            }
+                for (int i = 0; i < (SPLIT ? 1 : 2); ++i) {
+                    const int b = SPLIT ? m * 4 + tig : 2 * tig + i;
+                    buf[b * 16 + gid] = y[r][m][i];
+                    buf[b * 16 + gid + 8] = y[r][m][2 + i];
+                }
         }
         cluster_sync(size);
         // the outputs of the round: the row tiles go round the cluster's CTAs
@@ -409,14 +443,13 @@ __global__ void __launch_bounds__(kW4Threads, 1) w4_matvec_kernel(const __grid_c
     }
 }
 
-// Clusters of `cluster` CTAs of a kernel that the GPU holds at once, asked once per kernel, device and size.
+// Clusters of `cluster` CTAs of a kernel that the GPU holds at once; asked once per kernel and device, for the largest
+// shared memory that a launch may have.
 template <auto Kernel>
 static int clusters_at_once(const DeviceInfo& di, int cluster, size_t smem)
 {
-    if (cluster == 1) return di.sm_count;
-    static std::atomic<int> known[64][4];
-    const int log = cluster == 2 ? 1 : (cluster == 4 ? 2 : 3);
-    std::atomic<int>& slot = known[di.device & 63][log];
+    static std::atomic<int> known[64];
+    std::atomic<int>& slot = known[di.device & 63];
     int n = slot.load(std::memory_order_relaxed);
     if (n > 0) return n;
     cudaLaunchConfig_t cfg = {};
@@ -442,30 +475,34 @@ static coreinfer_status launch_group(W4Args& a, const DeviceInfo& di, cudaStream
     const int slots = a.batch * (sizeof(T) == 4 ? 2 : 1);
     const size_t per_block = (size_t)slots * 256 + (size_t)PER * a.batch * sizeof(float2);
     const size_t most = smem_room(di) - RING - PART;         // bytes of x fragments and group factors in a CTA
-    int cluster = 1;
-    while (cluster < kW4MaxCluster && (size_t)((a.KB + cluster - 1) / cluster) * per_block > most) cluster *= 2;
-    a.share = (a.KB + cluster - 1) / cluster;
-    if (a.share * per_block > most)
-        CI_FAIL(COREINFER_ERR_UNSUPPORTED, "K %d: with %d rows of x at most %d columns", a.K, a.batch,
-                (int)(most / per_block) * kW4MaxCluster * 128);
-    const size_t smem = RING + PART + a.share * per_block;
-    const coreinfer_status s = allow_smem<w4_matvec_kernel<T, Y, G>>(di);
+    coreinfer_status s = allow_smem<w4_matvec_kernel<T, Y, G, false>>(di);
     if (s != COREINFER_OK) return s;
-    int clusters = clusters_at_once<w4_matvec_kernel<T, Y, G>>(di, cluster, smem);
+    int cluster = a.KB * per_block > most ? 2 : 1;
+    if (a.KB * per_block > 2 * most && a.KB * per_block <= 4 * most) cluster = 4;
+    a.share = (a.KB + cluster - 1) / cluster;
+    a.chunk = a.share * per_block > most ? (int)(most / per_block) : a.share;
+    const size_t smem = RING + PART + a.chunk * per_block;
+    // pairs of SMs share a TPC, so clusters of two leave none empty
+    int clusters = cluster == 4 ? clusters_at_once<w4_matvec_kernel<T, Y, G, false>>(di, 4, smem) : di.sm_count / cluster;
     const int pairs = (a.tiles + 1) / 2;
     if (clusters > pairs) clusters = pairs;
-    // Warps per pair: as many as make the longest warp's list of blocks shortest.
+    // Warps per pair: as many as make the longest warp's list of blocks shortest, a join counting as kW4Join blocks.
     long long best = 0;
     for (int split = 1; split <= kW4Warps; split *= 2) {
         const long long groups = (long long)clusters * (kW4Warps / split);
-        const long long cost = ((pairs + groups - 1) / groups) * ((a.share + split - 1) / split);
+        const long long cost = ((pairs + groups - 1) / groups) * ((a.share + split - 1) / split + kW4Join);
         if (split == 1 || cost < best) {
             best = cost;
             a.split = split;
         }
     }
-    CI_CUDA(launch_overlapped(w4_matvec_kernel<T, Y, G>, dim3(clusters * cluster), dim3(kW4Threads), smem, st, a, cluster));
-    return COREINFER_OK;
+    auto go = [&](auto chunked) -> coreinfer_status {
+        constexpr bool CHUNKED = decltype(chunked)::value;
+        if (CHUNKED && (s = allow_smem<w4_matvec_kernel<T, Y, G, CHUNKED>>(di)) != COREINFER_OK) return s;
+        CI_CUDA(launch_overlapped(w4_matvec_kernel<T, Y, G, CHUNKED>, dim3(clusters * cluster), dim3(kW4Threads), smem, st, a, cluster));
+        return COREINFER_OK;
+    };
+    return a.chunk < a.share ? go(std::true_type()) : go(std::false_type());
 }
 
 template <typename T, typename Y>
