@@ -196,6 +196,9 @@ def _raw_stream(t, stream):
     return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
+_DTYPE_CODES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
 def dtype_code(t: torch.Tensor) -> int:
     if t.dtype == torch.float32:
         return F32
@@ -396,23 +399,31 @@ def coreinfer_w4_quantize(w, group, codes, pairs, stream=None):
                                         _raw_stream(w, stream)))
 
 
-def _row_stride(t):
+def _row_stride(t, n):
     """Elements between the rows of a [rows, n] tensor whose rows are contiguous."""
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    if t.is_contiguous():
+        return n
+    if n > 1 and t.stride(1) != 1:
         raise CoreInferError(ERR_INVALID_ARG, "rows must be contiguous (strides %s)" % (tuple(t.stride()),))
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return t.stride(0) if t.shape[0] > 1 else n
 
 
 def coreinfer_w4_matvec(w4, x, act, bias, mul, y, stream=None):
     """y [batch, N] = act(x [batch, K] W^T + bias) * mul, batch 1..8; w4 from make_w4_matrix()."""
-    if tuple(y.shape) != (x.shape[0], w4.N) or x.shape[1] != w4.K or (mul is not None and (mul.shape != y.shape or mul.dtype != y.dtype)) \
-            or (bias is not None and (bias.shape != (w4.N,) or bias.dtype != x.dtype or not bias.is_contiguous())):
+    batch, K = x.shape
+    N, dtype, y_dtype = w4.N, x.dtype, y.dtype
+    if y.shape != (batch, N) or K != w4.K or (mul is not None and (mul.shape != y.shape or mul.dtype != y_dtype)) \
+            or (bias is not None and (bias.numel() != N or bias.dtype != dtype or not bias.is_contiguous())):
         raise CoreInferError(ERR_INVALID_ARG, "x %s, y %s, bias or mul do not fit the %d x %d matrix"
-                             % (tuple(x.shape), tuple(y.shape), w4.N, w4.K))
-    _check(load().coreinfer_w4_matvec(w4, x.data_ptr(), x.shape[0], _row_stride(x), dtype_code(x), act,
-                                      None if bias is None else bias.data_ptr(), None if mul is None else mul.data_ptr(),
-                                      0 if mul is None else _row_stride(mul), y.data_ptr(), dtype_code(y), _row_stride(y),
-                                      _raw_stream(x, stream)))
+                             % (tuple(x.shape), tuple(y.shape), N, w4.K))
+    if dtype not in _DTYPE_CODES or y_dtype not in _DTYPE_CODES:
+        raise CoreInferError(ERR_UNSUPPORTED, "unsupported torch dtypes %s, %s" % (dtype, y_dtype))
+    status = load().coreinfer_w4_matvec(w4, x.data_ptr(), batch, _row_stride(x, K), _DTYPE_CODES[dtype], act,
+                                        None if bias is None else bias.data_ptr(), None if mul is None else mul.data_ptr(),
+                                        0 if mul is None else _row_stride(mul, N), y.data_ptr(), _DTYPE_CODES[y_dtype],
+                                        _row_stride(y, N), _raw_stream(x, stream))
+    if status:
+        _check(status)
 
 
 def make_kv4_cache(k_codes, k_pairs, v_codes, v_pairs, state, weight=None, position=None) -> KV4Cache:
@@ -433,27 +444,35 @@ def make_kv4_cache(k_codes, k_pairs, v_codes, v_pairs, state, weight=None, posit
                     B, H, n, 2 * half, 2 * half // groups, 0)
 
 
-def _token_stride(t, heads, head_dim):
-    """Elements between the tokens of a [batch, T, heads, head_dim] tensor (a slice of a wider projection is fine)."""
-    B, T, h, d = t.shape
+def _token_stride(t, shape):
+    """Elements between the tokens of a tensor of this [batch, T, heads, head_dim] (a slice of a wider projection is fine)."""
+    B, T, h, d = shape
+    if t.shape != shape:
+        raise CoreInferError(ERR_INVALID_ARG, "a tensor of shape %s was expected, got %s" % (tuple(shape), tuple(t.shape)))
+    if t.is_contiguous():
+        return h * d
     ld = t.stride(1) if T > 1 else (t.stride(0) if B > 1 else h * d)
-    if (h, d) != (heads, head_dim) or t.stride(3) != 1 or (h > 1 and t.stride(2) != d) or (B > 1 and t.stride(0) != T * ld):
-        raise CoreInferError(ERR_INVALID_ARG, "a [batch, T, %d, %d] tensor with evenly spaced tokens was expected: shape %s, "
-                             "strides %s" % (heads, head_dim, tuple(t.shape), tuple(t.stride())))
+    if t.stride(3) != 1 or (h > 1 and t.stride(2) != d) or (B > 1 and t.stride(0) != T * ld):
+        raise CoreInferError(ERR_INVALID_ARG, "evenly spaced tokens with contiguous heads were expected: shape %s, strides %s"
+                             % (tuple(t.shape), tuple(t.stride())))
     return ld
 
 
 def coreinfer_kv4_append(cache, k, v, k_stored=None, v_stored=None, stream=None):
     """k, v [batch, T, kv_heads, head_dim] into the cache; k_stored / v_stored: the values as stored, or None."""
-    ld = _token_stride(k, cache.kv_heads, cache.head_dim)
-    if v.shape != k.shape or v.dtype != k.dtype or _token_stride(v, cache.kv_heads, cache.head_dim) != ld or k.shape[0] != cache.batch:
-        raise CoreInferError(ERR_INVALID_ARG, "k %s and v %s do not match each other or the cache" % (tuple(k.shape), tuple(v.shape)))
+    T = k.shape[1] if k.dim() == 4 else 0
+    shape, dtype = (cache.batch, T, cache.kv_heads, cache.head_dim), k.dtype
+    ld = _token_stride(k, shape)
+    if v.dtype != dtype or _token_stride(v, shape) != ld or dtype not in _DTYPE_CODES:
+        raise CoreInferError(ERR_INVALID_ARG, "k (%s) and v (%s) must have one type and the same spacing of tokens" % (dtype, v.dtype))
     for t in (k_stored, v_stored):
-        if t is not None and (t.shape != k.shape or t.dtype != k.dtype or not t.is_contiguous()):
+        if t is not None and (t.shape != shape or t.dtype != dtype or not t.is_contiguous()):
             raise CoreInferError(ERR_INVALID_ARG, "k_stored and v_stored must be contiguous and shaped as k")
-    _check(load().coreinfer_kv4_append(cache, k.data_ptr(), v.data_ptr(), dtype_code(k), k.shape[1], ld,
-                                       None if k_stored is None else k_stored.data_ptr(),
-                                       None if v_stored is None else v_stored.data_ptr(), _raw_stream(k, stream)))
+    status = load().coreinfer_kv4_append(cache, k.data_ptr(), v.data_ptr(), _DTYPE_CODES[dtype], T, ld,
+                                         None if k_stored is None else k_stored.data_ptr(),
+                                         None if v_stored is None else v_stored.data_ptr(), _raw_stream(k, stream))
+    if status:
+        _check(status)
 
 
 def coreinfer_kv4_attention_workspace_bytes(cache, q_heads: int, T: int) -> int:
@@ -463,13 +482,15 @@ def coreinfer_kv4_attention_workspace_bytes(cache, q_heads: int, T: int) -> int:
 def coreinfer_kv4_attention(cache, q, scale, out, accumulate, workspace, stream=None):
     """q [batch, T, q_heads, head_dim] -> out of the same shape and type; accumulate: add every slot's
     attention weight to the cache's weights."""
-    heads = q.shape[2]
-    if out.shape != q.shape or out.dtype != q.dtype or q.shape[0] != cache.batch:
-        raise CoreInferError(ERR_INVALID_ARG, "q %s and out %s do not match each other or the cache" % (tuple(q.shape), tuple(out.shape)))
-    _check(load().coreinfer_kv4_attention(cache, q.data_ptr(), dtype_code(q), heads, q.shape[1],
-                                          _token_stride(q, heads, cache.head_dim), scale, out.data_ptr(),
-                                          _token_stride(out, heads, cache.head_dim), 1 if accumulate else 0, workspace.data_ptr(),
-                                          workspace.numel() * workspace.element_size(), _raw_stream(q, stream)))
+    _, T, heads, _ = q.shape
+    shape, dtype = (cache.batch, T, heads, cache.head_dim), q.dtype
+    if out.dtype != dtype or dtype not in _DTYPE_CODES:
+        raise CoreInferError(ERR_INVALID_ARG, "q (%s) and out (%s) must have one supported type" % (dtype, out.dtype))
+    status = load().coreinfer_kv4_attention(cache, q.data_ptr(), _DTYPE_CODES[dtype], heads, T, _token_stride(q, shape), scale,
+                                            out.data_ptr(), _token_stride(out, shape), 1 if accumulate else 0, workspace.data_ptr(),
+                                            workspace.nbytes, _raw_stream(q, stream))
+    if status:
+        _check(status)
 
 
 def coreinfer_kv4_evict_workspace_bytes(cache) -> int:
@@ -478,5 +499,7 @@ def coreinfer_kv4_evict_workspace_bytes(cache) -> int:
 
 def coreinfer_kv4_evict(src, dst, budget, recent, first, workspace, stream=None):
     """Keep `budget` slots per head (the first and recent tokens, then the heaviest); dst is src for in place."""
-    _check(load().coreinfer_kv4_evict(src, dst, budget, recent, first, workspace.data_ptr(),
-                                      workspace.numel() * workspace.element_size(), _raw_stream(workspace, stream)))
+    status = load().coreinfer_kv4_evict(src, dst, budget, recent, first, workspace.data_ptr(), workspace.nbytes,
+                                        _raw_stream(workspace, stream))
+    if status:
+        _check(status)
