@@ -31,22 +31,25 @@ __global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(const __grid
     const int4 state = *reinterpret_cast<const int4*>(c.state + b * 4);
     const int n0 = state.x < 0 ? 0 : (state.x > c.cap ? c.cap : state.x), seen = state.y;
     const bool fits = a.tokens <= c.cap - n0;
-    // row r holds keys (even r) or values (odd) of head (r / 2) % H of token r / 2 / H; stepping by an even number of rows
-    // keeps `which`, and moves token and head by a fixed amount with a carry
-    const int row0 = blockIdx.x * ROWS + threadIdx.x / LANES, step = gridDim.x * ROWS;
-    const int which = row0 & 1;
-    int t = (row0 >> 1) / c.H, h = (row0 >> 1) - t * c.H;
-    const int dt = (step >> 1) / c.H, dh = (step >> 1) - dt * c.H;
-    const T* src = (const T*)a.src[which] + l * 8;
-    T* stored = (T*)a.stored[which];
-    auto load = [&](int token, int head, T (&v)[8]) {
-        const T* p = src + ((long long)b * a.tokens + token) * a.ld + (long long)head * D;
+    // row r holds keys (even r) or values (odd) of head (r / 2) % H of token r / 2 / H; a step is a whole number of tokens,
+    // so a lane keeps its head and moves on by fixed strides
+    const int row0 = blockIdx.x * ROWS + threadIdx.x / LANES, dt = (int)(gridDim.x * ROWS) / (2 * c.H);
+    const int which = row0 & 1, t0 = (row0 >> 1) / c.H, h = (row0 >> 1) - t0 * c.H;
+    const bool first = t0 < a.tokens;
+    const T* src = (const T*)a.src[which] + ((long long)b * a.tokens + (first ? t0 : 0)) * a.ld + (long long)h * D + l * 8;
+    const long long src_step = dt * a.ld;
+    size_t slot = ((size_t)b * c.H + h) * c.cap + n0 + t0;
+    T* out = (T*)a.stored[which];
+    if (out) out += (((long long)b * a.tokens + t0) * c.H + h) * D + l * 8;
+    const long long out_step = (long long)dt * c.H * D;
+    auto load = [&](const T* p, T (&v)[8]) {
         *reinterpret_cast<uint4*>(v) = *reinterpret_cast<const uint4*>(p);
         if (sizeof(T) == 4) reinterpret_cast<uint4*>(v)[1] = reinterpret_cast<const uint4*>(p)[1];
     };
     T v[8];
-    load(t < a.tokens ? t : 0, t < a.tokens ? h : 0, v);
-    for (int base = blockIdx.x * ROWS; base < a.rows; base += step) {            // the same count for a whole CTA
+    load(src, v);
+    int t = t0;
+    for (int base = blockIdx.x * ROWS; base < a.rows; base += gridDim.x * ROWS) {             // the same count for a whole CTA
         const bool in = t < a.tokens;
         float x[8], lo, hi;
 #pragma unroll
@@ -55,13 +58,9 @@ __global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(const __grid
             lo = e ? min_nan(lo, x[e]) : x[e];
             hi = e ? max_nan(hi, x[e]) : x[e];
         }
-        int t1 = t + dt, h1 = h + dh;
-        if (h1 >= c.H) {
-            h1 -= c.H;
-            ++t1;
-        }
+        if (t + dt < a.tokens) src += src_step;
         T next[8];
-        load(t1 < a.tokens ? t1 : 0, t1 < a.tokens ? h1 : 0, next);               // on its way while this row is worked on
+        load(src, next);                                     // on its way while this row is worked on
         group_range(lo, hi, GL);
         const QuantPair p = quant_pair(lo, hi);
         const float s = __half2float(p.s), o = __half2float(p.o);
@@ -75,7 +74,6 @@ __global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(const __grid
         const unsigned got = __shfl_xor_sync(0xffffffffu, odd ? unit[0] : unit[1], 4);
         const unsigned word = odd ? got | unit[1] << 16 : unit[0] | got << 16;
         if (in && fits) {
-            const size_t slot = ((size_t)b * c.H + h) * c.cap + n0 + t;
             uint8_t* codes = c.codes[which] + slot * (D / 2);
             *reinterpret_cast<unsigned*>(codes + 2 * ((2 * (l & 3) + odd) * H32 + (h32 & ~1))) = word;
             if (l % GL == 0) c.pairs[which][slot * (D / G) + l / GL] = __halves2half2(p.s, p.o);
@@ -84,13 +82,13 @@ __global__ void __launch_bounds__(kAppendThreads) kv4_append_kernel(const __grid
                 c.position[slot] = seen + t;
             }
         }
-        if (in && stored) {
-            T* out = stored + (((long long)b * a.tokens + t) * c.H + h) * D + l * 8;
+        if (in && out) {
             *reinterpret_cast<uint4*>(out) = *reinterpret_cast<uint4*>(v);
             if (sizeof(T) == 4) reinterpret_cast<uint4*>(out)[1] = reinterpret_cast<uint4*>(v)[1];
+            out += out_step;
         }
-        t = t1;
-        h = h1;
+        t += dt;
+        slot += dt;
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = next[e];
     }
@@ -108,8 +106,11 @@ template <typename T, int D, int G>
 static cudaError_t launch_append(const AppendArgs& a, const DeviceInfo& di, cudaStream_t st)
 {
     constexpr int ROWS = kAppendThreads / (D / 8);
-    const int want = (a.rows + ROWS - 1) / ROWS, most = (di.sm_count * 8 + a.c.B - 1) / a.c.B;
-    return launch_overlapped(kv4_append_kernel<T, D, G>, dim3(want < most ? want : most, a.c.B), dim3(kAppendThreads), 0, st, a);
+    // CTAs per sequence: a multiple that makes a step a whole number of tokens, about six per SM in all where there is work
+    int unit = 2 * a.c.H;
+    while (unit > 1 && unit % 2 == 0 && (2 * a.c.H / unit) * 2 <= ROWS) unit /= 2;           // 2 H / gcd(2 H, ROWS), ROWS a power of two
+    const long long want = (a.rows + (long long)ROWS * unit - 1) / ((long long)ROWS * unit), most = (di.sm_count * 6 + a.c.B * unit - 1) / (a.c.B * unit);
+    return launch_overlapped(kv4_append_kernel<T, D, G>, dim3((unsigned)(want < most ? want : most) * unit, a.c.B), dim3(kAppendThreads), 0, st, a);
 }
 
 template <typename T>
@@ -127,7 +128,7 @@ static coreinfer_status pick_append(const AppendArgs& a, const DeviceInfo& di, c
 }
 
 // --------------------------------------------------------------------------------- evict --
-// kv4_evict_few_kernel, in place with at most 8 slots above the budget (the step of a decode loop at a full budget): one
+// kv4_evict_few_kernel, in place with at most 16 slots above the budget (the step of a decode loop at a full budget): one
 // CTA per sequence and head takes the smallest key out, once per slot that leaves, and moves what has to move.
 // kv4_select_kernel, otherwise: one CTA, or a cluster of up to 8 where heads are few and long, per sequence and head.  Keys
 // (the order of eviction as unsigned numbers) into shared memory, the key of the last slot that stays by
@@ -137,7 +138,7 @@ static coreinfer_status pick_append(const AppendArgs& a, const DeviceInfo& di, c
 // kv4_move_kernel copies the listed slots, many CTAs per head.
 // All are bound by latency (memory, barriers) at the sizes of a decode step, the moves by bytes after a prompt.
 constexpr int kEvictBins = 2048;
-constexpr int kEvictFew = 8;
+constexpr int kEvictFew = 16;
 constexpr int kEvictKeysMost = 48 * 1024;   // keys a CTA holds in shared memory; more slots are read again for each pass
 constexpr int kEvictMaxCluster = 8;
 constexpr int kMoveSlots = 64;              // slots per CTA of the moving kernel

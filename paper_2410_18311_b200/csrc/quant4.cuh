@@ -122,8 +122,8 @@ __device__ __forceinline__ QuantPair quant_pair(float lo, float hi)
     return p;
 }
 // Codes of N values in one unit or several: clamp(round((x - o) / s), 0, 15), 0 where s is 0 or NaN.  The quotients
-// come from a reciprocal good to a few units in the last place; adding 3 * 2^22 rounds them, ties to even, and leaves
-// the code in the low bits.  A quotient within 1e-4 of a tie between two codes could round to the other one, so the
+// come from a reciprocal, good to 2^-22 of at most 15.5 (4e-6); adding 3 * 2^22 rounds them, ties to even, and leaves
+// the code in the low bits.  A quotient within 1e-5 of a tie between two codes could round to the other one, so the
 // values then go through the division.  units[i] gets four codes; c the codes as numbers.
 constexpr float kRoundMagic = 12582912.f;
 __device__ __forceinline__ float clamp15(float q) { return fminf(fmaxf(q, 0.f), 15.f); }
@@ -139,7 +139,7 @@ __device__ __forceinline__ void quant_codes(const float (&x)[N], float s, float 
         const float q = clamp15(__fsub_rn(x[e], o) * r), t = q + kRoundMagic;
         bits[e] = __float_as_uint(t);
         c[e] = t - kRoundMagic;
-        close |= fabsf(q - c[e]) > 0.4999f;
+        close |= fabsf(q - c[e]) > 0.49999f;
     }
     if (close) {
 #pragma unroll
