@@ -307,6 +307,198 @@ __device__ __forceinline__ int ctas_before(int v, int* slots, unsigned rank, uns
     return before;
 }
 
+// The bin, from the top one down, in which the count reaches `want` (1 <= want <= sum of the bins): found = (bin, how many of it
+// are wanted, its count).  Called by a whole block of `warps` warps; a warp takes a run of bins, row by row of 32.
+__device__ __forceinline__ void find_bin(const unsigned* hist, int want, int warp, int warps, int* buf, int* found)
+{
+    const int lane = threadIdx.x & 31, run = kEvictBins / warps, first = kEvictBins - (warp + 1) * run;
+    int sum = 0;
+    for (int k = lane; k < run; k += 32) sum += hist[first + k];
+    sum = __reduce_add_sync(0xffffffffu, sum);
+    int total;
+    int acc = warps_before(sum, buf, warp, warps, &total);
+    if (acc < want && want <= acc + sum) {
+        for (int k = run - 32;; k -= 32) {
+            const int v = hist[first + k + 31 - lane];       // lane 0 has the row's top bin
+            int incl = v;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int u = __shfl_up_sync(0xffffffffu, incl, d);
+                if (lane >= d) incl += u;
+            }
+            const unsigned hit = __ballot_sync(0xffffffffu, acc + incl >= want);
+            if (hit) {
+                if (lane == __ffs(hit) - 1) {
+                    found[0] = first + k + 31 - lane;
+                    found[1] = want - (acc + incl - v);
+                    found[2] = v;
+                }
+                break;
+            }
+            acc += __shfl_sync(0xffffffffu, incl, 31);
+        }
+    }
+    __syncthreads();
+}
+
+// Sum of v over the threads before this one in the block, and over all.
+__device__ __forceinline__ int threads_before(int v, int* buf, int warp, int warps, int* total)
+{
+    const int lane = threadIdx.x & 31;
+    int incl = v;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int u = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += u;
+    }
+    return warps_before(__shfl_sync(0xffffffffu, incl, 31), buf, warp, warps, total) + incl - v;
+}
+
+// The selection where a head's slots fit the registers of its CTAs: a thread holds the keys of ITEMS consecutive slots,
+// so list order is thread order.  Every CTA of a cluster gets all histograms added up and finds the bins itself.
+template <int ITEMS>
+__global__ void __launch_bounds__(1024) kv4_select_held_kernel(const __grid_constant__ EvictArgs e)
+{
+    __shared__ __align__(16) unsigned local[kEvictBins];
+    __shared__ __align__(16) unsigned sums[3][kEvictBins + 4];               // per pass; entry kEvictBins: slots that stay for certain
+    __shared__ int buf[32], found[4], ties_s[kEvictMaxCluster], movers_s[kEvictMaxCluster], holes_s[kEvictMaxCluster];
+    const Kv4& a = e.a;
+    const unsigned size = cluster_size(), rank = cluster_rank();
+    const int h = blockIdx.x / size, b = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = warp_number(), warps = blockDim.x >> 5;
+    for (int i = tid; i < kEvictBins; i += blockDim.x) local[i] = 0u;
+    for (int i = tid; i < 3 * (kEvictBins + 4); i += blockDim.x) (&sums[0][0])[i] = 0u;
+    wait_for_stream();
+    const int n = kv4_length(a, b), seen = a.state[b * 4 + kStateSeen];
+    const int keep = n < e.budget ? n : e.budget;
+    const size_t base = ((size_t)b * a.H + h) * a.cap;
+    const int share = ((n + (int)size - 1) / (int)size + ITEMS - 1) / ITEMS * ITEMS;
+    const int lo = (int)rank * share < n ? (int)rank * share : n, hi = lo + share < n ? lo + share : n;
+    const int s0 = lo + tid * ITEMS;                        // this thread's slots; those from hi on are not there
+    unsigned key[ITEMS];
+    const bool all = keep == n;
+    if (!all) {
+#pragma unroll
+        for (int i = 0; i < ITEMS; i += 4) {
+            float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+            int4 p = make_int4(0, 0, 0, 0);
+            if (s0 + i < hi) {                              // slots and capacity are multiples of four
+                w = *reinterpret_cast<const float4*>(a.weight + base + s0 + i);
+                p = *reinterpret_cast<const int4*>(a.position + base + s0 + i);
+            }
+            key[i] = evict_key(w.x, p.x, seen, e.recent, e.first);
+            key[i + 1] = evict_key(w.y, p.y, seen, e.recent, e.first);
+            key[i + 2] = evict_key(w.z, p.z, seen, e.recent, e.first);
+            key[i + 3] = evict_key(w.w, p.w, seen, e.recent, e.first);
+        }
+    }
+    cluster_sync(size);                                     // the sums are clear everywhere
+
+    // the slots with (key >> shift) > prefix stay, and the first `left` of those with equality
+    unsigned prefix = 0u;
+    int shift = 0, left = 0;
+    bool whole = false;                                     // all of those with equality stay
+    if (!all && keep > 0) {
+        for (int pass = 0; pass < 3 && !whole; ++pass) {
+            shift = pass == 0 ? 21 : (pass == 1 ? 10 : 0);
+            const int bits = pass == 2 ? 10 : 11;
+            int certain = 0;
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) {
+                const bool in = s0 + i < hi;
+                if (key[i] == 0xffffffffu) certain += in;
+                else if (in && (pass == 0 || key[i] >> (shift + bits) == prefix)) atomicAdd(&local[(key[i] >> shift) & ((1u << bits) - 1u)], 1u);
+            }
+            if (pass == 0) {
+                certain = __reduce_add_sync(0xffffffffu, certain);
+                if (lane == 0 && certain)
+                    for (unsigned r = 0; r < size; ++r) cluster_add(cluster_address(&sums[0][kEvictBins], r), certain);
+            }
+            __syncthreads();
+            for (int i = tid * 4; i < kEvictBins; i += blockDim.x * 4) {
+                const uint4 v = *reinterpret_cast<const uint4*>(&local[i]);
+                const unsigned c[4] = {v.x, v.y, v.z, v.w};
+                if ((v.x | v.y | v.z | v.w) == 0u) continue;
+                *reinterpret_cast<uint4*>(&local[i]) = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (c[k])
+                        for (unsigned r = 0; r < size; ++r) cluster_add(cluster_address(&sums[pass][i + k], r), c[k]);
+            }
+            cluster_sync(size);
+            const int want = pass == 0 ? keep - (int)sums[0][kEvictBins] : left;
+            if (want <= 0) {
+                // only slots that stay for certain do (of more than the budget, with positions that append did not write, the first)
+                prefix = 0xffffffffu;
+                shift = 0;
+                left = keep;
+                break;
+            }
+            find_bin(sums[pass], want, warp, warps, buf, found);
+            prefix = pass == 0 ? (unsigned)found[0] : (prefix << bits) | (unsigned)found[0];
+            left = found[1];
+            whole = found[2] == left;
+        }
+    }
+
+    int movers = 0;
+    if (keep > 0 && !(all && e.in_place)) {
+        // bit i of the masks: slot s0 + i
+        unsigned ties = 0u, stay = 0u;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const bool in = s0 + i < hi, sure = key[i] == 0xffffffffu && prefix != 0xffffffffu;
+            const bool tie = !all && (key[i] >> shift) == prefix && !sure;
+            if (in && tie) ties |= 1u << i;
+            if (in && (all || sure || (key[i] >> shift) > prefix)) stay |= 1u << i;
+        }
+        int ignored;
+        if (whole) {
+            stay |= ties;
+        } else if (!all) {
+            int here;
+            int rank_of = threads_before(__popc(ties), buf, warp, warps, &here);
+            rank_of += ctas_before(here, ties_s, rank, size, &ignored);
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i)
+                if (ties >> i & 1u) {
+                    if (rank_of < left) stay |= 1u << i;
+                    ++rank_of;
+                }
+        }
+        unsigned move = stay, hole = 0u;
+        if (e.in_place) {
+            const int low = keep - s0 < 0 ? 0 : (keep - s0 > ITEMS ? ITEMS : keep - s0);     // of this thread's slots, those below the new length
+            const unsigned below = low >= 32 ? 0xffffffffu : (1u << low) - 1u;
+            const int there = hi - s0 < 0 ? 0 : (hi - s0 > ITEMS ? ITEMS : hi - s0);
+            const unsigned present = there >= 32 ? 0xffffffffu : (1u << there) - 1u;
+            hole = below & present & ~stay;
+            move = stay & ~below;
+        }
+        // one scan for both counts: a CTA has fewer than 2^16 slots
+        int here;
+        const int at = threads_before(__popc(move) | __popc(hole) << 16, buf, warp, warps, &here);
+        int m = (at & 0xffff) + ctas_before(here & 0xffff, movers_s, rank, size, &movers);
+        int* list = e.lists + base;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i)
+            if (move >> i & 1u) list[(e.in_place ? a.cap / 2 : 0) + m++] = s0 + i;
+        if (e.in_place) {
+            int o = (at >> 16) + ctas_before(here >> 16, holes_s, rank, size, &ignored);
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i)
+                if (hole >> i & 1u) list[o++] = s0 + i;
+        }
+    }
+    if (tid == 0 && rank == 0) e.counts[b * a.H + h] = movers;
+    if (size > 1) cluster_sync(size);                       // no CTA ends while another may still write to its shared memory
+    let_next_start();
+    if (kv4_last_of_sequence(a, b, gridDim.x)) {
+        e.z.state[b * 4 + kStateLength] = keep;
+        e.z.state[b * 4 + kStateSeen] = seen;
+    }
+}
+
+// The selection for heads of any length: keys in shared memory, or read again for each pass.
 __global__ void __launch_bounds__(1024) kv4_select_kernel(const __grid_constant__ EvictArgs e)
 {
     extern __shared__ __align__(16) unsigned keys[];
@@ -367,35 +559,8 @@ __global__ void __launch_bounds__(1024) kv4_select_kernel(const __grid_constant_
                 cluster_sync(size);
             }
             if (rank == 0) {
-                // From the top bin down: the bin in which the count reaches `left`.  A warp takes a run of bins, row by row of 32.
                 const int want = pass == 0 ? keep - (int)hist[kEvictBins] : left;
-                const int run = kEvictBins / warps, first = kEvictBins - (warp + 1) * run;
-                int sum = 0;
-                for (int k = lane; k < run; k += 32) sum += hist[first + k];
-                sum = __reduce_add_sync(0xffffffffu, sum);
-                int total;
-                int acc = warps_before(sum, buf, warp, warps, &total);
-                if (acc < want && want <= acc + sum) {
-                    for (int k = run - 32;; k -= 32) {
-                        const int v = hist[first + k + 31 - lane];          // lane 0 has the row's top bin
-                        int incl = v;
-#pragma unroll
-                        for (int d = 1; d < 32; d <<= 1) {
-                            const int u = __shfl_up_sync(0xffffffffu, incl, d);
-                            if (lane >= d) incl += u;
-                        }
-                        const unsigned hit = __ballot_sync(0xffffffffu, acc + incl >= want);
-                        if (hit) {
-                            if (lane == __ffs(hit) - 1) {
-                                found[0] = first + k + 31 - lane;
-                                found[1] = want - (acc + incl - v);
-                                found[2] = v;
-                            }
-                            break;
-                        }
-                        acc += __shfl_sync(0xffffffffu, incl, 31);
-                    }
-                }
+                if (want > 0) find_bin(hist, want, warp, warps, buf, found);
                 if (tid == 0 && want <= 0) found[1] = 0;     // only slots that stay for certain do
                 __syncthreads();
                 if (size > 1 && tid < size && tid > 0)
@@ -581,14 +746,24 @@ coreinfer_status coreinfer_kv4_evict(const coreinfer_kv4_cache* src, const corei
         CI_CUDA(launch_overlapped(kv4_evict_few_kernel, dim3(a.H, a.B), dim3(a.cap <= 4096 ? 256 : 1024), 0, st, e));
         return COREINFER_OK;
     }
-    // Up to 8 CTAs per head while that leaves each 4096 slots at least and all of them fit on the GPU at once.
+    // Up to 8 CTAs per head while that leaves each 4096 slots at least and all of them fit on the GPU at once (1 x 8 heads x
+    // 65536 slots: 137 us with one CTA per head, 23 with eight).
     int cluster = 1;
     while (cluster < kEvictMaxCluster && a.cap / (2 * cluster) >= 4096 && (long long)a.B * a.H * 2 * cluster <= di.sm_count) cluster *= 2;
-    const int slots = (a.cap + cluster - 1) / cluster + 32;
-    e.keys = slots < kEvictKeysMost ? slots : kEvictKeysMost;
-    if ((s = allow_smem<kv4_select_kernel>(di, 16384)) != COREINFER_OK) return s;
-    const dim3 grid(a.H * cluster, a.B), block(slots <= 4096 + 32 ? 512 : 1024);
-    CI_CUDA(launch_overlapped(kv4_select_kernel, grid, block, (size_t)e.keys * sizeof(unsigned), st, e, cluster));
+    const int per = (a.cap + cluster - 1) / cluster;         // slots per CTA, a multiple of 4 (ITEMS at most divides what follows)
+    if (per <= 16384) {
+        const dim3 held(a.H * cluster, a.B);
+        if (per <= 1024) CI_CUDA(launch_overlapped(kv4_select_held_kernel<4>, held, dim3(256), 0, st, e, cluster));
+        else if (per <= 2048) CI_CUDA(launch_overlapped(kv4_select_held_kernel<8>, held, dim3(256), 0, st, e, cluster));
+        else if (per <= 4096) CI_CUDA(launch_overlapped(kv4_select_held_kernel<8>, held, dim3(512), 0, st, e, cluster));
+        else if (per <= 8192) CI_CUDA(launch_overlapped(kv4_select_held_kernel<8>, held, dim3(1024), 0, st, e, cluster));
+        else CI_CUDA(launch_overlapped(kv4_select_held_kernel<16>, held, dim3(1024), 0, st, e, cluster));
+    } else {
+        const int slots = per + 32;
+        e.keys = slots < kEvictKeysMost ? slots : kEvictKeysMost;
+        if ((s = allow_smem<kv4_select_kernel>(di, 16384)) != COREINFER_OK) return s;
+        CI_CUDA(launch_overlapped(kv4_select_kernel, dim3(a.H * cluster, a.B), dim3(1024), (size_t)e.keys * sizeof(unsigned), st, e, cluster));
+    }
     const int most = e.in_place ? (a.cap - budget < a.cap / 2 ? a.cap - budget : a.cap / 2) : (budget < a.cap ? budget : a.cap);
     CI_CUDA(launch_overlapped(kv4_move_kernel, dim3((most + kMoveSlots - 1) / kMoveSlots, a.B * a.H), dim3(kMoveThreads), 0, st, e));
     return COREINFER_OK;
