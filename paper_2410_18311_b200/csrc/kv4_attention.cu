@@ -29,11 +29,11 @@
 
 namespace coreinfer {
 
+constexpr int kAttnWarps = 8;
+constexpr int kAttnThreads = 32 * kAttnWarps;
 // Slots per tile (a piece per warp): pieces of 32, so that waits, votes and addresses are paid once per 32 slots; of 16
 // where registers (head_dim 128 in groups of 32) or shared memory (256) do not carry two.
 template <int D, int G> constexpr int kAttnTile = D == 256 || (D == 128 && G == 32) ? 128 : 256;
-constexpr int kAttnWarps = 8;
-constexpr int kAttnThreads = 32 * kAttnWarps;
 constexpr int kAttnMaxCtas = 320;
 constexpr float kNoLogit = -1e30f;
 // A unit counts this many tiles more than it has when the list is cut: about what starting it costs a CTA (its query
@@ -53,10 +53,12 @@ struct AttnArgs {
     int RB;                 // units per (sequence, key head)
     int n_ctas;             // CTAs of the main kernel
     int tile;               // slots per tile
+    int finish_slots;       // slots per block of the finishing kernel
     float scale;
     int accumulate;
     float2* part_ml;        // [n_ctas][2][RU]: reference exponent and sum of a cut unit's piece
     float* part_o;          // [n_ctas][2][RU][D]
+    int2* pieces;           // [B][H][RB]: first and last CTA that works on a unit
     float2* stats;          // [B][H][RB][RU]: the same of whole units, for the weights
     float* logits;          // [B][H][R][cap], base-2 logits; only with accumulate
 };
@@ -317,6 +319,10 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
             const int first_tile = k.tile, b = k.b, len = lens[b], h = a.RB == 1 ? k.hr : k.hr / a.RB, rb = k.hr - h * a.RB;
             const int n_tiles = n_total - t < k.nt - first_tile ? n_total - t : k.nt - first_tile;
             const int row0 = rb * a.RU + rt * RPT;           // first query row of this warp's tile
+            if (tid == 0 && first_tile == 0) {
+                const int last = pre[b] * HR + k.hr * attn_entries(k.nt) + kAttnUnitCost + k.nt - 1;
+                a.pieces[((size_t)b * c.H + h) * a.RB + rb] = make_int2(me, n_tiles == k.nt ? me : cut.owner(last));
+            }
 
             // query rows as the B operand: column gid = row gid (or part gid & 1 of row gid >> 1), 8 values per 32
             uint32_t qf[H32][4];
@@ -338,17 +344,10 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                 m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
                 const int x = range_exponent(m);             // the largest value goes to [2^13, 2^14)
                 const float up = pow2(14 - x);
-                float gs[NG];
 #pragma unroll
-                for (int g = 0; g < NG; ++g) gs[g] = 0.f;
+                for (int j = 0; j < H32; ++j)
 #pragma unroll
-                for (int j = 0; j < H32; ++j) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        v[j][e] *= up;
-                        gs[j * 32 / G] += v[j][e];
-                    }
-                }
+                    for (int e = 0; e < 8; ++e) v[j][e] *= up;
                 const int low = PARTS ? gid & 1 : 0;
                 const float lo16 = 1.f / 16.f;               // odd codes stand 16 times higher
 #pragma unroll
@@ -360,20 +359,23 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                     qf[j][2] = pack_half2(half_part(p[1] * lo16, low), half_part(q[1] * lo16, low));
                     qf[j][3] = pack_half2(half_part(p[3] * lo16, low), half_part(q[3] * lo16, low));
                 }
-                // sums of c q carry 2^-24, so the sums of q do too; f undoes both scalings
+                // The sums of q over a group: the product with codes that are all 1, which carries the 2^-24 of the
+                // sums of c q as well.  f undoes both scalings.
                 const float ff = ldexpf(a.scale * 1.44269504088896341f, x - 14 + 24);
 #pragma unroll
                 for (int g = 0; g < NG; ++g) {
-                    gs[g] += __shfl_xor_sync(0xffffffffu, gs[g], 1);
-                    gs[g] += __shfl_xor_sync(0xffffffffu, gs[g], 2);
-                    gs[g] *= 1.f / kCodeScaleLow;
+                    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int j = g * G / 32; j < (g + 1) * G / 32; ++j) {
+                        mma_16816(acc, 0x00010001u, 0x00010001u, 0x00010001u, 0x00010001u, qf[j][0], qf[j][1]);
+                        mma_16816(acc, 0x00100010u, 0x00100010u, 0x00100010u, 0x00100010u, qf[j][2], qf[j][3]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < NV; ++i) qsum[g][i] = PARTS ? acc[0] + acc[1] : acc[i];
                 }
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
-                    const int from = (2 * tig + i) * 4;      // a lane of column 2 tig + i
-#pragma unroll
-                    for (int g = 0; g < NG; ++g) qsum[g][i] = __shfl_sync(0xffffffffu, gs[g], from);
-                    f[i] = __shfl_sync(0xffffffffu, ff, from);
+                    f[i] = __shfl_sync(0xffffffffu, ff, (2 * tig + i) * 4);  // from a lane of column 2 tig + i
                     const int rr = row0 + (WIDE ? tig : 2 * tig + i);
                     lim[i] = rr < a.R ? len - (a.T - 1 - token_of(rr)) : 0;
                 }
@@ -692,43 +694,33 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
 
 // ------------------------------------------------------------------------------ finish --
 // Blocks x < R of a (sequence, head): query row x, joined from the pieces of its unit where that was cut
-// (zeros where the sequence is empty).  Blocks beyond: 1024 slots each, whose weights get the
-// sum over rows of 2^(logit - maximum) / sum.
+// (zeros where the sequence is empty).  Blocks beyond: finish_slots slots each, whose weights get the
+// sum over rows of 2^(logit - maximum) / sum.  A thread has U quads of slots and BATCH rows in flight: 4 and 1 where
+// there is one row per key head, else 1 and 8.
 constexpr int kFinishThreads = 256;
-constexpr int kFinishSlots = 1024;
+constexpr int kFinishSlots = 4 * kFinishThreads;             // per round of a block
 
-template <typename T>
-__global__ void __launch_bounds__(kFinishThreads) kv4_finish_kernel(const __grid_constant__ AttnArgs a)
+template <typename T, int U, int BATCH>
+__global__ void __launch_bounds__(kFinishThreads, 3) kv4_finish_kernel(const __grid_constant__ AttnArgs a)
 {
     extern __shared__ __align__(128) uint8_t smem[];
     const Kv4& c = a.c;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int b = blockIdx.y / c.H, h = blockIdx.y % c.H, D = c.D;
-    // the state was complete before the main kernel started, whose end is awaited below
-    const int len = kv4_length(c, b);
-    if ((int)blockIdx.x >= a.R && ((int)blockIdx.x - a.R) * kFinishSlots >= len) return;
-    int before = 0, all = 0;                                 // tiles of a head, before this sequence and in all; every warp for itself
-    for (int i = lane; i < c.B; i += 32) {
-        const int n = attn_tiles(kv4_length(c, i), a.tile);
-        all += attn_entries(n);
-        if (i < b) before += attn_entries(n);
-    }
-    before = __reduce_add_sync(0xffffffffu, before);
-    all = __reduce_add_sync(0xffffffffu, all);
-    const int HR = c.H * a.RB, nt = attn_tiles(len, a.tile), total = all * HR;
-    const AttnCut cut(a.n_ctas, total);
+    const int tid = threadIdx.x, lane = tid & 31, warp = warp_number(), h = blockIdx.y, b = blockIdx.z, D = c.D;
+    const size_t unit0 = ((size_t)b * c.H + h) * a.RB;
     wait_for_stream();
+    let_next_start();
+    const int len = kv4_length(c, b);
 
     if ((int)blockIdx.x < a.R) {
         const int r = blockIdx.x, rb = r / a.RU, ru = r % a.RU;
         const int rt_ = a.T == 1 ? 0 : r / a.share;
         T* dst = (T*)a.out + ((long long)b * a.T + rt_) * a.ld_out + (long long)(h * a.share + r - rt_ * a.share) * D;
-        if (nt == 0) {
+        if (len == 0) {
             for (int d = tid; d < D; d += kFinishThreads) dst[d] = from_f32<T>(0.f);
             return;
         }
-        const int u0 = before * HR + (h * a.RB + rb) * attn_entries(nt) + kAttnUnitCost;
-        const int i0 = cut.owner(u0), i1 = cut.owner(u0 + nt - 1);
+        const int2 range = a.pieces[unit0 + rb];
+        const int i0 = range.x, i1 = range.y;
         if (i0 == i1) return;
         const int n = i1 - i0 + 1;
         auto piece = [&](int i) { return ((size_t)(i0 + i) * 2 + (i == 0 ? 1 : 0)) * a.RU + ru; };
@@ -768,54 +760,91 @@ __global__ void __launch_bounds__(kFinishThreads) kv4_finish_kernel(const __grid
         return;
     }
 
-    // weights: maximum and 1 / sum of every row, one warp per row
+    // weights: four slots a thread (the capacity is a multiple of 16, so they lie within a row of logits); the first rows'
+    // logits are on their way while the rows' maxima and sums are put together
+    const int first = ((int)blockIdx.x - a.R) * a.finish_slots, end = first + a.finish_slots < len ? first + a.finish_slots : len;
+    if (first >= end) return;
+    const float* lg = a.logits + ((size_t)b * c.H + h) * a.R * c.cap;
+    float* weight = c.weight + ((size_t)b * c.H + h) * c.cap;
+    float4 w[U], x[U][BATCH];
+    auto load_w = [&](int n0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (n0 + u * kFinishSlots < end) w[u] = *reinterpret_cast<const float4*>(weight + n0 + u * kFinishSlots);
+    };
+    auto load_x = [&](int n0, int r0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k)
+                if (n0 + u * kFinishSlots < end && r0 + k < a.R)
+                    x[u][k] = *reinterpret_cast<const float4*>(lg + (size_t)(r0 + k) * c.cap + n0 + u * kFinishSlots);
+    };
+    load_w(first + tid * 4);
+    load_x(first + tid * 4, 0);
+    // maximum and 1 / sum of every row, and how many slots it sees; one warp per row
     float2* rows = reinterpret_cast<float2*>(smem);                      // [R]
-    int* sees = reinterpret_cast<int*>(rows + a.R);                      // [R] slots that the row sees
+    int* sees = reinterpret_cast<int*>(rows + a.R);                      // [R]
+    int rb = -1, i0 = 0, i1 = 0;
     for (int r = warp; r < a.R; r += kFinishThreads / 32) {
-        const int rb = r / a.RU, ru = r % a.RU;
-        const int u0 = before * HR + (h * a.RB + rb) * attn_entries(nt) + kAttnUnitCost;
-        const int i0 = cut.owner(u0), i1 = cut.owner(u0 + nt - 1);
+        const int of = a.RB == 1 ? 0 : r / a.RU, ru = r - of * a.RU;
+        if (of != rb) {
+            rb = of;
+            const int2 range = a.pieces[unit0 + rb];
+            i0 = range.x;
+            i1 = range.y;
+        }
         float top, sum;
         if (i0 == i1) {
-            const float2 ml = a.stats[(((size_t)b * c.H + h) * a.RB + rb) * a.RU + ru];
+            const float2 ml = a.stats[(unit0 + rb) * a.RU + ru];
             top = ml.x;
             sum = ml.y;
         } else {
-            top = kNoLogit * 2.f;
-            for (int i = i0 + lane; i <= i1; i += 32) top = fmaxf(top, a.part_ml[((size_t)i * 2 + (i == i0)) * a.RU + ru].x);
+            float2 ml = make_float2(kNoLogit * 2.f, 0.f);                // up to 32 pieces are loaded once
+            if (i0 + lane <= i1) ml = a.part_ml[((size_t)(i0 + lane) * 2 + (lane == 0)) * a.RU + ru];
+            top = ml.x;
+            for (int i = i0 + lane + 32; i <= i1; i += 32) top = fmaxf(top, a.part_ml[(size_t)i * 2 * a.RU + ru].x);
 #pragma unroll
             for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-            sum = 0.f;
-            for (int i = i0 + lane; i <= i1; i += 32) {
-                const float2 ml = a.part_ml[((size_t)i * 2 + (i == i0)) * a.RU + ru];
-                sum = fmaf(ml.y, exp2_fast(ml.x - top), sum);
+            sum = ml.y * exp2_fast(ml.x - top);
+            for (int i = i0 + lane + 32; i <= i1; i += 32) {
+                const float2 more = a.part_ml[(size_t)i * 2 * a.RU + ru];
+                sum = fmaf(more.y, exp2_fast(more.x - top), sum);
             }
 #pragma unroll
             for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
         }
         if (lane == 0) {
             rows[r] = make_float2(top, sum == 0.f ? 0.f : 1.f / sum);
-            sees[r] = len - (a.T - 1 - r / a.share);
+            sees[r] = len - (a.T - 1 - (a.T == 1 ? 0 : r / a.share));
         }
     }
     __syncthreads();
-    // four slots a thread: the capacity is a multiple of 16, so they lie within a row of logits
-    const int n = ((int)blockIdx.x - a.R) * kFinishSlots + tid * 4;
-    if (n >= len) return;
-    const float* lg = a.logits + ((size_t)b * c.H + h) * a.R * c.cap + n;
-    float4* weight = reinterpret_cast<float4*>(c.weight + ((size_t)b * c.H + h) * c.cap + n);
-    float4 w = *weight;
-#pragma unroll 8
-    for (int r = 0; r < a.R; ++r) {
-        const float4 x = *reinterpret_cast<const float4*>(lg + (size_t)r * c.cap);
-        const float2 ml = rows[r];
-        const int see = sees[r] - n;                        // slots of the four that the row sees
-        if (see > 0) w.x = fmaf(exp2_fast(x.x - ml.x), ml.y, w.x);
-        if (see > 1) w.y = fmaf(exp2_fast(x.y - ml.x), ml.y, w.y);
-        if (see > 2) w.z = fmaf(exp2_fast(x.z - ml.x), ml.y, w.z);
-        if (see > 3) w.w = fmaf(exp2_fast(x.w - ml.x), ml.y, w.w);
+    for (int n0 = first + tid * 4; n0 < end; n0 += U * kFinishSlots) {
+        if (n0 >= first + U * kFinishSlots) {
+            load_w(n0);
+            load_x(n0, 0);
+        }
+        for (int r0 = 0; r0 < a.R; r0 += BATCH) {
+            if (r0 > 0) load_x(n0, r0);
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) {
+                if (r0 + k >= a.R) break;
+                const float2 ml = rows[r0 + k];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int see = sees[r0 + k] - (n0 + u * kFinishSlots);          // slots of the four that the row sees
+                    if (see > 0) w[u].x = fmaf(exp2_fast(x[u][k].x - ml.x), ml.y, w[u].x);
+                    if (see > 1) w[u].y = fmaf(exp2_fast(x[u][k].y - ml.x), ml.y, w[u].y);
+                    if (see > 2) w[u].z = fmaf(exp2_fast(x[u][k].z - ml.x), ml.y, w[u].z);
+                    if (see > 3) w[u].w = fmaf(exp2_fast(x[u][k].w - ml.x), ml.y, w[u].w);
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (n0 + u * kFinishSlots < end) *reinterpret_cast<float4*>(weight + n0 + u * kFinishSlots) = w[u];
     }
-    *weight = w;
 }
 
 // -------------------------------------------------------------------------------- host --
@@ -831,16 +860,17 @@ static void attn_rows(int R, int rpt, int* RT, int* RU, int* RB)
 }
 
 struct AttnLayout {
-    size_t ml, o, stats, logits, total;
+    size_t ml, o, pieces, stats, logits, total;
 };
 static AttnLayout attn_layout(const Kv4& c, int R, int rpt)
 {
     int RT, RU, RB;
     attn_rows(R, rpt, &RT, &RU, &RB);
     AttnLayout w;
-    w.ml = 256;
+    w.ml = 0;
     w.o = w.ml + up256((size_t)kAttnMaxCtas * 2 * RU * sizeof(float2));
-    w.stats = w.o + up256((size_t)kAttnMaxCtas * 2 * RU * c.D * sizeof(float));
+    w.pieces = w.o + up256((size_t)kAttnMaxCtas * 2 * RU * c.D * sizeof(float));
+    w.stats = w.pieces + up256((size_t)c.B * c.H * RB * sizeof(int2));
     w.logits = w.stats + up256((size_t)c.B * c.H * RB * RU * sizeof(float2));
     w.total = w.logits + (c.weight ? up256((size_t)c.B * c.H * R * c.cap * sizeof(float)) : 0);
     return w;
@@ -868,8 +898,13 @@ static coreinfer_status launch_mode(AttnArgs& a, const DeviceInfo& di, cudaStrea
     if (s != COREINFER_OK) return s;
     CI_CUDA(launch_overlapped(kv4_attention_kernel<T, D, G, MODE>, dim3(a.n_ctas), dim3(kAttnThreads), smem, st, a));
     const size_t join = kFinishThreads * sizeof(float4), rows = (size_t)a.R * (sizeof(float2) + sizeof(int));
-    const dim3 grid(a.R + (a.accumulate ? (a.c.cap + kFinishSlots - 1) / kFinishSlots : 0), a.c.B * a.c.H);
-    CI_CUDA(launch_overlapped(kv4_finish_kernel<T>, grid, dim3(kFinishThreads), join > rows ? join : rows, st, a));
+    // up to four rounds a block while that leaves about two blocks per SM and slot of it
+    a.finish_slots = kFinishSlots;
+    while (a.finish_slots < 4 * kFinishSlots &&
+           (long long)a.c.B * a.c.H * ((a.c.cap + 2 * a.finish_slots - 1) / (2 * a.finish_slots)) >= 6LL * di.sm_count) a.finish_slots *= 2;
+    const dim3 grid(a.R + (a.accumulate ? (a.c.cap + a.finish_slots - 1) / a.finish_slots : 0), a.c.H, a.c.B);
+    if (a.R == 1) CI_CUDA(launch_overlapped(kv4_finish_kernel<T, 4, 1>, grid, dim3(kFinishThreads), join > rows ? join : rows, st, a));
+    else CI_CUDA(launch_overlapped(kv4_finish_kernel<T, 1, 8>, grid, dim3(kFinishThreads), join > rows ? join : rows, st, a));
     return COREINFER_OK;
 }
 
@@ -932,7 +967,6 @@ coreinfer_status coreinfer_kv4_attention(const coreinfer_kv4_cache* cache, const
         CI_FAIL(COREINFER_ERR_INVALID_ARG, "q_heads %d is not a multiple of kv_heads %d", q_heads, a.c.H);
     const long long R = (long long)(q_heads / a.c.H) * T;
     if (R > kAttnMaxRows) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "%lld query rows per key head: at most %d", R, kAttnMaxRows);
-    if ((long long)a.c.B * a.c.H > 65535) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "batch * kv_heads: at most 65535");
     if (!q || !out || !aligned16(q) || !aligned16(out)) CI_FAIL(COREINFER_ERR_INVALID_ARG, "q / out NULL or not 16-byte aligned");
     const int64_t row = (int64_t)q_heads * a.c.D, e = (int64_t)dtype_size(dtype);
     if (ld_q < row || ld_out < row || (ld_q * e) % 16 != 0 || (ld_out * e) % 16 != 0)
@@ -960,6 +994,7 @@ coreinfer_status coreinfer_kv4_attention(const coreinfer_kv4_cache* cache, const
     a.accumulate = accumulate ? 1 : 0;
     a.part_ml = (float2*)(ws + w.ml);
     a.part_o = (float*)(ws + w.o);
+    a.pieces = (int2*)(ws + w.pieces);
     a.stats = (float2*)(ws + w.stats);
     a.logits = (float*)(ws + w.logits);
     cudaStream_t st = (cudaStream_t)cuda_stream;
