@@ -385,7 +385,7 @@ coreinfer_status coreinfer_prefill_activations(const void* x, int32_t T, coreinf
  *
  * Format.  A group of `group` (32, 64 or 128) consecutive values x of a row is held as codes
  * c in 0..15 and one fp16 pair (s, o):   x^ = s * c + o   with
- *   o = fp16(min x),  s = fp16((max x - min x) / 15),  c = clamp(round((x - o) / s), 0, 15)
+ *   o = fp16(min x),  s = fp16((max x - min x) * fp32(1/15)),  c = clamp(round((x - o) / s), 0, 15)
  * (fp32 arithmetic, ties to even; c = 0 where s is 0; o and s are clamped to the finite fp16
  * range; a group that holds a NaN is stored as NaN).  A row piece of 32 H values takes 16 H bytes
  * in units of two bytes: unit i * H + h (i = 0..7, h = 0..H-1) holds values 32 h + 4 i .. + 3,

@@ -1,9 +1,14 @@
 // Attention of a few new tokens per sequence over the 4-bit key/value cache.
 //
 // Mathematics.  With x^ = s c + o per group, a logit is  sum_g [ s_g sum_{d in g} q_d c_d + o_g sum_{d in g} q_d ]
-// and an output  sum_n (p_n s_n) c_nd + sum_n p_n o_n : both products run over the codes themselves, scales enter
-// as factors of fp32 sums (keys) or of the fp32 weights p (values).  One pass over the cache with a running
-// maximum per query row; rows = new tokens x query heads that share a key head.
+// and an output  sum_n (p_n s_n) c_nd + sum_n p_n o_n : both products run over the codes themselves, scales enter as factors
+// of fp32 sums (keys) or of the fp32 weights p (values).  One pass over the cache with a running maximum per query
+// row; rows = new tokens x query heads that share a key head.
+// Values average out and codes 0..15 do not: over 130000 slots of equal weight the sum of p s c is some thousand times the
+// output, and the MMA's accumulators cut off below their last place (4.2e-4 of the output instead of fp16's
+// 2.1e-4).  So every kAttnCentre pieces 8 times what p s came to is taken out of the accumulators, by an MMA with codes
+// that are all -8, and put into the sum of p o.  fp32 calls, whose outputs keep those bits, subtract 8 from every code
+// instead (one more instruction per two codes), and start the sums of q c at -8 sum q.
 //
 // What bounds it: the bytes of the cache (codes and pairs of keys and values, each read once).  The work per
 // byte is what has to be kept small, so the codes go to mma.sync.m16n8k16 as fp16 subnormals (quant4.cuh: one AND
@@ -117,6 +122,14 @@ __device__ __forceinline__ void store4(T* dst, float x, float y, float z, float 
     else *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<uint2*>(v);
 }
 
+// Two codes c (or 16 c) less 8 (128), as fp16: above 1024 the codes are the low bits of a number whose last place is 1.
+__device__ __forceinline__ uint32_t centred(uint32_t x, uint32_t mask, uint32_t middle)
+{
+    const uint32_t up = (x & mask) | 0x64006400u;
+    const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&up), *reinterpret_cast<const __half2*>(&middle));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+
 // A condition that is rarely true and the same for the warp: used as the bound of a loop of at most one round, so that
 // the compiler branches around the body instead of executing it under a predicate.
 __device__ __forceinline__ int opaque_zero()
@@ -125,6 +138,10 @@ __device__ __forceinline__ int opaque_zero()
     asm volatile("mov.u32 %0, 0;" : "=r"(z));
     return z;
 }
+
+// Pieces of a warp between two centrings: the accumulators hold at most their sum of p s c off centre, which costs
+// about 2^-24 of it per 16 slots: 5e-4 of the output over 130000 slots of equal weight for bf16, 1e-4 for the others.
+template <int MODE> constexpr int kAttnCentre = MODE == 2 ? 2 : 8;
 
 // Stages of a warp's ring: as many as two CTAs per SM (head_dim 256: one) leave room for.
 template <int D, int G, int MODE> constexpr int kAttnStages =
@@ -143,7 +160,7 @@ template <typename T, int D, int G, int MODE>
 __global__ void __launch_bounds__(kAttnThreads, D <= 128 ? 2 : 1)
 kv4_attention_kernel(const __grid_constant__ AttnArgs a)
 {
-    constexpr bool PARTS = MODE == kRows4Parts, WIDE = MODE != kRows8;
+    constexpr bool PARTS = MODE == kRows4Parts, WIDE = MODE != kRows8, CENTRED = sizeof(T) == 4;
     constexpr int H32 = D / 32, NG = D / G, RPT = WIDE ? 4 : 8, NV = WIDE ? 1 : 2, TILE = kAttnTile<D, G>;
     constexpr int UN = TILE / (16 * kAttnWarps);             // pieces of 16 slots per step of a warp
     constexpr uint32_t CODE_ROW = D / 2, PAIR_ROW = NG * 4;
@@ -388,7 +405,8 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
             }
             const int all_see = len - (a.T - 1);             // slots below this are seen by every row
 
-            float o[H32][2][4], om[NG][NV], l[NV], mx[NV];
+            float o[H32][2][4], om[NG][NV], sum_ps[NG][NV], l[NV], mx[NV];
+            int centre = kAttnCentre<MODE>;
             // The weights enter the second product as p s 2^E in fp16: E keeps the largest s near 2^9, so
             // that p s neither overflows nor loses bits to fp16's bottom for p down to about 2^-20.
             float E = 0.f, s_most = -1.f;
@@ -401,7 +419,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                 l[i] = 0.f;
                 mx[i] = kNoLogit;
 #pragma unroll
-                for (int g = 0; g < NG; ++g) om[g][i] = 0.f;
+                for (int g = 0; g < NG; ++g) om[g][i] = sum_ps[g][i] = 0.f;
             }
 
             const int seg_end = (first_tile + n_tiles) * TILE < len ? (first_tile + n_tiles) * TILE : len;
@@ -430,17 +448,25 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
 #pragma unroll
                         for (int g = 0; g < NG; ++g) {
                             float acc[4];
+                            if (CENTRED) {                   // fp32: the sums start at -8 sum q (columns of high parts)
+                                acc[0] = acc[2] = -8.f * qsum[g][0];
+                                acc[1] = acc[3] = 0.f;
+                            }
 #pragma unroll
                             for (int j = g * G / 32; j < (g + 1) * G / 32; ++j) {
                                 const uint32_t x0 = code_word<G, H32>(w0, j), x1 = code_word<G, H32>(w1, j);
                                 const uint32_t y0 = x0 >> 8, y1 = x1 >> 8;
-                                if (j == g * G / 32)
+                                if (j == g * G / 32 && !CENTRED)
                                     mma_16816_zero(acc, x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, qf[j][0], qf[j][1]);
                                 else
                                     mma_16816(acc, x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, qf[j][0], qf[j][1]);
                                 mma_16816(acc, x0 & 0x00f000f0u, x1 & 0x00f000f0u, y0 & 0x00f000f0u, y1 & 0x00f000f0u, qf[j][2], qf[j][3]);
                             }
-                            const float2 p0 = pair_f32(kp0[g]), p1 = pair_f32(kp1[g]);
+                            float2 p0 = pair_f32(kp0[g]), p1 = pair_f32(kp1[g]);
+                            if (CENTRED) {
+                                p0.y = fmaf(8.f, p0.x, p0.y);
+                                p1.y = fmaf(8.f, p1.x, p1.y);
+                            }
 #pragma unroll
                             for (int i = 0; i < NV; ++i) {
                                 const float a0 = PARTS ? acc[0] + acc[1] : acc[i], a1 = PARTS ? acc[2] + acc[3] : acc[2 + i];
@@ -535,7 +561,10 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                             mx[i] = m;
                             l[i] *= corr;
 #pragma unroll
-                            for (int g = 0; g < NG; ++g) om[g][i] *= corr;
+                            for (int g = 0; g < NG; ++g) {
+                                om[g][i] *= corr;
+                                sum_ps[g][i] *= corr;
+                            }
 #pragma unroll
                             for (int j = 0; j < H32; ++j)
 #pragma unroll
@@ -582,7 +611,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                                 for (int i = 0; i < NV; ++i) {
                                     om_was[i] = om[g][i];
                                     ps[i] = lo[u][v][i] * so.x;
-                                    om[g][i] = fmaf(lo[u][v][i], so.y, om[g][i]);
+                                    om[g][i] = fmaf(lo[u][v][i], CENTRED ? fmaf(8.f, so.x, so.y) : so.y, om[g][i]);
                                 }
                                 if (!WIDE && edge) {         // a slot that a row does not see adds nothing, whatever it holds
 #pragma unroll
@@ -592,6 +621,9 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                                             om[g][i] = om_was[i];
                                         }
                                 }
+#pragma unroll
+                                for (int i = 0; i < NV; ++i)
+                                    if (!CENTRED) sum_ps[g][i] += ps[i];
                                 if (PARTS) {
                                     const float high = __half2float(__float2half_rn(ps[0]));
                                     bf[v] = movmatrix_trans(pack_half2(high, ps[0] - high));
@@ -604,13 +636,40 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                                 const uint32_t x = __byte_perm(va[j / 2], vb[j / 2], j & 1 ? 0x7632 : 0x5410);
                                 const uint32_t y = __byte_perm(vc[j / 2], vd[j / 2], j & 1 ? 0x7632 : 0x5410);
                                 const uint32_t x8 = x >> 8, y8 = y >> 8;
-                                mma_16816(o[j][0], x & 0x000f000fu, x8 & 0x000f000fu, y & 0x000f000fu, y8 & 0x000f000fu, bf[0], bf[1]);
-                                mma_16816(o[j][1], x & 0x00f000f0u, x8 & 0x00f000f0u, y & 0x00f000f0u, y8 & 0x00f000f0u, bf[0], bf[1]);
+                                if (CENTRED) {
+                                    mma_16816(o[j][0], centred(x, 0x000f000fu, 0x64086408u), centred(x8, 0x000f000fu, 0x64086408u),
+                                              centred(y, 0x000f000fu, 0x64086408u), centred(y8, 0x000f000fu, 0x64086408u), bf[0], bf[1]);
+                                    mma_16816(o[j][1], centred(x, 0x00f000f0u, 0x64806480u), centred(x8, 0x00f000f0u, 0x64806480u),
+                                              centred(y, 0x00f000f0u, 0x64806480u), centred(y8, 0x00f000f0u, 0x64806480u), bf[0], bf[1]);
+                                } else {
+                                    mma_16816(o[j][0], x & 0x000f000fu, x8 & 0x000f000fu, y & 0x000f000fu, y8 & 0x000f000fu, bf[0], bf[1]);
+                                    mma_16816(o[j][1], x & 0x00f000f0u, x8 & 0x00f000f0u, y & 0x00f000f0u, y8 & 0x00f000f0u, bf[0], bf[1]);
+                                }
                             }
                         }
                     }
                 }
                 leave(1);
+                if (!CENTRED && --centre == 0) {
+                    centre = kAttnCentre<MODE>;
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) {
+                        // what is taken out and put back is one fp16 number per lane, so the two are the same; the rest waits
+                        float take[NV];
+#pragma unroll
+                        for (int i = 0; i < NV; ++i) {
+                            take[i] = __half2float(__float2half_rn(fminf(sum_ps[g][i], 60000.f)));
+                            sum_ps[g][i] -= take[i];
+                            om[g][i] = fmaf(8.f, take[i], om[g][i]);
+                        }
+                        const uint32_t b0 = movmatrix_trans(pack_half2(take[0], WIDE ? 0.f : take[NV - 1]));
+#pragma unroll
+                        for (int j = g * G / 32; j < (g + 1) * G / 32; ++j) {
+                            mma_16816(o[j][0], 0x80088008u, 0x80088008u, 0x80088008u, 0x80088008u, b0, 0u);
+                            mma_16816(o[j][1], 0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u, b0, 0u);
+                        }
+                    }
+                }
             }
 
             // ---- join the warps of a row tile ----
@@ -640,10 +699,11 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                         v.z = o[j][0][2 + i];
                         v.w = o[j][1][2 + i];
                     }
-                    v.x = fmaf(v.x, kCodeScaleLow, add);
-                    v.y = fmaf(v.y, kCodeScaleHigh, add);
-                    v.z = fmaf(v.z, kCodeScaleLow, add);
-                    v.w = fmaf(v.w, kCodeScaleHigh, add);
+                    constexpr float even = CENTRED ? 1.f : kCodeScaleLow, odd = CENTRED ? 1.f / 16.f : kCodeScaleHigh;
+                    v.x = fmaf(v.x, even, add);
+                    v.y = fmaf(v.y, odd, add);
+                    v.z = fmaf(v.z, even, add);
+                    v.w = fmaf(v.w, odd, add);
                     *reinterpret_cast<float4*>(obuf + ((size_t)warp * RPT + r) * D + j * 32 + gid * 4) = v;
                 }
             }

@@ -117,7 +117,7 @@ __device__ __forceinline__ QuantPair quant_pair(float lo, float hi)
 {
     QuantPair p;
     p.o = __float2half_rn(fminf(fmaxf(lo, -kHalfMax), kHalfMax));
-    p.s = __float2half_rn(min_nan(__fdiv_rn(__fsub_rn(hi, lo), 15.f), kHalfMax));
+    p.s = __float2half_rn(min_nan(__fmul_rn(__fsub_rn(hi, lo), 1.f / 15.f), kHalfMax));
     if (lo != lo) p.s = p.o = __ushort_as_half((unsigned short)0x7fff);
     return p;
 }

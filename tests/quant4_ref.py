@@ -20,7 +20,7 @@ def quantise(x, group):
         nan = np.isnan(g).any(-1)
         lo, hi = np.where(nan, np.float32(0), lo), np.where(nan, np.float32(0), hi)
         o = np.clip(lo, np.float32(-65504), np.float32(65504)).astype(np.float16)
-        s = np.minimum((hi - lo) / np.float32(15), np.float32(65504)).astype(np.float16)
+        s = np.minimum((hi - lo) * (np.float32(1) / np.float32(15)), np.float32(65504)).astype(np.float16)
         o, s = np.where(nan, np.float16(np.nan), o), np.where(nan, np.float16(np.nan), s)
         c = np.rint((g - o.astype(np.float32)[..., None]) / s.astype(np.float32)[..., None])
         c = np.where(s.astype(np.float32)[..., None] > 0, np.clip(c, 0, 15), 0)
