@@ -367,14 +367,17 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                     for (int e = 0; e < 8; ++e) v[j][e] *= up;
                 const int low = PARTS ? gid & 1 : 0;
                 const float lo16 = 1.f / 16.f;               // odd codes stand 16 times higher
+                // High parts are multiples of 8, fp16's step at the row's largest value, so that their sums are exact (with each value
+                // rounded by itself the logits were off by 1.2e-6 of their spread, now by 2e-7).
+                auto row_part = [low](float x, float step) { return PARTS ? half_part(x, step, low) : x; };
 #pragma unroll
                 for (int j = 0; j < H32; ++j) {
                     // the two entries beside each other in step j (code_word)
                     const float *p = G == 32 ? &v[j][0] : &v[j & ~1][(j & 1) * 4], *q = G == 32 ? &v[j][4] : &v[j | 1][(j & 1) * 4];
-                    qf[j][0] = pack_half2(half_part(p[0], low), half_part(q[0], low));
-                    qf[j][1] = pack_half2(half_part(p[2], low), half_part(q[2], low));
-                    qf[j][2] = pack_half2(half_part(p[1] * lo16, low), half_part(q[1] * lo16, low));
-                    qf[j][3] = pack_half2(half_part(p[3] * lo16, low), half_part(q[3] * lo16, low));
+                    qf[j][0] = pack_half2(row_part(p[0], 8.f), row_part(q[0], 8.f));
+                    qf[j][1] = pack_half2(row_part(p[2], 8.f), row_part(q[2], 8.f));
+                    qf[j][2] = pack_half2(row_part(p[1] * lo16, .5f), row_part(q[1] * lo16, .5f));
+                    qf[j][3] = pack_half2(row_part(p[3] * lo16, .5f), row_part(q[3] * lo16, .5f));
                 }
                 // The sums of q over a group: the product with codes that are all 1, which carries the 2^-24 of the
                 // sums of c q as well.  f undoes both scalings.
@@ -448,15 +451,11 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
 #pragma unroll
                         for (int g = 0; g < NG; ++g) {
                             float acc[4];
-                            if (CENTRED) {                   // fp32: the sums start at -8 sum q (columns of high parts)
-                                acc[0] = acc[2] = -8.f * qsum[g][0];
-                                acc[1] = acc[3] = 0.f;
-                            }
 #pragma unroll
                             for (int j = g * G / 32; j < (g + 1) * G / 32; ++j) {
                                 const uint32_t x0 = code_word<G, H32>(w0, j), x1 = code_word<G, H32>(w1, j);
                                 const uint32_t y0 = x0 >> 8, y1 = x1 >> 8;
-                                if (j == g * G / 32 && !CENTRED)
+                                if (j == g * G / 32)
                                     mma_16816_zero(acc, x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, qf[j][0], qf[j][1]);
                                 else
                                     mma_16816(acc, x0 & 0x000f000fu, x1 & 0x000f000fu, y0 & 0x000f000fu, y1 & 0x000f000fu, qf[j][0], qf[j][1]);
@@ -469,6 +468,10 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                             }
 #pragma unroll
                             for (int i = 0; i < NV; ++i) {
+                                if (CENTRED) {               // the sums of high parts are exact: what cancels leaves nothing behind
+                                    acc[0] = fmaf(-8.f, qsum[g][0], acc[0]);
+                                    acc[2] = fmaf(-8.f, qsum[g][0], acc[2]);
+                                }
                                 const float a0 = PARTS ? acc[0] + acc[1] : acc[i], a1 = PARTS ? acc[2] + acc[3] : acc[2 + i];
                                 const float o0 = p0.y * qsum[g][i], o1 = p1.y * qsum[g][i];
                                 lo[u][0][i] = fmaf(p0.x, a0, g ? lo[u][0][i] + o0 : o0);
@@ -625,7 +628,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                                 for (int i = 0; i < NV; ++i)
                                     if (!CENTRED) sum_ps[g][i] += ps[i];
                                 if (PARTS) {
-                                    const float high = __half2float(__float2half_rn(ps[0]));
+                                    const float high = __half2float(__float2half_rn(CENTRED ? round_to(ps[0], .5f) : ps[0]));
                                     bf[v] = movmatrix_trans(pack_half2(high, ps[0] - high));
                                 } else {
                                     bf[v] = movmatrix_trans(pack_half2(ps[0], WIDE ? 0.f : ps[NV - 1]));

@@ -185,11 +185,19 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi)
     const __half2 h = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
-// v rounded to fp16, or what that rounding left over: together 22 bits of v.
-__device__ __forceinline__ float half_part(float v, int low)
+// v rounded to a multiple of `step` (a power of two; |v| < 2^22 steps).  Sums of products of such numbers with codes
+// stay whole multiples of the step, which an fp32 accumulator holds exactly up to 2^24 of them; the MMA cuts off, and
+// does not round, what lies below its last place.
+__device__ __forceinline__ float round_to(float v, float step)
 {
-    const float h = __half2float(__float2half_rn(v));
-    return low ? v - h : v;
+    const float middle = 12582912.f * step;
+    return __fadd_rn(__fadd_rn(v, middle), -middle);
+}
+// The two fp16 parts of a v below 2048 steps, together 22 bits of the largest such v.
+__device__ __forceinline__ float half_part(float v, float step, int low)
+{
+    const float high = round_to(v, step);
+    return low ? v - high : high;
 }
 // Exponent x with m = max |v| in [2^(x-1), 2^x), at least -100; 14 where no scaling can help (m = 0, infinite or NaN).
 __device__ __forceinline__ int range_exponent(float m)

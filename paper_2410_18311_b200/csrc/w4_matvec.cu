@@ -212,11 +212,12 @@ struct XStage {
             const float up = pow2(14 - x), up16 = up * (1.f / 16.f);          // odd codes stand 16 times higher
 #pragma unroll
             for (int part = 0; part < (SPLIT ? 2 : 1); ++part) {
+                auto x_part = [part](float x, float step) { return SPLIT ? half_part(x, step, part) : x; };
                 uint4 f;
-                f.x = pack_half2(half_part(p[0] * up, part), half_part(q[0] * up, part));
-                f.y = pack_half2(half_part(p[2] * up, part), half_part(q[2] * up, part));
-                f.z = pack_half2(half_part(p[1] * up16, part), half_part(q[1] * up16, part));
-                f.w = pack_half2(half_part(p[3] * up16, part), half_part(q[3] * up16, part));
+                f.x = pack_half2(x_part(p[0] * up, 8.f), x_part(q[0] * up, 8.f));
+                f.y = pack_half2(x_part(p[2] * up, 8.f), x_part(q[2] * up, 8.f));
+                f.z = pack_half2(x_part(p[1] * up16, .5f), x_part(q[1] * up16, .5f));
+                f.w = pack_half2(x_part(p[3] * up16, .5f), x_part(q[3] * up16, .5f));
                 xs[((ks[u] * 4 + h) * slots + (SPLIT ? 2 * bs[u] + part : bs[u])) * 4 + tig] = f;
             }
             if ((l16 & (G / 8 - 1)) == 0) xg[(ks[u] * PER + l16 / (G / 8)) * a.batch + bs[u]] = make_float2(pow2(x - 14), sum);
