@@ -414,7 +414,7 @@ size_t coreinfer_w4_pairs_bytes(int32_t N, int32_t K, int32_t group);
  *           strides (1, d_model) the transposed compacted down projection [K, d_model] serves
  *           as the matrix [d_model, K].
  *   codes, pairs  device out, 16-byte aligned, sizes as above; every byte is written.
- * Errors: INVALID_ARG, UNSUPPORTED (dtype, group), CUDA. */
+ * Errors: INVALID_ARG, UNSUPPORTED (dtype, group, N above 65535 * 16), CUDA. */
 coreinfer_status coreinfer_w4_quantize(const void* w, coreinfer_dtype dtype, int32_t N, int32_t K,
                                        int64_t stride_n, int64_t stride_k, int32_t group,
                                        void* codes, void* pairs, void* cuda_stream);
@@ -447,7 +447,8 @@ coreinfer_status coreinfer_w4_matvec(const coreinfer_w4_matrix* w, const void* x
  *   state             [batch][4] int32: slots in use, tokens ever appended, tokens refused because
  *                     they did not fit, scratch.  All zero = empty; zero it to start new sequences.
  * head_dim is 64, 128 or 256, group 32, 64 or 128 and at most head_dim, capacity a multiple of 16,
- * batch at most COREINFER_KV4_MAX_BATCH.  Slots beyond the first `state[b][0]` may hold anything. */
+ * batch at most COREINFER_KV4_MAX_BATCH, kv_heads at most 1024 (otherwise UNSUPPORTED).  Slots beyond the first
+ * `state[b][0]` may hold anything. */
 #define COREINFER_KV4_MAX_BATCH 1024
 #define COREINFER_KV4_MAX_QUERIES 16
 
@@ -475,7 +476,7 @@ typedef struct {
  *   k_stored, v_stored  device out [batch][T][kv_heads][head_dim] in `dtype` (16-byte aligned), the values
  *            as the cache now holds them (x^ rounded to dtype), or both NULL.  Written for refused
  *            tokens too.
- * Errors: INVALID_ARG, UNSUPPORTED (head_dim, group, dtype, batch), CUDA. */
+ * Errors: INVALID_ARG, UNSUPPORTED (head_dim, group, dtype, batch, T * kv_heads above 2^29), CUDA. */
 coreinfer_status coreinfer_kv4_append(const coreinfer_kv4_cache* cache, const void* k, const void* v,
                                       coreinfer_dtype dtype, int32_t T, int64_t ld_token,
                                       void* k_stored, void* v_stored, void* cuda_stream);
@@ -490,7 +491,8 @@ coreinfer_status coreinfer_kv4_append(const coreinfer_kv4_cache* cache, const vo
  *   q        device, token t of sequence b at (b * T + t) * ld_q, [q_heads][head_dim] contiguous, in
  *            `dtype`; 16-byte aligned, ld_q * element size a multiple of 16.  out likewise with ld_out.
  *   workspace  device, 16-byte aligned, at least coreinfer_kv4_attention_workspace_bytes() (0 on bad sizes)
- * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, CUDA. */
+ * Errors: INVALID_ARG, UNSUPPORTED (as for append; more than 2048 query rows T * q_heads / kv_heads per key head; 2^32
+ * slots batch * kv_heads * capacity or more), WORKSPACE, CUDA. */
 size_t coreinfer_kv4_attention_workspace_bytes(const coreinfer_kv4_cache* cache, int32_t q_heads, int32_t T);
 
 coreinfer_status coreinfer_kv4_attention(const coreinfer_kv4_cache* cache, const void* q, coreinfer_dtype dtype,
@@ -507,7 +509,7 @@ coreinfer_status coreinfer_kv4_attention(const coreinfer_kv4_cache* cache, const
  *     src capacity): the kept slots are copied in ascending slot order; src is not changed; slots of
  *     dst beyond the new length are not written.
  *   state[b][0] of dst becomes the new length, state[b][1] is taken over.
- * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, CUDA. */
+ * Errors: INVALID_ARG, UNSUPPORTED (as for append; batch * kv_heads above 65535), WORKSPACE, CUDA. */
 size_t coreinfer_kv4_evict_workspace_bytes(const coreinfer_kv4_cache* src);
 
 coreinfer_status coreinfer_kv4_evict(const coreinfer_kv4_cache* src, const coreinfer_kv4_cache* dst,

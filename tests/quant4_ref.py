@@ -43,6 +43,15 @@ def dequantise(codes, s, o):
     return codes.astype(np.float64) * np.repeat(s.astype(np.float64), rep, -1) + np.repeat(o.astype(np.float64), rep, -1)
 
 
+def unpack_cache(codes, pairs):
+    """64-bit values of cache buffers: codes bytes [..., d / 2], pairs fp16 [..., d / group, 2] (tensors)."""
+    b, p = codes.cpu().numpy(), pairs.cpu().numpy()
+    d = 2 * b.shape[-1]
+    v = np.arange(d)
+    byte = 2 * (((v % 32) // 4) * (d // 32) + v // 32) + (v % 4) // 2
+    return dequantise((b[..., byte] >> (4 * (v % 2))) & 15, p[..., 0], p[..., 1])
+
+
 def pairs_array(s, o):
     return np.stack((s, o), -1)
 
