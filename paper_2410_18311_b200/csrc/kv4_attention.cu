@@ -38,7 +38,7 @@ constexpr int kAttnWarps = 8;
 constexpr int kAttnThreads = 32 * kAttnWarps;
 // Slots per tile (a piece per warp): pieces of 32, so that waits, votes and addresses are paid once per 32 slots; of 16
 // where registers (head_dim 128 in groups of 32) or shared memory (256) do not carry two.
-template <int D, int G> constexpr int kAttnTile = D == 256 || (D == 128 && G == 32) ? 128 : 256;
+template <int D, int G, int MODE> constexpr int kAttnTile = MODE == 3 || D == 256 || (D == 128 && G == 32) ? 128 : 256;
 constexpr int kAttnMaxCtas = 320;
 constexpr float kNoLogit = -1e30f;
 // A unit counts this many tiles more than it has when the list is cut: about what starting it costs a CTA (its query
@@ -130,6 +130,9 @@ __device__ __forceinline__ uint32_t centred(uint32_t x, uint32_t mask, uint32_t 
     return *reinterpret_cast<const uint32_t*>(&r);
 }
 
+__device__ __forceinline__ __half2 as_half2(uint32_t w) { return *reinterpret_cast<const __half2*>(&w); }
+__device__ __forceinline__ uint32_t as_word(__half2 h) { return *reinterpret_cast<const uint32_t*>(&h); }
+
 // A condition that is rarely true and the same for the warp: used as the bound of a loop of at most one round, so that
 // the compiler branches around the body instead of executing it under a predicate.
 __device__ __forceinline__ int opaque_zero()
@@ -145,7 +148,12 @@ template <int MODE> constexpr int kAttnCentre = MODE == 2 ? 2 : 8;
 
 // Stages of a warp's ring: as many as two CTAs per SM (head_dim 256: one) leave room for.
 template <int D, int G, int MODE> constexpr int kAttnStages =
-    D == 64 ? 9 : (D == 256 ? (G == 32 ? 6 : 8) : (G == 32 ? (MODE == 0 ? 7 : 9) : (MODE == 0 ? 4 : 5)));
+    MODE == 3 ? (D == 64 ? 10 : 6) : D == 64 ? 9 : (D == 256 ? (G == 32 ? 6 : 8) : (G == 32 ? (MODE == 0 ? 7 : 9) : (MODE == 0 ? 4 : 5)));
+
+// How far a logit (base 2) may exceed the running maximum before that is moved.  Rows change their maximum at different
+// pieces, and each change rescales all of a warp's outputs: of 15 rows, nearly every piece did (91 of 1100
+// instructions a piece).
+template <int MODE> constexpr float kAttnRoom = MODE == 3 ? 6.f : 4.f;
 
 // Position in the list of tiles.
 struct Cursor {
@@ -154,14 +162,23 @@ struct Cursor {
 
 // How query rows sit in the 8 columns of an MMA: a row per column; a row per two columns with the second empty
 // (up to 4 rows: half the softmax work per lane); a row per two columns, the second for the low part.
-enum { kRows8 = 0, kRows4 = 1, kRows4Parts = 2 };
+// kRows16: two MMAs of eight columns side by side, so that a warp unpacks the codes once for 16 rows.
+enum { kRows8 = 0, kRows4 = 1, kRows4Parts = 2, kRows16 = 3 };
+// A warp's query rows, and those that the join takes at a time.
+template <int MODE> constexpr int kAttnRows = MODE == kRows16 ? 16 : (MODE == kRows8 ? 8 : 4);
+template <int MODE> constexpr int kAttnJoinRows = MODE == kRows8 || MODE == kRows16 ? 8 : 4;
+// Query rows of kRows16 in shared memory, per row tile of a CTA: fragments of two MMAs, those of the sums over groups, and
+// (factor, slots seen) of each row.
+template <int D> constexpr int kAttnQueryBytes = 2 * (D / 32) * 512 + 2 * 256 + 16 * 8;
 
 template <typename T, int D, int G, int MODE>
 __global__ void __launch_bounds__(kAttnThreads, D <= 128 ? 2 : 1)
 kv4_attention_kernel(const __grid_constant__ AttnArgs a)
 {
-    constexpr bool PARTS = MODE == kRows4Parts, WIDE = MODE != kRows8, CENTRED = sizeof(T) == 4;
-    constexpr int H32 = D / 32, NG = D / G, RPT = WIDE ? 4 : 8, NV = WIDE ? 1 : 2, TILE = kAttnTile<D, G>;
+    constexpr bool PARTS = MODE == kRows4Parts, BOTH = MODE == kRows16, WIDE = MODE == kRows4 || PARTS, CENTRED = sizeof(T) == 4;
+    constexpr int H32 = D / 32, NG = D / G, RPT = kAttnRows<MODE>, JOIN = kAttnJoinRows<MODE>, TL = RPT / JOIN;
+    constexpr int NV = BOTH ? 4 : (WIDE ? 1 : 2);            // query rows whose logits a lane holds: 2 tig + (i & 1) of MMA i >> 1
+    constexpr int TILE = kAttnTile<D, G, MODE>;
     constexpr int UN = TILE / (16 * kAttnWarps);             // pieces of 16 slots per step of a warp
     constexpr uint32_t CODE_ROW = D / 2, PAIR_ROW = NG * 4;
     constexpr int CH = 16 * UN;                              // slots of a piece
@@ -171,9 +188,11 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
     const Kv4& c = a.c;
 
     extern __shared__ __align__(128) uint8_t smem[];
-    float* obuf = reinterpret_cast<float*>(smem + (size_t)kAttnWarps * STAGES * STAGE);                // [8 warps][RPT][D]
-    float2* mlbuf = reinterpret_cast<float2*>(obuf + kAttnWarps * RPT * D);                  // [8 warps][RPT]
-    int* pre = reinterpret_cast<int*>(mlbuf + kAttnWarps * RPT);                             // [B + 1] entries of a head before sequence b
+    float* obuf = reinterpret_cast<float*>(smem + (size_t)kAttnWarps * STAGES * STAGE);                // [8 warps][JOIN][D]
+    float2* mlbuf = reinterpret_cast<float2*>(obuf + kAttnWarps * JOIN * D);                 // [8 warps][JOIN]
+    float2* slot_power = mlbuf + kAttnWarps * JOIN + (BOTH ? warp_number() * 16 : 0);        // kRows16: [8 warps][16] (k, 2^-k)
+    uint8_t* queries = reinterpret_cast<uint8_t*>(mlbuf + kAttnWarps * (JOIN + (BOTH ? 16 : 0)));          // [RT][kAttnQueryBytes]
+    int* pre = reinterpret_cast<int*>(queries + (BOTH ? a.RT * kAttnQueryBytes<D> : 0));     // [B + 1] entries of a head before sequence b
     int* tiles_before = pre + c.B + 1;                                                       // [B] tiles of a head before sequence b
     int* lens = tiles_before + c.B;                                                          // [B]
     const int tid = threadIdx.x, warp = warp_number(), lane = tid & 31;
@@ -256,7 +275,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
         uint4 raw[H32][sizeof(T) / 2];                       // query rows of the unit at hand as they are in memory
         auto load_q = [&](const Cursor& k) {
             const int h = a.RB == 1 ? k.hr : k.hr / a.RB, rb = k.hr - h * a.RB;
-            const int r = rb * a.RU + rt * RPT + (WIDE ? gid >> 1 : gid);
+            const int r = rb * a.RU + rt * RPT + (WIDE ? gid >> 1 : (BOTH ? (sg & 1) * 8 : 0) + gid);
             const int rr = r < a.R && (MODE != kRows4 || (gid & 1) == 0) ? r : 0, rt_ = token_of(rr);
             const T* src = (const T*)a.q + ((long long)k.b * a.T + rt_) * a.ld_q + (long long)(h * a.share + rr - rt_ * a.share) * D + 8 * tig;
 #pragma unroll
@@ -342,10 +361,63 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
             }
 
             // query rows as the B operand: column gid = row gid (or part gid & 1 of row gid >> 1), 8 values per 32
-            uint32_t qf[H32][4];
-            float qsum[NG][NV], f[NV];
-            int lim[NV];                                     // slots this lane's columns see
-            {
+            uint32_t qf[BOTH ? 1 : H32][4];
+            float qsum[BOTH ? 1 : NG][NV], f[BOTH ? 1 : NV];
+            int lim[BOTH ? 1 : NV] = {};                     // slots this lane's columns see
+            uint8_t* const mine = queries + (BOTH ? rt * kAttnQueryBytes<D> : 0);
+            const uint4* const q_frag = reinterpret_cast<const uint4*>(mine) + lane;
+            const uint2* const q_sums = reinterpret_cast<const uint2*>(mine + TL * H32 * 512) + lane;
+            const float2* const q_row = reinterpret_cast<const float2*>(mine + TL * (H32 * 512 + 256)) + 2 * tig;
+            if constexpr (BOTH) {
+                // The first two warps of a row tile lay it out, eight rows each: values below 2^6, so that sums over groups
+                // are in fp16's range, as two parts.  (bf16 has eight bits: what falls below 2^-24 is 2^-30 of the row.)
+                if (sg < 2) {
+                    const bool valid = row0 + sg * 8 + gid < a.R;
+                    float v[H32][8], m = 0.f, sum[NG];
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) sum[g] = 0.f;
+#pragma unroll
+                    for (int j = 0; j < H32; ++j) {
+                        unpack8<T>(raw[j], v[j]);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            if (!valid) v[j][e] = 0.f;
+                            m = fmaxf(m, fabsf(v[j][e]));
+                        }
+                    }
+                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
+                    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
+                    const int x = range_exponent(m);
+                    const float up = pow2(6 - x), lo16 = 1.f / 16.f;
+#pragma unroll
+                    for (int j = 0; j < H32; ++j)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            v[j][e] *= up;
+                            sum[j * 32 / G] += v[j][e];
+                        }
+#pragma unroll
+                    for (int j = 0; j < H32; ++j) {
+                        const float *p = G == 32 ? &v[j][0] : &v[j & ~1][(j & 1) * 4], *q = G == 32 ? &v[j][4] : &v[j | 1][(j & 1) * 4];
+                        reinterpret_cast<uint4*>(mine)[(sg * H32 + j) * 32 + lane] =
+                            make_uint4(pack_half2(p[0], q[0]), pack_half2(p[2], q[2]), pack_half2(p[1] * lo16, q[1] * lo16), pack_half2(p[3] * lo16, q[3] * lo16));
+                    }
+                    float here[2] = {0.f, 0.f};              // sums over groups 2 tig and 2 tig + 1
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) {
+                        sum[g] += __shfl_xor_sync(0xffffffffu, sum[g], 1);
+                        sum[g] += __shfl_xor_sync(0xffffffffu, sum[g], 2);
+                        if (tig == g / 2) here[g & 1] = sum[g];
+                    }
+                    const float h0 = __half2float(__float2half_rn(here[0])), h1 = __half2float(__float2half_rn(here[1]));
+                    reinterpret_cast<uint2*>(mine + TL * H32 * 512)[sg * 32 + lane] = make_uint2(pack_half2(h0, h1), pack_half2(here[0] - h0, here[1] - h1));
+                    const int rr = row0 + sg * 8 + gid;
+                    if (tig == 0)
+                        reinterpret_cast<float2*>(mine + TL * (H32 * 512 + 256))[sg * 8 + gid] =
+                            make_float2(ldexpf(a.scale * 1.44269504088896341f, x - 6 + 24), __int_as_float(valid ? len - (a.T - 1 - token_of(rr)) : 0));
+                }
+                __syncthreads();
+            } else {
                 const bool valid = row0 + (WIDE ? gid >> 1 : gid) < a.R && (MODE != kRows4 || (gid & 1) == 0);
                 float v[H32][8], m = 0.f;
 #pragma unroll
@@ -400,29 +472,31 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                     lim[i] = rr < a.R ? len - (a.T - 1 - token_of(rr)) : 0;
                 }
             }
-            float* lg[NV];                                   // this lane's logits, NULL where none are kept
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int rr = row0 + (WIDE ? tig : 2 * tig + i);
-                lg[i] = a.accumulate && rr < a.R ? a.logits + (((size_t)b * c.H + h) * a.R + rr) * c.cap + tok0 : nullptr;
-            }
+            auto sees = [&](int i) { return BOTH ? __float_as_int(q_row[(i >> 1) * 8 + (i & 1)].y) : lim[BOTH ? 0 : i]; };
+            auto row_of = [&](int i) { return row0 + (WIDE ? tig : (i >> 1) * 8 + 2 * tig + (i & 1)); };
+            // this lane's logits of its first row; row_of(i) - row_of(0) rows further on the others'
+            float* const lg = a.logits + (((size_t)b * c.H + h) * a.R + row_of(0)) * c.cap + tok0;
             const int all_see = len - (a.T - 1);             // slots below this are seen by every row
 
-            float o[H32][2][4], om[NG][NV], sum_ps[NG][NV], l[NV], mx[NV];
+            float o[TL][H32][2][4], om[BOTH ? 1 : NG][NV], sum_ps[BOTH ? 1 : NG][NV], l[NV], mx[NV];
             int centre = kAttnCentre<MODE>;
-            // The weights enter the second product as p s 2^E in fp16: E keeps the largest s near 2^9, so
+            // p is relative to mx, which is moved only when a logit exceeds it by kAttnRoom: p may reach 2^kAttnRoom.
+            // The weights enter the second product as p s 2^E in fp16: E keeps the largest s near 2^8 (2^11 at most), so
             // that p s neither overflows nor loses bits to fp16's bottom for p down to about 2^-20.
-            float E = 0.f, s_most = -1.f;
+            // kRows16 follows p 2^k instead, 2^k the power of a slot's values: 2^(8 + 6) at most.
+            float E = BOTH ? 8.f : 0.f, s_most = -1.f;
 #pragma unroll
-            for (int j = 0; j < H32; ++j)
+            for (int tl = 0; tl < TL; ++tl)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[j][0][e] = o[j][1][e] = 0.f;
+                for (int j = 0; j < H32; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[tl][j][0][e] = o[tl][j][1][e] = 0.f;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 l[i] = 0.f;
                 mx[i] = kNoLogit;
 #pragma unroll
-                for (int g = 0; g < NG; ++g) om[g][i] = sum_ps[g][i] = 0.f;
+                for (int g = 0; g < (BOTH ? 1 : NG); ++g) om[g][i] = sum_ps[g][i] = 0.f;
             }
 
             const int seg_end = (first_tile + n_tiles) * TILE < len ? (first_tile + n_tiles) * TILE : len;
@@ -439,6 +513,57 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                         __syncwarp();
                     }
                     float lo[UN][2][NV];
+                    if constexpr (BOTH) {
+                        static_assert(!BOTH || UN == 1, "one piece of 16 slots at a time");
+                        const uint8_t *krow = kst + tok0 * CODE_ROW + tig * (D / 8), *kpr = kst + CODES + tok0 * PAIR_ROW;
+                        uint32_t w0[D / 32], w1[D / 32], kp0[NG], kp1[NG];
+                        ld_words<D / 32>(w0, krow);
+                        ld_words<D / 32>(w1, krow + 8 * CODE_ROW);
+                        ld_words<NG>(kp0, kpr);
+                        ld_words<NG>(kp1, kpr + 8 * PAIR_ROW);
+                        // o_g sum q of all groups in one MMA: offsets of groups 2 tig and 2 tig + 1 against the sums' two parts
+                        uint32_t o0 = 0u, o1 = 0u;
+                        if (NG == 1) {
+                            o0 = tig == 0 ? kp0[0] >> 16 : 0u;
+                            o1 = tig == 0 ? kp1[0] >> 16 : 0u;
+                        } else if (2 * tig < NG) {
+                            const uint2 p0 = *reinterpret_cast<const uint2*>(kpr + 8 * tig), p1 = *reinterpret_cast<const uint2*>(kpr + 8 * PAIR_ROW + 8 * tig);
+                            o0 = __byte_perm(p0.x, p0.y, 0x7632);
+                            o1 = __byte_perm(p1.x, p1.y, 0x7632);
+                        }
+#pragma unroll
+                        for (int tl = 0; tl < TL; ++tl) {
+                            float off[4];
+                            const uint2 sums = q_sums[tl * 32];
+                            mma_16816_zero(off, o0, o1, o0, o1, sums.x, sums.y);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) lo[0][e >> 1][2 * tl + (e & 1)] = off[e] * (1.f / kCodeScaleLow);
+                        }
+#pragma unroll
+                        for (int g = 0; g < NG; ++g) {
+                            float acc[TL][4];
+#pragma unroll
+                            for (int j = g * G / 32; j < (g + 1) * G / 32; ++j) {
+                                const uint32_t x0 = code_word<G, H32>(w0, j), x1 = code_word<G, H32>(w1, j);
+                                const uint32_t y0 = x0 >> 8, y1 = x1 >> 8;
+                                const uint32_t e0 = x0 & 0x000f000fu, e1 = x1 & 0x000f000fu, e2 = y0 & 0x000f000fu, e3 = y1 & 0x000f000fu;
+                                const uint32_t d0 = x0 & 0x00f000f0u, d1 = x1 & 0x00f000f0u, d2 = y0 & 0x00f000f0u, d3 = y1 & 0x00f000f0u;
+#pragma unroll
+                                for (int tl = 0; tl < TL; ++tl) {
+                                    const uint4 q = q_frag[(tl * H32 + j) * 32];
+                                    if (j == g * G / 32) mma_16816_zero(acc[tl], e0, e1, e2, e3, q.x, q.y);
+                                    else mma_16816(acc[tl], e0, e1, e2, e3, q.x, q.y);
+                                    mma_16816(acc[tl], d0, d1, d2, d3, q.z, q.w);
+                                }
+                            }
+                            const float s0 = pair_f32(kp0[g]).x, s1 = pair_f32(kp1[g]).x;
+#pragma unroll
+                            for (int i = 0; i < NV; ++i) {
+                                lo[0][0][i] = fmaf(s0, acc[i >> 1][i & 1], lo[0][0][i]);
+                                lo[0][1][i] = fmaf(s1, acc[i >> 1][2 + (i & 1)], lo[0][1][i]);
+                            }
+                        }
+                    } else
 #pragma unroll
                     for (int u = 0; u < UN; ++u) {
                         const uint8_t* krow = kst + (u * 16 + tok0) * CODE_ROW + tig * (D / 8);
@@ -485,21 +610,21 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
 #pragma unroll
                         for (int u = 0; u < UN; ++u)
 #pragma unroll
-                            for (int v = 0; v < 2; ++v) lo[u][v][i] *= f[i];
+                            for (int v = 0; v < 2; ++v) lo[u][v][i] *= BOTH ? q_row[(i >> 1) * 8 + (i & 1)].x : f[BOTH ? 0 : i];
 #pragma unroll 1
                         for (int e = edge; e; e = opaque_zero()) {
 #pragma unroll
                             for (int u = 0; u < UN; ++u)
 #pragma unroll
                                 for (int v = 0; v < 2; ++v)
-                                    if (na + 16 * u + 8 * v >= lim[i]) lo[u][v][i] = -__int_as_float(0x7f800000);
+                                    if (na + 16 * u + 8 * v >= sees(i)) lo[u][v][i] = -__int_as_float(0x7f800000);
                         }
                         most[i] = fmaxf(lo[0][0][i], lo[0][1][i]);
 #pragma unroll
                         for (int u = 1; u < UN; ++u) most[i] = fmaxf(most[i], fmaxf(lo[u][0][i], lo[u][1][i]));
-                        if (lg[i]) {
+                        if (a.accumulate && row_of(i) < a.R) {
                             // what a row does not see may be written too: it lies within the capacity and is never read
-                            float* to = lg[i] + n0;
+                            float* to = lg + (size_t)(row_of(i) - row_of(0)) * c.cap + n0;
 #pragma unroll
                             for (int u = 0; u < UN; ++u)
                                 if (UN == 1 || u == 0 || n0 + 16 < len) {
@@ -513,6 +638,70 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                     // ---- value pairs, running maximum ----
                     uint32_t vp[UN][2][NG];
                     __half2 smax = __float2half2_rn(0.f);
+                    float down[2] = {1.f, 1.f};
+                    if constexpr (BOTH) {
+                        uint32_t* const pairs = reinterpret_cast<uint32_t*>(vst + CODES);
+                        auto is_nan = [](uint32_t w) { return (w & 0x7fffu) > 0x7c00u || (w & 0x7fff0000u) > 0x7c000000u; };
+#pragma unroll 1
+                        for (int e = edge; e; e = opaque_zero()) {
+                            // Slots beyond the sequence count for nothing.  A NaN in a slot that some rows do not see goes to the
+                            // outputs of those that do here, and not through the MMA, where it would reach all.
+                            for (int i0 = 0; i0 < CH * NG; i0 += 32) {
+                                const int i = i0 + lane, n = n0 + i / NG;
+                                const uint32_t w = i < CH * NG ? pairs[i] : 0u;
+                                const bool bad = i < CH * NG && n >= all_see && n < len && is_nan(w);
+                                if (i < CH * NG && (n >= len || bad)) pairs[i] = 0u;
+                                for (unsigned left = __ballot_sync(0xffffffffu, bad); left; left &= left - 1u) {
+                                    const int at = i0 + __ffs(left) - 1;
+#pragma unroll
+                                    for (int r = 0; r < NV; ++r) {
+                                        const bool seen = n0 + at / NG < sees(r);
+#pragma unroll
+                                        for (int j = 0; j < H32; ++j) {
+                                            const float more = seen && j * 32 / G == at % NG ? __int_as_float(0x7fffffff) : 0.f;
+#pragma unroll
+                                            for (int d = 0; d < 4; ++d) o[r >> 1][j][d >> 1][2 * (d & 1) + (r & 1)] += more;
+                                        }
+                                    }
+                                }
+                            }
+                            __syncwarp();
+                        }
+                        // Every slot's pairs to a power of two: the largest s or |o| into [2^6, 2^7), so that 16 |s c + o| stays
+                        // below 2^15; p takes the power, and its reference follows p 2^k.  A lane per half a slot.
+                        constexpr int PER = NG > 1 ? 2 : 1, WORDS = NG / PER;
+                        const int slot = lane / PER;
+                        if (PER == 2 || lane < 16) {
+                            uint32_t w[WORDS];
+                            uint32_t* const at = pairs + slot * NG + (PER == 2 ? (lane & 1) * WORDS : 0);
+                            ld_words<WORDS>(w, reinterpret_cast<const uint8_t*>(at));
+                            __half2 m = __habs2(as_half2(w[0]));
+#pragma unroll
+                            for (int i = 1; i < WORDS; ++i) m = __hmax2(m, __habs2(as_half2(w[i])));
+                            uint32_t bits = as_word(m) & 0xffffu;
+                            bits = bits > as_word(m) >> 16 ? bits : as_word(m) >> 16;
+                            if (PER == 2) {
+                                const uint32_t other = __shfl_xor_sync(0xffffffffu, bits, 1);
+                                bits = bits > other ? bits : other;
+                            }
+                            int e = (int)(bits >> 10);       // its exponent + 15; a NaN counts as nothing
+                            e = e == 31 || e < 6 ? 6 : e;
+                            const uint32_t factor = (uint32_t)(36 - e) * 0x04000400u;        // 2^(21 - e) twice
+#pragma unroll
+                            for (int i = 0; i < WORDS; ++i) at[i] = as_word(__hmul2(as_half2(w[i]), as_half2(factor)));
+                            if (PER == 1 || (lane & 1) == 0) slot_power[slot] = make_float2((float)(e - 14), pow2(14 - e));
+                        }
+                        __syncwarp();
+                        const float2 power[2] = {slot_power[tok0], slot_power[tok0 + 8]};
+#pragma unroll
+                        for (int i = 0; i < NV; ++i) {
+                            lo[0][0][i] += power[0].x;
+                            lo[0][1][i] += power[1].x;
+                            most[i] = fmaxf(lo[0][0][i], lo[0][1][i]);
+                        }
+                        down[0] = power[0].y;
+                        down[1] = power[1].y;
+                    } else {
 #pragma unroll
                     for (int u = 0; u < UN; ++u)
 #pragma unroll
@@ -538,20 +727,21 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                                     smax = __hmax2(smax, *reinterpret_cast<const __half2*>(&vp[u][v][g]));
                                 }
                     }
-                    float s_here = __low2float(smax);
+                    }
+                    float s_here = BOTH ? -2.f : __low2float(smax);
                     bool change = s_here > s_most;
 #pragma unroll
-                    for (int i = 0; i < NV; ++i) change |= most[i] > mx[i];
+                    for (int i = 0; i < NV; ++i) change |= most[i] > mx[i] + kAttnRoom<MODE>;
                     if (__any_sync(0xffffffffu, change)) {
                         float e_new = E;
-                        if (__any_sync(0xffffffffu, s_here > s_most)) {
+                        if (!BOTH && __any_sync(0xffffffffu, s_here > s_most)) {
 #pragma unroll
                             for (int d = 1; d < 32; d <<= 1) s_here = fmaxf(s_here, __shfl_xor_sync(0xffffffffu, s_here, d));
                             int x;
                             frexpf(s_here, &x);
                             x = s_here > 0.f ? (x < -15 ? -15 : x) : -15;
-                            e_new = (float)(9 - x);
-                            s_most = ldexpf(1.f, x + 5);     // room for scales up to 32 times larger before E moves
+                            e_new = (float)(8 - x);
+                            s_most = ldexpf(1.f, x + 3);     // room for scales up to 8 times larger before E moves
                         }
 #pragma unroll
                         for (int i = 0; i < NV; ++i) {
@@ -559,12 +749,13 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
                             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
                             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+                            if (BOTH) m = ceilf(m);          // a whole number, as k is: their difference is exact
                             m = fmaxf(m, mx[i]);
                             const float corr = exp2_fast((mx[i] - E) - (m - e_new));
                             mx[i] = m;
                             l[i] *= corr;
 #pragma unroll
-                            for (int g = 0; g < NG; ++g) {
+                            for (int g = 0; g < (BOTH ? 1 : NG); ++g) {
                                 om[g][i] *= corr;
                                 sum_ps[g][i] *= corr;
                             }
@@ -572,11 +763,11 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                             for (int j = 0; j < H32; ++j)
 #pragma unroll
                                 for (int e = 0; e < 2; ++e) {
-                                    o[j][e][i] *= corr;
-                                    o[j][e][2 + i] *= corr;
+                                    o[i >> 1][j][e][i & 1] *= corr;
+                                    o[i >> 1][j][e][2 + (i & 1)] *= corr;
                                     if (PARTS) {
-                                        o[j][e][1] *= corr;
-                                        o[j][e][3] *= corr;
+                                        o[0][j][e][1] *= corr;
+                                        o[0][j][e][3] *= corr;
                                     }
                                 }
                         }
@@ -590,10 +781,53 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
 #pragma unroll
                             for (int v = 0; v < 2; ++v) {
                                 lo[u][v][i] = exp2_fast(lo[u][v][i] - ref);          // p from here on
-                                l[i] += lo[u][v][i];
+                                l[i] = BOTH ? fmaf(lo[u][v][i], down[v], l[i]) : l[i] + lo[u][v][i];
                             }
                     }
                     // ---- O^T += V^T P^T, per group of scales ----
+                    if constexpr (BOTH) {
+                        uint32_t bf[TL][2];
+#pragma unroll
+                        for (int tl = 0; tl < TL; ++tl)
+#pragma unroll
+                            for (int v = 0; v < 2; ++v) bf[tl][v] = movmatrix_trans(pack_half2(lo[0][v][2 * tl], lo[0][v][2 * tl + 1]));
+                        const uint8_t *vrow = vst + tig * CODE_ROW + gid * (D / 16), *vpr = vst + CODES + tig * PAIR_ROW;
+                        uint32_t va[H32 / 2], vb[H32 / 2], vc[H32 / 2], vd[H32 / 2];
+                        ld_words<H32 / 2>(va, vrow);
+                        ld_words<H32 / 2>(vb, vrow + 4 * CODE_ROW);
+                        ld_words<H32 / 2>(vc, vrow + 8 * CODE_ROW);
+                        ld_words<H32 / 2>(vd, vrow + 12 * CODE_ROW);
+#pragma unroll
+                        for (int g = 0; g < NG; ++g) {
+                            // the slots of an entry pair: tig and tig + 4, tig + 8 and tig + 12
+                            uint32_t pr[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) pr[e] = *reinterpret_cast<const uint32_t*>(vpr + 4 * e * PAIR_ROW + 4 * g);
+                            __half2 sc[2], even[2], odd[2];
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                sc[e] = as_half2(__byte_perm(pr[2 * e], pr[2 * e + 1], 0x5410));
+                                even[e] = __hfma2(sc[e], __float2half2_rn(8.f), as_half2(__byte_perm(pr[2 * e], pr[2 * e + 1], 0x7632)));
+                                odd[e] = __hmul2(even[e], __float2half2_rn(16.f));
+                            }
+                            auto value = [&](uint32_t x, int e) { return as_word(__hfma2(as_half2(centred(x, 0x000f000fu, 0x64086408u)), sc[e], even[e])); };
+                            auto value16 = [&](uint32_t x, int e) { return as_word(__hfma2(as_half2(centred(x, 0x00f000f0u, 0x64806480u)), sc[e], odd[e])); };
+#pragma unroll
+                            for (int j = g * G / 32; j < (g + 1) * G / 32; ++j) {
+                                const uint32_t x = __byte_perm(va[j / 2], vb[j / 2], j & 1 ? 0x7632 : 0x5410);
+                                const uint32_t y = __byte_perm(vc[j / 2], vd[j / 2], j & 1 ? 0x7632 : 0x5410);
+                                const uint32_t x8 = x >> 8, y8 = y >> 8;
+                                {
+                                    const uint32_t a0 = value(x, 0), a1 = value(x8, 0), a2 = value(y, 1), a3 = value(y8, 1);
+#pragma unroll
+                                    for (int tl = 0; tl < TL; ++tl) mma_16816(o[tl][j][0], a0, a1, a2, a3, bf[tl][0], bf[tl][1]);
+                                }
+                                const uint32_t a0 = value16(x, 0), a1 = value16(x8, 0), a2 = value16(y, 1), a3 = value16(y8, 1);
+#pragma unroll
+                                for (int tl = 0; tl < TL; ++tl) mma_16816(o[tl][j][1], a0, a1, a2, a3, bf[tl][0], bf[tl][1]);
+                            }
+                        }
+                    } else
 #pragma unroll
                     for (int u = 0; u < UN; ++u) {
                         const uint8_t* vrow = vst + (u * 16 + tig) * CODE_ROW + gid * (D / 16);
@@ -628,7 +862,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                                 for (int i = 0; i < NV; ++i)
                                     if (!CENTRED) sum_ps[g][i] += ps[i];
                                 if (PARTS) {
-                                    const float high = __half2float(__float2half_rn(CENTRED ? round_to(ps[0], .5f) : ps[0]));
+                                    const float high = __half2float(__float2half_rn(CENTRED ? round_to(ps[0], .25f) : ps[0]));
                                     bf[v] = movmatrix_trans(pack_half2(high, ps[0] - high));
                                 } else {
                                     bf[v] = movmatrix_trans(pack_half2(ps[0], WIDE ? 0.f : ps[NV - 1]));
@@ -640,20 +874,20 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                                 const uint32_t y = __byte_perm(vc[j / 2], vd[j / 2], j & 1 ? 0x7632 : 0x5410);
                                 const uint32_t x8 = x >> 8, y8 = y >> 8;
                                 if (CENTRED) {
-                                    mma_16816(o[j][0], centred(x, 0x000f000fu, 0x64086408u), centred(x8, 0x000f000fu, 0x64086408u),
+                                    mma_16816(o[0][j][0], centred(x, 0x000f000fu, 0x64086408u), centred(x8, 0x000f000fu, 0x64086408u),
                                               centred(y, 0x000f000fu, 0x64086408u), centred(y8, 0x000f000fu, 0x64086408u), bf[0], bf[1]);
-                                    mma_16816(o[j][1], centred(x, 0x00f000f0u, 0x64806480u), centred(x8, 0x00f000f0u, 0x64806480u),
+                                    mma_16816(o[0][j][1], centred(x, 0x00f000f0u, 0x64806480u), centred(x8, 0x00f000f0u, 0x64806480u),
                                               centred(y, 0x00f000f0u, 0x64806480u), centred(y8, 0x00f000f0u, 0x64806480u), bf[0], bf[1]);
                                 } else {
-                                    mma_16816(o[j][0], x & 0x000f000fu, x8 & 0x000f000fu, y & 0x000f000fu, y8 & 0x000f000fu, bf[0], bf[1]);
-                                    mma_16816(o[j][1], x & 0x00f000f0u, x8 & 0x00f000f0u, y & 0x00f000f0u, y8 & 0x00f000f0u, bf[0], bf[1]);
+                                    mma_16816(o[0][j][0], x & 0x000f000fu, x8 & 0x000f000fu, y & 0x000f000fu, y8 & 0x000f000fu, bf[0], bf[1]);
+                                    mma_16816(o[0][j][1], x & 0x00f000f0u, x8 & 0x00f000f0u, y & 0x00f000f0u, y8 & 0x00f000f0u, bf[0], bf[1]);
                                 }
                             }
                         }
                     }
                 }
                 leave(1);
-                if (!CENTRED && --centre == 0) {
+                if (!CENTRED && !BOTH && --centre == 0) {
                     centre = kAttnCentre<MODE>;
 #pragma unroll
                     for (int g = 0; g < NG; ++g) {
@@ -668,86 +902,107 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                         const uint32_t b0 = movmatrix_trans(pack_half2(take[0], WIDE ? 0.f : take[NV - 1]));
 #pragma unroll
                         for (int j = g * G / 32; j < (g + 1) * G / 32; ++j) {
-                            mma_16816(o[j][0], 0x80088008u, 0x80088008u, 0x80088008u, 0x80088008u, b0, 0u);
-                            mma_16816(o[j][1], 0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u, b0, 0u);
+                            mma_16816(o[0][j][0], 0x80088008u, 0x80088008u, 0x80088008u, 0x80088008u, b0, 0u);
+                            mma_16816(o[0][j][1], 0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u, b0, 0u);
                         }
                     }
                 }
             }
 
-            // ---- join the warps of a row tile ----
-            __syncthreads();                                 // the buffer's last use is over
+            // ---- join the warps of a row tile, JOIN rows of it at a time ----
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) {
                     l[i] += __shfl_xor_sync(0xffffffffu, l[i], d);
 #pragma unroll
-                    for (int g = 0; g < NG; ++g) om[g][i] += __shfl_xor_sync(0xffffffffu, om[g][i], d);
-                }
-                const int r = WIDE ? tig : 2 * tig + i;
-                if (gid == 0) mlbuf[warp * RPT + r] = make_float2(mx[i] - E, l[i]);
-#pragma unroll
-                for (int j = 0; j < H32; ++j) {
-                    const float add = om[j * 32 / G][i];
-                    float4 v;
-                    if (PARTS) {
-                        v.x = o[j][0][0] + o[j][0][1];
-                        v.y = o[j][1][0] + o[j][1][1];
-                        v.z = o[j][0][2] + o[j][0][3];
-                        v.w = o[j][1][2] + o[j][1][3];
-                    } else {
-                        v.x = o[j][0][i];
-                        v.y = o[j][1][i];
-                        v.z = o[j][0][2 + i];
-                        v.w = o[j][1][2 + i];
-                    }
-                    constexpr float even = CENTRED ? 1.f : kCodeScaleLow, odd = CENTRED ? 1.f / 16.f : kCodeScaleHigh;
-                    v.x = fmaf(v.x, even, add);
-                    v.y = fmaf(v.y, odd, add);
-                    v.z = fmaf(v.z, even, add);
-                    v.w = fmaf(v.w, odd, add);
-                    *reinterpret_cast<float4*>(obuf + ((size_t)warp * RPT + r) * D + j * 32 + gid * 4) = v;
+                    for (int g = 0; g < (BOTH ? 1 : NG); ++g) om[g][i] += __shfl_xor_sync(0xffffffffu, om[g][i], d);
                 }
             }
-            __syncthreads();
             const Cursor was = k;
-            if (t + n_tiles < n_total) {                     // the next unit's query rows are on their way during the join
-                k = advance(k, n_tiles);
-                load_q(k);
-            }
             const bool whole = n_tiles == was.nt;
             const int piece = blockIdx.x * 2 + (first_tile == 0 ? 1 : 0);
-            // nsg neighbouring lanes take the parts of one quad of outputs and add them up by shuffles
-            const int rows_here = a.R - rb * a.RU < a.RU ? a.R - rb * a.RU : a.RU, items = rows_here * (D / 4);
-            const int part = tid % nsg, per_round = 32 * kAttnWarps / nsg;
-            for (int i0 = 0; i0 < items; i0 += per_round) {
-                const int item = i0 + tid / nsg, ru = item < items ? item / (D / 4) : 0, d4 = item % (D / 4);
-                const int from = (part * a.RT + ru / RPT) * RPT + ru % RPT;      // row of the part's warp
-                const float2 ml = mlbuf[from];
-                const float4 x = *reinterpret_cast<const float4*>(obuf + (size_t)from * D + d4 * 4);
-                float top = ml.x;
-                for (int d = 1; d < nsg; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-                const float e = exp2_fast(ml.x - top);
-                float sum = ml.y * e;
-                float4 v = make_float4(x.x * e, x.y * e, x.z * e, x.w * e);
-                for (int d = 1; d < nsg; d <<= 1) {
-                    sum += __shfl_xor_sync(0xffffffffu, sum, d);
-                    v.x += __shfl_xor_sync(0xffffffffu, v.x, d);
-                    v.y += __shfl_xor_sync(0xffffffffu, v.y, d);
-                    v.z += __shfl_xor_sync(0xffffffffu, v.z, d);
-                    v.w += __shfl_xor_sync(0xffffffffu, v.w, d);
+#pragma unroll
+            for (int tl = 0; tl < TL; ++tl) {
+                __syncthreads();                             // the buffer's last use is over
+#pragma unroll
+                for (int i = 0; i < NV / TL; ++i) {
+                    const int ii = tl * 2 + i, r = WIDE ? tig : 2 * tig + i;
+                    if (gid == 0) mlbuf[warp * JOIN + r] = make_float2(mx[ii] - E, l[ii]);
+#pragma unroll
+                    for (int j = 0; j < H32; ++j) {
+                        const float add = BOTH ? 0.f : om[BOTH ? 0 : j * 32 / G][ii];
+                        float4 v;
+                        if (PARTS) {
+                            v.x = o[tl][j][0][0] + o[tl][j][0][1];
+                            v.y = o[tl][j][1][0] + o[tl][j][1][1];
+                            v.z = o[tl][j][0][2] + o[tl][j][0][3];
+                            v.w = o[tl][j][1][2] + o[tl][j][1][3];
+                        } else {
+                            v.x = o[tl][j][0][i];
+                            v.y = o[tl][j][1][i];
+                            v.z = o[tl][j][0][2 + i];
+                            v.w = o[tl][j][1][2 + i];
+                        }
+                        // kRows16: values entered with 2^(7 - k)
+                        constexpr float even = BOTH ? 1.f / 128.f : (CENTRED ? 1.f : kCodeScaleLow), odd = BOTH || CENTRED ? even / 16.f : kCodeScaleHigh;
+                        v.x = fmaf(v.x, even, add);
+                        v.y = fmaf(v.y, odd, add);
+                        v.z = fmaf(v.z, even, add);
+                        v.w = fmaf(v.w, odd, add);
+                        *reinterpret_cast<float4*>(obuf + ((size_t)warp * JOIN + r) * D + j * 32 + gid * 4) = v;
+                    }
                 }
-                if (part != 0 || item >= items) continue;
-                if (whole) {
-                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-                    const int r = rb * a.RU + ru, rt_ = token_of(r);
-                    T* dst = (T*)a.out + ((long long)b * a.T + rt_) * a.ld_out + (long long)(h * a.share + r - rt_ * a.share) * D + d4 * 4;
-                    store4(dst, v.x * inv, v.y * inv, v.z * inv, v.w * inv);
-                    if (d4 == 0 && a.accumulate) a.stats[(((size_t)b * c.H + h) * a.RB + rb) * a.RU + ru] = make_float2(top, sum);
-                } else {
-                    *reinterpret_cast<float4*>(a.part_o + ((size_t)piece * a.RU + ru) * D + d4 * 4) = v;
-                    if (d4 == 0) a.part_ml[(size_t)piece * a.RU + ru] = make_float2(top, sum);
+                __syncthreads();
+                if (tl == 0 && t + n_tiles < n_total) {      // the next unit's query rows are on their way during the join
+                    k = advance(k, n_tiles);
+                    load_q(k);
+                }
+                // `lanes` neighbouring lanes take the nsg parts of one quad of outputs in turn, and add them up by shuffles: as
+                // many as leave no lane without a quad (15 rows of 128: 1100 instructions a warp with 8, 250 with 1)
+                const int rows_here = a.R - rb * a.RU < a.RU ? a.R - rb * a.RU : a.RU;
+                const int items = (BOTH ? a.RT * JOIN : rows_here) * (D / 4);
+                int lanes = nsg;
+                while (lanes > 1 && items * lanes > kAttnThreads) lanes >>= 1;
+                const int part = tid & (lanes - 1), per_round = kAttnThreads / lanes;
+                for (int i0 = 0; i0 < items; i0 += per_round) {
+                    const int item = i0 + tid / lanes, at = item < items ? item / (D / 4) : 0, d4 = item % (D / 4);
+                    const int ru = BOTH ? at / JOIN * RPT + tl * JOIN + at % JOIN : at;
+                    const int from = (part * a.RT + at / JOIN) * JOIN + at % JOIN, step = lanes * a.RT * JOIN;       // row of the part's warp
+                    float top = kNoLogit * 2.f;
+                    for (int q = part, r = from; q < nsg; q += lanes, r += step) top = fmaxf(top, mlbuf[r].x);
+                    for (int d = 1; d < lanes; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                    float sum = 0.f;
+                    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+                    for (int q = part, r = from; q < nsg; q += lanes, r += step) {
+                        const float2 ml = mlbuf[r];
+                        const float4 x = *reinterpret_cast<const float4*>(obuf + (size_t)r * D + d4 * 4);
+                        const float e = exp2_fast(ml.x - top);
+                        sum = fmaf(ml.y, e, sum);
+                        v.x = fmaf(x.x, e, v.x);
+                        v.y = fmaf(x.y, e, v.y);
+                        v.z = fmaf(x.z, e, v.z);
+                        v.w = fmaf(x.w, e, v.w);
+                    }
+                    for (int d = 1; d < lanes; d <<= 1) {
+                        sum += __shfl_xor_sync(0xffffffffu, sum, d);
+                        v.x += __shfl_xor_sync(0xffffffffu, v.x, d);
+                        v.y += __shfl_xor_sync(0xffffffffu, v.y, d);
+                        v.z += __shfl_xor_sync(0xffffffffu, v.z, d);
+                        v.w += __shfl_xor_sync(0xffffffffu, v.w, d);
+                    }
+                    if (part != 0 || item >= items || ru >= rows_here) continue;
+                    if (whole) {
+                        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                        const int r = rb * a.RU + ru, rt_ = token_of(r);
+                        T* dst = (T*)a.out + ((long long)b * a.T + rt_) * a.ld_out + (long long)(h * a.share + r - rt_ * a.share) * D + d4 * 4;
+                        store4(dst, v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+                        if (d4 == 0 && a.accumulate) a.stats[(((size_t)b * c.H + h) * a.RB + rb) * a.RU + ru] = make_float2(top, sum);
+                    } else {
+                        *reinterpret_cast<float4*>(a.part_o + ((size_t)piece * a.RU + ru) * D + d4 * 4) = v;
+                        if (d4 == 0) a.part_ml[(size_t)piece * a.RU + ru] = make_float2(top, sum);
+                    }
                 }
             }
             t += n_tiles;
@@ -888,6 +1143,10 @@ __global__ void __launch_bounds__(kFinishThreads, 3) kv4_finish_kernel(const __g
             load_w(n0);
             load_x(n0, 0);
         }
+        // several rows are added up by themselves: one rounding of the weight, however large it is already
+        float4 add[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) add[u] = BATCH == 1 ? w[u] : make_float4(0.f, 0.f, 0.f, 0.f);
         for (int r0 = 0; r0 < a.R; r0 += BATCH) {
             if (r0 > 0) load_x(n0, r0);
 #pragma unroll
@@ -897,16 +1156,18 @@ __global__ void __launch_bounds__(kFinishThreads, 3) kv4_finish_kernel(const __g
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     const int see = sees[r0 + k] - (n0 + u * kFinishSlots);          // slots of the four that the row sees
-                    if (see > 0) w[u].x = fmaf(exp2_fast(x[u][k].x - ml.x), ml.y, w[u].x);
-                    if (see > 1) w[u].y = fmaf(exp2_fast(x[u][k].y - ml.x), ml.y, w[u].y);
-                    if (see > 2) w[u].z = fmaf(exp2_fast(x[u][k].z - ml.x), ml.y, w[u].z);
-                    if (see > 3) w[u].w = fmaf(exp2_fast(x[u][k].w - ml.x), ml.y, w[u].w);
+                    if (see > 0) add[u].x = fmaf(exp2_fast(x[u][k].x - ml.x), ml.y, add[u].x);
+                    if (see > 1) add[u].y = fmaf(exp2_fast(x[u][k].y - ml.x), ml.y, add[u].y);
+                    if (see > 2) add[u].z = fmaf(exp2_fast(x[u][k].z - ml.x), ml.y, add[u].z);
+                    if (see > 3) add[u].w = fmaf(exp2_fast(x[u][k].w - ml.x), ml.y, add[u].w);
                 }
             }
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (n0 + u * kFinishSlots < end) *reinterpret_cast<float4*>(weight + n0 + u * kFinishSlots) = w[u];
+            if (n0 + u * kFinishSlots < end)
+                *reinterpret_cast<float4*>(weight + n0 + u * kFinishSlots) =
+                    BATCH == 1 ? add[u] : make_float4(w[u].x + add[u].x, w[u].y + add[u].y, w[u].z + add[u].z, w[u].w + add[u].w);
     }
 }
 
@@ -917,7 +1178,7 @@ static inline size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 static void attn_rows(int R, int rpt, int* RT, int* RU, int* RB)
 {
     const int tiles = (R + rpt - 1) / rpt;
-    *RT = tiles > 4 ? 8 : (tiles > 2 ? 4 : tiles);
+    *RT = tiles > 4 && rpt < 16 ? 8 : (tiles > 2 ? 4 : tiles);               // of 16 rows: two warps per row tile at least
     *RU = *RT * rpt;
     *RB = (R + *RU - 1) / *RU;
 }
@@ -942,9 +1203,10 @@ static AttnLayout attn_layout(const Kv4& c, int R, int rpt)
 template <typename T, int D, int G, int MODE>
 static coreinfer_status launch_mode(AttnArgs& a, const DeviceInfo& di, cudaStream_t st)
 {
-    constexpr int RPT = MODE == kRows8 ? 8 : 4, NG = D / G, TILE = kAttnTile<D, G>;
+    constexpr int NG = D / G, TILE = kAttnTile<D, G, MODE>;
     const size_t ring = (size_t)kAttnStages<D, G, MODE> * (TILE / kAttnWarps) * (D / 2 + NG * 4);
-    const size_t smem = kAttnWarps * (ring + RPT * (D * sizeof(float) + sizeof(float2))) + (3 * a.c.B + 1) * sizeof(int);
+    const size_t smem = kAttnWarps * (ring + kAttnJoinRows<MODE> * (D * sizeof(float) + sizeof(float2))) +
+                        (MODE == kRows16 ? a.RT * kAttnQueryBytes<D> + kAttnWarps * 16 * sizeof(float2) : 0) + (3 * a.c.B + 1) * sizeof(int);
     // two CTAs per SM where registers (head_dim up to 128) and shared memory (batch up to some hundreds) allow it
     const int per_sm = D <= 128 && 2 * (smem + 1024 + 64) <= (size_t)di.smem_optin + 1024 ? 2 : 1;
     if (smem > smem_room(di)) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "not enough shared memory");
@@ -973,13 +1235,14 @@ static coreinfer_status launch_mode(AttnArgs& a, const DeviceInfo& di, cudaStrea
 
 // Rows per MMA tile for R query rows: fp32 and fp16 always carry two parts; bf16 takes the form with four rows where that
 // is enough.
-static inline int attn_rpt(coreinfer_dtype dtype, long long R) { return dtype != COREINFER_BF16 || R <= 4 ? 4 : 8; }
+static inline int attn_rpt(coreinfer_dtype dtype, long long R) { return dtype != COREINFER_BF16 || R <= 4 ? 4 : (R <= 8 ? 8 : 16); }
 
 template <typename T, int D, int G>
 static coreinfer_status launch_attention(AttnArgs& a, const DeviceInfo& di, cudaStream_t st)
 {
     if constexpr (std::is_same<T, __nv_bfloat16>::value)
-        return a.R <= 4 ? launch_mode<T, D, G, kRows4>(a, di, st) : launch_mode<T, D, G, kRows8>(a, di, st);
+        return a.R <= 4 ? launch_mode<T, D, G, kRows4>(a, di, st)
+                        : (a.R <= 8 ? launch_mode<T, D, G, kRows8>(a, di, st) : launch_mode<T, D, G, kRows16>(a, di, st));
     else
         return launch_mode<T, D, G, kRows4Parts>(a, di, st);
 }
@@ -1011,8 +1274,12 @@ size_t coreinfer_kv4_attention_workspace_bytes(const coreinfer_kv4_cache* cache,
     if (q_heads < 1 || T < 1 || q_heads % c.H != 0 || T > COREINFER_KV4_MAX_QUERIES) return 0;
     const long long R = (long long)(q_heads / c.H) * T;
     if (R > kAttnMaxRows) return 0;
-    const size_t x = attn_layout(c, (int)R, 8).total, y = attn_layout(c, (int)R, 4).total;
-    return x > y ? x : y;
+    size_t most = 0;
+    for (int rpt = 4; rpt <= 16; rpt *= 2) {
+        const size_t n = attn_layout(c, (int)R, rpt).total;
+        if (n > most) most = n;
+    }
+    return most;
 }
 
 coreinfer_status coreinfer_kv4_attention(const coreinfer_kv4_cache* cache, const void* q, coreinfer_dtype dtype,

@@ -92,15 +92,16 @@ def attend(ref, d, q, accumulate=True, scale=None, out=None, stream=None):
     return out
 
 
-def check_attention(ref, d, q, out, scale, before):
+def check_attention(ref, d, q, out, scale, before, roundings=1):
     """Bounds.  A logit is a sum of D products and their groups in fp32: it is off by at most (D / 8 + 32) spacings of
     its absolute terms (fp32 q enters with 22 bits: 4 spacings more), and by 2^-20 in its exponential.  An error e of a
     logit moves its p and the sum by factors e^(+-e) each.  The weights p s enter the second product with at least
-    11 bits for bf16 and 22 for the others; its sums over n slots add n / 8 + 32 spacings at most; then one rounding."""
+    11 bits for bf16 and 22 for the others; its sums over n slots add n / 8 + 32 spacings at most; then one rounding.
+    (More than 8 bf16 rows share values in fp16: p, the group's offset and the value are rounded, roundings = 3.)"""
     o, add, mass, logit_mass = ref.attention(values_np(q).astype(np.float64), scale)
     n = max(ref.length)
     e = 2 * ((ref.D / 8 + 36) * EPS32 * logit_mass + 2.0 ** -20)[..., None]
-    rel = e + (EPS16 if q.dtype == torch.bfloat16 else 2.0 ** -21) + (n / 8 + 32) * EPS32
+    rel = e + (roundings * EPS16 if q.dtype == torch.bfloat16 else 2.0 ** -21) + (n / 8 + 32) * EPS32
     tol = rel * mass + (OUT_EPS[q.dtype] * np.abs(o)) + 1e-30
     err = np.abs(values_np(out) - o)
     assert (err <= tol).all(), "outputs: worst %.3g of the bound" % (err / tol).max()
@@ -189,6 +190,68 @@ def test_attention_sharp_and_scaled(dtype):
         d = ref.to_cuda()
         out = attend(ref, d, q, scale=scale)
         check_attention(ref, d, q, out, scale, ref.weight)
+
+
+WIDE = [
+    # B, H, share, T, D, group, lengths: 9 to 142 bf16 query rows per key head
+    (2, 3, 16, 1, 64, 32, [300, 2]), (1, 2, 9, 1, 128, 128, [513]), (1, 2, 5, 4, 128, 64, [77]), (1, 1, 40, 1, 64, 64, [1000]),
+    (3, 1, 71, 2, 128, 32, [40, 0, 1]), (2, 2, 16, 1, 256, 32, [150, 31]), (1, 1, 4, 16, 256, 128, [40]), (1, 1, 3, 5, 256, 64, [2000]),
+    (1, 8, 4, 3, 128, 32, [3000]), (2, 2, 1, 16, 128, 64, [15, 100]), (7, 16, 11, 1, 128, 128, [16, 129, 1, 500, 300, 128, 64]),
+]
+
+
+@pytest.mark.parametrize("B,H,share,T,D,group,lengths", WIDE)
+def test_attention_many_rows(B, H, share, T, D, group, lengths):
+    require_gpu()
+    rng = np.random.default_rng(1000 + D + len(lengths))
+    ref = CacheRef(B, H, 16 * -(-max(lengths) // 16) + 16, D, group, rng)
+    ref.set_lengths(lengths)
+    d = ref.to_cuda()
+    q = torch.from_numpy(rng.standard_normal((B, T, H * share, D)).astype(np.float32)).cuda().bfloat16()
+    check_attention(ref, d, q, attend(ref, d, q), D ** -0.5, ref.weight, roundings=3)
+
+
+@pytest.mark.parametrize("D,group", [(64, 32), (128, 32), (128, 128), (256, 64)])
+def test_attention_many_rows_sharp_and_scaled(D, group):
+    """Logits in the hundreds and values from 1e-4 to 1e5 (scales and offsets beyond what fp16 holds 16 times)."""
+    require_gpu()
+    B, H, share, T = 2, 2, 6, 2
+    rng = np.random.default_rng(60 + D)
+    ref = CacheRef(B, H, 512, D, group, rng)
+    ref.set_lengths([500, 333])
+    scales = 10.0 ** rng.uniform(-4, 5, size=(B, H, 512, 1))
+    with np.errstate(over="ignore"):
+        ref.s[1], ref.o[1] = (np.minimum(ref.s[1] * scales, 65504).astype(np.float16), np.clip(ref.o[1] * scales, -65504, 65504).astype(np.float16))
+    for factor in (40.0, 1.0, 1e-4, 1e8):
+        q = torch.from_numpy((factor * rng.standard_normal((B, T, H * share, D))).astype(np.float32)).cuda().bfloat16()
+        scale = D ** -0.5 * (1.0 if factor < 1e3 else 100.0 / factor)
+        d = ref.to_cuda()
+        check_attention(ref, d, q, attend(ref, d, q, scale=scale), scale, ref.weight, roundings=3)
+
+
+@pytest.mark.parametrize("share", [1, 5])
+def test_attention_nan_in_slots_that_a_token_does_not_see(share):
+    """NaN in the newest token's key or value, and beyond the sequence: the tokens before it do not notice."""
+    require_gpu()
+    T, n = 3, 35
+    ref = CacheRef(1, 2, 48, 128, 32, np.random.default_rng(19))
+    ref.set_lengths([n])
+    q = torch.randn(1, T, 2 * share, 128, device="cuda", dtype=torch.bfloat16)
+    clean = ref.to_cuda()
+    want = attend(ref, clean, q)
+    d = ref.to_cuda()
+    d["v_pairs"][0, 1, n - 1, 2] = float("nan")
+    for name in ("k_pairs", "v_pairs"):
+        d[name][0, :, n:] = float("nan")
+    out = attend(ref, d, q)
+    assert torch.equal(out[:, :T - 1], want[:, :T - 1]) and torch.equal(out[:, T - 1, :share], want[:, T - 1, :share])
+    assert torch.isnan(out[0, T - 1, share:, 64:96]).all()
+    assert torch.isfinite(out[0, T - 1, share:, :64]).all() and torch.isfinite(out[0, T - 1, share:, 96:]).all()
+    assert torch.equal(d["weight"], clean["weight"])
+    d = ref.to_cuda()
+    d["k_pairs"][0, 1, n - 1, 0] = float("nan")
+    out = attend(ref, d, q)
+    assert torch.equal(out[:, :T - 1], want[:, :T - 1]) and torch.isnan(out[0, T - 1, share:]).all()
 
 
 def test_attention_nan_in_a_value_reaches_its_heads_only():
