@@ -1233,17 +1233,24 @@ static coreinfer_status launch_mode(AttnArgs& a, const DeviceInfo& di, cudaStrea
     return COREINFER_OK;
 }
 
-// Rows per MMA tile for R query rows: fp32 and fp16 always carry two parts; bf16 takes the form with four rows where that
-// is enough.
-static inline int attn_rpt(coreinfer_dtype dtype, long long R) { return dtype != COREINFER_BF16 || R <= 4 ? 4 : (R <= 8 ? 8 : 16); }
+// Rows per warp for R query rows and `groups` groups per head: fp32 and fp16 always carry two parts; bf16 takes the
+// form with four rows where that is enough, and above eight rows the one with sixteen where there are four groups or more
+// (4 x 8 heads x 4096 slots, 15 / 24 / 64 rows: head_dim 128 in groups of 32 24.7 / 35.1 / 62.8 us against 26.4 / 39.1 /
+// 72.3 with eight rows a warp; in groups of 64, where p s is formed for two groups only, 23.6 / 32.8 / 57.7 against 21.8 /
+// 30.6 / 55.5).
+static inline int attn_rpt(coreinfer_dtype dtype, long long R, int groups)
+{
+    return dtype != COREINFER_BF16 || R <= 4 ? 4 : (R <= 8 || groups < 4 ? 8 : 16);
+}
 
 template <typename T, int D, int G>
 static coreinfer_status launch_attention(AttnArgs& a, const DeviceInfo& di, cudaStream_t st)
 {
-    if constexpr (std::is_same<T, __nv_bfloat16>::value)
-        return a.R <= 4 ? launch_mode<T, D, G, kRows4>(a, di, st)
-                        : (a.R <= 8 ? launch_mode<T, D, G, kRows8>(a, di, st) : launch_mode<T, D, G, kRows16>(a, di, st));
-    else
+    if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+        if constexpr (D / G >= 4)
+            if (a.R > 8) return launch_mode<T, D, G, kRows16>(a, di, st);
+        return a.R <= 4 ? launch_mode<T, D, G, kRows4>(a, di, st) : launch_mode<T, D, G, kRows8>(a, di, st);
+    } else
         return launch_mode<T, D, G, kRows4Parts>(a, di, st);
 }
 
@@ -1308,7 +1315,7 @@ coreinfer_status coreinfer_kv4_attention(const coreinfer_kv4_cache* cache, const
     if (workspace_bytes < need) CI_FAIL(COREINFER_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
     DeviceInfo di;
     if ((s = device_info(&di)) != COREINFER_OK) return s;
-    const int rpt = attn_rpt(dtype, R);
+    const int rpt = attn_rpt(dtype, R, a.c.D / a.c.G);
     const AttnLayout w = attn_layout(a.c, (int)R, rpt);
     uint8_t* ws = (uint8_t*)workspace;
     a.q = q;

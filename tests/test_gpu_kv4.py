@@ -97,7 +97,7 @@ def check_attention(ref, d, q, out, scale, before, roundings=1):
     its absolute terms (fp32 q enters with 22 bits: 4 spacings more), and by 2^-20 in its exponential.  An error e of a
     logit moves its p and the sum by factors e^(+-e) each.  The weights p s enter the second product with at least
     11 bits for bf16 and 22 for the others; its sums over n slots add n / 8 + 32 spacings at most; then one rounding.
-    (More than 8 bf16 rows share values in fp16: p, the group's offset and the value are rounded, roundings = 3.)"""
+    (More than 8 bf16 rows may share values in fp16: p, the group's offset and the value are rounded, roundings = 3.)"""
     o, add, mass, logit_mass = ref.attention(values_np(q).astype(np.float64), scale)
     n = max(ref.length)
     e = 2 * ((ref.D / 8 + 36) * EPS32 * logit_mass + 2.0 ** -20)[..., None]
