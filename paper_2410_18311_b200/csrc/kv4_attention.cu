@@ -123,13 +123,23 @@ __device__ __forceinline__ void store4(T* dst, float x, float y, float z, float 
 }
 
 // Two codes c (or 16 c) less 8 (128), as fp16: above 1024 the codes are the low bits of a number whose last place is 1.
-__device__ __forceinline__ uint32_t centred(uint32_t x, uint32_t mask, uint32_t middle)
+// `above` holds 1024 twice in a register: with it as a literal, beside the mask, this takes an instruction more.
+__device__ __forceinline__ uint32_t literal_1024()
 {
-    const uint32_t up = (x & mask) | 0x64006400u;
+    uint32_t r;
+    asm volatile("mov.u32 %0, 0x64006400;" : "=r"(r));
+    return r;
+}
+template <uint32_t MASK>
+__device__ __forceinline__ uint32_t centred(uint32_t x, uint32_t above)
+{
+    static_assert(MASK == 0x000f000fu || MASK == 0x00f000f0u, "even or odd codes");
+    uint32_t up;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(up) : "r"(x), "n"(MASK), "r"(above));        // (x & MASK) | above
+    const uint32_t middle = MASK == 0x000f000fu ? 0x64086408u : 0x64806480u;
     const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&up), *reinterpret_cast<const __half2*>(&middle));
     return *reinterpret_cast<const uint32_t*>(&r);
 }
-
 __device__ __forceinline__ __half2 as_half2(uint32_t w) { return *reinterpret_cast<const __half2*>(&w); }
 __device__ __forceinline__ uint32_t as_word(__half2 h) { return *reinterpret_cast<const uint32_t*>(&h); }
 
@@ -337,6 +347,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
 #pragma unroll 1
             for (int s = 0; s < STAGES; ++s) feed(ring + s * STAGE, s & 1);
         }
+        const uint32_t above = CENTRED || BOTH ? literal_1024() : 0u;
         uint32_t stage = 0;                                  // offset of the stage at hand in the ring
         int t = 0;                                           // tiles done
         // Into a step: its stage has arrived, for every lane.  Out of it: all lanes have read it; it takes the piece STAGES
@@ -607,31 +618,41 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                     float most[NV];
 #pragma unroll
                     for (int i = 0; i < NV; ++i) {
+                        const float by = BOTH ? q_row[(i >> 1) * 8 + (i & 1)].x : f[BOTH ? 0 : i];
 #pragma unroll
                         for (int u = 0; u < UN; ++u)
 #pragma unroll
-                            for (int v = 0; v < 2; ++v) lo[u][v][i] *= BOTH ? q_row[(i >> 1) * 8 + (i & 1)].x : f[BOTH ? 0 : i];
+                            for (int v = 0; v < 2; ++v) lo[u][v][i] *= by;
+                    }
+                    if (a.accumulate) {
+                        // what a row does not see may be written too: it lies within the capacity and is never read
+#pragma unroll
+                        for (int i = 0; i < NV; ++i)
+                            if (row_of(i) < a.R) {
+                                float* to = lg + (size_t)(row_of(i) - row_of(0)) * c.cap + n0;
+#pragma unroll
+                                for (int u = 0; u < UN; ++u)
+                                    if (UN == 1 || u == 0 || n0 + 16 < len) {
+                                        to[16 * u] = lo[u][0][i];
+                                        to[16 * u + 8] = lo[u][1][i];
+                                    }
+                            }
+                    }
 #pragma unroll 1
-                        for (int e = edge; e; e = opaque_zero()) {
+                    for (int e = edge; e; e = opaque_zero()) {
+#pragma unroll
+                        for (int i = 0; i < NV; ++i)
 #pragma unroll
                             for (int u = 0; u < UN; ++u)
 #pragma unroll
                                 for (int v = 0; v < 2; ++v)
                                     if (na + 16 * u + 8 * v >= sees(i)) lo[u][v][i] = -__int_as_float(0x7f800000);
-                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < NV; ++i) {
                         most[i] = fmaxf(lo[0][0][i], lo[0][1][i]);
 #pragma unroll
                         for (int u = 1; u < UN; ++u) most[i] = fmaxf(most[i], fmaxf(lo[u][0][i], lo[u][1][i]));
-                        if (a.accumulate && row_of(i) < a.R) {
-                            // what a row does not see may be written too: it lies within the capacity and is never read
-                            float* to = lg + (size_t)(row_of(i) - row_of(0)) * c.cap + n0;
-#pragma unroll
-                            for (int u = 0; u < UN; ++u)
-                                if (UN == 1 || u == 0 || n0 + 16 < len) {
-                                    to[16 * u] = lo[u][0][i];
-                                    to[16 * u + 8] = lo[u][1][i];
-                                }
-                        }
                     }
                     leave(0);
                     uint8_t* vst = enter();
@@ -810,8 +831,8 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                                 even[e] = __hfma2(sc[e], __float2half2_rn(8.f), as_half2(__byte_perm(pr[2 * e], pr[2 * e + 1], 0x7632)));
                                 odd[e] = __hmul2(even[e], __float2half2_rn(16.f));
                             }
-                            auto value = [&](uint32_t x, int e) { return as_word(__hfma2(as_half2(centred(x, 0x000f000fu, 0x64086408u)), sc[e], even[e])); };
-                            auto value16 = [&](uint32_t x, int e) { return as_word(__hfma2(as_half2(centred(x, 0x00f000f0u, 0x64806480u)), sc[e], odd[e])); };
+                            auto value = [&](uint32_t x, int e) { return as_word(__hfma2(as_half2(centred<0x000f000fu>(x, above)), sc[e], even[e])); };
+                            auto value16 = [&](uint32_t x, int e) { return as_word(__hfma2(as_half2(centred<0x00f000f0u>(x, above)), sc[e], odd[e])); };
 #pragma unroll
                             for (int j = g * G / 32; j < (g + 1) * G / 32; ++j) {
                                 const uint32_t x = __byte_perm(va[j / 2], vb[j / 2], j & 1 ? 0x7632 : 0x5410);
@@ -874,10 +895,10 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                                 const uint32_t y = __byte_perm(vc[j / 2], vd[j / 2], j & 1 ? 0x7632 : 0x5410);
                                 const uint32_t x8 = x >> 8, y8 = y >> 8;
                                 if (CENTRED) {
-                                    mma_16816(o[0][j][0], centred(x, 0x000f000fu, 0x64086408u), centred(x8, 0x000f000fu, 0x64086408u),
-                                              centred(y, 0x000f000fu, 0x64086408u), centred(y8, 0x000f000fu, 0x64086408u), bf[0], bf[1]);
-                                    mma_16816(o[0][j][1], centred(x, 0x00f000f0u, 0x64806480u), centred(x8, 0x00f000f0u, 0x64806480u),
-                                              centred(y, 0x00f000f0u, 0x64806480u), centred(y8, 0x00f000f0u, 0x64806480u), bf[0], bf[1]);
+                                    mma_16816(o[0][j][0], centred<0x000f000fu>(x, above), centred<0x000f000fu>(x8, above),
+                                              centred<0x000f000fu>(y, above), centred<0x000f000fu>(y8, above), bf[0], bf[1]);
+                                    mma_16816(o[0][j][1], centred<0x00f000f0u>(x, above), centred<0x00f000f0u>(x8, above),
+                                              centred<0x00f000f0u>(y, above), centred<0x00f000f0u>(y8, above), bf[0], bf[1]);
                                 } else {
                                     mma_16816(o[0][j][0], x & 0x000f000fu, x8 & 0x000f000fu, y & 0x000f000fu, y8 & 0x000f000fu, bf[0], bf[1]);
                                     mma_16816(o[0][j][1], x & 0x00f000f0u, x8 & 0x00f000f0u, y & 0x00f000f0u, y8 & 0x00f000f0u, bf[0], bf[1]);
