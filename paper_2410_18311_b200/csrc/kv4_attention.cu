@@ -28,6 +28,13 @@
 // fp32 and fp16 calls carry query rows and p s as two fp16 parts in neighbouring columns (22 bits; four rows per
 // tile instead of eight): with one part the rounding of p s (2^-12, times the ratio of s c to the centred
 // value, about 3) would exceed fp16's own rounding.
+// Calls of more than eight bf16 rows per key head may take 16 rows per warp (attn_rpt): the codes are unpacked once for two
+// MMAs, and values enter as s c + o in fp16 (p itself instead of p s per group), under a power of two per slot that p makes
+// up for.  Three roundings of 2^-12, of p, o and the value, below bf16's 2^-9.
+// Measured (accumulating but for the last): 8 x 32 heads x 4001 bf16 38.7 us, 3200 GB/s, of which about 15 do not grow with the
+// length (launches, the lists, starting and joining units, finishing); 16384 slots 127 us, 5000 GB/s, the slope 5400;
+// 6 sequences x 8 heads x 15 rows in groups of 32 x 9000 slots 50 us, bound by instruction issue and latency (640
+// instructions per 16 slots and warp, 16 warps an SM); 2 x 8 heads x 4 fp16 rows x 130000 slots 57 us, 4200 GB/s.
 #include "kv4.cuh"
 
 #include <type_traits>
@@ -1035,7 +1042,8 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
 // Blocks x < R of a (sequence, head): query row x, joined from the pieces of its unit where that was cut
 // (zeros where the sequence is empty).  Blocks beyond: finish_slots slots each, whose weights get the
 // sum over rows of 2^(logit - maximum) / sum.  A thread has U quads of slots and BATCH rows in flight: 4 and 1 where
-// there is one row per key head, else 1 and 8.
+// there is one row per key head, else 1 and 8.  Bound by latency (4 to 5 us beside the attention kernel at 8 x 32 heads x
+// 4001), and by the bytes of the logits, which come from L2, where there are many rows.
 constexpr int kFinishThreads = 256;
 constexpr int kFinishSlots = 4 * kFinishThreads;             // per round of a block
 

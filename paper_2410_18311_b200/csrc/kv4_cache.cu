@@ -6,8 +6,10 @@ namespace coreinfer {
 // -------------------------------------------------------------------------------- append --
 // A row is one token's keys or values of one head.  A lane holds eight consecutive values of a row (D / 8 lanes
 // per row); the lanes of a group agree on its range by shuffles; neighbouring blocks of 32 values
-// exchange a unit so that codes are stored in words.  Bound by the bytes read and written; a CTA walks
-// rows of one sequence so that the sequence's state is read, and its ticket taken, a few hundred times at most.
+// exchange a unit so that codes are stored in words.  A CTA walks rows of one sequence so that the sequence's state is
+// read, and its ticket taken, a few hundred times at most; a lane moves on by fixed strides and has the next row under way
+// while it works on one.  Bound by instructions, about 280 per warp and row of eight values a lane: 1000 tokens x 32 heads
+// x 128 bf16, stored values out, 14.1 us, 2660 GB/s (issue slots 66 % busy).
 constexpr int kAppendThreads = 256;
 
 struct AppendArgs {
@@ -130,13 +132,16 @@ static coreinfer_status pick_append(const AppendArgs& a, const DeviceInfo& di, c
 // --------------------------------------------------------------------------------- evict --
 // kv4_evict_few_kernel, in place with at most 16 slots above the budget (the step of a decode loop at a full budget): one
 // CTA per sequence and head takes the smallest key out, once per slot that leaves, and moves what has to move.
-// kv4_select_kernel, otherwise: one CTA, or a cluster of up to 8 where heads are few and long, per sequence and head.  Keys
-// (the order of eviction as unsigned numbers) into shared memory, the key of the last slot that stays by
-// radix selection (11 + 11 + 10 bits, most significant first, stopping as soon as a whole bin stays; the CTAs of a cluster
-// add their histograms up in the first one's shared memory), then the lists of slots that move, by ballots and scans
-// over warps and CTAs.  A warp owns a contiguous range of slots, so that list order is slot order.
+// kv4_select_held_kernel, otherwise: one CTA, or a cluster of up to 8 where heads are few and long, per sequence and head.
+// Keys (the order of eviction as unsigned numbers) stay in registers, the key of the last slot that stays comes from
+// radix selection (11 + 11 + 10 bits, most significant first, stopping as soon as a whole bin stays), then the lists of slots
+// that move, by scans over threads and CTAs.
+// kv4_select_kernel, more than 16384 slots per CTA: the same with keys in shared memory, or read again for each pass, and
+// ballots; a warp owns a contiguous range of slots, so that list order is slot order.
 // kv4_move_kernel copies the listed slots, many CTAs per head.
-// All are bound by latency (memory, barriers) at the sizes of a decode step, the moves by bytes after a prompt.
+// All are bound by latency at the sizes of a decode step (append and few together 10.3 us for 8 sequences x 32 heads x 2049
+// slots, of which some 6 are two launches and the reads of the state), the moves by bytes after a prompt: 4 x 8 heads x
+// 16384 slots down to 2048 in another cache 19.3 us, about half of it the selection's barriers and three passes.
 constexpr int kEvictBins = 2048;
 constexpr int kEvictFew = 16;
 constexpr int kEvictKeysMost = 48 * 1024;   // keys a CTA holds in shared memory; more slots are read again for each pass
