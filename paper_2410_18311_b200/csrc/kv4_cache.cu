@@ -769,7 +769,8 @@ coreinfer_status coreinfer_kv4_evict(const coreinfer_kv4_cache* src, const corei
         if ((s = allow_smem<kv4_select_kernel>(di, 16384)) != COREINFER_OK) return s;
         CI_CUDA(launch_overlapped(kv4_select_kernel, dim3(a.H * cluster, a.B), dim3(1024), (size_t)e.keys * sizeof(unsigned), st, e, cluster));
     }
-    const int most = e.in_place ? (a.cap - budget < a.cap / 2 ? a.cap - budget : a.cap / 2) : (budget < a.cap ? budget : a.cap);
+    // in place, what moves comes from above the budget and goes to below it
+    const int most = e.in_place ? (a.cap - budget < budget ? a.cap - budget : budget) : (budget < a.cap ? budget : a.cap);
     CI_CUDA(launch_overlapped(kv4_move_kernel, dim3((most + kMoveSlots - 1) / kMoveSlots, a.B * a.H), dim3(kMoveThreads), 0, st, e));
     return COREINFER_OK;
 }

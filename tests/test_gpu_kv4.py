@@ -385,3 +385,34 @@ def test_append_attend_evict_loop():
     for b in range(B):
         for g in range(H):
             assert len(set(pos[b, g])) == budget and set(range(seen - recent, seen)) <= set(pos[b, g]) and {0, 1} <= set(pos[b, g])
+
+
+def test_offsets_beyond_32_bits():
+    """Three sequences of 64 heads with room for a million slots each: codes end beyond 2^32 bytes.  The same tokens in a
+    small cache give the same bits, through append, attention and eviction."""
+    require_gpu()
+    B, H, D, group = 3, 64, 64, 64
+    caches = []
+    for cap in (1 << 20, 128):
+        new = lambda *s, dtype: torch.empty((B, H, cap) + s, dtype=dtype, device="cuda")  # noqa: E731
+        d = {"k_codes": new(D // 2, dtype=torch.uint8), "v_codes": new(D // 2, dtype=torch.uint8), "k_pairs": new(1, 2, dtype=torch.float16),
+             "v_pairs": new(1, 2, dtype=torch.float16), "weight": new(dtype=torch.float32), "position": new(dtype=torch.int32),
+             "state": torch.zeros(B, 4, dtype=torch.int32, device="cuda")}
+        caches.append((d, handle(d)))
+    g = torch.Generator(device="cuda").manual_seed(4)
+    k, v = (torch.randn(B, 100, H, D, generator=g, device="cuda").bfloat16() for _ in range(2))
+    q = torch.randn(B, 1, H, D, generator=g, device="cuda").bfloat16()
+    outs = []
+    for d, h in caches:
+        ci.coreinfer_kv4_append(h, k, v)
+        out = torch.empty_like(q)
+        ws = torch.empty(ci.coreinfer_kv4_attention_workspace_bytes(h, H, 1), dtype=torch.uint8, device="cuda")
+        ci.coreinfer_kv4_attention(h, q, D ** -0.5, out, True, ws)
+        ws = torch.empty(ci.coreinfer_kv4_evict_workspace_bytes(h), dtype=torch.uint8, device="cuda")
+        ci.coreinfer_kv4_evict(h, h, 40, 10, 2, ws)
+        outs.append(out)
+    (big, _), (small, _) = caches
+    assert torch.equal(outs[0], outs[1]) and big["state"][:, :3].tolist() == [[40, 100, 0]] * B == small["state"][:, :3].tolist()
+    for name in big:
+        if name != "state":
+            assert torch.equal(big[name][:, :, :40], small[name][:, :, :40]), name
