@@ -148,6 +148,8 @@ constexpr int kEvictKeysMost = 48 * 1024;   // keys a CTA holds in shared memory
 constexpr int kEvictMaxCluster = 8;
 constexpr int kMoveSlots = 64;              // slots per CTA of the moving kernel
 constexpr int kMoveThreads = 256;
+constexpr int kMoveHere = 64;               // so few slots are moved by the CTA that selected them (room for 45 above the budget: 16.4 us with a
+                                            // launch more, 15.2 without; for 256: 13.9 and 20.8)
 
 __device__ __forceinline__ unsigned evict_key(float w, int pos, int seen, int recent, int first)
 {
@@ -215,6 +217,7 @@ struct EvictArgs {
     Kv4 a, z;
     int in_place, budget, recent, first;
     int keys;               // capacity of a CTA's key buffer
+    int move_here;          // the selecting CTA of a head moves what it listed
     int32_t* counts;        // [B * H] slots to move
     int32_t* lists;         // [B * H][cap]: sources; in place destinations [0, cap / 2), sources from cap / 2 on
 };
@@ -495,8 +498,9 @@ __global__ void __launch_bounds__(1024) kv4_select_held_kernel(const __grid_cons
         }
     }
     if (tid == 0 && rank == 0) e.counts[b * a.H + h] = movers;
-    if (size > 1) cluster_sync(size);                       // no CTA ends while another may still write to its shared memory
+    cluster_sync(size);                                     // the lists are complete, and no CTA ends while another may still write to its shared memory
     let_next_start();
+    if (e.move_here) move_slots(a, base, e.z, base, e.lists + base + a.cap / 2, e.lists + base, movers, tid, blockDim.x);
     if (kv4_last_of_sequence(a, b, gridDim.x)) {
         e.z.state[b * 4 + kStateLength] = keep;
         e.z.state[b * 4 + kStateSeen] = seen;
@@ -756,6 +760,9 @@ coreinfer_status coreinfer_kv4_evict(const coreinfer_kv4_cache* src, const corei
     int cluster = 1;
     while (cluster < kEvictMaxCluster && a.cap / (2 * cluster) >= 4096 && (long long)a.B * a.H * 2 * cluster <= di.sm_count) cluster *= 2;
     const int per = (a.cap + cluster - 1) / cluster;         // slots per CTA, a multiple of 4 (ITEMS at most divides what follows)
+    // in place, what moves comes from above the budget and goes to below it
+    const int most = e.in_place ? (a.cap - budget < budget ? a.cap - budget : budget) : (budget < a.cap ? budget : a.cap);
+    e.move_here = e.in_place && cluster == 1 && per <= 16384 && most <= kMoveHere;
     if (per <= 16384) {
         const dim3 held(a.H * cluster, a.B);
         if (per <= 1024) CI_CUDA(launch_overlapped(kv4_select_held_kernel<4>, held, dim3(256), 0, st, e, cluster));
@@ -769,8 +776,7 @@ coreinfer_status coreinfer_kv4_evict(const coreinfer_kv4_cache* src, const corei
         if ((s = allow_smem<kv4_select_kernel>(di, 16384)) != COREINFER_OK) return s;
         CI_CUDA(launch_overlapped(kv4_select_kernel, dim3(a.H * cluster, a.B), dim3(1024), (size_t)e.keys * sizeof(unsigned), st, e, cluster));
     }
-    // in place, what moves comes from above the budget and goes to below it
-    const int most = e.in_place ? (a.cap - budget < budget ? a.cap - budget : budget) : (budget < a.cap ? budget : a.cap);
+    if (e.move_here) return COREINFER_OK;
     CI_CUDA(launch_overlapped(kv4_move_kernel, dim3((most + kMoveSlots - 1) / kMoveSlots, a.B * a.H), dim3(kMoveThreads), 0, st, e));
     return COREINFER_OK;
 }
