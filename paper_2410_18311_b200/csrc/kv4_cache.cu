@@ -141,7 +141,7 @@ static coreinfer_status pick_append(const AppendArgs& a, const DeviceInfo& di, c
 // kv4_move_kernel copies the listed slots, many CTAs per head.
 // All are bound by latency at the sizes of a decode step (append and few together 10.3 us for 8 sequences x 32 heads x 2049
 // slots, of which some 6 are two launches and the reads of the state), the moves by bytes after a prompt: 4 x 8 heads x
-// 16384 slots down to 2048 in another cache 19.3 us, about half of it the selection's barriers and three passes.
+// 16384 slots down to 2048 in another cache 17.7 us, about half of it the selection's barriers and three passes.
 constexpr int kEvictBins = 2048;
 constexpr int kEvictFew = 16;
 constexpr int kEvictKeysMost = 48 * 1024;   // keys a CTA holds in shared memory; more slots are read again for each pass
@@ -755,20 +755,26 @@ coreinfer_status coreinfer_kv4_evict(const coreinfer_kv4_cache* src, const corei
         CI_CUDA(launch_overlapped(kv4_evict_few_kernel, dim3(a.H, a.B), dim3(a.cap <= 4096 ? 256 : 1024), 0, st, e));
         return COREINFER_OK;
     }
-    // Up to 8 CTAs per head while that leaves each 4096 slots at least and all of them fit on the GPU at once (1 x 8 heads x
-    // 65536 slots: 137 us with one CTA per head, 23 with eight).
+    // Up to 8 CTAs per head, until 1024 threads hold four slots each, while all of them fit on the GPU at once (1 x 8 heads x
+    // 65536 slots: 137 us with one CTA per head, 23 with eight; x 9008: 14.8 with two, 12.7 with four; x 4096: 12.5 with one, 14.4
+    // with two).
     int cluster = 1;
-    while (cluster < kEvictMaxCluster && a.cap / (2 * cluster) >= 4096 && (long long)a.B * a.H * 2 * cluster <= di.sm_count) cluster *= 2;
+    while (cluster < kEvictMaxCluster && a.cap > 4096 * cluster && (long long)a.B * a.H * 2 * cluster <= di.sm_count) cluster *= 2;
     const int per = (a.cap + cluster - 1) / cluster;         // slots per CTA, a multiple of 4 (ITEMS at most divides what follows)
     // in place, what moves comes from above the budget and goes to below it
     const int most = e.in_place ? (a.cap - budget < budget ? a.cap - budget : budget) : (budget < a.cap ? budget : a.cap);
     e.move_here = e.in_place && cluster == 1 && per <= 16384 && most <= kMoveHere;
     if (per <= 16384) {
+        // As many threads as there are slots for, while a CTA has an SM to itself (4 x 8 heads x 4096 slots: 14.3 us with 512
+        // threads, 12.5 with 1024); where there are more CTAs than SMs, two of 512 threads share one (8 x 32 x 4096: 40 against 46).
         const dim3 held(a.H * cluster, a.B);
+        const bool crowded = (long long)a.B * a.H * cluster > di.sm_count;
         if (per <= 1024) CI_CUDA(launch_overlapped(kv4_select_held_kernel<4>, held, dim3(256), 0, st, e, cluster));
-        else if (per <= 2048) CI_CUDA(launch_overlapped(kv4_select_held_kernel<8>, held, dim3(256), 0, st, e, cluster));
+        else if (per <= 2048) CI_CUDA(launch_overlapped(kv4_select_held_kernel<4>, held, dim3(512), 0, st, e, cluster));
+        else if (per <= 4096 && !crowded) CI_CUDA(launch_overlapped(kv4_select_held_kernel<4>, held, dim3(1024), 0, st, e, cluster));
         else if (per <= 4096) CI_CUDA(launch_overlapped(kv4_select_held_kernel<8>, held, dim3(512), 0, st, e, cluster));
-        else if (per <= 8192) CI_CUDA(launch_overlapped(kv4_select_held_kernel<8>, held, dim3(1024), 0, st, e, cluster));
+        else if (per <= 8192 && !crowded) CI_CUDA(launch_overlapped(kv4_select_held_kernel<8>, held, dim3(1024), 0, st, e, cluster));
+        else if (per <= 8192) CI_CUDA(launch_overlapped(kv4_select_held_kernel<16>, held, dim3(512), 0, st, e, cluster));
         else CI_CUDA(launch_overlapped(kv4_select_held_kernel<16>, held, dim3(1024), 0, st, e, cluster));
     } else {
         const int slots = per + 32;
