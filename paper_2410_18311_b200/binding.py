@@ -460,17 +460,23 @@ def _token_stride(t, shape):
 
 def coreinfer_kv4_append(cache, k, v, k_stored=None, v_stored=None, stream=None):
     """k, v [batch, T, kv_heads, head_dim] into the cache; k_stored / v_stored: the values as stored, or None."""
-    T = k.shape[1] if k.dim() == 4 else 0
-    shape, dtype = (cache.batch, T, cache.kv_heads, cache.head_dim), k.dtype
-    ld = _token_stride(k, shape)
-    if v.dtype != dtype or _token_stride(v, shape) != ld or dtype not in _DTYPE_CODES:
-        raise CoreInferError(ERR_INVALID_ARG, "k (%s) and v (%s) must have one type and the same spacing of tokens" % (dtype, v.dtype))
-    for t in (k_stored, v_stored):
-        if t is not None and (t.shape != shape or t.dtype != dtype or not t.is_contiguous()):
-            raise CoreInferError(ERR_INVALID_ARG, "k_stored and v_stored must be contiguous and shaped as k")
-    status = load().coreinfer_kv4_append(cache, k.data_ptr(), v.data_ptr(), _DTYPE_CODES[dtype], T, ld,
-                                         None if k_stored is None else k_stored.data_ptr(),
-                                         None if v_stored is None else v_stored.data_ptr(), _raw_stream(k, stream))
+    shape, dtype, H, D = k.shape, k.dtype, cache.kv_heads, cache.head_dim
+    T = shape[1] if len(shape) == 4 else 0
+    if shape != (cache.batch, T, H, D):
+        raise CoreInferError(ERR_INVALID_ARG, "k of shape %s does not fit the cache" % (tuple(shape),))
+    ld = H * D if k.is_contiguous() else _token_stride(k, shape)
+    if v.dtype != dtype or dtype not in _DTYPE_CODES or v.shape != shape or (H * D if v.is_contiguous() else _token_stride(v, shape)) != ld:
+        raise CoreInferError(ERR_INVALID_ARG, "k (%s) and v (%s) must have one type, shape and spacing of tokens" % (dtype, v.dtype))
+    ks = vs = None
+    if k_stored is not None:
+        if k_stored.shape != shape or k_stored.dtype != dtype or not k_stored.is_contiguous():
+            raise CoreInferError(ERR_INVALID_ARG, "k_stored must be contiguous and shaped as k")
+        ks = k_stored.data_ptr()
+    if v_stored is not None:
+        if v_stored.shape != shape or v_stored.dtype != dtype or not v_stored.is_contiguous():
+            raise CoreInferError(ERR_INVALID_ARG, "v_stored must be contiguous and shaped as v")
+        vs = v_stored.data_ptr()
+    status = load().coreinfer_kv4_append(cache, k.data_ptr(), v.data_ptr(), _DTYPE_CODES[dtype], T, ld, ks, vs, _raw_stream(k, stream))
     if status:
         _check(status)
 
