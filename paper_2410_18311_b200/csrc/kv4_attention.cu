@@ -31,9 +31,9 @@
 // Calls of more than eight bf16 rows per key head may take 16 rows per warp (attn_rpt): the codes are unpacked once for two
 // MMAs, and values enter as s c + o in fp16 (p itself instead of p s per group), under a power of two per slot that p makes
 // up for.  Three roundings of 2^-12, of p, o and the value, below bf16's 2^-9.
-// Measured (accumulating but for the last): 8 x 32 heads x 4001 bf16 38.7 us, 3200 GB/s, of which about 15 do not grow with the
+// Measured (accumulating but for the last): 8 x 32 heads x 4001 bf16 39 us, 3150 GB/s, of which about 15 do not grow with the
 // length (launches, the lists, starting and joining units, finishing); 16384 slots 127 us, 5000 GB/s, the slope 5400;
-// 6 sequences x 8 heads x 15 rows in groups of 32 x 9000 slots 50 us, bound by instruction issue and latency (640
+// 6 sequences x 8 heads x 15 rows in groups of 32 x up to 9000 slots 49 us, bound by instruction issue and latency (640
 // instructions per 16 slots and warp, 16 warps an SM); 2 x 8 heads x 4 fp16 rows x 130000 slots 57 us, 4200 GB/s.
 #include "kv4.cuh"
 

@@ -139,9 +139,9 @@ static coreinfer_status pick_append(const AppendArgs& a, const DeviceInfo& di, c
 // kv4_select_kernel, more than 16384 slots per CTA: the same with keys in shared memory, or read again for each pass, and
 // ballots; a warp owns a contiguous range of slots, so that list order is slot order.
 // kv4_move_kernel copies the listed slots, many CTAs per head.
-// All are bound by latency at the sizes of a decode step (append and few together 10.3 us for 8 sequences x 32 heads x 2049
+// All are bound by latency at the sizes of a decode step (append and few together 10.2 us for 8 sequences x 32 heads x 2049
 // slots, of which some 6 are two launches and the reads of the state), the moves by bytes after a prompt: 4 x 8 heads x
-// 16384 slots down to 2048 in another cache 17.7 us, about half of it the selection's barriers and three passes.
+// 16384 slots down to 2048 in another cache 16.9 us, about half of it the selection's barriers and three passes.
 constexpr int kEvictBins = 2048;
 constexpr int kEvictFew = 16;
 constexpr int kEvictKeysMost = 48 * 1024;   // keys a CTA holds in shared memory; more slots are read again for each pass
