@@ -1203,11 +1203,23 @@ __global__ void __launch_bounds__(kFinishThreads, 3) kv4_finish_kernel(const __g
 // -------------------------------------------------------------------------------- host --
 static inline size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// Rows per unit and units per key head for R query rows.
-static void attn_rows(int R, int rpt, int* RT, int* RU, int* RB)
+// Row tiles per unit, rows per unit and units per key head for R query rows: the split with the least work.  A tile of
+// rows costs the same wherever it is (its warps copy the codes for themselves, from L2), so padding decides over long caches; a unit
+// costs some tiles more, and the CTAs end apart by a tile of all the unit's rows.  (With as many rows per unit as eight
+// warps take: 16 sequences x 35 fp16 rows x 20000 slots 296 us, 173 now; 4 x 8 heads x 56 bf16 rows x 2000 64, 51 now.)
+static void attn_rows(const Kv4& c, int R, int rpt, int* RT, int* RU, int* RB)
 {
-    const int tiles = (R + rpt - 1) / rpt;
-    *RT = tiles > 4 && rpt < 16 ? 8 : (tiles > 2 ? 4 : tiles);               // of 16 rows: two warps per row tile at least
+    const int tiles = (R + rpt - 1) / rpt, slots = (c.cap + 255) / 256;
+    long long best = 0;
+    *RT = 0;
+    for (int rt = rpt < 16 ? 8 : 4; rt; rt >>= 1) {          // of 16 rows: two warps per row tile at least
+        const long long units = (tiles + rt - 1) / rt;
+        const long long cost = (long long)c.B * c.H * units * ((long long)rt * slots + 2 * kAttnUnitCost) + (long long)kAttnMaxCtas * rt;
+        if (*RT == 0 || cost < best) {
+            best = cost;
+            *RT = rt;
+        }
+    }
     *RU = *RT * rpt;
     *RB = (R + *RU - 1) / *RU;
 }
@@ -1218,7 +1230,7 @@ struct AttnLayout {
 static AttnLayout attn_layout(const Kv4& c, int R, int rpt)
 {
     int RT, RU, RB;
-    attn_rows(R, rpt, &RT, &RU, &RB);
+    attn_rows(c, R, rpt, &RT, &RU, &RB);
     AttnLayout w;
     w.ml = 0;
     w.o = w.ml + up256((size_t)kAttnMaxCtas * 2 * RU * sizeof(float2));
@@ -1355,7 +1367,7 @@ coreinfer_status coreinfer_kv4_attention(const coreinfer_kv4_cache* cache, const
     a.T = T;
     a.share = q_heads / a.c.H;
     a.R = (int)R;
-    attn_rows(a.R, rpt, &a.RT, &a.RU, &a.RB);
+    attn_rows(a.c, a.R, rpt, &a.RT, &a.RU, &a.RB);
     a.scale = scale;
     a.accumulate = accumulate ? 1 : 0;
     a.part_ml = (float2*)(ws + w.ml);
