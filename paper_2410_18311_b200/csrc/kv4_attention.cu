@@ -165,7 +165,7 @@ template <int MODE> constexpr int kAttnCentre = MODE == 2 ? 2 : 8;
 
 // Stages of a warp's ring: as many as two CTAs per SM (head_dim 256: one) leave room for.
 template <int D, int G, int MODE> constexpr int kAttnStages =
-    MODE == 3 ? (D == 64 ? 10 : 6) : D == 64 ? 9 : (D == 256 ? (G == 32 ? 6 : 8) : (G == 32 ? (MODE == 0 ? 7 : 9) : (MODE == 0 ? 4 : 5)));
+    MODE == 3 ? 6 : D == 64 ? 9 : (D == 256 ? (G == 32 ? 6 : 8) : (G == 32 ? (MODE == 0 ? 7 : 9) : (MODE == 0 ? 4 : 5)));
 
 // How far a logit (base 2) may exceed the running maximum before that is moved.  Rows change their maximum at different
 // pieces, and each change rescales all of a warp's outputs: of 15 rows, nearly every piece did (91 of 1100
@@ -532,7 +532,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                     }
                     float lo[UN][2][NV];
                     if constexpr (BOTH) {
-                        static_assert(!BOTH || UN == 1, "one piece of 16 slots at a time");
+                        static_assert(!BOTH || (UN == 1 && NG >= 4), "one piece of 16 slots at a time, pairs of a slot in two lanes");
                         const uint8_t *krow = kst + tok0 * CODE_ROW + tig * (D / 8), *kpr = kst + CODES + tok0 * PAIR_ROW;
                         uint32_t w0[D / 32], w1[D / 32], kp0[NG], kp1[NG];
                         ld_words<D / 32>(w0, krow);
@@ -541,10 +541,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                         ld_words<NG>(kp1, kpr + 8 * PAIR_ROW);
                         // o_g sum q of all groups in one MMA: offsets of groups 2 tig and 2 tig + 1 against the sums' two parts
                         uint32_t o0 = 0u, o1 = 0u;
-                        if (NG == 1) {
-                            o0 = tig == 0 ? kp0[0] >> 16 : 0u;
-                            o1 = tig == 0 ? kp1[0] >> 16 : 0u;
-                        } else if (2 * tig < NG) {
+                        if (2 * tig < NG) {
                             const uint2 p0 = *reinterpret_cast<const uint2*>(kpr + 8 * tig), p1 = *reinterpret_cast<const uint2*>(kpr + 8 * PAIR_ROW + 8 * tig);
                             o0 = __byte_perm(p0.x, p0.y, 0x7632);
                             o1 = __byte_perm(p1.x, p1.y, 0x7632);
@@ -697,28 +694,24 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                         }
                         // Every slot's pairs to a power of two: the largest s or |o| into [2^6, 2^7), so that 16 |s c + o| stays
                         // below 2^15; p takes the power, and its reference follows p 2^k.  A lane per half a slot.
-                        constexpr int PER = NG > 1 ? 2 : 1, WORDS = NG / PER;
-                        const int slot = lane / PER;
-                        if (PER == 2 || lane < 16) {
-                            uint32_t w[WORDS];
-                            uint32_t* const at = pairs + slot * NG + (PER == 2 ? (lane & 1) * WORDS : 0);
-                            ld_words<WORDS>(w, reinterpret_cast<const uint8_t*>(at));
-                            __half2 m = __habs2(as_half2(w[0]));
+                        constexpr int WORDS = NG / 2;
+                        const int slot = lane >> 1;
+                        uint32_t w[WORDS];
+                        uint32_t* const at = pairs + slot * NG + (lane & 1) * WORDS;
+                        ld_words<WORDS>(w, reinterpret_cast<const uint8_t*>(at));
+                        __half2 m = __habs2(as_half2(w[0]));
 #pragma unroll
-                            for (int i = 1; i < WORDS; ++i) m = __hmax2(m, __habs2(as_half2(w[i])));
-                            uint32_t bits = as_word(m) & 0xffffu;
-                            bits = bits > as_word(m) >> 16 ? bits : as_word(m) >> 16;
-                            if (PER == 2) {
-                                const uint32_t other = __shfl_xor_sync(0xffffffffu, bits, 1);
-                                bits = bits > other ? bits : other;
-                            }
-                            int e = (int)(bits >> 10);       // its exponent + 15; a NaN counts as nothing
-                            e = e == 31 || e < 6 ? 6 : e;
-                            const uint32_t factor = (uint32_t)(36 - e) * 0x04000400u;        // 2^(21 - e) twice
+                        for (int i = 1; i < WORDS; ++i) m = __hmax2(m, __habs2(as_half2(w[i])));
+                        uint32_t bits = as_word(m) & 0xffffu;
+                        bits = bits > as_word(m) >> 16 ? bits : as_word(m) >> 16;
+                        const uint32_t other = __shfl_xor_sync(0xffffffffu, bits, 1);
+                        bits = bits > other ? bits : other;
+                        int e = (int)(bits >> 10);           // its exponent + 15; a NaN counts as nothing
+                        e = e == 31 || e < 6 ? 6 : e;
+                        const uint32_t factor = (uint32_t)(36 - e) * 0x04000400u;            // 2^(21 - e) twice
 #pragma unroll
-                            for (int i = 0; i < WORDS; ++i) at[i] = as_word(__hmul2(as_half2(w[i]), as_half2(factor)));
-                            if (PER == 1 || (lane & 1) == 0) slot_power[slot] = make_float2((float)(e - 14), pow2(14 - e));
-                        }
+                        for (int i = 0; i < WORDS; ++i) at[i] = as_word(__hmul2(as_half2(w[i]), as_half2(factor)));
+                        if ((lane & 1) == 0) slot_power[slot] = make_float2((float)(e - 14), pow2(14 - e));
                         __syncwarp();
                         const float2 power[2] = {slot_power[tok0], slot_power[tok0 + 8]};
 #pragma unroll
