@@ -428,7 +428,8 @@ coreinfer_status coreinfer_w4_quantize(const void* w, coreinfer_dtype dtype, int
  *   y      device out [batch, N] in y_dtype (fp32 or `dtype`) with row stride ld_y; may be `mul`, not x
  * A gated FFN is two calls: g = act(W_gate x), then h = (W_up x) * g with mul = g.
  * An infinity or NaN in a row of x makes that row of y NaN or infinite as the formula says for at
- * least the outputs it reaches; other rows are not touched by it.
+ * least the outputs it reaches, through every activation; other rows are not touched by it.  (An
+ * infinity times the codes and times the offset of a group leaves a NaN in nearly all of them.)
  * Errors: INVALID_ARG, UNSUPPORTED (dtype, group, batch), CUDA. */
 coreinfer_status coreinfer_w4_matvec(const coreinfer_w4_matrix* w, const void* x, int32_t batch, int64_t ld_x,
                                      coreinfer_dtype dtype, coreinfer_act act,

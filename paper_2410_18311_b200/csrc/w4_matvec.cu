@@ -184,7 +184,7 @@ struct W4Args {
 
 __device__ __forceinline__ float w4_act(float v, int act)
 {
-    if (act == COREINFER_ACT_RELU) return fmaxf(v, 0.f);
+    if (act == COREINFER_ACT_RELU) return max_nan(v, 0.f);    // a NaN stays one, as in the other activations
     if (act == COREINFER_ACT_SILU) return v / (1.f + __expf(-v));
     return v;
 }

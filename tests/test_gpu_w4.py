@@ -170,3 +170,33 @@ def test_matvec_exact_integers():
         y = torch.empty(8, N, device="cuda")
         ci.coreinfer_w4_matvec(w4, torch.from_numpy(x).cuda().to(dt), ci.ACT_NONE, None, None, y)
         np.testing.assert_array_equal(y.cpu().numpy(), x @ w.T)
+
+
+@pytest.mark.parametrize("with_mul", [False, True])
+@pytest.mark.parametrize("act", ["none", "relu", "silu"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_matvec_nan_and_infinity_pass_every_activation(dtype, act, with_mul):
+    """A NaN or infinity in x leaves no finite output in its row, a NaN in the weights or the bias is NaN in its column,
+    whatever the activation; everything else is as it was."""
+    require_gpu()
+    N, K, group = 48, 640, 64
+    act = {"none": ci.ACT_NONE, "relu": ci.ACT_RELU, "silu": ci.ACT_SILU}[act]
+    g = torch.Generator(device="cuda").manual_seed(17)
+    w = torch.randn(N, K, generator=g, device="cuda") * 0.05
+    w[7, 130] = float("nan")
+    codes, pairs, w4 = lay_out(w, group)
+    x = torch.randn(5, K, generator=g, device="cuda")
+    x[1, 100], x[2, 639], x[3, 0] = float("inf"), float("nan"), float("-inf")
+    bias = torch.randn(N, generator=g, device="cuda")
+    bias[20] = float("nan")
+    x, bias = x.to(DT[dtype]), bias.to(DT[dtype])
+    m = torch.randn(5, N, generator=g, device="cuda").to(DT[dtype]) if with_mul else None
+    y = torch.zeros(5, N, dtype=DT[dtype], device="cuda")
+    ci.coreinfer_w4_matvec(w4, x, act, bias, m, y)
+    y = values_np(y)
+    assert not np.isfinite(y[1:4]).any()
+    assert np.isnan(y[:, [7, 20]]).all()
+    rows, cols = [0, 4], [n for n in range(N) if n not in (7, 20)]
+    ref, mass = reference(values_np(x).astype(np.float64)[rows], w4_layout(values_np(w), group)[2][cols], values_np(bias).astype(np.float64)[cols],
+                          act, None if m is None else values_np(m).astype(np.float64)[rows][:, cols])
+    check(y[rows][:, cols], ref, mass, 4.0, K, DT[dtype])
