@@ -699,14 +699,14 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                         uint32_t w[WORDS];
                         uint32_t* const at = pairs + slot * NG + (lane & 1) * WORDS;
                         ld_words<WORDS>(w, reinterpret_cast<const uint8_t*>(at));
-                        __half2 m = __habs2(as_half2(w[0]));
+                        __half2 m = __float2half2_rn(0.f);   // a NaN counts as nothing: of it and a number, the number is the larger one
 #pragma unroll
-                        for (int i = 1; i < WORDS; ++i) m = __hmax2(m, __habs2(as_half2(w[i])));
+                        for (int i = 0; i < WORDS; ++i) m = __hmax2(m, __habs2(as_half2(w[i])));
                         uint32_t bits = as_word(m) & 0xffffu;
                         bits = bits > as_word(m) >> 16 ? bits : as_word(m) >> 16;
                         const uint32_t other = __shfl_xor_sync(0xffffffffu, bits, 1);
                         bits = bits > other ? bits : other;
-                        int e = (int)(bits >> 10);           // its exponent + 15; a NaN counts as nothing
+                        int e = (int)(bits >> 10);           // its exponent + 15; 31 (an infinity) is not in the format
                         e = e == 31 || e < 6 ? 6 : e;
                         const uint32_t factor = (uint32_t)(36 - e) * 0x04000400u;            // 2^(21 - e) twice
 #pragma unroll

@@ -416,3 +416,26 @@ def test_offsets_beyond_32_bits():
     for name in big:
         if name != "state":
             assert torch.equal(big[name][:, :, :40], small[name][:, :, :40]), name
+
+
+@pytest.mark.parametrize("D,group,bad", [(128, 32, (0, 1)), (128, 32, (2, 3)), (128, 32, (0, 1, 3)), (256, 64, (0, 1)), (256, 32, (0, 1, 2, 3)), (256, 32, (4, 5, 6, 7))])
+def test_attention_many_rows_nan_groups_of_a_value(D, group, bad):
+    """NaN in neighbouring groups of one value that every row sees: its outputs there are NaN, the other groups' are as
+    exact as ever (large offsets beside it: a factor chosen from the NaN would take them out of range)."""
+    require_gpu()
+    n, share = 37, 12
+    ref = CacheRef(1, 2, 48, D, group, np.random.default_rng(23))
+    ref.set_lengths([n])
+    ref.s[1], ref.o[1] = (ref.s[1] * 100).astype(np.float16), (ref.o[1] * 100).astype(np.float16)
+    d = ref.to_cuda()
+    before = ref.weight.copy()
+    q = torch.from_numpy(np.random.default_rng(24).standard_normal((1, 1, 2 * share, D)).astype(np.float32)).cuda().bfloat16()
+    want = attend(ref, ref.to_cuda(), q)
+    for g in bad:
+        d["v_pairs"][0, 1, 5, g] = float("nan")
+    out = attend(ref, d, q)
+    lost = torch.zeros(out.shape, dtype=torch.bool, device="cuda")
+    for g in bad:
+        lost[0, 0, share:, g * group:(g + 1) * group] = True
+    assert torch.isnan(out[lost]).all() and torch.isfinite(out[~lost]).all()
+    check_attention(ref, d, q, torch.where(lost, want, out), D ** -0.5, before, roundings=3)
