@@ -491,7 +491,8 @@ coreinfer_status coreinfer_kv4_append(const coreinfer_kv4_cache* cache, const vo
  * Sums, maxima and accumulated weights are fp32 in a fixed order (the same call gives the same bits).
  *   q        device, token t of sequence b at (b * T + t) * ld_q, [q_heads][head_dim] contiguous, in
  *            `dtype`; 16-byte aligned, ld_q * element size a multiple of 16.  out likewise with ld_out.
- *   workspace  device, 16-byte aligned, at least coreinfer_kv4_attention_workspace_bytes() (0 on bad sizes)
+ *   workspace  device, 16-byte aligned, at least coreinfer_kv4_attention_workspace_bytes() (0 on bad sizes), which
+ *              covers every dtype and every call with up to T tokens: one sized for the most tokens serves all
  * Errors: INVALID_ARG, UNSUPPORTED (as for append; more than 2048 query rows T * q_heads / kv_heads per key head; 2^32
  * slots batch * kv_heads * capacity or more), WORKSPACE, CUDA. */
 size_t coreinfer_kv4_attention_workspace_bytes(const coreinfer_kv4_cache* cache, int32_t q_heads, int32_t T);

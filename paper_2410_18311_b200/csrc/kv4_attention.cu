@@ -1313,13 +1313,15 @@ size_t coreinfer_kv4_attention_workspace_bytes(const coreinfer_kv4_cache* cache,
     Kv4 c;
     if (kv4_take(cache, "the", &c) != COREINFER_OK) return 0;
     if (q_heads < 1 || T < 1 || q_heads % c.H != 0 || T > COREINFER_KV4_MAX_QUERIES) return 0;
-    const long long R = (long long)(q_heads / c.H) * T;
-    if (R > kAttnMaxRows) return 0;
+    if ((long long)(q_heads / c.H) * T > kAttnMaxRows) return 0;
+    // Fewer rows may take more of them per unit, and the parts of cut units then more bytes: the largest over all types and up to
+    // T tokens, so that one workspace serves every shorter call.
     size_t most = 0;
-    for (int rpt = 4; rpt <= 16; rpt *= 2) {
-        const size_t n = attn_layout(c, (int)R, rpt).total;
-        if (n > most) most = n;
-    }
+    for (int t = 1; t <= T; ++t)
+        for (int rpt = 4; rpt <= 16; rpt *= 2) {
+            const size_t n = attn_layout(c, q_heads / c.H * t, rpt).total;
+            if (n > most) most = n;
+        }
     return most;
 }
 
@@ -1345,12 +1347,11 @@ coreinfer_status coreinfer_kv4_attention(const coreinfer_kv4_cache* cache, const
     if (accumulate && !a.c.weight) CI_FAIL(COREINFER_ERR_INVALID_ARG, "accumulate needs a cache with weight and position");
     if (!(scale == scale) || scale - scale != 0.f) CI_FAIL(COREINFER_ERR_INVALID_ARG, "scale is not a finite number");
     if (!workspace || !aligned16(workspace)) CI_FAIL(COREINFER_ERR_WORKSPACE, "workspace is NULL or misaligned");
-    const size_t need = coreinfer_kv4_attention_workspace_bytes(cache, q_heads, T);
-    if (workspace_bytes < need) CI_FAIL(COREINFER_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
+    const int rpt = attn_rpt(dtype, R, a.c.D / a.c.G);
+    const AttnLayout w = attn_layout(a.c, (int)R, rpt);      // what this call needs, at most what the query says
+    if (workspace_bytes < w.total) CI_FAIL(COREINFER_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, w.total);
     DeviceInfo di;
     if ((s = device_info(&di)) != COREINFER_OK) return s;
-    const int rpt = attn_rpt(dtype, R, a.c.D / a.c.G);
-    const AttnLayout w = attn_layout(a.c, (int)R, rpt);
     uint8_t* ws = (uint8_t*)workspace;
     a.q = q;
     a.out = out;

@@ -439,3 +439,20 @@ def test_attention_many_rows_nan_groups_of_a_value(D, group, bad):
         lost[0, 0, share:, g * group:(g + 1) * group] = True
     assert torch.isnan(out[lost]).all() and torch.isfinite(out[~lost]).all()
     check_attention(ref, d, q, torch.where(lost, want, out), D ** -0.5, before, roundings=3)
+
+
+@pytest.mark.parametrize("share", [3, 7])
+def test_attention_one_workspace_for_every_number_of_tokens(share):
+    """A workspace of the size asked for at 16 tokens serves calls with fewer."""
+    require_gpu()
+    B, H, D, cap = 8, 4 if share == 7 else 12, 128, 32 if share == 3 else 1024
+    ref = CacheRef(B, H, cap, D, 64, np.random.default_rng(share))
+    ref.set_lengths([min(cap, 20 + 3 * b) for b in range(B)])
+    d = ref.to_cuda()
+    h = handle(d)
+    ws = scratch(ci.coreinfer_kv4_attention_workspace_bytes(h, H * share, ci.KV4_MAX_QUERIES))
+    for T in (1, 6, 8, 10, 12, 15, 16):
+        q = torch.from_numpy(np.random.default_rng(T).standard_normal((B, T, H * share, D)).astype(np.float32)).cuda().bfloat16()
+        out = torch.full_like(q, float("nan"))
+        ci.coreinfer_kv4_attention(h, q, D ** -0.5, out, False, ws)
+        check_attention(ref, d, q, out, D ** -0.5, None)

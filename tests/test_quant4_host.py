@@ -128,3 +128,14 @@ def test_binding_checks_shapes():
         ci.coreinfer_kv4_append(c, z(2, 1, 2, 64), z(2, 1, 2, 64).transpose(1, 2).reshape(2, 1, 2, 64)[:, :, :, :32])
     with pytest.raises(ci.CoreInferError):
         ci.coreinfer_kv4_append(c, z(2, 3, 3, 64)[:, :, :2].transpose(0, 1), z(2, 3, 3, 64)[:, :, :2].transpose(0, 1))
+
+
+def test_attention_workspace_does_not_shrink_with_more_tokens(lib):
+    """One workspace of the size asked for at the most tokens serves every shorter call."""
+    for B in (1, 2, 8, 64):
+        for H in (1, 4, 12, 32):
+            for share in (1, 2, 3, 5, 7, 8, 16, 40):
+                for D, group, capacity in ((64, 32, 16), (128, 64, 32), (128, 32, 1024), (256, 32, 9008)):
+                    c = cache(batch=B, kv_heads=H, capacity=capacity, head_dim=D, group=group)
+                    sizes = [ci.coreinfer_kv4_attention_workspace_bytes(c, H * share, T) for T in range(1, 17)]
+                    assert sizes[0] > 0 and sizes == sorted(sizes), (B, H, share, D, group, capacity)
