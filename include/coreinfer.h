@@ -452,6 +452,7 @@ coreinfer_status coreinfer_w4_matvec(const coreinfer_w4_matrix* w, const void* x
  * `state[b][0]` may hold anything. */
 #define COREINFER_KV4_MAX_BATCH 1024
 #define COREINFER_KV4_MAX_QUERIES 16
+#define COREINFER_KV4_MAX_ROWS 2048      /* query rows T * q_heads / kv_heads per key head */
 
 typedef struct {
     void* k_codes;
@@ -493,7 +494,7 @@ coreinfer_status coreinfer_kv4_append(const coreinfer_kv4_cache* cache, const vo
  *            `dtype`; 16-byte aligned, ld_q * element size a multiple of 16.  out likewise with ld_out.
  *   workspace  device, 16-byte aligned, at least coreinfer_kv4_attention_workspace_bytes() (0 on bad sizes), which
  *              covers every dtype and every call with up to T tokens: one sized for the most tokens serves all
- * Errors: INVALID_ARG, UNSUPPORTED (as for append; more than 2048 query rows T * q_heads / kv_heads per key head; 2^32
+ * Errors: INVALID_ARG, UNSUPPORTED (as for append; more than COREINFER_KV4_MAX_ROWS query rows per key head; 2^32
  * slots batch * kv_heads * capacity or more), WORKSPACE, CUDA. */
 size_t coreinfer_kv4_attention_workspace_bytes(const coreinfer_kv4_cache* cache, int32_t q_heads, int32_t T);
 

@@ -18,7 +18,7 @@ F32, BF16, F16 = 0, 1, 2
 FFN_RELU, FFN_RELU_GATED, FFN_SILU_GATED = 0, 1, 2
 ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
 MAX_BATCH, MAX_LAYERS = 8, 128
-KV4_MAX_BATCH, KV4_MAX_QUERIES = 1024, 16
+KV4_MAX_BATCH, KV4_MAX_QUERIES, KV4_MAX_ROWS = 1024, 16, 2048
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT = range(6)
 
 # every symbol include/coreinfer.h declares

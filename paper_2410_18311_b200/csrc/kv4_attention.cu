@@ -1300,7 +1300,8 @@ static coreinfer_status pick_attention(AttnArgs& a, const DeviceInfo& di, cudaSt
                    : (G == 64 ? launch_attention<T, 256, 64>(a, di, st) : launch_attention<T, 256, 128>(a, di, st));
 }
 
-constexpr int kAttnMaxRows = 2048;          // query rows per key head (they sit in shared memory of the finishing kernel)
+// The finishing kernel holds 12 bytes per query row in shared memory that needs no opt-in.
+static_assert(COREINFER_KV4_MAX_ROWS * (sizeof(float2) + sizeof(int)) <= 48 * 1024, "rows of the finishing kernel");
 
 }  // namespace coreinfer
 
@@ -1313,7 +1314,7 @@ size_t coreinfer_kv4_attention_workspace_bytes(const coreinfer_kv4_cache* cache,
     Kv4 c;
     if (kv4_take(cache, "the", &c) != COREINFER_OK) return 0;
     if (q_heads < 1 || T < 1 || q_heads % c.H != 0 || T > COREINFER_KV4_MAX_QUERIES) return 0;
-    if ((long long)(q_heads / c.H) * T > kAttnMaxRows) return 0;
+    if ((long long)(q_heads / c.H) * T > COREINFER_KV4_MAX_ROWS) return 0;
     // Fewer rows may take more of them per unit, and the parts of cut units then more bytes: the largest over all types and up to
     // T tokens, so that one workspace serves every shorter call.
     size_t most = 0;
@@ -1339,7 +1340,7 @@ coreinfer_status coreinfer_kv4_attention(const coreinfer_kv4_cache* cache, const
     if (q_heads < 1 || q_heads % a.c.H != 0)
         CI_FAIL(COREINFER_ERR_INVALID_ARG, "q_heads %d is not a multiple of kv_heads %d", q_heads, a.c.H);
     const long long R = (long long)(q_heads / a.c.H) * T;
-    if (R > kAttnMaxRows) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "%lld query rows per key head: at most %d", R, kAttnMaxRows);
+    if (R > COREINFER_KV4_MAX_ROWS) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "%lld query rows per key head: at most %d", R, COREINFER_KV4_MAX_ROWS);
     if (!q || !out || !aligned16(q) || !aligned16(out)) CI_FAIL(COREINFER_ERR_INVALID_ARG, "q / out NULL or not 16-byte aligned");
     const int64_t row = (int64_t)q_heads * a.c.D, e = (int64_t)dtype_size(dtype);
     if (ld_q < row || ld_out < row || (ld_q * e) % 16 != 0 || (ld_out * e) % 16 != 0)

@@ -118,7 +118,9 @@ class KV4Cache:
         self.weight, self.position = new(dtype=torch.float32), new(dtype=torch.int32)
         self.state = torch.zeros(batch, 4, dtype=torch.int32, device=device)
         self.cache = B.make_kv4_cache(self.k_codes, self.k_pairs, self.v_codes, self.v_pairs, self.state, self.weight, self.position)
-        need = max(B.coreinfer_kv4_attention_workspace_bytes(self.cache, q_heads, B.KV4_MAX_QUERIES),
+        # tokens of one attend() at most: with many query heads per key head the rows are the limit
+        self.max_tokens = min(B.KV4_MAX_QUERIES, B.KV4_MAX_ROWS * kv_heads // q_heads)
+        need = max(B.coreinfer_kv4_attention_workspace_bytes(self.cache, q_heads, self.max_tokens),
                    B.coreinfer_kv4_evict_workspace_bytes(self.cache))
         self.ws = torch.empty(need, dtype=torch.uint8, device=device)
 
@@ -188,7 +190,7 @@ class Core4Layer:
         ctx = torch.nn.functional.scaled_dot_product_attention(q.transpose(1, 2), k_stored.transpose(1, 2), v_stored.transpose(1, 2),
                                                                is_causal=True, enable_gqa=Hq != H).transpose(1, 2)
         h += torch.nn.functional.linear(ctx.reshape(self.batch, T, Hq * D), self.w_o)
-        seen = min(T, B.KV4_MAX_QUERIES)
+        seen = min(T, self.cache.max_tokens)
         last = q[:, T - seen:].contiguous()
         self.cache.attend(last, torch.empty_like(last))      # for its weights
         self.cache.evict(self.budget, self.recent, self.first)

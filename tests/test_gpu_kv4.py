@@ -456,3 +456,24 @@ def test_attention_one_workspace_for_every_number_of_tokens(share):
         out = torch.full_like(q, float("nan"))
         ci.coreinfer_kv4_attention(h, q, D ** -0.5, out, False, ws)
         check_attention(ref, d, q, out, D ** -0.5, None)
+
+
+def test_cache_object_with_many_query_heads():
+    """200 query heads on one key head: ten tokens a call at most, and a workspace for them."""
+    require_gpu()
+    from paper_2410_18311_b200.pipeline import KV4Cache
+    Hq, D = 200, 64
+    cache = KV4Cache(1, Hq, 1, 32, D, 32)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    k, v = (torch.randn(1, 20, 1, D, generator=g, device="cuda") for _ in "kv")
+    ks, vs = torch.empty_like(k), torch.empty_like(v)
+    cache.append(k, v, ks, vs)
+    for T in (1, cache.max_tokens):
+        q = torch.randn(1, T, Hq, D, generator=g, device="cuda")
+        out = torch.empty_like(q)
+        cache.attend(q, out)
+        mask = torch.arange(20, device="cuda") > 20 - T + torch.arange(T, device="cuda")[:, None]
+        p = torch.einsum("bthd,bnod->bthn", q.double(), ks.double()) * D ** -0.5
+        p = torch.softmax(p.masked_fill(mask[None, :, None], float("-inf")), -1)
+        # fp32 stored values carry one rounding (2^-24), the kernel about 2^-20 in p: 1e-5 of values of some units is above both
+        assert (out - torch.einsum("bthn,bnod->bthd", p, vs.double())).abs().max() < 1e-5 * 8

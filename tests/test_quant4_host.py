@@ -139,3 +139,13 @@ def test_attention_workspace_does_not_shrink_with_more_tokens(lib):
                     c = cache(batch=B, kv_heads=H, capacity=capacity, head_dim=D, group=group)
                     sizes = [ci.coreinfer_kv4_attention_workspace_bytes(c, H * share, T) for T in range(1, 17)]
                     assert sizes[0] > 0 and sizes == sorted(sizes), (B, H, share, D, group, capacity)
+
+
+@pytest.mark.parametrize("q_heads,kv_heads", [(4, 4), (128, 1), (129, 1), (200, 1), (512, 2), (2048, 1)])
+def test_cache_object_has_room_for_every_call(lib, q_heads, kv_heads):
+    """Above 128 query heads per key head the limit on rows, and not the 16 tokens, bounds a call."""
+    from paper_2410_18311_b200.pipeline import KV4Cache
+    c = KV4Cache(1, q_heads, kv_heads, 32, 64, 32, device="cpu")
+    assert c.max_tokens == max(T for T in range(1, 17) if T * q_heads // kv_heads <= ci.KV4_MAX_ROWS)
+    for T in range(1, c.max_tokens + 1):
+        assert 0 < ci.coreinfer_kv4_attention_workspace_bytes(c.cache, q_heads, T) <= c.ws.numel()
