@@ -45,8 +45,10 @@ constexpr int kAttnWarps = 8;
 constexpr int kAttnThreads = 32 * kAttnWarps;
 // Slots per tile (a piece per warp): pieces of 32, so that waits, votes and addresses are paid once per 32 slots; of 16
 // where registers (head_dim 128 in groups of 32) or shared memory (256) do not carry two.
-template <int D, int G, int MODE> constexpr int kAttnTile = MODE == 3 || D == 256 || (D == 128 && G == 32) ? 128 : 256;
+constexpr int kAttnTile16 = 128;
+template <int D, int G, int MODE> constexpr int kAttnTile = MODE == 3 ? kAttnTile16 : (D == 256 || (D == 128 && G == 32) ? 128 : 256);
 constexpr int kAttnMaxCtas = 320;
+constexpr size_t kAttnSmemRoom = 226 * 1024;                 // dynamic shared memory of a CTA on sm_100a, beside 1 KB
 constexpr float kNoLogit = -1e30f;
 // A unit counts this many tiles more than it has when the list is cut: about what starting it costs a CTA (its query
 // rows, the join of its warps).  Measured at 8 sequences x 32 heads x 4096 slots: CTAs with two units ended 3 to 6 us
@@ -164,8 +166,9 @@ __device__ __forceinline__ int opaque_zero()
 template <int MODE> constexpr int kAttnCentre = MODE == 2 ? 2 : 8;
 
 // Stages of a warp's ring: as many as two CTAs per SM (head_dim 256: one) leave room for.
+constexpr int kAttnStages16 = 6;
 template <int D, int G, int MODE> constexpr int kAttnStages =
-    MODE == 3 ? 6 : D == 64 ? 9 : (D == 256 ? (G == 32 ? 6 : 8) : (G == 32 ? (MODE == 0 ? 7 : 9) : (MODE == 0 ? 4 : 5)));
+    MODE == 3 ? kAttnStages16 : D == 64 ? 9 : (D == 256 ? (G == 32 ? 6 : 8) : (G == 32 ? (MODE == 0 ? 7 : 9) : (MODE == 0 ? 4 : 5)));
 
 // How far a logit (base 2) may exceed the running maximum before that is moved.  Rows change their maximum at different
 // pieces, and each change rescales all of a warp's outputs: of 15 rows, nearly every piece did (91 of 1100
@@ -1196,6 +1199,16 @@ __global__ void __launch_bounds__(kFinishThreads, 3) kv4_finish_kernel(const __g
 // -------------------------------------------------------------------------------- host --
 static inline size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 
+// Shared memory of the main kernel: rings, the join of the warps, the laid-out query rows of `query_tiles` row tiles (16-row form
+// only: 0 elsewhere) and the lists of sequences.
+static inline size_t attn_smem(const Kv4& c, int stages, int tile, int join_rows, int query_tiles)
+{
+    const size_t ring = (size_t)stages * (tile / kAttnWarps) * (c.D / 2 + c.D / c.G * 4);
+    const size_t query = 2 * (c.D / 32) * 512 + 2 * 256 + 16 * 8;
+    return kAttnWarps * (ring + join_rows * (c.D * sizeof(float) + sizeof(float2))) +
+           (query_tiles ? query_tiles * query + kAttnWarps * 16 * sizeof(float2) : 0) + (3 * c.B + 1) * sizeof(int);
+}
+
 // Row tiles per unit, rows per unit and units per key head for R query rows: the split with the least work.  A tile of
 // rows costs the same wherever it is (its warps copy the codes for themselves, from L2), so padding decides over long caches; a unit
 // costs some tiles more, and the CTAs end apart by a tile of all the unit's rows.  (With as many rows per unit as eight
@@ -1206,6 +1219,8 @@ static void attn_rows(const Kv4& c, int R, int rpt, int* RT, int* RU, int* RB)
     long long best = 0;
     *RT = 0;
     for (int rt = rpt < 16 ? 8 : 4; rt; rt >>= 1) {          // of 16 rows: two warps per row tile at least
+        // where the rows of four tiles do not fit beside the lists of many sequences (head_dim 256 in groups of 32 from batch 512 on)
+        if (rpt == 16 && rt > 1 && attn_smem(c, kAttnStages16, kAttnTile16, 8, rt) > kAttnSmemRoom) continue;
         const long long units = (tiles + rt - 1) / rt;
         const long long cost = (long long)c.B * c.H * units * ((long long)rt * slots + 2 * kAttnUnitCost) + (long long)kAttnMaxCtas * rt;
         if (*RT == 0 || cost < best) {
@@ -1237,10 +1252,9 @@ static AttnLayout attn_layout(const Kv4& c, int R, int rpt)
 template <typename T, int D, int G, int MODE>
 static coreinfer_status launch_mode(AttnArgs& a, const DeviceInfo& di, cudaStream_t st)
 {
-    constexpr int NG = D / G, TILE = kAttnTile<D, G, MODE>;
-    const size_t ring = (size_t)kAttnStages<D, G, MODE> * (TILE / kAttnWarps) * (D / 2 + NG * 4);
-    const size_t smem = kAttnWarps * (ring + kAttnJoinRows<MODE> * (D * sizeof(float) + sizeof(float2))) +
-                        (MODE == kRows16 ? a.RT * kAttnQueryBytes<D> + kAttnWarps * 16 * sizeof(float2) : 0) + (3 * a.c.B + 1) * sizeof(int);
+    constexpr int TILE = kAttnTile<D, G, MODE>;
+    static_assert(kAttnQueryBytes<D> == 2 * (D / 32) * 512 + 2 * 256 + 16 * 8 && kAttnJoinRows<kRows16> == 8, "attn_smem and attn_rows");
+    const size_t smem = attn_smem(a.c, kAttnStages<D, G, MODE>, TILE, kAttnJoinRows<MODE>, MODE == kRows16 ? a.RT : 0);
     // two CTAs per SM where registers (head_dim up to 128) and shared memory (batch up to some hundreds) allow it
     const int per_sm = D <= 128 && 2 * (smem + 1024 + 64) <= (size_t)di.smem_optin + 1024 ? 2 : 1;
     if (smem > smem_room(di)) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "not enough shared memory");

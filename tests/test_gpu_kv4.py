@@ -477,3 +477,17 @@ def test_cache_object_with_many_query_heads():
         p = torch.softmax(p.masked_fill(mask[None, :, None], float("-inf")), -1)
         # fp32 stored values carry one rounding (2^-24), the kernel about 2^-20 in p: 1e-5 of values of some units is above both
         assert (out - torch.einsum("bthn,bnod->bthd", p, vs.double())).abs().max() < 1e-5 * 8
+
+
+@pytest.mark.parametrize("D,group,share", [(256, 32, 64), (256, 32, 9), (256, 64, 64), (128, 32, 64)])
+def test_attention_many_rows_of_the_largest_batch(D, group, share):
+    """1024 sequences (the header's limit) with many bf16 rows: the lists of sequences take shared memory too."""
+    require_gpu()
+    B = ci.KV4_MAX_BATCH
+    rng = np.random.default_rng(D + share)
+    ref = CacheRef(B, 1, 16, D, group, rng)
+    ref.set_lengths(rng.integers(0, 17, size=B).tolist())
+    d = ref.to_cuda()
+    before = ref.weight.copy()
+    q = torch.from_numpy(rng.standard_normal((B, 1, share, D)).astype(np.float32)).cuda().bfloat16()
+    check_attention(ref, d, q, attend(ref, d, q), D ** -0.5, before, roundings=3)
