@@ -446,7 +446,8 @@ coreinfer_status coreinfer_w4_matvec(const coreinfer_w4_matrix* w, const void* x
  *   position          [batch][kv_heads][capacity] int32: which token of the sequence a slot holds
  *                     (weight and position both NULL for a cache that is never evicted from)
  *   state             [batch][4] int32: slots in use, tokens ever appended, tokens refused because
- *                     they did not fit, scratch.  All zero = empty; zero it to start new sequences.
+ *                     they did not fit, scratch (0 between calls: append and eviction in place count
+ *                     their thread blocks in it).  All zero = empty; zero it to start new sequences.
  * head_dim is 64, 128 or 256, group 32, 64 or 128 and at most head_dim, capacity a multiple of 16,
  * batch at most COREINFER_KV4_MAX_BATCH, kv_heads at most 1024 (otherwise UNSUPPORTED).  Slots beyond the first
  * `state[b][0]` may hold anything. */
@@ -509,8 +510,9 @@ coreinfer_status coreinfer_kv4_attention(const coreinfer_kv4_cache* cache, const
  *   dst == src (the same buffers): in place.  Kept slots below the new length stay where they are; the
  *     kept ones above it move, in ascending order, into the free ones below it.
  *   dst another cache of the same batch, kv_heads, head_dim and group, with capacity >= min(budget,
- *     src capacity): the kept slots are copied in ascending slot order; src is not changed; slots of
- *     dst beyond the new length are not written.
+ *     src capacity): the kept slots are copied in ascending slot order; src is not written at all, so
+ *     that calls which only read it may run beside this one (each with its own workspace); slots of dst
+ *     beyond the new length are not written.
  *   state[b][0] of dst becomes the new length, state[b][1] is taken over.
  * Errors: INVALID_ARG, UNSUPPORTED (as for append; batch * kv_heads above 65535), WORKSPACE, CUDA. */
 size_t coreinfer_kv4_evict_workspace_bytes(const coreinfer_kv4_cache* src);

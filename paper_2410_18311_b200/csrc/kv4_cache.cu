@@ -287,6 +287,16 @@ __global__ void __launch_bounds__(1024) kv4_evict_few_kernel(const __grid_consta
     if (kv4_last_of_sequence(a, b, gridDim.x)) a.state[b * 4 + kStateLength] = keep;
 }
 
+// The new length, by one thread of a sequence's CTAs.  In place it waits until all of them have read the old one; another cache's
+// state is read by none, and nothing of the source is written: other calls may be reading it.
+__device__ __forceinline__ void set_length(const EvictArgs& e, int b, int keep, int seen)
+{
+    if (e.in_place ? kv4_last_of_sequence(e.a, b, gridDim.x) : blockIdx.x == 0 && threadIdx.x == 0) {
+        e.z.state[b * 4 + kStateLength] = keep;
+        e.z.state[b * 4 + kStateSeen] = seen;
+    }
+}
+
 // Sum over the block's warps before this one, and over all of them.
 __device__ __forceinline__ int warps_before(int v, int* buf, int warp, int warps, int* total)
 {
@@ -501,10 +511,7 @@ __global__ void __launch_bounds__(1024) kv4_select_held_kernel(const __grid_cons
     cluster_sync(size);                                     // the lists are complete, and no CTA ends while another may still write to its shared memory
     let_next_start();
     if (e.move_here) move_slots(a, base, e.z, base, e.lists + base + a.cap / 2, e.lists + base, movers, tid, blockDim.x);
-    if (kv4_last_of_sequence(a, b, gridDim.x)) {
-        e.z.state[b * 4 + kStateLength] = keep;
-        e.z.state[b * 4 + kStateSeen] = seen;
-    }
+    set_length(e, b, keep, seen);
 }
 
 // The selection for heads of any length: keys in shared memory, or read again for each pass.
@@ -642,10 +649,7 @@ __global__ void __launch_bounds__(1024) kv4_select_kernel(const __grid_constant_
     if (tid == 0 && rank == 0) e.counts[b * a.H + h] = movers;
     cluster_sync(size);                                     // no CTA ends while another may still write to its shared memory
     let_next_start();
-    if (kv4_last_of_sequence(a, b, gridDim.x)) {
-        e.z.state[b * 4 + kStateLength] = keep;
-        e.z.state[b * 4 + kStateSeen] = seen;
-    }
+    set_length(e, b, keep, seen);
 }
 
 __global__ void __launch_bounds__(kMoveThreads) kv4_move_kernel(const __grid_constant__ EvictArgs e)

@@ -491,3 +491,44 @@ def test_attention_many_rows_of_the_largest_batch(D, group, share):
     before = ref.weight.copy()
     q = torch.from_numpy(rng.standard_normal((B, 1, share, D)).astype(np.float32)).cuda().bfloat16()
     check_attention(ref, d, q, attend(ref, d, q), D ** -0.5, before, roundings=3)
+
+
+@pytest.mark.parametrize("length,budget", [(100, 40), (30, 40), (5000, 1000), (40000, 700)])
+def test_evict_to_another_cache_leaves_the_source_alone(length, budget):
+    """Another call may be reading the source, or counting in its scratch word: nothing of it is used or changed."""
+    require_gpu()
+    H = 3
+    ref = CacheRef(1, H, -(-length // 16) * 16, 64, 64, np.random.default_rng(length))
+    ref.set_lengths([length])
+    d = ref.to_cuda()
+    d["state"][:, 3] = 1
+    small = CacheRef(1, H, -(-budget // 16) * 16, 64, 64, np.random.default_rng(1))
+    z = small.to_cuda()
+    evict(handle(d), handle(z), budget, 10, 2)
+    ref.evict_to(small, budget, 10, 2)
+    small.assert_equal(z)
+    assert d["state"].tolist() == [[length, length, 0, 1]]
+
+
+def test_evict_from_one_source_on_two_streams():
+    require_gpu()
+    B, H, n, budgets = 2, 16, 4000, (1500, 400)
+    ref = CacheRef(B, H, n, 64, 64, np.random.default_rng(31))
+    ref.set_lengths([n, n - 123])
+    d = ref.to_cuda()
+    src = handle(d)
+    wants, runs = [], []
+    for budget in budgets:
+        small = CacheRef(B, H, -(-budget // 16) * 16, 64, 64, np.random.default_rng(budget))
+        z = small.to_cuda()
+        ref.evict_to(small, budget, 64, 4)
+        wants.append(small)
+        runs.append((budget, z, handle(z), scratch(ci.coreinfer_kv4_evict_workspace_bytes(src)), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for budget, _, dst, ws, stream in runs:
+            ci.coreinfer_kv4_evict(src, dst, budget, 64, 4, ws, stream=stream)
+    torch.cuda.synchronize()
+    for small, (_, z, _, _, _) in zip(wants, runs):
+        small.assert_equal(z)
+    ref.assert_equal(d)
