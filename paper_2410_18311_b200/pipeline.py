@@ -180,8 +180,11 @@ class Core4Layer:
 
     def prompt(self, h):
         """h [batch, T, d] fp32, the prompts' residual stream: updated in place.  Fills the cache, lets the last
-        tokens' attention decide which slots the budget keeps, and fixes the core set."""
+        tokens' attention decide which slots the budget keeps, and fixes the core set.  T is at most what the cache holds."""
         cfg, T, (Hq, H, D) = self.cfg, h.shape[1], self.heads
+        if h.shape != (self.batch, T, cfg.d_model) or not 1 <= T <= self.cache.cache.capacity:
+            raise B.CoreInferError(B.ERR_INVALID_ARG, "a prompt of shape %s: %d sequences of 1 to %d tokens were expected"
+                                   % (tuple(h.shape), self.batch, self.cache.cache.capacity))
         q, k, v = self._split(torch.nn.functional.linear(self._norm(h), self.w_qkv), T)
         self.cache.state.zero_()
         k_stored, v_stored = (torch.empty(self.batch, T, H, D, dtype=k.dtype, device=h.device) for _ in range(2))

@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+import paper_2410_18311_b200 as ci
 from helpers import require_gpu
 from paper_2410_18311_b200.pipeline import Core4Layer
 from paper_2410_18311_b200.workloads import CONFIGS, layer_weights
@@ -105,4 +106,27 @@ def test_layer(gated, heads, group):
                 n = pos[b, j].tolist().index(gone.pop())
                 free = [i for i in range(budget + 1) if 2 <= pos[b, j, i] < seen - 6]
                 assert n in free and total[b, j, n] <= total[b, j, free].min() * (1 + 2.0 ** -5)
+    layer.cache.check()
+
+
+def small_layer(max_prompt=40, budget=24, batch=2):
+    cfg = CONFIGS["tiny"].with_(gated=True)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    new = lambda *s: (torch.randn(s, generator=g, device="cuda") * 0.06).to(cfg.torch_dtype)  # noqa: E731
+    return Core4Layer(cfg, batch, 4, 2, 64, budget, (new(8 * 64, cfg.d_model), new(cfg.d_model, 4 * 64)) + layer_weights(cfg, 0, "cuda"),
+                      recent=6, first=2, max_prompt=max_prompt, cache_group=32), cfg
+
+
+def test_prompt_longer_than_the_cache_is_refused():
+    """Nothing is computed and nothing of the cache changes, instead of attention over a cache that refused the tokens."""
+    require_gpu()
+    layer, cfg = small_layer(max_prompt=40)
+    layer.prompt(torch.randn(2, 40, cfg.d_model, device="cuda"))
+    state, core = layer.cache.state.clone(), layer.core_idx.clone()
+    h = torch.randn(2, 49, cfg.d_model, device="cuda")
+    before = h.clone()
+    with pytest.raises(ci.CoreInferError):
+        layer.prompt(h)
+    assert torch.equal(h, before) and torch.equal(layer.cache.state, state) and torch.equal(layer.core_idx, core)
+    layer.step(torch.randn(2, cfg.d_model, device="cuda"))
     layer.cache.check()
