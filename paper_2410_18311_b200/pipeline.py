@@ -101,7 +101,14 @@ class W4Linear:
         self.codes, self.pairs = new(B.coreinfer_w4_codes_bytes(N, K)), new(B.coreinfer_w4_pairs_bytes(N, K, group))
         self.bias, self.act = bias, act
         self.matrix = B.make_w4_matrix(self.codes, self.pairs, N, K, group)
-        B.coreinfer_w4_quantize(weight, group, self.codes, self.pairs, stream)
+        self.load(weight, stream)
+
+    def load(self, weight, stream=None):
+        """Other weights of the same shape into the same buffers, so that a captured graph runs on with them."""
+        if tuple(weight.shape) != (self.matrix.N, self.matrix.K):
+            raise B.CoreInferError(B.ERR_INVALID_ARG, "weights of shape %s do not fit the %d x %d matrix"
+                                   % (tuple(weight.shape), self.matrix.N, self.matrix.K))
+        B.coreinfer_w4_quantize(weight, self.matrix.group, self.codes, self.pairs, stream)
 
     def __call__(self, x, y, mul=None, stream=None):
         B.coreinfer_w4_matvec(self.matrix, x, self.act, self.bias, mul, y, stream)
@@ -153,7 +160,7 @@ class Core4Layer:
     weights = (w_qkv [(q_heads + 2 kv_heads) * head_dim, d], w_o [d, q_heads * head_dim], w_up, w_gate | None,
     w_down) in the configuration's 16-bit type; the residual stream is fp32, norms have no parameters.
     The prompt's dense products and the norms are torch's; a decode step runs in the library's kernels but for
-    the norms and the two additions, and can be captured in a CUDA graph."""
+    the norms and the two additions, and can be captured in a CUDA graph, which stays valid over later prompts."""
 
     def __init__(self, cfg: Config, batch, q_heads, kv_heads, head_dim, budget, weights, recent=32, first=4, max_prompt=None,
                  group=128, cache_group=64, device="cuda"):
@@ -210,9 +217,15 @@ class Core4Layer:
         up, down = (torch.empty(self.K, cfg.d_model, dtype=cfg.torch_dtype, device=h.device) for _ in range(2))
         gate = torch.empty_like(up) if cfg.gated else None
         B.coreinfer_compact(w_up, w_gate, w_down, None, self.core_idx, self.K, up, gate, down, None)
-        self.up = W4Linear(up, self.group, act=B.ACT_NONE if cfg.gated else B.ACT_RELU)
-        self.gate = W4Linear(gate, self.group, act=B.ACT_RELU) if cfg.gated else None
-        self.down = W4Linear(down.t(), self.group)           # the transposed down projection, by its strides
+        if self.up is None:
+            self.up = W4Linear(up, self.group, act=B.ACT_NONE if cfg.gated else B.ACT_RELU)
+            self.gate = W4Linear(gate, self.group, act=B.ACT_RELU) if cfg.gated else None
+            self.down = W4Linear(down.t(), self.group)       # the transposed down projection, by its strides
+        else:                                                # a step captured in a graph keeps the buffers
+            self.up.load(up)
+            if cfg.gated:
+                self.gate.load(gate)
+            self.down.load(down.t())
 
     def step(self, h):
         """h [batch, d] fp32, one new token per sequence: updated in place."""

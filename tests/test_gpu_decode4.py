@@ -130,3 +130,43 @@ def test_prompt_longer_than_the_cache_is_refused():
     assert torch.equal(h, before) and torch.equal(layer.cache.state, state) and torch.equal(layer.core_idx, core)
     layer.step(torch.randn(2, cfg.d_model, device="cuda"))
     layer.cache.check()
+
+
+def test_captured_step_serves_later_prompts():
+    """A step captured after one prompt gives, after the next ones, the bits of a step called directly: outputs and cache."""
+    require_gpu()
+    layer, cfg = small_layer()
+    g = torch.Generator(device="cuda").manual_seed(77)
+    new = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    x = new(2, cfg.d_model)
+    layer.prompt(new(2, 40, cfg.d_model))
+    first_core = layer.core_idx.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        layer.step(x)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer.step(x)
+    c = layer.cache
+    buffers = (c.k_codes, c.k_pairs, c.v_codes, c.v_pairs, c.weight, c.position, c.state)
+    for T in (40, 31):
+        layer.prompt(new(2, T, cfg.d_model))
+        assert not torch.equal(layer.core_idx, first_core)
+        start, tokens = [t.clone() for t in buffers], [new(2, cfg.d_model) for _ in range(4)]
+        outs = []
+        for token in tokens:
+            x.copy_(token)
+            graph.replay()
+            outs.append(x.clone())
+        end = [t.clone() for t in buffers]
+        for t, was in zip(buffers, start):
+            t.copy_(was)
+        for token, out in zip(tokens, outs):
+            layer.step(token)
+            assert torch.equal(token, out)
+        used = c.lengths()[0]
+        for t, was in zip(buffers, end):
+            assert torch.equal(t, was) if t is c.state else torch.equal(t[:, :, :used], was[:, :, :used])
+    c.check()
