@@ -58,12 +58,14 @@ class Layer(ctypes.Structure):
 
 class W4Matrix(ctypes.Structure):
     """coreinfer_w4_matrix"""
+    device = None         # of the buffers, where make_w4_matrix() has seen them
     _fields_ = [("codes", ctypes.c_void_p), ("pairs", ctypes.c_void_p), ("N", ctypes.c_int32), ("K", ctypes.c_int32),
                 ("group", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 class KV4Cache(ctypes.Structure):
     """coreinfer_kv4_cache"""
+    device = None         # of the buffers, where make_kv4_cache() has seen them
     _fields_ = [("k_codes", ctypes.c_void_p), ("k_pairs", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
                 ("v_pairs", ctypes.c_void_p), ("state", ctypes.c_void_p), ("weight", ctypes.c_void_p),
                 ("position", ctypes.c_void_p), ("batch", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
@@ -187,13 +189,24 @@ def _stream(stream=None):
     return ctypes.c_void_p(s.cuda_stream)
 
 
-def _raw_stream(t, stream):
-    """Stream handle for a call on tensor t: looking the current stream up as a number costs 0.1 us, as a
-    torch.cuda.Stream object 3 us."""
-    device = t.get_device()
+def _raw_stream(device, stream):
+    """Stream handle for a call on tensors of device number `device`: looking the current stream up as a number costs
+    0.1 us, as a torch.cuda.Stream object 3 us."""
     if device < 0:
         raise CoreInferError(ERR_INVALID_ARG, "a CUDA tensor was expected, got one on the host")
     return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+
+
+def _off_device(what):
+    raise CoreInferError(ERR_INVALID_ARG, "%s are not all on one CUDA device" % what)
+
+
+def _one_device(what, tensors):
+    """Device number of all the tensors that are not None."""
+    found = {t.get_device() for t in tensors if t is not None}
+    if len(found) != 1:
+        _off_device(what)
+    return found.pop()
 
 
 _DTYPE_CODES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
@@ -382,21 +395,33 @@ def coreinfer_w4_pairs_bytes(N: int, K: int, group: int) -> int:
     return int(load().coreinfer_w4_pairs_bytes(N, K, group))
 
 
-def make_w4_matrix(codes, pairs, N: int, K: int, group: int) -> W4Matrix:
-    """coreinfer_w4_matrix over the caller's two CUDA buffers (which must outlive it)."""
+def _w4_buffers(codes, pairs, N, K, group):
+    """Checks the two buffers of a weight matrix; their device number."""
     if (codes.numel() * codes.element_size() < coreinfer_w4_codes_bytes(N, K)
             or pairs.numel() * pairs.element_size() < coreinfer_w4_pairs_bytes(N, K, group)):
         raise CoreInferError(ERR_INVALID_ARG, "codes or pairs smaller than a %d x %d matrix takes" % (N, K))
     if not (codes.is_contiguous() and pairs.is_contiguous()):
         raise CoreInferError(ERR_INVALID_ARG, "codes and pairs must be contiguous")
-    return W4Matrix(codes.data_ptr(), pairs.data_ptr(), N, K, group, 0)
+    return _one_device("codes and pairs", (codes, pairs))
+
+
+def make_w4_matrix(codes, pairs, N: int, K: int, group: int) -> W4Matrix:
+    """coreinfer_w4_matrix over the caller's two CUDA buffers (which must outlive it)."""
+    device = _w4_buffers(codes, pairs, N, K, group)
+    w4 = W4Matrix(codes.data_ptr(), pairs.data_ptr(), N, K, group, 0)
+    w4.device = device
+    return w4
 
 
 def coreinfer_w4_quantize(w, group, codes, pairs, stream=None):
     """w [N, K] fp32, bf16 or fp16 with any strides (a transposed view is fine) -> codes, pairs."""
+    if w.dim() != 2:
+        raise CoreInferError(ERR_INVALID_ARG, "a matrix was expected, got shape %s" % (tuple(w.shape),))
     N, K = w.shape
+    if _w4_buffers(codes, pairs, N, K, int(group)) != w.get_device():
+        _off_device("w, codes and pairs")
     _check(load().coreinfer_w4_quantize(_p(w), dtype_code(w), N, K, w.stride(0), w.stride(1), int(group), _p(codes), _p(pairs),
-                                        _raw_stream(w, stream)))
+                                        _raw_stream(w.get_device(), stream)))
 
 
 def _row_stride(t, n):
@@ -418,10 +443,14 @@ def coreinfer_w4_matvec(w4, x, act, bias, mul, y, stream=None):
                              % (tuple(x.shape), tuple(y.shape), N, w4.K))
     if dtype not in _DTYPE_CODES or y_dtype not in _DTYPE_CODES:
         raise CoreInferError(ERR_UNSUPPORTED, "unsupported torch dtypes %s, %s" % (dtype, y_dtype))
-    status = load().coreinfer_w4_matvec(w4, x.data_ptr(), batch, _row_stride(x, K), _DTYPE_CODES[dtype], act,
+    device = x.get_device()
+    if y.get_device() != device or (w4.device != device and w4.device is not None) or (bias is not None and bias.get_device() != device) \
+            or (mul is not None and mul.get_device() != device):
+        _off_device("the matrix, x, y, bias and mul")
+    status = (_lib or load()).coreinfer_w4_matvec(w4, x.data_ptr(), batch, K if x.is_contiguous() else _row_stride(x, K), _DTYPE_CODES[dtype], act,
                                         None if bias is None else bias.data_ptr(), None if mul is None else mul.data_ptr(),
                                         0 if mul is None else _row_stride(mul, N), y.data_ptr(), _DTYPE_CODES[y_dtype],
-                                        _row_stride(y, N), _raw_stream(x, stream))
+                                        N if y.is_contiguous() else _row_stride(y, N), _raw_stream(device, stream))
     if status:
         _check(status)
 
@@ -439,9 +468,11 @@ def make_kv4_cache(k_codes, k_pairs, v_codes, v_pairs, state, weight=None, posit
         if t is not None and (t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous()):
             raise CoreInferError(ERR_INVALID_ARG, "a cache buffer of %s %s was expected contiguous as %s %s"
                                  % (t.dtype, tuple(t.shape), dtype, shape))
-    return KV4Cache(k_codes.data_ptr(), k_pairs.data_ptr(), v_codes.data_ptr(), v_pairs.data_ptr(), state.data_ptr(),
-                    None if weight is None else weight.data_ptr(), None if position is None else position.data_ptr(),
-                    B, H, n, 2 * half, 2 * half // groups, 0)
+    cache = KV4Cache(k_codes.data_ptr(), k_pairs.data_ptr(), v_codes.data_ptr(), v_pairs.data_ptr(), state.data_ptr(),
+                     None if weight is None else weight.data_ptr(), None if position is None else position.data_ptr(),
+                     B, H, n, 2 * half, 2 * half // groups, 0)
+    cache.device = _one_device("a cache's buffers", [t for t, _, _ in want])
+    return cache
 
 
 def _token_stride(t, shape):
@@ -461,22 +492,25 @@ def _token_stride(t, shape):
 def coreinfer_kv4_append(cache, k, v, k_stored=None, v_stored=None, stream=None):
     """k, v [batch, T, kv_heads, head_dim] into the cache; k_stored / v_stored: the values as stored, or None."""
     shape, dtype, H, D = k.shape, k.dtype, cache.kv_heads, cache.head_dim
-    T = shape[1] if len(shape) == 4 else 0
-    if shape != (cache.batch, T, H, D):
+    if len(shape) != 4 or shape[0] != cache.batch or shape[2] != H or shape[3] != D:
         raise CoreInferError(ERR_INVALID_ARG, "k of shape %s does not fit the cache" % (tuple(shape),))
-    ld = H * D if k.is_contiguous() else _token_stride(k, shape)
-    if v.dtype != dtype or dtype not in _DTYPE_CODES or v.shape != shape or (H * D if v.is_contiguous() else _token_stride(v, shape)) != ld:
+    T, row = shape[1], H * D
+    ld = row if k.is_contiguous() else _token_stride(k, shape)
+    if v.dtype != dtype or dtype not in _DTYPE_CODES or v.shape != shape or (row if v.is_contiguous() else _token_stride(v, shape)) != ld:
         raise CoreInferError(ERR_INVALID_ARG, "k (%s) and v (%s) must have one type, shape and spacing of tokens" % (dtype, v.dtype))
+    device = k.get_device()
+    if v.get_device() != device or (cache.device != device and cache.device is not None):
+        _off_device("the cache, k and v")
     ks = vs = None
     if k_stored is not None:
-        if k_stored.shape != shape or k_stored.dtype != dtype or not k_stored.is_contiguous():
-            raise CoreInferError(ERR_INVALID_ARG, "k_stored must be contiguous and shaped as k")
+        if k_stored.shape != shape or k_stored.dtype != dtype or not k_stored.is_contiguous() or k_stored.get_device() != device:
+            raise CoreInferError(ERR_INVALID_ARG, "k_stored must be contiguous, shaped as k and beside it")
         ks = k_stored.data_ptr()
     if v_stored is not None:
-        if v_stored.shape != shape or v_stored.dtype != dtype or not v_stored.is_contiguous():
-            raise CoreInferError(ERR_INVALID_ARG, "v_stored must be contiguous and shaped as v")
+        if v_stored.shape != shape or v_stored.dtype != dtype or not v_stored.is_contiguous() or v_stored.get_device() != device:
+            raise CoreInferError(ERR_INVALID_ARG, "v_stored must be contiguous, shaped as v and beside it")
         vs = v_stored.data_ptr()
-    status = load().coreinfer_kv4_append(cache, k.data_ptr(), v.data_ptr(), _DTYPE_CODES[dtype], T, ld, ks, vs, _raw_stream(k, stream))
+    status = (_lib or load()).coreinfer_kv4_append(cache, k.data_ptr(), v.data_ptr(), _DTYPE_CODES[dtype], T, ld, ks, vs, _raw_stream(device, stream))
     if status:
         _check(status)
 
@@ -488,13 +522,21 @@ def coreinfer_kv4_attention_workspace_bytes(cache, q_heads: int, T: int) -> int:
 def coreinfer_kv4_attention(cache, q, scale, out, accumulate, workspace, stream=None):
     """q [batch, T, q_heads, head_dim] -> out of the same shape and type; accumulate: add every slot's
     attention weight to the cache's weights."""
-    _, T, heads, _ = q.shape
-    shape, dtype = (cache.batch, T, heads, cache.head_dim), q.dtype
+    shape, dtype = q.shape, q.dtype
+    if len(shape) != 4 or shape[0] != cache.batch or shape[3] != cache.head_dim or out.shape != shape:
+        raise CoreInferError(ERR_INVALID_ARG, "q and out [batch, T, q_heads, head_dim] of the cache's batch %d and head_dim %d were expected, got %s and %s"
+                             % (cache.batch, cache.head_dim, tuple(shape), tuple(out.shape)))
     if out.dtype != dtype or dtype not in _DTYPE_CODES:
         raise CoreInferError(ERR_INVALID_ARG, "q (%s) and out (%s) must have one supported type" % (dtype, out.dtype))
-    status = load().coreinfer_kv4_attention(cache, q.data_ptr(), _DTYPE_CODES[dtype], heads, T, _token_stride(q, shape), scale,
-                                            out.data_ptr(), _token_stride(out, shape), 1 if accumulate else 0, workspace.data_ptr(),
-                                            workspace.nbytes, _raw_stream(q, stream))
+    T, heads = shape[1], shape[2]
+    row = heads * shape[3]
+    device = q.get_device()
+    if out.get_device() != device or workspace.get_device() != device or (cache.device != device and cache.device is not None):
+        _off_device("the cache, q, out and the workspace")
+    status = (_lib or load()).coreinfer_kv4_attention(cache, q.data_ptr(), _DTYPE_CODES[dtype], heads, T,
+                                            row if q.is_contiguous() else _token_stride(q, shape), scale, out.data_ptr(),
+                                            row if out.is_contiguous() else _token_stride(out, shape), 1 if accumulate else 0,
+                                            workspace.data_ptr(), workspace.nbytes, _raw_stream(device, stream))
     if status:
         _check(status)
 
@@ -505,7 +547,10 @@ def coreinfer_kv4_evict_workspace_bytes(cache) -> int:
 
 def coreinfer_kv4_evict(src, dst, budget, recent, first, workspace, stream=None):
     """Keep `budget` slots per head (the first and recent tokens, then the heaviest); dst is src for in place."""
-    status = load().coreinfer_kv4_evict(src, dst, budget, recent, first, workspace.data_ptr(), workspace.nbytes,
-                                        _raw_stream(workspace, stream))
+    device = workspace.get_device()
+    if (src.device != device and src.device is not None) or (dst.device != device and dst.device is not None):
+        _off_device("the caches and the workspace")
+    status = (_lib or load()).coreinfer_kv4_evict(src, dst, budget, recent, first, workspace.data_ptr(), workspace.nbytes,
+                                        _raw_stream(device, stream))
     if status:
         _check(status)

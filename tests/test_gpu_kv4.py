@@ -532,3 +532,39 @@ def test_evict_from_one_source_on_two_streams():
     for small, (_, z, _, _, _) in zip(wants, runs):
         small.assert_equal(z)
     ref.assert_equal(d)
+
+
+def test_tensors_on_the_host_are_refused():
+    """Any argument of the four-bit calls that is not beside the others raises before a kernel starts."""
+    require_gpu()
+    ref = CacheRef(1, 1, 16, 64, 32, np.random.default_rng(1))
+    ref.set_lengths([5])
+    d = ref.to_cuda()
+    h = handle(d)
+    with pytest.raises(ci.CoreInferError, match="one CUDA device"):
+        handle({**d, "v_pairs": d["v_pairs"].cpu()})
+    on_host = handle({n: t.cpu() for n, t in d.items()})
+    t = torch.zeros(1, 1, 1, 64, device="cuda")
+    ws = scratch(max(ci.coreinfer_kv4_attention_workspace_bytes(h, 1, 1), ci.coreinfer_kv4_evict_workspace_bytes(h)))
+    w, codes, pairs = torch.zeros(16, 128, device="cuda"), scratch(ci.coreinfer_w4_codes_bytes(16, 128)), scratch(ci.coreinfer_w4_pairs_bytes(16, 128, 32))
+    w4, x, y, b = ci.make_w4_matrix(codes, pairs, 16, 128, 32), torch.zeros(1, 128, device="cuda"), torch.zeros(1, 16, device="cuda"), torch.zeros(16, device="cuda")
+    w4_host = ci.make_w4_matrix(codes.cpu(), pairs.cpu(), 16, 128, 32)
+    with pytest.raises(ci.CoreInferError, match="one CUDA device"):
+        ci.make_w4_matrix(codes, pairs.cpu(), 16, 128, 32)
+    for call in (lambda: ci.coreinfer_kv4_append(h, t, t.cpu()), lambda: ci.coreinfer_kv4_append(h, t.cpu(), t.cpu()),
+                 lambda: ci.coreinfer_kv4_append(h, t, t, t.clone(), t.cpu()), lambda: ci.coreinfer_kv4_append(h, t, t, t.cpu(), t.clone()),
+                 lambda: ci.coreinfer_kv4_append(on_host, t, t),
+                 lambda: ci.coreinfer_kv4_attention(h, t, 1.0, t.cpu(), True, ws), lambda: ci.coreinfer_kv4_attention(h, t.cpu(), 1.0, t, True, ws),
+                 lambda: ci.coreinfer_kv4_attention(h, t, 1.0, t.clone(), True, ws.cpu()),
+                 lambda: ci.coreinfer_kv4_attention(on_host, t, 1.0, t.clone(), True, ws),
+                 lambda: ci.coreinfer_kv4_evict(h, h, 4, 0, 0, ws.cpu()), lambda: ci.coreinfer_kv4_evict(h, on_host, 4, 0, 0, ws),
+                 lambda: ci.coreinfer_kv4_evict(on_host, h, 4, 0, 0, ws),
+                 lambda: ci.coreinfer_w4_quantize(w.cpu(), 32, codes, pairs), lambda: ci.coreinfer_w4_quantize(w, 32, codes.cpu(), pairs.cpu()),
+                 lambda: ci.coreinfer_w4_quantize(w, 32, codes, pairs.cpu()),
+                 lambda: ci.coreinfer_w4_matvec(w4, x, 0, None, None, y.cpu()), lambda: ci.coreinfer_w4_matvec(w4, x.cpu(), 0, None, None, y),
+                 lambda: ci.coreinfer_w4_matvec(w4, x, 0, b.cpu(), None, y), lambda: ci.coreinfer_w4_matvec(w4, x, 0, b, y.cpu(), y),
+                 lambda: ci.coreinfer_w4_matvec(w4_host, x, 0, None, None, y)):
+        with pytest.raises(ci.CoreInferError):
+            call()
+    torch.cuda.synchronize()
+    ref.assert_equal(d)

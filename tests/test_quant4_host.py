@@ -149,3 +149,20 @@ def test_cache_object_has_room_for_every_call(lib, q_heads, kv_heads):
     assert c.max_tokens == max(T for T in range(1, 17) if T * q_heads // kv_heads <= ci.KV4_MAX_ROWS)
     for T in range(1, c.max_tokens + 1):
         assert 0 < ci.coreinfer_kv4_attention_workspace_bytes(c.cache, q_heads, T) <= c.ws.numel()
+
+
+def test_quantize_binding_checks_its_buffers(lib):
+    """The kernel writes as many bytes as the sizes say: smaller or strided buffers are refused before it starts."""
+    w = torch.zeros(33, 200)
+    codes, pairs = (torch.zeros(n, dtype=torch.uint8) for n in (ci.coreinfer_w4_codes_bytes(33, 200), ci.coreinfer_w4_pairs_bytes(33, 200, 64)))
+    for c, p in ((codes[:-1], pairs), (codes, pairs[:-2]), (torch.zeros(0, dtype=torch.uint8), pairs)):
+        with pytest.raises(ci.CoreInferError, match="smaller"):
+            ci.coreinfer_w4_quantize(w, 64, c, p)
+    with pytest.raises(ci.CoreInferError, match="contiguous"):
+        ci.coreinfer_w4_quantize(w, 64, torch.zeros(2 * codes.numel(), dtype=torch.uint8)[::2], pairs)
+    with pytest.raises(ci.CoreInferError, match="matrix"):
+        ci.coreinfer_w4_quantize(w[0], 64, codes, pairs)
+    with pytest.raises(ci.CoreInferError, match="host"):
+        ci.coreinfer_w4_quantize(w, 64, codes, pairs)
+    with pytest.raises(ci.CoreInferError, match="q_heads"):
+        ci.coreinfer_kv4_attention(cache(), torch.zeros(2, 4, 64), 1.0, torch.zeros(2, 4, 64), False, codes)
