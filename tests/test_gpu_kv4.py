@@ -568,3 +568,20 @@ def test_tensors_on_the_host_are_refused():
             call()
     torch.cuda.synchronize()
     ref.assert_equal(d)
+
+
+@pytest.mark.parametrize("flat", [False, True])
+@pytest.mark.parametrize("D,group,dtype", [(64, 32, "f32"), (128, 64, "f32"), (128, 128, "f16"), (256, 64, "f16"), (128, 64, "bf16")])
+def test_attention_over_long_caches(D, group, dtype, flat):
+    """20000 and 5000 slots: hundreds of MMAs add up in one accumulator, which cuts off below its last place.  flat: keys
+    so small that all slots weigh about the same, where the sums hold the most beside their result."""
+    require_gpu()
+    rng = np.random.default_rng(D + flat)
+    ref = CacheRef(2, 1, 20000, D, group, rng)
+    ref.set_lengths([20000, 5001])
+    if flat:
+        ref.s[0], ref.o[0] = (ref.s[0] * 0.01).astype(np.float16), (ref.o[0] * 0.01).astype(np.float16)
+    ref.weight[:] = 0
+    d = ref.to_cuda()
+    q = torch.from_numpy(rng.standard_normal((2, 2, 2, D)).astype(np.float32)).cuda().to(DT[dtype])
+    check_attention(ref, d, q, attend(ref, d, q), D ** -0.5, ref.weight.copy())

@@ -200,3 +200,17 @@ def test_matvec_nan_and_infinity_pass_every_activation(dtype, act, with_mul):
     ref, mass = reference(values_np(x).astype(np.float64)[rows], w4_layout(values_np(w), group)[2][cols], values_np(bias).astype(np.float64)[cols],
                           act, None if m is None else values_np(m).astype(np.float64)[rows][:, cols])
     check(y[rows][:, cols], ref, mass, 4.0, K, DT[dtype])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("N,K,group", [(1, 1, 32), (17, 129, 64), (70, 300, 128)])
+def test_layout_of_a_view_without_a_unit_stride(N, K, group, dtype):
+    """Every second row and every third column of a wider matrix, and rows that are all the same one (stride 0)."""
+    require_gpu()
+    g = torch.Generator(device="cuda").manual_seed(N + K)
+    wide = torch.randn(2 * N, 3 * K, generator=g, device="cuda").to(DT[dtype])
+    for w in (wide[::2, ::3], wide[:, ::3].t()[:, :N].t(), wide[:1, :K].expand(N, K), wide[:1, ::3].expand(N, K)):
+        codes, pairs, _ = lay_out(w, group)
+        c, p, _ = w4_layout(values_np(w), group)
+        np.testing.assert_array_equal(codes.cpu().numpy(), c.reshape(-1))
+        np.testing.assert_array_equal(pairs.cpu().numpy().view(np.uint16), p.reshape(-1).view(np.uint16))
