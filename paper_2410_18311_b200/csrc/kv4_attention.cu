@@ -581,7 +581,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                                 lo[0][1][i] = fmaf(s1, acc[i >> 1][2 + (i & 1)], lo[0][1][i]);
                             }
                         }
-                    } else
+                    } else {
 #pragma unroll
                     for (int u = 0; u < UN; ++u) {
                         const uint8_t* krow = kst + (u * 16 + tok0) * CODE_ROW + tig * (D / 8);
@@ -621,6 +621,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                                 lo[u][1][i] = fmaf(p1.x, a1, g ? lo[u][1][i] + o1 : o1);
                             }
                         }
+                    }
                     }
                     float most[NV];
 #pragma unroll
@@ -851,7 +852,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                                 for (int tl = 0; tl < TL; ++tl) mma_16816(o[tl][j][1], a0, a1, a2, a3, bf[tl][0], bf[tl][1]);
                             }
                         }
-                    } else
+                    } else {
 #pragma unroll
                     for (int u = 0; u < UN; ++u) {
                         const uint8_t* vrow = vst + (u * 16 + tig) * CODE_ROW + gid * (D / 16);
@@ -908,6 +909,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                                 }
                             }
                         }
+                    }
                     }
                 }
                 leave(1);
