@@ -5,10 +5,13 @@
 // of fp32 sums (keys) or of the fp32 weights p (values).  One pass over the cache with a running maximum per query
 // row; rows = new tokens x query heads that share a key head.
 // Values average out and codes 0..15 do not: over 130000 slots of equal weight the sum of p s c is some thousand times the
-// output, and the MMA's accumulators cut off below their last place (4.2e-4 of the output instead of fp16's
-// 2.1e-4).  So every kAttnCentre pieces 8 times what p s came to is taken out of the accumulators, by an MMA with codes
-// that are all -8, and put into the sum of p o.  fp32 calls, whose outputs keep those bits, subtract 8 from every code
-// instead (one more instruction per two codes), and start the sums of q c at -8 sum q.
+// output, and the MMA's accumulators cut off below their last place.  So every kAttnCentre pieces bf16 calls take 8 times
+// what p s came to out of the accumulators, by an MMA with codes that are all -8, and put it into the sum of p o.  An MMA also
+// lines its products up by exponent fields, which for a subnormal code is that of 2^-14: what it adds up keeps about
+// 2^-18 of the largest product (measured 3 to 5e-6 of the absolute terms).  bf16's one part of p s hides that; fp32 and fp16
+// calls subtract 8 from every value code, which makes it a normal number (one more instruction per two codes: 52.7 -> 53.9 us
+// at 2 x 8 heads x 4 fp16 rows x 130000 slots, error 4e-8 of the absolute terms).  The sums of q c stay exact with subnormals
+// in both, since high parts of q are multiples of one step; fp32 calls start them at -8 sum q.
 //
 // What bounds it: the bytes of the cache (codes and pairs of keys and values, each read once).  The work per
 // byte is what has to be kept small, so the codes go to mma.sync.m16n8k16 as fp16 subnormals (quant4.cuh: one AND
@@ -161,9 +164,9 @@ __device__ __forceinline__ int opaque_zero()
     return z;
 }
 
-// Pieces of a warp between two centrings: the accumulators hold at most their sum of p s c off centre, which costs
-// about 2^-24 of it per 16 slots: 5e-4 of the output over 130000 slots of equal weight for bf16, 1e-4 for the others.
-template <int MODE> constexpr int kAttnCentre = MODE == 2 ? 2 : 8;
+// Pieces of a warp between two centrings (bf16): the accumulators hold at most their sum of p s c off centre, which costs
+// about 2^-24 of it per 16 slots: 5e-4 of the output over 130000 slots of equal weight.
+constexpr int kAttnCentre = 8;
 
 // Stages of a warp's ring: as many as two CTAs per SM (head_dim 256: one) leave room for.
 constexpr int kAttnStages16 = 6;
@@ -357,7 +360,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
 #pragma unroll 1
             for (int s = 0; s < STAGES; ++s) feed(ring + s * STAGE, s & 1);
         }
-        const uint32_t above = CENTRED || BOTH ? literal_1024() : 0u;
+        const uint32_t above = PARTS || BOTH ? literal_1024() : 0u;
         uint32_t stage = 0;                                  // offset of the stage at hand in the ring
         int t = 0;                                           // tiles done
         // Into a step: its stage has arrived, for every lane.  Out of it: all lanes have read it; it takes the piece STAGES
@@ -500,7 +503,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
             const int all_see = len - (a.T - 1);             // slots below this are seen by every row
 
             float o[TL][H32][2][4], om[BOTH ? 1 : NG][NV], sum_ps[BOTH ? 1 : NG][NV], l[NV], mx[NV];
-            int centre = kAttnCentre<MODE>;
+            int centre = kAttnCentre;
             // p is relative to mx, which is moved only when a logit exceeds it by kAttnRoom: p may reach 2^kAttnRoom.
             // The weights enter the second product as p s 2^E in fp16: E keeps the largest s near 2^8 (2^11 at most), so
             // that p s neither overflows nor loses bits to fp16's bottom for p down to about 2^-20.
@@ -873,7 +876,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                                 for (int i = 0; i < NV; ++i) {
                                     om_was[i] = om[g][i];
                                     ps[i] = lo[u][v][i] * so.x;
-                                    om[g][i] = fmaf(lo[u][v][i], CENTRED ? fmaf(8.f, so.x, so.y) : so.y, om[g][i]);
+                                    om[g][i] = fmaf(lo[u][v][i], PARTS ? fmaf(8.f, so.x, so.y) : so.y, om[g][i]);
                                 }
                                 if (!WIDE && edge) {         // a slot that a row does not see adds nothing, whatever it holds
 #pragma unroll
@@ -885,7 +888,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                                 }
 #pragma unroll
                                 for (int i = 0; i < NV; ++i)
-                                    if (!CENTRED) sum_ps[g][i] += ps[i];
+                                    if (!PARTS) sum_ps[g][i] += ps[i];
                                 if (PARTS) {
                                     const float high = __half2float(__float2half_rn(CENTRED ? round_to(ps[0], .25f) : ps[0]));
                                     bf[v] = movmatrix_trans(pack_half2(high, ps[0] - high));
@@ -898,7 +901,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                                 const uint32_t x = __byte_perm(va[j / 2], vb[j / 2], j & 1 ? 0x7632 : 0x5410);
                                 const uint32_t y = __byte_perm(vc[j / 2], vd[j / 2], j & 1 ? 0x7632 : 0x5410);
                                 const uint32_t x8 = x >> 8, y8 = y >> 8;
-                                if (CENTRED) {
+                                if (PARTS) {
                                     mma_16816(o[0][j][0], centred<0x000f000fu>(x, above), centred<0x000f000fu>(x8, above),
                                               centred<0x000f000fu>(y, above), centred<0x000f000fu>(y8, above), bf[0], bf[1]);
                                     mma_16816(o[0][j][1], centred<0x00f000f0u>(x, above), centred<0x00f000f0u>(x8, above),
@@ -913,8 +916,8 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                     }
                 }
                 leave(1);
-                if (!CENTRED && !BOTH && --centre == 0) {
-                    centre = kAttnCentre<MODE>;
+                if (!PARTS && !BOTH && --centre == 0) {
+                    centre = kAttnCentre;
 #pragma unroll
                     for (int g = 0; g < NG; ++g) {
                         // what is taken out and put back is one fp16 number per lane, so the two are the same; the rest waits
@@ -971,7 +974,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                             v.w = o[tl][j][1][2 + i];
                         }
                         // kRows16: values entered with 2^(7 - k)
-                        constexpr float even = BOTH ? 1.f / 128.f : (CENTRED ? 1.f : kCodeScaleLow), odd = BOTH || CENTRED ? even / 16.f : kCodeScaleHigh;
+                        constexpr float even = BOTH ? 1.f / 128.f : (PARTS ? 1.f : kCodeScaleLow), odd = BOTH || PARTS ? even / 16.f : kCodeScaleHigh;
                         v.x = fmaf(v.x, even, add);
                         v.y = fmaf(v.y, odd, add);
                         v.z = fmaf(v.z, even, add);

@@ -585,3 +585,26 @@ def test_attention_over_long_caches(D, group, dtype, flat):
     d = ref.to_cuda()
     q = torch.from_numpy(rng.standard_normal((2, 2, 2, D)).astype(np.float32)).cuda().to(DT[dtype])
     check_attention(ref, d, q, attend(ref, d, q), D ** -0.5, ref.weight.copy())
+
+
+@pytest.mark.parametrize("D,group,share,dtype", [(64, 32, 1, "f16"), (64, 64, 4, "f16"), (128, 128, 2, "f16"), (256, 64, 1, "f16"), (64, 64, 1, "f32"), (128, 32, 4, "f32")])
+def test_attention_values_that_cancel(D, group, share, dtype):
+    """Sixteen slots in pairs of one weight and opposite values, whose sum is 0: the output is what the sums lose.  Weights fall
+    by 3 to 4 from pair to pair, so that products of many sizes meet in one MMA.  Products of 11-bit weights and codes are
+    exact; a sum of 17 terms that keeps 24 bits of the largest loses at most 17 units of 2^-24 of it, the rest of the way a few."""
+    require_gpu()
+    n = 16
+    rng = np.random.default_rng(D + share)
+    ref = CacheRef(2, 2, n, D, group, rng)
+    ref.set_lengths([n, n - 4])
+    ref.codes[1][:, :, 1::2] = 15 - ref.codes[1][:, :, ::2]
+    ref.s[1] = (rng.integers(8, 64, size=ref.s[1].shape) / 64).astype(np.float16)          # 7.5 s is an fp16 number
+    ref.s[1][:, :, 1::2] = ref.s[1][:, :, ::2]
+    ref.o[1] = (-7.5 * ref.s[1].astype(np.float64)).astype(np.float16)
+    ref.s[0][:], ref.o[0][:] = 0, -np.floor((1.2 * np.arange(n // 2)[:, None] + rng.uniform(0, 0.2, size=(2, 2, n // 2, 1))).repeat(2, 2) * 64) / 64
+    d = ref.to_cuda()
+    q = torch.full((2, 1, 2 * share, D), D ** -0.5, device="cuda").to(DT[dtype])
+    out = values_np(attend(ref, d, q))
+    want, _, mass, _ = ref.attention(values_np(q).astype(np.float64), D ** -0.5)
+    assert np.abs(want).max() < 1e-12
+    assert (np.abs(out) <= 24 * 2.0 ** -24 * mass + 2.0 ** -25).all(), "worst %.3g of the absolute terms" % (np.abs(out) / mass).max()
