@@ -173,7 +173,7 @@ constexpr int kAttnStages16 = 6;
 template <int D, int G, int MODE> constexpr int kAttnStages =
     MODE == 3 ? kAttnStages16 : D == 64 ? 9 : (D == 256 ? (G == 32 ? 6 : 8) : (G == 32 ? (MODE == 0 ? 7 : 9) : (MODE == 0 ? 4 : 5)));
 
-// How far a logit (base 2) may exceed the running maximum before that is moved.  Rows change their maximum at different
+// How far logit + log2 s (base 2) may exceed its running maximum before that is moved.  Rows change their maximum at different
 // pieces, and each change rescales all of a warp's outputs: of 15 rows, nearly every piece did (91 of 1100
 // instructions a piece).
 template <int MODE> constexpr float kAttnRoom = MODE == 3 ? 6.f : 4.f;
@@ -504,11 +504,12 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
 
             float o[TL][H32][2][4], om[BOTH ? 1 : NG][NV], sum_ps[BOTH ? 1 : NG][NV], l[NV], mx[NV];
             int centre = kAttnCentre;
-            // p is relative to mx, which is moved only when a logit exceeds it by kAttnRoom: p may reach 2^kAttnRoom.
-            // The weights enter the second product as p s 2^E in fp16: E keeps the largest s near 2^8 (2^11 at most), so
-            // that p s neither overflows nor loses bits to fp16's bottom for p down to about 2^-20.
-            // kRows16 follows p 2^k instead, 2^k the power of a slot's values: 2^(8 + 6) at most.
-            float E = BOTH ? 8.f : 0.f, s_most = -1.f;
+            // The weights enter the second product as p s in fp16.  mx is the largest logit + log2 s (s: a slot's largest scale)
+            // that the row has met, moved only when exceeded by kAttnRoom, and p is 2^(logit - mx + 8): a row's largest p s
+            // stands between 2^8 and 2^12 and keeps its bits, whatever the scales of slots that it gives no weight or does not
+            // see.  (Under one power for a warp's slots, a row lost them with values 1e-4 times the others'.)
+            // kRows16 follows p 2^k likewise, 2^k the power of a slot's values: 2^(8 + 6) at most.
+            constexpr float E = 8.f;
 #pragma unroll
             for (int tl = 0; tl < TL; ++tl)
 #pragma unroll
@@ -626,7 +627,6 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                         }
                     }
                     }
-                    float most[NV];
 #pragma unroll
                     for (int i = 0; i < NV; ++i) {
                         const float by = BOTH ? q_row[(i >> 1) * 8 + (i & 1)].x : f[BOTH ? 0 : i];
@@ -659,18 +659,11 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                                 for (int v = 0; v < 2; ++v)
                                     if (na + 16 * u + 8 * v >= sees(i)) lo[u][v][i] = -__int_as_float(0x7f800000);
                     }
-#pragma unroll
-                    for (int i = 0; i < NV; ++i) {
-                        most[i] = fmaxf(lo[0][0][i], lo[0][1][i]);
-#pragma unroll
-                        for (int u = 1; u < UN; ++u) most[i] = fmaxf(most[i], fmaxf(lo[u][0][i], lo[u][1][i]));
-                    }
                     leave(0);
                     uint8_t* vst = enter();
                     // ---- value pairs, running maximum ----
                     uint32_t vp[UN][2][NG];
-                    __half2 smax = __float2half2_rn(0.f);
-                    float down[2] = {1.f, 1.f};
+                    float most[NV], down[2] = {1.f, 1.f};
                     if constexpr (BOTH) {
                         uint32_t* const pairs = reinterpret_cast<uint32_t*>(vst + CODES);
                         auto is_nan = [](uint32_t w) { return (w & 0x7fffu) > 0x7c00u || (w & 0x7fff0000u) > 0x7c000000u; };
@@ -733,44 +726,37 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
 #pragma unroll
                     for (int u = 0; u < UN; ++u)
 #pragma unroll
-                        for (int v = 0; v < 2; ++v) {
-                            ld_words<NG>(vp[u][v], vst + CODES + (16 * u + 8 * v + tok0) * PAIR_ROW);
-#pragma unroll
-                            for (int g = 0; g < NG; ++g) {
-                                smax = __hmax2(smax, *reinterpret_cast<const __half2*>(&vp[u][v][g]));
-                            }
-                        }
+                        for (int v = 0; v < 2; ++v) ld_words<NG>(vp[u][v], vst + CODES + (16 * u + 8 * v + tok0) * PAIR_ROW);
 #pragma unroll 1
                     for (int e = edge; e; e = opaque_zero()) {
                         // A slot beyond the sequence counts for nothing, whatever it holds; nor does one that a lane's one
                         // column does not see (of two columns, one may: they are told apart below).
-                        smax = __float2half2_rn(0.f);
 #pragma unroll
                         for (int u = 0; u < UN; ++u)
 #pragma unroll
                             for (int v = 0; v < 2; ++v)
 #pragma unroll
-                                for (int g = 0; g < NG; ++g) {
+                                for (int g = 0; g < NG; ++g)
                                     if (na + 16 * u + 8 * v >= (WIDE ? lim[0] : len)) vp[u][v][g] = 0u;
-                                    smax = __hmax2(smax, *reinterpret_cast<const __half2*>(&vp[u][v][g]));
-                                }
                     }
+#pragma unroll
+                    for (int i = 0; i < NV; ++i) most[i] = -__int_as_float(0x7f800000);
+#pragma unroll
+                    for (int u = 0; u < UN; ++u)
+#pragma unroll
+                        for (int v = 0; v < 2; ++v) {
+                            __half2 s = as_half2(0x00010001u);           // 2^-24, the smallest number: for scales that are 0 or NaN
+#pragma unroll
+                            for (int g = 0; g < NG; ++g) s = __hmax2(s, as_half2(vp[u][v][g]));
+                            const float k = log2_fast(__low2float(s));
+#pragma unroll
+                            for (int i = 0; i < NV; ++i) most[i] = fmaxf(most[i], lo[u][v][i] + k);
+                        }
                     }
-                    float s_here = BOTH ? -2.f : __low2float(smax);
-                    bool change = s_here > s_most;
+                    bool change = false;
 #pragma unroll
                     for (int i = 0; i < NV; ++i) change |= most[i] > mx[i] + kAttnRoom<MODE>;
                     if (__any_sync(0xffffffffu, change)) {
-                        float e_new = E;
-                        if (!BOTH && __any_sync(0xffffffffu, s_here > s_most)) {
-#pragma unroll
-                            for (int d = 1; d < 32; d <<= 1) s_here = fmaxf(s_here, __shfl_xor_sync(0xffffffffu, s_here, d));
-                            int x;
-                            frexpf(s_here, &x);
-                            x = s_here > 0.f ? (x < -15 ? -15 : x) : -15;
-                            e_new = (float)(8 - x);
-                            s_most = ldexpf(1.f, x + 3);     // room for scales up to 8 times larger before E moves
-                        }
 #pragma unroll
                         for (int i = 0; i < NV; ++i) {
                             float m = most[i];
@@ -779,7 +765,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
                             if (BOTH) m = ceilf(m);          // a whole number, as k is: their difference is exact
                             m = fmaxf(m, mx[i]);
-                            const float corr = exp2_fast((mx[i] - E) - (m - e_new));
+                            const float corr = exp2_fast(mx[i] - m);
                             mx[i] = m;
                             l[i] *= corr;
 #pragma unroll
@@ -799,7 +785,6 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                                     }
                                 }
                         }
-                        E = e_new;
                     }
 #pragma unroll
                     for (int i = 0; i < NV; ++i) {

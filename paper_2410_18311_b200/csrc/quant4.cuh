@@ -215,6 +215,12 @@ __device__ __forceinline__ float exp2_fast(float v)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
+__device__ __forceinline__ float log2_fast(float v)
+{
+    float r;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
 
 // The word of the j-th step over a row piece of 32 H values, from the words a lane loads (units 2 tig and 2 tig + 1: H / 2
 // words each).  Steps 2 p and 2 p + 1 cover blocks 2 p and 2 p + 1 of 32 values.  In groups of 64 or 128 the words serve as

@@ -608,3 +608,30 @@ def test_attention_values_that_cancel(D, group, share, dtype):
     want, _, mass, _ = ref.attention(values_np(q).astype(np.float64), D ** -0.5)
     assert np.abs(want).max() < 1e-12
     assert (np.abs(out) <= 24 * 2.0 ** -24 * mass + 2.0 ** -25).all(), "worst %.3g of the absolute terms" % (np.abs(out) / mass).max()
+
+
+@pytest.mark.parametrize("T,D,group,dtype", [(16, 64, 32, "f32"), (4, 128, 64, "f32"), (3, 256, 128, "f32"), (16, 64, 64, "f16"), (2, 128, 128, "f16"),
+                                             (16, 64, 32, "bf16"), (8, 128, 128, "bf16"), (4, 128, 64, "bf16"), (2, 256, 32, "bf16"), (16, 128, 32, "bf16")])
+@pytest.mark.parametrize("sharp", [False, True])
+def test_attention_of_small_values_beside_large_ones(T, D, group, dtype, sharp):
+    """Values grow from slot to slot, up to 1e10 times in all.  Every token's largest ones are its newest, and those after it,
+    which it does not see, are far larger (sharp: or it sees them and gives them e^-80).  What a row gives weight to keeps its bits."""
+    require_gpu()
+    lengths = [T, T + 21]
+    ref = CacheRef(2, 2, 48, D, group, np.random.default_rng(D + T))
+    ref.set_lengths(lengths)
+    low, high = (-5.0, 5.0) if dtype != "f16" else (-2.5, 4.5)             # fp16 outputs stay above its subnormal numbers
+    scales = np.full((2, 1, 48, 1), 10.0 ** low)
+    for b, n in enumerate(lengths):
+        scales[b, 0, n - T:n, 0] = 10.0 ** np.linspace(low, high, T)
+    with np.errstate(over="ignore"):
+        ref.s[1], ref.o[1] = np.minimum(ref.s[1] * scales, 65504).astype(np.float16), np.clip(ref.o[1] * scales, -65504, 65504).astype(np.float16)
+    # keys that are one number each, so that logits are theirs: 0, or -80 for the newer half
+    ref.s[0][:], ref.o[0][:] = 0, 0
+    if sharp:
+        for b, n in enumerate(lengths):
+            ref.o[0][b, :, n - (T + 1) // 2:] = -80
+    d = ref.to_cuda()
+    before = ref.weight.copy()
+    q = torch.full((2, T, 2, D), D ** -0.5, device="cuda").to(DT[dtype])
+    check_attention(ref, d, q, attend(ref, d, q), D ** -0.5, before, roundings=3 if T > 8 and D // group >= 4 else 1)
