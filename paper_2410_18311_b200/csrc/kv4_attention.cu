@@ -508,6 +508,9 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
             // that the row has met, moved only when exceeded by kAttnRoom, and p is 2^(logit - mx + 8): a row's largest p s
             // stands between 2^8 and 2^12 and keeps its bits, whatever the scales of slots that it gives no weight or does not
             // see.  (Under one power for a warp's slots, a row lost them with values 1e-4 times the others'.)
+            // Two parts carry 22 bits of p s from 2^-3 up, so a group whose scale is 2^-11 of the slot's largest keeps them too
+            // (high parts as multiples of 2^-2, whose sums would be exact, kept 2^-24 of the largest only: 1e-4 at a ratio of 1e-3,
+            // and 4e-7 against 3e-7 where groups are alike).
             // kRows16 follows p 2^k likewise, 2^k the power of a slot's values: 2^(8 + 6) at most.
             constexpr float E = 8.f;
 #pragma unroll
@@ -875,7 +878,7 @@ kv4_attention_kernel(const __grid_constant__ AttnArgs a)
                                 for (int i = 0; i < NV; ++i)
                                     if (!PARTS) sum_ps[g][i] += ps[i];
                                 if (PARTS) {
-                                    const float high = __half2float(__float2half_rn(CENTRED ? round_to(ps[0], .25f) : ps[0]));
+                                    const float high = __half2float(__float2half_rn(ps[0]));
                                     bf[v] = movmatrix_trans(pack_half2(high, ps[0] - high));
                                 } else {
                                     bf[v] = movmatrix_trans(pack_half2(ps[0], WIDE ? 0.f : ps[NV - 1]));

@@ -635,3 +635,18 @@ def test_attention_of_small_values_beside_large_ones(T, D, group, dtype, sharp):
     before = ref.weight.copy()
     q = torch.full((2, T, 2, D), D ** -0.5, device="cuda").to(DT[dtype])
     check_attention(ref, d, q, attend(ref, d, q), D ** -0.5, before, roundings=3 if T > 8 and D // group >= 4 else 1)
+
+
+@pytest.mark.parametrize("D,group,T,dtype", [(128, 32, 1, "f32"), (64, 32, 2, "f32"), (256, 128, 1, "f32"), (128, 64, 3, "f16"), (128, 32, 1, "f16")])
+def test_attention_groups_of_different_scales(D, group, T, dtype):
+    """Every second group of the values is 1000 times smaller than its neighbours: its outputs are as exact as theirs."""
+    require_gpu()
+    ref = CacheRef(2, 2, 16, D, group, np.random.default_rng(D + T))
+    ref.set_lengths([9, 4])
+    ref.s[1][..., ::2], ref.o[1][..., ::2] = ref.s[1][..., ::2] / np.float16(16), ref.o[1][..., ::2] / np.float16(16)
+    ref.s[1][..., 1::2], ref.o[1][..., 1::2] = ref.s[1][..., 1::2] * np.float16(64), ref.o[1][..., 1::2] * np.float16(64)
+    ref.s[0][:], ref.o[0][:] = 0, (np.random.default_rng(1).integers(-64, 64, size=ref.o[0].shape[:3] + (1,)) / 64).astype(np.float16)
+    d = ref.to_cuda()
+    before = ref.weight.copy()
+    q = torch.full((2, T, 4, D), D ** -0.5, device="cuda").to(DT[dtype])
+    check_attention(ref, d, q, attend(ref, d, q), D ** -0.5, before)
