@@ -148,8 +148,12 @@ static cudaError_t pick_quantize(W4QuantArgs& a, int group, cudaStream_t st)
 // mma.sync.m16n8k16 (16 output rows on the M side, up to 8 rows of x on the N side, codes as fp16
 // subnormals: quant4.cuh), the scales are factors of fp32 sums.  Bound by the bytes of the weights,
 // read once.  x enters as fp16 after a power-of-two scaling per row and group that puts the group's largest
-// entry into [2^13, 2^14) - exact for bf16 and fp16 x, two parts of 22 bits for fp32 - so that no value of x
-// is out of fp16's range.
+// entry into [2^13, 2^14) - exact for bf16 and fp16 x but for what lies 2^-25 below it, two parts of 22 bits for fp32 (the high
+// ones multiples of one step, whose sums lose nothing) - so that no value of x is out of fp16's range.
+// What an MMA cuts off beside a subnormal's largest product (quant4.cuh) shows in fp32 outputs of 16-bit x only: error 3 to
+// 5e-7 of the output with normal x (bf16; fp16 up to 1.1e-6), 1e-5 where x has entries 200 times the others, far below the
+// rounding of such an x (torch's fp32 product 3e-7).  Codes shifted up to where the loss ends (3e-7) cost two shifts per four operands: 30.8 ->
+// 32.2 us at 36864 x 9216, 1 row, 18.7 -> 20.1 at 5120 x 20480.
 // Each of a CTA's 16 warps streams its own blocks of 32 rows (two row tiles: the fragments of x are read once for both) x
 // 128 columns through a ring of its own (cp.async, 16 bytes a lane; refilled as soon as it is read), so no warp waits for
 // another inside a pair of row tiles.  A pair's columns are split over `split` warps where pairs are few, and over
