@@ -63,13 +63,12 @@ struct AttnArgs {
     const void* q;
     void* out;
     long long ld_q, ld_out;
-    int Hq, T, share;
+    int T, share;
     int R;                  // query rows per key head: T * share, row r = t * share + head
     int RT;                 // row tiles (of 8 or 4 rows) per CTA, dividing the warps
     int RU;                 // rows per unit: RT * 8 or RT * 4
     int RB;                 // units per (sequence, key head)
     int n_ctas;             // CTAs of the main kernel
-    int tile;               // slots per tile
     int finish_slots;       // slots per block of the finishing kernel
     float scale;
     int accumulate;
@@ -1251,7 +1250,6 @@ static coreinfer_status launch_mode(AttnArgs& a, const DeviceInfo& di, cudaStrea
     // two CTAs per SM where registers (head_dim up to 128) and shared memory (batch up to some hundreds) allow it
     const int per_sm = D <= 128 && 2 * (smem + 1024 + 64) <= (size_t)di.smem_optin + 1024 ? 2 : 1;
     if (smem > smem_room(di)) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "not enough shared memory");
-    a.tile = TILE;
     const long long tiles = (long long)a.c.B * a.c.H * a.RB * ((a.c.cap + TILE - 1) / TILE + kAttnUnitCost);
     if ((unsigned long long)a.c.B * a.c.H * a.c.cap > 0xffffffffull)
         CI_FAIL(COREINFER_ERR_UNSUPPORTED, "the cache has more than 2^32 slots");
@@ -1365,7 +1363,6 @@ coreinfer_status coreinfer_kv4_attention(const coreinfer_kv4_cache* cache, const
     a.out = out;
     a.ld_q = ld_q;
     a.ld_out = ld_out;
-    a.Hq = q_heads;
     a.T = T;
     a.share = q_heads / a.c.H;
     a.R = (int)R;

@@ -514,8 +514,8 @@ __global__ void __launch_bounds__(kW4Threads, 1) w4_matvec_kernel(const __grid_c
     }
 }
 
-// Clusters of `cluster` CTAs of a kernel that the GPU holds at once; asked once per kernel and device, for the largest
-// shared memory that a launch may have.
+// Clusters of `cluster` CTAs of a kernel that the GPU holds at once; asked once per kernel and device: whatever x takes,
+// the rings and the sums of a CTA are over half of an SM's shared memory, so the answer is that for one CTA per SM.
 template <auto Kernel>
 static int clusters_at_once(const DeviceInfo& di, int cluster, size_t smem)
 {
