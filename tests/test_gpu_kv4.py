@@ -650,3 +650,19 @@ def test_attention_groups_of_different_scales(D, group, T, dtype):
     before = ref.weight.copy()
     q = torch.full((2, T, 4, D), D ** -0.5, device="cuda").to(DT[dtype])
     check_attention(ref, d, q, attend(ref, d, q), D ** -0.5, before)
+
+
+@pytest.mark.parametrize("share,T,lengths", [(5, 1, [300, 7]), (8, 1, [129, 0]), (2, 4, [3, 77]), (1, 7, [40, 16])])
+def test_attention_eight_rows_of_the_widest_heads(share, T, lengths):
+    """bf16 rows 5 to 8 of head_dim 256 in groups of 32, a form of their own; NaN beyond the sequences."""
+    require_gpu()
+    D, group = 256, 32
+    rng = np.random.default_rng(share)
+    ref = CacheRef(2, 2, 16 * -(-max(lengths) // 16) + 16, D, group, rng)
+    ref.set_lengths(lengths)
+    d = ref.to_cuda()
+    for b, n in enumerate(lengths):
+        d["k_pairs"][b, :, n:] = float("nan")
+        d["v_pairs"][b, :, n:] = float("nan")
+    q = torch.from_numpy(rng.standard_normal((2, T, 2 * share, D)).astype(np.float32)).cuda().bfloat16()
+    check_attention(ref, d, q, attend(ref, d, q), D ** -0.5, ref.weight.copy())
