@@ -30,14 +30,19 @@
 // logits into weights that it adds to the cache's where that is asked for.
 // fp32 and fp16 calls carry query rows and p s as two fp16 parts in neighbouring columns (22 bits; four rows per
 // tile instead of eight): with one part the rounding of p s (2^-12, times the ratio of s c to the centred
-// value, about 3) would exceed fp16's own rounding.
+// value, about 3) would exceed fp16's own rounding.  bf16 calls carry one part, which keeps eight rows a tile: some 4e-4 of the
+// output, below its rounding to bf16 (against 64 bits 1.7 to 1.8e-3, torch's form in fp32 1.7e-3; the last bit falls the other
+// way in a part of the outputs, so the two differ by 1.4e-3).
 // Calls of more than eight bf16 rows per key head may take 16 rows per warp (attn_rpt): the codes are unpacked once for two
 // MMAs, and values enter as s c + o in fp16 (p itself instead of p s per group), under a power of two per slot that p makes
 // up for.  Three roundings of 2^-12, of p, o and the value, below bf16's 2^-9.
-// Measured (accumulating but for the last): 8 x 32 heads x 4001 bf16 39 us, 3150 GB/s, of which about 15 do not grow with the
-// length (launches, the lists, starting and joining units, finishing); 16384 slots 127 us, 5000 GB/s, the slope 5400;
-// 6 sequences x 8 heads x 15 rows in groups of 32 x up to 9000 slots 49 us, bound by instruction issue and latency (640
-// instructions per 16 slots and warp, 16 warps an SM); 2 x 8 heads x 4 fp16 rows x 130000 slots 57 us, 4200 GB/s.
+// Measured from a graph over two or three sets of inputs, ragged lengths (accumulating but for the last): 8 x 32 heads x up to 4001
+// bf16 37.7 us, 3280 GB/s, of which about 16 do not grow with the length (launches, the lists, starting and joining units,
+// finishing); up to 16384 slots 104 us, 4870 GB/s, the slope 5800; 6 sequences x 8 heads x 15 rows in groups of 32 x up to
+// 9000 slots 48.8 us, bound by instruction issue and latency (640 instructions per 16 slots and warp, 16 warps an SM); 2 x 8
+// heads x 4 fp16 rows x up to 130000 slots 53.1 us, 4500 GB/s.  A call on a stream takes 0.5 to 1 us more, the shortest 8.4
+// against 7.1.  At the 128 registers of two CTAs per SM some forms spill, 4 to 44 bytes a thread stored (16 rows of head_dim
+// 128 in groups of 32: 96; head_dim 256 in groups of 32, of 255 registers: 44 to 72), some ten instructions a piece.
 #include "kv4.cuh"
 
 #include <type_traits>
@@ -1282,9 +1287,10 @@ static coreinfer_status launch_mode(AttnArgs& a, const DeviceInfo& di, cudaStrea
 
 // Rows per warp for R query rows and `groups` groups per head: fp32 and fp16 always carry two parts; bf16 takes the
 // form with four rows where that is enough, and above eight rows the one with sixteen where there are four groups or more
-// (4 x 8 heads x 4096 slots, 15 / 24 / 64 rows: head_dim 128 in groups of 32 24.7 / 35.1 / 62.8 us against 26.4 / 39.1 /
-// 72.3 with eight rows a warp; in groups of 64, where p s is formed for two groups only, 23.6 / 32.8 / 57.7 against 21.8 /
-// 30.6 / 55.5).
+// (4 x 8 heads x up to 4096 slots, 9 / 15 / 24 / 64 rows: head_dim 128 in groups of 32 21.4 / 24.9 / 37.0 / 68.8 us against 22.8 /
+// 25.8 / 34.8 / 76.3 with eight rows a warp, so it loses where it pads half a tile; head_dim 256 in groups of 32 31.4 / 35.3 / 51.2 /
+// 91.8 against 35.0 / 38.9 / 53.2 / 117; head_dim 128 in groups of 64, where p s is formed for two groups only, 15 / 24 / 64 rows
+// of 4096 slots each 23.6 / 32.8 / 57.7 against 21.8 / 30.6 / 55.5).
 static inline int attn_rpt(coreinfer_dtype dtype, long long R, int groups)
 {
     return dtype != COREINFER_BF16 || R <= 4 ? 4 : (R <= 8 || groups < 4 ? 8 : 16);

@@ -8,8 +8,9 @@ namespace coreinfer {
 // per row); the lanes of a group agree on its range by shuffles; neighbouring blocks of 32 values
 // exchange a unit so that codes are stored in words.  A CTA walks rows of one sequence so that the sequence's state is
 // read, and its ticket taken, a few hundred times at most; a lane moves on by fixed strides and has the next row under way
-// while it works on one.  Bound by instructions, about 280 per warp and row of eight values a lane: 1000 tokens x 32 heads
-// x 128 bf16, stored values out, 14.1 us, 2660 GB/s (issue slots 66 % busy).
+// while it works on one.  Bound by instructions, about 280 per warp and row of eight values a lane (issue slots 66 % busy): 1000
+// tokens x 32 heads x 128 bf16, stored values out, with the launch that clears the state before it 16.7 us from a graph over
+// three sets of inputs, 2250 GB/s, and 18.2 on a stream.
 constexpr int kAppendThreads = 256;
 
 struct AppendArgs {
@@ -140,8 +141,9 @@ static coreinfer_status pick_append(const AppendArgs& a, const DeviceInfo& di, c
 // ballots; a warp owns a contiguous range of slots, so that list order is slot order.
 // kv4_move_kernel copies the listed slots, many CTAs per head.
 // All are bound by latency at the sizes of a decode step (append and few together 10.2 us for 8 sequences x 32 heads x 2049
-// slots, of which some 6 are two launches and the reads of the state), the moves by bytes after a prompt: 4 x 8 heads x
-// 16384 slots down to 2048 in another cache 16.9 us, about half of it the selection's barriers and three passes.
+// slots from a graph, 10.9 on a stream, of which some 6 are two launches and the reads of the state), the moves by bytes after a
+// prompt: 4 x 8 heads x up to 16384 slots down to 2048 in another cache 18.4 us over three sets of inputs (16.9 over two, part of
+// which stays in L2), about half of it the selection's barriers and three passes.
 constexpr int kEvictBins = 2048;
 constexpr int kEvictFew = 16;
 constexpr int kEvictKeysMost = 48 * 1024;   // keys a CTA holds in shared memory; more slots are read again for each pass

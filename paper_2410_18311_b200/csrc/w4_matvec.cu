@@ -161,9 +161,10 @@ static cudaError_t pick_quantize(W4QuantArgs& a, int group, cudaStream_t st)
 // such clusters leave SMs empty, 57.6 against 36.7 us at 36864 x 9216 and 8 rows).  What does not fit four goes over
 // two in chunks of columns, laid out again for every pair.  The partial sums meet in shared memory, in a fixed
 // order, after every pair.
-// Measured back to back from a graph: 36864 x 9216, 8 rows of bf16 36.7 us, 4930 GB/s (1 row 30.5 us, 5940; what 8 rows cost
-// more is laying x out, about 4 us in which only the rings fill, and the MMAs' instructions); 4096 x 4096, 1 row 5.2 us and
-// 768 x 768, fp32 3.8 us: launch, x, the first blocks' latency and the join, one after the other.
+// Measured back to back from a graph over three sets of inputs: 36864 x 9216, 8 rows of bf16 36.9 us, 4910 GB/s (1 row 30.8 us,
+// 5880; what 8 rows cost more is laying x out, about 4 us in which only the rings fill, and the MMAs' instructions), 40.1 with
+// a bias, whose loads begin after the join of a pair; 4096 x 4096, 1 row 5.2 us and 768 x 768, fp32 3.7 us (5.5 and 4.1 with a
+// bias): launch, x, the first blocks' latency and the join, one after the other.  On a stream 1 us more each.
 constexpr int kW4Warps = 16;
 constexpr int kW4Threads = 32 * kW4Warps;
 constexpr int kW4Join = 3;                  // what the join of a pair costs, in column blocks (16384 x 4096 over clusters of two: 28.7 us without it)

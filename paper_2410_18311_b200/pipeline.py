@@ -115,7 +115,10 @@ class W4Linear:
 
 
 class KV4Cache:
-    """Keys, values, weights and positions of one layer's 4-bit cache, and the workspaces of its calls."""
+    """Keys, values, weights and positions of one layer's 4-bit cache, and the workspace of its calls.  The workspace holds an fp32
+    logit per slot and query row of the longest call, max_tokens tokens (64 bytes per slot and head where heads are not
+    shared, beside 2 * (head_dim / 2 + 4 * head_dim / group) + 8 of the cache); a caller with many layers can use the
+    binding's calls with one workspace for all."""
 
     def __init__(self, batch, q_heads, kv_heads, capacity, head_dim, group=64, device="cuda"):
         new = lambda *s, dtype: torch.empty((batch, kv_heads, capacity) + s, dtype=dtype, device=device)
@@ -158,8 +161,10 @@ class Core4Layer:
     that the prompt selected.  Up to 8 sequences decode together and share the core set.
 
     weights = (w_qkv [(q_heads + 2 kv_heads) * head_dim, d], w_o [d, q_heads * head_dim], w_up, w_gate | None,
-    w_down) in the configuration's 16-bit type; the residual stream is fp32, norms have no parameters.
-    The prompt's dense products and the norms are torch's; a decode step runs in the library's kernels but for
+    w_down) in the configuration's 16-bit type; the residual stream is fp32, norms have no parameters, there are no biases and no
+    rotary positions, and the FFN is ReLU or ReLU-gated as the configurations' are: a part of a decoder to build on rather than
+    one of the models.  The 16-bit weights stay for the next prompt beside their 4-bit copies, so four bits save the bytes of
+    a decode step and not memory.  The prompt's dense products and the norms are torch's; a decode step runs in the library's kernels but for
     the norms and the two additions, and can be captured in a CUDA graph, which stays valid over later prompts."""
 
     def __init__(self, cfg: Config, batch, q_heads, kv_heads, head_dim, budget, weights, recent=32, first=4, max_prompt=None,
