@@ -422,7 +422,8 @@ coreinfer_status coreinfer_w4_quantize(const void* w, coreinfer_dtype dtype, int
 /* Matrix-vector products with a 4-bit weight matrix:
  *   y[b, n] = act( sum_k x[b, k] * w^[n, k] + bias[n] ) * mul[b, n]
  * for 1 <= batch <= COREINFER_MAX_BATCH rows of x; every weight byte is read once for all rows.
- * Sums are fp32 in an order that does not change from run to run; y is rounded once.
+ * Sums are fp32 in an order that does not change from run to run, good to 1e-6 of the sum of absolute terms
+ * (16-bit x with entries hundreds of times the others: 1e-5); y is rounded once.
  *   x      device [batch, K] in `dtype` with row stride ld_x (element aligned)
  *   bias   device [N] in `dtype` or NULL;   mul  device [batch, N] in y_dtype with row stride ld_mul, or NULL
  *   y      device out [batch, N] in y_dtype (fp32 or `dtype`) with row stride ld_y; may be `mul`, not x
