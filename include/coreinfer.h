@@ -522,6 +522,134 @@ coreinfer_status coreinfer_kv4_evict(const coreinfer_kv4_cache* src, const corei
                                      int32_t budget, int32_t recent, int32_t first,
                                      void* workspace, size_t workspace_bytes, void* cuda_stream);
 
+/* ------------------------------------------------------------------ (9) --
+ * Rotary positions, and the norms of queries and keys that go with them.
+ *
+ * A head x of head_dim values is, where a norm is given, first scaled to  w * x / sqrt(mean(x^2) + eps).  Then the first
+ * rot_dim values are turned in pairs (a, b) by the angle  position * f_i:
+ *   a' = magnitude (a cos - b sin)      b' = magnitude (b cos + a sin)      i = 0 .. rot_dim / 2 - 1
+ * where pair i is (x_i, x_{i + rot_dim / 2}), or (x_{2i}, x_{2i+1}) with `interleaved`; the values behind rot_dim stay.
+ * All of it is computed in fp32 from exact angles and rounded once.
+ *
+ * Frequencies are kept as fractions of a turn, f_i / (2 pi) * 2^64 in 64 bits, so that position * f_i modulo a turn is
+ * an exact product of integers however far the position is (negative ones included).
+ *
+ * coreinfer_rope_frequencies (host only) writes the rot_dim / 2 fractions, to be copied to the device, and the magnitude:
+ *   PLAIN    f_i = base^(-2i / rot_dim)
+ *   LINEAR   f_i / factor
+ *   NTK      PLAIN with base * factor^(rot_dim / (rot_dim - 2))
+ *   YARN     f_i (1 - r_i + r_i / factor), r_i rising linearly from 0 to 1 between the pair that turns `high` times within
+ *            original_context positions (rounded down) and the one that turns `low` times (rounded up); magnitude
+ *            0.1 ln(factor) + 1.  Customary: low 1, high 32
+ *   BANDS    f_i s_i + f_i / factor (1 - s_i), s_i = clamp((original_context f_i / (2 pi) - low) / (high - low), 0, 1): short
+ *            wavelengths stay, long ones are stretched.  Customary: low 1, high 4
+ * magnitude is 1 but for YARN.  rot_dim is a multiple of 16, 16 to 256.
+ * Errors: INVALID_ARG (NULL, base <= 1, factor < 1, original_context < 1 or low >= high where they are used, low <= 0),
+ * UNSUPPORTED (rot_dim, scaling). */
+typedef enum {
+    COREINFER_ROPE_PLAIN = 0, COREINFER_ROPE_LINEAR = 1, COREINFER_ROPE_NTK = 2, COREINFER_ROPE_YARN = 3, COREINFER_ROPE_BANDS = 4
+} coreinfer_rope_scaling;
+
+coreinfer_status coreinfer_rope_frequencies(int32_t rot_dim, double base, coreinfer_rope_scaling scaling, double factor,
+                                            int32_t original_context, double low, double high,
+                                            uint64_t* turns, float* magnitude);
+
+typedef struct {
+    const uint64_t* turns;      /* device, rot_dim / 2 fractions of a turn */
+    const void* q_norm;         /* device, head_dim weights in the call's type, or NULL: queries are not normed */
+    const void* k_norm;         /* the same for keys */
+    float eps;                  /* >= 0 */
+    float magnitude;
+    int32_t rot_dim;            /* a multiple of 16, at most head_dim */
+    int32_t interleaved;
+} coreinfer_rope;
+
+/* Turns (and norms) the queries and keys of `tokens` tokens.
+ *   positions  device int32 [tokens]
+ *   q, k       device, token t at t * ld_q (ld_k) elements, its heads [heads][head_dim] contiguous; k may be NULL with
+ *              kv_heads 0, q with q_heads 0.  q_out, k_out likewise; each may be its input (in place), not overlap it otherwise
+ * head_dim is 64, 128 or 256; pointers 16-byte aligned, strides * element size multiples of 16.
+ * Errors: INVALID_ARG, UNSUPPORTED (dtype, head_dim, rot_dim, heads above 1024, tokens * heads above 2^29), CUDA. */
+coreinfer_status coreinfer_rope_apply(const coreinfer_rope* rope, const int32_t* positions, coreinfer_dtype dtype,
+                                      int32_t tokens, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                                      const void* q, int64_t ld_q, const void* k, int64_t ld_k,
+                                      void* q_out, int64_t ld_q_out, void* k_out, int64_t ld_k_out, void* cuda_stream);
+
+/* ----------------------------------------------------------------- (10) --
+ * A key/value cache in pages, and attention of new tokens over it.
+ *
+ * Two pools, keys and values in `dtype`: element d of slot s of key head h in page g lies at
+ * g * page_stride + h * head_stride + s * token_stride + d elements, so that [pages][heads][slots][head_dim] and
+ * [pages][slots][heads][head_dim] both serve.  Pages of page_size slots (16, 32, 64, 128 or 256); sequence b's positions
+ * g * page_size .. + page_size - 1 are in page table[b * max_pages + g].  Sequences may share pages that no call writes.
+ *
+ * A call's new tokens are packed: rows start[b] .. start[b + 1] - 1 of its tensors are sequence b's (start: device int32
+ * [batch + 1], ascending; a sequence may have none), rows before start[0] and behind start[batch] are nobody's and are left as
+ * they are in every output.  length[b] counts the tokens sequence b holds, the new ones of the call among them: row
+ * start[b] + t is at position length[b] - (start[b + 1] - start[b]) + t.  Nothing here changes table, length or start; the
+ * kernels read them when they run, so a captured call follows them.
+ *
+ * Whatever those arrays hold, no access leaves the buffers: `start` counts as clamped to [0, tokens]; a token with a position
+ * below 0, behind the table's max_pages * page_size positions or in a page outside [0, n_pages) is not stored; slots of
+ * such a page read as zeros; tokens see the positions of the table only.
+ *
+ * head_dim is 64, 128 or 256, batch at most COREINFER_PAGED_MAX_BATCH, kv_heads at most 1024, max_pages * page_size
+ * below 2^30, n_pages below 2^27 (otherwise UNSUPPORTED).  Pools are 16-byte aligned, strides * element size multiples
+ * of 16 bytes; they may be as large as the device.  Slots that hold no token may hold anything. */
+#define COREINFER_PAGED_MAX_BATCH 1024
+
+typedef struct {
+    void* k;                    /* device: the pools */
+    void* v;
+    const int32_t* table;       /* device [batch][max_pages] */
+    const int32_t* length;      /* device [batch] */
+    int64_t page_stride;        /* elements, of both pools */
+    int64_t head_stride;
+    int64_t token_stride;
+    coreinfer_dtype dtype;
+    int32_t n_pages;
+    int32_t page_size;
+    int32_t kv_heads;
+    int32_t head_dim;
+    int32_t batch;
+    int32_t max_pages;
+    int32_t reserved;
+} coreinfer_paged_cache;
+
+/* Stores the new tokens' keys and values in their slots; with `rope`, keys are normed and turned on the way, and so are
+ * the queries, into q_out.
+ *   k, v       device, row r at r * ld_k (ld_v) elements, [kv_heads][head_dim] contiguous, in the cache's type
+ *   rope       or NULL: keys are stored as they are (q and q_out must then be NULL)
+ *   positions  device int32 [tokens], the positions that tokens are turned by, or NULL: those of their slots
+ *   q, q_out   device, rows as k's with q_heads heads; both or neither (q_heads 0); q_out may be q
+ * All 16-byte aligned, strides * element size multiples of 16.  Two rows of one call must not be the same slot's.
+ * Errors: INVALID_ARG, UNSUPPORTED (as above; tokens * heads above 2^29), CUDA. */
+coreinfer_status coreinfer_paged_append(const coreinfer_paged_cache* cache, const int32_t* start, int32_t tokens,
+                                        const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                                        const coreinfer_rope* rope, const int32_t* positions,
+                                        const void* q, int64_t ld_q, int32_t q_heads, void* q_out, int64_t ld_q_out,
+                                        void* cuda_stream);
+
+/* Attention of the new tokens over the cache (append first), from one token a sequence to whole prompts:
+ *   out[r, head] = sum_j softmax_j( scale * q[r, head] . k_j ) v_j
+ * where the token at position p sees the positions j <= p with  j > p - window  or  j < sinks  (window 0: all j <= p),
+ * and `q_heads / kv_heads` consecutive query heads share a key head.  A token that sees no position gets zeros.
+ * A NaN or infinity in a key or value reaches the tokens that see it, and no other.  Sums, maxima and the joins of partial
+ * results are fp32 in a fixed order (the same call on the same arrays gives the same bits).  The softmax weights enter the product with the
+ * values in fp32 (fp32 caches), in the cache's type (more than 16 query rows per key head and sequence) or as two parts of it.
+ *   q, out     device, row r at r * ld_q (ld_out) elements, [q_heads][head_dim] contiguous, in the cache's type, 16-byte
+ *              aligned, strides * element size multiples of 16
+ *   workspace  device, 16-byte aligned, at least coreinfer_paged_attention_workspace_bytes() (0 on bad sizes), which covers
+ *              every call with up to that many tokens on this cache.  Its contents need not be initialised and mean nothing
+ *              afterwards; calls that may overlap need one each.
+ * Errors: INVALID_ARG, UNSUPPORTED (as above; q_heads above 4096, tokens * q_heads above 2^29, window or sinks above 2^30), WORKSPACE, CUDA. */
+size_t coreinfer_paged_attention_workspace_bytes(const coreinfer_paged_cache* cache, int32_t q_heads, int32_t tokens);
+
+coreinfer_status coreinfer_paged_attention(const coreinfer_paged_cache* cache, const int32_t* start, int32_t tokens,
+                                           const void* q, int64_t ld_q, int32_t q_heads, float scale,
+                                           int32_t window, int32_t sinks, void* out, int64_t ld_out,
+                                           void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -19,6 +19,8 @@ FFN_RELU, FFN_RELU_GATED, FFN_SILU_GATED = 0, 1, 2
 ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
 MAX_BATCH, MAX_LAYERS = 8, 128
 KV4_MAX_BATCH, KV4_MAX_QUERIES, KV4_MAX_ROWS = 1024, 16, 2048
+ROPE_PLAIN, ROPE_LINEAR, ROPE_NTK, ROPE_YARN, ROPE_BANDS = range(5)
+PAGED_MAX_BATCH = 1024
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT = range(6)
 
 # every symbol include/coreinfer.h declares
@@ -39,6 +41,8 @@ SYMBOLS = (
     "coreinfer_w4_codes_bytes", "coreinfer_w4_pairs_bytes", "coreinfer_w4_quantize", "coreinfer_w4_matvec",
     "coreinfer_kv4_append", "coreinfer_kv4_attention_workspace_bytes", "coreinfer_kv4_attention",
     "coreinfer_kv4_evict_workspace_bytes", "coreinfer_kv4_evict",
+    "coreinfer_rope_frequencies", "coreinfer_rope_apply",
+    "coreinfer_paged_append", "coreinfer_paged_attention_workspace_bytes", "coreinfer_paged_attention",
 )
 STAMP_SLOTS = 16
 
@@ -71,6 +75,23 @@ class KV4Cache(ctypes.Structure):
                 ("position", ctypes.c_void_p), ("batch", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
                 ("capacity", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("group", ctypes.c_int32),
                 ("reserved", ctypes.c_int32)]
+
+
+class Rope(ctypes.Structure):
+    """coreinfer_rope"""
+    device = norm = None  # of the table; type and length of the norms' weights, where make_rope() has seen them
+    _fields_ = [("turns", ctypes.c_void_p), ("q_norm", ctypes.c_void_p), ("k_norm", ctypes.c_void_p), ("eps", ctypes.c_float),
+                ("magnitude", ctypes.c_float), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+
+
+class PagedCache(ctypes.Structure):
+    """coreinfer_paged_cache"""
+    device = None         # of the buffers, where make_paged_cache() has seen them
+    torch_dtype = None
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("table", ctypes.c_void_p), ("length", ctypes.c_void_p),
+                ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("dtype", ctypes.c_int), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("batch", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 _lib = None
@@ -171,6 +192,17 @@ def load() -> ctypes.CDLL:
     lib.coreinfer_kv4_evict_workspace_bytes.argtypes = [pc]
     lib.coreinfer_kv4_evict.restype = ctypes.c_int
     lib.coreinfer_kv4_evict.argtypes = [pc, pc, i32, i32, i32, vp, sz, vp]
+    pr, pp = ctypes.POINTER(Rope), ctypes.POINTER(PagedCache)
+    lib.coreinfer_rope_frequencies.restype = ctypes.c_int
+    lib.coreinfer_rope_frequencies.argtypes = [i32, f64, ctypes.c_int, f64, i32, f64, f64, ctypes.POINTER(ctypes.c_uint64), ctypes.POINTER(f32)]
+    lib.coreinfer_rope_apply.restype = ctypes.c_int
+    lib.coreinfer_rope_apply.argtypes = [pr, vp, ctypes.c_int, i32, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+    lib.coreinfer_paged_append.restype = ctypes.c_int
+    lib.coreinfer_paged_append.argtypes = [pp, vp, i32, vp, i64, vp, i64, pr, vp, vp, i64, i32, vp, i64, vp]
+    lib.coreinfer_paged_attention_workspace_bytes.restype = sz
+    lib.coreinfer_paged_attention_workspace_bytes.argtypes = [pp, i32, i32]
+    lib.coreinfer_paged_attention.restype = ctypes.c_int
+    lib.coreinfer_paged_attention.argtypes = [pp, vp, i32, vp, i64, i32, f32, i32, i32, vp, i64, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -552,5 +584,163 @@ def coreinfer_kv4_evict(src, dst, budget, recent, first, workspace, stream=None)
         _off_device("the caches and the workspace")
     status = (_lib or load()).coreinfer_kv4_evict(src, dst, budget, recent, first, workspace.data_ptr(), workspace.nbytes,
                                         _raw_stream(device, stream))
+    if status:
+        _check(status)
+
+
+def coreinfer_rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: int = ROPE_PLAIN, factor: float = 1.0,
+                               original_context: int = 0, low: float = 1.0, high: float | None = None, device=None):
+    """(fractions of a turn per position, int64 [rot_dim / 2] on `device`, magnitude); high: 32 for ROPE_YARN and 4 for ROPE_BANDS unless given."""
+    if high is None:
+        high = 32.0 if scaling == ROPE_YARN else 4.0
+    turns, magnitude = torch.empty(max(1, int(rot_dim) // 2), dtype=torch.int64), ctypes.c_float()
+    _check(load().coreinfer_rope_frequencies(int(rot_dim), float(base), int(scaling), float(factor), int(original_context), float(low), float(high),
+                                             ctypes.cast(turns.data_ptr(), ctypes.POINTER(ctypes.c_uint64)), ctypes.byref(magnitude)))
+    return (turns if device is None else turns.to(device)), magnitude.value
+
+
+def make_rope(turns, interleaved: bool = False, magnitude: float = 1.0, q_norm=None, k_norm=None, eps: float = 1e-6) -> Rope:
+    """coreinfer_rope over the caller's CUDA buffers (which must outlive it): turns int64 [rot_dim / 2] from
+    coreinfer_rope_frequencies(), q_norm and k_norm [head_dim] weights in the calls' type, or None for no norm."""
+    norms = [t for t in (q_norm, k_norm) if t is not None]
+    if turns.dtype != torch.int64 or turns.dim() != 1 or not turns.is_contiguous() or any(t.dim() != 1 or not t.is_contiguous() for t in norms):
+        raise CoreInferError(ERR_INVALID_ARG, "turns int64 [rot_dim / 2] and norm weights [head_dim], all contiguous, were expected")
+    if len({(t.dtype, t.numel()) for t in norms}) > 1:
+        raise CoreInferError(ERR_INVALID_ARG, "the norms' weights differ in type or length")
+    rope = Rope(turns.data_ptr(), None if q_norm is None else q_norm.data_ptr(), None if k_norm is None else k_norm.data_ptr(),
+                eps, magnitude, 2 * turns.numel(), 1 if interleaved else 0)
+    rope.device = _one_device("turns and the norms' weights", (turns, q_norm, k_norm))
+    rope.norm = (norms[0].dtype, norms[0].numel()) if norms else None
+    return rope
+
+
+def _packed_stride(t, tokens, heads, dim):
+    """Elements between the rows of a packed [tokens, heads, head_dim] tensor (a slice of a wider projection is fine)."""
+    if t.is_contiguous():
+        return heads * dim
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
+        raise CoreInferError(ERR_INVALID_ARG, "rows with contiguous heads were expected: shape %s, strides %s" % (tuple(t.shape), tuple(t.stride())))
+    return t.stride(0) if tokens > 1 else heads * dim
+
+
+def _on_device(device, call, *args):
+    """The call with `device` current: launches go to the current device."""
+    if device >= 0 and torch._C._cuda_getDevice() != device:
+        with torch.cuda.device(device):
+            return call(*args)
+    return call(*args)
+
+
+def _check_rope(rope, dtype, dim, device):
+    if rope.device != device and rope.device is not None:
+        _off_device("rope and the tensors that it turns")
+    if rope.norm is not None and rope.norm != (dtype, dim):
+        raise CoreInferError(ERR_INVALID_ARG, "norm weights of %s [%d] do not fit heads of %s [%d]" % (*rope.norm, dtype, dim))
+
+
+def _index(t, n, device, what):
+    """Address of an int32 tensor of n numbers."""
+    if t.dtype != torch.int32 or t.numel() != n or not t.is_contiguous() or t.get_device() != device:
+        raise CoreInferError(ERR_INVALID_ARG, "%s: %d contiguous int32 on the tensors' device were expected, got %s %s" % (what, n, t.dtype, tuple(t.shape)))
+    return t.data_ptr()
+
+
+def coreinfer_rope_apply(rope, positions, q, k, q_out, k_out, stream=None):
+    """Turn (and norm) q [tokens, q_heads, head_dim] and k [tokens, kv_heads, head_dim], either of them None, to the
+    positions int32 [tokens]; q_out and k_out may be q and k."""
+    x = q if q is not None else k
+    if x is None or x.dim() != 3 or (k is not None and (k.dim() != 3 or k.shape[0] != x.shape[0] or k.shape[2] != x.shape[2])):
+        raise CoreInferError(ERR_INVALID_ARG, "q and k [tokens, heads, head_dim] were expected")
+    tokens, _, dim = x.shape
+    dtype, device = x.dtype, x.get_device()
+    if dtype not in _DTYPE_CODES:
+        raise CoreInferError(ERR_UNSUPPORTED, "unsupported torch dtype %s" % dtype)
+    given = []
+    for t, out in ((q, q_out), (k, k_out)):
+        if (t is None) != (out is None) or (t is not None and (out.shape != t.shape or t.dtype != dtype or out.dtype != dtype)):
+            raise CoreInferError(ERR_INVALID_ARG, "q with q_out and k with k_out, of one type and shape each, were expected")
+        if t is None:
+            given += [0, None, 0, None, 0]
+            continue
+        if t.get_device() != device or out.get_device() != device:
+            _off_device("q, k and their outputs")
+        heads = t.shape[1]
+        given += [heads, t.data_ptr(), _packed_stride(t, tokens, heads, dim), out.data_ptr(), _packed_stride(out, tokens, heads, dim)]
+    _check_rope(rope, dtype, dim, device)
+    hq, qp, lq, qo, lqo, hk, kp, lk, ko, lko = given
+    status = _on_device(device, (_lib or load()).coreinfer_rope_apply, rope, _index(positions, tokens, device, "positions"), _DTYPE_CODES[dtype], tokens,
+                        hq, hk, dim, qp, lq, kp, lk, qo, lqo, ko, lko, _raw_stream(device, stream))
+    if status:
+        _check(status)
+
+
+def make_paged_cache(k, v, table, length) -> PagedCache:
+    """coreinfer_paged_cache over the caller's CUDA buffers (which must outlive it): pools [pages, kv_heads, page_size,
+    head_dim] with any strides the library takes (a transposed [pages, page_size, kv_heads, head_dim] is fine), table int32
+    [batch, max_pages], length int32 [batch]."""
+    if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.stride() != v.stride() or k.stride(3) != 1:
+        raise CoreInferError(ERR_INVALID_ARG, "pools [pages, kv_heads, page_size, head_dim] of one type, shape and strides with contiguous rows were expected")
+    if k.dtype not in _DTYPE_CODES:
+        raise CoreInferError(ERR_UNSUPPORTED, "unsupported torch dtype %s" % k.dtype)
+    if table.dim() != 2 or table.dtype != torch.int32 or not table.is_contiguous() or length.dtype != torch.int32 \
+            or length.shape != table.shape[:1] or not length.is_contiguous():
+        raise CoreInferError(ERR_INVALID_ARG, "table int32 [batch, max_pages] and length int32 [batch], contiguous, were expected")
+    pages, heads, size, dim = k.shape
+    cache = PagedCache(k.data_ptr(), v.data_ptr(), table.data_ptr(), length.data_ptr(), k.stride(0), k.stride(1), k.stride(2),
+                       _DTYPE_CODES[k.dtype], pages, size, heads, dim, table.shape[0], table.shape[1], 0)
+    cache.device, cache.torch_dtype = _one_device("a cache's buffers", (k, v, table, length)), k.dtype
+    return cache
+
+
+def _packed(cache, t, tokens, heads, device, what):
+    """Address and row stride of a packed tensor of a call on the cache."""
+    if t.shape != (tokens, heads, cache.head_dim) or (t.dtype != cache.torch_dtype and cache.torch_dtype is not None) \
+            or t.dtype not in _DTYPE_CODES or _DTYPE_CODES[t.dtype] != cache.dtype:
+        raise CoreInferError(ERR_INVALID_ARG, "%s [%d, %d, %d] in the cache's type was expected, got %s %s"
+                             % (what, tokens, heads, cache.head_dim, t.dtype, tuple(t.shape)))
+    if t.get_device() != device or (cache.device != device and cache.device is not None):
+        _off_device("the cache and the call's tensors")
+    return t.data_ptr(), _packed_stride(t, tokens, heads, cache.head_dim)
+
+
+def coreinfer_paged_append(cache, start, k, v, rope=None, positions=None, q=None, q_out=None, stream=None):
+    """k, v [tokens, kv_heads, head_dim], rows start[b] .. start[b + 1] - 1 sequence b's newest, into their slots; with
+    rope (and positions int32 [tokens] in the slots' place) k turned, and q [tokens, q_heads, head_dim] into q_out."""
+    tokens, device, dim = k.shape[0], k.get_device(), cache.head_dim
+    kp, lk = _packed(cache, k, tokens, cache.kv_heads, device, "k")
+    vp, lv = _packed(cache, v, tokens, cache.kv_heads, device, "v")
+    qp = qo = None
+    heads = lq = lqo = 0
+    if (q is None) != (q_out is None):
+        raise CoreInferError(ERR_INVALID_ARG, "q and q_out come together")
+    if q is not None:
+        heads = q.shape[1] if q.dim() == 3 else 0
+        qp, lq = _packed(cache, q, tokens, heads, device, "q")
+        qo, lqo = _packed(cache, q_out, tokens, heads, device, "q_out")
+    if rope is not None:
+        _check_rope(rope, k.dtype, dim, device)
+    status = _on_device(device, (_lib or load()).coreinfer_paged_append, cache, _index(start, cache.batch + 1, device, "start"), tokens, kp, lk, vp, lv, rope,
+                        None if positions is None else _index(positions, tokens, device, "positions"), qp, lq, heads, qo, lqo, _raw_stream(device, stream))
+    if status:
+        _check(status)
+
+
+def coreinfer_paged_attention_workspace_bytes(cache, q_heads: int, tokens: int) -> int:
+    return int(load().coreinfer_paged_attention_workspace_bytes(cache, q_heads, tokens))
+
+
+def coreinfer_paged_attention(cache, start, q, scale, out, workspace, window=0, sinks=0, stream=None):
+    """q [tokens, q_heads, head_dim], rows start[b] .. start[b + 1] - 1 sequence b's newest tokens -> out of the same shape; a token
+    sees what its sequence holds up to itself, with `window` only that many positions and the first `sinks`."""
+    if q.dim() != 3:
+        raise CoreInferError(ERR_INVALID_ARG, "q [tokens, q_heads, head_dim] was expected, got %s" % (tuple(q.shape),))
+    tokens, heads, _ = q.shape
+    device = q.get_device()
+    qp, lq = _packed(cache, q, tokens, heads, device, "q")
+    op, lo = _packed(cache, out, tokens, heads, device, "out")
+    if workspace.get_device() != device:
+        _off_device("the workspace and the call's tensors")
+    status = _on_device(device, (_lib or load()).coreinfer_paged_attention, cache, _index(start, cache.batch + 1, device, "start"), tokens, qp, lq, heads, scale,
+                        window, sinks, op, lo, workspace.data_ptr(), workspace.nbytes, _raw_stream(device, stream))
     if status:
         _check(status)

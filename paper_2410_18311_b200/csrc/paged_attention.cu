@@ -1,0 +1,321 @@
+// Attention of new tokens over a paged cache: the entry points, the form in fp32, and the kernel that joins the pieces of units
+// that are cut.
+//
+// Mathematics.  One pass over the positions that a unit's rows see, with a running maximum m (base 2), sum l and output o
+// per row:  m' = max(m, s),  l' = 2^(m - m') l + sum 2^(s - m'),  o' = 2^(m - m') o + sum 2^(s - m') v;  out = o / l.  Pieces of
+// a unit are joined by the same rule.  A row whose seen logits are all -infinity comes out NaN, as the formula says (0 / 0);
+// one that sees nothing comes out 0.
+#include "paged_attention.cuh"
+
+namespace coreinfer {
+
+constexpr int kSimpleThreads = 256;
+constexpr int kSimpleRows = 16;
+constexpr int kSimpleTile = 64;
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kSimpleThreads) paged_simple_kernel(const __grid_constant__ PagedAttnArgs a)
+{
+    constexpr int RU = kSimpleRows, KT = kSimpleTile;
+    constexpr int KP = D + 4;                        // row of the keys: no two lanes of a 16-byte read share banks
+    constexpr int CG = D / 4, RPT = RU * CG / kSimpleThreads;
+    extern __shared__ __align__(16) float smem[];
+    float* qs = smem;                                // [RU][D]
+    float* ks = qs + RU * D;                         // [KT][KP]
+    float* vs = ks + KT * KP;                        // [KT][D]
+    float* ps = vs + KT * D;                         // [RU][KT + 4]
+    float* ms = ps + RU * (KT + 4);                  // [RU] reference exponents
+    float* ls = ms + RU;                             // [RU] sums
+    float* fs = ls + RU;                             // [RU] factor of what was summed before
+    long long* at = reinterpret_cast<long long*>(fs + RU);
+    const int tid = threadIdx.x;
+    wait_for_stream();
+    const long long total = paged_plan(a, at);
+    if (tid == 0) a.pieces[blockIdx.x].last = -1;
+    PagedWalk w;
+    for (w.begin(a, at, total, blockIdx.x); w.more(); w.next(a, at)) {
+        const int rows = paged_unit_rows(a, w), r0 = w.tile * RU;
+        const int from = w.from(a), to = w.to(a);
+        if (w.t.count > 0 && from >= to) continue;
+        __syncthreads();
+        for (int i = tid; i < RU * D; i += kSimpleThreads) {
+            const int r = i / D, d = i - r * D;
+            qs[i] = r < rows ? to_f32(reinterpret_cast<const T*>(a.q)[paged_row_offset(a, w.s, w.h, r0 + r, a.ld_q) + d]) : 0.f;
+        }
+        if (tid < RU) {
+            ms[tid] = -INFINITY;
+            ls[tid] = 0.f;
+        }
+        float o[RPT][4];
+#pragma unroll
+        for (int r = 0; r < RPT; ++r)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[r][e] = 0.f;
+        for (int i = from; i < to; ++i) {
+            const int j0 = paged_tile_at(w.t, i) * KT;
+            __syncthreads();
+            for (int x = tid; x < KT * D / 8; x += kSimpleThreads) {
+                const int j = x / (D / 8), d = (x - j * (D / 8)) * 8;
+                float k8[8], v8[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) k8[e] = v8[e] = 0.f;
+                const int page = j0 + j < w.t.hi ? paged_page(a.c, w.b, j0 + j) : -1;
+                if (page >= 0) {
+                    const long long at8 = paged_offset(a.c, page, w.h, j0 + j) + d;
+                    uint4 raw[sizeof(T) / 2];
+#pragma unroll
+                    for (int e = 0; e < (int)sizeof(T) / 2; ++e) raw[e] = reinterpret_cast<const uint4*>(a.c.pool[0] + at8 * sizeof(T))[e];
+                    unpack8<T>(raw, k8);
+#pragma unroll
+                    for (int e = 0; e < (int)sizeof(T) / 2; ++e) raw[e] = reinterpret_cast<const uint4*>(a.c.pool[1] + at8 * sizeof(T))[e];
+                    unpack8<T>(raw, v8);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    ks[j * KP + d + e] = k8[e];
+                    vs[j * D + d + e] = v8[e];
+                }
+            }
+            __syncthreads();
+            {
+                const int j = tid & (KT - 1), rg = tid / KT * 4;
+                float s[4] = {0.f, 0.f, 0.f, 0.f};
+                for (int d = 0; d < D; d += 4) {
+                    const float4 k = *reinterpret_cast<const float4*>(ks + j * KP + d);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float4 q = *reinterpret_cast<const float4*>(qs + (rg + r) * D + d);
+                        s[r] = fmaf(q.x, k.x, fmaf(q.y, k.y, fmaf(q.z, k.z, fmaf(q.w, k.w, s[r]))));
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const bool seen = rg + r < rows && paged_sees(a, paged_row(a, w.s, r0 + rg + r), j0 + j);
+                    ps[(rg + r) * (KT + 4) + j] = seen ? s[r] * a.scale2 : -INFINITY;
+                }
+            }
+            __syncthreads();
+            {
+                const int r = tid / 16, c = tid % 16;
+                float s[4], m = ms[r];
+                const float before = m;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[e] = ps[r * (KT + 4) + c + 16 * e];
+                    m = fmaxf(m, s[e]);
+                }
+#pragma unroll
+                for (int d = 1; d < 16; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+                const float ref = m == -INFINITY ? 0.f : m;
+                float sum = 0.f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[e] = exp2f(s[e] - ref);
+                    ps[r * (KT + 4) + c + 16 * e] = s[e];
+                    sum += s[e];
+                }
+#pragma unroll
+                for (int d = 1; d < 16; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+                if (c == 0) {
+                    const float f = exp2f(before - ref);
+                    fs[r] = f;
+                    ms[r] = m;
+                    ls[r] = fmaf(ls[r], f, sum);
+                }
+            }
+            __syncthreads();
+            {
+                const int c = tid % CG * 4, rg = tid / CG * RPT;
+                // where some row does not see some position, a weight of 0 must not meet what it must not see
+                const PagedRow low = paged_row(a, w.s, r0), high = paged_row(a, w.s, r0 + rows - 1);
+                const bool whole = j0 + KT <= low.hi && (j0 >= high.lo || j0 + KT <= a.sinks);
+#pragma unroll
+                for (int r = 0; r < RPT; ++r) {
+                    const float f = fs[rg + r];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[r][e] *= f;
+                    const PagedRow row = paged_row(a, w.s, r0 + rg + r);
+                    for (int j = 0; j < KT; ++j) {
+                        const float p = ps[(rg + r) * (KT + 4) + j];
+                        const float4 v = *reinterpret_cast<const float4*>(vs + j * D + c);
+                        if (whole || paged_sees(a, row, j0 + j)) {
+                            o[r][0] = fmaf(p, v.x, o[r][0]);
+                            o[r][1] = fmaf(p, v.y, o[r][1]);
+                            o[r][2] = fmaf(p, v.z, o[r][2]);
+                            o[r][3] = fmaf(p, v.w, o[r][3]);
+                        }
+                    }
+                }
+            }
+        }
+        __syncthreads();
+        const int c = tid % CG * 4, rg = tid / CG * RPT;
+        const bool head = from == 0, tail = to == w.t.count;
+#pragma unroll
+        for (int r = 0; r < RPT; ++r) {
+            const int row = rg + r;
+            if (row >= rows) continue;
+            if (head && tail) {
+                const PagedRow see = paged_row(a, w.s, r0 + row);
+                const float l = ls[row];
+                T* to_row = reinterpret_cast<T*>(a.out) + paged_row_offset(a, w.s, w.h, r0 + row, a.ld_out) + c;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) to_row[e] = from_f32<T>(see.hi > 0 ? o[r][e] / l : 0.f);
+            } else {
+                const size_t slot = (size_t)blockIdx.x * 2 + (head ? 1 : 0);
+                *reinterpret_cast<float4*>(a.part_o + (slot * RU + row) * D + c) = make_float4(o[r][0], o[r][1], o[r][2], o[r][3]);
+                if (c == 0) a.part_ml[slot * RU + row] = make_float2(ms[row], ls[row]);
+            }
+        }
+        if (head && !tail && tid == 0) {
+            PagedPiece p;
+            p.b = w.b;
+            p.h = w.h;
+            p.tile = w.tile;
+            p.last = paged_owner(total, w.base + a.cost + w.t.count - 1, w.n);
+            a.pieces[blockIdx.x] = p;
+        }
+    }
+    let_next_start();
+}
+
+// Joins the pieces of a unit that is cut: block (x, y) the rows y of the unit whose first tile CTA x has.  The first piece is in
+// that CTA's second slot, the others in the first slots of the CTAs behind it.
+constexpr int kJoinThreads = 256;
+template <typename T, int D>
+__global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_constant__ PagedAttnArgs a)
+{
+    constexpr int CG = D / 4, ROWS = kJoinThreads / CG;
+    wait_for_stream();
+    const PagedPiece p = a.pieces[blockIdx.x];
+    if (p.last < 0) return;
+    const PagedSeq s = paged_seq(a.c, p.b);
+    const int row = blockIdx.y * ROWS + threadIdx.x / CG, c = threadIdx.x % CG * 4;
+    const int global_row = p.tile * a.RU + row;
+    if (row >= a.RU || global_row >= paged_rows(a, s)) return;
+    const int first = blockIdx.x;
+    auto slot = [&](int i) { return (size_t)i * 2 + (i == first ? 1 : 0); };
+    float m = -INFINITY;
+    for (int i = first; i <= p.last; ++i) m = fmaxf(m, a.part_ml[slot(i) * a.RU + row].x);
+    const float ref = m == -INFINITY ? 0.f : m;
+    float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int i = first; i <= p.last; ++i) {
+        const float2 ml = a.part_ml[slot(i) * a.RU + row];
+        const float f = exp2f(ml.x - ref);
+        const float4 x = *reinterpret_cast<const float4*>(a.part_o + (slot(i) * a.RU + row) * D + c);
+        l = fmaf(ml.y, f, l);
+        // a piece in which the row sees nothing, or nothing but weights of 0, has nothing to add
+        if (ml.x == -INFINITY) continue;
+        o[0] = fmaf(x.x, f, o[0]);
+        o[1] = fmaf(x.y, f, o[1]);
+        o[2] = fmaf(x.z, f, o[2]);
+        o[3] = fmaf(x.w, f, o[3]);
+    }
+    const bool sees = paged_row(a, s, global_row).hi > 0;
+    T* to = reinterpret_cast<T*>(a.out) + paged_row_offset(a, s, p.h, global_row, a.ld_out) + c;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) to[e] = from_f32<T>(sees ? o[e] / l : 0.f);
+}
+
+template <typename T, int D>
+static coreinfer_status launch_simple(PagedAttnArgs& a, const DeviceInfo& di, cudaStream_t st)
+{
+    const size_t smem = (size_t)(kSimpleRows * D + kSimpleTile * (D + 4) + kSimpleTile * D + kSimpleRows * (kSimpleTile + 4) + 3 * kSimpleRows) * 4 +
+                        (size_t)(a.c.B + 1) * 8;
+    coreinfer_status s = allow_smem<paged_simple_kernel<T, D>>(di);
+    if (s != COREINFER_OK) return s;
+    CI_CUDA(launch_overlapped(paged_simple_kernel<T, D>, dim3(a.n_ctas), dim3(kSimpleThreads), smem, st, a));
+    constexpr int ROWS = kJoinThreads / (D / 4);
+    CI_CUDA(launch_overlapped(paged_join_kernel<T, D>, dim3(a.n_ctas, (a.RU + ROWS - 1) / ROWS), dim3(kJoinThreads), 0, st, a));
+    return COREINFER_OK;
+}
+
+template <typename T>
+static coreinfer_status pick_simple(PagedAttnArgs& a, const DeviceInfo& di, cudaStream_t st)
+{
+    if (a.c.D == 64) return launch_simple<T, 64>(a, di, st);
+    return a.c.D == 128 ? launch_simple<T, 128>(a, di, st) : launch_simple<T, 256>(a, di, st);
+}
+
+static size_t round16(size_t n) { return (n + 15) / 16 * 16; }
+// Rows of a unit and CTAs, of whichever form the call takes.
+static void paged_shape(coreinfer_dtype, int, int* ru, int* ctas)
+{
+    *ru = kSimpleRows;
+    *ctas = 148 * 2;
+}
+static size_t paged_workspace(int ru, int ctas, int D)
+{
+    return round16(ctas * sizeof(PagedPiece)) + round16((size_t)ctas * 2 * ru * sizeof(float2)) + (size_t)ctas * 2 * ru * D * sizeof(float);
+}
+
+}  // namespace coreinfer
+
+using namespace coreinfer;
+
+extern "C" {
+
+size_t coreinfer_paged_attention_workspace_bytes(const coreinfer_paged_cache* cache, int32_t q_heads, int32_t tokens)
+{
+    Paged c;
+    if (paged_take(cache, &c) != COREINFER_OK || q_heads < 1 || q_heads % c.H != 0 || tokens < 1) return 0;
+    int ru, ctas;
+    paged_shape(cache->dtype, c.D, &ru, &ctas);
+    return paged_workspace(ru, ctas, c.D);
+}
+
+coreinfer_status coreinfer_paged_attention(const coreinfer_paged_cache* cache, const int32_t* start, int32_t tokens,
+                                           const void* q, int64_t ld_q, int32_t q_heads, float scale,
+                                           int32_t window, int32_t sinks, void* out, int64_t ld_out,
+                                           void* workspace, size_t workspace_bytes, void* cuda_stream)
+{
+    PagedAttnArgs a = {};
+    coreinfer_status s = paged_take(cache, &a.c);
+    if (s != COREINFER_OK) return s;
+    const coreinfer_dtype dtype = cache->dtype;
+    if (q_heads < 1 || q_heads % a.c.H != 0)
+        CI_FAIL(COREINFER_ERR_INVALID_ARG, "q_heads %d is not a multiple of kv_heads %d", q_heads, a.c.H);
+    if (q_heads > 4096) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "q_heads %d: at most 4096", q_heads);
+    if (tokens < 1) CI_FAIL(COREINFER_ERR_INVALID_ARG, "tokens must be >= 1");
+    if ((long long)tokens * q_heads > 1LL << 29) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "tokens %d: too many for one call", tokens);
+    if (!start || !aligned_to(start, 4)) CI_FAIL(COREINFER_ERR_INVALID_ARG, "start NULL or misaligned");
+    if (!rows_fit(q, ld_q, q_heads, a.c.D, dtype) || !rows_fit(out, ld_out, q_heads, a.c.D, dtype))
+        CI_FAIL(COREINFER_ERR_INVALID_ARG, "q / out NULL, not 16-byte aligned, or strides too small or not multiples of 16 bytes");
+    if (window < 0 || sinks < 0) CI_FAIL(COREINFER_ERR_INVALID_ARG, "window and sinks must be >= 0");
+    if (window > 1 << 30 || sinks > 1 << 30) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "window and sinks: at most 2^30");
+    if (!isfinite(scale)) CI_FAIL(COREINFER_ERR_INVALID_ARG, "scale must be finite");
+    if (!workspace || !aligned16(workspace)) CI_FAIL(COREINFER_ERR_WORKSPACE, "workspace is NULL or misaligned");
+    int ru, ctas;
+    paged_shape(dtype, a.c.D, &ru, &ctas);
+    const size_t need = paged_workspace(ru, ctas, a.c.D);
+    if (workspace_bytes < need) CI_FAIL(COREINFER_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
+    DeviceInfo di;
+    if ((s = device_info(&di)) != COREINFER_OK) return s;
+    a.c.start = start;
+    a.c.tokens = tokens;
+    a.q = (const uint8_t*)q;
+    a.out = (uint8_t*)out;
+    a.ld_q = ld_q;
+    a.ld_out = ld_out;
+    a.share = q_heads / a.c.H;
+    a.window = window;
+    a.sinks = window ? sinks : 0;
+    a.scale2 = scale * kLog2e;
+    a.RU = ru;
+    a.KT = kSimpleTile;
+    a.cost = 1;
+    a.n_ctas = ctas;
+    uint8_t* ws = (uint8_t*)workspace;
+    a.pieces = (PagedPiece*)ws;
+    ws += round16(ctas * sizeof(PagedPiece));
+    a.part_ml = (float2*)ws;
+    ws += round16((size_t)ctas * 2 * ru * sizeof(float2));
+    a.part_o = (float*)ws;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (dtype == COREINFER_F32) return pick_simple<float>(a, di, st);
+    if (dtype == COREINFER_BF16) return pick_simple<__nv_bfloat16>(a, di, st);
+    return pick_simple<__half>(a, di, st);
+}
+
+}  // extern "C"

@@ -1,0 +1,190 @@
+// What the forms of attention over a paged cache share: the list of work, how it is cut over the CTAs, which positions a
+// row sees, and how the pieces of a unit are left for the kernel that joins them.
+//
+// A unit is RU query rows (row = token * share + head of the group) of one sequence and key head; its work is the tiles of
+// KT positions that some of its rows see (the first tokens' tiles, then those from the window's start on).  The tiles of all units,
+// with an entry cost for each unit's start, form one list that is cut into equal pieces, one per CTA, whatever the lengths
+// are: a CTA meets at most two units that it shares with others, its first and its last.  Lengths are known on the device only,
+// so every CTA works the list out for itself (a thread per sequence and a scan; about 1.5 us of latency).
+#pragma once
+
+#include "paged.cuh"
+
+namespace coreinfer {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kPagedMaxCtas = 640;
+
+// Which CTAs work on a unit that is cut; written by the CTA that has its first tile, read by the joining kernel.
+struct PagedPiece {
+    int b, h, tile;         // sequence, key head, row tile
+    int last;               // the last CTA with a piece of it; below 0: nothing to join
+};
+
+struct PagedAttnArgs {
+    Paged c;
+    const uint8_t* q;
+    uint8_t* out;
+    long long ld_q, ld_out;
+    int share;              // query heads per key head
+    int window, sinks;      // window 0: everything before a token
+    float scale2;           // scale * log2(e)
+    int RU, KT, cost;       // rows of a unit, positions of a tile, entries that a unit's start counts
+    int n_ctas;
+    PagedPiece* pieces;     // [n_ctas]
+    float2* part_ml;        // [n_ctas][2][RU]: reference exponent (base 2) and sum
+    float* part_o;          // [n_ctas][2][RU][D]
+};
+
+#ifdef __CUDACC__
+
+// The tiles that the rows of a unit see.
+struct PagedTiles {
+    int count;              // tiles of the unit
+    int first_tiles;        // of them, in front: tiles of the first tokens
+    int from;               // tile that follows those
+    int hi;                 // positions below this are seen by some row
+};
+__device__ __forceinline__ int paged_rows(const PagedAttnArgs& a, const PagedSeq& s) { return s.n * a.share; }
+__device__ __forceinline__ int paged_row_tiles(const PagedAttnArgs& a, const PagedSeq& s) { return (paged_rows(a, s) + a.RU - 1) / a.RU; }
+__device__ __forceinline__ PagedTiles paged_tiles(const PagedAttnArgs& a, const PagedSeq& s, int tile)
+{
+    const int rows = paged_rows(a, s), r0 = tile * a.RU;
+    const int r1 = (r0 + a.RU < rows ? r0 + a.RU : rows) - 1;
+    const int p0 = s.position + r0 / a.share, p1 = s.position + r1 / a.share;
+    PagedTiles t;
+    t.hi = clamp_int(p1 + 1, 0, a.c.cap);
+    const int lo = a.window ? clamp_int(p0 - a.window + 1, 0, t.hi) : 0;
+    t.from = lo / a.KT;
+    const int first = a.sinks < t.hi ? a.sinks : t.hi;
+    t.first_tiles = (first + a.KT - 1) / a.KT;
+    if (t.first_tiles > t.from) t.first_tiles = t.from;
+    t.count = (t.hi + a.KT - 1) / a.KT - t.from + t.first_tiles;
+    return t;
+}
+__device__ __forceinline__ int paged_tile_at(const PagedTiles& t, int i) { return i < t.first_tiles ? i : i - t.first_tiles + t.from; }
+
+// What one row sees: positions below hi that are at lo or behind it, or below `sinks`.
+struct PagedRow {
+    int lo, hi;
+};
+__device__ __forceinline__ PagedRow paged_row(const PagedAttnArgs& a, const PagedSeq& s, int row)
+{
+    const int p = s.position + row / a.share;
+    PagedRow r;
+    r.hi = clamp_int(p + 1, 0, a.c.cap);
+    r.lo = a.window ? p - a.window + 1 : 0;
+    return r;
+}
+__device__ __forceinline__ bool paged_sees(const PagedAttnArgs& a, const PagedRow& r, int j) { return j < r.hi && (j >= r.lo || j < a.sinks); }
+
+// The list.  `at` [B + 1] in shared memory; called by all threads of the CTA (a multiple of 32).
+__device__ __forceinline__ long long paged_plan(const PagedAttnArgs& a, long long* at)
+{
+    for (int b = threadIdx.x; b < a.c.B; b += blockDim.x) {
+        const PagedSeq s = paged_seq(a.c, b);
+        const int tiles = paged_row_tiles(a, s);
+        long long w = 0;
+        for (int i = 0; i < tiles; ++i) w += a.cost + paged_tiles(a, s, i).count;
+        at[b + 1] = w * a.c.H;
+    }
+    if (threadIdx.x == 0) at[0] = 0;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        long long carry = 0;
+        for (int b0 = 0; b0 < a.c.B; b0 += 32) {
+            const int b = b0 + threadIdx.x;
+            long long w = b < a.c.B ? at[b + 1] : 0;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const long long left = __shfl_up_sync(0xffffffffu, w, d);
+                if (threadIdx.x >= d) w += left;
+            }
+            w += carry;
+            if (b < a.c.B) at[b + 1] = w;
+            carry = __shfl_sync(0xffffffffu, w, 31);
+        }
+    }
+    __syncthreads();
+    return at[a.c.B];
+}
+// The list in n equal pieces (n at most its length, so that none is empty): piece i is [total * i / n, total * (i + 1) / n).
+__device__ __forceinline__ long long paged_cut(long long total, int i, int n) { return total / n * i + total % n * i / n; }
+// The piece that holds an entry: the largest i with total * i / n <= x.
+__device__ __forceinline__ int paged_owner(long long total, long long x, int n) { return (int)(((x + 1) * n - 1) / total); }
+
+// Walks the units of a piece [x, end) of the list.
+struct PagedWalk {
+    long long x, end;       // entries of the piece not walked yet
+    int n;                  // pieces
+    int b, h, tile;
+    long long base;         // entry where the unit starts
+    PagedSeq s;
+    PagedTiles t;
+
+    __device__ __forceinline__ void begin(const PagedAttnArgs& a, const long long* at, long long total, int cta)
+    {
+        n = total < a.n_ctas ? (int)total : a.n_ctas;
+        x = end = 0;
+        if (cta >= n) return;
+        x = paged_cut(total, cta, n);
+        end = paged_cut(total, cta + 1, n);
+        int lo = 0, hi = a.c.B;                      // at[lo] <= x < at[hi]
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (at[mid] <= x) lo = mid;
+            else hi = mid;
+        }
+        b = lo;
+        s = paged_seq(a.c, b);
+        const long long per_head = (at[b + 1] - at[b]) / a.c.H;
+        h = (int)((x - at[b]) / per_head);
+        base = at[b] + h * per_head;
+        tile = 0;
+        t = paged_tiles(a, s, 0);
+        while (base + a.cost + t.count <= x) {
+            base += a.cost + t.count;
+            t = paged_tiles(a, s, ++tile);
+        }
+    }
+    __device__ __forceinline__ bool more() const { return x < end; }
+    // Tiles from .. to - 1 of the unit are this piece's.
+    __device__ __forceinline__ int from(const PagedAttnArgs& a) const { return x > base + a.cost ? (int)(x - base) - a.cost : 0; }
+    __device__ __forceinline__ int to(const PagedAttnArgs& a) const
+    {
+        const long long n = end - base - a.cost;
+        return n < 0 ? 0 : (n < t.count ? (int)n : t.count);
+    }
+    __device__ __forceinline__ void next(const PagedAttnArgs& a, const long long* at)
+    {
+        base += a.cost + t.count;
+        x = base;
+        if (x >= end) return;
+        if (++tile == paged_row_tiles(a, s)) {
+            tile = 0;
+            if (++h == a.c.H) {
+                h = 0;
+                do ++b; while (at[b + 1] == at[b]);
+                s = paged_seq(a.c, b);
+            }
+        }
+        t = paged_tiles(a, s, tile);
+    }
+};
+
+// Rows of a unit.
+__device__ __forceinline__ int paged_unit_rows(const PagedAttnArgs& a, const PagedWalk& w)
+{
+    const int left = paged_rows(a, w.s) - w.tile * a.RU;
+    return left < a.RU ? left : a.RU;
+}
+// Element offset of a row of a unit in q or out.
+__device__ __forceinline__ long long paged_row_offset(const PagedAttnArgs& a, const PagedSeq& s, int h, int row, long long ld)
+{
+    const int t = row / a.share;
+    return (long long)(s.first + t) * ld + (long long)(h * a.share + row - t * a.share) * a.c.D;
+}
+
+#endif
+
+}  // namespace coreinfer

@@ -1,0 +1,222 @@
+"""Rotary positions, the paged cache and attention over it, against the formulas in 64 bits within bounds that follow from the
+arithmetic (paged_ref.py)."""
+import math
+
+import pytest
+import torch
+
+import paper_2410_18311_b200 as ci
+from helpers import require_gpu
+from paged_ref import DT, Batch, attention, check, frequencies, turn
+
+pytestmark = pytest.mark.gpu
+KIND = {"plain": ci.ROPE_PLAIN, "linear": ci.ROPE_LINEAR, "ntk": ci.ROPE_NTK, "yarn": ci.ROPE_YARN, "bands": ci.ROPE_BANDS}
+
+
+def rand(*shape, dt, seed=0):
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(seed)).to(dt).cuda()
+
+
+# ---------------------------------------------------------------------------------- rope --
+
+ROPE = [
+    # tokens, q heads, kv heads, D, rot, interleaved, norm, dtype, kind
+    (1, 12, 12, 64, 64, False, False, "f32", "plain"), (3, 8, 2, 128, 128, False, True, "bf16", "bands"), (5, 4, 4, 128, 64, True, True, "f16", "yarn"),
+    (2, 2, 1, 256, 256, False, True, "f32", "ntk"), (7, 1, 0, 256, 48, False, False, "bf16", "linear"), (300, 0, 3, 64, 16, True, True, "f32", "yarn"),
+    (1000, 1, 1, 64, 32, False, True, "f16", "plain"), (777, 5, 1, 128, 80, False, True, "bf16", "bands"), (601, 71, 1, 64, 48, True, False, "f16", "ntk"),
+    (2500, 2, 1, 64, 64, False, True, "bf16", "plain"), (3001, 1, 0, 64, 64, True, True, "f32", "plain"),
+]
+
+
+@pytest.mark.parametrize("tokens,Hq,H,D,rot,interleaved,norm,dtype,kind", ROPE)
+def test_rope(tokens, Hq, H, D, rot, interleaved, norm, dtype, kind):
+    """Slices of one projection, positions from negative ones to 2^31 - 1; then the same in place."""
+    require_gpu()
+    dt, eps = DT[dtype], 1e-5
+    args = dict(base=500000.0 if kind == "bands" else 10000.0, kind=kind, factor=8.0, context=4096)
+    f, magnitude = frequencies(rot, **args)
+    turns, got_magnitude = ci.coreinfer_rope_frequencies(rot, args["base"], KIND[kind], 8.0, 4096, device="cuda")
+    assert got_magnitude == pytest.approx(magnitude, rel=1e-6)
+    # far positions in the reference are exact products of the 64-bit fractions too, which are cut to steps of 2^-64 of a turn:
+    # 2 pi 2^-64 = 3.4e-19 radians, below 2^-61
+    fx = [int(t) & (2 ** 64 - 1) for t in turns.tolist()]
+    assert all(abs(x / 2 ** 64 * 2 * math.pi - y) <= 1e-14 * y + 2.0 ** -61 for x, y in zip(fx, f.tolist()))
+    fused = rand(tokens, (Hq + 2 * H) * D, dt=dt, seed=tokens) * 3
+    q = fused[:, :Hq * D].unflatten(-1, (Hq, D)) if Hq else None
+    k = fused[:, Hq * D:(Hq + H) * D].unflatten(-1, (H, D)) if H else None
+    wq, wk = ((1 + 0.2 * rand(D, dt=torch.float32, seed=s)).to(dt) if norm else None for s in (1, 2))
+    positions = torch.randint(0, 1 << 20, (tokens,), generator=torch.Generator().manual_seed(5), dtype=torch.int32)
+    positions[0] = 2 ** 31 - 1
+    positions[-1] = -77 if tokens > 1 else 2 ** 31 - 1
+    rope = ci.make_rope(turns, interleaved, got_magnitude, wq, wk, eps)
+    outs = [None if t is None else torch.full((tokens, t.shape[1] + 1, D), float("nan"), dtype=dt, device="cuda")[:, :-1] for t in (q, k)]
+    ci.coreinfer_rope_apply(rope, positions.cuda(), q, k, *outs)
+    # angles modulo a turn, from integers
+    small = torch.tensor([[int(p) * x % 2 ** 64 / 2 ** 64 * 2 * math.pi for x in fx] for p in positions.tolist()], dtype=torch.float64)
+    for x, out, w in ((q, outs[0], wq), (k, outs[1], wk)):
+        if x is None:
+            continue
+        want, tol = zip(*[turn(x[t:t + 1], torch.ones(1), small[t], magnitude, interleaved, w, eps) for t in range(tokens)])
+        check(out, torch.cat(want), torch.cat(tol))
+    ci.coreinfer_rope_apply(rope, positions.cuda(), q, k, q, k)
+    for x, out in zip((q, k), outs):
+        assert x is None or torch.equal(x, out)
+
+
+def test_rope_norm_of_one_side_and_unusual_values():
+    require_gpu()
+    D, dt = 128, torch.bfloat16
+    turns, _ = ci.coreinfer_rope_frequencies(64, device="cuda")
+    q, k = rand(4, 3, D, dt=dt), rand(4, 2, D, dt=dt, seed=1)
+    q[0, 0], q[1, 1, 100], q[2, 2, 5] = 0.0, float("nan"), float("inf")
+    w = (1 + rand(D, dt=dt, seed=2)).to(dt)
+    at = torch.arange(4, dtype=torch.int32).cuda()
+    f, m = frequencies(64, 10000.0)
+    for wq, wk in ((w, None), (None, w), (w, w)):
+        qo, ko = torch.empty_like(q), torch.empty_like(k)
+        ci.coreinfer_rope_apply(ci.make_rope(turns, False, 1.0, wq, wk, 1e-6), at, q, k, qo, ko)
+        for h in range(2):
+            check(ko[:, h], *[t[:, h] for t in turn(k, at, f, m, False, wk, 1e-6)])
+        want, tol = turn(q, at, f, m, False, wq, 1e-6)
+        assert torch.isfinite(qo[0]).all()
+        check(qo[3], want[3], tol[3])
+        check(qo[0, 1:], want[0, 1:], tol[0, 1:])
+        if wq is None:                                           # what is not finite reaches its own pair, or with a norm its head
+            bad = ~torch.isfinite(qo)
+            assert bad[1, 1].nonzero().flatten().tolist() == [100] and set(bad[2, 2].nonzero().flatten().tolist()) <= {5, 37} and bad.sum() <= 3
+        else:
+            assert torch.isnan(qo[1, 1]).all() and torch.isfinite(qo[1, 0]).all() and torch.isfinite(qo[2, :2]).all()
+
+
+# -------------------------------------------------------------------------------- append --
+
+APPEND = [
+    # new, length, H, share, D, page, dtype, order, rot, interleaved, norm
+    ([1], [1], 1, 1, 64, 16, "f32", "heads", 0, False, False), ([5, 0, 1], [21, 9, 33], 2, 2, 128, 16, "bf16", "tokens", 128, False, True),
+    ([40, 33], [40, 100], 3, 4, 64, 32, "f16", "heads", 32, True, False), ([3, 3], [300, 3], 1, 5, 256, 128, "bf16", "heads", 256, False, True),
+    ([1] * 70, list(range(1, 71)), 2, 1, 64, 16, "f16", "tokens", 64, False, False), ([700], [900], 1, 1, 128, 64, "f32", "tokens", 64, True, True),
+    ([17, 2], [256, 257], 2, 1, 256, 256, "f16", "heads", 0, False, False),
+]
+
+
+@pytest.mark.parametrize("new,length,H,share,D,page,dtype,order,rot,interleaved,norm", APPEND)
+def test_append(new, length, H, share, D, page, dtype, order, rot, interleaved, norm):
+    """Rows of nobody before and behind, slices of one projection; every other slot and row keeps its bits."""
+    require_gpu()
+    b = Batch(new, length, H, share, D, page, dtype, order, seed=page, front=2, pad=3, wide=8 if order == "heads" else 0)
+    Hq = H * share
+    fused = b.rand(Hq + 2 * H)
+    q, k, v = fused[:, :Hq], fused[:, Hq:Hq + H], fused[:, Hq + H:]
+    before = [p.clone() for p in (b.k, b.v)]
+    q_out = torch.full((b.tokens, Hq, D), float("nan"), dtype=b.dt, device="cuda")
+    if rot:
+        turns, m = ci.coreinfer_rope_frequencies(rot, device="cuda")
+        w = (1 + 0.1 * rand(D, dt=torch.float32, seed=9)).to(b.dt) if norm else None
+        f, _ = frequencies(rot, 10000.0)
+        ci.coreinfer_paged_append(b.handle(), b.start, k, v, ci.make_rope(turns, interleaved, m, w, w, 1e-6), None, q, q_out)
+    else:
+        ci.coreinfer_paged_append(b.handle(), b.start, k, v)
+    touched = torch.zeros(b.k.shape[0], page, dtype=torch.bool)
+    for s, n in enumerate(new):
+        at = torch.arange(length[s] - n, length[s])
+        rows = slice(b.starts[s], b.starts[s] + n)
+        page_of, slot = b.table[s].cpu()[at // page].long(), at % page
+        touched[page_of, slot] = True
+        got = b.k[page_of.cuda(), :, slot.cuda()]
+        assert torch.equal(b.v[page_of.cuda(), :, slot.cuda()], v[rows])
+        if rot:
+            check(got, *turn(k[rows], at, f, m, interleaved, w, 1e-6))
+            check(q_out[rows], *turn(q[rows], at, f, m, interleaved, w, 1e-6))
+        else:
+            assert torch.equal(got, k[rows])
+    bits = {2: torch.int16, 4: torch.int32}[b.k.element_size()]
+    for pool, old in ((b.k, before[0]), (b.v, before[1])):
+        same = pool.contiguous().view(bits) == old.contiguous().view(bits)
+        assert same.all(-1).all(1).cpu()[~touched].all()
+    assert torch.isnan(q_out[:2]).all() and torch.isnan(q_out[b.starts[-1]:]).all()
+    if not rot:
+        assert torch.isnan(q_out).all()
+
+
+def test_append_given_positions_equals_rope_apply():
+    """Positions of the caller's in the slots' place, and in place of q: the same bits as the operator alone."""
+    require_gpu()
+    b = Batch([6, 1], [30, 2], 2, 3, 128, 16, "bf16")
+    q, k, v = b.rand(6), b.rand(2), b.rand(2)
+    turns, m = ci.coreinfer_rope_frequencies(128, 500000.0, ci.ROPE_YARN, 4.0, 2048, device="cuda")
+    w = (1 + 0.1 * rand(128, dt=torch.float32)).to(b.dt)
+    rope = ci.make_rope(turns, True, m, w, w)
+    at = torch.tensor([5, 100000, 3, 3, 70, 1, 9], dtype=torch.int32).cuda()
+    qo, ko = torch.empty_like(q), torch.empty_like(k)
+    ci.coreinfer_rope_apply(rope, at, q, k, qo, ko)
+    ci.coreinfer_paged_append(b.handle(), b.start, k, v, rope, at, q, q)
+    assert torch.equal(q, qo)
+    stored = torch.cat([b.slots(0)[0][-6:], b.slots(1)[0][-1:]])
+    assert torch.equal(stored, ko.double())
+
+
+def test_append_outside_the_cache_stores_nothing():
+    """Pages that are none, positions below 0 and behind the table, starts that run backwards: no slot changes but those that exist."""
+    require_gpu()
+    H, D, page = 2, 64, 16
+    k, v = torch.zeros(3, H, page, D, device="cuda"), torch.zeros(3, H, page, D, device="cuda")
+    table = torch.tensor([[0, 5], [-1, 1], [2, 2]], dtype=torch.int32).cuda()
+    length = torch.tensor([20, 18, 1], dtype=torch.int32).cuda()
+    start = torch.tensor([0, 8, 12, 15], dtype=torch.int32).cuda()
+    x = torch.ones(15, H, D, device="cuda")
+    cache = ci.make_paged_cache(k, v, table, length)
+    ci.coreinfer_paged_append(cache, start, x, x)
+    # sequence 0: positions 12 .. 15 in page 0, 16 .. 19 in a page that is none; 1: 14, 15 in none, 16, 17 in page 1; 2: -2, -1, 0
+    for pool in (k, v):
+        want = torch.zeros_like(pool)
+        want[0, :, 12:16] = want[1, :, 0:2] = want[2, :, 0:1] = 1
+        assert torch.equal(pool, want)
+    k.zero_()
+    v.zero_()
+    ci.coreinfer_paged_append(cache, torch.tensor([9, 3, 900, -4], dtype=torch.int32).cuda(), x, x)
+    length.copy_(torch.tensor([1 << 30, -5, 2 ** 31 - 1], dtype=torch.int32))
+    ci.coreinfer_paged_append(cache, start, x, x)
+    torch.cuda.synchronize()
+    assert ((k == 0) | (k == 1)).all() and ((v == 0) | (v == 1)).all()
+
+
+# ----------------------------------------------------------------------------- attention --
+
+def attend(b, q, scale, window=0, sinks=0, out=None, stream=None):
+    out = torch.full(q.shape, 77.0, dtype=q.dtype, device="cuda") if out is None else out
+    n = ci.coreinfer_paged_attention_workspace_bytes(b.handle(), q.shape[1], q.shape[0])
+    ws = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")
+    ci.coreinfer_paged_attention(b.handle(), b.start, q, scale, out, ws, window, sinks, stream=stream)
+    return out
+
+
+def check_attention(b, q, out, scale, window=0, sinks=0):
+    want, tol = attention(b, q, scale, window, sinks)
+    rows = slice(b.starts[0], b.starts[-1])
+    check(out[rows], want[rows], tol[rows])
+    assert (out[:b.starts[0]] == 77).all() and (out[b.starts[-1]:] == 77).all()
+
+
+ATTN = [
+    # new, length, H, share, D, page, dtype, order, window, sinks
+    ([1], [1], 1, 1, 64, 16, "heads", 0, 0), ([1], [77], 12, 1, 64, 16, "tokens", 0, 0), ([2, 1], [2, 300], 2, 4, 128, 16, "heads", 0, 0),
+    ([1, 0, 3], [1000, 40, 129], 2, 5, 128, 32, "heads", 0, 0), ([7], [513], 1, 7, 64, 128, "tokens", 100, 4), ([1] * 5, [64, 65, 1, 500, 128], 4, 2, 256, 64, "heads", 0, 0),
+    ([16], [16], 2, 1, 128, 16, "heads", 0, 0), ([130], [130], 1, 2, 64, 16, "heads", 0, 0), ([65, 1], [400, 333], 2, 3, 128, 64, "tokens", 64, 3),
+    ([300, 20], [300, 290], 2, 1, 256, 256, "heads", 33, 40), ([1], [4000], 2, 8, 128, 64, "heads", 1, 0), ([257], [1025], 1, 4, 128, 128, "heads", 0, 0),
+    ([1] * 40, [5 * i + 1 for i in range(40)], 2, 1, 64, 16, "tokens", 0, 0), ([3, 500, 1], [2000, 600, 700], 3, 2, 64, 16, "tokens", 256, 130),
+    ([9], [9], 1, 71, 64, 16, "heads", 0, 0), ([384], [384], 2, 1, 128, 128, "heads", 0, 0), ([1], [20000], 1, 1, 128, 16, "heads", 0, 0),
+    ([100], [5000], 1, 2, 128, 16, "tokens", 1000, 500), ([33], [4100], 1, 3, 256, 32, "tokens", 0, 0),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("new,length,H,share,D,page,order,window,sinks", ATTN)
+def test_attention(new, length, H, share, D, page, order, window, sinks, dtype):
+    """Ragged batches in every form, all that no token holds NaN, rows of nobody left as they were, two calls the same bits."""
+    require_gpu()
+    b = Batch(new, length, H, share, D, page, dtype, order, seed=sum(length) + share, front=1, pad=2, spread=1.5, wide=8 if order == "heads" and D == 128 else 0)
+    q = b.rand(H * share, extra=16)
+    scale = D ** -0.5
+    out = attend(b, q, scale, window, sinks)
+    check_attention(b, q, out, scale, window, sinks)
+    assert torch.equal(out, attend(b, q, scale, window, sinks))
