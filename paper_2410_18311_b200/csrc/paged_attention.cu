@@ -226,9 +226,21 @@ static coreinfer_status launch_simple(PagedAttnArgs& a, const DeviceInfo& di, cu
     coreinfer_status s = allow_smem<paged_simple_kernel<T, D>>(di);
     if (s != COREINFER_OK) return s;
     CI_CUDA(launch_overlapped(paged_simple_kernel<T, D>, dim3(a.n_ctas), dim3(kSimpleThreads), smem, st, a));
+    return COREINFER_OK;
+}
+
+template <typename T, int D>
+static coreinfer_status launch_join(const PagedAttnArgs& a, cudaStream_t st)
+{
     constexpr int ROWS = kJoinThreads / (D / 4);
     CI_CUDA(launch_overlapped(paged_join_kernel<T, D>, dim3(a.n_ctas, (a.RU + ROWS - 1) / ROWS), dim3(kJoinThreads), 0, st, a));
     return COREINFER_OK;
+}
+template <typename T>
+static coreinfer_status pick_join(const PagedAttnArgs& a, cudaStream_t st)
+{
+    if (a.c.D == 64) return launch_join<T, 64>(a, st);
+    return a.c.D == 128 ? launch_join<T, 128>(a, st) : launch_join<T, 256>(a, st);
 }
 
 template <typename T>
@@ -239,15 +251,25 @@ static coreinfer_status pick_simple(PagedAttnArgs& a, const DeviceInfo& di, cuda
 }
 
 static size_t round16(size_t n) { return (n + 15) / 16 * 16; }
-// Rows of a unit and CTAs, of whichever form the call takes.
-static void paged_shape(coreinfer_dtype, int, int* ru, int* ctas)
+
+// Which form a call takes, by what the host knows: rows of a unit, positions of a tile, CTAs.
+struct PagedForm {
+    bool chunk;
+    int RU, KT, ctas;
+};
+static PagedForm paged_form(coreinfer_dtype dtype, int D, int B, int share, int tokens)
 {
-    *ru = kSimpleRows;
-    *ctas = 148 * 2;
+    PagedForm f;
+    f.chunk = dtype != COREINFER_F32 && D <= 128 && (long long)tokens * share > 16LL * B;
+    f.RU = f.chunk ? kPagedChunkRows : kSimpleRows;
+    f.KT = f.chunk ? kPagedChunkTile : kSimpleTile;
+    f.ctas = f.chunk ? kPagedChunkCtas : 2 * 148;
+    return f;
 }
-static size_t paged_workspace(int ru, int ctas, int D)
+// A status word (16 bytes), the pieces, their exponents and sums, their outputs.
+static size_t paged_workspace(const PagedForm& f, int D)
 {
-    return round16(ctas * sizeof(PagedPiece)) + round16((size_t)ctas * 2 * ru * sizeof(float2)) + (size_t)ctas * 2 * ru * D * sizeof(float);
+    return 16 + round16(f.ctas * sizeof(PagedPiece)) + round16((size_t)f.ctas * 2 * f.RU * sizeof(float2)) + (size_t)f.ctas * 2 * f.RU * D * sizeof(float);
 }
 
 }  // namespace coreinfer
@@ -260,9 +282,10 @@ size_t coreinfer_paged_attention_workspace_bytes(const coreinfer_paged_cache* ca
 {
     Paged c;
     if (paged_take(cache, &c) != COREINFER_OK || q_heads < 1 || q_heads % c.H != 0 || tokens < 1) return 0;
-    int ru, ctas;
-    paged_shape(cache->dtype, c.D, &ru, &ctas);
-    return paged_workspace(ru, ctas, c.D);
+    // fewer tokens may take the other form: the larger of the two
+    const size_t a = paged_workspace(paged_form(cache->dtype, c.D, c.B, q_heads / c.H, tokens), c.D);
+    const size_t b = paged_workspace(paged_form(cache->dtype, c.D, c.B, q_heads / c.H, 1), c.D);
+    return a > b ? a : b;
 }
 
 coreinfer_status coreinfer_paged_attention(const coreinfer_paged_cache* cache, const int32_t* start, int32_t tokens,
@@ -286,9 +309,9 @@ coreinfer_status coreinfer_paged_attention(const coreinfer_paged_cache* cache, c
     if (window > 1 << 30 || sinks > 1 << 30) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "window and sinks: at most 2^30");
     if (!isfinite(scale)) CI_FAIL(COREINFER_ERR_INVALID_ARG, "scale must be finite");
     if (!workspace || !aligned16(workspace)) CI_FAIL(COREINFER_ERR_WORKSPACE, "workspace is NULL or misaligned");
-    int ru, ctas;
-    paged_shape(dtype, a.c.D, &ru, &ctas);
-    const size_t need = paged_workspace(ru, ctas, a.c.D);
+    a.share = q_heads / a.c.H;
+    const PagedForm f = paged_form(dtype, a.c.D, a.c.B, a.share, tokens);
+    const size_t need = paged_workspace(f, a.c.D);
     if (workspace_bytes < need) CI_FAIL(COREINFER_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
     DeviceInfo di;
     if ((s = device_info(&di)) != COREINFER_OK) return s;
@@ -298,24 +321,27 @@ coreinfer_status coreinfer_paged_attention(const coreinfer_paged_cache* cache, c
     a.out = (uint8_t*)out;
     a.ld_q = ld_q;
     a.ld_out = ld_out;
-    a.share = q_heads / a.c.H;
     a.window = window;
     a.sinks = window ? sinks : 0;
     a.scale2 = scale * kLog2e;
-    a.RU = ru;
-    a.KT = kSimpleTile;
+    a.RU = f.RU;
+    a.KT = f.KT;
     a.cost = 1;
-    a.n_ctas = ctas;
-    uint8_t* ws = (uint8_t*)workspace;
+    a.n_ctas = f.ctas;
+    unsigned* status = (unsigned*)workspace;
+    uint8_t* ws = (uint8_t*)workspace + 16;
     a.pieces = (PagedPiece*)ws;
-    ws += round16(ctas * sizeof(PagedPiece));
+    ws += round16(f.ctas * sizeof(PagedPiece));
     a.part_ml = (float2*)ws;
-    ws += round16((size_t)ctas * 2 * ru * sizeof(float2));
+    ws += round16((size_t)f.ctas * 2 * f.RU * sizeof(float2));
     a.part_o = (float*)ws;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (dtype == COREINFER_F32) return pick_simple<float>(a, di, st);
-    if (dtype == COREINFER_BF16) return pick_simple<__nv_bfloat16>(a, di, st);
-    return pick_simple<__half>(a, di, st);
+    if (f.chunk) {
+        if ((s = paged_chunk(a, dtype == COREINFER_F16, status, di, st)) != COREINFER_OK) return s;
+    } else if ((s = dtype == COREINFER_F32 ? pick_simple<float>(a, di, st)
+                    : (dtype == COREINFER_BF16 ? pick_simple<__nv_bfloat16>(a, di, st) : pick_simple<__half>(a, di, st))) != COREINFER_OK) return s;
+    if (dtype == COREINFER_F32) return pick_join<float>(a, st);
+    return dtype == COREINFER_BF16 ? pick_join<__nv_bfloat16>(a, st) : pick_join<__half>(a, st);
 }
 
 }  // extern "C"

@@ -13,7 +13,6 @@
 namespace coreinfer {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kPagedMaxCtas = 640;
 
 // Which CTAs work on a unit that is cut; written by the CTA that has its first tile, read by the joining kernel.
 struct PagedPiece {
@@ -35,6 +34,12 @@ struct PagedAttnArgs {
     float2* part_ml;        // [n_ctas][2][RU]: reference exponent (base 2) and sum
     float* part_o;          // [n_ctas][2][RU][D]
 };
+
+// The tensor-core form (paged_attention_tc.cu): 16-bit caches of head_dim 64 and 128.
+constexpr int kPagedChunkRows = 256;
+constexpr int kPagedChunkTile = 128;
+constexpr int kPagedChunkCtas = 148;
+coreinfer_status paged_chunk(PagedAttnArgs& a, bool f16, unsigned* status, const DeviceInfo& di, cudaStream_t st);
 
 #ifdef __CUDACC__
 

@@ -1,0 +1,606 @@
+// Attention of chunks over a paged cache on the tensor cores: 16-bit caches, many query rows per key head.
+//
+// What bounds it: both products and the exponentials alike.  Per SM a tile of 128 rows x 128 positions x head_dim 128 takes 1024 cycles
+// of tcgen05.mma and, at 16 exponentials a cycle, 1024 cycles of those; so two row tiles run against each other: while one is in its
+// softmax the other is in its products.
+//
+// One persistent CTA per SM; a unit is 256 query rows of one sequence and key head, as two tiles A and B of 128 that share every
+// tile of 128 positions.
+//   warp 8      brings key and value tiles into a ring by tensor copies, a page (or 128 slots of it) a box; pages that are none
+//               lie outside the map and are filled with zeros
+//   warp 9      issues  S = Q K^T  into tensor memory, and  O += P V  with P from tensor memory, in the order
+//               PV_A(i) S_A(i+1) PV_B(i) S_B(i+1)
+//   warps 0..3  softmax of A, a thread a row: S from tensor memory, P back over it in 16 bits, running maximum and sum in registers;
+//   warps 4..7  the same for B; both write their rows out at the end of a unit
+//   warps 10,11 bring the next unit's queries, and look through value tiles in which some row does not see some position
+// The running maximum is moved, and O rescaled, only when a row exceeds it by 2^8 (a factor that cancels in O / l): P then stays below
+// 2^8, and in fp16 it is raised by 2^7 so that weights keep 11 bits down to 2^-21 of the largest.  P is rounded to the cache's type
+// for the product, as tcgen05.mma takes both operands in one type: an error of half a step of each weight, which averages out to
+// about the rounding of the output; the sum l is of the weights before that.
+// A weight of 0 times a value that is not finite would be NaN, and positions that a row does not see, or that hold no token, may
+// hold anything: in tiles where that can happen warps 10 and 11 set what is not finite to 0, and at the unit's end the rows that do see such
+// a value get it added.
+// Every wait is bounded: one that gives up sets the status word, and all roles leave their loops.
+#include "paged_attention.cuh"
+#include "tc.cuh"
+
+#include <type_traits>
+
+namespace coreinfer {
+
+constexpr int kChunkThreads = 384;
+constexpr int kChunkKT = kPagedChunkTile;
+constexpr int kChunkMaxStages = 8;
+constexpr long long kChunkWaitCycles = 3000000000LL;
+constexpr float kNoMax = -INFINITY;
+
+struct ChunkArgs {
+    PagedAttnArgs a;
+    int stages;
+    int box;                // slots of a tensor copy
+    int negative;           // scale below 0: the queries' signs are turned
+    unsigned* status;
+};
+
+struct ChunkBars {
+    uint64_t full[kChunkMaxStages], empty[kChunkMaxStages], looked[kChunkMaxStages];
+    uint64_t s_full[2], p_full[2], o_full[2], q_full, q_empty;
+    uint32_t tmem;
+    int abort;
+    int found[4];           // by unit modulo 4: number + 1 of a unit in which values were set to 0
+};
+
+// What the rows of one of the two tiles see.
+struct ChunkView {
+    bool any;
+    int lo_min, lo_max, hi_min, hi_max;
+};
+__device__ __forceinline__ ChunkView chunk_view(const PagedAttnArgs& a, const PagedWalk& w, int rows, int x)
+{
+    ChunkView v;
+    v.any = rows > x * 128;
+    if (!v.any) return v;
+    const int r0 = w.tile * a.RU + x * 128, r1 = w.tile * a.RU + (rows < x * 128 + 128 ? rows : x * 128 + 128) - 1;
+    const PagedRow low = paged_row(a, w.s, r0), high = paged_row(a, w.s, r1);
+    v.lo_min = low.lo;
+    v.lo_max = high.lo;
+    v.hi_min = low.hi;
+    v.hi_max = high.hi;
+    return v;
+}
+// Some row sees some position of the tile from j on.
+__device__ __forceinline__ bool chunk_needs(const PagedAttnArgs& a, const ChunkView& v, int j)
+{
+    return v.any && j < v.hi_max && (j + kChunkKT > v.lo_min || j < a.sinks);
+}
+// Every row sees all of it.
+__device__ __forceinline__ bool chunk_whole(const PagedAttnArgs& a, const ChunkView& v, int j)
+{
+    return j + kChunkKT <= v.hi_min && (j >= v.lo_max || j + kChunkKT <= a.sinks);
+}
+// Some row of a tile that takes part does not: the values are looked through.
+__device__ __forceinline__ bool chunk_look(const PagedAttnArgs& a, const ChunkView& va, const ChunkView& vb, int j)
+{
+    return (chunk_needs(a, va, j) && !chunk_whole(a, va, j)) || (chunk_needs(a, vb, j) && !chunk_whole(a, vb, j));
+}
+
+__device__ __forceinline__ bool chunk_wait(uint64_t& bar, uint32_t parity, ChunkBars* s, unsigned* status)
+{
+    const uint32_t b = smem_u32(&bar);
+    if (mbar_try_wait(b, parity)) return true;
+    const long long t0 = clock64();
+    volatile int* abort_flag = &s->abort;
+    for (;;) {
+        if (mbar_try_wait_parked(b, parity, 2000u)) return true;
+        if (*abort_flag) return false;
+        if (clock64() - t0 > kChunkWaitCycles) {
+            *abort_flag = 1;
+            atomicMax(status, (unsigned)kStatusTimeout);
+            return false;
+        }
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi)
+{
+    uint32_t r;
+    if constexpr (sizeof(T) == 2 && std::is_same<T, __half>::value) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// Whether one of the two 16-bit values is an infinity or NaN.
+template <typename T>
+__device__ __forceinline__ bool odd_pair(uint32_t w)
+{
+    constexpr uint32_t E = std::is_same<T, __half>::value ? 0x7c00u : 0x7f80u;
+    return (w & E) == E || (w & (E << 16)) == (E << 16);
+}
+template <typename T>
+__device__ __forceinline__ uint32_t without_odd(uint32_t w)
+{
+    constexpr uint32_t E = std::is_same<T, __half>::value ? 0x7c00u : 0x7f80u;
+    if ((w & E) == E) w &= 0xffff0000u;
+    if ((w & (E << 16)) == (E << 16)) w &= 0xffffu;
+    return w;
+}
+
+// Adds to 32 outputs of a row the infinities and NaN that it sees in tiles that were looked through.
+template <typename T, int D>
+__device__ __noinline__ void chunk_restore(const PagedAttnArgs& a, const PagedWalk& w, const ChunkView& va, const ChunkView& vb, int from, int to, int row, int d0, float* o)
+{
+    const PagedRow see = paged_row(a, w.s, row);
+    for (int i = from; i < to; ++i) {
+        const int j0 = paged_tile_at(w.t, i) * kChunkKT;
+        if (!chunk_look(a, va, vb, j0)) continue;
+        for (int j = j0; j < j0 + kChunkKT; ++j) {
+            if (!paged_sees(a, see, j)) continue;
+            const int page = paged_page(a.c, w.b, j);
+            if (page < 0) continue;
+            const T* v = reinterpret_cast<const T*>(a.c.pool[1]) + paged_offset(a.c, page, w.h, j) + d0;
+            for (int e = 0; e < 32; ++e) {
+                const float x = to_f32(v[e]);
+                if (!isfinite(x)) o[e] += x;
+            }
+        }
+    }
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                                                                        const __grid_constant__ ChunkArgs g)
+{
+    constexpr int KT = kChunkKT;
+    constexpr int BLOCKS = D / 64;
+    constexpr uint32_t BLOCK = 128 * 128;            // bytes of 128 rows of 64 values
+    constexpr uint32_t TILE = BLOCKS * BLOCK;
+    constexpr uint32_t TYPE = std::is_same<T, __half>::value ? 0u : 1u;
+    constexpr uint32_t IDESC_S = tc::idesc(TYPE, false, 128, KT);
+    constexpr uint32_t IDESC_O = tc::idesc(TYPE, true, 128, D);
+    constexpr float LIFT = std::is_same<T, __half>::value ? 7.f : 0.f;
+    const PagedAttnArgs& a = g.a;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    uint8_t* qs = smem;                              // [2][BLOCKS][128 rows][128 bytes]
+    uint8_t* ring = smem + 2 * TILE;                 // [stages][BLOCKS][128 positions][128 bytes]
+    ChunkBars* s = reinterpret_cast<ChunkBars*>(ring + (size_t)g.stages * TILE);
+    long long* at = reinterpret_cast<long long*>(s + 1);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    if (tid == 0) {
+        for (int i = 0; i < g.stages; ++i) {
+            mbar_init(smem_u32(&s->full[i]), 1);
+            mbar_init(smem_u32(&s->empty[i]), 1);
+            mbar_init(smem_u32(&s->looked[i]), 2);
+        }
+        for (int x = 0; x < 2; ++x) {
+            mbar_init(smem_u32(&s->s_full[x]), 1);
+            mbar_init(smem_u32(&s->p_full[x]), 4);
+            mbar_init(smem_u32(&s->o_full[x]), 1);
+        }
+        mbar_init(smem_u32(&s->q_full), 2);
+        mbar_init(smem_u32(&s->q_empty), 1);
+        s->abort = 0;
+        for (int i = 0; i < 4; ++i) s->found[i] = 0;
+        mbar_fence_init();
+    }
+    if (warp == 9) tc::alloc(smem_u32(&s->tmem), 512);
+    tc::fence_before();
+    __syncthreads();
+    tc::fence_after();
+    const uint32_t tmem = s->tmem;
+    wait_for_stream();
+    if (blockIdx.x == 0 && tid == 0) *g.status = kStatusOk;
+    const long long total = paged_plan(a, at);
+    if (tid == 0) a.pieces[blockIdx.x].last = -1;
+
+    if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        if (warp == 8) {
+            // ------------------------------------------------------- tiles --
+            int stage = 0;
+            uint32_t ph = 0;
+            bool ok = true;
+            const int boxes = KT / g.box;
+            PagedWalk w;
+            for (w.begin(a, at, total, blockIdx.x); ok && w.more(); w.next(a, at)) {
+                const int from = w.from(a), to = w.to(a);
+                for (int i = from; ok && i < to; ++i) {
+                    const int j = paged_tile_at(w.t, i) * KT + lane * g.box;
+                    int page = lane < boxes ? paged_page(a.c, w.b, j) : 0;
+                    if (page < 0) page = a.c.n_pages;            // outside the map: zeros
+                    const int slot = j & ((1 << a.c.page_shift) - 1);
+                    for (int kv = 0; kv < 2; ++kv) {
+                        if (!(ok = chunk_wait(s->empty[stage], ph ^ 1u, s, g.status))) break;
+                        const uint32_t bar = smem_u32(&s->full[stage]);
+                        if (lane == 0) mbar_arrive_expect_tx(bar, TILE);
+                        __syncwarp();
+                        if (lane < boxes) {
+                            const uint32_t dst = smem_u32(ring + (size_t)stage * TILE) + lane * g.box * 128;
+#pragma unroll
+                            for (int d = 0; d < BLOCKS; ++d) tc::copy_4d(dst + d * BLOCK, kv ? &map_v : &map_k, d * 64, slot, w.h, page, bar);
+                        }
+                        if (++stage == g.stages) { stage = 0; ph ^= 1u; }
+                    }
+                }
+            }
+        } else if (warp == 9) {
+            // ---------------------------------------------------- products --
+            if (lane == 0) {
+                int stage = 0;                                   // of K(i)
+                uint32_t ph = 0, looked = 0, p_ph[2] = {0, 0}, q_ph = 0;
+                bool ok = true;
+                auto advance = [&](int& st, uint32_t& p) { if (++st == g.stages) { st = 0; p ^= 1u; } };
+                auto scores = [&](int x, int st) {
+                    const uint64_t q = tc::desc_k(smem_u32(qs + x * TILE)), k = tc::desc_k(smem_u32(ring + (size_t)st * TILE));
+#pragma unroll
+                    for (int d = 0; d < D / 16; ++d) {
+                        const uint64_t ofs = (d / 4) * (BLOCK >> 4) + (d % 4) * 2;
+                        tc::mma_ss(tmem + x * 128, q + ofs, k + ofs, IDESC_S, d > 0);
+                    }
+                    tc::commit(smem_u32(&s->s_full[x]));
+                };
+                PagedWalk w;
+                for (w.begin(a, at, total, blockIdx.x); ok && w.more(); w.next(a, at)) {
+                    const int from = w.from(a), to = w.to(a);
+                    if (from >= to) continue;
+                    const int rows = paged_unit_rows(a, w);
+                    const ChunkView v[2] = {chunk_view(a, w, rows, 0), chunk_view(a, w, rows, 1)};
+                    bool begun[2] = {false, false};
+                    if (!(ok = chunk_wait(s->q_full, q_ph, s, g.status))) break;
+                    q_ph ^= 1u;
+                    tc::fence_after();
+                    int j = paged_tile_at(w.t, from) * KT;
+                    if (!(ok = chunk_wait(s->full[stage], ph, s, g.status))) break;
+                    tc::fence_after();
+                    for (int x = 0; x < 2; ++x)
+                        if (chunk_needs(a, v[x], j)) scores(x, stage);
+                    tc::commit(smem_u32(&s->empty[stage]));
+                    if (from + 1 == to) tc::commit(smem_u32(&s->q_empty));
+                    advance(stage, ph);
+                    for (int i = from; i < to; ++i) {
+                        // stage: V(i); the one behind it: K(i + 1)
+                        const int vs = stage;
+                        const uint32_t vph = ph;
+                        advance(stage, ph);
+                        const int ks = stage;
+                        const uint32_t kph = ph;
+                        const bool last = i + 1 == to;
+                        const int j_next = last ? 0 : paged_tile_at(w.t, i + 1) * KT;
+                        if (!(ok = chunk_wait(s->full[vs], vph, s, g.status))) break;
+                        if (!(ok = chunk_wait(s->looked[vs], looked >> vs & 1u, s, g.status))) break;
+                        looked ^= 1u << vs;
+                        bool have_k = false;
+                        for (int x = 0; x < 2; ++x) {
+                            if (chunk_needs(a, v[x], j)) {
+                                if (!(ok = chunk_wait(s->p_full[x], p_ph[x], s, g.status))) break;
+                                p_ph[x] ^= 1u;
+                                tc::fence_after();
+                                const uint64_t val = tc::desc_mn(smem_u32(ring + (size_t)vs * TILE), BLOCK);
+#pragma unroll
+                                for (int k = 0; k < KT / 16; ++k)
+                                    tc::mma_ts(tmem + 256 + x * 128, tmem + x * 128 + k * 8, val + k * (16 * 128 >> 4), IDESC_O, begun[x] || k > 0);
+                                begun[x] = true;
+                            }
+                            if (!last && chunk_needs(a, v[x], j_next)) {
+                                if (!have_k && !(ok = chunk_wait(s->full[ks], kph, s, g.status))) break;
+                                have_k = true;
+                                tc::fence_after();
+                                scores(x, ks);
+                            }
+                        }
+                        if (!ok) break;
+                        tc::commit(smem_u32(&s->empty[vs]));
+                        if (!last) {
+                            if (!have_k && !(ok = chunk_wait(s->full[ks], kph, s, g.status))) break;
+                            tc::commit(smem_u32(&s->empty[ks]));
+                            if (i + 2 == to) tc::commit(smem_u32(&s->q_empty));
+                            advance(stage, ph);
+                        }
+                        j = j_next;
+                    }
+                    for (int x = 0; x < 2; ++x)
+                        if (begun[x]) tc::commit(smem_u32(&s->o_full[x]));
+                }
+            }
+        } else {
+            // ------------------------------------- queries, looks at values --
+            const int t = tid - 320;
+            int stage = 0, unit = 0;
+            uint32_t ph = 0, q_ph = 0;
+            bool ok = true;
+            PagedWalk w;
+            for (w.begin(a, at, total, blockIdx.x); ok && w.more(); w.next(a, at)) {
+                const int from = w.from(a), to = w.to(a);
+                if (from >= to) continue;
+                const int rows = paged_unit_rows(a, w);
+                const ChunkView va = chunk_view(a, w, rows, 0), vb = chunk_view(a, w, rows, 1);
+                if (!(ok = chunk_wait(s->q_empty, q_ph ^ 1u, s, g.status))) break;
+                q_ph ^= 1u;
+                constexpr int CPR = D / 8;                       // 16-byte pieces of a row
+                const int padded = (rows + 127) / 128 * 128;
+                const int r_first = w.tile * a.RU;
+                for (int i = t; i < padded * CPR; i += 64) {
+                    const int r = i / CPR, c = i % CPR;
+                    const uint32_t dst = smem_u32(qs) + (r >> 7) * TILE + (c >> 3) * BLOCK + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4);
+                    const uint8_t* src = a.q + (paged_row_offset(a, w.s, w.h, r_first + (r < rows ? r : 0), a.ld_q) + c * 8) * 2;
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(r < rows ? 16 : 0) : "memory");
+                }
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                if (g.negative) {
+                    __syncwarp();                                // each lane turns what it has brought itself
+                    for (int i = t; i < padded * CPR; i += 64) {
+                        const int r = i / CPR, c = i % CPR;
+                        uint4* p = reinterpret_cast<uint4*>(qs + (r >> 7) * TILE + (c >> 3) * BLOCK + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4));
+                        uint4 x = *p;
+                        x.x ^= 0x80008000u; x.y ^= 0x80008000u; x.z ^= 0x80008000u; x.w ^= 0x80008000u;
+                        *p = x;
+                    }
+                }
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&s->q_full));
+                for (int i = from; i < to; ++i) {
+                    const int j = paged_tile_at(w.t, i) * KT;
+                    if (++stage == g.stages) { stage = 0; ph ^= 1u; }
+                    // each tile is waited for, so that neither the ring nor this warp is ever a round ahead of the other
+                    if (!(ok = chunk_wait(s->full[stage], ph, s, g.status))) break;
+                    if (chunk_look(a, va, vb, j)) {
+                        uint4* p = reinterpret_cast<uint4*>(ring + (size_t)stage * TILE);
+                        bool odd = false;
+#pragma unroll 4
+                        for (int c = t; c < (int)(TILE / 16); c += 64) {
+                            uint4 x = p[c];
+                            if (odd_pair<T>(x.x) || odd_pair<T>(x.y) || odd_pair<T>(x.z) || odd_pair<T>(x.w)) {
+                                x.x = without_odd<T>(x.x); x.y = without_odd<T>(x.y); x.z = without_odd<T>(x.z); x.w = without_odd<T>(x.w);
+                                p[c] = x;
+                                odd = true;
+                            }
+                        }
+                        if (odd) {
+                            *(volatile int*)&s->found[unit & 3] = unit + 1;
+                            fence_proxy_async();
+                        }
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&s->looked[stage]));
+                    if (++stage == g.stages) { stage = 0; ph ^= 1u; }
+                }
+                ++unit;
+            }
+        }
+    } else {
+        // -------------------------------------------------------- softmax --
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        const int x = warp >> 2;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t t_s = tmem + lanes + x * 128, t_o = tmem + lanes + 256 + x * 128;
+        const int r = (warp & 3) * 32 + lane;                    // row of the tile
+        const float scale2 = fmaxf(fabsf(a.scale2), 1e-30f);      // a scale of 0 times -infinity would be NaN
+        uint32_t s_ph = 0, o_ph = 0;
+        int unit = 0;
+        bool ok = true;
+        PagedWalk w;
+        for (w.begin(a, at, total, blockIdx.x); ok && w.more(); w.next(a, at)) {
+            const int from = w.from(a), to = w.to(a);
+            if (w.t.count > 0 && from >= to) continue;
+            const int rows = paged_unit_rows(a, w);
+            const ChunkView v = chunk_view(a, w, rows, x);
+            const int row = w.tile * a.RU + x * 128 + r;
+            const PagedRow see = paged_row(a, w.s, row);
+            float m = kNoMax, l = 0.f;                           // m: the exponent that weights are relative to, LIFT below the maximum it was taken from
+            bool begun = false;
+            for (int i = from; i < to; ++i) {
+                const int j = paged_tile_at(w.t, i) * KT;
+                if (!chunk_needs(a, v, j)) continue;
+                if (!(ok = chunk_wait(s->s_full[x], s_ph, s, g.status))) break;
+                s_ph ^= 1u;
+                tc::fence_after();
+                uint32_t raw[KT];
+#pragma unroll
+                for (int c = 0; c < KT / 32; ++c) tc::ld32(t_s + c * 32, raw + c * 32);
+                tc::wait_ld();
+                float (&f)[KT] = reinterpret_cast<float (&)[KT]>(raw);
+                if (!chunk_whole(a, v, j)) {
+#pragma unroll
+                    for (int c = 0; c < KT; ++c)
+                        if (!paged_sees(a, see, j + c)) f[c] = kNoMax;
+                }
+                float top[4] = {f[0], f[1], f[2], f[3]};
+#pragma unroll
+                for (int c = 4; c < KT; ++c) top[c & 3] = fmaxf(top[c & 3], f[c]);
+                const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * scale2;
+                const bool first = m == kNoMax;
+                const bool move = now > m + 8.f + LIFT;          // also when there is no m yet
+                if (__any_sync(0xffffffffu, move)) {
+                    const float before = m;
+                    if (move) m = now - LIFT;
+                    if (begun && __any_sync(0xffffffffu, move && !first)) {
+                        const float by = move && !first ? exp2_fast(before - m) : 1.f;
+                        l *= by;
+#pragma unroll
+                        for (int c = 0; c < D / 32; ++c) {
+                            uint32_t o[32];
+                            tc::ld32(t_o + c * 32, o);
+                            tc::wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
+                            tc::st32(t_o + c * 32, o);
+                        }
+                    }
+                }
+                begun = true;
+                const float ref = m == kNoMax ? 0.f : m;
+                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < KT / 32; ++c) {
+                    uint32_t p[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float p0 = exp2_fast(fmaf(f[c * 32 + 2 * e], scale2, -ref)), p1 = exp2_fast(fmaf(f[c * 32 + 2 * e + 1], scale2, -ref));
+                        sum[e & 1] += p0;
+                        sum[2 + (e & 1)] += p1;
+                        p[e] = pack2<T>(p0, p1);
+                    }
+                    tc::st16(t_s + c * 16, p);
+                }
+                tc::wait_st();
+                tc::fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&s->p_full[x]));
+                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            }
+            if (!ok) break;
+            if (begun) {
+                if (!(ok = chunk_wait(s->o_full[x], o_ph, s, g.status))) break;
+                o_ph ^= 1u;
+                tc::fence_after();
+            }
+            const bool head = from == 0, tail = to == w.t.count;
+            const bool mine = x * 128 + r < rows;
+            const bool restore = begun && *(volatile int*)&s->found[unit & 3] == unit + 1;
+            const size_t slot = (size_t)blockIdx.x * 2 + (head ? 1 : 0);
+            const float inv = see.hi > 0 ? 1.f / l : 0.f;
+            T* to_out = reinterpret_cast<T*>(a.out) + (mine ? paged_row_offset(a, w.s, w.h, row, a.ld_out) : 0);
+            float* to_part = a.part_o + (slot * a.RU + x * 128 + r) * D;
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+                uint32_t o[32];
+                if (begun) {
+                    tc::ld32(t_o + c * 32, o);
+                    tc::wait_ld();
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = 0u;
+                }
+                if (restore && mine) {
+                    float more[32];
+                    for (int e = 0; e < 32; ++e) more[e] = __uint_as_float(o[e]);
+                    chunk_restore<T, D>(a, w, chunk_view(a, w, rows, 0), chunk_view(a, w, rows, 1), from, to, row, c * 32, more);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(more[e]);
+                }
+                if (!mine) continue;
+                if (head && tail) {
+                    uint32_t p[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        p[e] = see.hi > 0 ? pack2<T>(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv) : 0u;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) reinterpret_cast<uint4*>(to_out + c * 32)[e] = make_uint4(p[4 * e], p[4 * e + 1], p[4 * e + 2], p[4 * e + 3]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) reinterpret_cast<uint4*>(to_part + c * 32)[e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                }
+            }
+            if (mine && !(head && tail)) a.part_ml[slot * a.RU + x * 128 + r] = make_float2(m, l);
+            if (head && !tail && tid == 0) {
+                PagedPiece p;
+                p.b = w.b;
+                p.h = w.h;
+                p.tile = w.tile;
+                p.last = paged_owner(total, w.base + a.cost + w.t.count - 1, w.n);
+                a.pieces[blockIdx.x] = p;
+            }
+            tc::fence_before();                                  // the reads of O come before the next unit's products
+            if (to > from) ++unit;
+        }
+    }
+
+    // Leaving: nothing may still be landing in this CTA's shared memory, and tensor memory goes back.
+    tc::fence_before();
+    __syncthreads();
+    if (s->abort) {
+        // after a wait that gave up copies may be in flight: a bounded time for them to land
+        const long long t0 = clock64();
+        while (clock64() - t0 < 20000000LL) __nanosleep(1000);
+        __syncthreads();
+    }
+    let_next_start();
+    if (warp == 9) {
+        tc::fence_after();
+        tc::dealloc(tmem, 512);
+    }
+}
+
+// cuTensorMapEncodeTiled, looked up through the runtime (the library links no libcuda symbol).
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+static coreinfer_status encode_fn(EncodeTiledFn* out)
+{
+    static std::atomic<EncodeTiledFn> cached{nullptr};
+    EncodeTiledFn f = cached.load(std::memory_order_acquire);
+    if (!f) {
+        void* fn = nullptr;
+        cudaDriverEntryPointQueryResult qres;
+        CI_CUDA(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres));
+        if (qres != cudaDriverEntryPointSuccess || !fn)
+            CI_FAIL(COREINFER_ERR_CUDA, "cuTensorMapEncodeTiled is not available from this driver");
+        f = (EncodeTiledFn)fn;
+        cached.store(f, std::memory_order_release);
+    }
+    *out = f;
+    return COREINFER_OK;
+}
+
+// A pool as [pages][heads][slots][head_dim], read in boxes of `box` slots x 64 values with the 128-byte swizzle.
+static coreinfer_status pool_map(CUtensorMap* map, const Paged& c, const void* pool, bool f16, int box)
+{
+    EncodeTiledFn enc;
+    coreinfer_status s = encode_fn(&enc);
+    if (s != COREINFER_OK) return s;
+    const long long page = 1LL << c.page_shift;
+    // the stride of an axis of one entry is never used, but has to be one that the map takes
+    const long long head_stride = c.H > 1 ? c.head_stride : c.token_stride, page_stride = c.n_pages > 1 ? c.page_stride : c.token_stride;
+    const cuuint64_t dims[4] = {(cuuint64_t)c.D, (cuuint64_t)page, (cuuint64_t)c.H, (cuuint64_t)c.n_pages};
+    const cuuint64_t strides[3] = {(cuuint64_t)c.token_stride * 2, (cuuint64_t)head_stride * 2, (cuuint64_t)page_stride * 2};
+    const cuuint32_t boxes[4] = {64, (cuuint32_t)box, 1, 1};
+    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    const CUresult r = enc(map, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(pool), dims, strides, boxes, estr,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) CI_FAIL(COREINFER_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
+    return COREINFER_OK;
+}
+
+template <typename T, int D>
+static coreinfer_status launch_chunk(ChunkArgs& g, const DeviceInfo& di, cudaStream_t st)
+{
+    CUtensorMap mk, mv;
+    const bool f16 = std::is_same<T, __half>::value;
+    const int page = 1 << g.a.c.page_shift;
+    g.box = page < kChunkKT ? page : kChunkKT;
+    coreinfer_status s = pool_map(&mk, g.a.c, g.a.c.pool[0], f16, g.box);
+    if (s != COREINFER_OK || (s = pool_map(&mv, g.a.c, g.a.c.pool[1], f16, g.box)) != COREINFER_OK) return s;
+    constexpr size_t TILE = D / 64 * 128 * 128;
+    const size_t fixed = 2 * TILE + sizeof(ChunkBars) + (size_t)(g.a.c.B + 1) * 8;
+    size_t stages = (smem_room(di, 0) - fixed) / TILE;
+    g.stages = (int)(stages < kChunkMaxStages ? stages : kChunkMaxStages);
+    const size_t smem = fixed + g.stages * TILE;
+    if ((s = allow_smem<paged_chunk_kernel<T, D>>(di, 0)) != COREINFER_OK) return s;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(g.a.n_ctas);
+    cfg.blockDim = dim3(kChunkThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    CI_CUDA(cudaLaunchKernelEx(&cfg, paged_chunk_kernel<T, D>, mk, mv, (const ChunkArgs)g));
+    return COREINFER_OK;
+}
+
+coreinfer_status paged_chunk(PagedAttnArgs& a, bool f16, unsigned* status, const DeviceInfo& di, cudaStream_t st)
+{
+    ChunkArgs g;
+    g.a = a;
+    g.negative = a.scale2 < 0.f;
+    g.status = status;
+    if (f16) return a.c.D == 64 ? launch_chunk<__half, 64>(g, di, st) : launch_chunk<__half, 128>(g, di, st);
+    return a.c.D == 64 ? launch_chunk<__nv_bfloat16, 64>(g, di, st) : launch_chunk<__nv_bfloat16, 128>(g, di, st);
+}
+
+}  // namespace coreinfer

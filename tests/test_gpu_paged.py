@@ -220,3 +220,24 @@ def test_attention(new, length, H, share, D, page, order, window, sinks, dtype):
     out = attend(b, q, scale, window, sinks)
     check_attention(b, q, out, scale, window, sinks)
     assert torch.equal(out, attend(b, q, scale, window, sinks))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_attention_many_units_per_block(dtype):
+    """Decoding sequences and long pieces of prompts in one call, more tiles than blocks: every block walks several units, most of
+    their tiles without a mask, and no wait gives up."""
+    require_gpu()
+    small = dtype == "f32"
+    new = [300 if small else 900, 1, 200 if small else 700, 1, 1]
+    b = Batch(new, [1500, 2000, 1000, 40, 1700], 4, 2, 64, 16, dtype, "tokens", seed=4, front=1, pad=2)
+    q = b.rand(8)
+    out = torch.full(q.shape, 77.0, dtype=q.dtype, device="cuda")
+    n = ci.coreinfer_paged_attention_workspace_bytes(b.handle(), 8, b.tokens)
+    ws = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")
+    for window, sinks in ((0, 0), (300, 4)):
+        for _ in range(3):
+            out.fill_(77.0)
+            ci.coreinfer_paged_attention(b.handle(), b.start, q, 0.125, out, ws, window, sinks)
+        if not small:
+            ci.coreinfer_workspace_status(ws)
+        check_attention(b, q, out, 0.125, window, sinks)
