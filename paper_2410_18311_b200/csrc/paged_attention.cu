@@ -155,6 +155,8 @@ __global__ void __launch_bounds__(kSimpleThreads) paged_simple_kernel(const __gr
         for (int r = 0; r < RPT; ++r) {
             const int row = rg + r;
             if (row >= rows) continue;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[r][e] = paged_mend<T>(a, w, from, to, r0 + row, c + e, o[r][e], ls[row]);
             if (head && tail) {
                 const PagedRow see = paged_row(a, w.s, r0 + row);
                 const float l = ls[row];
@@ -202,7 +204,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_c
 #pragma unroll 4
     for (int i = first; i <= p.last; ++i) {
         const float2 ml = a.part_ml[slot(i) * a.RU + row];
-        const float f = exp2f(ml.x - ref);
+        const float f = paged_join_factor(ml.x, ref);
         const float4 x = *reinterpret_cast<const float4*>(a.part_o + (slot(i) * a.RU + row) * D + c);
         l = fmaf(ml.y, f, l);
         // a piece in which the row sees nothing, or nothing but weights of 0, has nothing to add
@@ -252,19 +254,18 @@ static coreinfer_status pick_simple(PagedAttnArgs& a, const DeviceInfo& di, cuda
 
 static size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 
-// Which form a call takes, by what the host knows: rows of a unit, positions of a tile, CTAs.
+// Which form a call takes, by what the host knows (the lengths of the batch's pieces are on the device).
+enum PagedFormKind { kFormSimple, kFormFew, kFormChunk };
 struct PagedForm {
-    bool chunk;
-    int RU, KT, ctas;
+    PagedFormKind kind;
+    int RU, KT, ctas;           // rows of a unit, positions of a tile, CTAs
 };
 static PagedForm paged_form(coreinfer_dtype dtype, int D, int B, int share, int tokens)
 {
-    PagedForm f;
-    f.chunk = dtype != COREINFER_F32 && D <= 128 && (long long)tokens * share > 16LL * B;
-    f.RU = f.chunk ? kPagedChunkRows : kSimpleRows;
-    f.KT = f.chunk ? kPagedChunkTile : kSimpleTile;
-    f.ctas = f.chunk ? kPagedChunkCtas : 2 * 148;
-    return f;
+    if (dtype == COREINFER_F32) return {kFormSimple, kSimpleRows, kSimpleTile, 2 * 148};
+    if (D <= 128 && (long long)tokens * share > 16LL * B) return {kFormChunk, kPagedChunkRows, kPagedChunkTile, kPagedChunkCtas};
+    const PagedFewShape few = paged_few_shape(D, (int)((long long)tokens * share / B > 8 ? 16 : (tokens <= B ? share : 16)));
+    return {kFormFew, few.RU, few.KT, few.ctas};
 }
 // A status word (16 bytes), the pieces, their exponents and sums, their outputs.
 static size_t paged_workspace(const PagedForm& f, int D)
@@ -336,10 +337,9 @@ coreinfer_status coreinfer_paged_attention(const coreinfer_paged_cache* cache, c
     ws += round16((size_t)f.ctas * 2 * f.RU * sizeof(float2));
     a.part_o = (float*)ws;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (f.chunk) {
-        if ((s = paged_chunk(a, dtype == COREINFER_F16, status, di, st)) != COREINFER_OK) return s;
-    } else if ((s = dtype == COREINFER_F32 ? pick_simple<float>(a, di, st)
-                    : (dtype == COREINFER_BF16 ? pick_simple<__nv_bfloat16>(a, di, st) : pick_simple<__half>(a, di, st))) != COREINFER_OK) return s;
+    if (f.kind == kFormChunk) s = paged_chunk(a, dtype == COREINFER_F16, status, di, st);
+    else s = f.kind == kFormFew ? paged_few(a, dtype == COREINFER_F16, di, st) : pick_simple<float>(a, di, st);
+    if (s != COREINFER_OK) return s;
     if (dtype == COREINFER_F32) return pick_join<float>(a, st);
     return dtype == COREINFER_BF16 ? pick_join<__nv_bfloat16>(a, st) : pick_join<__half>(a, st);
 }

@@ -10,6 +10,8 @@
 
 #include "paged.cuh"
 
+#include <type_traits>
+
 namespace coreinfer {
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -40,6 +42,13 @@ constexpr int kPagedChunkRows = 256;
 constexpr int kPagedChunkTile = 128;
 constexpr int kPagedChunkCtas = 148;
 coreinfer_status paged_chunk(PagedAttnArgs& a, bool f16, unsigned* status, const DeviceInfo& di, cudaStream_t st);
+
+// The form for few rows (paged_attention_few.cu): 16-bit caches; rows of a unit 8 or 16.
+struct PagedFewShape {
+    int RU, KT, ctas;
+};
+static inline PagedFewShape paged_few_shape(int head_dim, int rows) { return {rows <= 8 ? 8 : 16, head_dim == 64 ? 256 : 128, head_dim == 256 ? 148 : 296}; }
+coreinfer_status paged_few(const PagedAttnArgs& a, bool f16, const DeviceInfo& di, cudaStream_t st);
 
 #ifdef __CUDACC__
 
@@ -183,11 +192,67 @@ __device__ __forceinline__ int paged_unit_rows(const PagedAttnArgs& a, const Pag
     const int left = paged_rows(a, w.s) - w.tile * a.RU;
     return left < a.RU ? left : a.RU;
 }
+// The infinities and NaN of one output that a row sees in the piece's tiles: in all of them, or in those that some row of the
+// unit sees in part only (the others' reach the sums by themselves).  hi_min, lo_max: of the unit's rows.
+template <typename T>
+__device__ __noinline__ float paged_odd_sum(const PagedAttnArgs& a, const PagedWalk& w, bool all, int hi_min, int lo_max, int from, int to, int row, int d)
+{
+    const PagedRow see = paged_row(a, w.s, row);
+    float sum = 0.f;
+    for (int i = from; i < to; ++i) {
+        const int j0 = paged_tile_at(w.t, i) * a.KT;
+        if (!all && j0 + a.KT <= hi_min && (j0 >= lo_max || j0 + a.KT <= a.sinks)) continue;
+        for (int j = j0; j < j0 + a.KT; ++j) {
+            if (!paged_sees(a, see, j)) continue;
+            const int page = paged_page(a.c, w.b, j);
+            if (page < 0) continue;
+            const float x = to_f32(reinterpret_cast<const T*>(a.c.pool[1])[paged_offset(a.c, page, w.h, j) + d]);
+            if (!isfinite(x)) sum += x;
+        }
+    }
+    return sum;
+}
+// An output that came out NaN although its row's weights are numbers: a weight that was rounded to 0, or one of its two parts, met
+// an infinity.  It is the sum of the infinities if that is one.
+template <typename T>
+__device__ __forceinline__ float paged_mend(const PagedAttnArgs& a, const PagedWalk& w, int from, int to, int row, int d, float o, float l)
+{
+    if (!isnan(o) || isnan(l)) return o;
+    const float x = paged_odd_sum<T>(a, w, true, 0, 0, from, to, row, d);
+    return isinf(x) ? x : o;
+}
+// Factor of a piece's output when pieces are joined; not 0, so that an infinity stays one (what it adds otherwise is below 2^-100
+// of the values).
+__device__ __forceinline__ float paged_join_factor(float m, float ref) { return fmaxf(exp2f(m - ref), 1e-37f); }
 // Element offset of a row of a unit in q or out.
 __device__ __forceinline__ long long paged_row_offset(const PagedAttnArgs& a, const PagedSeq& s, int h, int row, long long ld)
 {
     const int t = row / a.share;
     return (long long)(s.first + t) * ld + (long long)(h * a.share + row - t * a.share) * a.c.D;
+}
+
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi)
+{
+    uint32_t r;
+    if constexpr (sizeof(T) == 2 && std::is_same<T, __half>::value) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// Whether one of the two 16-bit values is an infinity or NaN.
+template <typename T>
+__device__ __forceinline__ bool odd_pair(uint32_t w)
+{
+    constexpr uint32_t E = std::is_same<T, __half>::value ? 0x7c00u : 0x7f80u;
+    return (w & E) == E || (w & (E << 16)) == (E << 16);
+}
+template <typename T>
+__device__ __forceinline__ uint32_t without_odd(uint32_t w)
+{
+    constexpr uint32_t E = std::is_same<T, __half>::value ? 0x7c00u : 0x7f80u;
+    if ((w & E) == E) w &= 0xffff0000u;
+    if ((w & (E << 16)) == (E << 16)) w &= 0xffffu;
+    return w;
 }
 
 #endif

@@ -101,51 +101,6 @@ __device__ __forceinline__ bool chunk_wait(uint64_t& bar, uint32_t parity, Chunk
     }
 }
 
-template <typename T>
-__device__ __forceinline__ uint32_t pack2(float lo, float hi)
-{
-    uint32_t r;
-    if constexpr (sizeof(T) == 2 && std::is_same<T, __half>::value) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-// Whether one of the two 16-bit values is an infinity or NaN.
-template <typename T>
-__device__ __forceinline__ bool odd_pair(uint32_t w)
-{
-    constexpr uint32_t E = std::is_same<T, __half>::value ? 0x7c00u : 0x7f80u;
-    return (w & E) == E || (w & (E << 16)) == (E << 16);
-}
-template <typename T>
-__device__ __forceinline__ uint32_t without_odd(uint32_t w)
-{
-    constexpr uint32_t E = std::is_same<T, __half>::value ? 0x7c00u : 0x7f80u;
-    if ((w & E) == E) w &= 0xffff0000u;
-    if ((w & (E << 16)) == (E << 16)) w &= 0xffffu;
-    return w;
-}
-
-// Adds to 32 outputs of a row the infinities and NaN that it sees in tiles that were looked through.
-template <typename T, int D>
-__device__ __noinline__ void chunk_restore(const PagedAttnArgs& a, const PagedWalk& w, const ChunkView& va, const ChunkView& vb, int from, int to, int row, int d0, float* o)
-{
-    const PagedRow see = paged_row(a, w.s, row);
-    for (int i = from; i < to; ++i) {
-        const int j0 = paged_tile_at(w.t, i) * kChunkKT;
-        if (!chunk_look(a, va, vb, j0)) continue;
-        for (int j = j0; j < j0 + kChunkKT; ++j) {
-            if (!paged_sees(a, see, j)) continue;
-            const int page = paged_page(a.c, w.b, j);
-            if (page < 0) continue;
-            const T* v = reinterpret_cast<const T*>(a.c.pool[1]) + paged_offset(a.c, page, w.h, j) + d0;
-            for (int e = 0; e < 32; ++e) {
-                const float x = to_f32(v[e]);
-                if (!isfinite(x)) o[e] += x;
-            }
-        }
-    }
-}
-
 template <typename T, int D>
 __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                                                                         const __grid_constant__ ChunkArgs g)
@@ -472,12 +427,17 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
 #pragma unroll
                     for (int e = 0; e < 32; ++e) o[e] = 0u;
                 }
-                if (restore && mine) {
-                    float more[32];
-                    for (int e = 0; e < 32; ++e) more[e] = __uint_as_float(o[e]);
-                    chunk_restore<T, D>(a, w, chunk_view(a, w, rows, 0), chunk_view(a, w, rows, 1), from, to, row, c * 32, more);
+                float spoilt = 0.f;                              // NaN where an output is
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(more[e]);
+                for (int e = 0; e < 32; ++e) spoilt += __uint_as_float(o[e]) * 0.f;
+                if (mine && (restore || isnan(spoilt))) {
+                    const PagedRow low = paged_row(a, w.s, w.tile * a.RU), high = paged_row(a, w.s, w.tile * a.RU + rows - 1);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        float y = __uint_as_float(o[e]);
+                        if (restore) y += paged_odd_sum<T>(a, w, false, low.hi, high.lo, from, to, row, c * 32 + e);
+                        o[e] = __float_as_uint(paged_mend<T>(a, w, from, to, row, c * 32 + e, y, l));
+                    }
                 }
                 if (!mine) continue;
                 if (head && tail) {

@@ -155,8 +155,8 @@ def attention(batch, q, scale, window=0, sinks=0):
                 out[rows, h] = 0
                 continue
             kept = seen[:, :, None]
-            logits = (x @ kh.nan_to_num(0, 0, 0).T + (x[:, None] * torch.where(torch.isfinite(kh), 0.0, kh)[None]).where(kept & ~torch.isfinite(kh), 0.0).sum(-1)
-                      if not torch.isfinite(kh).all() else x @ kh.T) * scale
+            logits = x @ kh.T if torch.isfinite(kh).all() else (x[:, None] * kh).sum(-1)
+            logits = logits * scale
             logits = logits.masked_fill(~seen, -math.inf)
             p = torch.exp(logits - logits.amax(-1, keepdim=True))
             p = p / p.sum(-1, keepdim=True)

@@ -241,3 +241,89 @@ def test_attention_many_units_per_block(dtype):
         if not small:
             ci.coreinfer_workspace_status(ws)
         check_attention(b, q, out, 0.125, window, sinks)
+
+
+ODD = [([1, 1], [300, 40], 2, 64, 16, 0, 0), ([4, 2], [300, 150], 2, 128, 32, 0, 0), ([60, 5], [200, 130], 3, 64, 16, 0, 0), ([150], [400], 1, 128, 64, 0, 0),
+       ([50, 1], [600, 290], 2, 128, 16, 100, 5), ([3], [500], 4, 256, 16, 130, 2), ([270], [270], 1, 64, 128, 0, 0), ([9], [1000], 2, 64, 16, 70, 9)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("new,length,share,D,page,window,sinks", ODD)
+def test_attention_odd_values_reach_only_who_sees_them(new, length, share, D, page, window, sinks, dtype):
+    """Infinities and NaN in keys and values among the new tokens, at a window's edges and far back."""
+    require_gpu()
+    b = Batch(new, length, 2, share, D, page, dtype, seed=D + sum(new), front=1, pad=2)
+    for s, n in enumerate(new):
+        L = length[s]
+        spots = {L - 1: float("nan"), L - (n + 1) // 2: float("inf"), max(0, L - n): float("-inf"), max(0, L - n - 3): float("inf")}
+        if window:
+            spots.update({max(0, L - n - window): float("nan"), max(0, L - window - n // 2): float("-inf"), 1: float("inf"), sinks + 3: float("nan")})
+        for x, (j, value) in enumerate(spots.items()):
+            b.v[b.table[s, j // page].item(), x % 2, j % page, (7 * x) % D] = value
+    q = b.rand(2 * share)
+    out = attend(b, q, D ** -0.5, window, sinks)
+    check_attention(b, q, out, D ** -0.5, window, sinks)
+    assert torch.isfinite(out[1:]).any()
+    for s, n in enumerate(new):                                  # a key that is not finite makes all of a row that sees it NaN, and no other
+        b.k[b.table[s, (length[s] - 1) // page].item(), 1, (length[s] - 1) % page, 3] = float("nan")
+    b.v.nan_to_num_(0, 0, 0)
+    out = attend(b, q, D ** -0.5, window, sinks)
+    rows = torch.arange(q.shape[0])
+    last = torch.tensor([b.starts[s + 1] - 1 for s, n in enumerate(new) if n])
+    bad = torch.isnan(out).any(-1).any(-1).cpu()
+    assert bad[last].all() and bad.sum() == len(last)
+    assert torch.isnan(out[last][:, share:]).all() and torch.isfinite(out[:, :share]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T,D", [(1, 64), (5, 128), (90, 128), (40, 256)])
+def test_attention_scales(T, D, dtype):
+    """A scale of 0 (all weights equal), one below 0, logits so large that a single weight is left; logits of -infinity alone give NaN."""
+    require_gpu()
+    b = Batch([T, T], [200, T], 1, 3, D, 16, dtype, seed=T)
+    q = b.rand(3)
+    for scale in (0.0, -0.2, 3.0):
+        out = attend(b, q, scale)
+        check_attention(b, q, out, scale)
+    b.k.nan_to_num_(0, 0, 0).abs_()
+    b.k[..., 0] = float("inf")
+    q = q.abs().contiguous()
+    assert torch.isnan(attend(b, q, -1.0)).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T", [1, 6, 100])
+def test_attention_outside_the_cache(T, dtype):
+    """Pages that are none read as zeros, tokens at positions below 0 see nothing, nobody sees behind the table, starts that run
+    backwards or behind the tensors reach nothing."""
+    require_gpu()
+    b = Batch([T, T, T], [130 + T, T // 2, 160], 2, 2, 128, 16, dtype, seed=T)
+    b.table = b.table.clone()
+    b.table[0, 2], b.table[0, 5], b.table[1, 0] = -1, b.n_pages, 2 ** 31 - 1
+    b.length_list[2] = b.table.shape[1] * 16 + 40                # behind the table
+    b.length[2] = b.length_list[2]
+    b.k.nan_to_num_(0, 0, 0), b.v.nan_to_num_(0, 0, 0)
+    q = b.rand(4)
+    for window, sinks in ((0, 0), (50, 3)):
+        out = attend(b, q, 0.1, window, sinks)
+        want, tol = attention(b, q, 0.1, window, sinks)
+        check(out, want, tol)
+    assert (out[T:T + T - T // 2] == 0).all()                    # positions below 0
+    for start in ([9, 3, 900, -4], [0, 0, 0, 0], [5, 5, 2 ** 31 - 1, 7], [-(2 ** 31), 2, 1, 2]):
+        b.start.copy_(torch.tensor(start, dtype=torch.int32))
+        b.length.copy_(torch.tensor([2 ** 31 - 1, -9, 50], dtype=torch.int32))
+        attend(b, q, 0.1, 10, 3)
+    torch.cuda.synchronize()
+
+
+def test_attention_shared_pages_and_equal_sequences():
+    """Two sequences on the same pages come out alike, whatever their place in the batch and the cut of the work."""
+    require_gpu()
+    for dtype, T in (("bf16", 1), ("f16", 40), ("f32", 3)):
+        b = Batch([T, T, T], [700, 333, 700], 2, 4, 64, 16, dtype, seed=2)
+        b.table[2] = b.table[0]
+        q = b.rand(8)
+        q[2 * T:] = q[:T]
+        out = attend(b, q, 0.125)
+        assert (out[2 * T:].float() - out[:T].float()).abs().max() <= 2.0 ** -7 * out.abs().max().float()
+        check_attention(b, q, out, 0.125)
