@@ -616,11 +616,10 @@ def make_rope(turns, interleaved: bool = False, magnitude: float = 1.0, q_norm=N
 
 def _packed_stride(t, tokens, heads, dim):
     """Elements between the rows of a packed [tokens, heads, head_dim] tensor (a slice of a wider projection is fine)."""
-    if t.is_contiguous():
-        return heads * dim
-    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
+    row, head, one = t.stride()
+    if one != 1 or (head != dim and heads > 1):
         raise CoreInferError(ERR_INVALID_ARG, "rows with contiguous heads were expected: shape %s, strides %s" % (tuple(t.shape), tuple(t.stride())))
-    return t.stride(0) if tokens > 1 else heads * dim
+    return row if tokens > 1 else heads * dim
 
 
 def _on_device(device, call, *args):
@@ -649,29 +648,35 @@ def coreinfer_rope_apply(rope, positions, q, k, q_out, k_out, stream=None):
     """Turn (and norm) q [tokens, q_heads, head_dim] and k [tokens, kv_heads, head_dim], either of them None, to the
     positions int32 [tokens]; q_out and k_out may be q and k."""
     x = q if q is not None else k
-    if x is None or x.dim() != 3 or (k is not None and (k.dim() != 3 or k.shape[0] != x.shape[0] or k.shape[2] != x.shape[2])):
-        raise CoreInferError(ERR_INVALID_ARG, "q and k [tokens, heads, head_dim] were expected")
+    if x is None or x.dim() != 3:
+        raise CoreInferError(ERR_INVALID_ARG, "q or k [tokens, heads, head_dim] was expected")
     tokens, _, dim = x.shape
     dtype, device = x.dtype, x.get_device()
     if dtype not in _DTYPE_CODES:
         raise CoreInferError(ERR_UNSUPPORTED, "unsupported torch dtype %s" % dtype)
-    given = []
-    for t, out in ((q, q_out), (k, k_out)):
-        if (t is None) != (out is None) or (t is not None and (out.shape != t.shape or t.dtype != dtype or out.dtype != dtype)):
-            raise CoreInferError(ERR_INVALID_ARG, "q with q_out and k with k_out, of one type and shape each, were expected")
-        if t is None:
-            given += [0, None, 0, None, 0]
-            continue
-        if t.get_device() != device or out.get_device() != device:
-            _off_device("q, k and their outputs")
-        heads = t.shape[1]
-        given += [heads, t.data_ptr(), _packed_stride(t, tokens, heads, dim), out.data_ptr(), _packed_stride(out, tokens, heads, dim)]
+    hq, qp, lq, qo, lqo = _turned(q, q_out, tokens, dim, dtype, device)
+    hk, kp, lk, ko, lko = _turned(k, k_out, tokens, dim, dtype, device)
     _check_rope(rope, dtype, dim, device)
-    hq, qp, lq, qo, lqo, hk, kp, lk, ko, lko = given
-    status = _on_device(device, (_lib or load()).coreinfer_rope_apply, rope, _index(positions, tokens, device, "positions"), _DTYPE_CODES[dtype], tokens,
-                        hq, hk, dim, qp, lq, kp, lk, qo, lqo, ko, lko, _raw_stream(device, stream))
+    at = _index(positions, tokens, device, "positions")
+    status = _on_device(device, (_lib or load()).coreinfer_rope_apply, rope, at, _DTYPE_CODES[dtype], tokens, hq, hk, dim, qp, lq, kp, lk, qo, lqo, ko, lko,
+                        _raw_stream(device, stream))
     if status:
         _check(status)
+
+
+def _turned(t, out, tokens, dim, dtype, device):
+    """Heads, address and row stride of a tensor that is turned, and its output's."""
+    if t is None and out is None:
+        return 0, None, 0, None, 0
+    if t is None or out is None:
+        raise CoreInferError(ERR_INVALID_ARG, "q with q_out and k with k_out were expected")
+    shape = t.shape
+    if len(shape) != 3 or shape[0] != tokens or shape[2] != dim or out.shape != shape or t.dtype != dtype or out.dtype != dtype:
+        raise CoreInferError(ERR_INVALID_ARG, "q, k and their outputs [tokens, heads, head_dim] of one type were expected")
+    if t.get_device() != device or out.get_device() != device:
+        _off_device("q, k and their outputs")
+    heads = shape[1]
+    return heads, t.data_ptr(), _packed_stride(t, tokens, heads, dim), out.data_ptr(), _packed_stride(out, tokens, heads, dim)
 
 
 def make_paged_cache(k, v, table, length) -> PagedCache:

@@ -6,18 +6,18 @@
 // quarter of a turn goes to sincospif as an fp32 number of at most 1/4 (error 2e-8 in the angle, below fp32's rounding of
 // cosine and sine).
 //
-// What bounds it: bytes (each value read and written once), and a launch's latency where the tokens are few.  Eight values a
-// lane, so that a pair's other half is a shuffle away (or in the same lane) and a head's sum of squares stays in a warp; the
-// lanes of a CTA share one table of cosines and sines per token, which would otherwise cost more instructions than all else.
-// Few tokens: the heads of a token are spread over CTAs (grid y) until there is one for every SM.
+// What bounds it: bytes (each value read and written once), and a launch's latency where the tokens are few.  A warp takes a token, or a
+// part of its heads where the tokens are few, so that the cosines and sines are formed once per token (two pairs a lane, through
+// shared memory) and no warp waits for another.  Eight values a lane: a pair's other half is a shuffle away (of packed words) or in the
+// same lane.  Norm weights enter the table's factors, so that a value costs a product, a fused product and the product with 1 / root:
+//   y = r (x (w c) + x' (w' s)),  r = 1 / sqrt(mean x^2 + eps),  x', w': the pair's other value and its weight.
 #include "paged.cuh"
 
 #include <math.h>
 
 namespace coreinfer {
 
-constexpr int kRopeThreads = 256;
-constexpr int kRopeMaxTokens = 8;                    // tokens per CTA
+constexpr int kRopeWarps = 8;
 constexpr int kRopeMaxPairs = 128;
 
 struct RopeArgs {
@@ -35,9 +35,7 @@ struct RopeArgs {
     float eps, magnitude;
     int rot, interleaved;
     int tokens, Hq, H;
-    int units;                      // heads of a token, those of the values among them
-    int per_token;                  // threads of a token
-    int unit_step;                  // heads of a token per CTA
+    int split;                      // warps per token
 };
 
 template <typename T>
@@ -67,129 +65,167 @@ __device__ __forceinline__ int row_sequence(const Paged& c, int row)
 }
 
 template <typename T, int D, bool APPEND>
-__global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constant__ RopeArgs a)
+__global__ void __launch_bounds__(32 * kRopeWarps, 3) rope_kernel(const __grid_constant__ RopeArgs a)
 {
     constexpr int LPH = D / 8;                       // lanes per head
+    constexpr int HPW = 32 / LPH;                    // heads at a time
     constexpr int E = sizeof(T);
-    __shared__ float2 table[kRopeMaxTokens][kRopeMaxPairs];
-    __shared__ int at[kRopeMaxTokens];               // position a token is turned by
-    const int tid = threadIdx.x;
-    const int mine = tid / a.per_token;              // token of the CTA
-    const int tokens = kRopeThreads / a.per_token;
-    const int row = blockIdx.x * tokens + mine;
-    const int slots = a.per_token / LPH;             // heads of a token at a time
-    const int l = tid % LPH;
-    const int first = blockIdx.y * a.unit_step;
-    const int end = first + a.unit_step < a.units ? first + a.unit_step : a.units;
-    const bool norms = a.q_norm != nullptr || a.k_norm != nullptr;
+    constexpr int WORDS = E / 2;                     // 16-byte words of eight values
+    constexpr int U = E == 2 ? 8 : 4;                // loads under way per lane
+    __shared__ float2 tables[kRopeWarps][kRopeMaxPairs];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, l = lane % LPH;
+    float2* table = tables[warp];
+    const unsigned id = blockIdx.x * kRopeWarps + warp;
+    const int row = id / (unsigned)a.split, part = id - row * a.split;
+    const int rounds_q = (a.Hq + HPW - 1) / HPW, rounds_h = (a.H + HPW - 1) / HPW;
+    const int total = rounds_q + (APPEND ? 2 : 1) * rounds_h;
+    const int first = total * part / a.split, end = total * (part + 1) / a.split;
     wait_for_stream();
+    if (row >= a.tokens) return;
 
-    // a token's place: the same in all its lanes, whole warps per token
-    bool live = row < a.tokens;
     int page = -1, slot_position = 0;
     if (APPEND) {
         const int b = row_sequence(a.c, row);
-        live = live && b >= 0;
-        if (live) {
-            const PagedSeq s = paged_seq(a.c, b);
-            live = row - s.first < s.n;
-            slot_position = s.position + row - s.first;
-            if (live) page = paged_page(a.c, b, slot_position);
-        }
+        if (b < 0) return;
+        const PagedSeq s = paged_seq(a.c, b);
+        if (row - s.first >= s.n) return;
+        slot_position = s.position + row - s.first;
+        page = paged_page(a.c, b, slot_position);
     }
-    auto source = [&](int u) -> const uint8_t* {
-        if (u < a.Hq) return a.q + ((long long)row * a.ld_q + u * D + l * 8) * E;
-        if (u < a.Hq + a.H) return a.k + ((long long)row * a.ld_k + (u - a.Hq) * D + l * 8) * E;
-        return a.v + ((long long)row * a.ld_v + (u - a.Hq - a.H) * D + l * 8) * E;
-    };
-    int u = first + (tid % a.per_token) / LPH;
-    uint4 raw[E / 2];
-    if (live && u < end) load8<T>(source(u), raw);
-
-    float wq[8], wk[8];
-    if (norms) {
-        uint4 w[E / 2];
-        if (a.q_norm) { load8<T>((const uint8_t*)a.q_norm + l * 8 * E, w); unpack8<T>(w, wq); }
-        if (a.k_norm) { load8<T>((const uint8_t*)a.k_norm + l * 8 * E, w); unpack8<T>(w, wk); }
-    }
-    if (a.rot) {
-        if (tid % a.per_token == 0) at[mine] = !live ? 0 : (a.positions ? a.positions[row] : slot_position);
-        __syncthreads();
-        const int pairs = a.rot / 2;
-        for (int i = tid; i < pairs * tokens; i += kRopeThreads) {
-            const int t = i / pairs, j = i - t * pairs;
-            const uint64_t turn = (uint64_t)(int64_t)at[t] * a.turns[j];
-            const uint64_t quarter = (turn + (1ull << 61)) >> 62;
+    if (a.rot && first < rounds_q + rounds_h) {
+        const uint64_t at = (uint64_t)(int64_t)(a.positions ? a.positions[row] : slot_position);
+        for (int j = lane; j < a.rot / 2; j += 32) {
+            const uint64_t turn = at * a.turns[j];
+            const uint64_t quarter = (turn + (1ull << 61)) >> 62 & 3;
             float sine, cosine;
             sincospif((float)(int64_t)(turn - (quarter << 62)) * 0x1p-63f, &sine, &cosine);
             const float x = quarter & 1 ? sine : cosine, y = quarter & 1 ? cosine : sine;
-            table[t][j] = make_float2(a.magnitude * (quarter == 1 || quarter == 2 ? -x : x), a.magnitude * (quarter & 2 ? -y : y));
+            table[j] = make_float2(a.magnitude * (quarter == 1 || quarter == 2 ? -x : x), a.magnitude * (quarter & 2 ? -y : y));
         }
-        __syncthreads();
+        __syncwarp();
     }
-    if (!live) return;                               // whole warps: the shuffles below stay full
 
-    // x' = c x + s (its partner's x)
-    float c[8], s[8];
     const bool turned = l * 8 < a.rot;
     const int half = a.rot / 16;                     // lanes of the first halves
     const int partner = a.interleaved || !turned ? l : (l < half ? l + half : l - half);
-    if (turned) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float2 t = table[mine][a.interleaved ? l * 4 + e / 2 : (l < half ? l : l - half) * 8 + e];
-            c[e] = t.x;
-            s[e] = (a.interleaved ? !(e & 1) : l < half) ? -t.y : t.y;
-        }
-    }
-    // lanes of a warp may hold different heads: all of them go round as often as the first
-    for (; u - (tid % a.per_token & 31) / LPH < end; u += slots) {
-        const bool here = u < end;
-        uint4 ahead[E / 2];
-        if (u + slots < end) load8<T>(source(u + slots), ahead);
-        float x[8];
-        if (here) unpack8<T>(raw, x);
+    const uint32_t keep = turned ? 0xffffffffu : 0u; // what is not turned takes nothing from another value
+
+    // heads [from, to) of rounds of queries or keys; kind 0 queries, 1 keys
+    auto turn_heads = [&](int kind, int from, int to) {
+        const uint8_t* in = kind == 0 ? a.q : a.k;
+        const long long ld = kind == 0 ? a.ld_q : a.ld_k;
+        const int heads = kind == 0 ? a.Hq : a.H;
+        const uint8_t* weight = (const uint8_t*)(kind == 0 ? a.q_norm : a.k_norm);
+        const uint8_t* src = in + ((long long)row * ld + l * 8) * E;
+        uint8_t* dst;
+        long long step;                              // bytes between heads
+        if (kind == 0) { dst = a.q_out + ((long long)row * a.ld_q_out + l * 8) * E; step = D * E; }
+        else if (!APPEND) { dst = a.k_out + ((long long)row * a.ld_k_out + l * 8) * E; step = D * E; }
         else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = 0.f;
+            if (page < 0) return;
+            dst = const_cast<uint8_t*>(a.c.pool[0]) + (paged_offset(a.c, page, 0, slot_position) + l * 8) * E;
+            step = a.c.head_stride * E;
         }
-        const bool is_q = u < a.Hq, is_v = u >= a.Hq + a.H;
-        if (norms) {
-            float sum = 0.f;
+        float cw[8], sw[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
+        for (int e = 0; e < 8; ++e) { cw[e] = 1.f; sw[e] = 0.f; }
+        if (turned) {
 #pragma unroll
-            for (int d = 1; d < LPH; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-            const float r = __frsqrt_rn(sum * (1.f / D) + a.eps);
-            if (is_q ? a.q_norm != nullptr : (!is_v && a.k_norm != nullptr)) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = x[e] * r * (is_q ? wq[e] : wk[e]);
+            for (int e = 0; e < 8; ++e) {
+                const float2 t = table[a.interleaved ? l * 4 + e / 2 : (l < half ? l : l - half) * 8 + e];
+                cw[e] = t.x;
+                sw[e] = (a.interleaved ? !(e & 1) : l < half) ? -t.y : t.y;
             }
         }
-        if (a.rot) {
-            float y[8];
+        if (weight) {
+            uint4 raw[WORDS];
+            float w[8];
+            load8<T>(weight + l * 8 * E, raw);
+            unpack8<T>(raw, w);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = a.interleaved ? x[e ^ 1] : __shfl_sync(0xffffffffu, x[e], partner, LPH);
-            if (turned && !is_v) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = fmaf(s[e], y[e], c[e] * x[e]);
+            for (int e = 0; e < 8; ++e) {
+                const float other = a.interleaved ? w[e ^ 1] : __shfl_sync(0xffffffffu, w[e], partner, LPH);
+                cw[e] *= w[e];
+                sw[e] *= other;
             }
         }
-        if (here) {
-            if (is_q) store8<T>(a.q_out + ((long long)row * a.ld_q_out + u * D + l * 8) * E, x);
-            else if (APPEND) {
-                const int h = is_v ? u - a.Hq - a.H : u - a.Hq;
-                if (page >= 0) {
-                    uint8_t* to = const_cast<uint8_t*>(a.c.pool[is_v]) + (paged_offset(a.c, page, h, slot_position) + l * 8) * E;
-                    if (is_v) {
+        for (int i = from; i < to; i += U) {
+            uint4 raw[U][WORDS];
 #pragma unroll
-                        for (int i = 0; i < E / 2; ++i) reinterpret_cast<uint4*>(to)[i] = raw[i];
-                    } else store8<T>(to, x);
+            for (int x = 0; x < U; ++x) {
+                const int h = (i + x) * HPW + lane / LPH;
+                if (i + x < to && h < heads) load8<T>(src + (long long)h * D * E, raw[x]);
+            }
+#pragma unroll
+            for (int x = 0; x < U; ++x) {
+                if (i + x >= to) break;
+                const int h = (i + x) * HPW + lane / LPH;
+                float v[8], o[8], r = 1.f;
+                uint4 other[WORDS];
+#pragma unroll
+                for (int y = 0; y < WORDS; ++y) {
+                    other[y] = raw[x][y];
+                    if (!a.interleaved && a.rot) {
+                        other[y].x = __shfl_sync(0xffffffffu, raw[x][y].x, partner, LPH) & keep;
+                        other[y].y = __shfl_sync(0xffffffffu, raw[x][y].y, partner, LPH) & keep;
+                        other[y].z = __shfl_sync(0xffffffffu, raw[x][y].z, partner, LPH) & keep;
+                        other[y].w = __shfl_sync(0xffffffffu, raw[x][y].w, partner, LPH) & keep;
+                    }
                 }
-            } else store8<T>(a.k_out + ((long long)row * a.ld_k_out + (u - a.Hq) * D + l * 8) * E, x);
-        }
+                unpack8<T>(raw[x], v);
+                unpack8<T>(other, o);
+                if (a.interleaved) {
 #pragma unroll
-        for (int i = 0; i < E / 2; ++i) raw[i] = ahead[i];
+                    for (int e = 0; e < 8; ++e) o[e] = turned ? v[e ^ 1] : 0.f;
+                }
+                if (weight) {
+                    float sum = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum = fmaf(v[e], v[e], sum);
+#pragma unroll
+                    for (int d = 1; d < LPH; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+                    r = __frsqrt_rn(sum * (1.f / D) + a.eps);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    v[e] = fmaf(o[e], sw[e], v[e] * cw[e]);
+                    if (weight) v[e] *= r;
+                }
+                if (h < heads) store8<T>(dst + h * step, v);
+            }
+        }
+    };
+    // heads that are stored as they are
+    auto copy_heads = [&](int which, int from, int to) {
+        if (page < 0) return;
+        const uint8_t* src = (which ? a.v : a.k) + ((long long)row * (which ? a.ld_v : a.ld_k) + l * 8) * E;
+        uint8_t* dst = const_cast<uint8_t*>(a.c.pool[which]) + (paged_offset(a.c, page, 0, slot_position) + l * 8) * E;
+        for (int i = from; i < to; i += U) {
+            uint4 raw[U][WORDS];
+#pragma unroll
+            for (int x = 0; x < U; ++x) {
+                const int h = (i + x) * HPW + lane / LPH;
+                if (i + x < to && h < a.H) load8<T>(src + (long long)h * D * E, raw[x]);
+            }
+#pragma unroll
+            for (int x = 0; x < U; ++x) {
+                const int h = (i + x) * HPW + lane / LPH;
+                if (i + x < to && h < a.H) {
+#pragma unroll
+                    for (int y = 0; y < WORDS; ++y) reinterpret_cast<uint4*>(dst + h * a.c.head_stride * E)[y] = raw[x][y];
+                }
+            }
+        }
+    };
+    if (first < rounds_q) turn_heads(0, first, end < rounds_q ? end : rounds_q);
+    const int k0 = first > rounds_q ? first - rounds_q : 0, k1 = end - rounds_q < rounds_h ? end - rounds_q : rounds_h;
+    if (k0 < k1) {
+        if (APPEND && !a.rot) copy_heads(0, k0, k1);
+        else turn_heads(1, k0, k1);
+    }
+    if (APPEND) {
+        const int v0 = first > rounds_q + rounds_h ? first - rounds_q - rounds_h : 0, v1 = end - rounds_q - rounds_h;
+        if (v0 < v1) copy_heads(1, v0, v1);
     }
     let_next_start();
 }
@@ -197,20 +233,15 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constan
 template <typename T, int D, bool APPEND>
 static coreinfer_status launch_rope(RopeArgs& a, const DeviceInfo& di, cudaStream_t st)
 {
-    constexpr int LPH = D / 8;
-    // several tokens per CTA where their heads leave room, but not fewer CTAs than two for every SM
-    int tokens = 1;
-    while (tokens < kRopeMaxTokens && 2 * tokens * a.units * LPH <= kRopeThreads && a.tokens / (2 * tokens) >= 2 * di.sm_count) tokens *= 2;
-    a.per_token = kRopeThreads / tokens;
-    const int slots = a.per_token / LPH;
-    const int ctas = (a.tokens + tokens - 1) / tokens;
-    // few tokens: their heads over several CTAs, one round of heads each at least
-    const int rounds = (a.units + slots - 1) / slots;
-    int split = (di.sm_count + ctas - 1) / ctas;
+    constexpr int HPW = 256 / D;
+    // a warp per token, or as many as bring 16 to every SM, but not more than there are rounds of heads
+    const int rounds = (a.Hq + HPW - 1) / HPW + (APPEND ? 2 : 1) * ((a.H + HPW - 1) / HPW);
+    const long long wanted = 16LL * di.sm_count;
+    long long split = (wanted + a.tokens - 1) / a.tokens;
     if (split > rounds) split = rounds;
-    a.unit_step = (rounds + split - 1) / split * slots;
-    const int y = (a.units + a.unit_step - 1) / a.unit_step;
-    CI_CUDA(launch_overlapped(rope_kernel<T, D, APPEND>, dim3(ctas, y), dim3(kRopeThreads), 0, st, a));
+    a.split = (int)split;
+    const long long warps = a.tokens * split;
+    CI_CUDA(launch_overlapped(rope_kernel<T, D, APPEND>, dim3((unsigned)((warps + kRopeWarps - 1) / kRopeWarps)), dim3(32 * kRopeWarps), 0, st, a));
     return COREINFER_OK;
 }
 
@@ -337,7 +368,6 @@ coreinfer_status coreinfer_rope_apply(const coreinfer_rope* rope, const int32_t*
     a.tokens = tokens;
     a.Hq = q_heads;
     a.H = kv_heads;
-    a.units = q_heads + kv_heads;
     return launch_typed<false>(a, dtype, head_dim, (cudaStream_t)cuda_stream);
 }
 
@@ -376,7 +406,6 @@ coreinfer_status coreinfer_paged_append(const coreinfer_paged_cache* cache, cons
     a.tokens = tokens;
     a.Hq = q_heads;
     a.H = a.c.H;
-    a.units = q_heads + 2 * a.c.H;
     return launch_typed<true>(a, dtype, D, (cudaStream_t)cuda_stream);
 }
 
