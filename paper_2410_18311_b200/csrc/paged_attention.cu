@@ -27,10 +27,10 @@ __global__ void __launch_bounds__(kSimpleThreads) paged_simple_kernel(const __gr
     float* ms = ps + RU * (KT + 4);                  // [RU] reference exponents
     float* ls = ms + RU;                             // [RU] sums
     float* fs = ls + RU;                             // [RU] factor of what was summed before
-    long long* at = reinterpret_cast<long long*>(fs + RU);
+    int* at = reinterpret_cast<int*>(fs + RU);
     const int tid = threadIdx.x;
     wait_for_stream();
-    const long long total = paged_plan(a, at);
+    const int total = paged_plan(a, at);
     if (tid == 0) a.pieces[blockIdx.x].last = -1;
     PagedWalk w;
     for (w.begin(a, at, total, blockIdx.x); w.more(); w.next(a, at)) {
@@ -224,7 +224,7 @@ template <typename T, int D>
 static coreinfer_status launch_simple(PagedAttnArgs& a, const DeviceInfo& di, cudaStream_t st)
 {
     const size_t smem = (size_t)(kSimpleRows * D + kSimpleTile * (D + 4) + kSimpleTile * D + kSimpleRows * (kSimpleTile + 4) + 3 * kSimpleRows) * 4 +
-                        (size_t)(a.c.B + 1) * 8;
+                        (size_t)(a.c.B + 1) * 4;
     coreinfer_status s = allow_smem<paged_simple_kernel<T, D>>(di);
     if (s != COREINFER_OK) return s;
     CI_CUDA(launch_overlapped(paged_simple_kernel<T, D>, dim3(a.n_ctas), dim3(kSimpleThreads), smem, st, a));
@@ -267,10 +267,10 @@ static PagedForm paged_form(coreinfer_dtype dtype, int D, int B, int share, int 
     const PagedFewShape few = paged_few_shape(D, (int)((long long)tokens * share / B > 8 ? 16 : (tokens <= B ? share : 16)));
     return {kFormFew, few.RU, few.KT, few.ctas};
 }
-// A status word (16 bytes), the pieces, their exponents and sums, their outputs.
+// A status word (16 bytes), the pieces, their exponents and sums, their outputs (from a multiple of 32 bytes on).
 static size_t paged_workspace(const PagedForm& f, int D)
 {
-    return 16 + round16(f.ctas * sizeof(PagedPiece)) + round16((size_t)f.ctas * 2 * f.RU * sizeof(float2)) + (size_t)f.ctas * 2 * f.RU * D * sizeof(float);
+    return 16 + round16(f.ctas * sizeof(PagedPiece)) + round16((size_t)f.ctas * 2 * f.RU * sizeof(float2)) + 16 + (size_t)f.ctas * 2 * f.RU * D * sizeof(float);
 }
 
 }  // namespace coreinfer
@@ -310,8 +310,11 @@ coreinfer_status coreinfer_paged_attention(const coreinfer_paged_cache* cache, c
     if (window > 1 << 30 || sinks > 1 << 30) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "window and sinks: at most 2^30");
     if (!isfinite(scale)) CI_FAIL(COREINFER_ERR_INVALID_ARG, "scale must be finite");
     if (!workspace || !aligned16(workspace)) CI_FAIL(COREINFER_ERR_WORKSPACE, "workspace is NULL or misaligned");
-    a.share = q_heads / a.c.H;
+    paged_set_share(a, q_heads / a.c.H);
     const PagedForm f = paged_form(dtype, a.c.D, a.c.B, a.share, tokens);
+    // the list of work counts in 32 bits: row tiles of all sequences, each with all tiles of the table at most
+    if ((double)a.c.H * ((double)tokens * a.share / f.RU + a.c.B) * ((double)a.c.cap / f.KT + 3) >= 2147483648.0)
+        CI_FAIL(COREINFER_ERR_UNSUPPORTED, "%d tokens x %d heads over a table of %d positions: too much for one call", tokens, q_heads, a.c.cap);
     const size_t need = paged_workspace(f, a.c.D);
     if (workspace_bytes < need) CI_FAIL(COREINFER_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
     DeviceInfo di;
@@ -335,7 +338,7 @@ coreinfer_status coreinfer_paged_attention(const coreinfer_paged_cache* cache, c
     ws += round16(f.ctas * sizeof(PagedPiece));
     a.part_ml = (float2*)ws;
     ws += round16((size_t)f.ctas * 2 * f.RU * sizeof(float2));
-    a.part_o = (float*)ws;
+    a.part_o = (float*)(((uintptr_t)ws + 31) & ~(uintptr_t)31);
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (f.kind == kFormChunk) s = paged_chunk(a, dtype == COREINFER_F16, status, di, st);
     else s = f.kind == kFormFew ? paged_few(a, dtype == COREINFER_F16, di, st) : pick_simple<float>(a, di, st);

@@ -27,7 +27,8 @@ struct PagedAttnArgs {
     const uint8_t* q;
     uint8_t* out;
     long long ld_q, ld_out;
-    int share;              // query heads per key head
+    int share;              // query heads per key head, and what divides by it:
+    unsigned share_mul, share_shift;
     int window, sinks;      // window 0: everything before a token
     float scale2;           // scale * log2(e)
     int RU, KT, cost;       // rows of a unit, positions of a tile, entries that a unit's start counts
@@ -50,7 +51,22 @@ struct PagedFewShape {
 static inline PagedFewShape paged_few_shape(int head_dim, int rows) { return {rows <= 8 ? 8 : 16, head_dim == 64 ? 256 : 128, head_dim == 256 ? 148 : 296}; }
 coreinfer_status paged_few(const PagedAttnArgs& a, bool f16, const DeviceInfo& di, cudaStream_t st);
 
+// n / share = (n * mul) >> 32 >> shift for 0 <= n < 2^31, with mul = ceil(2^(31 + l) / share), l = ceil(log2 share), shift = l - 1: the
+// error n (mul share - 2^(31 + l)) / (share 2^(31 + l)) is below 1 / share.  mul 0: share is 1.
+static inline void paged_set_share(PagedAttnArgs& a, int share)
+{
+    a.share = share;
+    a.share_mul = a.share_shift = 0;
+    if (share == 1) return;
+    int l = 1;
+    while ((1 << l) < share) ++l;
+    a.share_mul = (unsigned)(((1ull << (31 + l)) + share - 1) / share);
+    a.share_shift = l - 1;
+}
+
 #ifdef __CUDACC__
+
+__device__ __forceinline__ int by_share(const PagedAttnArgs& a, int n) { return a.share_mul ? (int)(__umulhi((unsigned)n, a.share_mul) >> a.share_shift) : n; }
 
 // The tiles that the rows of a unit see.
 struct PagedTiles {
@@ -65,7 +81,7 @@ __device__ __forceinline__ PagedTiles paged_tiles(const PagedAttnArgs& a, const 
 {
     const int rows = paged_rows(a, s), r0 = tile * a.RU;
     const int r1 = (r0 + a.RU < rows ? r0 + a.RU : rows) - 1;
-    const int p0 = s.position + r0 / a.share, p1 = s.position + r1 / a.share;
+    const int p0 = s.position + by_share(a, r0), p1 = s.position + by_share(a, r1);
     PagedTiles t;
     t.hi = clamp_int(p1 + 1, 0, a.c.cap);
     const int lo = a.window ? clamp_int(p0 - a.window + 1, 0, t.hi) : 0;
@@ -84,7 +100,7 @@ struct PagedRow {
 };
 __device__ __forceinline__ PagedRow paged_row(const PagedAttnArgs& a, const PagedSeq& s, int row)
 {
-    const int p = s.position + row / a.share;
+    const int p = s.position + by_share(a, row);
     PagedRow r;
     r.hi = clamp_int(p + 1, 0, a.c.cap);
     r.lo = a.window ? p - a.window + 1 : 0;
@@ -92,26 +108,27 @@ __device__ __forceinline__ PagedRow paged_row(const PagedAttnArgs& a, const Page
 }
 __device__ __forceinline__ bool paged_sees(const PagedAttnArgs& a, const PagedRow& r, int j) { return j < r.hi && (j >= r.lo || j < a.sinks); }
 
-// The list.  `at` [B + 1] in shared memory; called by all threads of the CTA (a multiple of 32).
-__device__ __forceinline__ long long paged_plan(const PagedAttnArgs& a, long long* at)
+// The list (the host has seen to it that it is shorter than 2^31).  `at` [B + 1] in shared memory; called by all threads of the CTA (a
+// multiple of 32).
+__device__ __forceinline__ int paged_plan(const PagedAttnArgs& a, int* at)
 {
     for (int b = threadIdx.x; b < a.c.B; b += blockDim.x) {
         const PagedSeq s = paged_seq(a.c, b);
         const int tiles = paged_row_tiles(a, s);
-        long long w = 0;
+        int w = 0;
         for (int i = 0; i < tiles; ++i) w += a.cost + paged_tiles(a, s, i).count;
         at[b + 1] = w * a.c.H;
     }
     if (threadIdx.x == 0) at[0] = 0;
     __syncthreads();
     if (threadIdx.x < 32) {
-        long long carry = 0;
+        int carry = 0;
         for (int b0 = 0; b0 < a.c.B; b0 += 32) {
             const int b = b0 + threadIdx.x;
-            long long w = b < a.c.B ? at[b + 1] : 0;
+            int w = b < a.c.B ? at[b + 1] : 0;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
-                const long long left = __shfl_up_sync(0xffffffffu, w, d);
+                const int left = __shfl_up_sync(0xffffffffu, w, d);
                 if (threadIdx.x >= d) w += left;
             }
             w += carry;
@@ -123,22 +140,26 @@ __device__ __forceinline__ long long paged_plan(const PagedAttnArgs& a, long lon
     return at[a.c.B];
 }
 // The list in n equal pieces (n at most its length, so that none is empty): piece i is [total * i / n, total * (i + 1) / n).
-__device__ __forceinline__ long long paged_cut(long long total, int i, int n) { return total / n * i + total % n * i / n; }
+__device__ __forceinline__ int paged_cut(int total, int i, int n)
+{
+    const unsigned each = (unsigned)total / (unsigned)n;
+    return (int)(each * i + ((unsigned)total - each * n) * i / (unsigned)n);
+}
 // The piece that holds an entry: the largest i with total * i / n <= x.
-__device__ __forceinline__ int paged_owner(long long total, long long x, int n) { return (int)(((x + 1) * n - 1) / total); }
+__device__ __forceinline__ int paged_owner(int total, int x, int n) { return (int)((((unsigned long long)x + 1) * n - 1) / (unsigned)total); }
 
 // Walks the units of a piece [x, end) of the list.
 struct PagedWalk {
-    long long x, end;       // entries of the piece not walked yet
+    int x, end;             // entries of the piece not walked yet
     int n;                  // pieces
     int b, h, tile;
-    long long base;         // entry where the unit starts
+    int base;               // entry where the unit starts
     PagedSeq s;
     PagedTiles t;
 
-    __device__ __forceinline__ void begin(const PagedAttnArgs& a, const long long* at, long long total, int cta)
+    __device__ __forceinline__ void begin(const PagedAttnArgs& a, const int* at, int total, int cta)
     {
-        n = total < a.n_ctas ? (int)total : a.n_ctas;
+        n = total < a.n_ctas ? total : a.n_ctas;
         x = end = 0;
         if (cta >= n) return;
         x = paged_cut(total, cta, n);
@@ -151,8 +172,8 @@ struct PagedWalk {
         }
         b = lo;
         s = paged_seq(a.c, b);
-        const long long per_head = (at[b + 1] - at[b]) / a.c.H;
-        h = (int)((x - at[b]) / per_head);
+        const unsigned per_head = (unsigned)(at[b + 1] - at[b]) / (unsigned)a.c.H;
+        h = (int)((unsigned)(x - at[b]) / per_head);
         base = at[b] + h * per_head;
         tile = 0;
         t = paged_tiles(a, s, 0);
@@ -163,13 +184,13 @@ struct PagedWalk {
     }
     __device__ __forceinline__ bool more() const { return x < end; }
     // Tiles from .. to - 1 of the unit are this piece's.
-    __device__ __forceinline__ int from(const PagedAttnArgs& a) const { return x > base + a.cost ? (int)(x - base) - a.cost : 0; }
+    __device__ __forceinline__ int from(const PagedAttnArgs& a) const { return x > base + a.cost ? x - base - a.cost : 0; }
     __device__ __forceinline__ int to(const PagedAttnArgs& a) const
     {
-        const long long n = end - base - a.cost;
-        return n < 0 ? 0 : (n < t.count ? (int)n : t.count);
+        const int n = end - base - a.cost;
+        return n < 0 ? 0 : (n < t.count ? n : t.count);
     }
-    __device__ __forceinline__ void next(const PagedAttnArgs& a, const long long* at)
+    __device__ __forceinline__ void next(const PagedAttnArgs& a, const int* at)
     {
         base += a.cost + t.count;
         x = base;
@@ -227,7 +248,7 @@ __device__ __forceinline__ float paged_join_factor(float m, float ref) { return 
 // Element offset of a row of a unit in q or out.
 __device__ __forceinline__ long long paged_row_offset(const PagedAttnArgs& a, const PagedSeq& s, int h, int row, long long ld)
 {
-    const int t = row / a.share;
+    const int t = by_share(a, row);
     return (long long)(s.first + t) * ld + (long long)(h * a.share + row - t * a.share) * a.c.D;
 }
 

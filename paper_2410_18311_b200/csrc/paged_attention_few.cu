@@ -69,12 +69,12 @@ __global__ void __launch_bounds__(kFewThreads, D == 256 ? 1 : 2) paged_few_kerne
     extern __shared__ __align__(128) uint8_t smem[];
     float2* stats = reinterpret_cast<float2*>(smem + kFewWarps * RING);              // [warps][RU]
     int* found = reinterpret_cast<int*>(stats + kFewWarps * RU);
-    long long* at = reinterpret_cast<long long*>(found + 2);
+    int* at = reinterpret_cast<int*>(found + 2);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     uint8_t* ring = smem + warp * RING;
     const uint32_t ring_at = smem_u32(ring);
     wait_for_stream();
-    const long long total = paged_plan(a, at);
+    const int total = paged_plan(a, at);
     if (tid == 0) {
         a.pieces[blockIdx.x].last = -1;
         found[0] = 0;
@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(kFewThreads, D == 256 ? 1 : 2) paged_few_kerne
 template <typename T, int D, int NT>
 static coreinfer_status launch_few(const PagedAttnArgs& a, const DeviceInfo& di, cudaStream_t st)
 {
-    const size_t smem = (size_t)kFewWarps * kFewStages * kFewStageBytes<D> + kFewWarps * 8 * NT * sizeof(float2) + 8 + (size_t)(a.c.B + 1) * 8;
+    const size_t smem = (size_t)kFewWarps * kFewStages * kFewStageBytes<D> + kFewWarps * 8 * NT * sizeof(float2) + 8 + (size_t)(a.c.B + 1) * 4;
     const coreinfer_status s = allow_smem<paged_few_kernel<T, D, NT>>(di, 0);
     if (s != COREINFER_OK) return s;
     CI_CUDA(launch_overlapped(paged_few_kernel<T, D, NT>, dim3(a.n_ctas), dim3(kFewThreads), smem, st, a));

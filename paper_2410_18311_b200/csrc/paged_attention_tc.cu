@@ -33,6 +33,7 @@ constexpr int kChunkKT = kPagedChunkTile;
 constexpr int kChunkMaxStages = 8;
 constexpr long long kChunkWaitCycles = 3000000000LL;
 constexpr float kNoMax = -INFINITY;
+constexpr int kChunkPoly = 0;        // of four pairs of exponentials, those that are formed on the FMA pipe
 
 struct ChunkArgs {
     PagedAttnArgs a;
@@ -44,7 +45,7 @@ struct ChunkArgs {
 
 struct ChunkBars {
     uint64_t full[kChunkMaxStages], empty[kChunkMaxStages], looked[kChunkMaxStages];
-    uint64_t s_full[2], p_full[2], o_full[2], q_full, q_empty;
+    uint64_t s_full[2], p_full[2][2], o_full[2], q_full[2], q_empty;
     uint32_t tmem;
     int abort;
     int found[4];           // by unit modulo 4: number + 1 of a unit in which values were set to 0
@@ -84,21 +85,92 @@ __device__ __forceinline__ bool chunk_look(const PagedAttnArgs& a, const ChunkVi
     return (chunk_needs(a, va, j) && !chunk_whole(a, va, j)) || (chunk_needs(a, vb, j) && !chunk_whole(a, vb, j));
 }
 
+// Called by whole warps, whose lanes all get the same answer: false when the wait gave up.
 __device__ __forceinline__ bool chunk_wait(uint64_t& bar, uint32_t parity, ChunkBars* s, unsigned* status)
 {
     const uint32_t b = smem_u32(&bar);
-    if (mbar_try_wait(b, parity)) return true;
+    if (__all_sync(0xffffffffu, mbar_try_wait(b, parity))) return true;
     const long long t0 = clock64();
     volatile int* abort_flag = &s->abort;
     for (;;) {
-        if (mbar_try_wait_parked(b, parity, 2000u)) return true;
-        if (*abort_flag) return false;
-        if (clock64() - t0 > kChunkWaitCycles) {
-            *abort_flag = 1;
-            atomicMax(status, (unsigned)kStatusTimeout);
+        if (__all_sync(0xffffffffu, mbar_try_wait_parked(b, parity, 2000u))) return true;
+        const bool late = clock64() - t0 > kChunkWaitCycles;
+        if (__any_sync(0xffffffffu, late || *abort_flag)) {
+            if (late) {
+                *abort_flag = 1;
+                atomicMax(status, (unsigned)kStatusTimeout);
+            }
             return false;
         }
     }
+}
+
+// 32 bytes of a row, in one store where the address is a multiple of 32.
+__device__ __forceinline__ void store32(void* to, const uint32_t* w, bool wide)
+{
+    if (wide)
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                     ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+    else {
+        reinterpret_cast<uint4*>(to)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4*>(to)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+}
+// Two fp32 numbers in a register pair, for the instructions that take both at once.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair(float a, float b)
+{
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void split(f32x2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
+{
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b)
+{
+    f32x2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float max3_nan(float a, float b, float c)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// Bits 0 .. n - 1.
+__device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : (n >= 32 ? 0xffffffffu : (1u << n) - 1u); }
+
+// Two powers of two on the FMA pipe:  x = n + f, n the nearest whole number (read from the last bits of x + 1.5 * 2^23), 2^f by the
+// polynomial of least relative error on [-1/2, 1/2] (Remez exchange; degree 3: 7.5e-5, a sixth of bf16's rounding step or less;
+// degree 4: 2.6e-6), n added to the exponent.  0 below 2^-125, -infinity included; x is at most 15.
+template <bool FINE>
+__device__ __forceinline__ void exp2_poly(f32x2 x, float& a, float& b)
+{
+    const f32x2 shifted = add2(x, pair(12582912.f, 12582912.f));
+    const f32x2 f = fma2(add2(shifted, pair(-12582912.f, -12582912.f)), pair(-1.f, -1.f), x);
+    f32x2 y;
+    if (FINE) {
+        y = fma2(f, pair(0.009570102f, 0.009570102f), pair(0.05591786f, 0.05591786f));
+        y = fma2(f, y, pair(0.24024744f, 0.24024744f));
+        y = fma2(f, y, pair(0.6931218f, 0.6931218f));
+        y = fma2(f, y, pair(0.9999993f, 0.9999993f));
+    } else {
+        y = fma2(f, pair(0.05517167f, 0.05517167f), pair(0.24261113f, 0.24261113f));
+        y = fma2(f, y, pair(0.69326097f, 0.69326097f));
+        y = fma2(f, y, pair(0.99992806f, 0.99992806f));
+    }
+    float n0, n1, x0, x1;
+    split(shifted, n0, n1);
+    split(x, x0, x1);
+    split(y, a, b);
+    a = x0 < -125.f ? 0.f : __uint_as_float(__float_as_uint(a) + (__float_as_uint(n0) << 23));
+    b = x1 < -125.f ? 0.f : __uint_as_float(__float_as_uint(b) + (__float_as_uint(n1) << 23));
 }
 
 template <typename T, int D>
@@ -118,7 +190,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
     uint8_t* qs = smem;                              // [2][BLOCKS][128 rows][128 bytes]
     uint8_t* ring = smem + 2 * TILE;                 // [stages][BLOCKS][128 positions][128 bytes]
     ChunkBars* s = reinterpret_cast<ChunkBars*>(ring + (size_t)g.stages * TILE);
-    long long* at = reinterpret_cast<long long*>(s + 1);
+    int* at = reinterpret_cast<int*>(s + 1);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
     if (tid == 0) {
@@ -129,10 +201,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
         }
         for (int x = 0; x < 2; ++x) {
             mbar_init(smem_u32(&s->s_full[x]), 1);
-            mbar_init(smem_u32(&s->p_full[x]), 4);
+            for (int h = 0; h < 2; ++h) mbar_init(smem_u32(&s->p_full[x][h]), 4);
             mbar_init(smem_u32(&s->o_full[x]), 1);
+            mbar_init(smem_u32(&s->q_full[x]), 2);
         }
-        mbar_init(smem_u32(&s->q_full), 2);
         mbar_init(smem_u32(&s->q_empty), 1);
         s->abort = 0;
         for (int i = 0; i < 4; ++i) s->found[i] = 0;
@@ -145,7 +217,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
     const uint32_t tmem = s->tmem;
     wait_for_stream();
     if (blockIdx.x == 0 && tid == 0) *g.status = kStatusOk;
-    const long long total = paged_plan(a, at);
+    const int total = paged_plan(a, at);
     if (tid == 0) a.pieces[blockIdx.x].last = -1;
 
     if (warp >= 8) {
@@ -180,82 +252,93 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
             }
         } else if (warp == 9) {
             // ---------------------------------------------------- products --
-            if (lane == 0) {
-                int stage = 0;                                   // of K(i)
-                uint32_t ph = 0, looked = 0, p_ph[2] = {0, 0}, q_ph = 0;
-                bool ok = true;
-                auto advance = [&](int& st, uint32_t& p) { if (++st == g.stages) { st = 0; p ^= 1u; } };
-                auto scores = [&](int x, int st) {
-                    const uint64_t q = tc::desc_k(smem_u32(qs + x * TILE)), k = tc::desc_k(smem_u32(ring + (size_t)st * TILE));
+            // The whole warp walks along, so that addresses and descriptors stay in uniform registers, and one lane issues.
+            int stage = 0;                                       // of K(i)
+            uint32_t ph = 0, looked = 0, p_ph[2] = {0, 0}, q_ph = 0;
+            bool ok = true;
+            const uint32_t ring_at = smem_u32(ring), qs_at = smem_u32(qs);
+            auto advance = [&](int& st, uint32_t& p) { if (++st == g.stages) { st = 0; p ^= 1u; } };
+            auto scores = [&](int x, int st) {
+                const uint64_t q = tc::desc_k(qs_at + x * TILE), k = tc::desc_k(ring_at + st * TILE);
+                if (tc::elect()) {
 #pragma unroll
                     for (int d = 0; d < D / 16; ++d) {
                         const uint64_t ofs = (d / 4) * (BLOCK >> 4) + (d % 4) * 2;
                         tc::mma_ss(tmem + x * 128, q + ofs, k + ofs, IDESC_S, d > 0);
                     }
                     tc::commit(smem_u32(&s->s_full[x]));
-                };
-                PagedWalk w;
-                for (w.begin(a, at, total, blockIdx.x); ok && w.more(); w.next(a, at)) {
-                    const int from = w.from(a), to = w.to(a);
-                    if (from >= to) continue;
-                    const int rows = paged_unit_rows(a, w);
-                    const ChunkView v[2] = {chunk_view(a, w, rows, 0), chunk_view(a, w, rows, 1)};
-                    bool begun[2] = {false, false};
-                    if (!(ok = chunk_wait(s->q_full, q_ph, s, g.status))) break;
-                    q_ph ^= 1u;
-                    tc::fence_after();
-                    int j = paged_tile_at(w.t, from) * KT;
-                    if (!(ok = chunk_wait(s->full[stage], ph, s, g.status))) break;
-                    tc::fence_after();
-                    for (int x = 0; x < 2; ++x)
-                        if (chunk_needs(a, v[x], j)) scores(x, stage);
-                    tc::commit(smem_u32(&s->empty[stage]));
-                    if (from + 1 == to) tc::commit(smem_u32(&s->q_empty));
-                    advance(stage, ph);
-                    for (int i = from; i < to; ++i) {
-                        // stage: V(i); the one behind it: K(i + 1)
-                        const int vs = stage;
-                        const uint32_t vph = ph;
-                        advance(stage, ph);
-                        const int ks = stage;
-                        const uint32_t kph = ph;
-                        const bool last = i + 1 == to;
-                        const int j_next = last ? 0 : paged_tile_at(w.t, i + 1) * KT;
-                        if (!(ok = chunk_wait(s->full[vs], vph, s, g.status))) break;
-                        if (!(ok = chunk_wait(s->looked[vs], looked >> vs & 1u, s, g.status))) break;
-                        looked ^= 1u << vs;
-                        bool have_k = false;
-                        for (int x = 0; x < 2; ++x) {
-                            if (chunk_needs(a, v[x], j)) {
-                                if (!(ok = chunk_wait(s->p_full[x], p_ph[x], s, g.status))) break;
-                                p_ph[x] ^= 1u;
-                                tc::fence_after();
-                                const uint64_t val = tc::desc_mn(smem_u32(ring + (size_t)vs * TILE), BLOCK);
-#pragma unroll
-                                for (int k = 0; k < KT / 16; ++k)
-                                    tc::mma_ts(tmem + 256 + x * 128, tmem + x * 128 + k * 8, val + k * (16 * 128 >> 4), IDESC_O, begun[x] || k > 0);
-                                begun[x] = true;
-                            }
-                            if (!last && chunk_needs(a, v[x], j_next)) {
-                                if (!have_k && !(ok = chunk_wait(s->full[ks], kph, s, g.status))) break;
-                                have_k = true;
-                                tc::fence_after();
-                                scores(x, ks);
-                            }
-                        }
-                        if (!ok) break;
-                        tc::commit(smem_u32(&s->empty[vs]));
-                        if (!last) {
-                            if (!have_k && !(ok = chunk_wait(s->full[ks], kph, s, g.status))) break;
-                            tc::commit(smem_u32(&s->empty[ks]));
-                            if (i + 2 == to) tc::commit(smem_u32(&s->q_empty));
-                            advance(stage, ph);
-                        }
-                        j = j_next;
-                    }
-                    for (int x = 0; x < 2; ++x)
-                        if (begun[x]) tc::commit(smem_u32(&s->o_full[x]));
                 }
+                __syncwarp();
+            };
+            auto done = [&](uint64_t& bar) {
+                if (tc::elect()) tc::commit(smem_u32(&bar));
+                __syncwarp();
+            };
+            PagedWalk w;
+            for (w.begin(a, at, total, blockIdx.x); ok && w.more(); w.next(a, at)) {
+                const int from = w.from(a), to = w.to(a);
+                if (from >= to) continue;
+                const int rows = paged_unit_rows(a, w);
+                const ChunkView v[2] = {chunk_view(a, w, rows, 0), chunk_view(a, w, rows, 1)};
+                bool begun[2] = {false, false};
+                int j = paged_tile_at(w.t, from) * KT;
+                if (!(ok = chunk_wait(s->full[stage], ph, s, g.status))) break;
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    if (!v[x].any) continue;
+                    if (ok) ok = chunk_wait(s->q_full[x], q_ph >> x & 1u, s, g.status);
+                    q_ph ^= 1u << x;
+                    tc::fence_after();
+                    if (ok && chunk_needs(a, v[x], j)) scores(x, stage);
+                }
+                if (!ok) break;
+                done(s->empty[stage]);
+                if (from + 1 == to) done(s->q_empty);
+                advance(stage, ph);
+                for (int i = from; i < to; ++i) {
+                    // stage: V(i); the one behind it: K(i + 1)
+                    const int vs = stage;
+                    const uint32_t vph = ph;
+                    advance(stage, ph);
+                    const int ks = stage;
+                    const bool last = i + 1 == to;
+                    const int j_next = last ? 0 : paged_tile_at(w.t, i + 1) * KT;
+                    if (!(ok = chunk_wait(s->full[vs], vph, s, g.status))) break;
+                    if (!(ok = chunk_wait(s->looked[vs], looked >> vs & 1u, s, g.status))) break;
+                    looked ^= 1u << vs;
+                    if (!last && !(ok = chunk_wait(s->full[ks], ph, s, g.status))) break;
+                    const uint64_t val = tc::desc_mn(ring_at + vs * TILE, BLOCK);
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        if (ok && chunk_needs(a, v[x], j)) {
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                if (ok) ok = chunk_wait(s->p_full[x][h], p_ph[x], s, g.status);
+                                tc::fence_after();
+                                if (ok && tc::elect()) {
+#pragma unroll
+                                    for (int k = h * KT / 32; k < (h + 1) * KT / 32; ++k)
+                                        tc::mma_ts(tmem + 256 + x * 128, tmem + x * 128 + k * 8, val + k * (16 * 128 >> 4), IDESC_O, begun[x] || k > 0);
+                                }
+                                __syncwarp();
+                            }
+                            p_ph[x] ^= 1u;
+                            begun[x] = true;
+                        }
+                        if (ok && !last && chunk_needs(a, v[x], j_next)) scores(x, ks);
+                    }
+                    if (!ok) break;
+                    done(s->empty[vs]);
+                    if (!last) {
+                        done(s->empty[ks]);
+                        if (i + 2 == to) done(s->q_empty);
+                        advance(stage, ph);
+                    }
+                    j = j_next;
+                }
+                if (!ok) break;
+                for (int x = 0; x < 2; ++x)
+                    if (begun[x]) done(s->o_full[x]);
             }
         } else {
             // ------------------------------------- queries, looks at values --
@@ -271,29 +354,46 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                 const ChunkView va = chunk_view(a, w, rows, 0), vb = chunk_view(a, w, rows, 1);
                 if (!(ok = chunk_wait(s->q_empty, q_ph ^ 1u, s, g.status))) break;
                 q_ph ^= 1u;
-                constexpr int CPR = D / 8;                       // 16-byte pieces of a row
-                const int padded = (rows + 127) / 128 * 128;
-                const int r_first = w.tile * a.RU;
-                for (int i = t; i < padded * CPR; i += 64) {
-                    const int r = i / CPR, c = i % CPR;
-                    const uint32_t dst = smem_u32(qs) + (r >> 7) * TILE + (c >> 3) * BLOCK + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4);
-                    const uint8_t* src = a.q + (paged_row_offset(a, w.s, w.h, r_first + (r < rows ? r : 0), a.ld_q) + c * 8) * 2;
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(r < rows ? 16 : 0) : "memory");
-                }
-                asm volatile("cp.async.wait_all;" ::: "memory");
-                if (g.negative) {
-                    __syncwarp();                                // each lane turns what it has brought itself
-                    for (int i = t; i < padded * CPR; i += 64) {
-                        const int r = i / CPR, c = i % CPR;
-                        uint4* p = reinterpret_cast<uint4*>(qs + (r >> 7) * TILE + (c >> 3) * BLOCK + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4));
-                        uint4 x = *p;
-                        x.x ^= 0x80008000u; x.y ^= 0x80008000u; x.z ^= 0x80008000u; x.w ^= 0x80008000u;
-                        *p = x;
+                // a lane brings the same 16 bytes of every row that is its own, rows STEP apart
+                constexpr int CPR = D / 8, STEP = 64 / CPR;
+                const int c = t % CPR, r_first = w.tile * a.RU;
+                const int token_step = by_share(a, STEP), head_step = STEP - token_step * a.share;
+                int token = by_share(a, r_first + t / CPR), head = r_first + t / CPR - token * a.share;
+                const uint8_t* base = a.q + ((long long)w.s.first * a.ld_q + (long long)w.h * a.share * D + c * 8) * 2;
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    if (x * 128 < rows) {
+                        const uint32_t to_tile = smem_u32(qs) + x * TILE + (c >> 3) * BLOCK;
+#pragma unroll 4
+                        for (int r = t / CPR; r < 128; r += STEP) {
+                            const bool live = x * 128 + r < rows;
+                            const uint8_t* src = base + ((long long)token * a.ld_q + head * D) * 2;
+                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to_tile + r * 128 + (((c & 7) ^ (r & 7)) << 4)),
+                                         "l"(live ? src : a.q), "r"(live ? 16 : 0) : "memory");
+                            token += token_step;
+                            head += head_step;
+                            if (head >= a.share) { head -= a.share; ++token; }
+                        }
                     }
+                    asm volatile("cp.async.commit_group;" ::: "memory");
                 }
-                fence_proxy_async();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&s->q_full));
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    if (x == 0) asm volatile("cp.async.wait_group 1;" ::: "memory");
+                    else asm volatile("cp.async.wait_group 0;" ::: "memory");
+                    if (x * 128 >= rows) continue;
+                    if (g.negative) {                            // each lane turns what it has brought itself
+                        for (int r = t / CPR; r < 128; r += STEP) {
+                            uint4* p = reinterpret_cast<uint4*>(qs + x * TILE + (c >> 3) * BLOCK + r * 128 + (((c & 7) ^ (r & 7)) << 4));
+                            uint4 y = *p;
+                            y.x ^= 0x80008000u; y.y ^= 0x80008000u; y.z ^= 0x80008000u; y.w ^= 0x80008000u;
+                            *p = y;
+                        }
+                    }
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&s->q_full[x]));
+                }
                 for (int i = from; i < to; ++i) {
                     const int j = paged_tile_at(w.t, i) * KT;
                     if (++stage == g.stages) { stage = 0; ph ^= 1u; }
@@ -343,31 +443,46 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
             const int row = w.tile * a.RU + x * 128 + r;
             const PagedRow see = paged_row(a, w.s, row);
             float m = kNoMax, l = 0.f;                           // m: the exponent that weights are relative to, LIFT below the maximum it was taken from
-            bool begun = false;
-            for (int i = from; i < to; ++i) {
-                const int j = paged_tile_at(w.t, i) * KT;
-                if (!chunk_needs(a, v, j)) continue;
+            bool begun = false, whole = false;
+            int i = from, j = 0;
+            auto seek = [&]() {                                  // the next tile that takes part
+                for (; i < to; ++i) {
+                    j = paged_tile_at(w.t, i) * KT;
+                    if (chunk_needs(a, v, j)) break;
+                }
+                whole = chunk_whole(a, v, j);
+            };
+            seek();
+            while (i < to) {
                 if (!(ok = chunk_wait(s->s_full[x], s_ph, s, g.status))) break;
                 s_ph ^= 1u;
                 tc::fence_after();
                 uint32_t raw[KT];
 #pragma unroll
                 for (int c = 0; c < KT / 32; ++c) tc::ld32(t_s + c * 32, raw + c * 32);
+                const bool masked = !whole;
+                const int hi = see.hi - j, lo = see.lo - j, first_few = a.sinks - j;
+                ++i;
+                seek();
                 tc::wait_ld();
                 float (&f)[KT] = reinterpret_cast<float (&)[KT]>(raw);
-                if (!chunk_whole(a, v, j)) {
+                if (masked) {
 #pragma unroll
-                    for (int c = 0; c < KT; ++c)
-                        if (!paged_sees(a, see, j + c)) f[c] = kNoMax;
+                    for (int c = 0; c < KT; c += 32) {
+                        const uint32_t seen = bits_below(hi - c) & (~bits_below(lo - c) | bits_below(first_few - c));
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (!(seen >> e & 1u)) f[c + e] = kNoMax;
+                    }
                 }
                 float top[4] = {f[0], f[1], f[2], f[3]};
 #pragma unroll
-                for (int c = 4; c < KT; ++c) top[c & 3] = fmaxf(top[c & 3], f[c]);
-                const float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * scale2;
-                const bool first = m == kNoMax;
-                const bool move = now > m + 8.f + LIFT;          // also when there is no m yet
+                for (int c = 4; c < KT; c += 2) top[c / 2 & 3] = max3_nan(top[c / 2 & 3], f[c], f[c + 1]);
+                const float now = max_nan(max3_nan(top[0], top[1], top[2]), top[3]) * scale2;
+                const bool move = !(now <= m + (8.f + LIFT));    // also when there is no m yet, or a NaN
                 if (__any_sync(0xffffffffu, move)) {
                     const float before = m;
+                    const bool first = m == kNoMax;
                     if (move) m = now - LIFT;
                     if (begun && __any_sync(0xffffffffu, move && !first)) {
                         const float by = move && !first ? exp2_fast(before - m) : 1.f;
@@ -385,24 +500,35 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                 }
                 begun = true;
                 const float ref = m == kNoMax ? 0.f : m;
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                const f32x2 scale22 = pair(scale2, scale2), ref2 = pair(-ref, -ref);
+                f32x2 sum[2] = {pair(0.f, 0.f), pair(0.f, 0.f)};
 #pragma unroll
                 for (int c = 0; c < KT / 32; ++c) {
                     uint32_t p[16];
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        const float p0 = exp2_fast(fmaf(f[c * 32 + 2 * e], scale2, -ref)), p1 = exp2_fast(fmaf(f[c * 32 + 2 * e + 1], scale2, -ref));
-                        sum[e & 1] += p0;
-                        sum[2 + (e & 1)] += p1;
+                        const f32x2 y = fma2(pair(f[c * 32 + 2 * e], f[c * 32 + 2 * e + 1]), scale22, ref2);
+                        float p0, p1;
+                        if (e % 4 >= 4 - kChunkPoly) exp2_poly<LIFT != 0.f>(y, p0, p1);
+                        else {
+                            split(y, p0, p1);
+                            p0 = exp2_fast(p0);
+                            p1 = exp2_fast(p1);
+                        }
+                        sum[e & 1] = add2(sum[e & 1], pair(p0, p1));
                         p[e] = pack2<T>(p0, p1);
                     }
                     tc::st16(t_s + c * 16, p);
+                    if (c == KT / 64 - 1 || c == KT / 32 - 1) {  // half of the weights: their product may begin
+                        tc::wait_st();
+                        tc::fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(&s->p_full[x][c == KT / 32 - 1]));
+                    }
                 }
-                tc::wait_st();
-                tc::fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&s->p_full[x]));
-                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                float s0, s1;
+                split(add2(sum[0], sum[1]), s0, s1);
+                l += s0 + s1;
             }
             if (!ok) break;
             if (begun) {
@@ -413,6 +539,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
             const bool head = from == 0, tail = to == w.t.count;
             const bool mine = x * 128 + r < rows;
             const bool restore = begun && *(volatile int*)&s->found[unit & 3] == unit + 1;
+            const bool wide = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.ld_out * 2)) & 31) == 0;
             const size_t slot = (size_t)blockIdx.x * 2 + (head ? 1 : 0);
             const float inv = see.hi > 0 ? 1.f / l : 0.f;
             T* to_out = reinterpret_cast<T*>(a.out) + (mine ? paged_row_offset(a, w.s, w.h, row, a.ld_out) : 0);
@@ -446,10 +573,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                     for (int e = 0; e < 16; ++e)
                         p[e] = see.hi > 0 ? pack2<T>(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv) : 0u;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) reinterpret_cast<uint4*>(to_out + c * 32)[e] = make_uint4(p[4 * e], p[4 * e + 1], p[4 * e + 2], p[4 * e + 3]);
+                    for (int e = 0; e < 2; ++e) store32(to_out + c * 32 + e * 16, p + 8 * e, wide);
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) reinterpret_cast<uint4*>(to_part + c * 32)[e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                    for (int e = 0; e < 4; ++e) store32(to_part + c * 32 + e * 8, o + 8 * e, true);
                 }
             }
             if (mine && !(head && tail)) a.part_ml[slot * a.RU + x * 128 + r] = make_float2(m, l);
@@ -534,7 +661,7 @@ static coreinfer_status launch_chunk(ChunkArgs& g, const DeviceInfo& di, cudaStr
     coreinfer_status s = pool_map(&mk, g.a.c, g.a.c.pool[0], f16, g.box);
     if (s != COREINFER_OK || (s = pool_map(&mv, g.a.c, g.a.c.pool[1], f16, g.box)) != COREINFER_OK) return s;
     constexpr size_t TILE = D / 64 * 128 * 128;
-    const size_t fixed = 2 * TILE + sizeof(ChunkBars) + (size_t)(g.a.c.B + 1) * 8;
+    const size_t fixed = 2 * TILE + sizeof(ChunkBars) + (size_t)(g.a.c.B + 1) * 4;
     size_t stages = (smem_room(di, 0) - fixed) / TILE;
     g.stages = (int)(stages < kChunkMaxStages ? stages : kChunkMaxStages);
     const size_t smem = fixed + g.stages * TILE;

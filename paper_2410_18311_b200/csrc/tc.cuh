@@ -48,6 +48,14 @@ __device__ __forceinline__ void commit(uint32_t bar)
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 
+// True in one lane of the warp, which has to be converged.
+__device__ __forceinline__ bool elect()
+{
+    uint32_t one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one != 0;
+}
+
 // 32 lanes x 32 consecutive columns: thread i of the warp has row (lane base + i).
 __device__ __forceinline__ void ld32(uint32_t taddr, uint32_t* r)
 {
