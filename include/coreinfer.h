@@ -634,7 +634,7 @@ coreinfer_status coreinfer_paged_append(const coreinfer_paged_cache* cache, cons
  *   out[r, head] = sum_j softmax_j( scale * q[r, head] . k_j ) v_j
  * where the token at position p sees the positions j <= p with  j > p - window  or  j < sinks  (window 0: all j <= p),
  * and `q_heads / kv_heads` consecutive query heads share a key head.  A token that sees no position gets zeros.
- * A NaN or infinity in a key or value reaches the tokens that see it, and no other.  Sums, maxima and the joins of partial
+ * A NaN or infinity in a key or value makes the outputs that see it NaN or infinite, and no other.  Sums, maxima and the joins of partial
  * results are fp32 in a fixed order (the same call on the same arrays gives the same bits).  The softmax weights enter the product with the
  * values in fp32 (fp32 caches), in the cache's type (more than 16 query rows per key head and sequence) or as two parts of it.
  *   q, out     device, row r at r * ld_q (ld_out) elements, [q_heads][head_dim] contiguous, in the cache's type, 16-byte

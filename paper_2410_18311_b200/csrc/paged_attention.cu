@@ -155,8 +155,6 @@ __global__ void __launch_bounds__(kSimpleThreads) paged_simple_kernel(const __gr
         for (int r = 0; r < RPT; ++r) {
             const int row = rg + r;
             if (row >= rows) continue;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[r][e] = paged_mend<T>(a, w, from, to, r0 + row, c + e, o[r][e], ls[row]);
             if (head && tail) {
                 const PagedRow see = paged_row(a, w.s, r0 + row);
                 const float l = ls[row];
@@ -165,7 +163,7 @@ __global__ void __launch_bounds__(kSimpleThreads) paged_simple_kernel(const __gr
                 for (int e = 0; e < 4; ++e) to_row[e] = from_f32<T>(see.hi > 0 ? o[r][e] / l : 0.f);
             } else {
                 const size_t slot = (size_t)blockIdx.x * 2 + (head ? 1 : 0);
-                *reinterpret_cast<float4*>(a.part_o + (slot * RU + row) * D + c) = make_float4(o[r][0], o[r][1], o[r][2], o[r][3]);
+                *reinterpret_cast<float4*>(a.part_o + slot * RU * D + (c * RU + row * 4)) = make_float4(o[r][0], o[r][1], o[r][2], o[r][3]);
                 if (c == 0) a.part_ml[slot * RU + row] = make_float2(ms[row], ls[row]);
             }
         }
@@ -184,15 +182,16 @@ __global__ void __launch_bounds__(kSimpleThreads) paged_simple_kernel(const __gr
 // Joins the pieces of a unit that is cut: block (x, y) the rows y of the unit whose first tile CTA x has.  The first piece is in
 // that CTA's second slot, the others in the first slots of the CTAs behind it.
 constexpr int kJoinThreads = 256;
+template <int D> constexpr int kJoinRows = kJoinThreads * 4 / D;         // eight rows of 32 quarters at head_dim 128
 template <typename T, int D>
 __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_constant__ PagedAttnArgs a)
 {
-    constexpr int CG = D / 4, ROWS = kJoinThreads / CG;
+    constexpr int ROWS = kJoinRows<D>;
     wait_for_stream();
     const PagedPiece p = a.pieces[blockIdx.x];
     if (p.last < 0) return;
     const PagedSeq s = paged_seq(a.c, p.b);
-    const int row = blockIdx.y * ROWS + threadIdx.x / CG, c = threadIdx.x % CG * 4;
+    const int row = blockIdx.y * ROWS + threadIdx.x % ROWS, c = threadIdx.x / ROWS * 4;
     const int global_row = p.tile * a.RU + row;
     if (row >= a.RU || global_row >= paged_rows(a, s)) return;
     const int first = blockIdx.x;
@@ -204,8 +203,8 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_c
 #pragma unroll 4
     for (int i = first; i <= p.last; ++i) {
         const float2 ml = a.part_ml[slot(i) * a.RU + row];
-        const float f = paged_join_factor(ml.x, ref);
-        const float4 x = *reinterpret_cast<const float4*>(a.part_o + (slot(i) * a.RU + row) * D + c);
+        const float f = exp2f(ml.x - ref);
+        const float4 x = *reinterpret_cast<const float4*>(a.part_o + slot(i) * a.RU * D + (c * a.RU + row * 4));
         l = fmaf(ml.y, f, l);
         // a piece in which the row sees nothing, or nothing but weights of 0, has nothing to add
         if (ml.x == -INFINITY) continue;
@@ -216,8 +215,11 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_c
     }
     const bool sees = paged_row(a, s, global_row).hi > 0;
     T* to = reinterpret_cast<T*>(a.out) + paged_row_offset(a, s, p.h, global_row, a.ld_out) + c;
+    T y[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) to[e] = from_f32<T>(sees ? o[e] / l : 0.f);
+    for (int e = 0; e < 4; ++e) y[e] = from_f32<T>(sees ? o[e] / l : 0.f);
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(y);
+    else *reinterpret_cast<uint2*>(to) = *reinterpret_cast<const uint2*>(y);
 }
 
 template <typename T, int D>
@@ -234,7 +236,7 @@ static coreinfer_status launch_simple(PagedAttnArgs& a, const DeviceInfo& di, cu
 template <typename T, int D>
 static coreinfer_status launch_join(const PagedAttnArgs& a, cudaStream_t st)
 {
-    constexpr int ROWS = kJoinThreads / (D / 4);
+    constexpr int ROWS = kJoinRows<D>;
     CI_CUDA(launch_overlapped(paged_join_kernel<T, D>, dim3(a.n_ctas, (a.RU + ROWS - 1) / ROWS), dim3(kJoinThreads), 0, st, a));
     return COREINFER_OK;
 }

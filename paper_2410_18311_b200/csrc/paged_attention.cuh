@@ -35,7 +35,7 @@ struct PagedAttnArgs {
     int n_ctas;
     PagedPiece* pieces;     // [n_ctas]
     float2* part_ml;        // [n_ctas][2][RU]: reference exponent (base 2) and sum
-    float* part_o;          // [n_ctas][2][RU][D]
+    float* part_o;          // [n_ctas][2][D / 4][RU][4]: rows side by side, as the threads that write them are
 };
 
 // The tensor-core form (paged_attention_tc.cu): 16-bit caches of head_dim 64 and 128.
@@ -213,16 +213,16 @@ __device__ __forceinline__ int paged_unit_rows(const PagedAttnArgs& a, const Pag
     const int left = paged_rows(a, w.s) - w.tile * a.RU;
     return left < a.RU ? left : a.RU;
 }
-// The infinities and NaN of one output that a row sees in the piece's tiles: in all of them, or in those that some row of the
-// unit sees in part only (the others' reach the sums by themselves).  hi_min, lo_max: of the unit's rows.
+// The infinities and NaN of one output that a row sees in the piece's tiles that some row of the unit (hi_min, lo_max: of its
+// rows) sees in part only.  There they were set to 0 for the product; in the other tiles they reach the sums by themselves.
 template <typename T>
-__device__ __noinline__ float paged_odd_sum(const PagedAttnArgs& a, const PagedWalk& w, bool all, int hi_min, int lo_max, int from, int to, int row, int d)
+__device__ __noinline__ float paged_odd_sum(const PagedAttnArgs& a, const PagedWalk& w, int hi_min, int lo_max, int from, int to, int row, int d)
 {
     const PagedRow see = paged_row(a, w.s, row);
     float sum = 0.f;
     for (int i = from; i < to; ++i) {
         const int j0 = paged_tile_at(w.t, i) * a.KT;
-        if (!all && j0 + a.KT <= hi_min && (j0 >= lo_max || j0 + a.KT <= a.sinks)) continue;
+        if (j0 + a.KT <= hi_min && (j0 >= lo_max || j0 + a.KT <= a.sinks)) continue;
         for (int j = j0; j < j0 + a.KT; ++j) {
             if (!paged_sees(a, see, j)) continue;
             const int page = paged_page(a.c, w.b, j);
@@ -233,18 +233,6 @@ __device__ __noinline__ float paged_odd_sum(const PagedAttnArgs& a, const PagedW
     }
     return sum;
 }
-// An output that came out NaN although its row's weights are numbers: a weight that was rounded to 0, or one of its two parts, met
-// an infinity.  It is the sum of the infinities if that is one.
-template <typename T>
-__device__ __forceinline__ float paged_mend(const PagedAttnArgs& a, const PagedWalk& w, int from, int to, int row, int d, float o, float l)
-{
-    if (!isnan(o) || isnan(l)) return o;
-    const float x = paged_odd_sum<T>(a, w, true, 0, 0, from, to, row, d);
-    return isinf(x) ? x : o;
-}
-// Factor of a piece's output when pieces are joined; not 0, so that an infinity stays one (what it adds otherwise is below 2^-100
-// of the values).
-__device__ __forceinline__ float paged_join_factor(float m, float ref) { return fmaxf(exp2f(m - ref), 1e-37f); }
 // Element offset of a row of a unit in q or out.
 __device__ __forceinline__ long long paged_row_offset(const PagedAttnArgs& a, const PagedSeq& s, int h, int row, long long ld)
 {

@@ -302,7 +302,7 @@ __global__ void __launch_bounds__(kFewThreads, D == 256 ? 1 : 2) paged_few_kerne
 #pragma unroll
             for (int y = 0; y < kFewWarps; ++y) {
                 const float2 st = stats[y * RU + r];
-                const float f = paged_join_factor(st.x, ref);
+                const float f = exp2_fast(st.x - ref);
                 sum = fmaf(st.y, f, sum);
                 const float4 part = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(smem + y * RING) + r * OP + d);
                 if (st.x != -INFINITY) {
@@ -313,9 +313,7 @@ __global__ void __launch_bounds__(kFewThreads, D == 256 ? 1 : 2) paged_few_kerne
                 }
             }
             if (restore)
-                for (int e = 0; e < 4; ++e) v[e] += paged_odd_sum<T>(a, w, false, low.hi, high.lo, from, to, r0 + r, d + e);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = paged_mend<T>(a, w, from, to, r0 + r, d + e, v[e], sum);
+                for (int e = 0; e < 4; ++e) v[e] += paged_odd_sum<T>(a, w, low.hi, high.lo, from, to, r0 + r, d + e);
             if (head && tail) {
                 const bool sees = paged_row(a, w.s, r0 + r).hi > 0;
                 const float inv = 1.f / sum;
@@ -323,7 +321,7 @@ __global__ void __launch_bounds__(kFewThreads, D == 256 ? 1 : 2) paged_few_kerne
                 if (!sees) packed = make_uint2(0u, 0u);
                 *reinterpret_cast<uint2*>(reinterpret_cast<T*>(a.out) + paged_row_offset(a, w.s, w.h, r0 + r, a.ld_out) + d) = packed;
             } else {
-                *reinterpret_cast<float4*>(a.part_o + (slot * RU + r) * D + d) = make_float4(v[0], v[1], v[2], v[3]);
+                *reinterpret_cast<float4*>(a.part_o + slot * RU * D + (d * RU + r * 4)) = make_float4(v[0], v[1], v[2], v[3]);
                 if (d == 0) a.part_ml[slot * RU + r] = make_float2(top, sum);
             }
         }

@@ -18,7 +18,7 @@
 // for the product, as tcgen05.mma takes both operands in one type: an error of half a step of each weight, which averages out to
 // about the rounding of the output; the sum l is of the weights before that.
 // A weight of 0 times a value that is not finite would be NaN, and positions that a row does not see, or that hold no token, may
-// hold anything: in tiles where that can happen warps 10 and 11 set what is not finite to 0, and at the unit's end the rows that do see such
+// hold anything: in tiles where that can happen the helpers set what is not finite to 0, and at the unit's end the rows that do see such
 // a value get it added.
 // Every wait is bounded: one that gives up sets the status word, and all roles leave their loops.
 #include "paged_attention.cuh"
@@ -28,7 +28,7 @@
 
 namespace coreinfer {
 
-constexpr int kChunkThreads = 384;
+constexpr int kChunkThreads = 640;
 constexpr int kChunkKT = kPagedChunkTile;
 constexpr int kChunkMaxStages = 8;
 constexpr long long kChunkWaitCycles = 3000000000LL;
@@ -45,7 +45,8 @@ struct ChunkArgs {
 
 struct ChunkBars {
     uint64_t full[kChunkMaxStages], empty[kChunkMaxStages], looked[kChunkMaxStages];
-    uint64_t s_full[2], p_full[2][2], o_full[2], q_full[2], q_empty;
+    uint64_t s_full[2], p_full[2], o_full[2], met[2], q_full[2], q_empty;
+    float row[2][2][128];   // by tile and half: a row's maximum of its 64 columns, at a unit's end its sum
     uint32_t tmem;
     int abort;
     int found[4];           // by unit modulo 4: number + 1 of a unit in which values were set to 0
@@ -60,6 +61,7 @@ __device__ __forceinline__ ChunkView chunk_view(const PagedAttnArgs& a, const Pa
 {
     ChunkView v;
     v.any = rows > x * 128;
+    v.lo_min = v.lo_max = v.hi_min = v.hi_max = 0;
     if (!v.any) return v;
     const int r0 = w.tile * a.RU + x * 128, r1 = w.tile * a.RU + (rows < x * 128 + 128 ? rows : x * 128 + 128) - 1;
     const PagedRow low = paged_row(a, w.s, r0), high = paged_row(a, w.s, r1);
@@ -143,6 +145,18 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c)
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
+// The maximum of 32 values in four parts; -infinity where a bit is not set.
+__device__ __forceinline__ void top32(float (&top)[4], const uint32_t* f)
+{
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) top[e / 2 & 3] = max3_nan(top[e / 2 & 3], __uint_as_float(f[e]), __uint_as_float(f[e + 1]));
+}
+__device__ __forceinline__ void mask32(uint32_t* f, uint32_t seen)
+{
+#pragma unroll
+    for (int e = 0; e < 32; ++e)
+        if (!(seen >> e & 1u)) f[e] = 0xff800000u;
+}
 // Bits 0 .. n - 1.
 __device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : (n >= 32 ? 0xffffffffu : (1u << n) - 1u); }
 
@@ -201,7 +215,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
         }
         for (int x = 0; x < 2; ++x) {
             mbar_init(smem_u32(&s->s_full[x]), 1);
-            for (int h = 0; h < 2; ++h) mbar_init(smem_u32(&s->p_full[x][h]), 4);
+            mbar_init(smem_u32(&s->p_full[x]), 8);
+            mbar_init(smem_u32(&s->met[x]), 8);
             mbar_init(smem_u32(&s->o_full[x]), 1);
             mbar_init(smem_u32(&s->q_full[x]), 2);
         }
@@ -210,7 +225,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
         for (int i = 0; i < 4; ++i) s->found[i] = 0;
         mbar_fence_init();
     }
-    if (warp == 9) tc::alloc(smem_u32(&s->tmem), 512);
+    if (warp == 17) tc::alloc(smem_u32(&s->tmem), 512);
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
@@ -220,9 +235,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
     const int total = paged_plan(a, at);
     if (tid == 0) a.pieces[blockIdx.x].last = -1;
 
-    if (warp >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-        if (warp == 8) {
+    if (warp >= 16) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        if (warp == 16) {
             // ------------------------------------------------------- tiles --
             int stage = 0;
             uint32_t ph = 0;
@@ -250,7 +265,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                     }
                 }
             }
-        } else if (warp == 9) {
+        } else if (warp == 17) {
             // ---------------------------------------------------- products --
             // The whole warp walks along, so that addresses and descriptors stay in uniform registers, and one lane issues.
             int stage = 0;                                       // of K(i)
@@ -311,17 +326,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
                         if (ok && chunk_needs(a, v[x], j)) {
+                            ok = chunk_wait(s->p_full[x], p_ph[x], s, g.status);
+                            tc::fence_after();
+                            if (ok && tc::elect()) {
 #pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                if (ok) ok = chunk_wait(s->p_full[x][h], p_ph[x], s, g.status);
-                                tc::fence_after();
-                                if (ok && tc::elect()) {
-#pragma unroll
-                                    for (int k = h * KT / 32; k < (h + 1) * KT / 32; ++k)
-                                        tc::mma_ts(tmem + 256 + x * 128, tmem + x * 128 + k * 8, val + k * (16 * 128 >> 4), IDESC_O, begun[x] || k > 0);
-                                }
-                                __syncwarp();
+                                for (int k = 0; k < KT / 16; ++k)
+                                    tc::mma_ts(tmem + 256 + x * 128, tmem + x * 128 + (k >> 2) * 64 + (k & 3) * 8, val + k * (16 * 128 >> 4), IDESC_O, begun[x] || k > 0);
                             }
+                            __syncwarp();
                             p_ph[x] ^= 1u;
                             begun[x] = true;
                         }
@@ -342,7 +354,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
             }
         } else {
             // ------------------------------------- queries, looks at values --
-            const int t = tid - 320;
+            const int t = tid - 576;
             int stage = 0, unit = 0;
             uint32_t ph = 0, q_ph = 0;
             bool ok = true;
@@ -401,6 +413,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                     if (!(ok = chunk_wait(s->full[stage], ph, s, g.status))) break;
                     if (chunk_look(a, va, vb, j)) {
                         uint4* p = reinterpret_cast<uint4*>(ring + (size_t)stage * TILE);
+                        const int hi = va.hi_max > vb.hi_max ? va.hi_max : vb.hi_max;
                         bool odd = false;
 #pragma unroll 4
                         for (int c = t; c < (int)(TILE / 16); c += 64) {
@@ -408,7 +421,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                             if (odd_pair<T>(x.x) || odd_pair<T>(x.y) || odd_pair<T>(x.z) || odd_pair<T>(x.w)) {
                                 x.x = without_odd<T>(x.x); x.y = without_odd<T>(x.y); x.z = without_odd<T>(x.z); x.w = without_odd<T>(x.w);
                                 p[c] = x;
-                                odd = true;
+                                const int at_j = j + (c >> 3 & 127);     // what no row sees is not missed
+                                odd = odd || (at_j < hi && (at_j >= va.lo_min || at_j < a.sinks));
                             }
                         }
                         if (odd) {
@@ -425,15 +439,28 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
         }
     } else {
         // -------------------------------------------------------- softmax --
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-        const int x = warp >> 2;
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+        const int x = warp >> 3, h = warp >> 2 & 1;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t t_s = tmem + lanes + x * 128, t_o = tmem + lanes + 256 + x * 128;
+        const uint32_t t_s = tmem + lanes + x * 128 + h * 64, t_o = tmem + lanes + 256 + x * 128 + h * (D / 2);
         const int r = (warp & 3) * 32 + lane;                    // row of the tile
-        const float scale2 = fmaxf(fabsf(a.scale2), 1e-30f);      // a scale of 0 times -infinity would be NaN
-        uint32_t s_ph = 0, o_ph = 0;
+        const float scale2 = fmaxf(fabsf(a.scale2), 1e-30f);     // a scale of 0 times -infinity would be NaN
+        float* mine_s = &s->row[x][h][r];
+        const volatile float* other_s = &s->row[x][h ^ 1][r];
+        uint32_t s_ph = 0, o_ph = 0, met_ph = 0;
         int unit = 0;
         bool ok = true;
+        // the eight warps of the row tile
+        auto meet_again = [&]() {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&s->met[x]));
+            met_ph ^= 1u;
+            return chunk_wait(s->met[x], met_ph ^ 1u, s, g.status);
+        };
+        auto meet = [&](float value) {
+            *mine_s = value;
+            return meet_again();
+        };
         PagedWalk w;
         for (w.begin(a, at, total, blockIdx.x); ok && w.more(); w.next(a, at)) {
             const int from = w.from(a), to = w.to(a);
@@ -443,42 +470,33 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
             const int row = w.tile * a.RU + x * 128 + r;
             const PagedRow see = paged_row(a, w.s, row);
             float m = kNoMax, l = 0.f;                           // m: the exponent that weights are relative to, LIFT below the maximum it was taken from
-            bool begun = false, whole = false;
-            int i = from, j = 0;
-            auto seek = [&]() {                                  // the next tile that takes part
-                for (; i < to; ++i) {
-                    j = paged_tile_at(w.t, i) * KT;
-                    if (chunk_needs(a, v, j)) break;
-                }
-                whole = chunk_whole(a, v, j);
-            };
-            seek();
-            while (i < to) {
+            bool begun = false;
+            for (int i = from; i < to; ++i) {
+                const int j = paged_tile_at(w.t, i) * KT;
+                if (!chunk_needs(a, v, j)) continue;
+                const bool masked = !chunk_whole(a, v, j);
                 if (!(ok = chunk_wait(s->s_full[x], s_ph, s, g.status))) break;
                 s_ph ^= 1u;
                 tc::fence_after();
-                uint32_t raw[KT];
-#pragma unroll
-                for (int c = 0; c < KT / 32; ++c) tc::ld32(t_s + c * 32, raw + c * 32);
-                const bool masked = !whole;
-                const int hi = see.hi - j, lo = see.lo - j, first_few = a.sinks - j;
-                ++i;
-                seek();
+                uint32_t f0[32], f1[32];
+                tc::ld32(t_s, f0);
+                tc::ld32(t_s + 32, f1);
                 tc::wait_ld();
-                float (&f)[KT] = reinterpret_cast<float (&)[KT]>(raw);
+                tc::settle32(f0);
+                tc::settle32(f1);
                 if (masked) {
-#pragma unroll
-                    for (int c = 0; c < KT; c += 32) {
-                        const uint32_t seen = bits_below(hi - c) & (~bits_below(lo - c) | bits_below(first_few - c));
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (!(seen >> e & 1u)) f[c + e] = kNoMax;
-                    }
+                    const int hi = see.hi - j - h * 64, lo = see.lo - j - h * 64, first_few = a.sinks - j - h * 64;
+                    mask32(f0, bits_below(hi) & (~bits_below(lo) | bits_below(first_few)));
+                    mask32(f1, bits_below(hi - 32) & (~bits_below(lo - 32) | bits_below(first_few - 32)));
                 }
-                float top[4] = {f[0], f[1], f[2], f[3]};
-#pragma unroll
-                for (int c = 4; c < KT; c += 2) top[c / 2 & 3] = max3_nan(top[c / 2 & 3], f[c], f[c + 1]);
-                const float now = max_nan(max3_nan(top[0], top[1], top[2]), top[3]) * scale2;
+                float top[4] = {kNoMax, kNoMax, kNoMax, kNoMax};
+                top32(top, f0);
+                top32(top, f1);
+                // the other 64 columns are another warp's; what it reads here it has read before it hands its weights over, and the next
+                // scores come behind that
+                const float half_top = max_nan(max3_nan(top[0], top[1], top[2]), top[3]);
+                if (!(ok = meet(half_top))) break;
+                const float now = max_nan(half_top, *other_s) * scale2;
                 const bool move = !(now <= m + (8.f + LIFT));    // also when there is no m yet, or a NaN
                 if (__any_sync(0xffffffffu, move)) {
                     const float before = m;
@@ -487,14 +505,15 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                     if (begun && __any_sync(0xffffffffu, move && !first)) {
                         const float by = move && !first ? exp2_fast(before - m) : 1.f;
                         l *= by;
-#pragma unroll
-                        for (int c = 0; c < D / 32; ++c) {
-                            uint32_t o[32];
-                            tc::ld32(t_o + c * 32, o);
+#pragma unroll 1
+                        for (int c = 0; c < D / 32; ++c) {       // this warp's half of the columns
+                            uint32_t o[16];
+                            tc::ld16(t_o + c * 16, o);
                             tc::wait_ld();
+                            tc::settle16(o);
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
-                            tc::st32(t_o + c * 32, o);
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
+                            tc::st16(t_o + c * 16, o);
                         }
                     }
                 }
@@ -502,12 +521,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                 const float ref = m == kNoMax ? 0.f : m;
                 const f32x2 scale22 = pair(scale2, scale2), ref2 = pair(-ref, -ref);
                 f32x2 sum[2] = {pair(0.f, 0.f), pair(0.f, 0.f)};
-#pragma unroll
-                for (int c = 0; c < KT / 32; ++c) {
+                auto weights = [&](const uint32_t* f, uint32_t to) {
                     uint32_t p[16];
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        const f32x2 y = fma2(pair(f[c * 32 + 2 * e], f[c * 32 + 2 * e + 1]), scale22, ref2);
+                        const f32x2 y = fma2(pair(__uint_as_float(f[2 * e]), __uint_as_float(f[2 * e + 1])), scale22, ref2);
                         float p0, p1;
                         if (e % 4 >= 4 - kChunkPoly) exp2_poly<LIFT != 0.f>(y, p0, p1);
                         else {
@@ -518,14 +536,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                         sum[e & 1] = add2(sum[e & 1], pair(p0, p1));
                         p[e] = pack2<T>(p0, p1);
                     }
-                    tc::st16(t_s + c * 16, p);
-                    if (c == KT / 64 - 1 || c == KT / 32 - 1) {  // half of the weights: their product may begin
-                        tc::wait_st();
-                        tc::fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(smem_u32(&s->p_full[x][c == KT / 32 - 1]));
-                    }
-                }
+                    tc::st16(to, p);
+                };
+                weights(f0, t_s);
+                weights(f1, t_s + 16);
+                tc::wait_st();
+                tc::fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&s->p_full[x]));
                 float s0, s1;
                 split(add2(sum[0], sum[1]), s0, s1);
                 l += s0 + s1;
@@ -535,6 +553,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                 if (!(ok = chunk_wait(s->o_full[x], o_ph, s, g.status))) break;
                 o_ph ^= 1u;
                 tc::fence_after();
+                if (!(ok = meet(l))) break;
+                const float other = *other_s;
+                if (!(ok = meet_again())) break;                 // before the next unit's maxima take its place
+                l = h == 0 ? l + other : other + l;              // the same bits in both
             }
             const bool head = from == 0, tail = to == w.t.count;
             const bool mine = x * 128 + r < rows;
@@ -542,44 +564,54 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
             const bool wide = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.ld_out * 2)) & 31) == 0;
             const size_t slot = (size_t)blockIdx.x * 2 + (head ? 1 : 0);
             const float inv = see.hi > 0 ? 1.f / l : 0.f;
-            T* to_out = reinterpret_cast<T*>(a.out) + (mine ? paged_row_offset(a, w.s, w.h, row, a.ld_out) : 0);
-            float* to_part = a.part_o + (slot * a.RU + x * 128 + r) * D;
-#pragma unroll 1
-            for (int c = 0; c < D / 32; ++c) {
-                uint32_t o[32];
-                if (begun) {
-                    tc::ld32(t_o + c * 32, o);
-                    tc::wait_ld();
-                } else {
+            constexpr int C = D / 2;                             // this warp's columns
+            T* to_out = reinterpret_cast<T*>(a.out) + (mine ? paged_row_offset(a, w.s, w.h, row, a.ld_out) : 0) + h * C;
+            float* to_part = a.part_o + slot * a.RU * D + (size_t)h * C * a.RU + (x * 128 + r) * 4;
+            uint32_t o[C];
+            if (begun) {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = 0u;
-                }
-                float spoilt = 0.f;                              // NaN where an output is
+                for (int c = 0; c < C / 32; ++c) tc::ld32(t_o + c * 32, o + c * 32);
+                tc::wait_ld();
 #pragma unroll
-                for (int e = 0; e < 32; ++e) spoilt += __uint_as_float(o[e]) * 0.f;
-                if (mine && (restore || isnan(spoilt))) {
-                    const PagedRow low = paged_row(a, w.s, w.tile * a.RU), high = paged_row(a, w.s, w.tile * a.RU + rows - 1);
+                for (int c = 0; c < C / 32; ++c) tc::settle32(o + c * 32);
+            } else {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        float y = __uint_as_float(o[e]);
-                        if (restore) y += paged_odd_sum<T>(a, w, false, low.hi, high.lo, from, to, row, c * 32 + e);
-                        o[e] = __float_as_uint(paged_mend<T>(a, w, from, to, row, c * 32 + e, y, l));
-                    }
-                }
-                if (!mine) continue;
-                if (head && tail) {
-                    uint32_t p[16];
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        p[e] = see.hi > 0 ? pack2<T>(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv) : 0u;
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) store32(to_out + c * 32 + e * 16, p + 8 * e, wide);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) store32(to_part + c * 32 + e * 8, o + 8 * e, true);
-                }
+                for (int e = 0; e < C; ++e) o[e] = 0u;
             }
-            if (mine && !(head && tail)) a.part_ml[slot * a.RU + x * 128 + r] = make_float2(m, l);
+            if (restore) {                                       // rare: column by column in tensor memory, then read again
+                const PagedRow low = paged_row(a, w.s, w.tile * a.RU), high = paged_row(a, w.s, w.tile * a.RU + rows - 1);
+#pragma unroll 1
+                for (int e = 0; e < C; ++e) {
+                    uint32_t word;
+                    tc::ld1(t_o + e, word);
+                    float y = __uint_as_float(word);
+                    if (mine) y += paged_odd_sum<T>(a, w, low.hi, high.lo, from, to, row, h * C + e);
+                    __syncwarp();
+                    tc::st1(t_o + e, __float_as_uint(y));
+                }
+                tc::wait_st();
+#pragma unroll
+                for (int c = 0; c < C / 32; ++c) tc::ld32(t_o + c * 32, o + c * 32);
+                tc::wait_ld();
+#pragma unroll
+                for (int c = 0; c < C / 32; ++c) tc::settle32(o + c * 32);
+            }
+            if (!mine) {
+            } else if (head && tail) {
+#pragma unroll
+                for (int c = 0; c < C / 16; ++c) {
+                    uint32_t p[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        p[e] = see.hi > 0 ? pack2<T>(__uint_as_float(o[c * 16 + 2 * e]) * inv, __uint_as_float(o[c * 16 + 2 * e + 1]) * inv) : 0u;
+                    store32(to_out + c * 16, p, wide);
+                }
+            } else {
+#pragma unroll
+                for (int c = 0; c < C / 4; ++c)
+                    *reinterpret_cast<uint4*>(to_part + (size_t)c * a.RU * 4) = make_uint4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+                if (h == 0) a.part_ml[slot * a.RU + x * 128 + r] = make_float2(m, l);
+            }
             if (head && !tail && tid == 0) {
                 PagedPiece p;
                 p.b = w.b;
@@ -603,7 +635,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
         __syncthreads();
     }
     let_next_start();
-    if (warp == 9) {
+    if (warp == 17) {
         tc::fence_after();
         tc::dealloc(tmem, 512);
     }

@@ -58,11 +58,14 @@ def turn(x, positions, f, magnitude, interleaved, weight=None, eps=0.0):
 
 
 def check(got, want, tol, what=""):
-    """|got - want| within tol and one rounding to got's type; NaN where `want` is NaN, infinities equal."""
+    """|got - want| within tol and one rounding to got's type; NaN or infinite where `want` is, and NaN where that is NaN.  (An
+    infinity may come out NaN: a weight, or one of its two parts, may be 0.)"""
     got64, want = got.double().cpu(), want.cpu()
     fine = torch.isfinite(want)
-    assert torch.equal(torch.isnan(got64), torch.isnan(want)), what + ": NaN elsewhere"
-    assert torch.equal(got64[~fine & ~torch.isnan(want)], want[~fine & ~torch.isnan(want)]), what + ": infinities"
+    assert torch.equal(torch.isfinite(got64), fine), what + ": not finite elsewhere"
+    assert torch.isnan(got64[torch.isnan(want)]).all(), what + ": NaN"
+    left = ~fine & ~torch.isnan(want) & ~torch.isnan(got64)
+    assert torch.equal(got64[left], want[left]), what + ": infinities"
     bound = (tol.cpu() * 1.01 + OUT[got.dtype] * want.abs() + (2.0 ** -25 if got.dtype == torch.float16 else 1e-38))[fine]
     err = (got64 - want).abs()[fine]
     assert (err <= bound).all(), "%s: worst %.3g of the bound" % (what, (err / bound).max().item())
