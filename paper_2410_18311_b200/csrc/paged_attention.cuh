@@ -112,12 +112,26 @@ __device__ __forceinline__ bool paged_sees(const PagedAttnArgs& a, const PagedRo
 // multiple of 32).
 __device__ __forceinline__ int paged_plan(const PagedAttnArgs& a, int* at)
 {
-    for (int b = threadIdx.x; b < a.c.B; b += blockDim.x) {
-        const PagedSeq s = paged_seq(a.c, b);
+    const int lane = threadIdx.x & 31;
+    for (int b0 = (int)(threadIdx.x >> 5) * 32; b0 < a.c.B; b0 += blockDim.x) {
+        // a lane per sequence, and the warp together for those of many row tiles
+        const int b = b0 + lane;
+        PagedSeq s = {0, 0, 0};
+        if (b < a.c.B) s = paged_seq(a.c, b);
         const int tiles = paged_row_tiles(a, s);
         int w = 0;
-        for (int i = 0; i < tiles; ++i) w += a.cost + paged_tiles(a, s, i).count;
-        at[b + 1] = w * a.c.H;
+        if (tiles <= 2)
+            for (int i = 0; i < tiles; ++i) w += a.cost + paged_tiles(a, s, i).count;
+        for (unsigned many = __ballot_sync(0xffffffffu, tiles > 2); many; many &= many - 1) {
+            const int l = __ffs(many) - 1;
+            const PagedSeq one = {0, __shfl_sync(0xffffffffu, s.n, l), __shfl_sync(0xffffffffu, s.position, l)};
+            const int n = __shfl_sync(0xffffffffu, tiles, l);
+            int sum = 0;
+            for (int i = lane; i < n; i += 32) sum += a.cost + paged_tiles(a, one, i).count;
+            sum = __reduce_add_sync(0xffffffffu, sum);
+            if (lane == l) w = sum;
+        }
+        if (b < a.c.B) at[b + 1] = w * a.c.H;
     }
     if (threadIdx.x == 0) at[0] = 0;
     __syncthreads();
@@ -157,6 +171,7 @@ struct PagedWalk {
     PagedSeq s;
     PagedTiles t;
 
+    // Called by whole warps.
     __device__ __forceinline__ void begin(const PagedAttnArgs& a, const int* at, int total, int cta)
     {
         n = total < a.n_ctas ? total : a.n_ctas;
@@ -175,12 +190,26 @@ struct PagedWalk {
         const unsigned per_head = (unsigned)(at[b + 1] - at[b]) / (unsigned)a.c.H;
         h = (int)((unsigned)(x - at[b]) / per_head);
         base = at[b] + h * per_head;
-        tile = 0;
-        t = paged_tiles(a, s, 0);
-        while (base + a.cost + t.count <= x) {
-            base += a.cost + t.count;
-            t = paged_tiles(a, s, ++tile);
+        // the row tile, 32 at a time: a lane each
+        const int lane = threadIdx.x & 31, tiles = paged_row_tiles(a, s);
+        for (tile = 0;; tile += 32) {
+            int sum = tile + lane < tiles ? a.cost + paged_tiles(a, s, tile + lane).count : 0;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int left = __shfl_up_sync(0xffffffffu, sum, d);
+                if (lane >= d) sum += left;
+            }
+            const unsigned behind = __ballot_sync(0xffffffffu, base + sum > x);
+            if (behind) {
+                const int l = __ffs(behind) - 1;
+                const int before = __shfl_sync(0xffffffffu, sum, l > 0 ? l - 1 : 0);
+                tile += l;
+                if (l > 0) base += before;
+                break;
+            }
+            base += __shfl_sync(0xffffffffu, sum, 31);
         }
+        t = paged_tiles(a, s, tile);
     }
     __device__ __forceinline__ bool more() const { return x < end; }
     // Tiles from .. to - 1 of the unit are this piece's.

@@ -24,22 +24,23 @@ __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::aft
 __device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// D[tensor memory] (+)= A[shared] * B[shared], 16-bit operands of one type, fp32 sums.
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+// D[tensor memory] (+)= A[shared] * B[shared], 16-bit operands of one type, fp32 sums.  Operands by the low words of their
+// descriptors; the high word (desc_high) is the same for all.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t high, uint32_t idesc, uint32_t accumulate)
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        "{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 x, {%1, %3};\n\tmov.b64 y, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %4, p;\n\t}"
+        ::"r"(d), "r"(a), "r"(b), "r"(high), "r"(idesc), "r"(accumulate)
         : "memory");
 }
 // The same with A in tensor memory: row of lane, two 16-bit values per column.
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t high, uint32_t idesc, uint32_t accumulate)
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-        ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        "{\n\t.reg .pred p;\n\t.reg .b64 y;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 y, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %4, p;\n\t}"
+        ::"r"(d), "r"(a), "r"(b), "r"(high), "r"(idesc), "r"(accumulate)
         : "memory");
 }
 // One arrival when all MMAs that this thread has issued so far have completed.
@@ -134,14 +135,9 @@ __device__ __forceinline__ void copy_4d(uint32_t dst, const CUtensorMap* map, in
 
 // Descriptors of operands in rows of 128 swizzled bytes, eight rows 1024 bytes apart (what a copy with the 128-byte swizzle leaves).
 // K-major: rows are M or N, 64 values of K a row.  MN-major: rows are K, 64 values of N a row, `block` bytes to the next 64.
-__device__ __forceinline__ uint64_t desc_k(uint32_t addr)
-{
-    return (uint64_t)((addr >> 4) & 0x3fffu) | (1ull << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
-}
-__device__ __forceinline__ uint64_t desc_mn(uint32_t addr, uint32_t block)
-{
-    return (uint64_t)((addr >> 4) & 0x3fffu) | ((uint64_t)(block >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
-}
+constexpr uint32_t desc_high = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_k(uint32_t addr) { return ((addr >> 4) & 0x3fffu) | (1u << 16); }
+__device__ __forceinline__ uint32_t desc_mn(uint32_t addr, uint32_t block) { return ((addr >> 4) & 0x3fffu) | ((block >> 4) << 16); }
 // fp32 sums; operands fp16 (0) or bf16 (1); B MN-major or not; M rows, N columns.
 __host__ __device__ constexpr uint32_t idesc(uint32_t type, bool b_mn, uint32_t m, uint32_t n)
 {
