@@ -265,7 +265,7 @@ struct PagedForm {
 static PagedForm paged_form(coreinfer_dtype dtype, int D, int B, int share, int tokens)
 {
     if (dtype == COREINFER_F32) return {kFormSimple, kSimpleRows, kSimpleTile, 2 * 148};
-    if (D <= 128 && (long long)tokens * share > 16LL * B) return {kFormChunk, kPagedChunkRows, kPagedChunkTile, kPagedChunkCtas};
+    if ((long long)tokens * share > 16LL * B) return {kFormChunk, paged_chunk_rows(D), kPagedChunkTile, kPagedChunkCtas};
     const PagedFewShape few = paged_few_shape(D, (int)((long long)tokens * share / B > 8 ? 16 : (tokens <= B ? share : 16)));
     return {kFormFew, few.RU, few.KT, few.ctas};
 }

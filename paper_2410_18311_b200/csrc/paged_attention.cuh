@@ -38,8 +38,8 @@ struct PagedAttnArgs {
     float* part_o;          // [n_ctas][2][D / 4][RU][4]: rows side by side, as the threads that write them are
 };
 
-// The tensor-core form (paged_attention_tc.cu): 16-bit caches of head_dim 64 and 128.
-constexpr int kPagedChunkRows = 256;
+// The tensor-core form (paged_attention_tc.cu): 16-bit caches.
+static inline int paged_chunk_rows(int head_dim) { return head_dim == 256 ? 128 : 256; }
 constexpr int kPagedChunkTile = 128;
 constexpr int kPagedChunkCtas = 148;
 coreinfer_status paged_chunk(PagedAttnArgs& a, bool f16, unsigned* status, const DeviceInfo& di, cudaStream_t st);

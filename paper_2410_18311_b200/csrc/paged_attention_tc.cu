@@ -5,14 +5,15 @@
 // softmax the other is in its products.
 //
 // One persistent CTA per SM; a unit is 256 query rows of one sequence and key head, as two tiles A and B of 128 that share every
-// tile of 128 positions.
-//   warp 8      brings key and value tiles into a ring by tensor copies, a page (or 128 slots of it) a box; pages that are none
-//               lie outside the map and are filled with zeros
-//   warp 9      issues  S = Q K^T  into tensor memory, and  O += P V  with P from tensor memory, in the order
-//               PV_A(i) S_A(i+1) PV_B(i) S_B(i+1)
-//   warps 0..3  softmax of A, a thread a row: S from tensor memory, P back over it in 16 bits, running maximum and sum in registers;
-//   warps 4..7  the same for B; both write their rows out at the end of a unit
-//   warps 10,11 bring the next unit's queries, and look through value tiles in which some row does not see some position
+// tile of 128 positions (head_dim 256: one tile of 128 rows, whose O takes half of tensor memory).
+//   warps 0..7   softmax of A, two threads a row with 64 columns each (they exchange their maxima through shared memory): S from tensor memory, P back
+//   warps 8..15  over it in 16 bits, maximum and sum in registers; the same for B.  They write their rows out at the end of a unit
+//   warp 16      brings key and value tiles into a ring by tensor copies, a page (or 128 slots of it) a box; pages that are none
+//                lie outside the map and are filled with zeros
+//   warp 17      one lane issues  S = Q K^T  into tensor memory, and  O += P V  with P from tensor memory, in the order
+//                PV_A(i) S_A(i+1) PV_B(i) S_B(i+1)
+//   warps 18,19  bring the next unit's queries (by tensor copies where whole tokens fill a tile), and look through value tiles in which
+//                some row does not see some position
 // The running maximum is moved, and O rescaled, only when a row exceeds it by 2^8 (a factor that cancels in O / l): P then stays below
 // 2^8, and in fp16 it is raised by 2^7 so that weights keep 11 bits down to 2^-21 of the largest.  P is rounded to the cache's type
 // for the product, as tcgen05.mma takes both operands in one type: an error of half a step of each weight, which averages out to
@@ -33,13 +34,18 @@ constexpr int kChunkKT = kPagedChunkTile;
 constexpr int kChunkMaxStages = 8;
 constexpr long long kChunkWaitCycles = 3000000000LL;
 constexpr float kNoMax = -INFINITY;
-constexpr int kChunkPoly = 0;        // of four pairs of exponentials, those that are formed on the FMA pipe
+// Of four pairs of exponentials, those that are formed on the FMA pipe: where head_dim is 64 the products take half as long and the exponentials
+// are what is waited for (batch of windows 160 -> 151 us with one of four; head_dim 128 560 and 564 us).
+template <int D> constexpr int kChunkPoly = D == 64 ? 1 : 0;
+// Row tiles of a unit: O takes head_dim columns of tensor memory for each, beside 128 of S.
+template <int D> constexpr int kChunkPipes = D == 256 ? 1 : 2;
 
 struct ChunkArgs {
     PagedAttnArgs a;
-    int stages;
+    int k_stages, v_stages; // rings of key and of value tiles
     int box;                // slots of a tensor copy
     int negative;           // scale below 0: the queries' signs are turned
+    int map_q;              // queries come by tensor copies
     unsigned* status;
 };
 
@@ -206,6 +212,7 @@ __device__ __forceinline__ void exp2_poly(f32x2 x, float& a, float& b)
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                                                                        const __grid_constant__ CUtensorMap map_q,
                                                                         const __grid_constant__ ChunkArgs g)
 {
     constexpr int KT = kChunkKT;
@@ -216,16 +223,20 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
     constexpr uint32_t IDESC_S = tc::idesc(TYPE, false, 128, KT);
     constexpr uint32_t IDESC_O = tc::idesc(TYPE, true, 128, D);
     constexpr float LIFT = std::is_same<T, __half>::value ? 7.f : 0.f;
+    constexpr int PIPES = kChunkPipes<D>;
     const PagedAttnArgs& a = g.a;
     extern __shared__ __align__(1024) uint8_t smem[];
-    uint8_t* qs = smem;                              // [2][BLOCKS][128 rows][128 bytes]
-    uint8_t* ring = smem + 2 * TILE;                 // [stages][BLOCKS][128 positions][128 bytes]
-    ChunkBars* s = reinterpret_cast<ChunkBars*>(ring + (size_t)g.stages * TILE);
+    uint8_t* qs = smem;                              // [PIPES][BLOCKS][128 rows][128 bytes]
+    // Two rings [stages][BLOCKS][128 positions][128 bytes], of keys and of values: copies may land out of their order, and who waits for value
+    // tiles alone must not take a phase of its barrier that a key tile ended for its own.
+    uint8_t* ring = smem + PIPES * TILE;
+    const int stages = g.k_stages + g.v_stages;
+    ChunkBars* s = reinterpret_cast<ChunkBars*>(ring + (size_t)stages * TILE);
     int* at = reinterpret_cast<int*>(s + 1);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
     if (tid == 0) {
-        for (int i = 0; i < g.stages; ++i) {
+        for (int i = 0; i < stages; ++i) {
             mbar_init(smem_u32(&s->full[i]), 1);
             mbar_init(smem_u32(&s->empty[i]), 1);
             mbar_init(smem_u32(&s->looked[i]), 2);
@@ -256,8 +267,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (warp == 16) {
             // ------------------------------------------------------- tiles --
-            int stage = 0;
-            uint32_t ph = 0;
+            int at_stage[2] = {0, 0};
+            uint32_t phase[2] = {0, 0};
             bool ok = true;
             const int boxes = KT / g.box;
             PagedWalk w;
@@ -268,8 +279,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                     int page = lane < boxes ? paged_page(a.c, w.b, j) : 0;
                     if (page < 0) page = a.c.n_pages;            // outside the map: zeros
                     const int slot = j & ((1 << a.c.page_shift) - 1);
+#pragma unroll
                     for (int kv = 0; kv < 2; ++kv) {
-                        if (!(ok = chunk_wait(s->empty[stage], ph ^ 1u, s, g.status))) break;
+                        const int stage = at_stage[kv] + (kv ? g.k_stages : 0);
+                        if (!(ok = chunk_wait(s->empty[stage], phase[kv] ^ 1u, s, g.status))) break;
                         const uint32_t bar = smem_u32(&s->full[stage]);
                         if (lane == 0) mbar_arrive_expect_tx(bar, TILE);
                         __syncwarp();
@@ -278,7 +291,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
 #pragma unroll
                             for (int d = 0; d < BLOCKS; ++d) tc::copy_4d(dst + d * BLOCK, kv ? &map_v : &map_k, d * 64, slot, w.h, page, bar);
                         }
-                        if (++stage == g.stages) { stage = 0; ph ^= 1u; }
+                        if (++at_stage[kv] == (kv ? g.v_stages : g.k_stages)) { at_stage[kv] = 0; phase[kv] ^= 1u; }
                     }
                 }
             }
@@ -289,11 +302,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
             PagedWalk w;
             w.begin(a, at, total, blockIdx.x);
             if (tc::elect()) {
-                int stage = 0;                                   // of K(i), then V(i)
-                uint32_t ph = 0, looked = 0, p_ph[2] = {0, 0}, q_ph[2] = {0, 0};
+                int ks = 0, vs = 0;                              // stages of the next K and V
+                uint32_t k_ph = 0, v_ph = 0, p_ph[2] = {0, 0}, q_ph[2] = {0, 0};
                 bool ok = true;
-                const uint32_t q_desc = tc::desc_k(smem_u32(qs)), k_desc = tc::desc_k(smem_u32(ring)), v_desc = tc::desc_mn(smem_u32(ring), BLOCK);
-                auto advance = [&](int& st, uint32_t& p) { if (++st == g.stages) { st = 0; p ^= 1u; } };
+                const uint32_t q_desc = tc::desc_k(smem_u32(qs)), k_desc = tc::desc_k(smem_u32(ring)), v_desc = tc::desc_mn(smem_u32(ring + (size_t)g.k_stages * TILE), BLOCK);
+                auto next_k = [&]() { if (++ks == g.k_stages) { ks = 0; k_ph ^= 1u; } };
                 auto scores = [&](int x, int st) {
                     const uint32_t q = q_desc + x * (TILE >> 4), k = k_desc + st * (TILE >> 4);
 #pragma unroll
@@ -313,37 +326,33 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                     const int sink_tiles = sinks_end > w.t.first_tiles ? sinks_end : w.t.first_tiles;
                     bool begun[2] = {false, false};
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
+                    for (int x = 0; x < PIPES; ++x) {
                         const ChunkView v = chunk_view(a, w, rows, x);
                         first[x] = v.any ? (v.lo_min > 0 ? v.lo_min / KT : 0) - w.t.from + w.t.first_tiles : to;
                         end[x] = v.any ? (v.hi_max + KT - 1) / KT - w.t.from + w.t.first_tiles : 0;
                     }
                     auto needs = [&](int x, int i) { return i < end[x] && (i < sink_tiles || i >= first[x]); };
-                    if (!(ok = chunk_wait_one(s->full[stage], ph, s, g.status))) break;
+                    if (!(ok = chunk_wait_one(s->full[ks], k_ph, s, g.status))) break;
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
+                    for (int x = 0; x < PIPES; ++x) {
                         if (x * 128 >= rows) continue;
                         if (ok) ok = chunk_wait_one(s->q_full[x], q_ph[x], s, g.status);
                         q_ph[x] ^= 1u;
                         tc::fence_after();
-                        if (ok && needs(x, from)) scores(x, stage);
+                        if (ok && needs(x, from)) scores(x, ks);
                     }
                     if (!ok) break;
-                    tc::commit(smem_u32(&s->empty[stage]));
+                    tc::commit(smem_u32(&s->empty[ks]));
                     if (from + 1 == to) tc::commit(smem_u32(&s->q_empty));
-                    advance(stage, ph);
+                    next_k();
                     for (int i = from; i < to; ++i) {
-                        // stage: V(i), which is there when it has been looked at; the one behind it: K(i + 1)
-                        const int vs = stage;
-                        advance(stage, ph);
-                        const int ks = stage;
+                        // V(i), which is there when it has been looked at, and K(i + 1)
                         const bool last = i + 1 == to;
-                        if (!(ok = chunk_wait_one(s->looked[vs], looked >> vs & 1u, s, g.status))) break;
-                        looked ^= 1u << vs;
-                        if (!last && !(ok = chunk_wait_one(s->full[ks], ph, s, g.status))) break;
+                        if (!(ok = chunk_wait_one(s->looked[vs], v_ph, s, g.status))) break;
+                        if (!last && !(ok = chunk_wait_one(s->full[ks], k_ph, s, g.status))) break;
                         const uint32_t val = v_desc + vs * (TILE >> 4);
 #pragma unroll
-                        for (int x = 0; x < 2; ++x) {
+                        for (int x = 0; x < PIPES; ++x) {
                             if (ok && needs(x, i)) {
                                 ok = chunk_wait_one(s->p_full[x], p_ph[x], s, g.status);
                                 p_ph[x] ^= 1u;
@@ -365,11 +374,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                             if (ok && !last && needs(x, i + 1)) scores(x, ks);
                         }
                         if (!ok) break;
-                        tc::commit(smem_u32(&s->empty[vs]));
+                        tc::commit(smem_u32(&s->empty[g.k_stages + vs]));
+                        if (++vs == g.v_stages) { vs = 0; v_ph ^= 1u; }
                         if (!last) {
                             tc::commit(smem_u32(&s->empty[ks]));
                             if (i + 2 == to) tc::commit(smem_u32(&s->q_empty));
-                            advance(stage, ph);
+                            next_k();
                         }
                     }
                 }
@@ -378,7 +388,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
         } else {
             // ------------------------------------- queries, looks at values --
             const int t = tid - 576;
-            int stage = 0, unit = 0;
+            int stage = 0, unit = 0;                             // of value tiles
             uint32_t ph = 0, q_ph = 0;
             bool ok = true;
             PagedWalk w;
@@ -389,6 +399,16 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                 const ChunkView va = chunk_view(a, w, rows, 0), vb = chunk_view(a, w, rows, 1);
                 if (!(ok = chunk_wait(s->q_empty, q_ph ^ 1u, s, g.status))) break;
                 q_ph ^= 1u;
+                if (g.map_q) {                                   // rows of a tile: 128 / share tokens, each the heads of the group
+                    if (t < 2 && t * 128 < rows) {
+                        const uint32_t bar = smem_u32(&s->q_full[t]);
+                        mbar_arrive_expect_tx(bar, TILE);
+                        const int token = w.s.first + by_share(a, w.tile * a.RU + t * 128);
+#pragma unroll
+                        for (int d = 0; d < BLOCKS; ++d) tc::copy_3d(smem_u32(qs) + t * TILE + d * BLOCK, &map_q, d * 64, w.h * a.share, token, bar);
+                        mbar_arrive(bar);
+                    }
+                } else {
                 // a lane brings the same 16 bytes of every row that is its own, rows STEP apart
                 constexpr int CPR = D / 8, STEP = 64 / CPR;
                 const int c = t % CPR, r_first = w.tile * a.RU;
@@ -396,7 +416,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                 int token = by_share(a, r_first + t / CPR), head = r_first + t / CPR - token * a.share;
                 const uint8_t* base = a.q + ((long long)w.s.first * a.ld_q + (long long)w.h * a.share * D + c * 8) * 2;
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
+                for (int x = 0; x < PIPES; ++x) {
                     if (x * 128 < rows) {
                         const uint32_t to_tile = smem_u32(qs) + x * TILE + (c >> 3) * BLOCK;
 #pragma unroll 4
@@ -413,8 +433,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                     asm volatile("cp.async.commit_group;" ::: "memory");
                 }
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    if (x == 0) asm volatile("cp.async.wait_group 1;" ::: "memory");
+                for (int x = 0; x < PIPES; ++x) {
+                    if (x + 1 < PIPES) asm volatile("cp.async.wait_group 1;" ::: "memory");
                     else asm volatile("cp.async.wait_group 0;" ::: "memory");
                     if (x * 128 >= rows) continue;
                     if (g.negative) {                            // each lane turns what it has brought itself
@@ -429,13 +449,13 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                     __syncwarp();
                     if (lane == 0) mbar_arrive(smem_u32(&s->q_full[x]));
                 }
+                }
                 for (int i = from; i < to; ++i) {
                     const int j = paged_tile_at(w.t, i) * KT;
-                    if (++stage == g.stages) { stage = 0; ph ^= 1u; }
                     // each tile is waited for, so that neither the ring nor this warp is ever a round ahead of the other
-                    if (!(ok = chunk_wait(s->full[stage], ph, s, g.status))) break;
+                    if (!(ok = chunk_wait(s->full[g.k_stages + stage], ph, s, g.status))) break;
                     if (chunk_look(a, va, vb, j)) {
-                        uint4* p = reinterpret_cast<uint4*>(ring + (size_t)stage * TILE);
+                        uint4* p = reinterpret_cast<uint4*>(ring + (size_t)(g.k_stages + stage) * TILE);
                         const int hi = va.hi_max > vb.hi_max ? va.hi_max : vb.hi_max;
                         bool odd = false;
 #pragma unroll 4
@@ -455,7 +475,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                     }
                     __syncwarp();
                     if (lane == 0) mbar_arrive(smem_u32(&s->looked[stage]));
-                    if (++stage == g.stages) { stage = 0; ph ^= 1u; }
+                    if (++stage == g.v_stages) { stage = 0; ph ^= 1u; }
                 }
                 ++unit;
             }
@@ -463,7 +483,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
     } else {
         // -------------------------------------------------------- softmax --
         asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
-        const int x = warp >> 3, h = warp >> 2 & 1;
+        const int x = warp >> 3, h = warp >> 2 & 1;              // with one row tile a unit the second eight warps have no rows
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t t_s = tmem + lanes + x * 128 + h * 64, t_o = tmem + lanes + 256 + x * 128 + h * (D / 2);
         const int r = (warp & 3) * 32 + lane;                    // row of the tile
@@ -550,7 +570,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                     for (int e = 0; e < 16; ++e) {
                         const f32x2 y = fma2(pair(__uint_as_float(f[2 * e]), __uint_as_float(f[2 * e + 1])), scale22, ref2);
                         float p0, p1;
-                        if (e % 4 >= 4 - kChunkPoly) exp2_poly<LIFT != 0.f>(y, p0, p1);
+                        if (e % 4 >= 4 - kChunkPoly<D>) exp2_poly<LIFT != 0.f>(y, p0, p1);
                         else {
                             split(y, p0, p1);
                             p0 = exp2_fast(p0);
@@ -590,18 +610,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
             constexpr int C = D / 2;                             // this warp's columns
             T* to_out = reinterpret_cast<T*>(a.out) + (mine ? paged_row_offset(a, w.s, w.h, row, a.ld_out) : 0) + h * C;
             float* to_part = a.part_o + slot * a.RU * D + (size_t)h * C * a.RU + (x * 128 + r) * 4;
-            uint32_t o[C];
-            if (begun) {
-#pragma unroll
-                for (int c = 0; c < C / 32; ++c) tc::ld32(t_o + c * 32, o + c * 32);
-                tc::wait_ld();
-#pragma unroll
-                for (int c = 0; c < C / 32; ++c) tc::settle32(o + c * 32);
-            } else {
-#pragma unroll
-                for (int e = 0; e < C; ++e) o[e] = 0u;
-            }
-            if (restore) {                                       // rare: column by column in tensor memory, then read again
+            if (restore) {                                       // rare: column by column in tensor memory
                 const PagedRow low = paged_row(a, w.s, w.tile * a.RU), high = paged_row(a, w.s, w.tile * a.RU + rows - 1);
 #pragma unroll 1
                 for (int e = 0; e < C; ++e) {
@@ -613,28 +622,38 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                     tc::st1(t_o + e, __float_as_uint(y));
                 }
                 tc::wait_st();
-#pragma unroll
-                for (int c = 0; c < C / 32; ++c) tc::ld32(t_o + c * 32, o + c * 32);
-                tc::wait_ld();
-#pragma unroll
-                for (int c = 0; c < C / 32; ++c) tc::settle32(o + c * 32);
             }
-            if (!mine) {
-            } else if (head && tail) {
+            constexpr int S = C < 64 ? C : 64;                   // at a time
+#pragma unroll 1
+            for (int c0 = 0; c0 < C; c0 += S) {
+                uint32_t o[S];
+                if (begun) {
 #pragma unroll
-                for (int c = 0; c < C / 16; ++c) {
-                    uint32_t p[8];
+                    for (int c = 0; c < S / 32; ++c) tc::ld32(t_o + c0 + c * 32, o + c * 32);
+                    tc::wait_ld();
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        p[e] = see.hi > 0 ? pack2<T>(__uint_as_float(o[c * 16 + 2 * e]) * inv, __uint_as_float(o[c * 16 + 2 * e + 1]) * inv) : 0u;
-                    store32(to_out + c * 16, p, wide);
+                    for (int c = 0; c < S / 32; ++c) tc::settle32(o + c * 32);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < S; ++e) o[e] = 0u;
                 }
-            } else {
+                if (!mine) {
+                } else if (head && tail) {
 #pragma unroll
-                for (int c = 0; c < C / 4; ++c)
-                    *reinterpret_cast<uint4*>(to_part + (size_t)c * a.RU * 4) = make_uint4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
-                if (h == 0) a.part_ml[slot * a.RU + x * 128 + r] = make_float2(m, l);
+                    for (int c = 0; c < S / 16; ++c) {
+                        uint32_t p[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            p[e] = see.hi > 0 ? pack2<T>(__uint_as_float(o[c * 16 + 2 * e]) * inv, __uint_as_float(o[c * 16 + 2 * e + 1]) * inv) : 0u;
+                        store32(to_out + c0 + c * 16, p, wide);
+                    }
+                } else {
+#pragma unroll
+                    for (int c = 0; c < S / 4; ++c)
+                        *reinterpret_cast<uint4*>(to_part + (size_t)(c0 / 4 + c) * a.RU * 4) = make_uint4(o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+                }
             }
+            if (mine && !(head && tail) && h == 0) a.part_ml[slot * a.RU + x * 128 + r] = make_float2(m, l);
             if (head && !tail && tid == 0) {
                 PagedPiece p;
                 p.b = w.b;
@@ -706,20 +725,44 @@ static coreinfer_status pool_map(CUtensorMap* map, const Paged& c, const void* p
     return COREINFER_OK;
 }
 
+// Queries as [tokens][heads][head_dim], read in boxes of a key head's share of 128 / share tokens.
+static coreinfer_status query_map(CUtensorMap* map, const PagedAttnArgs& a, bool f16)
+{
+    EncodeTiledFn enc;
+    coreinfer_status s = encode_fn(&enc);
+    if (s != COREINFER_OK) return s;
+    const cuuint64_t dims[3] = {(cuuint64_t)a.c.D, (cuuint64_t)a.c.H * a.share, (cuuint64_t)a.c.tokens};
+    const cuuint64_t strides[2] = {(cuuint64_t)a.c.D * 2, (cuuint64_t)a.ld_q * 2};
+    const cuuint32_t boxes[3] = {64, (cuuint32_t)a.share, (cuuint32_t)(128 / a.share)};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    const CUresult r = enc(map, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<uint8_t*>(a.q), dims, strides, boxes, estr,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) CI_FAIL(COREINFER_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
+    return COREINFER_OK;
+}
+
 template <typename T, int D>
 static coreinfer_status launch_chunk(ChunkArgs& g, const DeviceInfo& di, cudaStream_t st)
 {
-    CUtensorMap mk, mv;
+    CUtensorMap mk, mv, mq;
     const bool f16 = std::is_same<T, __half>::value;
     const int page = 1 << g.a.c.page_shift;
     g.box = page < kChunkKT ? page : kChunkKT;
     coreinfer_status s = pool_map(&mk, g.a.c, g.a.c.pool[0], f16, g.box);
     if (s != COREINFER_OK || (s = pool_map(&mv, g.a.c, g.a.c.pool[1], f16, g.box)) != COREINFER_OK) return s;
+    // a box is whole tokens: shares that divide 128, and queries as they are
+    g.map_q = !g.negative && g.a.share <= 128 && (g.a.share & (g.a.share - 1)) == 0 && g.a.ld_q < 1LL << 38;
+    if (g.map_q) {
+        if ((s = query_map(&mq, g.a, f16)) != COREINFER_OK) return s;
+    } else mq = mk;
     constexpr size_t TILE = D / 64 * 128 * 128;
-    const size_t fixed = 2 * TILE + sizeof(ChunkBars) + (size_t)(g.a.c.B + 1) * 4;
+    const size_t fixed = kChunkPipes<D> * TILE + sizeof(ChunkBars) + (size_t)(g.a.c.B + 1) * 4;
     size_t stages = (smem_room(di, 0) - fixed) / TILE;
-    g.stages = (int)(stages < kChunkMaxStages ? stages : kChunkMaxStages);
-    const size_t smem = fixed + g.stages * TILE;
+    if (stages > kChunkMaxStages) stages = kChunkMaxStages;
+    g.k_stages = (int)stages / 2;
+    g.v_stages = (int)stages - g.k_stages;
+    const size_t smem = fixed + stages * TILE;
     if ((s = allow_smem<paged_chunk_kernel<T, D>>(di, 0)) != COREINFER_OK) return s;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(g.a.n_ctas);
@@ -731,8 +774,15 @@ static coreinfer_status launch_chunk(ChunkArgs& g, const DeviceInfo& di, cudaStr
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    CI_CUDA(cudaLaunchKernelEx(&cfg, paged_chunk_kernel<T, D>, mk, mv, (const ChunkArgs)g));
+    CI_CUDA(cudaLaunchKernelEx(&cfg, paged_chunk_kernel<T, D>, mk, mv, mq, (const ChunkArgs)g));
     return COREINFER_OK;
+}
+
+template <typename T>
+static coreinfer_status chunk_dim(ChunkArgs& g, const DeviceInfo& di, cudaStream_t st)
+{
+    if (g.a.c.D == 64) return launch_chunk<T, 64>(g, di, st);
+    return g.a.c.D == 128 ? launch_chunk<T, 128>(g, di, st) : launch_chunk<T, 256>(g, di, st);
 }
 
 coreinfer_status paged_chunk(PagedAttnArgs& a, bool f16, unsigned* status, const DeviceInfo& di, cudaStream_t st)
@@ -741,8 +791,7 @@ coreinfer_status paged_chunk(PagedAttnArgs& a, bool f16, unsigned* status, const
     g.a = a;
     g.negative = a.scale2 < 0.f;
     g.status = status;
-    if (f16) return a.c.D == 64 ? launch_chunk<__half, 64>(g, di, st) : launch_chunk<__half, 128>(g, di, st);
-    return a.c.D == 64 ? launch_chunk<__nv_bfloat16, 64>(g, di, st) : launch_chunk<__nv_bfloat16, 128>(g, di, st);
+    return f16 ? chunk_dim<__half>(g, di, st) : chunk_dim<__nv_bfloat16>(g, di, st);
 }
 
 }  // namespace coreinfer

@@ -133,6 +133,14 @@ __device__ __forceinline__ void copy_4d(uint32_t dst, const CUtensorMap* map, in
         : "memory");
 }
 
+__device__ __forceinline__ void copy_3d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+        ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+        : "memory");
+}
+
 // Descriptors of operands in rows of 128 swizzled bytes, eight rows 1024 bytes apart (what a copy with the 128-byte swizzle leaves).
 // K-major: rows are M or N, 64 values of K a row.  MN-major: rows are K, 64 values of N a row, `block` bytes to the next 64.
 constexpr uint32_t desc_high = (1024u >> 4) | (1u << 14) | (2u << 29);

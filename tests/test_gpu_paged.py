@@ -327,3 +327,35 @@ def test_attention_shared_pages_and_equal_sequences():
         out = attend(b, q, 0.125)
         assert (out[2 * T:].float() - out[:T].float()).abs().max() <= 2.0 ** -7 * out.abs().max().float()
         check_attention(b, q, out, 0.125)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_attention_long_prompts_again_and_again(D):
+    """Many launches one behind the other from a graph, keys and values beyond what the L2 holds nearby, so that tiles arrive in any order:
+    the same bits each time, and no wait gives up."""
+    require_gpu()
+    H, T, page, dt = 16, 4096, 128, torch.bfloat16
+    pages = 2 * T // page
+    states = []
+    for seed in range(3):
+        k, v = rand(pages, H, page, D, dt=dt, seed=seed), rand(pages, H, page, D, dt=dt, seed=seed + 9)
+        table = torch.randperm(pages, generator=torch.Generator().manual_seed(seed))[None].to(torch.int32).cuda()
+        length, start = torch.tensor([T], dtype=torch.int32).cuda(), torch.tensor([0, T], dtype=torch.int32).cuda()
+        cache = ci.make_paged_cache(k, v, table, length)
+        q = rand(T, H, D, dt=dt, seed=seed + 5)
+        ws = torch.empty(ci.coreinfer_paged_attention_workspace_bytes(cache, H, T), dtype=torch.uint8, device="cuda")
+        out = torch.empty_like(q)
+        ci.coreinfer_paged_attention(cache, start, q, D ** -0.5, out, ws)
+        states.append((cache, start, q, out, ws, out.clone(), k, v, table, length))
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        for cache, start, q, out, ws, *_ in states:
+            ci.coreinfer_paged_attention(cache, start, q, D ** -0.5, out, ws)
+    for _ in range(40):
+        for s in states:
+            s[3].zero_()
+        graph.replay()
+        for s in states:
+            ci.coreinfer_workspace_status(s[4])
+            assert torch.equal(s[3], s[5])
