@@ -261,13 +261,18 @@ enum PagedFormKind { kFormSimple, kFormFew, kFormChunk };
 struct PagedForm {
     PagedFormKind kind;
     int RU, KT, ctas;           // rows of a unit, positions of a tile, CTAs
+    int cost;                   // what starting and ending a unit takes, in tiles
 };
 static PagedForm paged_form(coreinfer_dtype dtype, int D, int B, int share, int tokens)
 {
-    if (dtype == COREINFER_F32) return {kFormSimple, kSimpleRows, kSimpleTile, 2 * 148};
-    if ((long long)tokens * share > 16LL * B) return {kFormChunk, paged_chunk_rows(D), kPagedChunkTile, kPagedChunkCtas};
-    const PagedFewShape few = paged_few_shape(D, (int)((long long)tokens * share / B > 8 ? 16 : (tokens <= B ? share : 16)));
-    return {kFormFew, few.RU, few.KT, few.ctas};
+    if (dtype == COREINFER_F32) return {kFormSimple, kSimpleRows, kSimpleTile, 2 * 148, 1};
+    // By the rows of a sequence and key head on the average.  head_dim 128: 16 rows a warp of the form for few spill registers (15 rows x 4096
+    // of 9000 positions 48.0 us, in the form for chunks 41.9; 16 x 100000 106 and 91 us); 64 and 256 carry them (12 rows of 64 x 4000 26.7 and 31.5 us,
+    // 16 of 256 41.0 and 47.2).  One row x 4000 of 128 75 and 101 us.
+    const long long rows = ((long long)tokens * share + B - 1) / B;
+    if (rows > (D == 128 ? 8 : 16)) return {kFormChunk, paged_chunk_rows(D), kPagedChunkTile, kPagedChunkCtas, 2};
+    const PagedFewShape few = paged_few_shape(D, (int)rows);
+    return {kFormFew, few.RU, few.KT, few.ctas, 2};
 }
 // A status word (16 bytes), the pieces, their exponents and sums, their outputs (from a multiple of 32 bytes on).
 static size_t paged_workspace(const PagedForm& f, int D)
@@ -332,7 +337,7 @@ coreinfer_status coreinfer_paged_attention(const coreinfer_paged_cache* cache, c
     a.scale2 = scale * kLog2e;
     a.RU = f.RU;
     a.KT = f.KT;
-    a.cost = 1;
+    a.cost = f.cost;
     a.n_ctas = f.ctas;
     unsigned* status = (unsigned*)workspace;
     uint8_t* ws = (uint8_t*)workspace + 16;

@@ -89,36 +89,6 @@ __global__ void __launch_bounds__(kFewThreads, D == 256 ? 1 : 2) paged_few_kerne
         const int rows = paged_unit_rows(a, w), r0 = w.tile * RU;
         const PagedRow low = paged_row(a, w.s, r0), high = paged_row(a, w.s, r0 + rows - 1);
         const bool one_token = low.hi == high.hi && low.lo == high.lo;
-        // queries as the second operand: row lane / 4 (of each group of eight), values 2 (lane % 4) and the next, and 8 further
-        uint32_t q[NT][KS][2];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int r = n * 8 + lane / 4;
-            const T* src = reinterpret_cast<const T*>(a.q) + (r < rows ? paged_row_offset(a, w.s, w.h, r0 + r, a.ld_q) : 0) + 2 * (lane & 3);
-#pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                q[n][k][0] = r < rows ? *reinterpret_cast<const uint32_t*>(src + k * 16) : 0u;
-                q[n][k][1] = r < rows ? *reinterpret_cast<const uint32_t*>(src + k * 16 + 8) : 0u;
-            }
-        }
-        // a lane's rows: 2 (lane % 4) and the next of each group
-        PagedRow see[NT][2];
-        float m[NT][2], l[NT][2], o[NT][KS][4];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int r = n * 8 + 2 * (lane & 3) + e;
-                see[n][e] = paged_row(a, w.s, r0 + (r < rows ? r : rows - 1));
-                m[n][e] = -INFINITY;
-                l[n][e] = 0.f;
-            }
-#pragma unroll
-            for (int k = 0; k < KS; ++k)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[n][k][e] = 0.f;
-        }
-
         const int steps = 2 * (to - from);
         // pages of the next 32 / HALVES tiles, a lane each
         int pages = 0;
@@ -153,6 +123,37 @@ __global__ void __launch_bounds__(kFewThreads, D == 256 ? 1 : 2) paged_few_kerne
         };
 #pragma unroll
         for (int x = 0; x < kFewStages - 1; ++x) issue(x, x);
+        // while the first slots are on their way:
+        // queries as the second operand: row lane / 4 (of each group of eight), values 2 (lane % 4) and the next, and 8 further
+        uint32_t q[NT][KS][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int r = n * 8 + lane / 4;
+            const T* src = reinterpret_cast<const T*>(a.q) + (r < rows ? paged_row_offset(a, w.s, w.h, r0 + r, a.ld_q) : 0) + 2 * (lane & 3);
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                q[n][k][0] = r < rows ? *reinterpret_cast<const uint32_t*>(src + k * 16) : 0u;
+                q[n][k][1] = r < rows ? *reinterpret_cast<const uint32_t*>(src + k * 16 + 8) : 0u;
+            }
+        }
+        // a lane's rows: 2 (lane % 4) and the next of each group
+        PagedRow see[NT][2];
+        float m[NT][2], l[NT][2], o[NT][KS][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int r = n * 8 + 2 * (lane & 3) + e;
+                see[n][e] = paged_row(a, w.s, r0 + (r < rows ? r : rows - 1));
+                m[n][e] = -INFINITY;
+                l[n][e] = 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[n][k][e] = 0.f;
+        }
+
         int stage = 0;
         bool odd = false;
         for (int i = from; i < to; ++i) {
@@ -350,7 +351,8 @@ static coreinfer_status launch_few(const PagedAttnArgs& a, const DeviceInfo& di,
 template <typename T, int D>
 static coreinfer_status few_rows(const PagedAttnArgs& a, const DeviceInfo& di, cudaStream_t st)
 {
-    return a.RU == 8 ? launch_few<T, D, 1>(a, di, st) : launch_few<T, D, 2>(a, di, st);
+    if constexpr (D == 128) return launch_few<T, D, 1>(a, di, st);           // more rows go to the form for chunks
+    else return a.RU == 8 ? launch_few<T, D, 1>(a, di, st) : launch_few<T, D, 2>(a, di, st);
 }
 template <typename T>
 static coreinfer_status few_dim(const PagedAttnArgs& a, const DeviceInfo& di, cudaStream_t st)

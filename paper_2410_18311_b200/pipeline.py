@@ -155,20 +155,183 @@ class KV4Cache:
             raise B.CoreInferError(B.ERR_INVALID_ARG, "tokens refused by a full cache: %s" % refused)
 
 
+class Rotary:
+    """Rotary positions of queries and keys (binding.ROPE_* scalings) and, where weights [head_dim] are given, the norms of
+    their heads that go before.  Keeps the table of frequencies on the device."""
+
+    def __init__(self, rot_dim, base=10000.0, scaling=B.ROPE_PLAIN, factor=1.0, original_context=0, interleaved=False, q_norm=None,
+                 k_norm=None, eps=1e-6, device="cuda"):
+        self.turns, magnitude = B.coreinfer_rope_frequencies(rot_dim, base, scaling, factor, original_context, device=device)
+        self.norms = q_norm, k_norm
+        self.rope = B.make_rope(self.turns, interleaved, magnitude, q_norm, k_norm, eps)
+
+    def __call__(self, positions, q, k, q_out=None, k_out=None, stream=None):
+        """q, k [tokens, heads, head_dim] to the positions int32 [tokens]; in place unless outputs are given."""
+        B.coreinfer_rope_apply(self.rope, positions, q, k, q if q_out is None else q_out, k if k_out is None else k_out, stream)
+
+
+class Pages:
+    """Which pages hold which sequence's tokens: the table and lengths that the caches of all layers share, and the packing of
+    a call's new tokens.  Pages are given out and taken back on the host."""
+
+    def __init__(self, batch, n_pages, page_size, max_tokens, device="cuda"):
+        self.page_size, self.n_pages = page_size, n_pages
+        self.max_pages = -(-max_tokens // page_size)
+        self.free = list(range(n_pages - 1, -1, -1))
+        self.held = [[] for _ in range(batch)]
+        self.tokens = [0] * batch
+        self.table = torch.full((batch, self.max_pages), -1, dtype=torch.int32, device=device)
+        self.length = torch.zeros(batch, dtype=torch.int32, device=device)
+        self.start = torch.zeros(batch + 1, dtype=torch.int32, device=device)
+
+    def reserve(self, tokens):
+        """Pages for that many tokens of every sequence (a number or one per sequence), so that a captured step may run on."""
+        want = [tokens] * len(self.held) if isinstance(tokens, int) else list(tokens)
+        need = [max(0, -(-n // self.page_size) - len(h)) for n, h in zip(want, self.held)]
+        if max(want) > self.max_pages * self.page_size or sum(need) > len(self.free):
+            raise B.CoreInferError(B.ERR_INVALID_ARG, "%d pages of %d left, %d needed for %s tokens; a sequence takes %d tokens at most"
+                                   % (len(self.free), self.n_pages, sum(need), want, self.max_pages * self.page_size))
+        for b, n in enumerate(need):
+            if n:
+                at = len(self.held[b])
+                self.held[b] += [self.free.pop() for _ in range(n)]
+                self.table[b, at:at + n] = torch.tensor(self.held[b][at:], dtype=torch.int32)
+
+    def add(self, new):
+        """Room for new[b] more tokens of each sequence, which the next calls bring: sets lengths and packing.  The total."""
+        self.reserve([t + n for t, n in zip(self.tokens, new)])
+        self.tokens = [t + n for t, n in zip(self.tokens, new)]
+        self.length.copy_(torch.tensor(self.tokens, dtype=torch.int32))
+        self.start.copy_(torch.tensor([sum(new[:b]) for b in range(len(new) + 1)], dtype=torch.int32))
+        return sum(new)
+
+    def decoding(self):
+        """Packing for one token of every sequence."""
+        self.start.copy_(torch.arange(len(self.held) + 1, dtype=torch.int32))
+
+    def one_more(self):
+        """Lengths for the next token of every sequence, on the device alone: what a captured step does in add()'s place, behind
+        decoding() and within what reserve() has given.  Replays are told to counted()."""
+        self.length += 1
+
+    def counted(self, steps):
+        """That many steps by one_more() have run."""
+        self.tokens = [t + steps for t in self.tokens]
+
+    def release(self, b):
+        """Sequence b has ended."""
+        self.free += reversed(self.held[b])
+        self.held[b], self.tokens[b] = [], 0
+        self.table[b] = -1
+        self.length[b] = 0
+
+
+class PagedKVCache:
+    """Keys and values of one layer in pages, and attention over them."""
+
+    def __init__(self, pages, q_heads, kv_heads, head_dim, dtype=torch.bfloat16, max_tokens=1):
+        dev = pages.table.device
+        self.pages, self.q_heads, self.head_dim = pages, q_heads, head_dim
+        self.k, self.v = (torch.zeros(pages.n_pages, kv_heads, pages.page_size, head_dim, dtype=dtype, device=dev) for _ in range(2))
+        self.cache = B.make_paged_cache(self.k, self.v, pages.table, pages.length)
+        self.ws = torch.empty(B.coreinfer_paged_attention_workspace_bytes(self.cache, q_heads, max_tokens), dtype=torch.uint8, device=dev)
+
+    def append(self, k, v, rotary=None, q=None, q_out=None, positions=None, stream=None):
+        B.coreinfer_paged_append(self.cache, self.pages.start, k, v, None if rotary is None else rotary.rope, positions, q, q_out, stream)
+
+    def attend(self, q, out, scale=None, window=0, sinks=0, stream=None):
+        need = B.coreinfer_paged_attention_workspace_bytes(self.cache, self.q_heads, q.shape[0])
+        if need > self.ws.numel():                           # more tokens than were announced
+            self.ws = torch.empty(need, dtype=torch.uint8, device=self.ws.device)
+        B.coreinfer_paged_attention(self.cache, self.pages.start, q, self.head_dim ** -0.5 if scale is None else scale, out, self.ws, window, sinks, stream)
+
+    def check(self, stream=None):
+        """Raises if a wait of the last attend() gave up (synchronises)."""
+        B.coreinfer_workspace_status(self.ws, stream)
+
+
+class CorePagedLayer:
+    """A decoder layer in 16 bits whose prompts arrive in pieces: rotary positions, a paged cache, attention with an optional window
+    and first tokens that stay visible, and the FFN, dense for the prompt's tokens and over the core neurons afterwards.  Counts of
+    the pieces add up (Eq. 3 is a sum over tokens); `fix_core()` ends the prompt: it takes the top beta of the counts and compacts.
+
+    weights as Core4Layer's; the residual stream is fp32, norms of the stream have no parameters and there are no biases.  All layers of a
+    model share one Pages.  `piece` and `step` take what Pages.add() announced; up to 8 sequences decode together."""
+
+    def __init__(self, cfg: Config, pages, q_heads, kv_heads, head_dim, weights, rotary=None, window=0, sinks=0, max_piece=512):
+        dev = pages.table.device
+        self.cfg, self.pages, self.heads, self.rotary, self.span = cfg, pages, (q_heads, kv_heads, head_dim), rotary, (window, sinks)
+        self.w_qkv, self.w_o, *self.w_ffn = weights
+        self.cache = PagedKVCache(pages, q_heads, kv_heads, head_dim, cfg.torch_dtype, max_piece)
+        self.kind = B.FFN_RELU_GATED if cfg.gated else B.FFN_RELU
+        self.K = B.coreinfer_count(cfg.beta, cfg.d_ff)
+        new = lambda *s, dtype=cfg.torch_dtype: torch.empty(s, dtype=dtype, device=dev)
+        self.counts, self.seen = torch.zeros(cfg.d_ff, dtype=torch.int32, device=dev), 0
+        self._f, self.core_idx = new(cfg.d_ff, dtype=torch.int32), new(self.K, dtype=torch.int32)
+        self.up, self.down = new(self.K, cfg.d_model), new(self.K, cfg.d_model)
+        self.gate = new(self.K, cfg.d_model) if cfg.gated else None
+        self._ffn_ws = new(B.coreinfer_ffn_decode_workspace_bytes(B.MAX_BATCH, cfg.d_model, self.K), dtype=torch.uint8)
+        self._act_ws = new(B.coreinfer_prefill_activations_workspace_bytes(), dtype=torch.uint8)
+
+    def _norm(self, h):
+        return torch.nn.functional.layer_norm(h, (self.cfg.d_model,)).to(self.cfg.torch_dtype)
+
+    def _attention(self, h):
+        Hq, H, D = self.heads
+        q, k, v = torch.nn.functional.linear(self._norm(h), self.w_qkv).split((Hq * D, H * D, H * D), dim=-1)
+        q, k, v = q.unflatten(-1, (Hq, D)), k.unflatten(-1, (H, D)), v.unflatten(-1, (H, D))
+        if self.rotary is None:
+            self.cache.append(k, v)
+        else:
+            self.cache.append(k, v, self.rotary, q, q)
+        ctx = torch.empty(h.shape[0], Hq, D, dtype=q.dtype, device=h.device)
+        self.cache.attend(q, ctx, None, *self.span)
+        h += torch.nn.functional.linear(ctx.flatten(1), self.w_o)
+
+    def piece(self, h):
+        """h [tokens, d] fp32, packed pieces of prompts: updated in place; their activations are counted."""
+        cfg = self.cfg
+        self._attention(h)
+        w_up, w_gate, w_down = self.w_ffn
+        x = self._norm(h)
+        act = torch.empty(h.shape[0], cfg.d_ff, dtype=cfg.torch_dtype, device=h.device)
+        B.coreinfer_prefill_activations(x, self.kind, w_up, w_gate, None, act, self._act_ws)
+        h += torch.nn.functional.linear(act, w_down)
+        ws = torch.empty(B.coreinfer_select_workspace_bytes(*act.shape), dtype=torch.uint8, device=h.device)
+        B.coreinfer_select_core(act, cfg.alpha, cfg.beta, self.core_idx, self._f, ws)
+        B.coreinfer_counts_add(self.counts, self._f)
+        self.seen += h.shape[0]
+
+    def fix_core(self):
+        """Deploys the top beta of the neurons by the counts of the pieces so far, which start anew."""
+        w_up, w_gate, w_down = self.w_ffn
+        B.coreinfer_top_by_count(self.counts, self.seen, self.cfg.beta, self.core_idx)
+        B.coreinfer_compact(w_up, w_gate, w_down, None, self.core_idx, self.K, self.up, self.gate, self.down, None)
+        self.counts.zero_()
+        self.seen = 0
+
+    def step(self, h):
+        """h [batch, d] fp32, one new token per sequence: updated in place."""
+        self._attention(h)
+        y = torch.empty_like(h)
+        B.coreinfer_ffn_decode(self._norm(h), self.kind, self.up, self.gate, self.down, None, None, y, self._ffn_ws)
+        h += y
+
+
 class Core4Layer:
     """A decoder layer whose decode step streams four bits per weight and per cached value: projections,
     attention over a cache that is kept within `budget` slots per head, and the FFN over the core neurons
     that the prompt selected.  Up to 8 sequences decode together and share the core set.
 
     weights = (w_qkv [(q_heads + 2 kv_heads) * head_dim, d], w_o [d, q_heads * head_dim], w_up, w_gate | None,
-    w_down) in the configuration's 16-bit type; the residual stream is fp32, norms have no parameters, there are no biases and no
-    rotary positions, and the FFN is ReLU or ReLU-gated as the configurations' are: a part of a decoder to build on rather than
+    w_down) in the configuration's 16-bit type; the residual stream is fp32, norms have no parameters, there are no biases, positions
+    are rotary where a Rotary is given and not marked otherwise, and the FFN is ReLU or ReLU-gated as the configurations' are: a part of a decoder to build on rather than
     one of the models.  The 16-bit weights stay for the next prompt beside their 4-bit copies, so four bits save the bytes of
     a decode step and not memory.  The prompt's dense products and the norms are torch's; a decode step runs in the library's kernels but for
     the norms and the two additions, and can be captured in a CUDA graph, which stays valid over later prompts."""
 
     def __init__(self, cfg: Config, batch, q_heads, kv_heads, head_dim, budget, weights, recent=32, first=4, max_prompt=None,
-                 group=128, cache_group=64, device="cuda"):
+                 group=128, cache_group=64, device="cuda", rotary=None):
         self.cfg, self.batch, self.heads = cfg, batch, (q_heads, kv_heads, head_dim)
         self.budget, self.recent, self.first, self.group = budget, recent, first, group
         self.w_qkv, self.w_o, *self.w_ffn = weights
@@ -181,6 +344,7 @@ class Core4Layer:
         new = lambda n, dtype=cfg.torch_dtype: torch.empty(batch, n, dtype=dtype, device=device)
         self._qkv, self._ctx = new(self.w_qkv.shape[0]), new(q_heads * head_dim)
         self._g, self._h, self._y = new(self.K), new(self.K), new(cfg.d_model, torch.float32)
+        self.rotary, self._position = rotary, torch.zeros(batch, dtype=torch.int32, device=device)   # of the next token
 
     def _norm(self, h):
         return torch.nn.functional.layer_norm(h, (self.cfg.d_model,)).to(self.cfg.torch_dtype)
@@ -198,6 +362,10 @@ class Core4Layer:
             raise B.CoreInferError(B.ERR_INVALID_ARG, "a prompt of shape %s: %d sequences of 1 to %d tokens were expected"
                                    % (tuple(h.shape), self.batch, self.cache.cache.capacity))
         q, k, v = self._split(torch.nn.functional.linear(self._norm(h), self.w_qkv), T)
+        if self.rotary is not None:
+            at = torch.arange(T, dtype=torch.int32, device=h.device).repeat(self.batch)
+            self.rotary(at, q.flatten(0, 1), k.flatten(0, 1))
+            self._position.fill_(T)
         self.cache.state.zero_()
         k_stored, v_stored = (torch.empty(self.batch, T, H, D, dtype=k.dtype, device=h.device) for _ in range(2))
         self.cache.append(k, v, k_stored, v_stored)
@@ -236,6 +404,9 @@ class Core4Layer:
         """h [batch, d] fp32, one new token per sequence: updated in place."""
         self.qkv(self._norm(h), self._qkv)
         q, k, v = self._split(self._qkv, 1)
+        if self.rotary is not None:
+            self.rotary(self._position, q.flatten(0, 1), k.flatten(0, 1))
+            self._position += 1
         self.cache.append(k, v)
         self.cache.attend(q, self._ctx.view_as(q))
         self.cache.evict(self.budget, self.recent, self.first)
