@@ -6,6 +6,10 @@
 // quarter of a turn goes to sincospif as an fp32 number of at most 1/4 (error 2e-8 in the angle, below fp32's rounding of
 // cosine and sine).
 //
+// Measured from a graph, three sets of inputs: 8191 tokens x 40 heads of 128 fp16, norms 35.7 us, 4700 GB/s; 16000 x 64 bf16 92 us, 5670; 6000 x 40
+// fp32, norms 45.8 us, 5370; 5000 tokens x 48 heads bf16 into pages 36 us, 3400 (a round of warps and a bit).
+// Two loads ahead and 32 warps an SM: four loads and 24 warps 39.5, 89, 67, 35; eight at once and none ahead 47.6, 108, 46.7, 41.
+//
 // What bounds it: bytes (each value read and written once), and a launch's latency where the tokens are few.  A warp takes a token, or a
 // part of its heads where the tokens are few, so that the cosines and sines are formed once per token (two pairs a lane, through
 // shared memory) and no warp waits for another.  Eight values a lane: a pair's other half is a shuffle away (of packed words) or in the
@@ -65,13 +69,13 @@ __device__ __forceinline__ int row_sequence(const Paged& c, int row)
 }
 
 template <typename T, int D, bool APPEND>
-__global__ void __launch_bounds__(32 * kRopeWarps, 3) rope_kernel(const __grid_constant__ RopeArgs a)
+__global__ void __launch_bounds__(32 * kRopeWarps, sizeof(T) == 2 ? 4 : 3) rope_kernel(const __grid_constant__ RopeArgs a)
 {
     constexpr int LPH = D / 8;                       // lanes per head
     constexpr int HPW = 32 / LPH;                    // heads at a time
     constexpr int E = sizeof(T);
     constexpr int WORDS = E / 2;                     // 16-byte words of eight values
-    constexpr int U = E == 2 ? 8 : 4;                // loads under way per lane
+    constexpr int U = 2;                             // loads a lane makes ahead of those it works on
     __shared__ float2 tables[kRopeWarps][kRopeMaxPairs];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, l = lane % LPH;
     float2* table = tables[warp];
@@ -149,13 +153,17 @@ __global__ void __launch_bounds__(32 * kRopeWarps, 3) rope_kernel(const __grid_c
                 sw[e] *= other;
             }
         }
-        for (int i = from; i < to; i += U) {
-            uint4 raw[U][WORDS];
+        uint4 raw[U][WORDS], ahead[U][WORDS];
+        auto fetch = [&](int i, uint4 (&to_regs)[U][WORDS]) {
 #pragma unroll
             for (int x = 0; x < U; ++x) {
                 const int h = (i + x) * HPW + lane / LPH;
-                if (i + x < to && h < heads) load8<T>(src + (long long)h * D * E, raw[x]);
+                if (i + x < to && h < heads) load8<T>(src + (long long)h * D * E, to_regs[x]);
             }
+        };
+        fetch(from, raw);
+        for (int i = from; i < to; i += U) {
+            fetch(i + U, ahead);
 #pragma unroll
             for (int x = 0; x < U; ++x) {
                 if (i + x >= to) break;
@@ -193,6 +201,10 @@ __global__ void __launch_bounds__(32 * kRopeWarps, 3) rope_kernel(const __grid_c
                 }
                 if (h < heads) store8<T>(dst + h * step, v);
             }
+#pragma unroll
+            for (int x = 0; x < U; ++x)
+#pragma unroll
+                for (int y = 0; y < WORDS; ++y) raw[x][y] = ahead[x][y];
         }
     };
     // heads that are stored as they are
@@ -236,8 +248,7 @@ static coreinfer_status launch_rope(RopeArgs& a, const DeviceInfo& di, cudaStrea
     constexpr int HPW = 256 / D;
     // a warp per token, or as many as bring 16 to every SM, but not more than there are rounds of heads
     const int rounds = (a.Hq + HPW - 1) / HPW + (APPEND ? 2 : 1) * ((a.H + HPW - 1) / HPW);
-    const long long wanted = 16LL * di.sm_count;
-    long long split = (wanted + a.tokens - 1) / a.tokens;
+    long long split = (16LL * di.sm_count + a.tokens - 1) / a.tokens;
     if (split > rounds) split = rounds;
     a.split = (int)split;
     const long long warps = a.tokens * split;
