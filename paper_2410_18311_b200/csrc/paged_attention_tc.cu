@@ -51,7 +51,7 @@ struct ChunkArgs {
 
 struct ChunkBars {
     uint64_t full[kChunkMaxStages], empty[kChunkMaxStages], looked[kChunkMaxStages];
-    uint64_t s_full[2], p_full[2], o_full[2], met[2], q_full[2], q_empty;
+    uint64_t s_full[2], p_full[2], o_full[2], q_full[2], q_empty;
     float row[2][2][128];   // by tile and half: a row's maximum of its 64 columns, at a unit's end its sum
     uint32_t tmem;
     int abort;
@@ -244,7 +244,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
         for (int x = 0; x < 2; ++x) {
             mbar_init(smem_u32(&s->s_full[x]), 1);
             mbar_init(smem_u32(&s->p_full[x]), 8);
-            mbar_init(smem_u32(&s->met[x]), 8);
             mbar_init(smem_u32(&s->o_full[x]), 1);
             mbar_init(smem_u32(&s->q_full[x]), 2);
         }
@@ -490,15 +489,15 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
         const float scale2 = fmaxf(fabsf(a.scale2), 1e-30f);     // a scale of 0 times -infinity would be NaN
         float* mine_s = &s->row[x][h][r];
         const volatile float* other_s = &s->row[x][h ^ 1][r];
-        uint32_t s_ph = 0, o_ph = 0, met_ph = 0;
+        uint32_t s_ph = 0, o_ph = 0;
         int unit = 0;
         bool ok = true;
-        // the eight warps of the row tile
+        // The eight warps of the row tile meet at a hardware barrier.  It cannot give up by itself, so no warp goes there once some wait
+        // has (the flag is looked at before), and one that leaves for that reason arrives once, for those that are there already.
         auto meet_again = [&]() {
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&s->met[x]));
-            met_ph ^= 1u;
-            return chunk_wait(s->met[x], met_ph ^ 1u, s, g.status);
+            if (__any_sync(0xffffffffu, *(volatile int*)&s->abort)) return false;
+            named_bar_sync(1 + x, 256);
+            return true;
         };
         auto meet = [&](float value) {
             *mine_s = value;
@@ -665,6 +664,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
             tc::fence_before();                                  // the reads of O come before the next unit's products
             if (to > from) ++unit;
         }
+        if (!ok) named_bar_arrive(1 + x, 256);
     }
 
     // Leaving: nothing may still be landing in this CTA's shared memory, and tensor memory goes back.
