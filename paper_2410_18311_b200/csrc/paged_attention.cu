@@ -257,7 +257,7 @@ static coreinfer_status pick_simple(PagedAttnArgs& a, const DeviceInfo& di, cuda
 static size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 
 // Which form a call takes, by what the host knows (the lengths of the batch's pieces are on the device).
-enum PagedFormKind { kFormSimple, kFormFew, kFormChunk };
+enum PagedFormKind { kFormSimple, kFormRows, kFormFew, kFormChunk };
 struct PagedForm {
     PagedFormKind kind;
     int RU, KT, ctas;           // rows of a unit, positions of a tile, CTAs
@@ -265,11 +265,12 @@ struct PagedForm {
 };
 static PagedForm paged_form(coreinfer_dtype dtype, int D, int B, int share, int tokens)
 {
+    const long long rows = ((long long)tokens * share + B - 1) / B;
+    if (dtype == COREINFER_F32 && rows <= kPagedRowsMost) return {kFormRows, rows == 1 ? 1 : kPagedRowsMost, paged_rows_tile(D), rows == 1 ? 2 * 148 : 148, 2};
     if (dtype == COREINFER_F32) return {kFormSimple, kSimpleRows, kSimpleTile, 2 * 148, 1};
     // By the rows of a sequence and key head on the average.  head_dim 128: 16 rows a warp of the form for few spill registers (15 rows x 4096
     // of 9000 positions 48.0 us, in the form for chunks 41.9; 16 x 100000 106 and 91 us); 64 and 256 carry them (12 rows of 64 x 4000 26.7 and 31.5 us,
     // 16 of 256 41.0 and 47.2).  One row x 4000 of 128 75 and 101 us.
-    const long long rows = ((long long)tokens * share + B - 1) / B;
     if (rows > (D == 128 ? 8 : 16)) return {kFormChunk, paged_chunk_rows(D), kPagedChunkTile, kPagedChunkCtas, 2};
     const PagedFewShape few = paged_few_shape(D, (int)rows);
     return {kFormFew, few.RU, few.KT, few.ctas, 2};
@@ -348,6 +349,7 @@ coreinfer_status coreinfer_paged_attention(const coreinfer_paged_cache* cache, c
     a.part_o = (float*)(((uintptr_t)ws + 31) & ~(uintptr_t)31);
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (f.kind == kFormChunk) s = paged_chunk(a, dtype == COREINFER_F16, status, di, st);
+    else if (f.kind == kFormRows) s = paged_rows_f32(a, di, st);
     else s = f.kind == kFormFew ? paged_few(a, dtype == COREINFER_F16, di, st) : pick_simple<float>(a, di, st);
     if (s != COREINFER_OK) return s;
     if (dtype == COREINFER_F32) return pick_join<float>(a, st);

@@ -64,6 +64,11 @@ static inline void paged_set_share(PagedAttnArgs& a, int share)
     a.share_shift = l - 1;
 }
 
+// The form for few rows of fp32 caches (paged_attention_rows.cu): up to four rows a unit.
+constexpr int kPagedRowsMost = 4;
+static inline int paged_rows_tile(int head_dim) { return 8192 / head_dim; }
+coreinfer_status paged_rows_f32(const PagedAttnArgs& a, const DeviceInfo& di, cudaStream_t st);
+
 #ifdef __CUDACC__
 
 __device__ __forceinline__ int by_share(const PagedAttnArgs& a, int n) { return a.share_mul ? (int)(__umulhi((unsigned)n, a.share_mul) >> a.share_shift) : n; }

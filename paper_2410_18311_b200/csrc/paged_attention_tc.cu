@@ -34,9 +34,6 @@ constexpr int kChunkKT = kPagedChunkTile;
 constexpr int kChunkMaxStages = 8;
 constexpr long long kChunkWaitCycles = 3000000000LL;
 constexpr float kNoMax = -INFINITY;
-// Of four pairs of exponentials, those that are formed on the FMA pipe: where head_dim is 64 the products take half as long and the exponentials
-// are what is waited for (batch of windows 160 -> 151 us with one of four; head_dim 128 560 and 564 us).
-template <int D> constexpr int kChunkPoly = D == 64 ? 1 : 0;
 // Row tiles of a unit: O takes head_dim columns of tensor memory for each, beside 128 of S.
 template <int D> constexpr int kChunkPipes = D == 256 ? 1 : 2;
 
@@ -182,33 +179,6 @@ __device__ __forceinline__ void mask32(uint32_t* f, uint32_t seen)
 }
 // Bits 0 .. n - 1.
 __device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : (n >= 32 ? 0xffffffffu : (1u << n) - 1u); }
-
-// Two powers of two on the FMA pipe:  x = n + f, n the nearest whole number (read from the last bits of x + 1.5 * 2^23), 2^f by the
-// polynomial of least relative error on [-1/2, 1/2] (Remez exchange; degree 3: 7.5e-5, a sixth of bf16's rounding step or less;
-// degree 4: 2.6e-6), n added to the exponent.  0 below 2^-125, -infinity included; x is at most 15.
-template <bool FINE>
-__device__ __forceinline__ void exp2_poly(f32x2 x, float& a, float& b)
-{
-    const f32x2 shifted = add2(x, pair(12582912.f, 12582912.f));
-    const f32x2 f = fma2(add2(shifted, pair(-12582912.f, -12582912.f)), pair(-1.f, -1.f), x);
-    f32x2 y;
-    if (FINE) {
-        y = fma2(f, pair(0.009570102f, 0.009570102f), pair(0.05591786f, 0.05591786f));
-        y = fma2(f, y, pair(0.24024744f, 0.24024744f));
-        y = fma2(f, y, pair(0.6931218f, 0.6931218f));
-        y = fma2(f, y, pair(0.9999993f, 0.9999993f));
-    } else {
-        y = fma2(f, pair(0.05517167f, 0.05517167f), pair(0.24261113f, 0.24261113f));
-        y = fma2(f, y, pair(0.69326097f, 0.69326097f));
-        y = fma2(f, y, pair(0.99992806f, 0.99992806f));
-    }
-    float n0, n1, x0, x1;
-    split(shifted, n0, n1);
-    split(x, x0, x1);
-    split(y, a, b);
-    a = x0 < -125.f ? 0.f : __uint_as_float(__float_as_uint(a) + (__float_as_uint(n0) << 23));
-    b = x1 < -125.f ? 0.f : __uint_as_float(__float_as_uint(b) + (__float_as_uint(n1) << 23));
-}
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
@@ -569,12 +539,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                     for (int e = 0; e < 16; ++e) {
                         const f32x2 y = fma2(pair(__uint_as_float(f[2 * e]), __uint_as_float(f[2 * e + 1])), scale22, ref2);
                         float p0, p1;
-                        if (e % 4 >= 4 - kChunkPoly<D>) exp2_poly<LIFT != 0.f>(y, p0, p1);
-                        else {
-                            split(y, p0, p1);
-                            p0 = exp2_fast(p0);
-                            p1 = exp2_fast(p1);
-                        }
+                        split(y, p0, p1);
+                        p0 = exp2_fast(p0);
+                        p1 = exp2_fast(p1);
                         sum[e & 1] = add2(sum[e & 1], pair(p0, p1));
                         p[e] = pack2<T>(p0, p1);
                     }

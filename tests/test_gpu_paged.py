@@ -206,6 +206,8 @@ ATTN = [
     ([1] * 40, [5 * i + 1 for i in range(40)], 2, 1, 64, 16, "tokens", 0, 0), ([3, 500, 1], [2000, 600, 700], 3, 2, 64, 16, "tokens", 256, 130),
     ([9], [9], 1, 71, 64, 16, "heads", 0, 0), ([384], [384], 2, 1, 128, 128, "heads", 0, 0), ([1], [20000], 1, 1, 128, 16, "heads", 0, 0),
     ([100], [5000], 1, 2, 128, 16, "tokens", 1000, 500), ([33], [4100], 1, 3, 256, 32, "tokens", 0, 0),
+    ([2, 1, 0], [5000, 3, 700], 2, 2, 128, 16, "heads", 0, 0), ([1, 1], [6000, 900], 2, 1, 256, 16, "tokens", 700, 20), ([4], [900], 3, 1, 64, 32, "heads", 300, 7),
+    ([3, 1], [2000, 1], 1, 1, 256, 64, "heads", 0, 0),
 ]
 
 
