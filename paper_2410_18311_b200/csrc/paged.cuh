@@ -4,6 +4,8 @@
 
 #include "quant4.cuh"
 
+#include <type_traits>
+
 namespace coreinfer {
 
 struct Paged {
@@ -80,6 +82,15 @@ static inline bool rows_fit(const void* p, long long ld, long long heads, int he
 
 #ifdef __CUDACC__
 
+// Two values rounded to 16 bits, the first in the lower half.
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi)
+{
+    uint32_t r;
+    if constexpr (sizeof(T) == 2 && std::is_same<T, __half>::value) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
 // A sequence's new rows first .. first + n - 1 and the position of the first of them (below 0 where length and
 // start do not fit together).
 struct PagedSeq {

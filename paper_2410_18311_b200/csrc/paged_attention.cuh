@@ -10,8 +10,6 @@
 
 #include "paged.cuh"
 
-#include <type_traits>
-
 namespace coreinfer {
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -274,14 +272,6 @@ __device__ __forceinline__ long long paged_row_offset(const PagedAttnArgs& a, co
     return (long long)(s.first + t) * ld + (long long)(h * a.share + row - t * a.share) * a.c.D;
 }
 
-template <typename T>
-__device__ __forceinline__ uint32_t pack2(float lo, float hi)
-{
-    uint32_t r;
-    if constexpr (sizeof(T) == 2 && std::is_same<T, __half>::value) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
 // Whether one of the two 16-bit values is an infinity or NaN.
 template <typename T>
 __device__ __forceinline__ bool odd_pair(uint32_t w)

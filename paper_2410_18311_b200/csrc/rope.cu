@@ -51,11 +51,10 @@ __device__ __forceinline__ void load8(const uint8_t* p, uint4 (&raw)[sizeof(T) /
 template <typename T>
 __device__ __forceinline__ void store8(uint8_t* p, const float (&x)[8])
 {
-    T v[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = from_f32<T>(x[e]);
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(p)[i] = reinterpret_cast<const uint4*>(v)[i];
+    if constexpr (sizeof(T) == 4) {
+        reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+        reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+    } else *reinterpret_cast<uint4*>(p) = make_uint4(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]), pack2<T>(x[4], x[5]), pack2<T>(x[6], x[7]));
 }
 
 // The sequence that a packed row belongs to, or -1: every lane of the warp counts its share of the starts at or before the row.
@@ -112,7 +111,6 @@ __global__ void __launch_bounds__(32 * kRopeWarps, sizeof(T) == 2 ? 4 : 3) rope_
     const bool turned = l * 8 < a.rot;
     const int half = a.rot / 16;                     // lanes of the first halves
     const int partner = a.interleaved || !turned ? l : (l < half ? l + half : l - half);
-    const uint32_t keep = turned ? 0xffffffffu : 0u; // what is not turned takes nothing from another value
 
     // heads [from, to) of rounds of queries or keys; kind 0 queries, 1 keys
     auto turn_heads = [&](int kind, int from, int to) {
@@ -169,22 +167,20 @@ __global__ void __launch_bounds__(32 * kRopeWarps, sizeof(T) == 2 ? 4 : 3) rope_
                 if (i + x >= to) break;
                 const int h = (i + x) * HPW + lane / LPH;
                 float v[8], o[8], r = 1.f;
-                uint4 other[WORDS];
-#pragma unroll
-                for (int y = 0; y < WORDS; ++y) {
-                    other[y] = raw[x][y];
-                    if (!a.interleaved && a.rot) {
-                        other[y].x = __shfl_sync(0xffffffffu, raw[x][y].x, partner, LPH) & keep;
-                        other[y].y = __shfl_sync(0xffffffffu, raw[x][y].y, partner, LPH) & keep;
-                        other[y].z = __shfl_sync(0xffffffffu, raw[x][y].z, partner, LPH) & keep;
-                        other[y].w = __shfl_sync(0xffffffffu, raw[x][y].w, partner, LPH) & keep;
-                    }
-                }
                 unpack8<T>(raw[x], v);
-                unpack8<T>(other, o);
                 if (a.interleaved) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) o[e] = turned ? v[e ^ 1] : 0.f;
+                    for (int e = 0; e < 8; ++e) o[e] = v[e ^ 1];
+                } else {
+                    uint4 other[WORDS];
+#pragma unroll
+                    for (int y = 0; y < WORDS; ++y) {
+                        other[y].x = __shfl_sync(0xffffffffu, raw[x][y].x, partner, LPH);
+                        other[y].y = __shfl_sync(0xffffffffu, raw[x][y].y, partner, LPH);
+                        other[y].z = __shfl_sync(0xffffffffu, raw[x][y].z, partner, LPH);
+                        other[y].w = __shfl_sync(0xffffffffu, raw[x][y].w, partner, LPH);
+                    }
+                    unpack8<T>(other, o);
                 }
                 if (weight) {
                     float sum = 0.f;
@@ -195,9 +191,14 @@ __global__ void __launch_bounds__(32 * kRopeWarps, sizeof(T) == 2 ? 4 : 3) rope_
                     r = __frsqrt_rn(sum * (1.f / D) + a.eps);
                 }
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    v[e] = fmaf(o[e], sw[e], v[e] * cw[e]);
-                    if (weight) v[e] *= r;
+                for (int e = 0; e < 8; ++e) v[e] *= cw[e];
+                if (turned) {                        // what is not takes nothing from another value, be it infinite
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = fmaf(o[e], sw[e], v[e]);
+                }
+                if (weight) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] *= r;
                 }
                 if (h < heads) store8<T>(dst + h * step, v);
             }
