@@ -636,13 +636,17 @@ coreinfer_status coreinfer_paged_append(const coreinfer_paged_cache* cache, cons
  * and `q_heads / kv_heads` consecutive query heads share a key head.  A token that sees no position gets zeros.
  * A NaN or infinity in a key or value makes the outputs that see it NaN or infinite, and no other.  Sums, maxima and the joins of partial
  * results are fp32 in a fixed order (the same call on the same arrays gives the same bits).  The softmax weights enter the product with the
- * values in fp32 (fp32 caches), in the cache's type (more than 16 query rows per key head and sequence) or as two parts of it.
+ * values in fp32 (fp32 caches), as two 16-bit parts (16-bit caches and few query rows, tokens * q_heads / kv_heads / batch up to 8 at
+ * head_dim 128 and 16 otherwise) or rounded to the cache's type (more rows).
  *   q, out     device, row r at r * ld_q (ld_out) elements, [q_heads][head_dim] contiguous, in the cache's type, 16-byte
  *              aligned, strides * element size multiples of 16
  *   workspace  device, 16-byte aligned, at least coreinfer_paged_attention_workspace_bytes() (0 on bad sizes), which covers
- *              every call with up to that many tokens on this cache.  Its contents need not be initialised and mean nothing
- *              afterwards; calls that may overlap need one each.
- * Errors: INVALID_ARG, UNSUPPORTED (as above; q_heads above 4096, tokens * q_heads above 2^29, window or sinks above 2^30), WORKSPACE, CUDA. */
+ *              every call with up to that many tokens on this cache.  Its contents need not be initialised; calls that may overlap
+ *              need one each.  Its first word is a status word readable with coreinfer_workspace_status: thread blocks wait for
+ *              their own copies and products only, every such wait is bounded, and one that gives up is recorded there (outputs
+ *              of that call are then undefined).
+ * Errors: INVALID_ARG, UNSUPPORTED (as above; q_heads above 4096, tokens * q_heads above 2^29, window or sinks above 2^30, a table
+ * and tokens that could make 2^31 tiles of work or more), WORKSPACE, CUDA. */
 size_t coreinfer_paged_attention_workspace_bytes(const coreinfer_paged_cache* cache, int32_t q_heads, int32_t tokens);
 
 coreinfer_status coreinfer_paged_attention(const coreinfer_paged_cache* cache, const int32_t* start, int32_t tokens,

@@ -1,5 +1,10 @@
-// Attention of new tokens over a paged cache: the entry points, the form in fp32, and the kernel that joins the pieces of units
-// that are cut.
+// Attention of new tokens over a paged cache: the entry points, the form for many fp32 rows, and the kernel that joins the pieces of
+// units that are cut.
+//
+// Four forms over one list of work: fp32 caches with up to four rows (tokens * query heads per key head) a sequence
+// (paged_attention_rows.cu) and with more (here, 16 rows x 64 positions on the FMA pipe, bound by shared memory's reads:
+// 2 x 500 tokens x 12 heads of 64 over up to 1000 positions 186 us); 16-bit caches with few rows (paged_attention_few.cu) and with
+// many (paged_attention_tc.cu).  The host chooses by what it knows, the average of rows.
 //
 // Mathematics.  One pass over the positions that a unit's rows see, with a running maximum m (base 2), sum l and output o
 // per row:  m' = max(m, s),  l' = 2^(m - m') l + sum 2^(s - m'),  o' = 2^(m - m') o + sum 2^(s - m') v;  out = o / l.  Pieces of
@@ -179,6 +184,9 @@ __global__ void __launch_bounds__(kSimpleThreads) paged_simple_kernel(const __gr
     let_next_start();
 }
 
+// What a launch of its own costs: 3 to 5 us of a call, mostly under the end of the kernel before; a join by the CTA that comes last would need
+// counters that somebody has set to 0.
+//
 // Joins the pieces of a unit that is cut: block (x, y) the rows y of the unit whose first tile CTA x has.  The first piece is in
 // that CTA's second slot, the others in the first slots of the CTAs behind it.
 constexpr int kJoinThreads = 256;

@@ -5,7 +5,7 @@
 // KT positions that some of its rows see (the first tokens' tiles, then those from the window's start on).  The tiles of all units,
 // with an entry cost for each unit's start, form one list that is cut into equal pieces, one per CTA, whatever the lengths
 // are: a CTA meets at most two units that it shares with others, its first and its last.  Lengths are known on the device only,
-// so every CTA works the list out for itself (a thread per sequence and a scan; about 1.5 us of latency).
+// so every CTA works the list out for itself (a lane per sequence or, where they are many, per row tile, and a scan; about 1.5 us of latency).
 #pragma once
 
 #include "paged.cuh"

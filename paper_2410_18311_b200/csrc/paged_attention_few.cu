@@ -11,6 +11,11 @@
 // the lanes 16 or 32 tiles ahead.  The maximum is moved only when a logit exceeds it by 2^8, which one vote finds out; fp16 weights are raised by
 // 2^7 as in the form for chunks.  Slots that no row sees, or that lie in pages that are none, are not read but set to 0; values that only
 // some rows see are looked through, and what is not finite is set to 0 and added at the end to the rows that see it.
+//
+// Measured from a graph, three sets of inputs, ragged lengths: 8 sequences x 32 heads x up to 4001 positions bf16 75 us, 5560 GB/s (under the
+// profiler 74.7 us, 417 MB read, issue 49 %); 2 x 8 heads x 4 rows x up to 130000 fp16 161 us, 5590 GB/s; 16 x 8 heads x 8 rows x 4000 44 us;
+// 4 x 32 heads x 200 12.5 us.  Some 10 to 12 us do not grow with the length: launch and list 2 us, a unit's start (page, first slots) 3,
+// its end (the warps' results) 3, the join.
 #include "paged_attention.cuh"
 
 namespace coreinfer {
