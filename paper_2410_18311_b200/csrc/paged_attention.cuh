@@ -139,19 +139,21 @@ __device__ __forceinline__ int paged_plan(const PagedAttnArgs& a, int* at)
     if (threadIdx.x == 0) at[0] = 0;
     __syncthreads();
     if (threadIdx.x < 32) {
-        int carry = 0;
+        long long carry = 0;
         for (int b0 = 0; b0 < a.c.B; b0 += 32) {
             const int b = b0 + threadIdx.x;
-            int w = b < a.c.B ? at[b + 1] : 0;
+            long long w = b < a.c.B ? at[b + 1] : 0;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
-                const int left = __shfl_up_sync(0xffffffffu, w, d);
+                const long long left = __shfl_up_sync(0xffffffffu, w, d);
                 if (threadIdx.x >= d) w += left;
             }
             w += carry;
-            if (b < a.c.B) at[b + 1] = w;
+            if (b < a.c.B) at[b + 1] = (int)w;
             carry = __shfl_sync(0xffffffffu, w, 31);
         }
+        // sequences that share rows, as no packing has them, can exceed what the host allowed for: then nothing is done
+        if (threadIdx.x == 0 && carry > 0x7fffffff) at[a.c.B] = 0;
     }
     __syncthreads();
     return at[a.c.B];

@@ -361,3 +361,26 @@ def test_attention_long_prompts_again_and_again(D):
         for s in states:
             ci.coreinfer_workspace_status(s[4])
             assert torch.equal(s[3], s[5])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+def test_attention_of_a_packing_that_is_none(dtype):
+    """Hundreds of sequences that all claim the same rows of a long table: more work than any packing holds, which is left undone or
+    done in bounds; the next call is as any other."""
+    require_gpu()
+    B, T, H, D, page = 400, 300, 2, 64, 16
+    dt = DT[dtype]
+    k, v = rand(4, H, page, D, dt=dt), rand(4, H, page, D, dt=dt, seed=1)
+    table = torch.full((B, 1 << 17), -1, dtype=torch.int32, device="cuda")
+    length = torch.full((B,), 1 << 21, dtype=torch.int32, device="cuda")
+    start = torch.tensor([0, T] * (B // 2) + [0], dtype=torch.int32, device="cuda")
+    cache = ci.make_paged_cache(k, v, table, length)
+    q = rand(T, 4, D, dt=dt, seed=2)
+    out = torch.zeros_like(q)
+    ws = torch.empty(ci.coreinfer_paged_attention_workspace_bytes(cache, 4, T), dtype=torch.uint8, device="cuda")
+    ci.coreinfer_paged_attention(cache, start, q, 0.125, out, ws, 64, 3)
+    torch.cuda.synchronize()
+    assert torch.isfinite(out).all()
+    b = Batch([3, 1], [40, 9], 2, 2, 64, 16, dtype, seed=8)
+    q = b.rand(4)
+    check_attention(b, q, attend(b, q, 0.125), 0.125)
