@@ -276,10 +276,9 @@ static PagedForm paged_form(coreinfer_dtype dtype, int D, int B, int share, int 
     const long long rows = ((long long)tokens * share + B - 1) / B;
     if (dtype == COREINFER_F32 && rows <= kPagedRowsMost) return {kFormRows, rows == 1 ? 1 : kPagedRowsMost, paged_rows_tile(D), rows == 1 ? 2 * 148 : 148, 2};
     if (dtype == COREINFER_F32) return {kFormSimple, kSimpleRows, kSimpleTile, 2 * 148, 1};
-    // By the rows of a sequence and key head on the average.  head_dim 128: 16 rows a warp of the form for few spill registers (15 rows x 4096
-    // of 9000 positions 48.0 us, in the form for chunks 41.9; 16 x 100000 106 and 91 us); 64 and 256 carry them (12 rows of 64 x 4000 26.7 and 31.5 us,
-    // 16 of 256 41.0 and 47.2).  One row x 4000 of 128 75 and 101 us.
-    if (rows > (D == 128 ? 8 : 16)) return {kFormChunk, paged_chunk_rows(D), kPagedChunkTile, kPagedChunkCtas, 2};
+    // By the rows of a sequence and key head on the average.  In the form for few and in that for chunks: 15 rows of 128 x 4096
+    // of 9000 positions 34.4 and 41.0 us, 16 of 128 x 100000 78 and 88, 12 of 64 x 4000 26.7 and 31.5, 16 of 256 41.0 and 47.2.  One row x 4000 of 128 75 and 101 us.
+    if (rows > 16) return {kFormChunk, paged_chunk_rows(D), kPagedChunkTile, kPagedChunkCtas, 2};
     const PagedFewShape few = paged_few_shape(D, (int)rows);
     return {kFormFew, few.RU, few.KT, few.ctas, 2};
 }

@@ -46,7 +46,7 @@ coreinfer_status paged_chunk(PagedAttnArgs& a, bool f16, unsigned* status, const
 struct PagedFewShape {
     int RU, KT, ctas;
 };
-static inline PagedFewShape paged_few_shape(int head_dim, int rows) { return {rows <= 8 ? 8 : 16, head_dim == 64 ? 256 : 128, head_dim == 256 ? 148 : 296}; }
+static inline PagedFewShape paged_few_shape(int head_dim, int rows) { return {rows <= 8 ? 8 : 16, head_dim == 64 ? 256 : 128, head_dim * (rows <= 8 ? 1 : 2) >= 256 ? 148 : 296}; }
 coreinfer_status paged_few(const PagedAttnArgs& a, bool f16, const DeviceInfo& di, cudaStream_t st);
 
 // n / share = (n * mul) >> 32 >> shift for 0 <= n < 2^31, with mul = ceil(2^(31 + l) / share), l = ceil(log2 share), shift = l - 1: the

@@ -5,8 +5,9 @@
 // O^T = V^T P^T, P^T made from the accumulators of S^T by movmatrix.  Weights enter as two parts (the value in 16 bits
 // and what that leaves), so their rounding is below the output's: 16 bits of a weight for bf16, 22 for fp16.
 //
-// Persistent CTAs of 8 warps over the common list.  A tile is 8 pieces of 16 positions (32 where head_dim is 64), one per warp.  Each
-// warp brings its own pieces through a ring of three stages of its own (keys or values of a piece; cp.async, 16 bytes a
+// Persistent CTAs of 8 warps over the common list, two an SM or, where the outputs and queries of a warp's rows fill 255 registers (head_dim 128
+// with 16 rows, 256), one.  A tile is 8 pieces of 16 positions (32 where head_dim is 64), one per warp.  Each
+// warp brings its own pieces through a ring of three stages of its own, six where 128 leaves room (keys or values of a piece; cp.async, 16 bytes a
 // lane) and keeps its own maximum, sum and output: no warp waits for another before the end of a unit.  Page numbers are loaded by
 // the lanes 16 or 32 tiles ahead.  The maximum is moved only when a logit exceeds it by 2^8, which one vote finds out; fp16 weights are raised by
 // 2^7 as in the form for chunks.  Slots that no row sees, or that lie in pages that are none, are not read but set to 0; values that only
@@ -22,10 +23,11 @@ namespace coreinfer {
 
 constexpr int kFewWarps = 8;
 constexpr int kFewThreads = 32 * kFewWarps;
-constexpr int kFewStages = 3;
 
 template <int D> constexpr int kFewPiece = D == 64 ? 32 : 16;                       // positions of a piece
 template <int D> constexpr int kFewStageBytes = kFewPiece<D> * D * 2;
+template <int D, int NT> constexpr int kFewCtas = D * NT >= 256 ? 1 : 2;              // per SM
+template <int D, int NT> constexpr int kFewStages = D == 128 && NT == 2 ? 6 : 3;
 
 template <typename T>
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
@@ -60,10 +62,10 @@ __device__ __forceinline__ float2 unpack2(uint32_t w)
 }
 
 template <typename T, int D, int NT>
-__global__ void __launch_bounds__(kFewThreads, D == 256 ? 1 : 2) paged_few_kernel(const __grid_constant__ PagedAttnArgs a)
+__global__ void __launch_bounds__(kFewThreads, kFewCtas<D, NT>) paged_few_kernel(const __grid_constant__ PagedAttnArgs a)
 {
     constexpr int KW = kFewPiece<D>, KT = KW * kFewWarps, RU = 8 * NT;
-    constexpr int STAGE = kFewStageBytes<D>, RING = kFewStages * STAGE;
+    constexpr int STAGE = kFewStageBytes<D>, STAGES = kFewStages<D, NT>, RING = STAGES * STAGE;
     constexpr int CPR = D / 8;                       // 16-byte pieces of a slot
     constexpr int SPI = 32 / CPR;                    // slots that a warp copies at once
     constexpr int KS = D / 16;
@@ -127,7 +129,7 @@ __global__ void __launch_bounds__(kFewThreads, D == 256 ? 1 : 2) paged_few_kerne
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
 #pragma unroll
-        for (int x = 0; x < kFewStages - 1; ++x) issue(x, x);
+        for (int x = 0; x < STAGES - 1; ++x) issue(x, x);
         // while the first slots are on their way:
         // queries as the second operand: row lane / 4 (of each group of eight), values 2 (lane % 4) and the next, and 8 further
         uint32_t q[NT][KS][2];
@@ -166,9 +168,9 @@ __global__ void __launch_bounds__(kFewThreads, D == 256 ? 1 : 2) paged_few_kerne
             const int step = 2 * (i - from);
             float s[NT][HALVES][4];
             // ---- keys
-            asm volatile("cp.async.wait_group %0;" ::"n"(kFewStages - 2) : "memory");
+            asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
             __syncwarp();
-            issue(step + kFewStages - 1, stage == 0 ? kFewStages - 1 : stage - 1);
+            issue(step + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
             const uint32_t key_at = ring_at + stage * STAGE;
 #pragma unroll
             for (int h = 0; h < HALVES; ++h) {
@@ -185,7 +187,7 @@ __global__ void __launch_bounds__(kFewThreads, D == 256 ? 1 : 2) paged_few_kerne
                     for (int n = 0; n < NT; ++n) mma16816<T>(s[n][h], f, q[n][k][0], q[n][k][1]);
                 }
             }
-            if (++stage == kFewStages) stage = 0;
+            if (++stage == STAGES) stage = 0;
             // ---- weights: element e of a half is position lane / 4 (+ 8 for e >= 2), row 2 (lane % 4) + e % 2
             const bool whole = j0 + KW <= low.hi && (j0 >= high.lo || j0 + KW <= a.sinks);
             bool move = false;
@@ -239,9 +241,9 @@ __global__ void __launch_bounds__(kFewThreads, D == 256 ? 1 : 2) paged_few_kerne
                     }
             }
             // ---- values
-            asm volatile("cp.async.wait_group %0;" ::"n"(kFewStages - 2) : "memory");
+            asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
             __syncwarp();
-            issue(step + kFewStages, stage == 0 ? kFewStages - 1 : stage - 1);
+            issue(step + STAGES, stage == 0 ? STAGES - 1 : stage - 1);
             const uint32_t value_at = ring_at + stage * STAGE;
             const bool look = !whole && !one_token;
 #pragma unroll
@@ -266,7 +268,7 @@ __global__ void __launch_bounds__(kFewThreads, D == 256 ? 1 : 2) paged_few_kerne
                     }
                 }
             }
-            if (++stage == kFewStages) stage = 0;
+            if (++stage == STAGES) stage = 0;
         }
 
         // ---- the warps' results: maxima and sums, then outputs in the rings' place
@@ -347,7 +349,7 @@ __global__ void __launch_bounds__(kFewThreads, D == 256 ? 1 : 2) paged_few_kerne
 template <typename T, int D, int NT>
 static coreinfer_status launch_few(const PagedAttnArgs& a, const DeviceInfo& di, cudaStream_t st)
 {
-    const size_t smem = (size_t)kFewWarps * kFewStages * kFewStageBytes<D> + kFewWarps * 8 * NT * sizeof(float2) + 8 + (size_t)(a.c.B + 1) * 4;
+    const size_t smem = (size_t)kFewWarps * kFewStages<D, NT> * kFewStageBytes<D> + kFewWarps * 8 * NT * sizeof(float2) + 8 + (size_t)(a.c.B + 1) * 4;
     const coreinfer_status s = allow_smem<paged_few_kernel<T, D, NT>>(di, 0);
     if (s != COREINFER_OK) return s;
     CI_CUDA(launch_overlapped(paged_few_kernel<T, D, NT>, dim3(a.n_ctas), dim3(kFewThreads), smem, st, a));
@@ -356,8 +358,7 @@ static coreinfer_status launch_few(const PagedAttnArgs& a, const DeviceInfo& di,
 template <typename T, int D>
 static coreinfer_status few_rows(const PagedAttnArgs& a, const DeviceInfo& di, cudaStream_t st)
 {
-    if constexpr (D == 128) return launch_few<T, D, 1>(a, di, st);           // more rows go to the form for chunks
-    else return a.RU == 8 ? launch_few<T, D, 1>(a, di, st) : launch_few<T, D, 2>(a, di, st);
+    return a.RU == 8 ? launch_few<T, D, 1>(a, di, st) : launch_few<T, D, 2>(a, di, st);
 }
 template <typename T>
 static coreinfer_status few_dim(const PagedAttnArgs& a, const DeviceInfo& di, cudaStream_t st)

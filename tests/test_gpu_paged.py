@@ -224,6 +224,27 @@ def test_attention(new, length, H, share, D, page, order, window, sinks, dtype):
     assert torch.equal(out, attend(b, q, scale, window, sinks))
 
 
+NINE_TO_SIXTEEN = [([1], [3000], 2, 16, 16, 0, 0), ([3], [2100], 2, 5, 32, 700, 4), ([12, 9], [600, 20], 3, 1, 64, 0, 0), ([2, 30, 0, 1, 1, 1], [900, 31, 50, 1, 128, 700], 2, 2, 16, 0, 0),
+                   ([1, 1], [20000, 5], 1, 13, 128, 0, 0), ([11], [11], 1, 1, 16, 3, 1), ([4] * 9, [4 + 77 * i for i in range(9)], 2, 3, 16, 100, 130)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("new,length,H,share,page,window,sinks", NINE_TO_SIXTEEN)
+def test_attention_nine_to_sixteen_rows_of_128(new, length, H, share, page, window, sinks, dtype):
+    """Two groups of eight rows a warp, the second of them not full, sequences of more rows beside them; then infinities and NaN in what some rows see."""
+    require_gpu()
+    b = Batch(new, length, H, share, 128, page, dtype, seed=sum(length) + share, front=1, pad=2, spread=1.5)
+    q = b.rand(H * share, extra=16)
+    scale = 128 ** -0.5
+    out = attend(b, q, scale, window, sinks)
+    check_attention(b, q, out, scale, window, sinks)
+    assert torch.equal(out, attend(b, q, scale, window, sinks))
+    for s, n in enumerate(new):
+        for x, j in enumerate({length[s] - 1, max(0, length[s] - n), length[s] // 2} if n else ()):
+            b.v[b.table[s, j // page].item(), x % H, j % page, (7 * x) % 128] = (float("nan"), float("inf"), float("-inf"))[x]
+    check_attention(b, q, attend(b, q, scale, window, sinks), scale, window, sinks)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 def test_attention_many_units_per_block(dtype):
     """Decoding sequences and long pieces of prompts in one call, more tiles than blocks: every block walks several units, most of
