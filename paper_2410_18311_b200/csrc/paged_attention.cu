@@ -187,11 +187,13 @@ __global__ void __launch_bounds__(kSimpleThreads) paged_simple_kernel(const __gr
 // What a launch of its own costs: 3 to 5 us of a call, mostly under the end of the kernel before; a join by the CTA that comes last would need
 // counters that somebody has set to 0.
 //
-// Joins the pieces of a unit that is cut: block (x, y) the rows y of the unit whose first tile CTA x has.  The first piece is in
+// Joins the pieces of a unit that is cut, AHEAD of them on the way at once: eight where units are small (a unit of few rows is often cut into 20
+// pieces: 16 x 4 rows x 130000 positions 153.5 -> 151.8 us against four), four in the form for chunks (eight take 70 registers, and its 200 to 600
+// blocks no longer fit side by side: 500 tokens x 40 heads over 16000 157.0 and 161.0 us).  Block (x, y) the rows y of the unit whose first tile CTA x has.  The first piece is in
 // that CTA's second slot, the others in the first slots of the CTAs behind it.
 constexpr int kJoinThreads = 256;
 template <int D> constexpr int kJoinRows = kJoinThreads * 4 / D;         // eight rows of 32 quarters at head_dim 128
-template <typename T, int D>
+template <typename T, int D, int AHEAD>
 __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_constant__ PagedAttnArgs a)
 {
     constexpr int ROWS = kJoinRows<D>;
@@ -204,22 +206,40 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_c
     if (row >= a.RU || global_row >= paged_rows(a, s)) return;
     const int first = blockIdx.x;
     auto slot = [&](int i) { return (size_t)i * 2 + (i == first ? 1 : 0); };
-    float m = -INFINITY;
-    for (int i = first; i <= p.last; ++i) m = fmaxf(m, a.part_ml[slot(i) * a.RU + row].x);
-    const float ref = m == -INFINITY ? 0.f : m;
-    float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int i = first; i <= p.last; ++i) {
-        const float2 ml = a.part_ml[slot(i) * a.RU + row];
-        const float f = exp2f(ml.x - ref);
-        const float4 x = *reinterpret_cast<const float4*>(a.part_o + slot(i) * a.RU * D + (c * a.RU + row * 4));
-        l = fmaf(ml.y, f, l);
-        // a piece in which the row sees nothing, or nothing but weights of 0, has nothing to add
-        if (ml.x == -INFINITY) continue;
-        o[0] = fmaf(x.x, f, o[0]);
-        o[1] = fmaf(x.y, f, o[1]);
-        o[2] = fmaf(x.z, f, o[2]);
-        o[3] = fmaf(x.w, f, o[3]);
+    // eight pieces' loads at once; the maximum moves from one eight to the next
+    float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = first; i0 <= p.last; i0 += AHEAD) {
+        float2 ml[AHEAD];
+        float4 x[AHEAD];
+        float top = m;
+#pragma unroll
+        for (int e = 0; e < AHEAD; ++e) {
+            ml[e] = make_float2(-INFINITY, 0.f);
+            if (i0 + e > p.last) continue;
+            ml[e] = a.part_ml[slot(i0 + e) * a.RU + row];
+            x[e] = *reinterpret_cast<const float4*>(a.part_o + slot(i0 + e) * a.RU * D + (c * a.RU + row * 4));
+        }
+#pragma unroll
+        for (int e = 0; e < AHEAD; ++e) top = fmaxf(top, ml[e].x);
+        const float ref = top == -INFINITY ? 0.f : top;
+        if (m != -INFINITY) {
+            const float by = exp2f(m - ref);
+            l *= by;
+#pragma unroll
+            for (int d = 0; d < 4; ++d) o[d] *= by;
+        }
+        m = top;
+#pragma unroll
+        for (int e = 0; e < AHEAD; ++e) {
+            const float f = exp2f(ml[e].x - ref);
+            l = fmaf(ml[e].y, f, l);
+            // a piece in which the row sees nothing, or nothing but weights of 0, has nothing to add
+            if (ml[e].x == -INFINITY) continue;
+            o[0] = fmaf(x[e].x, f, o[0]);
+            o[1] = fmaf(x[e].y, f, o[1]);
+            o[2] = fmaf(x[e].z, f, o[2]);
+            o[3] = fmaf(x[e].w, f, o[3]);
+        }
     }
     const bool sees = paged_row(a, s, global_row).hi > 0;
     T* to = reinterpret_cast<T*>(a.out) + paged_row_offset(a, s, p.h, global_row, a.ld_out) + c;
@@ -245,7 +265,9 @@ template <typename T, int D>
 static coreinfer_status launch_join(const PagedAttnArgs& a, cudaStream_t st)
 {
     constexpr int ROWS = kJoinRows<D>;
-    CI_CUDA(launch_overlapped(paged_join_kernel<T, D>, dim3(a.n_ctas, (a.RU + ROWS - 1) / ROWS), dim3(kJoinThreads), 0, st, a));
+    const dim3 grid(a.n_ctas, (a.RU + ROWS - 1) / ROWS);
+    if (a.RU <= 16) CI_CUDA(launch_overlapped(paged_join_kernel<T, D, 8>, grid, dim3(kJoinThreads), 0, st, a));
+    else CI_CUDA(launch_overlapped(paged_join_kernel<T, D, 4>, grid, dim3(kJoinThreads), 0, st, a));
     return COREINFER_OK;
 }
 template <typename T>
@@ -277,7 +299,7 @@ static PagedForm paged_form(coreinfer_dtype dtype, int D, int B, int share, int 
     if (dtype == COREINFER_F32 && rows <= kPagedRowsMost) return {kFormRows, rows == 1 ? 1 : kPagedRowsMost, paged_rows_tile(D), rows == 1 ? 2 * 148 : 148, 2};
     if (dtype == COREINFER_F32) return {kFormSimple, kSimpleRows, kSimpleTile, 2 * 148, 1};
     // By the rows of a sequence and key head on the average.  In the form for few and in that for chunks: 15 rows of 128 x 4096
-    // of 9000 positions 34.4 and 41.0 us, 16 of 128 x 100000 78 and 88, 12 of 64 x 4000 26.7 and 31.5, 16 of 256 41.0 and 47.2.  One row x 4000 of 128 75 and 101 us.
+    // of 9000 positions 32.7 and 41.0 us, 16 of 128 x 100000 71 and 88, 12 of 64 x 4000 26.7 and 31.5, 16 of 256 41.0 and 47.2.  One row x 4000 of 128 75 and 101 us.
     if (rows > 16) return {kFormChunk, paged_chunk_rows(D), kPagedChunkTile, kPagedChunkCtas, 2};
     const PagedFewShape few = paged_few_shape(D, (int)rows);
     return {kFormFew, few.RU, few.KT, few.ctas, 2};

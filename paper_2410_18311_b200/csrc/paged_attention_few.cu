@@ -13,9 +13,10 @@
 // 2^7 as in the form for chunks.  Slots that no row sees, or that lie in pages that are none, are not read but set to 0; values that only
 // some rows see are looked through, and what is not finite is set to 0 and added at the end to the rows that see it.
 //
-// Measured from a graph, three sets of inputs, ragged lengths: 8 sequences x 32 heads x up to 4001 positions bf16 75 us, 5560 GB/s (under the
-// profiler 74.7 us, 417 MB read, issue 49 %); 2 x 8 heads x 4 rows x up to 130000 fp16 161 us, 5590 GB/s; 16 x 8 heads x 8 rows x 4000 44 us;
-// 4 x 32 heads x 200 12.5 us.  Some 10 to 12 us do not grow with the length: launch and list 2 us, a unit's start (page, first slots) 3,
+// Measured from a graph, three sets of inputs, ragged lengths: 8 sequences x 32 heads x up to 4001 positions bf16 73 us, 5710 GB/s (under the
+// profiler 74.7 us, 417 MB read, issue 49 %); 2 x 8 heads x 4 rows x up to 130000 fp16 152 us, 5920 GB/s; 16 x 8 heads x 8 rows x 4000 44 us;
+// 4 x 32 heads x 200 12.4 us; 2 x 4 heads x 16 rows x 100000 71 us, 6 x 8 heads x 15 rows x 4096 of 9000 33 us (issue 37 %; twelve warps and rings
+// of four take 78 and 38.7 where eight took 78 and 34.4).  Some 10 to 12 us do not grow with the length: launch and list 2 us, a unit's start (page, first slots) 3,
 // its end (the warps' results) 3, the join.
 #include "paged_attention.cuh"
 
