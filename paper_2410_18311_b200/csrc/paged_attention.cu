@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(kSimpleThreads) paged_simple_kernel(const __gr
             p.b = w.b;
             p.h = w.h;
             p.tile = w.tile;
-            p.last = paged_owner(total, w.base + a.cost + w.t.count - 1, w.n);
+            p.last = w.last(a, at);
             a.pieces[blockIdx.x] = p;
         }
     }
@@ -367,6 +367,8 @@ coreinfer_status coreinfer_paged_attention(const coreinfer_paged_cache* cache, c
     a.scale2 = scale * kLog2e;
     a.RU = f.RU;
     a.KT = f.KT;
+    for (a.ru_shift = 0; 1 << a.ru_shift < a.RU;) ++a.ru_shift;
+    for (a.kt_shift = 0; 1 << a.kt_shift < a.KT;) ++a.kt_shift;
     a.cost = f.cost;
     a.n_ctas = f.ctas;
     unsigned* status = (unsigned*)workspace;

@@ -29,7 +29,8 @@ struct PagedAttnArgs {
     unsigned share_mul, share_shift;
     int window, sinks;      // window 0: everything before a token
     float scale2;           // scale * log2(e)
-    int RU, KT, cost;       // rows of a unit, positions of a tile, entries that a unit's start counts
+    int RU, KT, cost;       // rows of a unit, positions of a tile (powers of two), entries that a unit's start counts
+    int ru_shift, kt_shift; // log2 of the two
     int n_ctas;
     PagedPiece* pieces;     // [n_ctas]
     float2* part_ml;        // [n_ctas][2][RU]: reference exponent (base 2) and sum
@@ -79,7 +80,7 @@ struct PagedTiles {
     int hi;                 // positions below this are seen by some row
 };
 __device__ __forceinline__ int paged_rows(const PagedAttnArgs& a, const PagedSeq& s) { return s.n * a.share; }
-__device__ __forceinline__ int paged_row_tiles(const PagedAttnArgs& a, const PagedSeq& s) { return (paged_rows(a, s) + a.RU - 1) / a.RU; }
+__device__ __forceinline__ int paged_row_tiles(const PagedAttnArgs& a, const PagedSeq& s) { return (paged_rows(a, s) + a.RU - 1) >> a.ru_shift; }
 __device__ __forceinline__ PagedTiles paged_tiles(const PagedAttnArgs& a, const PagedSeq& s, int tile)
 {
     const int rows = paged_rows(a, s), r0 = tile * a.RU;
@@ -88,11 +89,11 @@ __device__ __forceinline__ PagedTiles paged_tiles(const PagedAttnArgs& a, const 
     PagedTiles t;
     t.hi = clamp_int(p1 + 1, 0, a.c.cap);
     const int lo = a.window ? clamp_int(p0 - a.window + 1, 0, t.hi) : 0;
-    t.from = lo / a.KT;
+    t.from = lo >> a.kt_shift;
     const int first = a.sinks < t.hi ? a.sinks : t.hi;
-    t.first_tiles = (first + a.KT - 1) / a.KT;
+    t.first_tiles = (first + a.KT - 1) >> a.kt_shift;
     if (t.first_tiles > t.from) t.first_tiles = t.from;
-    t.count = (t.hi + a.KT - 1) / a.KT - t.from + t.first_tiles;
+    t.count = ((t.hi + a.KT - 1) >> a.kt_shift) - t.from + t.first_tiles;
     return t;
 }
 __device__ __forceinline__ int paged_tile_at(const PagedTiles& t, int i) { return i < t.first_tiles ? i : i - t.first_tiles + t.from; }
@@ -158,19 +159,27 @@ __device__ __forceinline__ int paged_plan(const PagedAttnArgs& a, int* at)
     __syncthreads();
     return at[a.c.B];
 }
-// The list in n equal pieces (n at most its length, so that none is empty): piece i is [total * i / n, total * (i + 1) / n).
-__device__ __forceinline__ int paged_cut(int total, int i, int n)
-{
-    const unsigned each = (unsigned)total / (unsigned)n;
-    return (int)(each * i + ((unsigned)total - each * n) * i / (unsigned)n);
-}
-// The piece that holds an entry: the largest i with total * i / n <= x.
-__device__ __forceinline__ int paged_owner(int total, int x, int n) { return (int)((((unsigned long long)x + 1) * n - 1) / (unsigned)total); }
+// The list in a piece per CTA, or as many as it has entries: `each` entries, one more in the first `longer` of them.
+struct PagedCut {
+    int each, longer;
+    __device__ __forceinline__ void set(const PagedAttnArgs& a, int total)
+    {
+        const int n = total < a.n_ctas ? total : a.n_ctas;
+        each = (unsigned)total / (unsigned)n;
+        longer = total - each * n;
+    }
+    __device__ __forceinline__ int start(int i) const { return i * each + (i < longer ? i : longer); }
+    // The piece that holds entry x.
+    __device__ __forceinline__ int owner(int x) const
+    {
+        const int before = longer * (each + 1);      // at most the list's length
+        return x < before ? (unsigned)x / (unsigned)(each + 1) : longer + (unsigned)(x - before) / (unsigned)each;
+    }
+};
 
 // Walks the units of a piece [x, end) of the list.
 struct PagedWalk {
     int x, end;             // entries of the piece not walked yet
-    int n;                  // pieces
     int b, h, tile;
     int base;               // entry where the unit starts
     PagedSeq s;
@@ -179,11 +188,12 @@ struct PagedWalk {
     // Called by whole warps.
     __device__ __forceinline__ void begin(const PagedAttnArgs& a, const int* at, int total, int cta)
     {
-        n = total < a.n_ctas ? total : a.n_ctas;
         x = end = 0;
-        if (cta >= n) return;
-        x = paged_cut(total, cta, n);
-        end = paged_cut(total, cta + 1, n);
+        if (cta >= total) return;
+        PagedCut cut;
+        cut.set(a, total);
+        x = cut.start(cta);
+        end = cut.start(cta + 1);
         int lo = 0, hi = a.c.B;                      // at[lo] <= x < at[hi]
         while (hi - lo > 1) {
             const int mid = (lo + hi) / 2;
@@ -217,6 +227,13 @@ struct PagedWalk {
         t = paged_tiles(a, s, tile);
     }
     __device__ __forceinline__ bool more() const { return x < end; }
+    // The last piece that has a part of the unit.  (Worked out again: the registers would be held through every unit.)
+    __device__ __forceinline__ int last(const PagedAttnArgs& a, const int* at) const
+    {
+        PagedCut cut;
+        cut.set(a, at[a.c.B]);
+        return cut.owner(base + a.cost + t.count - 1);
+    }
     // Tiles from .. to - 1 of the unit are this piece's.
     __device__ __forceinline__ int from(const PagedAttnArgs& a) const { return x > base + a.cost ? x - base - a.cost : 0; }
     __device__ __forceinline__ int to(const PagedAttnArgs& a) const

@@ -339,7 +339,7 @@ __global__ void __launch_bounds__(kFewThreads, kFewCtas<D, NT>) paged_few_kernel
             piece.b = w.b;
             piece.h = w.h;
             piece.tile = w.tile;
-            piece.last = paged_owner(total, w.base + a.cost + w.t.count - 1, w.n);
+            piece.last = w.last(a, at);
             a.pieces[blockIdx.x] = piece;
         }
         __syncthreads();

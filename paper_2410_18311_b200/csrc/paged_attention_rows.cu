@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(kRowsThreads, R == 1 ? 2 : 1) paged_rows_kerne
             piece.b = w.b;
             piece.h = w.h;
             piece.tile = w.tile;
-            piece.last = paged_owner(total, w.base + a.cost + w.t.count - 1, w.n);
+            piece.last = w.last(a, at);
             a.pieces[blockIdx.x] = piece;
         }
         __syncthreads();

@@ -239,7 +239,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
     wait_for_stream();
     if (blockIdx.x == 0 && tid == 0) *g.status = kStatusOk;
     const int total = paged_plan(a, at);
-    if (tid == 0) a.pieces[blockIdx.x].last = -1;
+    if (tid == 576) a.pieces[blockIdx.x].last = -1;  // the thread that names the unit which others join
 
     if (warp >= 16) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
@@ -373,6 +373,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
             for (w.begin(a, at, total, blockIdx.x); ok && w.more(); w.next(a, at)) {
                 const int from = w.from(a), to = w.to(a);
                 if (from >= to) continue;
+                if (t == 0 && from == 0 && to < w.t.count) {
+                    PagedPiece p;
+                    p.b = w.b;
+                    p.h = w.h;
+                    p.tile = w.tile;
+                    p.last = w.last(a, at);
+                    a.pieces[blockIdx.x] = p;
+                }
                 const int rows = paged_unit_rows(a, w);
                 const ChunkView va = chunk_view(a, w, rows, 0), vb = chunk_view(a, w, rows, 1);
                 if (!(ok = chunk_wait(s->q_empty, q_ph ^ 1u, s, g.status))) break;
@@ -629,14 +637,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                 }
             }
             if (mine && !(head && tail) && h == 0) a.part_ml[slot * a.RU + x * 128 + r] = make_float2(m, l);
-            if (head && !tail && tid == 0) {
-                PagedPiece p;
-                p.b = w.b;
-                p.h = w.h;
-                p.tile = w.tile;
-                p.last = paged_owner(total, w.base + a.cost + w.t.count - 1, w.n);
-                a.pieces[blockIdx.x] = p;
-            }
             tc::fence_before();                                  // the reads of O come before the next unit's products
             if (to > from) ++unit;
         }
