@@ -300,7 +300,9 @@ static PagedForm paged_form(coreinfer_dtype dtype, int D, int B, int share, int 
     if (dtype == COREINFER_F32) return {kFormSimple, kSimpleRows, kSimpleTile, 2 * 148, 1};
     // By the rows of a sequence and key head on the average.  In the form for few and in that for chunks: 15 rows of 128 x 4096
     // of 9000 positions 32.7 and 41.0 us, 16 of 128 x 100000 71 and 88, 12 of 64 x 4000 26.7 and 31.5, 16 of 256 41.0 and 47.2.  One row x 4000 of 128 75 and 101 us.
-    if (rows > 16) return {kFormChunk, paged_chunk_rows(D), kPagedChunkTile, kPagedChunkCtas, 2};
+    // A unit's start and end take about what two tiles do; counted as three, fewer units are cut (prompt of 8192 tokens 536 -> 529 us, 4 sequences of 64
+    // rows over 6000 positions 33.0 -> 31.8, 500 tokens over 16000 158.3 -> 159.0; head_dim 256, whose tiles take longer, 160.4 -> 162.9).
+    if (rows > 16) return {kFormChunk, paged_chunk_rows(D), kPagedChunkTile, kPagedChunkCtas, D == 256 ? 2 : 3};
     const PagedFewShape few = paged_few_shape(D, (int)rows);
     return {kFormFew, few.RU, few.KT, few.ctas, 2};
 }
@@ -350,7 +352,7 @@ coreinfer_status coreinfer_paged_attention(const coreinfer_paged_cache* cache, c
     paged_set_share(a, q_heads / a.c.H);
     const PagedForm f = paged_form(dtype, a.c.D, a.c.B, a.share, tokens);
     // the list of work counts in 32 bits: row tiles of all sequences, each with all tiles of the table at most
-    if ((double)a.c.H * ((double)tokens * a.share / f.RU + a.c.B) * ((double)a.c.cap / f.KT + 3) >= 2147483648.0)
+    if ((double)a.c.H * ((double)tokens * a.share / f.RU + a.c.B) * ((double)a.c.cap / f.KT + 1 + f.cost) >= 2147483648.0)
         CI_FAIL(COREINFER_ERR_UNSUPPORTED, "%d tokens x %d heads over a table of %d positions: too much for one call", tokens, q_heads, a.c.cap);
     const size_t need = paged_workspace(f, a.c.D);
     if (workspace_bytes < need) CI_FAIL(COREINFER_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
