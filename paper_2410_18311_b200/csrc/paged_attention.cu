@@ -2,8 +2,7 @@
 // units that are cut.
 //
 // Four forms over one list of work: fp32 caches with up to four rows (tokens * query heads per key head) a sequence
-// (paged_attention_rows.cu) and with more (here, 16 rows x 64 positions on the FMA pipe, bound by shared memory's reads:
-// 2 x 500 tokens x 12 heads of 64 over up to 1000 positions 186 us); 16-bit caches with few rows (paged_attention_few.cu) and with
+// (paged_attention_rows.cu) and with more (here, 16 or 64 rows x 64 positions on the FMA pipe); 16-bit caches with few rows (paged_attention_few.cu) and with
 // many (paged_attention_tc.cu).  The host chooses by what it knows, the average of rows.
 //
 // Mathematics.  One pass over the positions that a unit's rows see, with a running maximum m (base 2), sum l and output o
@@ -14,162 +13,188 @@
 
 namespace coreinfer {
 
-constexpr int kSimpleThreads = 256;
-constexpr int kSimpleRows = 16;
-constexpr int kSimpleTile = 64;
+// Many fp32 rows.  Blocks of 256 threads as 16 x 16; a unit is 16 RT rows over tiles of 64 positions.  A thread has RT x 4 logits (rows ty RT + r,
+// positions tx + 16 e), then RT x D / 16 outputs of the same rows, so that a row's maximum and sum stay in the registers of half a warp and its
+// weights are written and read by one warp.  All operands come from shared memory in 16-byte reads: at RT = 4 twelve
+// wavefronts for 64 FMA instructions.  Keys, values and queries are brought by cp.async; at head_dim 128 and 256
+// the weights take the keys' place, so that two blocks fit an SM at 128.  Measured: 2 x 500 tokens x 12 heads of 64 over up to 1000 positions 77 us,
+// 1000 tokens x 16 heads over 2000 positions 220 us at head_dim 64, 392 at 128, 832 at 256 (at 128: FMA pipe 54 %,
+// shared memory's wavefronts 69 %, issue 70 %).
+constexpr int kManyThreads = 256;
+constexpr int kManyTile = 64;
+template <int D> constexpr int kManyCtas = D == 256 ? 1 : 2;                         // per SM
+template <int D> constexpr bool kManyApart = D == 64;                                // weights have a place of their own
+template <int D, int RT> constexpr int kManyFloats = 16 * RT * (D + 4) + kManyTile * (D + 4) + kManyTile * D + (kManyApart<D> ? 16 * RT * (kManyTile + 4) : 0);
 
-template <typename T, int D>
-__global__ void __launch_bounds__(kSimpleThreads) paged_simple_kernel(const __grid_constant__ PagedAttnArgs a)
+__device__ __forceinline__ void many_copy(float* to, const float* from, bool read)
 {
-    constexpr int RU = kSimpleRows, KT = kSimpleTile;
-    constexpr int KP = D + 4;                        // row of the keys: no two lanes of a 16-byte read share banks
-    constexpr int CG = D / 4, RPT = RU * CG / kSimpleThreads;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(read ? 16 : 0) : "memory");
+}
+
+template <int D, int RT>
+__global__ void __launch_bounds__(kManyThreads, kManyCtas<D>) paged_many_kernel(const __grid_constant__ PagedAttnArgs a)
+{
+    constexpr int RU = 16 * RT, KT = kManyTile, DP = D + 4, PP = KT + 4, NV = D / 64;
+    static_assert(kManyApart<D> || RU * PP <= KT * DP, "weights in the keys' place");
     extern __shared__ __align__(16) float smem[];
-    float* qs = smem;                                // [RU][D]
-    float* ks = qs + RU * D;                         // [KT][KP]
-    float* vs = ks + KT * KP;                        // [KT][D]
-    float* ps = vs + KT * D;                         // [RU][KT + 4]
-    float* ms = ps + RU * (KT + 4);                  // [RU] reference exponents
-    float* ls = ms + RU;                             // [RU] sums
-    float* fs = ls + RU;                             // [RU] factor of what was summed before
-    int* at = reinterpret_cast<int*>(fs + RU);
-    const int tid = threadIdx.x;
+    float* qs = smem;                                // [RU][DP]
+    float* ks = qs + RU * DP;                        // [KT][DP]
+    float* vs = ks + KT * DP;                        // [KT][D]
+    float* ps = kManyApart<D> ? vs + KT * D : ks;    // [RU][PP]
+    int* at = reinterpret_cast<int*>(smem + kManyFloats<D, RT>);
+    const int tid = threadIdx.x, lane = tid & 31, tx = tid & 15, ty = tid >> 4;
+    const float* keys = reinterpret_cast<const float*>(a.c.pool[0]);
+    const float* values = reinterpret_cast<const float*>(a.c.pool[1]);
     wait_for_stream();
     const int total = paged_plan(a, at);
     if (tid == 0) a.pieces[blockIdx.x].last = -1;
     PagedWalk w;
     for (w.begin(a, at, total, blockIdx.x); w.more(); w.next(a, at)) {
-        const int rows = paged_unit_rows(a, w), r0 = w.tile * RU;
         const int from = w.from(a), to = w.to(a);
         if (w.t.count > 0 && from >= to) continue;
-        __syncthreads();
-        for (int i = tid; i < RU * D; i += kSimpleThreads) {
-            const int r = i / D, d = i - r * D;
-            qs[i] = r < rows ? to_f32(reinterpret_cast<const T*>(a.q)[paged_row_offset(a, w.s, w.h, r0 + r, a.ld_q) + d]) : 0.f;
-        }
-        if (tid < RU) {
-            ms[tid] = -INFINITY;
-            ls[tid] = 0.f;
-        }
-        float o[RPT][4];
+        const int rows = paged_unit_rows(a, w), r0 = w.tile * RU;
+        const PagedRow low = paged_row(a, w.s, r0), high = paged_row(a, w.s, r0 + rows - 1);
+        // a tile's keys, then its values; what no row sees is 0
+        auto fetch = [&](int i) {
+            const int j0 = paged_tile_at(w.t, i) * KT;
+            const int pages = lane < KT / 16 ? paged_page(a.c, w.b, j0 + lane * 16) : -1;
 #pragma unroll
-        for (int r = 0; r < RPT; ++r)
+            for (int kv = 0; kv < 2; ++kv) {
+#pragma unroll 4
+                for (int x = tid; x < KT * (D / 4); x += kManyThreads) {
+                    const int j = x / (D / 4), d = x % (D / 4) * 4;
+                    const int page = __shfl_sync(0xffffffffu, pages, j / 16);
+                    const bool read = page >= 0 && j0 + j < high.hi && (j0 + j >= low.lo || j0 + j < a.sinks);
+                    const float* pool = kv ? values : keys;
+                    many_copy(kv ? vs + j * D + d : ks + j * DP + d, read ? pool + paged_offset(a.c, page, w.h, j0 + j) + d : pool, read);
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+            }
+        };
+        __syncthreads();                             // the unit before is done with shared memory
+        for (int x = tid; x < RU * (D / 4); x += kManyThreads) {
+            const int r = x / (D / 4), d = x % (D / 4) * 4;
+            const float* q = reinterpret_cast<const float*>(a.q);
+            many_copy(qs + r * DP + d, r < rows ? q + paged_row_offset(a, w.s, w.h, r0 + r, a.ld_q) + d : q, r < rows);
+        }
+        if (from < to) fetch(from);
+        PagedRow see[RT];
+        float m[RT], l[RT], o[RT][NV][4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[r][e] = 0.f;
+        for (int r = 0; r < RT; ++r) {
+            const int row = ty * RT + r;
+            see[r] = paged_row(a, w.s, r0 + (row < rows ? row : rows - 1));
+            m[r] = -INFINITY;
+            l[r] = 0.f;
+#pragma unroll
+            for (int n = 0; n < NV; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[r][n][e] = 0.f;
+        }
         for (int i = from; i < to; ++i) {
             const int j0 = paged_tile_at(w.t, i) * KT;
+            const bool whole = j0 + KT <= low.hi && (j0 >= high.lo || j0 + KT <= a.sinks);
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
             __syncthreads();
-            for (int x = tid; x < KT * D / 8; x += kSimpleThreads) {
-                const int j = x / (D / 8), d = (x - j * (D / 8)) * 8;
-                float k8[8], v8[8];
+            float s[RT][4];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) k8[e] = v8[e] = 0.f;
-                const int page = j0 + j < w.t.hi ? paged_page(a.c, w.b, j0 + j) : -1;
-                if (page >= 0) {
-                    const long long at8 = paged_offset(a.c, page, w.h, j0 + j) + d;
-                    uint4 raw[sizeof(T) / 2];
+            for (int r = 0; r < RT; ++r)
 #pragma unroll
-                    for (int e = 0; e < (int)sizeof(T) / 2; ++e) raw[e] = reinterpret_cast<const uint4*>(a.c.pool[0] + at8 * sizeof(T))[e];
-                    unpack8<T>(raw, k8);
+                for (int e = 0; e < 4; ++e) s[r][e] = 0.f;
+#pragma unroll 4
+            for (int d = 0; d < D; d += 4) {
+                float4 k[4];
 #pragma unroll
-                    for (int e = 0; e < (int)sizeof(T) / 2; ++e) raw[e] = reinterpret_cast<const uint4*>(a.c.pool[1] + at8 * sizeof(T))[e];
-                    unpack8<T>(raw, v8);
-                }
+                for (int e = 0; e < 4; ++e) k[e] = *reinterpret_cast<const float4*>(ks + (tx + 16 * e) * DP + d);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    ks[j * KP + d + e] = k8[e];
-                    vs[j * D + d + e] = v8[e];
+                for (int r = 0; r < RT; ++r) {
+                    const float4 q = *reinterpret_cast<const float4*>(qs + (ty * RT + r) * DP + d);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[r][e] = fmaf(q.x, k[e].x, fmaf(q.y, k[e].y, fmaf(q.z, k[e].z, fmaf(q.w, k[e].w, s[r][e]))));
                 }
             }
-            __syncthreads();
-            {
-                const int j = tid & (KT - 1), rg = tid / KT * 4;
-                float s[4] = {0.f, 0.f, 0.f, 0.f};
-                for (int d = 0; d < D; d += 4) {
-                    const float4 k = *reinterpret_cast<const float4*>(ks + j * KP + d);
+            if (!kManyApart<D>) __syncthreads();
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float4 q = *reinterpret_cast<const float4*>(qs + (rg + r) * D + d);
-                        s[r] = fmaf(q.x, k.x, fmaf(q.y, k.y, fmaf(q.z, k.z, fmaf(q.w, k.w, s[r]))));
+            for (int r = 0; r < RT; ++r) {
+                float top = m[r];
+                unsigned seen = 0xfu;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[r][e] *= a.scale2;
+                    if (!whole && !paged_sees(a, see[r], j0 + tx + 16 * e)) {
+                        seen &= ~(1u << e);
+                        s[r][e] = -INFINITY;
                     }
+                    top = fmaxf(top, s[r][e]);
                 }
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const bool seen = rg + r < rows && paged_sees(a, paged_row(a, w.s, r0 + rg + r), j0 + j);
-                    ps[(rg + r) * (KT + 4) + j] = seen ? s[r] * a.scale2 : -INFINITY;
-                }
-            }
-            __syncthreads();
-            {
-                const int r = tid / 16, c = tid % 16;
-                float s[4], m = ms[r];
-                const float before = m;
+                for (int d = 1; d < 16; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                const float ref = top == -INFINITY ? 0.f : top;
+                const float by = exp2f(m[r] - ref);
+                m[r] = top;
+                l[r] *= by;
+#pragma unroll
+                for (int n = 0; n < NV; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[r][n][e] *= by;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    s[e] = ps[r * (KT + 4) + c + 16 * e];
-                    m = fmaxf(m, s[e]);
-                }
-#pragma unroll
-                for (int d = 1; d < 16; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-                const float ref = m == -INFINITY ? 0.f : m;
-                float sum = 0.f;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[e] = exp2f(s[e] - ref);
-                    ps[r * (KT + 4) + c + 16 * e] = s[e];
-                    sum += s[e];
-                }
-#pragma unroll
-                for (int d = 1; d < 16; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-                if (c == 0) {
-                    const float f = exp2f(before - ref);
-                    fs[r] = f;
-                    ms[r] = m;
-                    ls[r] = fmaf(ls[r], f, sum);
+                    const float p = exp2f(s[r][e] - ref);
+                    l[r] += p;
+                    // below 0: the row does not see the position, and no value there may reach it, as 0 times infinity would
+                    ps[(ty * RT + r) * PP + tx + 16 * e] = seen >> e & 1u ? p : -1.f;
                 }
             }
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
             __syncthreads();
-            {
-                const int c = tid % CG * 4, rg = tid / CG * RPT;
-                // where some row does not see some position, a weight of 0 must not meet what it must not see
-                const PagedRow low = paged_row(a, w.s, r0), high = paged_row(a, w.s, r0 + rows - 1);
-                const bool whole = j0 + KT <= low.hi && (j0 >= high.lo || j0 + KT <= a.sinks);
+            auto add = [&](auto all) {
+#pragma unroll 2
+                for (int j = 0; j < KT; j += 4) {
+                    float p[RT][4];
 #pragma unroll
-                for (int r = 0; r < RPT; ++r) {
-                    const float f = fs[rg + r];
+                    for (int r = 0; r < RT; ++r) *reinterpret_cast<float4*>(p[r]) = *reinterpret_cast<const float4*>(ps + (ty * RT + r) * PP + j);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) o[r][e] *= f;
-                    const PagedRow row = paged_row(a, w.s, r0 + rg + r);
-                    for (int j = 0; j < KT; ++j) {
-                        const float p = ps[(rg + r) * (KT + 4) + j];
-                        const float4 v = *reinterpret_cast<const float4*>(vs + j * D + c);
-                        if (whole || paged_sees(a, row, j0 + j)) {
-                            o[r][0] = fmaf(p, v.x, o[r][0]);
-                            o[r][1] = fmaf(p, v.y, o[r][1]);
-                            o[r][2] = fmaf(p, v.z, o[r][2]);
-                            o[r][3] = fmaf(p, v.w, o[r][3]);
+                    for (int x = 0; x < 4; ++x)
+#pragma unroll
+                        for (int n = 0; n < NV; ++n) {
+                            const float4 v = *reinterpret_cast<const float4*>(vs + (j + x) * D + tx * 4 + 64 * n);
+#pragma unroll
+                            for (int r = 0; r < RT; ++r) {
+                                if (!decltype(all)::value && p[r][x] < 0.f) continue;
+                                o[r][n][0] = fmaf(p[r][x], v.x, o[r][n][0]);
+                                o[r][n][1] = fmaf(p[r][x], v.y, o[r][n][1]);
+                                o[r][n][2] = fmaf(p[r][x], v.z, o[r][n][2]);
+                                o[r][n][3] = fmaf(p[r][x], v.w, o[r][n][3]);
+                            }
                         }
-                    }
                 }
-            }
+            };
+            if (whole) add(std::true_type());
+            else add(std::false_type());
+            __syncthreads();
+            if (i + 1 < to) fetch(i + 1);
         }
-        __syncthreads();
-        const int c = tid % CG * 4, rg = tid / CG * RPT;
+        asm volatile("cp.async.wait_all;" ::: "memory");
         const bool head = from == 0, tail = to == w.t.count;
+        const size_t slot = (size_t)blockIdx.x * 2 + (head ? 1 : 0);
 #pragma unroll
-        for (int r = 0; r < RPT; ++r) {
-            const int row = rg + r;
+        for (int r = 0; r < RT; ++r) {
+#pragma unroll
+            for (int d = 1; d < 16; d <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], d);
+            const int row = ty * RT + r;
             if (row >= rows) continue;
             if (head && tail) {
-                const PagedRow see = paged_row(a, w.s, r0 + row);
-                const float l = ls[row];
-                T* to_row = reinterpret_cast<T*>(a.out) + paged_row_offset(a, w.s, w.h, r0 + row, a.ld_out) + c;
+                float* to_row = reinterpret_cast<float*>(a.out) + paged_row_offset(a, w.s, w.h, r0 + row, a.ld_out) + tx * 4;
+                const bool any = see[r].hi > 0;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) to_row[e] = from_f32<T>(see.hi > 0 ? o[r][e] / l : 0.f);
+                for (int n = 0; n < NV; ++n)
+                    *reinterpret_cast<float4*>(to_row + 64 * n) = any ? make_float4(o[r][n][0] / l[r], o[r][n][1] / l[r], o[r][n][2] / l[r], o[r][n][3] / l[r])
+                                                                      : make_float4(0.f, 0.f, 0.f, 0.f);
             } else {
-                const size_t slot = (size_t)blockIdx.x * 2 + (head ? 1 : 0);
-                *reinterpret_cast<float4*>(a.part_o + slot * RU * D + (c * RU + row * 4)) = make_float4(o[r][0], o[r][1], o[r][2], o[r][3]);
-                if (c == 0) a.part_ml[slot * RU + row] = make_float2(ms[row], ls[row]);
+#pragma unroll
+                for (int n = 0; n < NV; ++n)
+                    *reinterpret_cast<float4*>(a.part_o + slot * RU * D + ((tx * 4 + 64 * n) * RU + row * 4)) = make_float4(o[r][n][0], o[r][n][1], o[r][n][2], o[r][n][3]);
+                if (tx == 0) a.part_ml[slot * RU + row] = make_float2(m[r], l[r]);
             }
         }
         if (head && !tail && tid == 0) {
@@ -250,17 +275,20 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_c
     else *reinterpret_cast<uint2*>(to) = *reinterpret_cast<const uint2*>(y);
 }
 
-template <typename T, int D>
-static coreinfer_status launch_simple(PagedAttnArgs& a, const DeviceInfo& di, cudaStream_t st)
+template <int D, int RT>
+static coreinfer_status launch_many(const PagedAttnArgs& a, const DeviceInfo& di, cudaStream_t st)
 {
-    const size_t smem = (size_t)(kSimpleRows * D + kSimpleTile * (D + 4) + kSimpleTile * D + kSimpleRows * (kSimpleTile + 4) + 3 * kSimpleRows) * 4 +
-                        (size_t)(a.c.B + 1) * 4;
-    coreinfer_status s = allow_smem<paged_simple_kernel<T, D>>(di);
+    const size_t smem = (size_t)kManyFloats<D, RT> * 4 + (size_t)(a.c.B + 1) * 4;
+    const coreinfer_status s = allow_smem<paged_many_kernel<D, RT>>(di, 0);
     if (s != COREINFER_OK) return s;
-    CI_CUDA(launch_overlapped(paged_simple_kernel<T, D>, dim3(a.n_ctas), dim3(kSimpleThreads), smem, st, a));
+    CI_CUDA(launch_overlapped(paged_many_kernel<D, RT>, dim3(a.n_ctas), dim3(kManyThreads), smem, st, a));
     return COREINFER_OK;
 }
-
+template <int D>
+static coreinfer_status many_rows(const PagedAttnArgs& a, const DeviceInfo& di, cudaStream_t st)
+{
+    return a.RU == 16 ? launch_many<D, 1>(a, di, st) : launch_many<D, 4>(a, di, st);
+}
 template <typename T, int D>
 static coreinfer_status launch_join(const PagedAttnArgs& a, cudaStream_t st)
 {
@@ -277,17 +305,16 @@ static coreinfer_status pick_join(const PagedAttnArgs& a, cudaStream_t st)
     return a.c.D == 128 ? launch_join<T, 128>(a, st) : launch_join<T, 256>(a, st);
 }
 
-template <typename T>
-static coreinfer_status pick_simple(PagedAttnArgs& a, const DeviceInfo& di, cudaStream_t st)
+static coreinfer_status pick_many(const PagedAttnArgs& a, const DeviceInfo& di, cudaStream_t st)
 {
-    if (a.c.D == 64) return launch_simple<T, 64>(a, di, st);
-    return a.c.D == 128 ? launch_simple<T, 128>(a, di, st) : launch_simple<T, 256>(a, di, st);
+    if (a.c.D == 64) return many_rows<64>(a, di, st);
+    return a.c.D == 128 ? many_rows<128>(a, di, st) : many_rows<256>(a, di, st);
 }
 
 static size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 
 // Which form a call takes, by what the host knows (the lengths of the batch's pieces are on the device).
-enum PagedFormKind { kFormSimple, kFormRows, kFormFew, kFormChunk };
+enum PagedFormKind { kFormMany, kFormRows, kFormFew, kFormChunk };
 struct PagedForm {
     PagedFormKind kind;
     int RU, KT, ctas;           // rows of a unit, positions of a tile, CTAs
@@ -297,7 +324,9 @@ static PagedForm paged_form(coreinfer_dtype dtype, int D, int B, int share, int 
 {
     const long long rows = ((long long)tokens * share + B - 1) / B;
     if (dtype == COREINFER_F32 && rows <= kPagedRowsMost) return {kFormRows, rows == 1 ? 1 : kPagedRowsMost, paged_rows_tile(D), rows == 1 ? 2 * 148 : 148, 2};
-    if (dtype == COREINFER_F32) return {kFormSimple, kSimpleRows, kSimpleTile, 2 * 148, 1};
+    // 16 or 64 rows a unit: 6 rows over 3000 positions 60 and 87 us at head_dim 128, 130 and 177 at 256; 24 rows 90.0 and 89.3, 199 and 178 (48 and 54 at
+    // 64).
+    if (dtype == COREINFER_F32) return {kFormMany, rows <= 16 ? 16 : 64, kManyTile, 148 * (D == 256 ? 1 : 2), 1};
     // By the rows of a sequence and key head on the average.  In the form for few and in that for chunks: 15 rows of 128 x 4096
     // of 9000 positions 32.7 and 41.0 us, 16 of 128 x 100000 71 and 88, 12 of 64 x 4000 26.7 and 31.5, 16 of 256 41.0 and 47.2.  One row x 4000 of 128 75 and 101 us.
     // A unit's start and end take about what two tiles do; counted as three, fewer units are cut (prompt of 8192 tokens 536 -> 529 us, 4 sequences of 64
@@ -383,7 +412,7 @@ coreinfer_status coreinfer_paged_attention(const coreinfer_paged_cache* cache, c
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (f.kind == kFormChunk) s = paged_chunk(a, dtype == COREINFER_F16, status, di, st);
     else if (f.kind == kFormRows) s = paged_rows_f32(a, di, st);
-    else s = f.kind == kFormFew ? paged_few(a, dtype == COREINFER_F16, di, st) : pick_simple<float>(a, di, st);
+    else s = f.kind == kFormFew ? paged_few(a, dtype == COREINFER_F16, di, st) : pick_many(a, di, st);
     if (s != COREINFER_OK) return s;
     if (dtype == COREINFER_F32) return pick_join<float>(a, st);
     return dtype == COREINFER_BF16 ? pick_join<__nv_bfloat16>(a, st) : pick_join<__half>(a, st);
