@@ -47,7 +47,7 @@ __global__ void __launch_bounds__(kManyThreads, kManyCtas<D>) paged_many_kernel(
     const float* values = reinterpret_cast<const float*>(a.c.pool[1]);
     wait_for_stream();
     const int total = paged_plan(a, at);
-    if (tid == 0) a.pieces[blockIdx.x].last = -1;
+    if (tid == 0) paged_first_words(a);
     PagedWalk w;
     for (w.begin(a, at, total, blockIdx.x); w.more(); w.next(a, at)) {
         const int from = w.from(a), to = w.to(a);
@@ -402,7 +402,7 @@ coreinfer_status coreinfer_paged_attention(const coreinfer_paged_cache* cache, c
     for (a.kt_shift = 0; 1 << a.kt_shift < a.KT;) ++a.kt_shift;
     a.cost = f.cost;
     a.n_ctas = f.ctas;
-    unsigned* status = (unsigned*)workspace;
+    a.status = (unsigned*)workspace;
     uint8_t* ws = (uint8_t*)workspace + 16;
     a.pieces = (PagedPiece*)ws;
     ws += round16(f.ctas * sizeof(PagedPiece));
@@ -410,7 +410,7 @@ coreinfer_status coreinfer_paged_attention(const coreinfer_paged_cache* cache, c
     ws += round16((size_t)f.ctas * 2 * f.RU * sizeof(float2));
     a.part_o = (float*)(((uintptr_t)ws + 31) & ~(uintptr_t)31);
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (f.kind == kFormChunk) s = paged_chunk(a, dtype == COREINFER_F16, status, di, st);
+    if (f.kind == kFormChunk) s = paged_chunk(a, dtype == COREINFER_F16, di, st);
     else if (f.kind == kFormRows) s = paged_rows_f32(a, di, st);
     else s = f.kind == kFormFew ? paged_few(a, dtype == COREINFER_F16, di, st) : pick_many(a, di, st);
     if (s != COREINFER_OK) return s;

@@ -32,6 +32,7 @@ struct PagedAttnArgs {
     int RU, KT, cost;       // rows of a unit, positions of a tile (powers of two), entries that a unit's start counts
     int ru_shift, kt_shift; // log2 of the two
     int n_ctas;
+    unsigned* status;       // the workspace's first word
     PagedPiece* pieces;     // [n_ctas]
     float2* part_ml;        // [n_ctas][2][RU]: reference exponent (base 2) and sum
     float* part_o;          // [n_ctas][2][D / 4][RU][4]: rows side by side, as the threads that write them are
@@ -41,7 +42,7 @@ struct PagedAttnArgs {
 static inline int paged_chunk_rows(int head_dim) { return head_dim == 256 ? 128 : 256; }
 constexpr int kPagedChunkTile = 128;
 constexpr int kPagedChunkCtas = 148;
-coreinfer_status paged_chunk(PagedAttnArgs& a, bool f16, unsigned* status, const DeviceInfo& di, cudaStream_t st);
+coreinfer_status paged_chunk(PagedAttnArgs& a, bool f16, const DeviceInfo& di, cudaStream_t st);
 
 // The form for few rows (paged_attention_few.cu): 16-bit caches; rows of a unit 8 or 16.
 struct PagedFewShape {
@@ -258,6 +259,12 @@ struct PagedWalk {
     }
 };
 
+// What every form leaves for who comes after it, by one thread of a CTA: no unit is cut until one is, and no wait has given up.
+__device__ __forceinline__ void paged_first_words(const PagedAttnArgs& a)
+{
+    a.pieces[blockIdx.x].last = -1;
+    if (blockIdx.x == 0) *a.status = kStatusOk;
+}
 // Rows of a unit.
 __device__ __forceinline__ int paged_unit_rows(const PagedAttnArgs& a, const PagedWalk& w)
 {

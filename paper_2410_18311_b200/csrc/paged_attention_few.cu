@@ -84,7 +84,7 @@ __global__ void __launch_bounds__(kFewThreads, kFewCtas<D, NT>) paged_few_kernel
     wait_for_stream();
     const int total = paged_plan(a, at);
     if (tid == 0) {
-        a.pieces[blockIdx.x].last = -1;
+        paged_first_words(a);
         found[0] = 0;
     }
     int unit = 0;

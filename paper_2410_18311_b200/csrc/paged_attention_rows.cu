@@ -33,7 +33,7 @@ __global__ void __launch_bounds__(kRowsThreads, R == 1 ? 2 : 1) paged_rows_kerne
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, d0 = lane % LPK * 4;
     wait_for_stream();
     const int total = paged_plan(a, at);
-    if (tid == 0) a.pieces[blockIdx.x].last = -1;
+    if (tid == 0) paged_first_words(a);
     PagedWalk w;
     for (w.begin(a, at, total, blockIdx.x); w.more(); w.next(a, at)) {
         const int from = w.from(a), to = w.to(a);

@@ -52,7 +52,6 @@ struct ChunkArgs {
     int box;                // slots of a tensor copy
     int negative;           // scale below 0: the queries' signs are turned
     int map_q;              // queries come by tensor copies
-    unsigned* status;
 };
 
 struct ChunkBars {
@@ -237,9 +236,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
     tc::fence_after();
     const uint32_t tmem = s->tmem;
     wait_for_stream();
-    if (blockIdx.x == 0 && tid == 0) *g.status = kStatusOk;
     const int total = paged_plan(a, at);
-    if (tid == 576) a.pieces[blockIdx.x].last = -1;  // the thread that names the unit which others join
+    if (tid == 576) paged_first_words(a);            // the thread that names the unit which others join
 
     if (warp >= 16) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
@@ -260,7 +258,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
 #pragma unroll
                     for (int kv = 0; kv < 2; ++kv) {
                         const int stage = at_stage[kv] + (kv ? g.k_stages : 0);
-                        if (!(ok = chunk_wait(s->empty[stage], phase[kv] ^ 1u, s, g.status))) break;
+                        if (!(ok = chunk_wait(s->empty[stage], phase[kv] ^ 1u, s, a.status))) break;
                         const uint32_t bar = smem_u32(&s->full[stage]);
                         if (lane == 0) mbar_arrive_expect_tx(bar, TILE);
                         __syncwarp();
@@ -310,11 +308,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                         end[x] = v.any ? (v.hi_max + KT - 1) / KT - w.t.from + w.t.first_tiles : 0;
                     }
                     auto needs = [&](int x, int i) { return i < end[x] && (i < sink_tiles || i >= first[x]); };
-                    if (!(ok = chunk_wait_one(s->full[ks], k_ph, s, g.status))) break;
+                    if (!(ok = chunk_wait_one(s->full[ks], k_ph, s, a.status))) break;
 #pragma unroll
                     for (int x = 0; x < PIPES; ++x) {
                         if (x * 128 >= rows) continue;
-                        if (ok) ok = chunk_wait_one(s->q_full[x], q_ph[x], s, g.status);
+                        if (ok) ok = chunk_wait_one(s->q_full[x], q_ph[x], s, a.status);
                         q_ph[x] ^= 1u;
                         tc::fence_after();
                         if (ok && needs(x, from)) scores(x, ks);
@@ -326,13 +324,13 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                     for (int i = from; i < to; ++i) {
                         // V(i), which is there when it has been looked at, and K(i + 1)
                         const bool last = i + 1 == to;
-                        if (!(ok = chunk_wait_one(s->looked[vs], v_ph, s, g.status))) break;
-                        if (!last && !(ok = chunk_wait_one(s->full[ks], k_ph, s, g.status))) break;
+                        if (!(ok = chunk_wait_one(s->looked[vs], v_ph, s, a.status))) break;
+                        if (!last && !(ok = chunk_wait_one(s->full[ks], k_ph, s, a.status))) break;
                         const uint32_t val = v_desc + vs * (TILE >> 4);
 #pragma unroll
                         for (int x = 0; x < PIPES; ++x) {
                             if (ok && needs(x, i)) {
-                                ok = chunk_wait_one(s->p_full[x], p_ph[x], s, g.status);
+                                ok = chunk_wait_one(s->p_full[x], p_ph[x], s, a.status);
                                 p_ph[x] ^= 1u;
                                 tc::fence_after();
                                 if (ok) {
@@ -383,7 +381,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                 }
                 const int rows = paged_unit_rows(a, w);
                 const ChunkView va = chunk_view(a, w, rows, 0), vb = chunk_view(a, w, rows, 1);
-                if (!(ok = chunk_wait(s->q_empty, q_ph ^ 1u, s, g.status))) break;
+                if (!(ok = chunk_wait(s->q_empty, q_ph ^ 1u, s, a.status))) break;
                 q_ph ^= 1u;
                 if (g.map_q) {                                   // rows of a tile: 128 / share tokens, each the heads of the group
                     if (t < 2 && t * 128 < rows) {
@@ -439,7 +437,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                 for (int i = from; i < to; ++i) {
                     const int j = paged_tile_at(w.t, i) * KT;
                     // each tile is waited for, so that neither the ring nor this warp is ever a round ahead of the other
-                    if (!(ok = chunk_wait(s->full[g.k_stages + stage], ph, s, g.status))) break;
+                    if (!(ok = chunk_wait(s->full[g.k_stages + stage], ph, s, a.status))) break;
                     if (chunk_look(a, va, vb, j)) {
                         uint4* p = reinterpret_cast<uint4*>(ring + (size_t)(g.k_stages + stage) * TILE);
                         const int hi = va.hi_max > vb.hi_max ? va.hi_max : vb.hi_max;
@@ -504,7 +502,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                 const int j = paged_tile_at(w.t, i) * KT;
                 if (!chunk_needs(a, v, j)) continue;
                 const bool masked = !chunk_whole(a, v, j);
-                if (!(ok = chunk_wait(s->s_full[x], s_ph, s, g.status))) break;
+                if (!(ok = chunk_wait(s->s_full[x], s_ph, s, a.status))) break;
                 s_ph ^= 1u;
                 tc::fence_after();
                 uint32_t f0[32], f1[32];
@@ -576,7 +574,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
             }
             if (!ok) break;
             if (begun) {
-                if (!(ok = chunk_wait(s->o_full[x], o_ph, s, g.status))) break;
+                if (!(ok = chunk_wait(s->o_full[x], o_ph, s, a.status))) break;
                 o_ph ^= 1u;
                 tc::fence_after();
                 if (!(ok = meet(l))) break;
@@ -761,12 +759,11 @@ static coreinfer_status chunk_dim(ChunkArgs& g, const DeviceInfo& di, cudaStream
     return g.a.c.D == 128 ? launch_chunk<T, 128>(g, di, st) : launch_chunk<T, 256>(g, di, st);
 }
 
-coreinfer_status paged_chunk(PagedAttnArgs& a, bool f16, unsigned* status, const DeviceInfo& di, cudaStream_t st)
+coreinfer_status paged_chunk(PagedAttnArgs& a, bool f16, const DeviceInfo& di, cudaStream_t st)
 {
     ChunkArgs g;
     g.a = a;
     g.negative = a.scale2 < 0.f;
-    g.status = status;
     return f16 ? chunk_dim<__half>(g, di, st) : chunk_dim<__nv_bfloat16>(g, di, st);
 }
 

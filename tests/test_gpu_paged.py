@@ -246,6 +246,21 @@ def test_attention_nine_to_sixteen_rows_of_128(new, length, H, share, page, wind
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("new", [1, 7, 12, 40])
+def test_attention_writes_its_status_word(new, dtype):
+    """Every form, in a workspace that holds anything, with nothing to do as well."""
+    require_gpu()
+    b = Batch([new, 0], [200, 30], 2, 1, 128, 16, dtype, seed=new)
+    q = b.rand(2)
+    out = torch.empty_like(q)
+    n = ci.coreinfer_paged_attention_workspace_bytes(b.handle(), 2, b.tokens)
+    for start in (b.start, torch.zeros_like(b.start)):
+        ws = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")
+        ci.coreinfer_paged_attention(b.handle(), start, q, 0.1, out, ws)
+        ci.coreinfer_workspace_status(ws)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 def test_attention_many_units_per_block(dtype):
     """Decoding sequences and long pieces of prompts in one call, more tiles than blocks: every block walks several units, most of
     their tiles without a mask, and no wait gives up."""
