@@ -23,14 +23,15 @@
 // a value get it added.
 // Every wait is bounded: one that gives up sets the status word, and all roles leave their loops.
 //
-// Measured from a graph, three sets of inputs: a prompt of 8192 tokens x 32 heads of 128 bf16 533 us (1030 TFLOP/s of what the mask leaves); 500
-// tokens x 40 heads, five a key head, over 16000 positions fp16 158 us (1020; under the profiler tensor pipe 53 %, exponentials 54 %, issue 39 %);
-// 2 x 1000 x 16 heads of 256 over 4000 163 us (505); seven sequences, windows of 1024, 32 heads of 64 fp16 156 us (340: 11 tiles a unit, four of them masked).
+// Measured from a graph, three sets of inputs: a prompt of 8192 tokens x 32 heads of 128 bf16 529 us (1040 TFLOP/s of what the mask leaves); 500
+// tokens x 40 heads, five a key head, over 16000 positions fp16 159 us (1015; under the profiler tensor pipe 53 %, exponentials 54 %, issue 39 %);
+// 2 x 1000 x 16 heads of 256 over 4000 162 us (510); seven sequences, windows of 1024, 32 heads of 64 fp16 150 us (354: 11 tiles a unit, four of them masked).
 // A tile of 128 positions for both row tiles takes 3400 to 3700 cycles at head_dim 128, where products alone would take 2050 (tcgen05.mma
 // M 128 N 128 K 16: 64 cycles each, also with A in tensor memory) and exponentials alone as many: scores, maximum, weights and product of a row tile follow
 // one another (170, 450, 1300 and 1500 cycles with the hand-overs), and two row tiles do not quite hide that; starting a unit costs about
 // 6000 cycles more.  Tried and slower or no better: halves of 64 positions with S doubled (N 64 products take 52 cycles for half the work),
-// one thread a row, P handed over in halves, products issued by two warps, part of the exponentials as polynomials, P apart from S at head_dim 64.
+// one thread a row, P handed over in halves, products issued by two warps, part of the exponentials as polynomials, P apart from S at head_dim 64,
+// units of at most 128 rows split by tiles between both pipelines.
 #include "paged_attention.cuh"
 #include "tc.cuh"
 
