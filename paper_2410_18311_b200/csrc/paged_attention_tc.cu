@@ -442,21 +442,21 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                     if (chunk_look(a, va, vb, j)) {
                         uint4* p = reinterpret_cast<uint4*>(ring + (size_t)(g.k_stages + stage) * TILE);
                         const int hi = va.hi_max > vb.hi_max ? va.hi_max : vb.hi_max;
-                        bool odd = false;
+                        bool odd = false, wrote = false;
 #pragma unroll 4
                         for (int c = t; c < (int)(TILE / 16); c += 64) {
                             uint4 x = p[c];
                             if (odd_pair<T>(x.x) || odd_pair<T>(x.y) || odd_pair<T>(x.z) || odd_pair<T>(x.w)) {
                                 x.x = without_odd<T>(x.x); x.y = without_odd<T>(x.y); x.z = without_odd<T>(x.z); x.w = without_odd<T>(x.w);
                                 p[c] = x;
+                                wrote = true;
                                 const int at_j = j + (c >> 3 & 127);     // what no row sees is not missed
                                 odd = odd || (at_j < hi && (at_j >= va.lo_min || at_j < a.sinks));
                             }
                         }
-                        if (odd) {
-                            *(volatile int*)&s->found[unit & 3] = unit + 1;
-                            fence_proxy_async();
-                        }
+                        // the product and the copy that takes the tile's place come behind these stores, whoever sees what was there
+                        if (wrote) fence_proxy_async();
+                        if (odd) *(volatile int*)&s->found[unit & 3] = unit + 1;
                     }
                     __syncwarp();
                     if (lane == 0) mbar_arrive(smem_u32(&s->looked[stage]));

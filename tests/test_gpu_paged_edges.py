@@ -1,0 +1,45 @@
+"""Paged attention and its pipeline where they can go wrong beside the ordinary calls: garbage in slots that nobody sees, positions behind
+the table, scales at the ends of their range, workspaces that grow, sequences that end while others decode."""
+import pytest
+import torch
+
+import paper_2410_18311_b200 as ci
+from helpers import require_gpu
+from paged_ref import Batch, check
+from test_gpu_paged import attend, check_attention, rand
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("garbage", [float("nan"), float("inf")])
+@pytest.mark.parametrize("D,window,sinks", [(64, 0, 0), (128, 0, 0), (128, 70, 3), (256, 0, 0)])
+def test_garbage_that_nobody_sees_never_reaches_a_product(D, window, sinks, garbage):
+    """Chunks whose last tiles hold garbage behind the sequences' ends, and in front of their windows, and none that a row sees: the
+    same bits as with zeros there, in each of many launches (the zeros are written beside the product's own reads, so an order
+    that is missing would show now and then)."""
+    require_gpu()
+    new, length = [150, 33, 90], [401, 33, 290]
+    b = Batch(new, length, 4, 1, D, 16, "bf16", seed=D + window)
+    q = b.rand(4)
+    unseen = [~torch.isfinite(p) for p in (b.k, b.v)]             # what no token holds
+    if window:
+        for s, n in enumerate(new):
+            for j in range(sinks, length[s] - n - window + 1):
+                unseen[1][b.table[s, j // 16].item(), :, j % 16] = True
+    assert all(u.any() for u in unseen)
+    outs = []
+    for value in (0.0, garbage):
+        for pool, u in zip((b.k, b.v), unseen):
+            pool[u] = value
+        outs.append(attend(b, q, D ** -0.5, window, sinks))
+    assert torch.isfinite(outs[0]).all()
+    n = ci.coreinfer_paged_attention_workspace_bytes(b.handle(), 4, b.tokens)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    many = torch.empty(50, *q.shape, dtype=q.dtype, device="cuda")
+    handle = b.handle()
+    for _ in range(20):
+        many.fill_(77.0)
+        for out in many:
+            ci.coreinfer_paged_attention(handle, b.start, q, D ** -0.5, out, ws, window, sinks)
+        assert torch.equal(many, outs[0].expand_as(many))
+    ci.coreinfer_workspace_status(ws)
