@@ -81,12 +81,10 @@ __global__ void __launch_bounds__(kFewThreads, kFewCtas<D, NT>) paged_few_kernel
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     uint8_t* ring = smem + warp * RING;
     const uint32_t ring_at = smem_u32(ring);
+    if (tid == 0) found[0] = 0;                      // the plan's barriers stand between this and who sets it
     wait_for_stream();
     const int total = paged_plan(a, at);
-    if (tid == 0) {
-        paged_first_words(a);
-        found[0] = 0;
-    }
+    if (tid == 0) paged_first_words(a);
     int unit = 0;
     const long long page_bytes = a.c.page_stride * 2, head_bytes = a.c.head_stride * 2, slot_bytes = a.c.token_stride * 2;
 

@@ -43,3 +43,28 @@ def test_garbage_that_nobody_sees_never_reaches_a_product(D, window, sinks, garb
             ci.coreinfer_paged_attention(handle, b.start, q, D ** -0.5, out, ws, window, sinks)
         assert torch.equal(many, outs[0].expand_as(many))
     ci.coreinfer_workspace_status(ws)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("new,length,share,D", [([3] * 4, [20, 9, 3, 31], 2, 128), ([2, 5], [64, 40], 1, 64), ([4, 3], [50, 7], 4, 128), ([2], [9], 3, 256)])
+def test_few_rows_find_infinities_in_their_first_unit(new, length, share, D, dtype):
+    """An infinity that the last tokens see and the first do not, in the first unit of every block: in each of many launches it reaches
+    those who see it."""
+    require_gpu()
+    b = Batch(new, length, 2, share, D, 16, dtype, seed=D + share)
+    for s, n in enumerate(new):
+        j = length[s] - 1
+        b.v[b.table[s, j // 16].item(), :, j % 16, 5] = float("inf")
+    q = b.rand(2 * share)
+    first = attend(b, q, D ** -0.5)
+    check_attention(b, q, first, D ** -0.5)
+    last = torch.tensor([b.starts[s + 1] - 1 for s in range(len(new))])
+    assert (~torch.isfinite(first[last][..., 5])).all() and torch.isfinite(first).sum() == first.numel() - len(new) * 2 * share
+    ws = torch.empty(ci.coreinfer_paged_attention_workspace_bytes(b.handle(), 2 * share, b.tokens), dtype=torch.uint8, device="cuda")
+    handle, many = b.handle(), torch.empty(500, *q.shape, dtype=q.dtype, device="cuda")
+    bits = first.view(torch.int16)
+    for _ in range(4):
+        many.fill_(77.0)
+        for out in many:
+            ci.coreinfer_paged_attention(handle, b.start, q, D ** -0.5, out, ws)
+        assert torch.equal(many.view(torch.int16), bits.expand_as(many))
