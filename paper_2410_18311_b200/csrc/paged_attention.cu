@@ -185,7 +185,7 @@ __global__ void __launch_bounds__(kManyThreads, kManyCtas<D>) paged_many_kernel(
             if (row >= rows) continue;
             if (head && tail) {
                 float* to_row = reinterpret_cast<float*>(a.out) + paged_row_offset(a, w.s, w.h, r0 + row, a.ld_out) + tx * 4;
-                const bool any = see[r].hi > 0;
+                const bool any = paged_sees_some(a, see[r]);
 #pragma unroll
                 for (int n = 0; n < NV; ++n)
                     *reinterpret_cast<float4*>(to_row + 64 * n) = any ? make_float4(o[r][n][0] / l[r], o[r][n][1] / l[r], o[r][n][2] / l[r], o[r][n][3] / l[r])
@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_c
             o[3] = fmaf(x[e].w, f, o[3]);
         }
     }
-    const bool sees = paged_row(a, s, global_row).hi > 0;
+    const bool sees = paged_sees_some(a, paged_row(a, s, global_row));
     T* to = reinterpret_cast<T*>(a.out) + paged_row_offset(a, s, p.h, global_row, a.ld_out) + c;
     T y[4];
 #pragma unroll

@@ -111,6 +111,8 @@ __device__ __forceinline__ PagedRow paged_row(const PagedAttnArgs& a, const Page
     r.lo = a.window ? p - a.window + 1 : 0;
     return r;
 }
+// Whether it sees anything: a token that lies a window or more behind the table sees the first tokens at most.
+__device__ __forceinline__ bool paged_sees_some(const PagedAttnArgs& a, const PagedRow& r) { return r.hi > 0 && (r.lo < r.hi || a.sinks > 0); }
 __device__ __forceinline__ bool paged_sees(const PagedAttnArgs& a, const PagedRow& r, int j) { return j < r.hi && (j >= r.lo || j < a.sinks); }
 
 // The list (the host has seen to it that it is shorter than 2^31).  `at` [B + 1] in shared memory; called by all threads of the CTA (a

@@ -322,7 +322,7 @@ __global__ void __launch_bounds__(kFewThreads, kFewCtas<D, NT>) paged_few_kernel
             if (restore)
                 for (int e = 0; e < 4; ++e) v[e] += paged_odd_sum<T>(a, w, low.hi, high.lo, from, to, r0 + r, d + e);
             if (head && tail) {
-                const bool sees = paged_row(a, w.s, r0 + r).hi > 0;
+                const bool sees = paged_sees_some(a, paged_row(a, w.s, r0 + r));
                 const float inv = 1.f / sum;
                 uint2 packed = make_uint2(pack2<T>(v[0] * inv, v[1] * inv), pack2<T>(v[2] * inv, v[3] * inv));
                 if (!sees) packed = make_uint2(0u, 0u);

@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(kRowsThreads, R == 1 ? 2 : 1) paged_rows_kerne
                 t.w = fmaf(part.w, f, t.w);
             }
             if (head && tail) {
-                const bool sees = paged_row(a, w.s, r0 + r).hi > 0;
+                const bool sees = paged_sees_some(a, paged_row(a, w.s, r0 + r));
                 const float4 y = sees ? make_float4(t.x / sum, t.y / sum, t.z / sum, t.w / sum) : make_float4(0.f, 0.f, 0.f, 0.f);
                 *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + paged_row_offset(a, w.s, w.h, r0 + r, a.ld_out) + d) = y;
             } else {

@@ -588,7 +588,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
             const bool restore = begun && *(volatile int*)&s->found[unit & 3] == unit + 1;
             const bool wide = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.ld_out * 2)) & 31) == 0;
             const size_t slot = (size_t)blockIdx.x * 2 + (head ? 1 : 0);
-            const float inv = see.hi > 0 ? 1.f / l : 0.f;
+            const bool sees = paged_sees_some(a, see);
+            const float inv = 1.f / l;
             constexpr int C = D / 2;                             // this warp's columns
             T* to_out = reinterpret_cast<T*>(a.out) + (mine ? paged_row_offset(a, w.s, w.h, row, a.ld_out) : 0) + h * C;
             float* to_part = a.part_o + slot * a.RU * D + (size_t)h * C * a.RU + (x * 128 + r) * 4;
@@ -626,7 +627,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                         uint32_t p[8];
 #pragma unroll
                         for (int e = 0; e < 8; ++e)
-                            p[e] = see.hi > 0 ? pack2<T>(__uint_as_float(o[c * 16 + 2 * e]) * inv, __uint_as_float(o[c * 16 + 2 * e + 1]) * inv) : 0u;
+                            p[e] = sees ? pack2<T>(__uint_as_float(o[c * 16 + 2 * e]) * inv, __uint_as_float(o[c * 16 + 2 * e + 1]) * inv) : 0u;
                         store32(to_out + c0 + c * 16, p, wide);
                     }
                 } else {

@@ -68,3 +68,27 @@ def test_few_rows_find_infinities_in_their_first_unit(new, length, share, D, dty
         for out in many:
             ci.coreinfer_paged_attention(handle, b.start, q, D ** -0.5, out, ws)
         assert torch.equal(many.view(torch.int16), bits.expand_as(many))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T,D,window,pages", [(1, 64, 30, 9), (3, 128, 16, 8), (8, 128, 3000, 230), (2, 256, 1, 3), (12, 128, 700, 60), (40, 64, 25, 9),
+                                              (300, 128, 1500, 130), (70, 256, 900, 64)])
+def test_tokens_a_window_behind_the_table_get_zeros(T, D, window, pages, dtype):
+    """Lengths so far behind the table that the last six tokens' windows (or the only one's) hold none of its positions; with first
+    tokens they see those."""
+    require_gpu()
+    b = Batch([T, T], [16 * (pages - 1), 5 + T], 2, 2, D, 16, dtype, seed=T)
+    assert b.table.shape[1] == pages or b.table.shape[1] * 16 > 5 + T
+    cap = b.table.shape[1] * 16
+    b.length_list[0] = cap + window + 5
+    b.length[0] = b.length_list[0]
+    for pool in (b.k, b.v):
+        pool.nan_to_num_(0, 0, 0)
+    q = b.rand(4)
+    for sinks in (0, 3):
+        out = attend(b, q, 0.1, window, sinks)
+        check_attention(b, q, out, 0.1, window, sinks)
+        if not sinks:
+            assert (out[max(0, T - 6):T] == 0).all() and (out[T:] != 0).any()
+            # token T - 7 sees the table's last position only, each one before it one more; the last 16 are a page that is none, zeros
+            assert T <= 22 or (out[:T - 22] != 0).any()
