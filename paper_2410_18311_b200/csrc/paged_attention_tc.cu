@@ -51,7 +51,7 @@ struct ChunkArgs {
     PagedAttnArgs a;
     int k_stages, v_stages; // rings of key and of value tiles
     int box;                // slots of a tensor copy
-    int negative;           // scale below 0: the queries' signs are turned
+    int sign;               // of the scale; below 0 the queries' signs are turned, at 0 they are multiplied by it
     int map_q;              // queries come by tensor copies
 };
 
@@ -185,6 +185,13 @@ __device__ __forceinline__ void mask32(uint32_t* f, uint32_t seen)
 #pragma unroll
     for (int e = 0; e < 32; ++e)
         if (!(seen >> e & 1u)) f[e] = 0xff800000u;
+}
+// Two 16-bit values times 0: NaN where they are not finite, as an infinity's or NaN's bits with those one place lower are.
+template <typename T>
+__device__ __forceinline__ uint32_t times_zero(uint32_t w)
+{
+    const uint32_t odd = w ^ without_odd<T>(w);
+    return odd | odd >> 1;
 }
 // Bits 0 .. n - 1.
 __device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : (n >= 32 ? 0xffffffffu : (1u << n) - 1u); }
@@ -422,11 +429,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
                     if (x + 1 < PIPES) asm volatile("cp.async.wait_group 1;" ::: "memory");
                     else asm volatile("cp.async.wait_group 0;" ::: "memory");
                     if (x * 128 >= rows) continue;
-                    if (g.negative) {                            // each lane turns what it has brought itself
+                    if (g.sign <= 0) {                           // each lane turns what it has brought itself
                         for (int r = t / CPR; r < 128; r += STEP) {
                             uint4* p = reinterpret_cast<uint4*>(qs + x * TILE + (c >> 3) * BLOCK + r * 128 + (((c & 7) ^ (r & 7)) << 4));
                             uint4 y = *p;
-                            y.x ^= 0x80008000u; y.y ^= 0x80008000u; y.z ^= 0x80008000u; y.w ^= 0x80008000u;
+                            if (g.sign < 0) { y.x ^= 0x80008000u; y.y ^= 0x80008000u; y.z ^= 0x80008000u; y.w ^= 0x80008000u; }
+                            else y = make_uint4(times_zero<T>(y.x), times_zero<T>(y.y), times_zero<T>(y.z), times_zero<T>(y.w));
                             *p = y;
                         }
                     }
@@ -472,7 +480,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) paged_chunk_kernel(const __g
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t t_s = tmem + lanes + x * 128 + h * 64, t_o = tmem + lanes + 256 + x * 128 + h * (D / 2);
         const int r = (warp & 3) * 32 + lane;                    // row of the tile
-        const float scale2 = fmaxf(fabsf(a.scale2), 1e-30f);     // a scale of 0 times -infinity would be NaN
+        const float scale2 = g.sign ? fabsf(a.scale2) : 1.f;     // above 0: times the -infinity of what is masked it stays that
         float* mine_s = &s->row[x][h][r];
         const volatile float* other_s = &s->row[x][h ^ 1][r];
         uint32_t s_ph = 0, o_ph = 0;
@@ -728,7 +736,7 @@ static coreinfer_status launch_chunk(ChunkArgs& g, const DeviceInfo& di, cudaStr
     coreinfer_status s = pool_map(&mk, g.a.c, g.a.c.pool[0], f16, g.box);
     if (s != COREINFER_OK || (s = pool_map(&mv, g.a.c, g.a.c.pool[1], f16, g.box)) != COREINFER_OK) return s;
     // a box is whole tokens: shares that divide 128, and queries as they are
-    g.map_q = !g.negative && g.a.share <= 128 && (g.a.share & (g.a.share - 1)) == 0 && g.a.ld_q < 1LL << 38;
+    g.map_q = g.sign > 0 && g.a.share <= 128 && (g.a.share & (g.a.share - 1)) == 0 && g.a.ld_q < 1LL << 38;
     if (g.map_q) {
         if ((s = query_map(&mq, g.a, f16)) != COREINFER_OK) return s;
     } else mq = mk;
@@ -765,7 +773,7 @@ coreinfer_status paged_chunk(PagedAttnArgs& a, bool f16, const DeviceInfo& di, c
 {
     ChunkArgs g;
     g.a = a;
-    g.negative = a.scale2 < 0.f;
+    g.sign = a.scale2 > 0.f ? 1 : (a.scale2 < 0.f ? -1 : 0);
     return f16 ? chunk_dim<__half>(g, di, st) : chunk_dim<__nv_bfloat16>(g, di, st);
 }
 

@@ -92,3 +92,27 @@ def test_tokens_a_window_behind_the_table_get_zeros(T, D, window, pages, dtype):
             assert (out[max(0, T - 6):T] == 0).all() and (out[T:] != 0).any()
             # token T - 7 sees the table's last position only, each one before it one more; the last 16 are a page that is none, zeros
             assert T <= 22 or (out[:T - 22] != 0).any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T,D", [(1, 64), (5, 128), (12, 128), (90, 128), (90, 64), (40, 256)])
+def test_a_scale_of_0_times_an_infinite_logit_is_nan(T, D, dtype):
+    """In every form alike, whatever the infinity's sign; rows that do not see the key have equal weights."""
+    require_gpu()
+    b = Batch([T, T], [200, 100 + T], 2, 2, D, 16, dtype, seed=T)
+    q = b.rand(4).abs().contiguous()
+    at = 200 - (T + 1) // 2                                      # seen by the first sequence's last (T + 1) // 2 tokens
+    for value in (float("inf"), float("-inf")):
+        b.k[b.table[0, at // 16].item(), 1, at % 16, 3] = value
+        for scale in (0.0, -0.0):
+            out = attend(b, q, scale)
+            bad = torch.isnan(out)
+            hit = slice(T - (T + 1) // 2, T)
+            assert bad[hit, 2:].all() and bad.sum() == bad[hit, 2:].numel()
+            b.k[b.table[0, at // 16].item(), 1, at % 16, 3] = 0.0
+            want = attend(b, q, scale)
+            b.k[b.table[0, at // 16].item(), 1, at % 16, 3] = value
+            assert torch.equal(out[~bad], want[~bad])
+    b.k[b.table[0, at // 16].item(), 1, at % 16, 3] = 0.0
+    for scale in (0.0, 1e-40, -1e-40, 3e-32):                    # the last two steps below what fp32 holds in full
+        check_attention(b, q, attend(b, q, scale), scale)
