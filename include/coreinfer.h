@@ -633,7 +633,7 @@ coreinfer_status coreinfer_paged_append(const coreinfer_paged_cache* cache, cons
 /* Attention of the new tokens over the cache (append first), from one token a sequence to whole prompts:
  *   out[r, head] = sum_j softmax_j( scale * q[r, head] . k_j ) v_j
  * where the token at position p sees the positions j <= p with  j > p - window  or  j < sinks  (window 0: all j <= p),
- * and `q_heads / kv_heads` consecutive query heads share a key head.  A token that sees no position gets zeros.
+ * and `q_heads / kv_heads` consecutive query heads share a key head.  A token that sees no position gets zeros.  scale * log2(e) is finite.
  * A NaN or infinity in a key or value makes the outputs that see it NaN or infinite, and no other.  Sums, maxima and the joins of partial
  * results are fp32 in a fixed order (the same call on the same arrays gives the same bits).  The softmax weights enter the product with the
  * values in fp32 (fp32 caches), as two 16-bit parts (16-bit caches and few query rows, tokens * q_heads / kv_heads / batch up to 8 at

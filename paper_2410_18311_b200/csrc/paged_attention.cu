@@ -376,7 +376,7 @@ coreinfer_status coreinfer_paged_attention(const coreinfer_paged_cache* cache, c
         CI_FAIL(COREINFER_ERR_INVALID_ARG, "q / out NULL, not 16-byte aligned, or strides too small or not multiples of 16 bytes");
     if (window < 0 || sinks < 0) CI_FAIL(COREINFER_ERR_INVALID_ARG, "window and sinks must be >= 0");
     if (window > 1 << 30 || sinks > 1 << 30) CI_FAIL(COREINFER_ERR_UNSUPPORTED, "window and sinks: at most 2^30");
-    if (!isfinite(scale)) CI_FAIL(COREINFER_ERR_INVALID_ARG, "scale must be finite");
+    if (!isfinite(scale * kLog2e)) CI_FAIL(COREINFER_ERR_INVALID_ARG, "scale, and scale * log2(e), must be finite");
     if (!workspace || !aligned16(workspace)) CI_FAIL(COREINFER_ERR_WORKSPACE, "workspace is NULL or misaligned");
     paged_set_share(a, q_heads / a.c.H);
     const PagedForm f = paged_form(dtype, a.c.D, a.c.B, a.share, tokens);
