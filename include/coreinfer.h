@@ -569,7 +569,8 @@ typedef struct {
  *   q, k       device, token t at t * ld_q (ld_k) elements, its heads [heads][head_dim] contiguous; k may be NULL with
  *              kv_heads 0, q with q_heads 0.  q_out, k_out likewise; each may be its input (in place), not overlap it otherwise
  * head_dim is 64, 128 or 256; pointers 16-byte aligned, strides * element size multiples of 16.
- * Errors: INVALID_ARG, UNSUPPORTED (dtype, head_dim, rot_dim, heads above 1024, tokens * heads above 2^29), CUDA. */
+ * Errors: INVALID_ARG, UNSUPPORTED (dtype, head_dim, rot_dim, q_heads above 4096, kv_heads above 1024, tokens * (q_heads + 2 kv_heads)
+ * above 2^29), CUDA. */
 coreinfer_status coreinfer_rope_apply(const coreinfer_rope* rope, const int32_t* positions, coreinfer_dtype dtype,
                                       int32_t tokens, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
                                       const void* q, int64_t ld_q, const void* k, int64_t ld_k,
@@ -623,7 +624,7 @@ typedef struct {
  *   positions  device int32 [tokens], the positions that tokens are turned by, or NULL: those of their slots
  *   q, q_out   device, rows as k's with q_heads heads; both or neither (q_heads 0); q_out may be q
  * All 16-byte aligned, strides * element size multiples of 16.  Two rows of one call must not be the same slot's.
- * Errors: INVALID_ARG, UNSUPPORTED (as above; tokens * heads above 2^29), CUDA. */
+ * Errors: INVALID_ARG, UNSUPPORTED (as above; q_heads above 4096, tokens * (q_heads + 2 kv_heads) above 2^29), CUDA. */
 coreinfer_status coreinfer_paged_append(const coreinfer_paged_cache* cache, const int32_t* start, int32_t tokens,
                                         const void* k, int64_t ld_k, const void* v, int64_t ld_v,
                                         const coreinfer_rope* rope, const int32_t* positions,
@@ -634,10 +635,12 @@ coreinfer_status coreinfer_paged_append(const coreinfer_paged_cache* cache, cons
  *   out[r, head] = sum_j softmax_j( scale * q[r, head] . k_j ) v_j
  * where the token at position p sees the positions j <= p with  j > p - window  or  j < sinks  (window 0: all j <= p),
  * and `q_heads / kv_heads` consecutive query heads share a key head.  A token that sees no position gets zeros.  scale * log2(e) is finite.
- * A NaN or infinity in a key or value makes the outputs that see it NaN or infinite, and no other.  Sums, maxima and the joins of partial
- * results are fp32 in a fixed order (the same call on the same arrays gives the same bits).  The softmax weights enter the product with the
- * values in fp32 (fp32 caches), as two 16-bit parts (16-bit caches and few query rows, tokens * q_heads / kv_heads / batch up to 8 at
- * head_dim 128 and 16 otherwise) or rounded to the cache's type (more rows).
+ * A NaN or infinity in a value makes the outputs that see it NaN or infinite, one in a key does what the formula says to the rows that see it (a
+ * logit of -infinity is a weight of 0), and neither reaches any other.  Sums, maxima and the joins of partial results are fp32 in a fixed
+ * order (the same call on the same arrays gives the same bits), and are divided at the end: values above 2^120 over the number of positions
+ * seen can overflow.  The softmax weights enter the product with the values in fp32 (fp32 caches), as two 16-bit parts (16-bit caches and up to 16
+ * query rows, tokens * q_heads / kv_heads / batch) or rounded to the cache's type (more rows), so that a row's last bits depend on
+ * the batch that it comes in.
  *   q, out     device, row r at r * ld_q (ld_out) elements, [q_heads][head_dim] contiguous, in the cache's type, 16-byte
  *              aligned, strides * element size multiples of 16
  *   workspace  device, 16-byte aligned, at least coreinfer_paged_attention_workspace_bytes() (0 on bad sizes), which covers
