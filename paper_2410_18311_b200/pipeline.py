@@ -227,27 +227,36 @@ class Pages:
 
 
 class PagedKVCache:
-    """Keys and values of one layer in pages, and attention over them."""
+    """Keys and values of one layer in pages, and attention over them: up to max_tokens new tokens a call, or the workspace grows (at most
+    a few times: the forms of the attention differ in it, not the lengths) and the ones before stay, as captured calls may use them."""
 
     def __init__(self, pages, q_heads, kv_heads, head_dim, dtype=torch.bfloat16, max_tokens=1):
         dev = pages.table.device
         self.pages, self.q_heads, self.head_dim = pages, q_heads, head_dim
         self.k, self.v = (torch.zeros(pages.n_pages, kv_heads, pages.page_size, head_dim, dtype=dtype, device=dev) for _ in range(2))
         self.cache = B.make_paged_cache(self.k, self.v, pages.table, pages.length)
-        self.ws = torch.empty(B.coreinfer_paged_attention_workspace_bytes(self.cache, q_heads, max_tokens), dtype=torch.uint8, device=dev)
+        self.ws, self._outgrown = self._workspace(max_tokens), []
+
+    def _workspace(self, tokens):
+        ws = torch.empty(B.coreinfer_paged_attention_workspace_bytes(self.cache, self.q_heads, tokens), dtype=torch.uint8, device=self.k.device)
+        ws[:16] = 0                                          # no wait of a call has given up yet
+        return ws
 
     def append(self, k, v, rotary=None, q=None, q_out=None, positions=None, stream=None):
         B.coreinfer_paged_append(self.cache, self.pages.start, k, v, None if rotary is None else rotary.rope, positions, q, q_out, stream)
 
     def attend(self, q, out, scale=None, window=0, sinks=0, stream=None):
-        need = B.coreinfer_paged_attention_workspace_bytes(self.cache, self.q_heads, q.shape[0])
-        if need > self.ws.numel():                           # more tokens than were announced
-            self.ws = torch.empty(need, dtype=torch.uint8, device=self.ws.device)
+        if B.coreinfer_paged_attention_workspace_bytes(self.cache, self.q_heads, q.shape[0]) > self.ws.numel():
+            # more tokens than were announced; calls captured before, or under way on another stream, still write the old one
+            self._outgrown.append(self.ws)
+            with torch.cuda.stream(stream):
+                self.ws = self._workspace(q.shape[0])
         B.coreinfer_paged_attention(self.cache, self.pages.start, q, self.head_dim ** -0.5 if scale is None else scale, out, self.ws, window, sinks, stream)
 
     def check(self, stream=None):
-        """Raises if a wait of the last attend() gave up (synchronises)."""
-        B.coreinfer_workspace_status(self.ws, stream)
+        """Raises if a wait of the last attend(), or of the last in a workspace since outgrown, gave up (synchronises)."""
+        for ws in self._outgrown + [self.ws]:
+            B.coreinfer_workspace_status(ws, stream)
 
 
 class CorePagedLayer:

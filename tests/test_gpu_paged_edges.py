@@ -5,8 +5,9 @@ import torch
 
 import paper_2410_18311_b200 as ci
 from helpers import require_gpu
-from paged_ref import Batch, check
-from test_gpu_paged import attend, check_attention, rand
+from paged_ref import Batch
+from paper_2410_18311_b200.pipeline import PagedKVCache, Pages
+from test_gpu_paged import attend, check_attention
 
 pytestmark = pytest.mark.gpu
 
@@ -116,3 +117,44 @@ def test_a_scale_of_0_times_an_infinite_logit_is_nan(T, D, dtype):
     b.k[b.table[0, at // 16].item(), 1, at % 16, 3] = 0.0
     for scale in (0.0, 1e-40, -1e-40, 3e-32):                    # the last two steps below what fp32 holds in full
         check_attention(b, q, attend(b, q, scale), scale)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_captured_step_outlives_a_longer_call(dtype):
+    """A step is captured, then the same cache attends to pieces longer than announced, on the current stream and on another: replays give
+    the step's bits and write nobody else's memory."""
+    require_gpu()
+    g = torch.Generator(device="cuda").manual_seed(2)
+    new = lambda *s: torch.randn(s, generator=g, device="cuda").to(dtype)  # noqa: E731
+    pages = Pages(2, 40, 16, 300)
+    one = PagedKVCache(pages, 8, 2, 128, dtype)
+    total = pages.add([250, 170])
+    one.append(new(total, 2, 128), new(total, 2, 128))
+    pages.decoding()
+    q, out = new(2, 8, 128), torch.empty(2, 8, 128, dtype=dtype, device="cuda")
+    one.attend(q, out)
+    want = out.clone()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        one.attend(q, out)
+    size = one.ws.numel()
+    for T, stream in ((12, None), (120, torch.cuda.Stream())):
+        pages.start.copy_(torch.tensor([0, T, 2 * T], dtype=torch.int32))
+        x, y, z = new(2 * T, 8, 128), torch.zeros(2 * T, 8, 128, dtype=dtype, device="cuda"), torch.zeros(2 * T, 8, 128, dtype=dtype, device="cuda")
+        torch.cuda.synchronize()
+        one.attend(x, y, stream=stream)
+        torch.cuda.synchronize()
+        other = PagedKVCache(pages, 8, 2, 128, dtype, max_tokens=2 * T)
+        other.k.copy_(one.k), other.v.copy_(one.v)
+        other.attend(x, z)
+        assert torch.equal(y, z)
+        assert one.ws.numel() > size
+        taken = [torch.full((size,), 85, dtype=torch.uint8, device="cuda") for _ in range(8)]
+        pages.decoding()
+        for _ in range(5):
+            out.zero_()
+            graph.replay()
+            assert torch.equal(out, want)
+        assert all((t == 85).all() for t in taken)
+    one.check()

@@ -14,3 +14,31 @@ def test_attention_refuses_scales_beyond_what_base_2_takes(lib):  # noqa: F811
         assert call(scale) == ci.ERR_INVALID_ARG
     for scale in (2.3e38, -2.3e38, 1e-45, 0.0):
         assert call(scale) == ci.ERR_WORKSPACE
+
+
+def test_a_workspace_that_grows_leaves_the_one_before_alone():
+    """Calls captured before hold its address: it stays allocated, and check() looks at it too."""
+    import weakref
+
+    from paper_2410_18311_b200.pipeline import PagedKVCache, Pages
+    pages = Pages(1, 8, 16, 64, device="cpu")
+    one = PagedKVCache(pages, 4, 2, 64)
+    before, size = weakref.ref(one.ws), one.ws.numel()
+    q = torch.zeros(500, 4, 64, dtype=torch.bfloat16)
+    for _ in range(2):
+        with pytest.raises(ci.CoreInferError):                   # host tensors: no call is made
+            one.attend(q, torch.zeros_like(q))
+        assert before() is not None and before().numel() == size
+        assert one.ws.numel() >= ci.coreinfer_paged_attention_workspace_bytes(one.cache, 4, 500) > size
+    grown = one.ws.data_ptr()
+    with pytest.raises(ci.CoreInferError):
+        one.attend(q[:1], torch.zeros_like(q[:1]))
+    assert one.ws.data_ptr() == grown
+    looked = []
+    status, ci.binding.coreinfer_workspace_status = ci.binding.coreinfer_workspace_status, lambda ws, stream=None: looked.append(ws.data_ptr())
+    try:
+        one.check()
+    finally:
+        ci.binding.coreinfer_workspace_status = status
+    assert set(looked) == {before().data_ptr(), grown}
+    assert (before()[:4] == 0).all() and (one.ws[:4] == 0).all()     # neither has been written by a call
