@@ -183,6 +183,8 @@ class Pages:
         self.table = torch.full((batch, self.max_pages), -1, dtype=torch.int32, device=device)
         self.length = torch.zeros(batch, dtype=torch.int32, device=device)
         self.start = torch.zeros(batch + 1, dtype=torch.int32, device=device)
+        # who takes part in steps: who holds tokens, or before the first add() everybody
+        self.runs, self._runs = [1] * batch, torch.ones(batch, dtype=torch.int32, device=device)
 
     def reserve(self, tokens):
         """Pages for that many tokens of every sequence (a number or one per sequence), so that a captured step may run on."""
@@ -202,28 +204,32 @@ class Pages:
         self.reserve([t + n for t, n in zip(self.tokens, new)])
         self.tokens = [t + n for t, n in zip(self.tokens, new)]
         self.length.copy_(torch.tensor(self.tokens, dtype=torch.int32))
+        self.runs = [int(t > 0) for t in self.tokens]
+        self._runs.copy_(torch.tensor(self.runs, dtype=torch.int32))
         self.start.copy_(torch.tensor([sum(new[:b]) for b in range(len(new) + 1)], dtype=torch.int32))
         return sum(new)
 
     def decoding(self):
-        """Packing for one token of every sequence."""
+        """Packing for one token of every sequence.  One that has ended or not begun keeps its row, which is at position -1: it is stored
+        nowhere and attends to nothing."""
         self.start.copy_(torch.arange(len(self.held) + 1, dtype=torch.int32))
 
     def one_more(self):
-        """Lengths for the next token of every sequence, on the device alone: what a captured step does in add()'s place, behind
-        decoding() and within what reserve() has given.  Replays are told to counted()."""
-        self.length += 1
+        """Lengths for the next token of every sequence that holds some, on the device alone: what a captured step does in add()'s
+        place, behind decoding() and within what reserve() has given.  Replays are told to counted()."""
+        self.length += self._runs
 
     def counted(self, steps):
         """That many steps by one_more() have run."""
-        self.tokens = [t + steps for t in self.tokens]
+        self.tokens = [t + steps * runs for t, runs in zip(self.tokens, self.runs)]
 
     def release(self, b):
-        """Sequence b has ended."""
+        """Sequence b has ended: its pages are free, and it sits out the steps until add() brings it new tokens."""
         self.free += reversed(self.held[b])
-        self.held[b], self.tokens[b] = [], 0
+        self.held[b], self.tokens[b], self.runs[b] = [], 0, 0
         self.table[b] = -1
         self.length[b] = 0
+        self._runs[b] = 0
 
 
 class PagedKVCache:

@@ -6,7 +6,7 @@ import torch
 import paper_2410_18311_b200 as ci
 from helpers import require_gpu
 from paged_ref import Batch
-from paper_2410_18311_b200.pipeline import PagedKVCache, Pages
+from paper_2410_18311_b200.pipeline import PagedKVCache, Pages, Rotary
 from test_gpu_paged import attend, check_attention
 
 pytestmark = pytest.mark.gpu
@@ -158,3 +158,57 @@ def test_a_captured_step_outlives_a_longer_call(dtype):
             assert torch.equal(out, want)
         assert all((t == 85).all() for t in taken)
     one.check()
+
+
+@pytest.mark.parametrize("n", [3, 60])
+def test_a_prompt_behind_one_that_ended_while_others_decoded(n):
+    """Captured steps with an ended sequence beside one that goes on: the ended one's row comes out 0 and stores nothing, and the next
+    prompt in its place gives a fresh cache's bits."""
+    require_gpu()
+    g = torch.Generator(device="cuda").manual_seed(n)
+    new = lambda *s: torch.randn(s, generator=g, device="cuda").half()  # noqa: E731
+    rotary = Rotary(64)
+
+    def made():
+        pages = Pages(2, 16, 16, 120)
+        return pages, PagedKVCache(pages, 4, 2, 64, torch.float16, max_tokens=128)
+
+    def bring(pages, cache, counts, seed):
+        g.manual_seed(seed)
+        total = pages.add(counts)
+        q, k, v = new(total, 4, 64), new(total, 2, 64), new(total, 2, 64)
+        out = torch.empty_like(q)
+        cache.append(k, v, rotary, q, q)
+        cache.attend(q, out)
+        return out
+
+    pages, cache = made()
+    bring(pages, cache, [30, 20], 1)
+    pages.reserve(48)
+    pages.decoding()
+    q, k, v, out = new(2, 4, 64), new(2, 2, 64), new(2, 2, 64), new(2, 4, 64)
+    x = torch.empty_like(q)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        pages.one_more()
+        cache.append(k, v, rotary, q, x)
+        cache.attend(x, out)
+    graph.replay()
+    pages.counted(1)
+    assert (out != 0).any(-1).all()
+    pages.release(0)
+    before = cache.k.clone()
+    for _ in range(5):
+        graph.replay()
+        assert (out[0] == 0).all() and (out[1] != 0).any(-1).all()
+    pages.counted(5)
+    assert pages.length.tolist() == pages.tokens == [0, 26]
+    assert (cache.k != before).any(1).any(-1).sum() == 5             # slots of the one that goes on
+    got = bring(pages, cache, [n, 0], 2)
+    assert torch.equal(got, bring(*made(), [n, 0], 2))
+    pages.decoding()
+    graph.replay()
+    pages.counted(1)
+    assert pages.length.tolist() == pages.tokens == [n + 1, 27] and (out != 0).any(-1).all()
+    cache.check()

@@ -42,3 +42,46 @@ def test_a_workspace_that_grows_leaves_the_one_before_alone():
         ci.binding.coreinfer_workspace_status = status
     assert set(looked) == {before().data_ptr(), grown}
     assert (before()[:4] == 0).all() and (one.ws[:4] == 0).all()     # neither has been written by a call
+
+
+def pages_of(batch=3, n_pages=12, size=16, most=64):
+    from paper_2410_18311_b200.pipeline import Pages
+    return Pages(batch, n_pages, size, most, device="cpu")
+
+
+def test_a_sequence_that_has_ended_sits_out_the_steps():
+    """Lengths on the device and counts on the host stay 0 from release() to the next add(), whose prompt then begins at position 0."""
+    pages = pages_of()
+    pages.add([20, 5, 9])
+    pages.reserve(40)
+    pages.decoding()
+    for _ in range(3):
+        pages.one_more()
+    pages.counted(3)
+    pages.release(1)
+    for _ in range(4):
+        pages.one_more()
+    pages.counted(4)
+    assert pages.length.tolist() == pages.tokens == [27, 0, 16]
+    assert pages.add([1, 7, 1]) == 9
+    assert pages.length.tolist() == pages.tokens == [28, 7, 17]
+    assert [len(h) for h in pages.held] == [3, 1, 3] and (pages.table[1, 1:] == -1).all()
+    pages.one_more()
+    pages.counted(1)
+    assert pages.length.tolist() == pages.tokens == [29, 8, 18]
+
+
+def test_a_sequence_not_begun_sits_out_and_a_batch_may_begin_with_steps():
+    pages = pages_of()
+    pages.add([20, 0, 9])
+    pages.reserve(40)
+    pages.one_more()
+    pages.counted(1)
+    assert pages.length.tolist() == pages.tokens == [21, 0, 10]
+    pages = pages_of()
+    pages.reserve(16)
+    pages.decoding()
+    for _ in range(16):
+        pages.one_more()
+    pages.counted(16)
+    assert pages.length.tolist() == pages.tokens == [16, 16, 16]
