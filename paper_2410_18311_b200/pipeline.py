@@ -3,6 +3,8 @@ weights and workspaces, allocated once with torch and reused.  No arithmetic her
 compaction and decoding all run in the library's kernels."""
 from __future__ import annotations
 
+import operator
+
 import torch
 
 from . import binding as B
@@ -186,9 +188,18 @@ class Pages:
         # who takes part in steps: who holds tokens, or before the first add() everybody
         self.runs, self._runs = [1] * batch, torch.ones(batch, dtype=torch.int32, device=device)
 
+    def _per_sequence(self, numbers):
+        try:
+            numbers = [operator.index(n) for n in numbers]
+        except TypeError:
+            numbers = []
+        if len(numbers) != len(self.held) or min(numbers) < 0:
+            raise B.CoreInferError(B.ERR_INVALID_ARG, "%d numbers >= 0 were expected, one per sequence" % len(self.held))
+        return numbers
+
     def reserve(self, tokens):
         """Pages for that many tokens of every sequence (a number or one per sequence), so that a captured step may run on."""
-        want = [tokens] * len(self.held) if isinstance(tokens, int) else list(tokens)
+        want = self._per_sequence([tokens] * len(self.held) if isinstance(tokens, int) else tokens)
         need = [max(0, -(-n // self.page_size) - len(h)) for n, h in zip(want, self.held)]
         if max(want) > self.max_pages * self.page_size or sum(need) > len(self.free):
             raise B.CoreInferError(B.ERR_INVALID_ARG, "%d pages of %d left, %d needed for %s tokens; a sequence takes %d tokens at most"
@@ -201,6 +212,7 @@ class Pages:
 
     def add(self, new):
         """Room for new[b] more tokens of each sequence, which the next calls bring: sets lengths and packing.  The total."""
+        new = self._per_sequence(new)
         self.reserve([t + n for t, n in zip(self.tokens, new)])
         self.tokens = [t + n for t, n in zip(self.tokens, new)]
         self.length.copy_(torch.tensor(self.tokens, dtype=torch.int32))
@@ -225,6 +237,8 @@ class Pages:
 
     def release(self, b):
         """Sequence b has ended: its pages are free, and it sits out the steps until add() brings it new tokens."""
+        if b not in range(len(self.held)) or not hasattr(b, "__index__"):
+            raise B.CoreInferError(B.ERR_INVALID_ARG, "sequence %s of %d" % (b, len(self.held)))
         self.free += reversed(self.held[b])
         self.held[b], self.tokens[b], self.runs[b] = [], 0, 0
         self.table[b] = -1

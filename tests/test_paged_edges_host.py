@@ -85,3 +85,28 @@ def test_a_sequence_not_begun_sits_out_and_a_batch_may_begin_with_steps():
         pages.one_more()
     pages.counted(16)
     assert pages.length.tolist() == pages.tokens == [16, 16, 16]
+
+
+@pytest.mark.parametrize("new", [[1], [1, 2], [1, 2, 3, 4], [3, -1, 1], [-20, 0, 0], 5, [1.5, 0, 0], []])
+def test_pages_refuse_numbers_that_are_not_one_per_sequence(new):
+    pages = pages_of()
+    pages.add([20, 0, 9])
+    state = lambda: ([list(h) for h in pages.held], list(pages.free), pages.tokens, pages.length.tolist(), pages.start.tolist(),  # noqa: E731
+                     pages.table.tolist(), pages.runs)
+    before = state()
+    with pytest.raises(ci.CoreInferError):
+        pages.add(new)
+    assert state() == before
+    if new != 5:                                                 # a number is one for all there
+        with pytest.raises(ci.CoreInferError):
+            pages.reserve(new)
+    assert state() == before
+
+
+@pytest.mark.parametrize("b", [-1, 3, 1.0])
+def test_pages_refuse_to_release_what_is_no_sequence(b):
+    pages = pages_of()
+    pages.add([20, 3, 9])
+    with pytest.raises(ci.CoreInferError):
+        pages.release(b)
+    assert pages.tokens == [20, 3, 9] and len(pages.free) == 12 - 4
