@@ -232,8 +232,15 @@ class Pages:
         self.length += self._runs
 
     def counted(self, steps):
-        """That many steps by one_more() have run."""
-        self.tokens = [t + steps * runs for t, runs in zip(self.tokens, self.runs)]
+        """That many steps by one_more() have run.  Raises where they went on behind the pages that reserve() had given: the tokens there
+        were not stored, and the sequence holds what its pages do."""
+        if steps < 0:
+            raise B.CoreInferError(B.ERR_INVALID_ARG, "%d steps" % steps)
+        ran = [t + steps * runs for t, runs in zip(self.tokens, self.runs)]
+        self.tokens = [min(t, len(h) * self.page_size) for t, h in zip(ran, self.held)]
+        if self.tokens != ran:
+            self.length.copy_(torch.tensor(self.tokens, dtype=torch.int32))
+            raise B.CoreInferError(B.ERR_INVALID_ARG, "steps to %s tokens ran behind the reserved pages: %s are held" % (ran, self.tokens))
 
     def release(self, b):
         """Sequence b has ended: its pages are free, and it sits out the steps until add() brings it new tokens."""

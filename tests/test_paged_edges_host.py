@@ -110,3 +110,24 @@ def test_pages_refuse_to_release_what_is_no_sequence(b):
     with pytest.raises(ci.CoreInferError):
         pages.release(b)
     assert pages.tokens == [20, 3, 9] and len(pages.free) == 12 - 4
+
+
+def test_steps_behind_the_reserved_pages_are_told():
+    """counted() raises where steps had no pages for their tokens; what is held stays usable."""
+    pages = pages_of()
+    pages.add([20, 16, 9])
+    pages.decoding()
+    pages.reserve([32, 20, 0])
+    for _ in range(16):
+        pages.one_more()
+    with pytest.raises(ci.CoreInferError):
+        pages.counted(16)
+    assert pages.tokens == pages.length.tolist() == [32, 32, 16]
+    pages.release(0)
+    pages.one_more()
+    with pytest.raises(ci.CoreInferError):
+        pages.counted(1)
+    assert pages.tokens == pages.length.tolist() == [0, 32, 16]
+    with pytest.raises(ci.CoreInferError):
+        pages.counted(-1)
+    assert pages.add([1, 2, 3]) == 6 and pages.tokens == pages.length.tolist() == [1, 34, 19]
