@@ -303,7 +303,7 @@ class CorePagedLayer:
         self.K = B.coreinfer_count(cfg.beta, cfg.d_ff)
         new = lambda *s, dtype=cfg.torch_dtype: torch.empty(s, dtype=dtype, device=dev)
         self.counts, self.seen = torch.zeros(cfg.d_ff, dtype=torch.int32, device=dev), 0
-        self._f, self.core_idx = new(cfg.d_ff, dtype=torch.int32), new(self.K, dtype=torch.int32)
+        self._f, self._top, self.core_idx = new(cfg.d_ff, dtype=torch.int32), new(self.K, dtype=torch.int32), new(self.K, dtype=torch.int32)
         self.up, self.down = new(self.K, cfg.d_model), new(self.K, cfg.d_model)
         self.gate = new(self.K, cfg.d_model) if cfg.gated else None
         self._ffn_ws = new(B.coreinfer_ffn_decode_workspace_bytes(B.MAX_BATCH, cfg.d_model, self.K), dtype=torch.uint8)
@@ -334,7 +334,7 @@ class CorePagedLayer:
         B.coreinfer_prefill_activations(x, self.kind, w_up, w_gate, None, act, self._act_ws)
         h += torch.nn.functional.linear(act, w_down)
         ws = torch.empty(B.coreinfer_select_workspace_bytes(*act.shape), dtype=torch.uint8, device=h.device)
-        B.coreinfer_select_core(act, cfg.alpha, cfg.beta, self.core_idx, self._f, ws)
+        B.coreinfer_select_core(act, cfg.alpha, cfg.beta, self._top, self._f, ws)        # the counts are what is wanted of it
         B.coreinfer_counts_add(self.counts, self._f)
         self.seen += h.shape[0]
 

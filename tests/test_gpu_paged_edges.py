@@ -6,7 +6,8 @@ import torch
 import paper_2410_18311_b200 as ci
 from helpers import require_gpu
 from paged_ref import Batch
-from paper_2410_18311_b200.pipeline import PagedKVCache, Pages, Rotary
+from paper_2410_18311_b200.pipeline import CorePagedLayer, PagedKVCache, Pages, Rotary
+from paper_2410_18311_b200.workloads import CONFIGS, layer_weights
 from test_gpu_paged import attend, check_attention
 
 pytestmark = pytest.mark.gpu
@@ -212,3 +213,31 @@ def test_a_prompt_behind_one_that_ended_while_others_decoded(n):
     pages.counted(1)
     assert pages.length.tolist() == pages.tokens == [n + 1, 27] and (out != 0).any(-1).all()
     cache.check()
+
+
+def layer_of(batch=2, gated=True, pieces=()):
+    """A small layer with rotary positions that has been brought pieces of that many tokens a sequence, and its generator."""
+    cfg = CONFIGS["tiny"].with_(gated=gated)
+    g = torch.Generator(device="cuda").manual_seed(batch)
+    new = lambda *s: (torch.randn(s, generator=g, device="cuda") * 0.06).to(cfg.torch_dtype)  # noqa: E731
+    pages = Pages(batch, 12 * batch, 16, 200)
+    layer = CorePagedLayer(cfg, pages, 8, 2, 64, (new(12 * 64, cfg.d_model), new(cfg.d_model, 8 * 64)) + layer_weights(cfg, 0, "cuda"), Rotary(64))
+    for counts in pieces:
+        layer.piece(torch.randn(pages.add(counts), cfg.d_model, generator=g, device="cuda"))
+    return layer, g
+
+
+def test_pieces_leave_the_deployed_set_alone():
+    """core_idx names the neurons whose weights up, gate and down hold, until the next fix_core()."""
+    require_gpu()
+    layer, g = layer_of(pieces=([30, 20],))
+    layer.fix_core()
+    deployed = layer.core_idx.clone()
+    w_up, w_gate, w_down = layer.w_ffn
+    layer.pages.release(0)
+    for counts in ([50, 0], [1, 40]):
+        layer.piece(torch.randn(layer.pages.add(counts), layer.cfg.d_model, generator=g, device="cuda") * 3 + 1)
+        assert torch.equal(layer.core_idx, deployed)
+        assert torch.equal(layer.up, w_up[deployed.long()]) and torch.equal(layer.gate, w_gate[deployed.long()])
+    layer.fix_core()
+    assert not torch.equal(layer.core_idx, deployed) and torch.equal(layer.up, w_up[layer.core_idx.long()])
