@@ -306,6 +306,7 @@ class CorePagedLayer:
         self._f, self._top, self.core_idx = new(cfg.d_ff, dtype=torch.int32), new(self.K, dtype=torch.int32), new(self.K, dtype=torch.int32)
         self.up, self.down = new(self.K, cfg.d_model), new(self.K, cfg.d_model)
         self.gate = new(self.K, cfg.d_model) if cfg.gated else None
+        self.deployed = False                                # whether up, gate and down hold the neurons of core_idx
         self._ffn_ws = new(B.coreinfer_ffn_decode_workspace_bytes(B.MAX_BATCH, cfg.d_model, self.K), dtype=torch.uint8)
         self._act_ws = new(B.coreinfer_prefill_activations_workspace_bytes(), dtype=torch.uint8)
 
@@ -340,14 +341,18 @@ class CorePagedLayer:
 
     def fix_core(self):
         """Deploys the top beta of the neurons by the counts of the pieces so far, which start anew."""
+        if not self.seen:
+            raise B.CoreInferError(B.ERR_INVALID_ARG, "no piece has been counted since the last core set")
         w_up, w_gate, w_down = self.w_ffn
         B.coreinfer_top_by_count(self.counts, self.seen, self.cfg.beta, self.core_idx)
         B.coreinfer_compact(w_up, w_gate, w_down, None, self.core_idx, self.K, self.up, self.gate, self.down, None)
         self.counts.zero_()
-        self.seen = 0
+        self.seen, self.deployed = 0, True
 
     def step(self, h):
         """h [batch, d] fp32, one new token per sequence: updated in place."""
+        if not self.deployed:
+            raise B.CoreInferError(B.ERR_INVALID_ARG, "a step decodes over the core set, which fix_core() chooses")
         self._attention(h)
         y = torch.empty_like(h)
         B.coreinfer_ffn_decode(self._norm(h), self.kind, self.up, self.gate, self.down, None, None, y, self._ffn_ws)

@@ -241,3 +241,24 @@ def test_pieces_leave_the_deployed_set_alone():
         assert torch.equal(layer.up, w_up[deployed.long()]) and torch.equal(layer.gate, w_gate[deployed.long()])
     layer.fix_core()
     assert not torch.equal(layer.core_idx, deployed) and torch.equal(layer.up, w_up[layer.core_idx.long()])
+
+
+def test_a_layer_without_a_core_set_takes_no_step():
+    """Before the first fix_core() there are no weights to decode with; fix_core() needs counts."""
+    require_gpu()
+    layer, g = layer_of()
+    with pytest.raises(ci.CoreInferError):
+        layer.fix_core()
+    layer.piece(torch.randn(layer.pages.add([5, 4]), layer.cfg.d_model, generator=g, device="cuda"))
+    h = torch.randn(layer.pages.add([1, 1]), layer.cfg.d_model, generator=g, device="cuda")
+    before, k = h.clone(), layer.cache.k.clone()
+    with pytest.raises(ci.CoreInferError):
+        layer.step(h)
+    assert torch.equal(h, before) and torch.equal(layer.cache.k, k)
+    layer.fix_core()
+    deployed = layer.core_idx.clone()
+    layer.step(h)
+    assert torch.isfinite(h).all() and not torch.equal(h, before)
+    with pytest.raises(ci.CoreInferError):
+        layer.fix_core()
+    assert torch.equal(layer.core_idx, deployed)
