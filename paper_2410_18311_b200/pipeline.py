@@ -185,6 +185,7 @@ class Pages:
         self.table = torch.full((batch, self.max_pages), -1, dtype=torch.int32, device=device)
         self.length = torch.zeros(batch, dtype=torch.int32, device=device)
         self.start = torch.zeros(batch + 1, dtype=torch.int32, device=device)
+        self.total = 0                                       # rows of the packing
         # who takes part in steps: who holds tokens, or before the first add() everybody
         self.runs, self._runs = [1] * batch, torch.ones(batch, dtype=torch.int32, device=device)
 
@@ -219,12 +220,14 @@ class Pages:
         self.runs = [int(t > 0) for t in self.tokens]
         self._runs.copy_(torch.tensor(self.runs, dtype=torch.int32))
         self.start.copy_(torch.tensor([sum(new[:b]) for b in range(len(new) + 1)], dtype=torch.int32))
-        return sum(new)
+        self.total = sum(new)
+        return self.total
 
     def decoding(self):
         """Packing for one token of every sequence.  One that has ended or not begun keeps its row, which is at position -1: it is stored
         nowhere and attends to nothing."""
         self.start.copy_(torch.arange(len(self.held) + 1, dtype=torch.int32))
+        self.total = len(self.held)
 
     def one_more(self):
         """Lengths for the next token of every sequence that holds some, on the device alone: what a captured step does in add()'s
@@ -313,7 +316,10 @@ class CorePagedLayer:
     def _norm(self, h):
         return torch.nn.functional.layer_norm(h, (self.cfg.d_model,)).to(self.cfg.torch_dtype)
 
-    def _attention(self, h):
+    def _attention(self, h, most=None):
+        if h.shape != (self.pages.total, self.cfg.d_model) or h.shape[0] > (most or h.shape[0]):
+            raise B.CoreInferError(B.ERR_INVALID_ARG, "rows [%d, %d] were announced%s, got %s"
+                                   % (self.pages.total, self.cfg.d_model, ", up to %d are taken" % most if most else "", tuple(h.shape)))
         Hq, H, D = self.heads
         q, k, v = torch.nn.functional.linear(self._norm(h), self.w_qkv).split((Hq * D, H * D, H * D), dim=-1)
         q, k, v = q.unflatten(-1, (Hq, D)), k.unflatten(-1, (H, D)), v.unflatten(-1, (H, D))
@@ -353,7 +359,7 @@ class CorePagedLayer:
         """h [batch, d] fp32, one new token per sequence: updated in place."""
         if not self.deployed:
             raise B.CoreInferError(B.ERR_INVALID_ARG, "a step decodes over the core set, which fix_core() chooses")
-        self._attention(h)
+        self._attention(h, B.MAX_BATCH)
         y = torch.empty_like(h)
         B.coreinfer_ffn_decode(self._norm(h), self.kind, self.up, self.gate, self.down, None, None, y, self._ffn_ws)
         h += y

@@ -262,3 +262,21 @@ def test_a_layer_without_a_core_set_takes_no_step():
     with pytest.raises(ci.CoreInferError):
         layer.fix_core()
     assert torch.equal(layer.core_idx, deployed)
+
+
+@pytest.mark.parametrize("batch,counts,rows", [(2, [5, 4], 8), (2, [5, 4], 10), (2, [1, 1], 3), (2, [1, 0], 2), (9, [1] * 9, 9)])
+def test_a_layer_refuses_rows_that_were_not_announced(batch, counts, rows):
+    """Nothing is stored, updated or counted; more than 8 sequences have no step, but pieces."""
+    require_gpu()
+    layer, g = layer_of(batch, pieces=([3] * batch,))
+    layer.fix_core()
+    layer.pages.add(counts)
+    h = torch.randn(rows, layer.cfg.d_model, generator=g, device="cuda")
+    before, k, seen = h.clone(), layer.cache.k.clone(), layer.seen
+    for call in (layer.step,) if rows == sum(counts) else (layer.step, layer.piece):
+        with pytest.raises(ci.CoreInferError):
+            call(h)
+        assert torch.equal(h, before) and torch.equal(layer.cache.k, k) and layer.seen == seen and not layer.counts.any()
+    h = torch.randn(sum(counts), layer.cfg.d_model, generator=g, device="cuda")
+    layer.piece(h)
+    assert torch.isfinite(h).all() and layer.seen == sum(counts)
