@@ -18,10 +18,11 @@ namespace coreinfer {
 // weights are written and read by one warp.  All operands come from shared memory in 16-byte reads: at RT = 4 twelve
 // wavefronts for 64 FMA instructions.  Keys, values and queries are brought by cp.async; at head_dim 128 and 256
 // the weights take the keys' place, so that two blocks fit an SM at 128.  Measured: 2 x 500 tokens x 12 heads of 64 over up to 1000 positions 77 us,
-// 1000 tokens x 16 heads over 2000 positions 220 us at head_dim 64, 392 at 128, 832 at 256 (at 128: FMA pipe 54 %,
-// shared memory's wavefronts 69 %, issue 70 %).
+// 1000 tokens x 16 heads over 2000 positions 225 us at head_dim 64, 403 at 128, 838 at 256 (as one chain of sums a unit 224, 399, 826; at 128: FMA pipe
+// 54 %, shared memory's wavefronts 69 %, issue 70 %); 16 x 8 heads x 8 rows x 7600 of 128 481 us.
 constexpr int kManyThreads = 256;
 constexpr int kManyTile = 64;
+constexpr int kManyKeep = 16;                                                        // tiles whose sums are one chain of additions
 template <int D> constexpr int kManyCtas = D == 256 ? 1 : 2;                         // per SM
 template <int D> constexpr bool kManyApart = D == 64;                                // weights have a place of their own
 template <int D, int RT> constexpr int kManyFloats = 16 * RT * (D + 4) + kManyTile * (D + 4) + kManyTile * D + (kManyApart<D> ? 16 * RT * (kManyTile + 4) : 0);
@@ -78,8 +79,41 @@ __global__ void __launch_bounds__(kManyThreads, kManyCtas<D>) paged_many_kernel(
             many_copy(qs + r * DP + d, r < rows ? q + paged_row_offset(a, w.s, w.h, r0 + r, a.ld_q) + d : q, r < rows);
         }
         if (from < to) fetch(from);
+        const bool head = from == 0, tail = to == w.t.count;
+        const size_t slot = (size_t)blockIdx.x * 2 + (head ? 1 : 0);
         PagedRow see[RT];
         float m[RT], l[RT], o[RT][NV][4];
+        // Sums of kManyKeep tiles are added to those before, which wait in the unit's slot of the workspace (the first time there is nothing
+        // yet): one chain over all positions would lose bits (8 rows x 10000 positions of 64, 16 sequences x 12 heads: error against
+        // 64 bits 1.5e-6, so 0.9e-6; values that are all alike x 40000 of 256: off by 1.4e-4, so 1e-5).
+        auto add_kept = [&](bool any) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+#pragma unroll
+                for (int d = 1; d < 16; d <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], d);
+                if (!any) continue;
+                const int row = ty * RT + r;
+                const float2 kept = a.part_ml[slot * RU + row];
+                const float by = kept.x == -INFINITY ? 0.f : exp2f(kept.x - m[r]);
+                l[r] = fmaf(kept.y, by, l[r]);
+#pragma unroll
+                for (int n = 0; n < NV; ++n) {
+                    const float4 x = *reinterpret_cast<const float4*>(a.part_o + slot * RU * D + ((tx * 4 + 64 * n) * RU + row * 4));
+                    o[r][n][0] = fmaf(x.x, by, o[r][n][0]);
+                    o[r][n][1] = fmaf(x.y, by, o[r][n][1]);
+                    o[r][n][2] = fmaf(x.z, by, o[r][n][2]);
+                    o[r][n][3] = fmaf(x.w, by, o[r][n][3]);
+                }
+            }
+            __syncwarp();                            // a row's exponent and sum have been read by all that share it
+        };
+        auto keep = [&](int r) {
+            const int row = ty * RT + r;
+#pragma unroll
+            for (int n = 0; n < NV; ++n)
+                *reinterpret_cast<float4*>(a.part_o + slot * RU * D + ((tx * 4 + 64 * n) * RU + row * 4)) = make_float4(o[r][n][0], o[r][n][1], o[r][n][2], o[r][n][3]);
+            if (tx == 0) a.part_ml[slot * RU + row] = make_float2(m[r], l[r]);
+        };
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             const int row = ty * RT + r;
@@ -173,14 +207,24 @@ __global__ void __launch_bounds__(kManyThreads, kManyCtas<D>) paged_many_kernel(
             else add(std::false_type());
             __syncthreads();
             if (i + 1 < to) fetch(i + 1);
+            if ((i - from) % kManyKeep == kManyKeep - 1 && i + 1 < to) {
+                add_kept(i - from >= kManyKeep);
+#pragma unroll
+                for (int r = 0; r < RT; ++r) {
+                    keep(r);
+                    l[r] = 0.f;
+#pragma unroll
+                    for (int n = 0; n < NV; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[r][n][e] = 0.f;
+                }
+                __syncwarp();
+            }
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
-        const bool head = from == 0, tail = to == w.t.count;
-        const size_t slot = (size_t)blockIdx.x * 2 + (head ? 1 : 0);
+        add_kept(to - from > kManyKeep);
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
-#pragma unroll
-            for (int d = 1; d < 16; d <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], d);
             const int row = ty * RT + r;
             if (row >= rows) continue;
             if (head && tail) {
@@ -190,12 +234,7 @@ __global__ void __launch_bounds__(kManyThreads, kManyCtas<D>) paged_many_kernel(
                 for (int n = 0; n < NV; ++n)
                     *reinterpret_cast<float4*>(to_row + 64 * n) = any ? make_float4(o[r][n][0] / l[r], o[r][n][1] / l[r], o[r][n][2] / l[r], o[r][n][3] / l[r])
                                                                       : make_float4(0.f, 0.f, 0.f, 0.f);
-            } else {
-#pragma unroll
-                for (int n = 0; n < NV; ++n)
-                    *reinterpret_cast<float4*>(a.part_o + slot * RU * D + ((tx * 4 + 64 * n) * RU + row * 4)) = make_float4(o[r][n][0], o[r][n][1], o[r][n][2], o[r][n][3]);
-                if (tx == 0) a.part_ml[slot * RU + row] = make_float2(m[r], l[r]);
-            }
+            } else keep(r);
         }
         if (head && !tail && tid == 0) {
             PagedPiece p;

@@ -280,3 +280,25 @@ def test_a_layer_refuses_rows_that_were_not_announced(batch, counts, rows):
     h = torch.randn(sum(counts), layer.cfg.d_model, generator=g, device="cuda")
     layer.piece(h)
     assert torch.isfinite(h).all() and layer.seen == sum(counts)
+
+
+@pytest.mark.parametrize("B,H,share,D,T,L", [(16, 12, 1, 64, 1, 400000), (16, 10, 4, 128, 1, 400000), (40, 8, 1, 256, 1, 150000), (40, 8, 8, 64, 1, 60000),
+                                             (38, 8, 1, 128, 12, 60000), (20, 8, 8, 256, 1, 60000), (1, 8, 1, 64, 2400, 60000), (1, 5, 1, 256, 2000, 40000)])
+def test_sums_over_many_fp32_positions_are_no_single_chain(B, H, share, D, T, L):
+    """Equal weights and equal values, whose sum a chain of additions always rounds to the same side: units that one block sums alone.
+
+    Weights are 1 and their sum a whole number below 2^24, so both are exact.  An addition or fused product is off by half a spacing,
+    2^-24 of the sum: at most 1024 of them in a chain, one for every 1024 positions, 300 in the join, and the division."""
+    require_gpu()
+    pool = torch.empty(1, H, 16, D, device="cuda")
+    pool.copy_((torch.arange(D, device="cuda") % 37 + 1) / -97)
+    table = torch.zeros(B, -(-L // 16), dtype=torch.int32, device="cuda")
+    length = torch.full((B,), L, dtype=torch.int32, device="cuda")
+    start = (torch.arange(B + 1, device="cuda") * T).to(torch.int32)
+    cache = ci.make_paged_cache(pool, pool, table, length)
+    q = torch.zeros(B * T, H * share, D, device="cuda")
+    out = torch.empty_like(q)
+    ws = torch.empty(ci.coreinfer_paged_attention_workspace_bytes(cache, H * share, B * T), dtype=torch.uint8, device="cuda")
+    ci.coreinfer_paged_attention(cache, start, q, 0.1, out, ws)
+    want = pool[0, 0, 0].double()
+    assert ((out.double() - want).abs() <= (1024 + L / 1024 + 302) * 2.0 ** -24 * want.abs()).all()
