@@ -302,3 +302,31 @@ def test_sums_over_many_fp32_positions_are_no_single_chain(B, H, share, D, T, L)
     ci.coreinfer_paged_attention(cache, start, q, 0.1, out, ws)
     want = pool[0, 0, 0].double()
     assert ((out.double() - want).abs() <= (1024 + L / 1024 + 302) * 2.0 ** -24 * want.abs()).all()
+
+
+@pytest.mark.parametrize("dtype,T,share", [(torch.float32, 1, 2), (torch.float32, 9, 1), (torch.bfloat16, 1, 4), (torch.bfloat16, 80, 2), (torch.float16, 90, 3)])
+def test_pools_and_rows_beyond_32_bits(dtype, T, share):
+    """Pages behind 2^32 elements of the pools, and rows of queries and outputs that lie 2^22 elements apart, behind 2^32 of them where many
+    are new: the bits of a small cache with rows side by side."""
+    require_gpu()
+    H, D, page, length = 8, 128, 64, [700, 333]
+    g = torch.Generator(device="cuda").manual_seed(T)
+    new = lambda *s: torch.randn(s, generator=g, device="cuda").to(dtype)  # noqa: E731
+    k, v, q = new(1033, H, D), new(1033, H, D), new(2 * T, H * share, D)
+    whole = torch.tensor([0, 700, 1033], dtype=torch.int32, device="cuda")
+    lengths = torch.tensor(length, dtype=torch.int32, device="cuda")
+    pages = torch.randperm(22, generator=torch.Generator().manual_seed(T)).view(2, 11).to(torch.int32)
+    outs = []
+    for n_pages, step in ((22, H * share * D), (70000, 1 << 22)):
+        tokens = 2 * T if n_pages == 22 or T < 10 else 1100
+        start = torch.tensor([tokens - 2 * T, tokens - T, tokens], dtype=torch.int32, device="cuda")
+        table = (pages + n_pages - 22).cuda()
+        pools = [torch.empty(n_pages, H, page, D, dtype=dtype, device="cuda") for _ in range(2)]
+        cache = ci.make_paged_cache(*pools, table, lengths)
+        x, out = (torch.empty(tokens * step, dtype=dtype, device="cuda").as_strided((tokens, H * share, D), (step, D, 1)) for _ in range(2))
+        x[-2 * T:] = q
+        ws = torch.empty(ci.coreinfer_paged_attention_workspace_bytes(cache, H * share, tokens), dtype=torch.uint8, device="cuda")
+        ci.coreinfer_paged_append(cache, whole, k, v)
+        ci.coreinfer_paged_attention(cache, start, x, 0.1, out, ws)
+        outs.append(out[-2 * T:].contiguous())
+    assert torch.isfinite(outs[0]).all() and (outs[0] != 0).any(-1).all() and torch.equal(*outs)
