@@ -539,8 +539,8 @@ coreinfer_status coreinfer_kv4_evict(const coreinfer_kv4_cache* src, const corei
  *   LINEAR   f_i / factor
  *   NTK      PLAIN with base * factor^(rot_dim / (rot_dim - 2))
  *   YARN     f_i (1 - r_i + r_i / factor), r_i rising linearly from 0 to 1 between the pair that turns `high` times within
- *            original_context positions (rounded down) and the one that turns `low` times (rounded up); magnitude
- *            0.1 ln(factor) + 1.  Customary: low 1, high 32
+ *            original_context positions (rounded down, 0 at least) and the one that turns `low` times (rounded up, rot_dim - 1
+ *            at most); magnitude 0.1 ln(factor) + 1.  Customary: low 1, high 32
  *   BANDS    f_i s_i + f_i / factor (1 - s_i), s_i = clamp((original_context f_i / (2 pi) - low) / (high - low), 0, 1): short
  *            wavelengths stay, long ones are stretched.  Customary: low 1, high 4
  * magnitude is 1 but for YARN.  rot_dim is a multiple of 16, 16 to 256.

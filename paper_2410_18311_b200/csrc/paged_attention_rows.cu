@@ -8,8 +8,9 @@
 // own maximum, sum and output, asks for the next piece's keys as soon as it has used the last ones and for its values after
 // that, and no warp waits for another before the end of a unit.
 //
-// Measured from a graph, three sets of inputs: 8 x 12 heads x up to 4001 positions of 64 41 us (3800 GB/s), 12 heads x 77 6.8 us (launch, list,
-// page, keys, join: one latency after the other).
+// Measured from a graph, three sets of inputs: 8 x 12 heads x up to 4001 positions of 64 41 us (3800 GB/s), 16 x 8 heads x up to 7600 of 128 135 us, four
+// rows of them 404 us (as far from the bytes as one CTA an SM and four sums over the lanes a slot leave it), 12 heads x 77 7 us (launch,
+// list, page, keys, join: one latency after the other).  One row spills 120 to 152 bytes a thread at the 128 registers that two CTAs an SM have.
 #include "paged_attention.cuh"
 
 namespace coreinfer {

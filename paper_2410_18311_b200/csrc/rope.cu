@@ -8,7 +8,8 @@
 //
 // Measured from a graph, three sets of inputs: 8191 tokens x 40 heads of 128 fp16, norms 35.7 us, 4700 GB/s; 16000 x 64 bf16 92 us, 5670; 6000 x 40
 // fp32, norms 45.8 us, 5370; 5000 tokens x 48 heads bf16 into pages 36 us, 3400 (a round of warps and a bit).
-// Two loads ahead and 32 warps an SM: four loads and 24 warps 39.5, 89, 67, 35; eight at once and none ahead 47.6, 108, 46.7, 41.
+// Two loads ahead and 32 warps an SM: four loads and 24 warps 39.5, 89, 67, 35; eight at once and none ahead 47.6, 108, 46.7, 41.  At 64 registers
+// ptxas spills 16 to 68 bytes a thread (fp32, at 80: up to 12).
 //
 // What bounds it: bytes (each value read and written once), and a launch's latency where the tokens are few.  A warp takes a token, or a
 // part of its heads where the tokens are few, so that the cosines and sines are formed once per token (two pairs a lane, through
