@@ -592,7 +592,7 @@ coreinfer_status coreinfer_rope_apply(const coreinfer_rope* rope, const int32_t*
  *
  * Whatever those arrays hold, no access leaves the buffers: `start` counts as clamped to [0, tokens]; a token with a position
  * below 0, behind the table's max_pages * page_size positions or in a page outside [0, n_pages) is not stored; slots of
- * such a page read as zeros; tokens see the positions of the table only.
+ * such a page read as zeros; tokens see the positions of the table only.  Arrays that change while a call runs make its outputs undefined, no more.
  *
  * head_dim is 64, 128 or 256, batch at most COREINFER_PAGED_MAX_BATCH, kv_heads at most 1024, max_pages * page_size
  * below 2^30, n_pages below 2^27 (otherwise UNSUPPORTED).  Pools are 16-byte aligned, strides * element size multiples

@@ -319,7 +319,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_c
 template <int D, int RT>
 static coreinfer_status launch_many(const PagedAttnArgs& a, const DeviceInfo& di, cudaStream_t st)
 {
-    const size_t smem = (size_t)kManyFloats<D, RT> * 4 + (size_t)(a.c.B + 1) * 4;
+    const size_t smem = (size_t)kManyFloats<D, RT> * 4 + paged_list_bytes(a.c.B);
     const coreinfer_status s = allow_smem<paged_many_kernel<D, RT>>(di, 0);
     if (s != COREINFER_OK) return s;
     CI_CUDA(launch_overlapped(paged_many_kernel<D, RT>, dim3(a.n_ctas), dim3(kManyThreads), smem, st, a));

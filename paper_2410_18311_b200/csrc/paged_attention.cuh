@@ -5,7 +5,9 @@
 // KT positions that some of its rows see (the first tokens' tiles, then those from the window's start on).  The tiles of all units,
 // with an entry cost for each unit's start, form one list that is cut into equal pieces, one per CTA, whatever the lengths
 // are: a CTA meets at most two units that it shares with others, its first and its last.  Lengths are known on the device only,
-// so every CTA works the list out for itself (a lane per sequence or, where they are many, per row tile, and a scan; about 1.5 us of latency).
+// so every CTA works the list out for itself (a lane per sequence or, where they are many, per row tile, and a scan; about 1.5 us of latency).  It reads
+// packing and lengths once and keeps them in shared memory: all its warps go by the same numbers, and come to their ends by them, also where
+// somebody changes the arrays under a call.
 #pragma once
 
 #include "paged.cuh"
@@ -69,7 +71,14 @@ constexpr int kPagedRowsMost = 4;
 static inline int paged_rows_tile(int head_dim) { return 8192 / head_dim; }
 coreinfer_status paged_rows_f32(const PagedAttnArgs& a, const DeviceInfo& di, cudaStream_t st);
 
+// Shared memory of the list: its starts [B + 1], then what the sequences are [B].
+static inline size_t paged_list_bytes(int B) { return (size_t)(B + 1) * 4 + (size_t)B * 12; }
+
 #ifdef __CUDACC__
+
+static_assert(sizeof(PagedSeq) == 12, "three numbers");
+__device__ __forceinline__ PagedSeq* paged_kept(const PagedAttnArgs& a, int* at) { return reinterpret_cast<PagedSeq*>(at + a.c.B + 1); }
+__device__ __forceinline__ const PagedSeq& paged_kept(const PagedAttnArgs& a, const int* at, int b) { return reinterpret_cast<const PagedSeq*>(at + a.c.B + 1)[b]; }
 
 __device__ __forceinline__ int by_share(const PagedAttnArgs& a, int n) { return a.share_mul ? (int)(__umulhi((unsigned)n, a.share_mul) >> a.share_shift) : n; }
 
@@ -115,8 +124,8 @@ __device__ __forceinline__ PagedRow paged_row(const PagedAttnArgs& a, const Page
 __device__ __forceinline__ bool paged_sees_some(const PagedAttnArgs& a, const PagedRow& r) { return r.hi > 0 && (r.lo < r.hi || a.sinks > 0); }
 __device__ __forceinline__ bool paged_sees(const PagedAttnArgs& a, const PagedRow& r, int j) { return j < r.hi && (j >= r.lo || j < a.sinks); }
 
-// The list (the host has seen to it that it is shorter than 2^31).  `at` [B + 1] in shared memory; called by all threads of the CTA (a
-// multiple of 32).
+// The list (the host has seen to it that it is shorter than 2^31).  `at`: paged_list_bytes() of shared memory; called by all threads of the
+// CTA (a multiple of 32).
 __device__ __forceinline__ int paged_plan(const PagedAttnArgs& a, int* at)
 {
     const int lane = threadIdx.x & 31;
@@ -124,7 +133,7 @@ __device__ __forceinline__ int paged_plan(const PagedAttnArgs& a, int* at)
         // a lane per sequence, and the warp together for those of many row tiles
         const int b = b0 + lane;
         PagedSeq s = {0, 0, 0};
-        if (b < a.c.B) s = paged_seq(a.c, b);
+        if (b < a.c.B) paged_kept(a, at)[b] = s = paged_seq(a.c, b);
         const int tiles = paged_row_tiles(a, s);
         int w = 0;
         if (tiles <= 2)
@@ -204,7 +213,7 @@ struct PagedWalk {
             else hi = mid;
         }
         b = lo;
-        s = paged_seq(a.c, b);
+        s = paged_kept(a, at, b);
         const unsigned per_head = (unsigned)(at[b + 1] - at[b]) / (unsigned)a.c.H;
         h = (int)((unsigned)(x - at[b]) / per_head);
         base = at[b] + h * per_head;
@@ -254,7 +263,7 @@ struct PagedWalk {
             if (++h == a.c.H) {
                 h = 0;
                 do ++b; while (at[b + 1] == at[b]);
-                s = paged_seq(a.c, b);
+                s = paged_kept(a, at, b);
             }
         }
         t = paged_tiles(a, s, tile);

@@ -348,7 +348,7 @@ __global__ void __launch_bounds__(kFewThreads, kFewCtas<D, NT>) paged_few_kernel
 template <typename T, int D, int NT>
 static coreinfer_status launch_few(const PagedAttnArgs& a, const DeviceInfo& di, cudaStream_t st)
 {
-    const size_t smem = (size_t)kFewWarps * kFewStages<D, NT> * kFewStageBytes<D> + kFewWarps * 8 * NT * sizeof(float2) + 8 + (size_t)(a.c.B + 1) * 4;
+    const size_t smem = (size_t)kFewWarps * kFewStages<D, NT> * kFewStageBytes<D> + kFewWarps * 8 * NT * sizeof(float2) + 8 + paged_list_bytes(a.c.B);
     const coreinfer_status s = allow_smem<paged_few_kernel<T, D, NT>>(di, 0);
     if (s != COREINFER_OK) return s;
     CI_CUDA(launch_overlapped(paged_few_kernel<T, D, NT>, dim3(a.n_ctas), dim3(kFewThreads), smem, st, a));

@@ -230,7 +230,7 @@ __global__ void __launch_bounds__(kRowsThreads, R == 1 ? 2 : 1) paged_rows_kerne
 template <int D, int R>
 static coreinfer_status launch_rows(const PagedAttnArgs& a, const DeviceInfo& di, cudaStream_t st)
 {
-    const size_t smem = (size_t)kRowsWarps * R * (D * sizeof(float) + sizeof(float2)) + (size_t)(a.c.B + 1) * 4;
+    const size_t smem = (size_t)kRowsWarps * R * (D * sizeof(float) + sizeof(float2)) + paged_list_bytes(a.c.B);
     const coreinfer_status s = allow_smem<paged_rows_kernel<D, R>>(di, 0);
     if (s != COREINFER_OK) return s;
     CI_CUDA(launch_overlapped(paged_rows_kernel<D, R>, dim3(a.n_ctas), dim3(kRowsThreads), smem, st, a));

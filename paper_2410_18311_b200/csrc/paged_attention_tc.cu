@@ -746,7 +746,7 @@ static coreinfer_status launch_chunk(ChunkArgs& g, const DeviceInfo& di, cudaStr
         if ((s = query_map(&mq, g.a, f16)) != COREINFER_OK) return s;
     } else mq = mk;
     constexpr size_t TILE = D / 64 * 128 * 128;
-    const size_t fixed = kChunkPipes<D> * TILE + sizeof(ChunkBars) + (size_t)(g.a.c.B + 1) * 4;
+    const size_t fixed = kChunkPipes<D> * TILE + sizeof(ChunkBars) + paged_list_bytes(g.a.c.B);
     size_t stages = (smem_room(di, 0) - fixed) / TILE;
     if (stages > kChunkMaxStages) stages = kChunkMaxStages;
     g.k_stages = (int)stages / 2;

@@ -330,3 +330,41 @@ def test_pools_and_rows_beyond_32_bits(dtype, T, share):
         ci.coreinfer_paged_attention(cache, start, x, 0.1, out, ws)
         outs.append(out[-2 * T:].contiguous())
     assert torch.isfinite(outs[0]).all() and (outs[0] != 0).any(-1).all() and torch.equal(*outs)
+
+
+@pytest.mark.parametrize("dtype,T", [(torch.float32, 1), (torch.float32, 30), (torch.bfloat16, 1), (torch.bfloat16, 6), (torch.float16, 200)])
+def test_lengths_that_change_under_a_call(dtype, T):
+    """Another stream changes lengths, packing and pages while calls run: what comes out then is nobody's business, but every call ends,
+    no wait gives up, no other memory is written, and the next call is as any other."""
+    require_gpu()
+    B, H, share, D, page = 5, 4, 2, 128, 16
+    g = torch.Generator(device="cuda").manual_seed(T)
+    new = lambda *s: torch.randn(s, generator=g, device="cuda").to(dtype)  # noqa: E731
+    k, v = new(300, H, page, D), new(300, H, page, D)
+    table = torch.randperm(300, generator=torch.Generator().manual_seed(1))[:B * 60].view(B, 60).to(torch.int32).cuda()
+    length = torch.tensor([900, 40 + T, 700, T, 333 + T], dtype=torch.int32, device="cuda")
+    start = (torch.arange(B + 1, device="cuda") * T).to(torch.int32)
+    cache = ci.make_paged_cache(k, v, table, length)
+    held = torch.full((B * T + 2, H * share, D), 77.0, dtype=dtype, device="cuda")
+    q, out = new(B * T, H * share, D), held[1:-1]
+    n = ci.coreinfer_paged_attention_workspace_bytes(cache, H * share, B * T)
+    ws = torch.full((n + 64,), 85, dtype=torch.uint8, device="cuda")
+    ci.coreinfer_paged_attention(cache, start, q, 0.1, out, ws[:n])
+    want, was = out.clone(), [t.clone() for t in (length, start, table)]
+    others = [(length * 0 + x, start * y, table.flip(0) - z) for x, y, z in ((950, 1, 0), (T, 0, 1), (0, 2, 400), (1 << 30, 1, 0), (500, -1, 0))]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for x in others:
+            with torch.cuda.stream(side):
+                for _ in range(4):
+                    for t, y in zip((length, start, table), x):
+                        t.copy_(y)
+                    for t, y in zip((length, start, table), was):
+                        t.copy_(y)
+            for window in (0, 100):
+                ci.coreinfer_paged_attention(cache, start, q, 0.1, out, ws[:n], window, 3)
+    torch.cuda.synchronize()
+    ci.coreinfer_workspace_status(ws)
+    ci.coreinfer_paged_attention(cache, start, q, 0.1, out, ws[:n])
+    assert torch.equal(out, want) and (held[0] == 77).all() and (held[-1] == 77).all() and (ws[n:] == 85).all()
