@@ -265,7 +265,9 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_c
     constexpr int ROWS = kJoinRows<D>;
     wait_for_stream();
     const PagedPiece p = a.pieces[blockIdx.x];
+    // the second line: what another call has left there, where two overlap in one workspace against the rules
     if (p.last < 0) return;
+    if (p.last >= a.n_ctas || (unsigned)p.b >= (unsigned)a.c.B || (unsigned)p.h >= (unsigned)a.c.H || p.tile >> (30 - a.ru_shift)) return;
     const PagedSeq s = paged_seq(a.c, p.b);
     const int row = blockIdx.y * ROWS + threadIdx.x % ROWS, c = threadIdx.x / ROWS * 4;
     const int global_row = p.tile * a.RU + row;

@@ -368,3 +368,35 @@ def test_lengths_that_change_under_a_call(dtype, T):
     ci.coreinfer_workspace_status(ws)
     ci.coreinfer_paged_attention(cache, start, q, 0.1, out, ws[:n])
     assert torch.equal(out, want) and (held[0] == 77).all() and (held[-1] == 77).all() and (ws[n:] == 85).all()
+
+
+@pytest.mark.parametrize("dtype,T", [(torch.float32, 1), (torch.bfloat16, 2), (torch.float16, 90)])
+def test_calls_that_overlap_in_one_workspace_stay_in_their_buffers(dtype, T):
+    """Against the rules: calls of other batches, heads and lengths on two streams with one workspace.  Outputs may be anything, rows beside
+    them are as they were, and each call alone is right again."""
+    require_gpu()
+    g = torch.Generator(device="cuda").manual_seed(T)
+    new = lambda *s: torch.randn(s, generator=g, device="cuda").to(dtype)  # noqa: E731
+    calls = []
+    for B, H, L in ((1, 2, 3000), (40, 8, 900)):
+        pool = new(64, H, 16, 64), new(64, H, 16, 64)
+        table = torch.randint(0, 64, (B, 190), generator=torch.Generator().manual_seed(B), dtype=torch.int32).cuda()
+        length, start = torch.full((B,), L, dtype=torch.int32, device="cuda"), (torch.arange(B + 1, device="cuda") * T).to(torch.int32)
+        held = torch.full((B * T + 2, 2 * H, 64), 77.0, dtype=dtype, device="cuda")
+        calls.append((ci.make_paged_cache(*pool, table, length), start, new(B * T, 2 * H, 64), held, pool, table, length))
+    ws = torch.empty(max(ci.coreinfer_paged_attention_workspace_bytes(c[0], c[2].shape[1], c[2].shape[0]) for c in calls), dtype=torch.uint8, device="cuda")
+    run = lambda c, stream=None: ci.coreinfer_paged_attention(c[0], c[1], c[2], 0.1, c[3][1:-1], ws, stream=stream)  # noqa: E731
+    wants = []
+    for c in calls:
+        run(c)
+        wants.append(c[3].clone())
+    streams = [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    for _ in range(200):
+        for c, s in zip(calls, streams):
+            run(c, s)
+    torch.cuda.synchronize()
+    for c, want in zip(calls, wants):
+        assert (c[3][0] == 77).all() and (c[3][-1] == 77).all()
+        run(c)
+        assert torch.equal(c[3], want)
