@@ -400,3 +400,13 @@ def test_calls_that_overlap_in_one_workspace_stay_in_their_buffers(dtype, T):
         assert (c[3][0] == 77).all() and (c[3][-1] == 77).all()
         run(c)
         assert torch.equal(c[3], want)
+
+
+@pytest.mark.parametrize("dtype,D,share,most", [("f32", 64, 1, 1), ("f32", 256, 6, 9), ("bf16", 128, 1, 1), ("f16", 128, 16, 1), ("bf16", 256, 6, 9)])
+def test_the_largest_batch(dtype, D, share, most):
+    """1024 sequences, whose list takes the most of the shared memory, in every form; some of them without new tokens."""
+    require_gpu()
+    new = [(5 * i) % (most + 1) if i % 3 else most for i in range(1024)]
+    b = Batch(new, [n + (7 * i) % 12 for i, n in enumerate(new)], 1, share, D, 16, dtype, seed=share, front=1, pad=1)
+    q = b.rand(share)
+    check_attention(b, q, attend(b, q, D ** -0.5), D ** -0.5)
