@@ -30,7 +30,7 @@
 // 8192 tokens x 32 heads of 128 bf16 542 us (1015 TFLOP/s of what the mask leaves) and 632 (870, 1575 MHz); 500 tokens x 40 heads, five a key head, over
 // 16000 positions fp16 168 (960) and 187 us (865, 1657 MHz; under the profiler tensor pipe 53 %, exponentials 54 %, issue 39 %); 2 x 1000 x 16
 // heads of 256 over 4000 170 us (485); seven sequences, windows of 1024, 32 heads of 64 fp16 150 us (354: 11 tiles a unit, four of them masked).
-// ptxas spills 80 to 112 bytes a thread at 96 registers (which setmaxnreg then divides).
+// ptxas spills 84 to 116 bytes a thread at 96 registers (which setmaxnreg then divides).
 // A tile of 128 positions for both row tiles takes 3400 to 3700 cycles at head_dim 128, where products alone would take 2050 (tcgen05.mma
 // M 128 N 128 K 16: 64 cycles each, also with A in tensor memory) and exponentials alone as many: scores, maximum, weights and product of a row tile follow
 // one another (170, 450, 1300 and 1500 cycles with the hand-overs), and two row tiles do not quite hide that; starting a unit costs about
